@@ -690,6 +690,197 @@ int32_t dsp_breadth_update(dsp_breadth_state *state, const dsp_breadth_params *p
                            int32_t B, int32_t L,
                            int32_t *next_K /* host, out, nullable */, int32_t *next_W /* host, out, nullable */);
 
+/* -------------------------------------------------------------------------
+ * The model pass around the step  (Alg. 1 lines 4 and 9: the drafter's and the
+ * target's forward over the block; the paper runs both with a KV cache on and
+ * leaves them to the model code): a paged cache whose lengths move by the
+ * accepted length every step, and attention over it in the three forms that a
+ * step needs: causal (one token, a chain of drafted tokens, a prompt), full
+ * (the drafter's block, seen from both sides), and a token tree of
+ * dsp_beam_tree.  Keys and values are held in 4 bits.
+ *
+ * Requests are ragged: request b brings new_len[b] tokens, packed one request
+ * after the other into T rows; cu_new [B+1] are the prefix sums.  All lengths
+ * stay on the device, so the calls can be recorded in a CUDA graph with T, B
+ * and max_new as upper bounds.
+ */
+#define DSP_ROW_NO_BLOCKS    64u   /* dsp_cache_plan: the pool has too few free blocks for this row */
+#define DSP_ROW_TABLE_FULL  128u   /* dsp_cache_plan: the row needs more than max_blocks blocks */
+#define DSP_ROW_PLAN_FULL   256u   /* dsp_cache_plan: the row's tokens do not fit into T */
+#define DSP_ROW_BAD_LENGTH  512u   /* dsp_cache_plan: a negative length, seq_len + new_len beyond 2^31 - 1, a block
+                                      count outside 0..max_blocks, or more new tokens than the tree has nodes (+ 1) */
+#define DSP_MAX_PLAN_ROWS 8192     /* largest B of dsp_cache_plan */
+
+/* Which tokens a query sees (dsp_attn_kv4); j counts the request's new tokens, i is the query's own. */
+enum dsp_attn_mask {
+    DSP_MASK_CAUSAL = 0,  /* all cached tokens before the block, and new tokens j <= i */
+    DSP_MASK_FULL = 1,    /* all of the request's tokens */
+    DSP_MASK_BITS = 2     /* all cached tokens before the block, and the new tokens whose bit is set */
+};
+
+/* Block tables, slots and positions of a step's tokens from the requests' lengths.
+ *
+ * Request b holds seq_len[b] tokens in the cache, in block_count_in[b] blocks of
+ * page_size tokens (block_table[b, 0 .. count-1]), and brings new_len[b] more.
+ * It needs n = ceil((seq_len + new_len) / page_size) blocks: what it lacks is
+ * taken from the free list, what it has too many (the last step drafted more
+ * than was accepted) is given back.  The free list is a ring of n_blocks block
+ * numbers: ring_pos_in = {head, tail}, tail - head blocks are free, taken from
+ * ring[head % n_blocks] on, given back at ring[tail % n_blocks] on; both in the
+ * order of the requests, then of the table.
+ * A row that cannot be served keeps its blocks, brings no token (its kv_len is
+ * its seq_len) and says why in row_status: DSP_ROW_BAD_LENGTH (kv_len is then
+ * max(seq_len, 0), block_count clipped to 0..max_blocks), DSP_ROW_TABLE_FULL;
+ * DSP_ROW_PLAN_FULL for rows with new tokens from the first on whose tokens,
+ * counted over the rows without those two flags, pass T; DSP_ROW_NO_BLOCKS for
+ * rows that lack blocks from the first on whose lack, summed over the rows
+ * without the other flags, passes the free blocks (blocks given back in this
+ * call are free from the next call on).
+ *
+ * Inputs : seq_len, new_len, block_count_in int32 [B]; ring_pos_in int64 [2].
+ *          node_parent, node_depth int32 [B,N] (both or neither): the new tokens
+ *          are the last kept token and then a tree's nodes in dsp_beam_tree's
+ *          numbering (new_len = 1 + n_nodes).  A parent that is not an earlier
+ *          node counts as the root.
+ * In/out : block_table int32 [B, max_blocks] (stride table_stride): only the
+ *          entries of newly taken blocks are written; entries beyond the count
+ *          mean nothing.  free_ring int32 [n_blocks].
+ *          A call writes the same values when it is repeated on the same inputs
+ *          (block_count and ring_pos are outputs of their own), so a step that
+ *          failed later on can be planned again.
+ * Outputs: block_count int32 [B], ring_pos int64 [2] (must not overlap the
+ *          inputs), cu_new int32 [B+1], kv_len int32 [B] (= seq_len + new tokens),
+ *          row_status uint32 [B]; and for the T token rows (row cu_new[b] + i is
+ *          the i-th new token of request b, rows from cu_new[B] on are padding):
+ *          slot int64 [T]      block * page_size + place in the block; padding -1
+ *          position int32 [T]  seq_len + i, in a tree seq_len + 1 + depth (the
+ *                              root: seq_len); padding -1
+ *          token_row int32 [T] b; padding -1 (nullable)
+ *          mask uint32 [T, mask_words] (with a tree only): bit j % 32 of word
+ *                              j / 32 is set if the token sees the request's
+ *                              j-th new token: itself and its path to the root
+ *                              (token 0).  Padding rows are 0.
+ * Errors : INVALID_ARG (null pointer, B < 0, T < 0, page_size < 1, n_blocks < 1,
+ *          max_blocks < 1, table_stride < max_blocks, only one of the tree's two
+ *          arrays, N < 1 or mask_words * 32 < N + 1 with a tree),
+ *          UNSUPPORTED (B > DSP_MAX_PLAN_ROWS, N + 1 > DSP_MAX_L), CUDA.
+ *          B == 0 with T == 0 is a no-op returning DSP_OK.
+ */
+int32_t dsp_cache_plan(const int32_t *seq_len, const int32_t *new_len, const int32_t *block_count_in,
+                       const int64_t *ring_pos_in, int32_t B, int32_t T, int32_t page_size,
+                       int32_t n_blocks, int32_t max_blocks,
+                       int32_t *block_table, int64_t table_stride, int32_t *free_ring,
+                       const int32_t *node_parent, const int32_t *node_depth, int32_t N,
+                       int32_t *block_count, int64_t *ring_pos, int32_t *cu_new, int32_t *kv_len,
+                       int64_t *slot, int32_t *position, int32_t *token_row,
+                       uint32_t *mask, int32_t mask_words, uint32_t *row_status, dsp_stream_t stream);
+
+/* Norm of every query and key head and the rotation by position, in one pass.
+ *
+ *   y = x * r * w,  r = 1 / sqrt(mean_d x_d^2 + eps)         (per token and head)
+ *   rotation of the first `rot` channels by the angles of the token's position:
+ *   (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s) for the pairs (a, b) =
+ *   (i, i + rot/2), or (2i, 2i+1) if interleaved, i < rot/2; c = cos_sin[pos, i],
+ *   s = cos_sin[pos, rot/2 + i].  fp32 throughout, one rounding at the end.  The
+ *   sum of squares is formed as a tree of neighbouring channels and no product is
+ *   fused with a sum, so equal rows give equal bits whatever the call's shape.
+ *
+ * q [T,Hq,D], k [T,Hkv,D] (dtype; strides in elements, channels contiguous);
+ * q_weight / k_weight [D] (dtype; null: that side is not normed); positions
+ * int32 [T] and cos_sin float [max_pos, rot] (null: no rotation, rot is then not
+ * read).  A token with a negative position is padding: its output rows are 0; one
+ * with a position >= max_pos gets NaN (positions may be null without a rotation).
+ * q_out [T,Hq,D], k_out [T,Hkv,D]: contiguous, 16-byte aligned, not overlapping
+ * the inputs.
+ * Rows that start on 16 bytes are read with 128-bit loads, others by element.
+ * Errors : INVALID_ARG (null pointer, T < 0, Hq < 1, Hkv < 1, strides below the
+ *          extent they skip, eps < 0 or not finite, max_pos < 1, misaligned
+ *          output), UNSUPPORTED (dtype, D not 64 / 128 / 256, rot not a multiple
+ *          of 16 in 16..D, more than 2^24 tokens, 4096 heads or 2^30 heads of all
+ *          tokens together), CUDA.
+ */
+int32_t dsp_qk_norm_rope(const void *q, const void *k, int32_t dtype, int32_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                         int64_t q_stride_t, int64_t q_stride_h, int64_t k_stride_t, int64_t k_stride_h,
+                         const void *q_weight, const void *k_weight, float eps,
+                         const int32_t *positions, const float *cos_sin, int32_t max_pos, int32_t rot,
+                         int32_t interleaved, void *q_out, void *k_out, dsp_stream_t stream);
+
+/* A cache with keys and values in 4 bits.
+ *
+ * A token's key (or value) of one head is D codes 0..15 with one scale s and one
+ * offset z in bf16; it stands for code * s + z.  For x in fp32 (x: the key as
+ * dsp_qk_norm_rope returns it, rounded to dtype; the value as it comes):
+ *   z = the largest bf16 <= min x,  s = the smallest bf16 >= fl((max x - z) / 15)
+ *   (0 if below 2^-126),  code = (x - z) / s rounded to the nearest, ties to even,
+ *   at most 15 (0 if s = 0).  A head with a NaN or an infinity, or whose s or z is
+ *   not finite, is held as s = z = NaN: every channel of it reads as NaN.
+ * cache: uint8 [n_blocks, Hkv, page_size * (D + 8)], 16-byte aligned, contiguous.
+ * A page is cut into runs of 16 tokens of 16 * (D + 8) bytes: 8*D bytes of key
+ * codes, 8*D bytes of value codes, then (key s, key z, value s, value z) of each
+ * token.  Eight consecutive channels 0..7 are one 32-bit word with the channels
+ * 0 2 4 6 1 3 5 7 from its lowest four bits up.  Of the words of a run, those that
+ * one lane of a warp multiplies lie together (lane = 4 r + c):
+ *   keys,   D = 128: lane's 16 bytes = words 4c..4c+3 of token r; token r + 8 is
+ *           512 bytes on.  D = 64: words 2c, 2c+1 of token r, then of token r + 8.
+ *   values, D = 128: words 2r, 2r+1 of token 2c, then of 2c + 1; tokens 2c + 8 and
+ *           2c + 9 are 512 bytes on.  D = 64: word r of tokens 2c, 2c+1, 2c+8, 2c+9.
+ *
+ * dsp_kv4_append: q, k, v as in dsp_qk_norm_rope (v is neither normed nor rotated);
+ * q_out like there; token t's key and value enter slot[t] (int64; block * page_size
+ * + place).  A slot outside 0 .. n_blocks * page_size - 1 or a negative position
+ * stores nothing.  Of two tokens with the same slot, either may win.  (After a tree
+ * was verified, the accepted nodes' rows are appended again at the slots of their
+ * final places, with slot -1 for the others.)  q and q_out null: keys and values only.
+ * dsp_kv4_read: the values that the cache holds for the tokens in slot [T], in
+ * `dtype`, [T,Hkv,D] contiguous, 16-byte aligned; an outside slot reads as 0.
+ * Errors : as dsp_qk_norm_rope; INVALID_ARG (n_blocks < 1, page_size not a multiple
+ *          of 16, misaligned cache), UNSUPPORTED (D not 64 / 128).
+ */
+int32_t dsp_kv4_append(const void *q, const void *k, const void *v, int32_t dtype,
+                       int32_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                       int64_t q_stride_t, int64_t q_stride_h, int64_t k_stride_t, int64_t k_stride_h,
+                       int64_t v_stride_t, int64_t v_stride_h,
+                       const void *q_weight, const void *k_weight, float eps,
+                       const int32_t *positions, const float *cos_sin, int32_t max_pos, int32_t rot,
+                       int32_t interleaved, const int64_t *slot, void *cache, int32_t n_blocks, int32_t page_size,
+                       void *q_out, dsp_stream_t stream);
+int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int32_t Hkv, int32_t D,
+                     const int64_t *slot, int32_t T, int32_t dtype, void *k_out, void *v_out, dsp_stream_t stream);
+
+/* Attention over the 4-bit cache.
+ *
+ *   out[t,h] = sum_u p_u v_u / sum_u p_u,  p_u = exp(scale * q[t,h] . k_u)
+ * over the tokens u that query t sees, k_u and v_u of head h / (Hq / Hkv).
+ * Request b's tokens are those of block_table[b] up to kv_len[b], its new ones the
+ * last cu_new[b+1] - cu_new[b] of them (dsp_kv4_append has stored them); what of
+ * them a query sees goes by `mask_kind`.  A query that sees nothing, or whose
+ * scores are all -inf, gets 0.  Tokens that are not seen are not multiplied by
+ * anything: whatever their bytes hold, NaN included, changes nothing.
+ *
+ * q bf16 [T,Hq,D] (strides in elements, rows 16-byte aligned); out bf16 [T,Hq,D]
+ * contiguous; rows from cu_new[B] on are not written.  block_table int32 [B,
+ * max_blocks]; kv_len int32 [B]; cu_new int32 [B+1]; max_new: no request has more
+ * new tokens (more are not answered).  mask_bits uint32 [T, mask_words] for
+ * DSP_MASK_BITS, else null; new tokens from 32 * mask_words on are not seen.
+ * A block number outside 0..n_blocks-1 hides its tokens.  Lengths outside what the
+ * table holds are clipped.  Scores, sums and outputs are accumulated in fp32.
+ * workspace: dsp_attn_kv4_workspace_bytes(...), 256-byte aligned; garbage before
+ * and after.
+ * Errors : INVALID_ARG (null pointer, negative sizes, Hq not a multiple of Hkv,
+ *          max_new < 1, max_blocks < 1, strides, page_size not a multiple of 16,
+ *          alignment, scale not finite, mask), UNSUPPORTED (dtype not DSP_BF16,
+ *          D not 64 / 128, B > 65535, more than 2^24 tokens or 4096 heads), WORKSPACE, CUDA.
+ */
+int32_t dsp_attn_kv4_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new,
+                                     size_t *bytes /* host, out */);
+int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                     int64_t q_stride_t, int64_t q_stride_h,
+                     const void *cache, int32_t n_blocks, int32_t page_size,
+                     const int32_t *block_table, int64_t table_stride, int32_t max_blocks,
+                     const int32_t *kv_len, const int32_t *cu_new, int32_t max_new, float scale,
+                     int32_t mask_kind, const uint32_t *mask_bits, int32_t mask_words,
+                     void *out, void *workspace, size_t workspace_bytes, dsp_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

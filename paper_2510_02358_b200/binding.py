@@ -24,6 +24,9 @@ DSP_STATIC_WS_BYTES = 4 << 20
 DSP_F32, DSP_BF16 = 0, 1
 ROW_NONFINITE_INPUT, ROW_ZERO_RESIDUAL, ROW_NO_BONUS_ROW, ROW_EOS_ACCEPTED, ROW_EOS_STOPPED = 1, 2, 4, 8, 16
 ROW_TIMEOUT = 32
+ROW_NO_BLOCKS, ROW_TABLE_FULL, ROW_PLAN_FULL, ROW_BAD_LENGTH = 64, 128, 256, 512
+DSP_MASK_CAUSAL, DSP_MASK_FULL, DSP_MASK_BITS = 0, 1, 2
+DSP_MAX_PLAN_ROWS = 8192
 DSP_MAX_K, DSP_MAX_W, DSP_MAX_L = 32, 32, 1024
 
 EXPORTS = ["dsp_strerror", "dsp_last_cuda_error", "dsp_version", "dsp_profile_events", "dsp_read_probe", "dsp_lattice_workspace_bytes",
@@ -34,6 +37,8 @@ EXPORTS = ["dsp_strerror", "dsp_last_cuda_error", "dsp_version", "dsp_profile_ev
            "dsp_target_shard", "dsp_verify_merge_workspace_bytes", "dsp_verify_merge",
            "dsp_residual_sample_workspace_bytes", "dsp_residual_sample",
            "dsp_beam_tree", "dsp_verify_tree_workspace_bytes", "dsp_verify_tree", "dsp_verify_tree_stochastic",
+           "dsp_cache_plan", "dsp_qk_norm_rope", "dsp_kv4_append", "dsp_kv4_read",
+           "dsp_attn_kv4_workspace_bytes", "dsp_attn_kv4",
            "dsp_adl_init", "dsp_adl_update", "dsp_breadth_init", "dsp_breadth_update"]
 
 
@@ -644,3 +649,189 @@ def dsp_breadth_update(state: BreadthState, params: BreadthParams, entropy, acce
         C.byref(state), C.byref(params), C.c_void_p(e.data_ptr()), C.c_void_p(a.data_ptr()), C.c_void_p(g.data_ptr()),
         e.shape[0], e.shape[1], C.byref(K), C.byref(W)))
     return K.value, W.value
+
+
+# ---- the model pass around the step: paged 4-bit cache and attention over it ----
+
+def _ints(name: str, t: torch.Tensor, shape, dtype, dev) -> torch.Tensor:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), dev))
+    return t
+
+
+def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: torch.Tensor, ring_pos: torch.Tensor,
+                   block_table: torch.Tensor, free_ring: torch.Tensor, page_size: int, T: int, *,
+                   node_parent: Optional[torch.Tensor] = None, node_depth: Optional[torch.Tensor] = None,
+                   mask_words: int = 0, out: Optional[SimpleNamespace] = None, stream=None) -> SimpleNamespace:
+    """Block tables, slots and positions of ``T`` token rows from the requests' lengths (int32 [B] CUDA tensors).
+    ``block_table`` (int32 [B, max_blocks]) and ``free_ring`` (int32 [n_blocks]) are updated in place;
+    ``block_count`` and ``ring_pos`` (int64 {head, tail}) are inputs whose new values are returned."""
+    B, dev = seq_len.shape[0], seq_len.device
+    if not seq_len.is_cuda or block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.dtype != torch.int32 \
+            or block_table.shape[0] != B or block_table.device != dev:
+        raise ValueError("block_table must be an int32 CUDA tensor [B, max_blocks] with contiguous rows")
+    for name, t in (("seq_len", seq_len), ("new_len", new_len), ("block_count", block_count)):
+        _ints(name, t, (B,), torch.int32, dev)
+    _ints("ring_pos", ring_pos, (2,), torch.int64, dev)
+    _ints("free_ring", free_ring, (free_ring.numel(),), torch.int32, dev)
+    N = 0
+    if node_parent is not None or node_depth is not None:
+        if node_parent is None or node_depth is None or node_parent.dim() != 2:
+            raise ValueError("a tree needs node_parent and node_depth, [B, N] each")
+        N = node_parent.shape[1]
+        _ints("node_parent", node_parent, (B, N), torch.int32, dev)
+        _ints("node_depth", node_depth, (B, N), torch.int32, dev)
+        mask_words = mask_words or (N + 32) // 32
+    if out is None:
+        i32, i64 = torch.int32, torch.int64
+        rows = torch.empty(4 * B + 1, dtype=i32, device=dev)
+        toks = torch.empty(2 * T, dtype=i32, device=dev)
+        out = SimpleNamespace(block_count=rows[:B], kv_len=rows[B:2 * B], row_status=rows[2 * B:3 * B], cu_new=rows[3 * B:],
+                              ring_pos=torch.empty(2, dtype=i64, device=dev), slot=torch.empty(T, dtype=i64, device=dev),
+                              position=toks[:T], token_row=toks[T:],
+                              mask=torch.empty((T, mask_words), dtype=i32, device=dev) if N else None)
+    _check("dsp_cache_plan", lib().dsp_cache_plan(
+        _ptr(seq_len), _ptr(new_len), _ptr(block_count), _ptr(ring_pos), B, int(T), int(page_size), free_ring.numel(),
+        block_table.shape[1], _ptr(block_table), C.c_int64(block_table.stride(0) if B > 1 else block_table.shape[1]),
+        _ptr(free_ring), _ptr(node_parent), _ptr(node_depth), N, _ptr(out.block_count), _ptr(out.ring_pos),
+        _ptr(out.cu_new), _ptr(out.kv_len), _ptr(out.slot), _ptr(out.position), _ptr(out.token_row),
+        _ptr(out.mask), int(mask_words) if N else 0, _ptr(out.row_status), _stream(stream)))
+    return out
+
+
+def _heads(name: str, t: torch.Tensor, T: int, D: int, like: torch.Tensor):
+    """Heads and strides of a CUDA tensor [T, H, D] with contiguous channels (strides of single rows are free)."""
+    if t.dim() != 3 or not t.is_cuda or t.shape[0] != T or t.shape[2] != D or t.stride(2) != 1 \
+            or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError("%s must be a CUDA tensor [T, heads, D] with contiguous channels, of q's or k's dtype" % name)
+    H = t.shape[1]
+    sh = t.stride(1) if H > 1 else D
+    return H, (t.stride(0) if T > 1 else max(H * sh, D)), sh
+
+
+def _rope(q_weight, k_weight, positions, cos_sin, T: int, D: int, like: torch.Tensor):
+    dev = like.device
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _ints(name, w, (D,), like.dtype, dev)
+    if positions is not None:
+        _ints("positions", positions, (T,), torch.int32, dev)
+    if cos_sin is not None:
+        if positions is None or cos_sin.dim() != 2:
+            raise ValueError("cos_sin is a float [max_pos, rot] tensor and needs positions")
+        _ints("cos_sin", cos_sin, cos_sin.shape, torch.float32, dev)
+    rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
+    return _ptr(positions), _ptr(cos_sin), rows, rot
+
+
+def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
+                     interleaved: bool = False, out=None, stream=None):
+    """Norm and rotation of every query and key head: ``q`` [T, Hq, D], ``k`` [T, Hkv, D]; returns (q_out, k_out)."""
+    T, D = q.shape[0], q.shape[-1]
+    Hq, qt, qh = _heads("q", q, T, D, q)
+    Hkv, kt, kh = _heads("k", k, T, D, q)
+    pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, q)
+    if out is None:
+        out = (torch.empty((T, Hq, D), dtype=q.dtype, device=q.device), torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device))
+    _ints("out[0]", out[0], (T, Hq, D), q.dtype, q.device)
+    _ints("out[1]", out[1], (T, Hkv, D), q.dtype, q.device)
+    _check("dsp_qk_norm_rope", lib().dsp_qk_norm_rope(
+        _ptr(q), _ptr(k), _dtype(q), T, Hq, Hkv, D, C.c_int64(qt), C.c_int64(qh), C.c_int64(kt), C.c_int64(kh),
+        _ptr(q_weight), _ptr(k_weight), C.c_float(eps), pos, cs, rows, rot, int(interleaved),
+        _ptr(out[0]), _ptr(out[1]), _stream(stream)))
+    return out
+
+
+def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device) -> torch.Tensor:
+    """An empty 4-bit cache."""
+    return torch.zeros((n_blocks, Hkv, page_size * (D + 8)), dtype=torch.uint8, device=device)
+
+
+def _cache(cache: torch.Tensor, Hkv: int, D: int, dev):
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.device != dev \
+            or cache.shape[1] != Hkv or cache.shape[2] % (D + 8) != 0:
+        raise ValueError("cache must be a contiguous uint8 [n_blocks, Hkv, page_size * (D + 8)] tensor on the inputs' device")
+    return cache.shape[0], cache.shape[2] // (D + 8)
+
+
+def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, cache: torch.Tensor, *,
+                   q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
+                   interleaved: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Norm and rotation like dsp_qk_norm_rope; keys and values enter ``cache`` at ``slot`` (int64 [T]); returns q_out."""
+    T, D = k.shape[0], k.shape[-1]
+    Hkv, kt, kh = _heads("k", k, T, D, k)
+    Hv, vt, vh = _heads("v", v, T, D, k)
+    if Hv != Hkv:
+        raise ValueError("k and v must have the same number of heads")
+    Hq, qt, qh = (0, 0, 0) if q is None else _heads("q", q, T, D, k)
+    pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, k)
+    _ints("slot", slot, (T,), torch.int64, k.device)
+    n_blocks, page = _cache(cache, Hkv, D, k.device)
+    if q is not None:
+        if out is None:
+            out = torch.empty((T, Hq, D), dtype=k.dtype, device=k.device)
+        _ints("out", out, (T, Hq, D), k.dtype, k.device)
+    i64 = C.c_int64
+    _check("dsp_kv4_append", lib().dsp_kv4_append(
+        _ptr(q), _ptr(k), _ptr(v), _dtype(k), T, Hq, Hkv, D, i64(qt), i64(qh), i64(kt), i64(kh), i64(vt), i64(vh),
+        _ptr(q_weight), _ptr(k_weight), C.c_float(eps), pos, cs, rows, rot, int(interleaved),
+        _ptr(slot), _ptr(cache), n_blocks, page, _ptr(None if q is None else out), _stream(stream)))
+    return out if q is not None else None
+
+
+def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bfloat16, *, out=None, stream=None):
+    """The keys and values, [T, Hkv, D] each, that ``cache`` holds for the tokens in ``slot``."""
+    T, Hkv, dev = slot.shape[0], cache.shape[1], cache.device
+    n_blocks, page = _cache(cache, Hkv, D, dev)
+    _ints("slot", slot, (T,), torch.int64, dev)
+    if out is None:
+        out = (torch.empty((T, Hkv, D), dtype=dtype, device=dev), torch.empty((T, Hkv, D), dtype=dtype, device=dev))
+    for t in out:
+        _ints("out", t, (T, Hkv, D), dtype, dev)
+    _check("dsp_kv4_read", lib().dsp_kv4_read(_ptr(cache), n_blocks, page, Hkv, int(D), _ptr(slot), T, _dtype(out[0]),
+                                              _ptr(out[0]), _ptr(out[1]), _stream(stream)))
+    return out
+
+
+def dsp_attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int) -> int:
+    n = C.c_size_t(0)
+    _check("dsp_attn_kv4_workspace_bytes", lib().dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new, C.byref(n)))
+    return n.value
+
+
+def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                 cu_new: torch.Tensor, max_new: int, *, scale: Optional[float] = None, mask="causal",
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of ``q`` (bf16 [T, Hq, D]) over the 4-bit cache; ``mask`` is "causal", "full" or the visibility bits
+    (int32 [T, words]) of dsp_cache_plan; ``scale`` defaults to 1 / sqrt(D)."""
+    T, D = q.shape[0], q.shape[-1]
+    Hq, qt, qh = _heads("q", q, T, D, q)
+    B, dev, Hkv = kv_len.shape[0], q.device, cache.shape[1]
+    n_blocks, page = _cache(cache, Hkv, D, dev)
+    if block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.dtype != torch.int32 \
+            or block_table.shape[0] != B or block_table.device != dev:
+        raise ValueError("block_table must be an int32 CUDA tensor [B, max_blocks] with contiguous rows")
+    _ints("kv_len", kv_len, (B,), torch.int32, dev)
+    _ints("cu_new", cu_new, (B + 1,), torch.int32, dev)
+    kind, bits, words = DSP_MASK_BITS, None, 0
+    if isinstance(mask, str):
+        if mask not in ("causal", "full"):
+            raise ValueError("mask must be 'causal', 'full' or a tensor of bits")
+        kind = DSP_MASK_CAUSAL if mask == "causal" else DSP_MASK_FULL
+    else:
+        words = mask.shape[-1]
+        bits = _ints("mask", mask, (T, words), torch.int32, dev)
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
+    _ints("out", out, (T, Hq, D), q.dtype, dev)
+    if workspace is None:
+        workspace = alloc_workspace(dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new), dev)
+    _check("dsp_attn_kv4", lib().dsp_attn_kv4(
+        _ptr(q), _dtype(q), B, T, Hq, Hkv, D, C.c_int64(qt), C.c_int64(qh), _ptr(cache), n_blocks, page,
+        _ptr(block_table), C.c_int64(block_table.stride(0) if B > 1 else block_table.shape[1]), block_table.shape[1],
+        _ptr(kv_len), _ptr(cu_new), int(max_new), C.c_float(D ** -0.5 if scale is None else scale), kind, _ptr(bits), words,
+        _ptr(out), _ptr(workspace), C.c_size_t(workspace.numel()), _stream(stream)))
+    return out
