@@ -20,35 +20,44 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
-// Two codes as bf16 numbers 128 + code (0x4300 is 128, whose last mantissa bit is worth 1).
-__device__ __forceinline__ uint32_t biased(uint32_t w, int i) { return code_pair(w, i) | 0x43004300u; }
+// Two codes as bf16 numbers 128 + code (0x4300 is 128, whose last mantissa bit is worth 1): (w >> 4i & 0x000F000F) | 0x43004300.
+__device__ __forceinline__ uint32_t biased(uint32_t w, int i) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(y) : "r"(w >> (4 * i)));
+    return y;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void await_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
 
 constexpr float kBias = 128.0f;
+constexpr int kU = 2;                            // runs of 16 tokens a warp takes per iteration
 
-// A run of 16 tokens of one key head on its way through a warp's registers.
-template <int D> struct Run {
-    static constexpr int kVec = D / 64;          // 16-byte vectors of codes a lane holds, for keys and for values
-    uint4 k[kVec], v[kVec];
-    uint2 p[2];                                  // scales and offsets of the tokens r and r + 8
-    bool there;                                  // false: no such block, nothing was read
-    __device__ __forceinline__ void load(const uint8_t *run, int lane, bool ok) {
-        there = ok;
-        if (ok) {
+// A lane's codes of a run of 16 tokens, keys or values.
+template <int D> struct Codes {
+    uint4 v[D / 64];
+    __device__ __forceinline__ void load(uint32_t at) {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) k[i] = ldg_stream(run + i * 512 + lane * 16);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) v[i] = ldg_stream(run + Kv4<D>::kValueOff + i * 512 + lane * 16);
-            p[0] = __ldg(reinterpret_cast<const uint2 *>(run + Kv4<D>::kParamOff) + (lane >> 2));
-            p[1] = __ldg(reinterpret_cast<const uint2 *>(run + Kv4<D>::kParamOff) + (lane >> 2) + 8);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
-            p[0] = p[1] = make_uint2(0u, 0u);
-        }
+        for (int i = 0; i < D / 64; ++i) v[i] = lds128(at + i * 512);
     }
     // word i of the keys of token r + 8 * hi
     __device__ __forceinline__ uint32_t key(int i, int hi) const {
-        const uint4 &u = D == 128 ? k[D == 128 ? hi : 0] : k[0];
+        const uint4 &u = D == 128 ? v[D == 128 ? hi : 0] : v[0];
         const int at = D == 128 ? i : 2 * hi + i;
         return at == 0 ? u.x : at == 1 ? u.y : at == 2 ? u.z : u.w;
     }
@@ -75,11 +84,14 @@ template <int D> struct Run {
 // Each warp walks its own runs of 16 tokens with the next run's loads in flight, and keeps its own
 // running maximum: it moves only when a score passes it by 2^8 (the sums cannot overflow by that, and
 // the division at the end takes it out), so most runs need no exchange between lanes for it.
-template <int D, int NT, int kW, int kCtas>
+template <int D, int NT, int kW, int kCtas, int kStages>
 __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnArgs a) {
-    constexpr int kRows = 8 * NT, kStep = 16 * kW, kKs = D / 16, kMt = D / 16;
+    constexpr int kRows = 8 * NT, kStep = 16 * kU * kW, kKs = D / 16, kMt = D / 16;
     constexpr int kFrag = NT * kMt * 4 * 32;                      // floats of a partial output, in fragment order
-    __shared__ float s_o[kW][NT * kMt * 4][32];
+    constexpr int kStage = kU * Kv4<D>::kRunBytes, kRing = kStages * kStage;
+    // a ring of kStages iterations' codes for each warp; after a segment the same place takes its output
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    float (*s_o)[NT * kMt * 4][32] = reinterpret_cast<float (*)[NT * kMt * 4][32]>(s_dyn);
     __shared__ float s_m[kW][kRows], s_l[kW][kRows];
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
@@ -92,6 +104,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     const int runs_page = a.page >> 4;
     const long long head_bytes = (long long)runs_page * Kv4<D>::kRunBytes, block_bytes = head_bytes * a.Hkv;
 
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_dyn) + warp * kRing;
     Request rq;
     long long before = s_line.before;
     rq.load(a, s_line.b, kRows, kStep);
@@ -139,103 +152,140 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         const int safe = a.mask_kind == DSP_MASK_CAUSAL ? past + i_first + 1 : a.mask_kind == DSP_MASK_FULL ? rq.kv : past;
         const int stop = a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i_last + 1) : rq.kv;
 
-        float o[NT][kMt][4], ps[NT][4], m[NT][2], nm[NT][2], l[NT][2], zs[NT][2];
+        float o[NT][kMt][4], ps[NT][4], m[NT][2], l[NT][2], zs[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int j = 0; j < kMt; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.0f;
             ps[t][0] = ps[t][1] = ps[t][2] = ps[t][3] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { m[t][e] = -CUDART_INF_F; nm[t][e] = 0.0f; l[t][e] = 0.0f; zs[t][e] = 0.0f; }
+            for (int e = 0; e < 2; ++e) { m[t][e] = -CUDART_INF_F; l[t][e] = 0.0f; zs[t][e] = 0.0f; }
         }
-        // this warp's runs: run0, run0 + kW, ...; their blocks are looked up two runs ahead, loaded one ahead
-        int run = step0 * kW + warp;
-        const int run_end = min(step1 * kW, (max(stop, 0) + 15) >> 4);
-        const int hop_blk = kW / runs_page, hop_sub = kW - hop_blk * runs_page;
-        int blk = run / runs_page, sub = run - blk * runs_page;
+        // this warp's runs: kU neighbouring ones an iteration, kW iterations' worth on from one to the next
+        int run = (step0 * kW + warp) * kU;
+        const int run_end = min(step1 * kW * kU, (max(stop, 0) + 15) >> 4);
         const int32_t *table = a.table + (long long)rq.b * a.table_stride;
-        const uint8_t *head = a.cache + h * head_bytes;
-        auto advance = [&]() {
-            blk += hop_blk;
-            sub += hop_sub;
-            if (sub >= runs_page) { sub -= runs_page; ++blk; }
+        const uint8_t *head = a.cache + h * head_bytes + lane * 16;
+        // lane l looks up the run that is l / kU iterations ahead (its l % kU-th), the whole warp at once
+        int ids = -1, ids_sub = 0, ids_left = 0, ids_run = run;
+        auto lookup = [&]() {
+            const int mine = ids_run + (lane / kU) * (kW * kU) + lane % kU;
+            ids = -1;
+            if (mine < run_end) {
+                const int blk = runs_page == 1 ? mine : mine / runs_page;
+                ids = table[blk];
+                ids_sub = mine - blk * runs_page;
+                if (ids >= a.n_blocks) ids = -1;
+            }
+            ids_run += (32 / kU) * (kW * kU);
+            ids_left = 32;
         };
-        Run<D> next;
-        int id = -1, id_sub = 0;
-        if (run < run_end) {
-            const int first_id = table[blk];
-            next.load(head + first_id * block_bytes + (long long)sub * Kv4<D>::kRunBytes, lane, first_id >= 0 && first_id < a.n_blocks);
-            advance();
-            if (run + kW < run_end) { id = table[blk]; id_sub = sub; }
-        }
-        for (; run < run_end; run += kW) {
-            const Run<D> cur = next;
-            if (run + kW < run_end) {
-                next.load(head + id * block_bytes + (long long)id_sub * Kv4<D>::kRunBytes, lane, id >= 0 && id < a.n_blocks);
-                advance();
-                if (run + 2 * kW < run_end) { id = table[blk]; id_sub = sub; }
+        uint32_t there = 0u;                                      // per stage and run: whether its block exists
+        auto fetch = [&](int stage, bool more) {
+            if (more) {
+                if (ids_left == 0) lookup();
+#pragma unroll
+                for (int x = 0; x < kU; ++x) {
+                    const int from = 32 - ids_left + x;
+                    const int id = __shfl_sync(0xFFFFFFFFu, ids, from), sub = __shfl_sync(0xFFFFFFFFu, ids_sub, from);
+                    const uint32_t bit = 1u << (stage * kU + x), dst = ring + stage * kStage + x * Kv4<D>::kRunBytes + lane * 16;
+                    there &= ~bit;
+                    if (id >= 0) {
+                        there |= bit;
+                        const uint8_t *src = head + id * block_bytes + (long long)sub * Kv4<D>::kRunBytes;
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) copy16(dst + i * 512, src + i * 512);
+                        copy4(dst - lane * 12 + Kv4<D>::kParamOff, src - lane * 12 + Kv4<D>::kParamOff);
+                    }
+                }
+                ids_left -= kU;
             }
-            float s[NT][4];
+            copies_done();                                        // an empty group keeps the count of groups that of iterations
+        };
+        int ahead = run, stage = 0;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.0f;
+        for (int i = 0; i < kStages - 1; ++i, ahead += kW * kU) fetch(i, ahead < run_end);
+        for (; run < run_end; run += kW * kU, ahead += kW * kU) {
+            await_copies<kStages - 2>();
+            __syncwarp();                                         // every lane's copies have landed, and all have read the stage before
+            fetch(stage == 0 ? kStages - 1 : stage - 1, ahead < run_end);
+            const uint32_t codes = ring + stage * kStage + lane * 16, params = ring + stage * kStage + Kv4<D>::kParamOff + r * 8;
+            const uint32_t here = there >> (stage * kU);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            // a run beyond the end or of no block leaves its operands at whatever the ring holds (codes are finite) and is not seen
+            float s[kU][NT][4], va[kU][2], vz[kU][2];
 #pragma unroll
-            for (int j = 0; j < kKs; ++j) {
-                const uint32_t w0 = cur.key(j >> 1, 0), w1 = cur.key(j >> 1, 1);
-                const int i = 2 * (j & 1);
-                const uint32_t a0 = biased(w0, i), a1 = biased(w1, i), a2 = biased(w0, i + 1), a3 = biased(w1, i + 1);
+            for (int x = 0; x < kU; ++x) {
+                Codes<D> k;
+                k.load(codes + x * Kv4<D>::kRunBytes);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma_bf16(s[t], a0, a1, a2, a3, q[t][2 * j], q[t][2 * j + 1]);
+                for (int t = 0; t < NT; ++t) s[x][t][0] = s[x][t][1] = s[x][t][2] = s[x][t][3] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kKs; ++j) {
+                    const uint32_t w0 = k.key(j >> 1, 0), w1 = k.key(j >> 1, 1);
+                    const int i = 2 * (j & 1);
+                    const uint32_t a0 = biased(w0, i), a1 = biased(w1, i), a2 = biased(w0, i + 1), a3 = biased(w1, i + 1);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma_bf16(s[x][t], a0, a1, a2, a3, q[t][2 * j], q[t][2 * j + 1]);
+                }
+                // tokens r (e < 2) and r + 8: their scales, in base 2
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint2 p = lds64(params + x * Kv4<D>::kRunBytes + y * 64);
+                    const float ks = bf16_lo(p.x), kz = bf16_hi(p.x);
+                    const float ka = ks * a.scale_log2, kb = fmaf(-kBias, ks, kz) * a.scale_log2;
+                    va[x][y] = bf16_lo(p.y);
+                    vz[x][y] = fmaf(8.0f, va[x][y], bf16_hi(p.y));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) s[x][t][2 * y + e] = fmaf(ka, s[x][t][2 * y + e], kb * qs[t][e]);
+                }
             }
-            // tokens r (e < 2) and r + 8: their scales, in base 2
-            float ka[2], kb[2], va[2], vz[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const float ks = bf16_lo(cur.p[x].x), kz = bf16_hi(cur.p[x].x);
-                ka[x] = ks * a.scale_log2;
-                kb[x] = fmaf(-kBias, ks, kz) * a.scale_log2;
-                va[x] = bf16_lo(cur.p[x].y);
-                vz[x] = fmaf(8.0f, va[x], bf16_hi(cur.p[x].y));
-            }
-            const bool whole = run * 16 + 16 <= safe && cur.there;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = fmaf(ka[e >> 1], s[t][e], kb[e >> 1] * qs[t][e & 1]);
-            uint32_t seen = 0xFFFFFFFFu;                          // bit 4t + e
+            const bool whole = (run + kU) * 16 <= min(safe, run_end * 16) && (here & ((1u << kU) - 1)) == (1u << kU) - 1;
+            uint32_t seen = 0xFFFFFFFFu;                          // bit (x NT + t) 4 + e
             if (!whole) {
                 seen = 0u;
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int x = 0; x < kU; ++x)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int u = run * 16 + r + 8 * (e >> 1);
-                        bool ok = cur.there && u < lim[t][e & 1];
-                        if (a.mask_kind == DSP_MASK_BITS && ok && u >= past) {
-                            const int j = u - past, i = (row_first + t * 8 + 2 * c + (e & 1)) / a.group;
-                            ok = j < a.words * 32 && ((__ldg(a.bits + (long long)(rq.row0 + i) * a.words + (j >> 5)) >> (j & 31)) & 1u);
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int u = (run + x) * 16 + r + 8 * (e >> 1);
+                            bool ok = ((here >> x) & 1u) && run + x < run_end && u < lim[t][e & 1];
+                            if (a.mask_kind == DSP_MASK_BITS && ok && u >= past) {
+                                const int j = u - past, i = (row_first + t * 8 + 2 * c + (e & 1)) / a.group;
+                                ok = j < a.words * 32 && ((__ldg(a.bits + (long long)(rq.row0 + i) * a.words + (j >> 5)) >> (j & 31)) & 1u);
+                            }
+                            if (!ok) s[x][t][e] = -CUDART_INF_F;
+                            seen |= (ok ? 1u : 0u) << ((x * NT + t) * 4 + e);
                         }
-                        if (!ok) s[t][e] = -CUDART_INF_F;
-                        seen |= (ok ? 1u : 0u) << (4 * t + e);
-                    }
             }
             bool move = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) move = move || s[t][e] > m[t][e & 1] + 8.0f;
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(s[0][t][e], s[0][t][e + 2]);
+#pragma unroll
+                    for (int x = 1; x < kU; ++x) top = fmaxf(top, fmaxf(s[x][t][e], s[x][t][e + 2]));
+                    move = move || top > m[t][e] + 8.0f;
+                }
             if (__any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(s[t][e], s[t][e + 2]);
+                        float top = fmaxf(s[0][t][e], s[0][t][e + 2]);
+#pragma unroll
+                        for (int x = 1; x < kU; ++x) top = fmaxf(top, fmaxf(s[x][t][e], s[x][t][e + 2]));
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
                         top = fmaxf(top, m[t][e]);
                         const float keep = m[t][e] == top ? 1.0f : ex2_approx(m[t][e] - top);
                         m[t][e] = top;
-                        nm[t][e] = top == -CUDART_INF_F ? 0.0f : -top;
                         l[t][e] *= keep;
                         zs[t][e] *= keep;
                         ps[t][e] *= keep;
@@ -243,45 +293,52 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                         for (int j = 0; j < kMt; ++j) { o[t][j][e] *= keep; o[t][j][e + 2] *= keep; }
                     }
             }
-            uint32_t p[NT][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float w[4];
+            for (int x = 0; x < kU; ++x) {
+                uint32_t p[NT][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = ex2_approx(s[t][e] + nm[t][e & 1]);
-                    l[t][e & 1] += w[e];
-                }
-                if (whole) {
+                for (int t = 0; t < NT; ++t) {
+                    float w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        zs[t][e & 1] = fmaf(w[e], vz[e >> 1], zs[t][e & 1]);
-                        w[e] *= va[e >> 1];
+                        const float base = m[t][e & 1] == -CUDART_INF_F ? 0.0f : m[t][e & 1];
+                        w[e] = ex2_approx(s[x][t][e] - base);
+                        l[t][e & 1] += w[e];
                     }
-                } else {
+                    if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool ok = (seen >> (4 * t + e)) & 1u;      // what is not seen is not multiplied: its scale may be NaN
-                        zs[t][e & 1] += ok ? w[e] * vz[e >> 1] : 0.0f;
-                        w[e] = ok ? w[e] * va[e >> 1] : 0.0f;
+                        for (int e = 0; e < 4; ++e) {
+                            zs[t][e & 1] = fmaf(w[e], vz[x][e >> 1], zs[t][e & 1]);
+                            w[e] *= va[x][e >> 1];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool ok = (seen >> ((x * NT + t) * 4 + e)) & 1u;      // what is not seen is not multiplied: its scale may be NaN
+                            zs[t][e & 1] += ok ? w[e] * vz[x][e >> 1] : 0.0f;
+                            w[e] = ok ? w[e] * va[x][e >> 1] : 0.0f;
+                        }
                     }
+                    p[t][0] = transpose8x8(pack_bf16(w[0], w[1]));
+                    p[t][1] = transpose8x8(pack_bf16(w[2], w[3]));
+                    mma_bf16(ps[t], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, p[t][0], p[t][1]);
                 }
-                p[t][0] = transpose8x8(pack_bf16(w[0], w[1]));
-                p[t][1] = transpose8x8(pack_bf16(w[2], w[3]));
-                mma_bf16(ps[t], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, p[t][0], p[t][1]);
-            }
+                Codes<D> v;
+                v.load(codes + x * Kv4<D>::kRunBytes + Kv4<D>::kValueOff);
 #pragma unroll
-            for (int i = 0; i < kMt / 4; ++i) {
-                const uint32_t e0 = __byte_perm(cur.val(i, 0, 0), cur.val(i, 0, 1), 0x5410), o0 = __byte_perm(cur.val(i, 0, 0), cur.val(i, 0, 1), 0x7632);
-                const uint32_t e1 = __byte_perm(cur.val(i, 1, 0), cur.val(i, 1, 1), 0x5410), o1 = __byte_perm(cur.val(i, 1, 0), cur.val(i, 1, 1), 0x7632);
+                for (int i = 0; i < kMt / 4; ++i) {
+                    const uint32_t e0 = __byte_perm(v.val(i, 0, 0), v.val(i, 0, 1), 0x5410), o0 = __byte_perm(v.val(i, 0, 0), v.val(i, 0, 1), 0x7632);
+                    const uint32_t e1 = __byte_perm(v.val(i, 1, 0), v.val(i, 1, 1), 0x5410), o1 = __byte_perm(v.val(i, 1, 0), v.val(i, 1, 1), 0x7632);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t a0 = biased(e0, x), a1 = biased(o0, x), a2 = biased(e1, x), a3 = biased(o1, x);
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t a0 = biased(e0, y), a1 = biased(o0, y), a2 = biased(e1, y), a3 = biased(o1, y);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma_bf16(o[t][4 * i + x], a0, a1, a2, a3, p[t][0], p[t][1]);
+                        for (int t = 0; t < NT; ++t) mma_bf16(o[t][4 * i + y], a0, a1, a2, a3, p[t][0], p[t][1]);
+                    }
                 }
             }
         }
+        __syncthreads();                                          // the rings' places become s_o
         // the warps' results: common maximum, then one sum per output in the order of the warps
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -414,10 +471,13 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
     return s;
 }
 
-template <int D, int NT, int kW, int kCtas>
+template <int D, int NT, int kW, int kCtas, int kStages>
 cudaError_t launch_stream(const AttnArgs &a, int grid, cudaStream_t st) {
-    attn_stream_kernel<D, NT, kW, kCtas><<<grid, kW * 32, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    constexpr int ring = kW * kStages * kU * Kv4<D>::kRunBytes, outs = kW * NT * (D / 16) * 4 * 32 * 4, smem = ring > outs ? ring : outs;
+    cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, NT, kW, kCtas, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    attn_stream_kernel<D, NT, kW, kCtas, kStages><<<grid, kW * 32, smem, st>>>(a);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_dependent(attn_join_kernel<D, NT>, (unsigned)grid, 128, 0, st, a, true);
 }
@@ -473,14 +533,14 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + align_up(s.grid * sizeof(SplitUnit), 256));
     // no more CTAs than the line can have steps, as far as the host knows the lengths
     const long long tokens = (long long)max_blocks * page_size, rows = (long long)a.max_new * a.group;
-    const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * s.warps - 1) / (16 * s.warps));
+    const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * kU * s.warps - 1) / (16 * kU * s.warps));
     const int grid = (int)(most < s.grid ? most : s.grid);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (D == 64)
-        e = s.nt == 1 ? launch_stream<64, 1, 8, 2>(a, grid, st) : launch_stream<64, 2, 4, 3>(a, grid, st);
+        e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 3>(a, grid, st) : launch_stream<64, 2, 4, 3, 3>(a, grid, st);
     else
-        e = s.nt == 1 ? launch_stream<128, 1, 8, 2>(a, grid, st) : launch_stream<128, 2, 4, 3>(a, grid, st);
+        e = s.nt == 1 ? launch_stream<128, 1, 8, 2, 3>(a, grid, st) : launch_stream<128, 2, 4, 3, 3>(a, grid, st);
     DSP_CUDA_TRY(e);
     return DSP_OK;
 }
