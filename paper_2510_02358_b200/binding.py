@@ -61,6 +61,15 @@ class AdlState(C.Structure):
                 ("steps", C.c_int32)]
 
 
+# p pointer, i int32, l int64, f float, z size_t, in the order of the header
+_SIGNATURES = {
+    "dsp_cache_plan": "ppppiiiiiplpppippppppppipp",
+    "dsp_qk_norm_rope": "ppiiiiillllppfppiiippp",
+    "dsp_kv4_append": "pppiiiiillllllppfppiiippiipp",
+    "dsp_kv4_read": "piiiipiippp",
+    "dsp_attn_kv4": "piiiiiillpiiplippifipippzp",
+}
+
 _lib = None
 
 
@@ -76,6 +85,10 @@ def lib():
         l.dsp_strerror.argtypes = [C.c_int32]
         for name in EXPORTS[1:]:
             getattr(l, name).restype = C.c_int32
+        # Calls made once per layer take plain integers: with declared types ctypes converts them in C.
+        kinds = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "z": C.c_size_t}
+        for name, args in _SIGNATURES.items():
+            getattr(l, name).argtypes = [kinds[c] for c in args]
         _lib = l
     return _lib
 
@@ -652,11 +665,30 @@ def dsp_breadth_update(state: BreadthState, params: BreadthParams, entropy, acce
 
 
 # ---- the model pass around the step: paged 4-bit cache and attention over it ----
+# These calls are made once per layer, so their checks are kept short.
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _queue(stream, dev: torch.device) -> int:
+    """Raw handle of the stream that a call goes to: torch's current one on the tensors' device."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
 
 def _ints(name: str, t: torch.Tensor, shape, dtype, dev) -> torch.Tensor:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
+    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), dev))
     return t
+
+
+def _table(t: torch.Tensor, B: int, dev):
+    if t.dim() != 2 or t.dtype != torch.int32 or t.shape[0] != B or t.device != dev or t.stride(1) != 1:
+        raise ValueError("block_table must be an int32 CUDA tensor [B, max_blocks] with contiguous rows")
+    width = t.shape[1]
+    return t.data_ptr(), (t.stride(0) if B > 1 else width), width
 
 
 def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: torch.Tensor, ring_pos: torch.Tensor,
@@ -666,62 +698,67 @@ def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: to
     """Block tables, slots and positions of ``T`` token rows from the requests' lengths (int32 [B] CUDA tensors).
     ``block_table`` (int32 [B, max_blocks]) and ``free_ring`` (int32 [n_blocks]) are updated in place;
     ``block_count`` and ``ring_pos`` (int64 {head, tail}) are inputs whose new values are returned."""
-    B, dev = seq_len.shape[0], seq_len.device
-    if not seq_len.is_cuda or block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.dtype != torch.int32 \
-            or block_table.shape[0] != B or block_table.device != dev:
-        raise ValueError("block_table must be an int32 CUDA tensor [B, max_blocks] with contiguous rows")
+    dev, i32, i64 = seq_len.device, torch.int32, torch.int64
+    if not seq_len.is_cuda:
+        raise ValueError("seq_len must be a CUDA tensor")
+    B = seq_len.shape[0]
     for name, t in (("seq_len", seq_len), ("new_len", new_len), ("block_count", block_count)):
-        _ints(name, t, (B,), torch.int32, dev)
-    _ints("ring_pos", ring_pos, (2,), torch.int64, dev)
-    _ints("free_ring", free_ring, (free_ring.numel(),), torch.int32, dev)
+        _ints(name, t, (B,), i32, dev)
+    _ints("ring_pos", ring_pos, (2,), i64, dev)
+    n_blocks = free_ring.numel()
+    _ints("free_ring", free_ring, (n_blocks,), i32, dev)
+    table, stride, width = _table(block_table, B, dev)
     N = 0
     if node_parent is not None or node_depth is not None:
         if node_parent is None or node_depth is None or node_parent.dim() != 2:
             raise ValueError("a tree needs node_parent and node_depth, [B, N] each")
         N = node_parent.shape[1]
-        _ints("node_parent", node_parent, (B, N), torch.int32, dev)
-        _ints("node_depth", node_depth, (B, N), torch.int32, dev)
+        _ints("node_parent", node_parent, (B, N), i32, dev)
+        _ints("node_depth", node_depth, (B, N), i32, dev)
         mask_words = mask_words or (N + 32) // 32
     if out is None:
-        i32, i64 = torch.int32, torch.int64
-        rows = torch.empty(4 * B + 1, dtype=i32, device=dev)
-        toks = torch.empty(2 * T, dtype=i32, device=dev)
-        out = SimpleNamespace(block_count=rows[:B], kv_len=rows[B:2 * B], row_status=rows[2 * B:3 * B], cu_new=rows[3 * B:],
-                              ring_pos=torch.empty(2, dtype=i64, device=dev), slot=torch.empty(T, dtype=i64, device=dev),
-                              position=toks[:T], token_row=toks[T:],
+        count, kv_len, status = torch.empty((3, B), dtype=i32, device=dev).unbind(0)
+        position, token_row = torch.empty((2, T), dtype=i32, device=dev).unbind(0)
+        out = SimpleNamespace(block_count=count, kv_len=kv_len, row_status=status, position=position, token_row=token_row,
+                              cu_new=torch.empty(B + 1, dtype=i32, device=dev), ring_pos=torch.empty(2, dtype=i64, device=dev),
+                              slot=torch.empty(T, dtype=i64, device=dev),
                               mask=torch.empty((T, mask_words), dtype=i32, device=dev) if N else None)
     _check("dsp_cache_plan", lib().dsp_cache_plan(
-        _ptr(seq_len), _ptr(new_len), _ptr(block_count), _ptr(ring_pos), B, int(T), int(page_size), free_ring.numel(),
-        block_table.shape[1], _ptr(block_table), C.c_int64(block_table.stride(0) if B > 1 else block_table.shape[1]),
-        _ptr(free_ring), _ptr(node_parent), _ptr(node_depth), N, _ptr(out.block_count), _ptr(out.ring_pos),
-        _ptr(out.cu_new), _ptr(out.kv_len), _ptr(out.slot), _ptr(out.position), _ptr(out.token_row),
-        _ptr(out.mask), int(mask_words) if N else 0, _ptr(out.row_status), _stream(stream)))
+        seq_len.data_ptr(), new_len.data_ptr(), block_count.data_ptr(), ring_pos.data_ptr(), B, T, page_size, n_blocks, width,
+        table, stride, free_ring.data_ptr(), _at(node_parent), _at(node_depth), N,
+        out.block_count.data_ptr(), out.ring_pos.data_ptr(), out.cu_new.data_ptr(), out.kv_len.data_ptr(),
+        out.slot.data_ptr(), out.position.data_ptr(), _at(out.token_row), _at(out.mask), mask_words if N else 0,
+        out.row_status.data_ptr(), _queue(stream, dev)))
     return out
 
 
-def _heads(name: str, t: torch.Tensor, T: int, D: int, like: torch.Tensor):
+def _heads(name: str, t: torch.Tensor, T: int, D: int, dtype, dev):
     """Heads and strides of a CUDA tensor [T, H, D] with contiguous channels (strides of single rows are free)."""
-    if t.dim() != 3 or not t.is_cuda or t.shape[0] != T or t.shape[2] != D or t.stride(2) != 1 \
-            or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError("%s must be a CUDA tensor [T, heads, D] with contiguous channels, of q's or k's dtype" % name)
-    H = t.shape[1]
-    sh = t.stride(1) if H > 1 else D
-    return H, (t.stride(0) if T > 1 else max(H * sh, D)), sh
+    if t.dim() != 3 or t.dtype != dtype or t.device != dev or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor [T, heads, D] of the call's dtype and device" % name)
+    n, H, d = t.shape
+    st, sh, sd = t.stride()
+    if n != T or d != D or sd != 1:
+        raise ValueError("%s must be [T, heads, D] with T = %d, D = %d and contiguous channels" % (name, T, D))
+    if H == 1:
+        sh = D
+    return H, (st if T > 1 else max(H * sh, D)), sh
 
 
-def _rope(q_weight, k_weight, positions, cos_sin, T: int, D: int, like: torch.Tensor):
-    dev = like.device
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _ints(name, w, (D,), like.dtype, dev)
+def _rope(q_weight, k_weight, positions, cos_sin, T: int, D: int, dtype, dev):
+    if q_weight is not None:
+        _ints("q_weight", q_weight, (D,), dtype, dev)
+    if k_weight is not None:
+        _ints("k_weight", k_weight, (D,), dtype, dev)
     if positions is not None:
         _ints("positions", positions, (T,), torch.int32, dev)
-    if cos_sin is not None:
-        if positions is None or cos_sin.dim() != 2:
-            raise ValueError("cos_sin is a float [max_pos, rot] tensor and needs positions")
-        _ints("cos_sin", cos_sin, cos_sin.shape, torch.float32, dev)
-    rows, rot = (0, 0) if cos_sin is None else cos_sin.shape
-    return _ptr(positions), _ptr(cos_sin), rows, rot
+    if cos_sin is None:
+        return _at(q_weight), _at(k_weight), _at(positions), None, 0, 0
+    if positions is None or cos_sin.dim() != 2:
+        raise ValueError("cos_sin is a float [max_pos, rot] tensor and needs positions")
+    rows, rot = cos_sin.shape
+    _ints("cos_sin", cos_sin, (rows, rot), torch.float32, dev)
+    return _at(q_weight), _at(k_weight), positions.data_ptr(), cos_sin.data_ptr(), rows, rot
 
 
 def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[torch.Tensor] = None,
@@ -729,19 +766,18 @@ def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[tor
                      positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
                      interleaved: bool = False, out=None, stream=None):
     """Norm and rotation of every query and key head: ``q`` [T, Hq, D], ``k`` [T, Hkv, D]; returns (q_out, k_out)."""
-    T, D = q.shape[0], q.shape[-1]
-    Hq, qt, qh = _heads("q", q, T, D, q)
-    Hkv, kt, kh = _heads("k", k, T, D, q)
-    pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, q)
+    T, D, dt, dev = q.shape[0], q.shape[-1], q.dtype, q.device
+    Hq, qt, qh = _heads("q", q, T, D, dt, dev)
+    Hkv, kt, kh = _heads("k", k, T, D, dt, dev)
+    wq, wk, pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, dt, dev)
     if out is None:
-        out = (torch.empty((T, Hq, D), dtype=q.dtype, device=q.device), torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device))
-    _ints("out[0]", out[0], (T, Hq, D), q.dtype, q.device)
-    _ints("out[1]", out[1], (T, Hkv, D), q.dtype, q.device)
+        q_out, k_out = torch.empty((T, Hq, D), dtype=dt, device=dev), torch.empty((T, Hkv, D), dtype=dt, device=dev)
+    else:
+        q_out, k_out = _ints("out[0]", out[0], (T, Hq, D), dt, dev), _ints("out[1]", out[1], (T, Hkv, D), dt, dev)
     _check("dsp_qk_norm_rope", lib().dsp_qk_norm_rope(
-        _ptr(q), _ptr(k), _dtype(q), T, Hq, Hkv, D, C.c_int64(qt), C.c_int64(qh), C.c_int64(kt), C.c_int64(kh),
-        _ptr(q_weight), _ptr(k_weight), C.c_float(eps), pos, cs, rows, rot, int(interleaved),
-        _ptr(out[0]), _ptr(out[1]), _stream(stream)))
-    return out
+        q.data_ptr(), k.data_ptr(), _dtype(q), T, Hq, Hkv, D, qt, qh, kt, kh, wq, wk, eps, pos, cs, rows, rot,
+        interleaved, q_out.data_ptr(), k_out.data_ptr(), _queue(stream, dev)))
+    return q_out, k_out
 
 
 def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device) -> torch.Tensor:
@@ -750,10 +786,11 @@ def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device) -> torch.
 
 
 def _cache(cache: torch.Tensor, Hkv: int, D: int, dev):
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.device != dev \
-            or cache.shape[1] != Hkv or cache.shape[2] % (D + 8) != 0:
-        raise ValueError("cache must be a contiguous uint8 [n_blocks, Hkv, page_size * (D + 8)] tensor on the inputs' device")
-    return cache.shape[0], cache.shape[2] // (D + 8)
+    if cache.dim() == 3:
+        n_blocks, H, size = cache.shape
+        if H == Hkv and size % (D + 8) == 0 and cache.dtype == torch.uint8 and cache.device == dev and cache.is_contiguous():
+            return n_blocks, size // (D + 8)
+    raise ValueError("cache must be a contiguous uint8 [n_blocks, Hkv, page_size * (D + 8)] tensor on the inputs' device")
 
 
 def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, cache: torch.Tensor, *,
@@ -761,25 +798,25 @@ def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
                    positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
                    interleaved: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """Norm and rotation like dsp_qk_norm_rope; keys and values enter ``cache`` at ``slot`` (int64 [T]); returns q_out."""
-    T, D = k.shape[0], k.shape[-1]
-    Hkv, kt, kh = _heads("k", k, T, D, k)
-    Hv, vt, vh = _heads("v", v, T, D, k)
+    T, D, dt, dev = k.shape[0], k.shape[-1], k.dtype, k.device
+    Hkv, kt, kh = _heads("k", k, T, D, dt, dev)
+    Hv, vt, vh = _heads("v", v, T, D, dt, dev)
     if Hv != Hkv:
         raise ValueError("k and v must have the same number of heads")
-    Hq, qt, qh = (0, 0, 0) if q is None else _heads("q", q, T, D, k)
-    pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, k)
-    _ints("slot", slot, (T,), torch.int64, k.device)
-    n_blocks, page = _cache(cache, Hkv, D, k.device)
-    if q is not None:
-        if out is None:
-            out = torch.empty((T, Hq, D), dtype=k.dtype, device=k.device)
-        _ints("out", out, (T, Hq, D), k.dtype, k.device)
-    i64 = C.c_int64
+    Hq, qt, qh = (0, 0, 0) if q is None else _heads("q", q, T, D, dt, dev)
+    wq, wk, pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, dt, dev)
+    _ints("slot", slot, (T,), torch.int64, dev)
+    n_blocks, page = _cache(cache, Hkv, D, dev)
+    if q is None:
+        out = None
+    elif out is None:
+        out = torch.empty((T, Hq, D), dtype=dt, device=dev)
+    else:
+        _ints("out", out, (T, Hq, D), dt, dev)
     _check("dsp_kv4_append", lib().dsp_kv4_append(
-        _ptr(q), _ptr(k), _ptr(v), _dtype(k), T, Hq, Hkv, D, i64(qt), i64(qh), i64(kt), i64(kh), i64(vt), i64(vh),
-        _ptr(q_weight), _ptr(k_weight), C.c_float(eps), pos, cs, rows, rot, int(interleaved),
-        _ptr(slot), _ptr(cache), n_blocks, page, _ptr(None if q is None else out), _stream(stream)))
-    return out if q is not None else None
+        _at(q), k.data_ptr(), v.data_ptr(), _dtype(k), T, Hq, Hkv, D, qt, qh, kt, kh, vt, vh, wq, wk, eps, pos, cs, rows, rot,
+        interleaved, slot.data_ptr(), cache.data_ptr(), n_blocks, page, _at(out), _queue(stream, dev)))
+    return out
 
 
 def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bfloat16, *, out=None, stream=None):
@@ -788,12 +825,12 @@ def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bf
     n_blocks, page = _cache(cache, Hkv, D, dev)
     _ints("slot", slot, (T,), torch.int64, dev)
     if out is None:
-        out = (torch.empty((T, Hkv, D), dtype=dtype, device=dev), torch.empty((T, Hkv, D), dtype=dtype, device=dev))
-    for t in out:
-        _ints("out", t, (T, Hkv, D), dtype, dev)
-    _check("dsp_kv4_read", lib().dsp_kv4_read(_ptr(cache), n_blocks, page, Hkv, int(D), _ptr(slot), T, _dtype(out[0]),
-                                              _ptr(out[0]), _ptr(out[1]), _stream(stream)))
-    return out
+        k, v = torch.empty((T, Hkv, D), dtype=dtype, device=dev), torch.empty((T, Hkv, D), dtype=dtype, device=dev)
+    else:
+        k, v = (_ints("out", t, (T, Hkv, D), dtype, dev) for t in out)
+    _check("dsp_kv4_read", lib().dsp_kv4_read(cache.data_ptr(), n_blocks, page, Hkv, D, slot.data_ptr(), T, _dtype(k),
+                                              k.data_ptr(), v.data_ptr(), _queue(stream, dev)))
+    return k, v
 
 
 def dsp_attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int) -> int:
@@ -807,13 +844,11 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of ``q`` (bf16 [T, Hq, D]) over the 4-bit cache; ``mask`` is "causal", "full" or the visibility bits
     (int32 [T, words]) of dsp_cache_plan; ``scale`` defaults to 1 / sqrt(D)."""
-    T, D = q.shape[0], q.shape[-1]
-    Hq, qt, qh = _heads("q", q, T, D, q)
-    B, dev, Hkv = kv_len.shape[0], q.device, cache.shape[1]
+    T, D, dt, dev = q.shape[0], q.shape[-1], q.dtype, q.device
+    Hq, qt, qh = _heads("q", q, T, D, dt, dev)
+    B, Hkv = kv_len.shape[0], cache.shape[1]
     n_blocks, page = _cache(cache, Hkv, D, dev)
-    if block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.dtype != torch.int32 \
-            or block_table.shape[0] != B or block_table.device != dev:
-        raise ValueError("block_table must be an int32 CUDA tensor [B, max_blocks] with contiguous rows")
+    table, stride, width = _table(block_table, B, dev)
     _ints("kv_len", kv_len, (B,), torch.int32, dev)
     _ints("cu_new", cu_new, (B + 1,), torch.int32, dev)
     kind, bits, words = DSP_MASK_BITS, None, 0
@@ -825,13 +860,13 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
         words = mask.shape[-1]
         bits = _ints("mask", mask, (T, words), torch.int32, dev)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
-    _ints("out", out, (T, Hq, D), q.dtype, dev)
+        out = torch.empty((T, Hq, D), dtype=dt, device=dev)
+    else:
+        _ints("out", out, (T, Hq, D), dt, dev)
     if workspace is None:
         workspace = alloc_workspace(dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new), dev)
     _check("dsp_attn_kv4", lib().dsp_attn_kv4(
-        _ptr(q), _dtype(q), B, T, Hq, Hkv, D, C.c_int64(qt), C.c_int64(qh), _ptr(cache), n_blocks, page,
-        _ptr(block_table), C.c_int64(block_table.stride(0) if B > 1 else block_table.shape[1]), block_table.shape[1],
-        _ptr(kv_len), _ptr(cu_new), int(max_new), C.c_float(D ** -0.5 if scale is None else scale), kind, _ptr(bits), words,
-        _ptr(out), _ptr(workspace), C.c_size_t(workspace.numel()), _stream(stream)))
+        q.data_ptr(), _dtype(q), B, T, Hq, Hkv, D, qt, qh, cache.data_ptr(), n_blocks, page, table, stride, width,
+        kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,
+        out.data_ptr(), workspace.data_ptr(), workspace.numel(), _queue(stream, dev)))
     return out

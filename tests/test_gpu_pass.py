@@ -7,6 +7,8 @@ mean, so scores of unit spread give a relative error of 3.3e-3 over a case's out
 is allowed, and 2% of the largest value for a single output.
 """
 import ctypes as C
+import os
+import re
 from types import SimpleNamespace
 
 import numpy as np
@@ -445,6 +447,17 @@ def test_rows_beyond_the_requests_are_left_alone_and_graphs_replay_with_other_le
 
 
 # --------------------------------------------------------------------------------------- refusals
+def test_declared_argument_types_are_those_of_the_header():
+    text = open(os.path.join(os.path.dirname(dsp.LIB_PATH), "..", "include", "dsp.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    for name, kinds in dsp._SIGNATURES.items():
+        args = re.search(r"int32_t %s\(([^;]*)\);" % name, text, flags=re.S).group(1).split(",")
+        assert len(args) == len(kinds)
+        for a, k in zip(args, kinds):
+            want = "p" if "*" in a or "dsp_stream_t" in a else next(c for w, c in (("int64_t", "l"), ("int32_t", "i"), ("float", "f"), ("size_t", "z")) if w in a)
+            assert k == want, (name, a)
+
+
 def test_refusals_happen_on_the_host():
     lib, z, one, odd = dsp.lib(), C.c_void_p(0), C.c_void_p(4096), C.c_void_p(4098)
     i64, f = C.c_int64, C.c_float
