@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include "attn.cuh"
+#include "attn_block.h"
 
 namespace dsp {
 namespace {
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     __shared__ LineStart s_line;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     if (threadIdx.x == 0) a.split[blockIdx.x].last_cta = -1;
-    enter_line(a, kRows, kStep, s_scan, &s_line);
+    enter_line<Request>(a, kRows, kStep, 1, s_scan, &s_line);
     long long at = s_line.begin;
     const long long end = s_line.end, total = s_line.total;
     if (at >= end) return;
@@ -450,6 +451,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs a) {
 
 // Launch shape of a call, from what the host knows of it.
 struct Shape {
+    bool block;                                  // the kernel for many rows
     int nt, warps, ctas_sm, grid;
     size_t part_bytes;
 };
@@ -463,6 +465,14 @@ int sm_count() {
 Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
     Shape s;
     const long long rows = (long long)max_new * (Hq / Hkv);
+    s.block = rows > 16;
+    if (s.block) {
+        s.nt = s.warps = 0;
+        s.ctas_sm = 1;
+        s.grid = sm_count();
+        s.part_bytes = attn_block_part_bytes(D);
+        return s;
+    }
     s.nt = rows <= 8 ? 1 : 2;
     s.warps = s.nt == 1 ? 8 : 4;
     s.ctas_sm = s.nt == 1 ? 2 : 3;
@@ -532,10 +542,14 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     a.split = static_cast<SplitUnit *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + align_up(s.grid * sizeof(SplitUnit), 256));
     // no more CTAs than the line can have steps, as far as the host knows the lengths
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (s.block) {
+        DSP_CUDA_TRY(attn_block_launch(a, D, s.grid, st));
+        return DSP_OK;
+    }
     const long long tokens = (long long)max_blocks * page_size, rows = (long long)a.max_new * a.group;
     const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * kU * s.warps - 1) / (16 * kU * s.warps));
     const int grid = (int)(most < s.grid ? most : s.grid);
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (D == 64)
         e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 3>(a, grid, st) : launch_stream<64, 2, 4, 3, 3>(a, grid, st);

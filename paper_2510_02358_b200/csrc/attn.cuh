@@ -60,18 +60,20 @@ __device__ __forceinline__ int cta_of(long long x, long long total, int ctas) { 
 // Where the line is entered: request, and the step within the request, at which the CTA's share begins.
 struct LineStart {
     long long total, begin, end;                 // of the line; this CTA's share
-    int ctas;                                    // CTAs with a share (no more than there are steps, so none is empty)
+    int ctas;                                    // CTAs with a share: none is empty
     int b;
     long long before;                            // line place where request b begins
 };
 // Every thread of the CTA calls it; scratch: 32 long longs and the result's place in shared memory.
-__device__ __forceinline__ void enter_line(const AttnArgs &a, int tile_rows, int step_tokens, long long *scratch, LineStart *out) {
+// min_share: no CTA's share is shorter.
+template <typename Req>
+__device__ __forceinline__ void enter_line(const AttnArgs &a, int tile_rows, int step_tokens, int min_share, long long *scratch, LineStart *out) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int per = (a.B + blockDim.x - 1) / blockDim.x;
     const int b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
     long long mine = 0;
     for (int b = b0; b < b1; ++b) {
-        Request r;
+        Req r;
         r.load(a, b, tile_rows, step_tokens);
         mine += r.length(a.Hkv);
     }
@@ -89,12 +91,12 @@ __device__ __forceinline__ void enter_line(const AttnArgs &a, int tile_rows, int
         total += v;
         if (w < warp) before += v;
     }
-    const int ctas = (int)min((long long)gridDim.x, total);
+    const int ctas = (int)min((long long)gridDim.x, total > 0 ? max(1LL, total / min_share) : 0LL);
     const bool idle = (int)blockIdx.x >= ctas;
     const long long begin = idle ? total : share_begin(total, blockIdx.x, ctas), end = idle ? total : share_begin(total, blockIdx.x + 1, ctas);
     if (begin >= before && begin < before + mine) {
         for (int b = b0; b < b1; ++b) {
-            Request r;
+            Req r;
             r.load(a, b, tile_rows, step_tokens);
             const long long n = r.length(a.Hkv);
             if (begin < before + n) {
