@@ -9,9 +9,9 @@
 //
 //   warps 0-7   softmax, four per slot, one thread per query row: maximum, exponentials, weights in bf16
 //               back into the scores' columns as the second product's operand
-//   warps 8-15  the tiles' codes (four warps keys, four values): 16-byte loads one tile ahead in
-//               registers, four bits to bf16 values, swizzled stores; two stages of each
-//   warp 16     one thread issues the products: S = Q K^T, O += P V
+//   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
+//               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
+//   warp 16     one lane issues the products: S = Q K^T, O += P V (warps 17-19 only complete its warpgroup)
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
@@ -28,7 +28,11 @@
 namespace dsp {
 namespace {
 
-constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 1) * 32;
+constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 4) * 32;
+// Registers per thread: the block is launched with 96 for each of its 640 threads; of that sum the softmax
+// warpgroups take 144 (256 x 144), the fill warpgroups 72, the last one (whose first warp issues the products) 48.
+constexpr int kSoftRegs = 144, kFillRegs = 72, kProductRegs = 48;
+static_assert(256 * kSoftRegs + 256 * kFillRegs + 128 * kProductRegs <= kBlockThreads * 96, "register split");
 constexpr int kTile = 128;                       // query rows of a slot, tokens of a tile
 constexpr int kRunsTile = kTile / 16;
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
@@ -63,6 +67,11 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void commit_to(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+    return ok != 0u;
 }
 // Operand tiles lie in shared memory as blocks of 64 channels: [block][row][128 bytes], the 16-byte
 // pieces of a row exchanged by its number modulo 8 (the 128-byte swizzle).  The same bytes serve as an
@@ -201,8 +210,8 @@ struct Walk {
 struct Bars {
     uint64_t key_full[2], key_empty[2], val_full[2], val_empty[2], score_full[2], weight_ready[2], query_ready, out_done;
 };
-struct Info {                                    // beside a token tile, one bit per token
-    uint32_t there[4], poison[4];
+struct __align__(16) Info {                      // beside a token tile, one bit per token
+    uint32_t there[4], poison[4];                // 16 bits from each fill warp
 };
 
 // ------------------------------------------------------------------------------- codes to values
@@ -233,202 +242,198 @@ __device__ __forceinline__ uint32_t piece_at(int t, int piece) {
     return (uint32_t)((piece >> 3) * (kTile * 128) + t * 128 + (((piece & 7) ^ (t & 7)) << 4));
 }
 
-// One fill warp's two runs of a tile, keys or values.
-template <int D, bool kKeys> struct Fill {
+// A fill warp's run of a tile: 16 tokens, keys and values.
+template <int D> struct Fill {
     static constexpr int kVec = D / 64;
-    uint4 v[2][kVec];
-    uint4 p[2][2];                               // keys: {.xy} of the tokens r and r + 8; values: tokens 2c, 2c+1 and 2c+8, 2c+9
-    bool ok[2];
-    __device__ __forceinline__ void load(const AttnArgs &a, const Walk &w, int step, int warp, const int (&id)[2], const int (&sub)[2],
-                                         long long head_bytes, int lane) {
+    uint4 k[kVec], v[kVec];
+    uint2 kp[2];                                 // scales and offsets of the tokens r and r + 8
+    uint4 vp[2];                                 // of the tokens 2c, 2c+1 and 2c+8, 2c+9
+    bool ok;
+    __device__ __forceinline__ void load(const uint8_t *run, bool there, int lane) {
+        ok = there;
+        if (!ok) return;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            ok[x] = id[x] >= 0 && id[x] < a.n_blocks;
-            if (!ok[x]) continue;
-            const uint8_t *run = a.cache + ((long long)id[x] * a.Hkv + w.h) * head_bytes + (long long)sub[x] * Kv4<D>::kRunBytes;
+        for (int i = 0; i < kVec; ++i) k[i] = ldg_stream(run + i * 512 + lane * 16);
+        const uint8_t *par = run + Kv4<D>::kParamOff;
+        kp[0] = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2));
+        kp[1] = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2) + 8);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) v[x][i] = ldg_stream(run + (kKeys ? 0 : Kv4<D>::kValueOff) + i * 512 + lane * 16);
-            const uint8_t *par = run + Kv4<D>::kParamOff;
-            if (kKeys) {
-                const uint2 lo = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2)), hi = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2) + 8);
-                p[x][0] = make_uint4(lo.x, lo.y, 0u, 0u);
-                p[x][1] = make_uint4(hi.x, hi.y, 0u, 0u);
-            } else {
-                p[x][0] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3));
-                p[x][1] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3) + 4);
-            }
-        }
+        for (int i = 0; i < kVec; ++i) v[i] = ldg_stream(run + Kv4<D>::kValueOff + i * 512 + lane * 16);
+        vp[0] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3));
+        vp[1] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3) + 4);
     }
-    // Into the tile at shared address `tile`; token0: place of the tile's first token in the request, kv: its length.
-    __device__ __forceinline__ void put(uint32_t tile, Info *info, int token0, int kv, int warp, int lane) const {
+    // Keys into the tile at shared address `tile`; `left`: tokens of the request from the run's first on.  Returns the run's
+    // tokens that are there (low half) and those of them that hold NaN (high half).
+    __device__ __forceinline__ uint32_t put_keys(uint32_t tile, int t0, int left, int lane) const {
         const int r = lane >> 2, c = lane & 3;
-        uint32_t there = 0u, poison = 0u;
+        uint32_t mark = 0u;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int t0 = (warp * 2 + x) * 16;
-            if (kKeys) {
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi) {
-                    const int t = t0 + r + 8 * hi;
-                    const bool live = ok[x] && token0 + t < kv, nan = live && (not_finite(p[x][hi].x) || not_finite(p[x][hi].y));
-                    there |= (live ? 1u : 0u) << (t & 31);
-                    poison |= (nan ? 1u : 0u) << (t & 31);
-                    const bool use = live && !nan;
-                    const uint32_t s2 = use ? both_lo(p[x][hi].x) : 0u, z2 = use ? both_hi(p[x][hi].x) : 0u;
-                    if (D == 128) {
-                        // the lanes c and c + 2 write to the same banks: the upper two take their words the other way round
-                        const uint4 u = v[x][D == 128 ? hi : 0];
-                        const bool swap = (c & 2) != 0;
-                        const uint32_t w0 = swap ? u.z : u.x, w1 = swap ? u.w : u.y, w2 = swap ? u.x : u.z, w3 = swap ? u.y : u.w;
-                        const int p0 = 4 * c + (swap ? 2 : 0), p2 = 4 * c + (swap ? 0 : 2);
-                        store16(tile + piece_at(t, p0), values8(w0, s2, z2));
-                        store16(tile + piece_at(t, p0 + 1), values8(w1, s2, z2));
-                        store16(tile + piece_at(t, p2), values8(w2, s2, z2));
-                        store16(tile + piece_at(t, p2 + 1), values8(w3, s2, z2));
-                    } else {
-                        const uint4 u = v[x][0];
-                        store16(tile + piece_at(t, 2 * c), values8(hi ? u.z : u.x, s2, z2));
-                        store16(tile + piece_at(t, 2 * c + 1), values8(hi ? u.w : u.y, s2, z2));
-                    }
-                }
+        for (int hi = 0; hi < 2; ++hi) {
+            const int t = r + 8 * hi;
+            const bool live = ok && t < left, nan = live && (not_finite(kp[hi].x) || not_finite(kp[hi].y));
+            mark |= ((live ? 1u : 0u) | (nan ? 0x10000u : 0u)) << t;
+            const bool use = live && !nan;
+            const uint32_t s2 = use ? both_lo(kp[hi].x) : 0u, z2 = use ? both_hi(kp[hi].x) : 0u;
+            if (D == 128) {
+                // the lanes c and c + 2 write to the same banks: the upper two take their words the other way round
+                const uint4 u = k[D == 128 ? hi : 0];
+                const bool swap = (c & 2) != 0;
+                const uint32_t w0 = swap ? u.z : u.x, w1 = swap ? u.w : u.y, w2 = swap ? u.x : u.z, w3 = swap ? u.y : u.w;
+                const int p0 = 4 * c + (swap ? 2 : 0), p2 = 4 * c + (swap ? 0 : 2);
+                store16(tile + piece_at(t0 + t, p0), values8(w0, s2, z2));
+                store16(tile + piece_at(t0 + t, p0 + 1), values8(w1, s2, z2));
+                store16(tile + piece_at(t0 + t, p2), values8(w2, s2, z2));
+                store16(tile + piece_at(t0 + t, p2 + 1), values8(w3, s2, z2));
             } else {
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int t = t0 + 2 * c + e + 8 * hi;
-                        const uint32_t par = e ? p[x][hi].w : p[x][hi].y;
-                        const bool use = ok[x] && token0 + t < kv && !not_finite(par);
-                        const uint32_t s2 = use ? both_lo(par) : 0u, z2 = use ? both_hi(par) : 0u;
-                        if (D == 128) {
-                            const uint4 u = v[x][D == 128 ? hi : 0];
-                            const uint32_t a0 = e ? u.z : u.x, a1 = e ? u.w : u.y;
-                            const bool swap = (r & 1) != 0;              // as above: odd r the other way round
-                            store16(tile + piece_at(t, 2 * r + (swap ? 1 : 0)), values8(swap ? a1 : a0, s2, z2));
-                            store16(tile + piece_at(t, 2 * r + (swap ? 0 : 1)), values8(swap ? a0 : a1, s2, z2));
-                        } else {
-                            const uint4 u = v[x][0];
-                            store16(tile + piece_at(t, r), values8(hi ? (e ? u.w : u.z) : (e ? u.y : u.x), s2, z2));
-                        }
-                    }
+                store16(tile + piece_at(t0 + t, 2 * c), values8(hi ? k[0].z : k[0].x, s2, z2));
+                store16(tile + piece_at(t0 + t, 2 * c + 1), values8(hi ? k[0].w : k[0].y, s2, z2));
             }
         }
-        if (kKeys) {
-            there = __reduce_or_sync(0xFFFFFFFFu, there);
-            poison = __reduce_or_sync(0xFFFFFFFFu, poison);
-            if (lane == 0) {
-                info->there[warp] = there;
-                info->poison[warp] = poison;
+        return __reduce_or_sync(0xFFFFFFFFu, mark);
+    }
+    __device__ __forceinline__ void put_values(uint32_t tile, int t0, int left, int lane) const {
+        const int r = lane >> 2, c = lane & 3;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = 2 * c + e + 8 * hi;
+                const uint32_t par = e ? vp[hi].w : vp[hi].y;
+                const bool use = ok && t < left && !not_finite(par);
+                const uint32_t s2 = use ? both_lo(par) : 0u, z2 = use ? both_hi(par) : 0u;
+                if (D == 128) {
+                    const uint4 u = v[D == 128 ? hi : 0];
+                    const uint32_t a0 = e ? u.z : u.x, a1 = e ? u.w : u.y;
+                    const bool swap = (r & 1) != 0;                  // as above: odd r the other way round
+                    store16(tile + piece_at(t0 + t, 2 * r + (swap ? 1 : 0)), values8(swap ? a1 : a0, s2, z2));
+                    store16(tile + piece_at(t0 + t, 2 * r + (swap ? 0 : 1)), values8(swap ? a0 : a1, s2, z2));
+                } else {
+                    store16(tile + piece_at(t0 + t, r), values8(hi ? (e ? v[0].w : v[0].z) : (e ? v[0].y : v[0].x), s2, z2));
+                }
             }
-        }
     }
 };
 
-template <int D, bool kKeys>
-__device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &line, uint32_t tiles, Info *info, const uint32_t (&full)[2],
-                                          const uint32_t (&empty)[2], volatile int *dead, int warp, int lane) {
+template <int D>
+__device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &line, uint32_t k_at, uint32_t v_at, Info *info, Bars *bars,
+                                          volatile int *dead, int warp, int lane) {
+    constexpr uint32_t kTileBytes = D * 2 * kTile;
     const int runs_page = a.page >> 4;
     const long long head_bytes = (long long)runs_page * Kv4<D>::kRunBytes;
+    const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
+    const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
     Walk w;
     w.enter(a, line);
     uint32_t n = 0u;                             // tiles filled so far
     while (w.next(a)) {
         const int32_t *table = a.table + (long long)w.rq.b * a.table_stride;
-        const int last_run = (w.rq.kv + 15) >> 4;
-        int id[2], sub[2];
-        auto lookup = [&](int step) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int run = step * kRunsTile + warp * 2 + x;
-                id[x] = -1;
-                sub[x] = 0;
-                if (step < w.step1 && run < last_run) {
-                    const int blk = run / runs_page;
-                    id[x] = __ldg(table + blk);
-                    sub[x] = run - blk * runs_page;
-                }
+        const uint8_t *head = a.cache + w.h * head_bytes;
+        const int step1 = w.step1, kv = w.rq.kv;
+        int step = w.step0, id = -1, sub = 0;
+        auto lookup = [&](int s) {
+            const int run = s * kRunsTile + warp;
+            id = -1;
+            if (s < step1 && run * 16 < kv) {
+                const int blk = run / runs_page;
+                id = __ldg(table + blk);
+                sub = run - blk * runs_page;
             }
         };
-        Fill<D, kKeys> f;
-        lookup(w.step0);
-        f.load(a, w, w.step0, warp, id, sub, head_bytes, lane);
-        lookup(w.step0 + 1);
-        for (int step = w.step0; step < w.step1; ++step, ++n) {
-            const Fill<D, kKeys> cur = f;
-            if (step + 1 < w.step1) f.load(a, w, step + 1, warp, id, sub, head_bytes, lane);
-            lookup(step + 2);
-            const int st = n & 1;
-            if (!warp_wait(empty[st], ((n >> 1) & 1) ^ 1u, dead)) return;
-            cur.put(tiles + st * (D * 2 * kTile), info + (n & 3), step * kTile, w.rq.kv, warp, lane);
+        Fill<D> f;
+        auto load = [&]() { f.load(head + id * (head_bytes * a.Hkv) + (long long)sub * Kv4<D>::kRunBytes, id >= 0 && id < a.n_blocks, lane); };
+        lookup(step);
+        load();
+        lookup(step + 1);
+#pragma unroll 1
+        for (; step < step1; ++step, ++n) {
+            const uint32_t st = n & 1u, parity = ((n >> 1) & 1u) ^ 1u;
+            const int t0 = warp * 16, left = kv - step * kTile - t0;
+            if (!warp_wait(key_empty + 8 * st, parity, dead)) return;
+            const uint32_t mark = f.put_keys(k_at + st * kTileBytes, t0, left, lane);
+            if (lane == 0) {
+                reinterpret_cast<uint16_t *>(info[n & 3].there)[warp] = (uint16_t)mark;
+                reinterpret_cast<uint16_t *>(info[n & 3].poison)[warp] = (uint16_t)(mark >> 16);
+            }
             fence_smem();
             __syncwarp();
-            if (lane == 0) bar_arrive(full[st]);
+            if (lane == 0) bar_arrive(key_full + 8 * st);
+            if (!warp_wait(val_empty + 8 * st, parity, dead)) return;
+            f.put_values(v_at + st * kTileBytes, t0, left, lane);
+            fence_smem();
+            __syncwarp();
+            if (lane == 0) bar_arrive(val_full + 8 * st);
+            // the next tile's loads are in flight while its stage is waited for
+            load();
+            lookup(step + 2);
         }
         w.leave(a);
     }
 }
 
 // ---------------------------------------------------------------------------------------- products
+// The whole warp walks, one lane issues.
 template <int D>
 __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, uint32_t tmem, uint32_t q_at, uint32_t k_at, uint32_t v_at,
                                              Bars *bars, volatile int *dead) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
     constexpr uint32_t kScore = kBf16Product | (uint32_t)(kTile >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
+    const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
+    const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
+    const uint32_t score_full = smem_u32(bars->score_full), weight_ready = smem_u32(bars->weight_ready);
+    const uint64_t q_desc = tile_desc(q_at, 16, 1024), k_desc = tile_desc(k_at, 16, 1024), v_desc = tile_desc(v_at, kTile * 128, 1024);
     Walk w;
     w.enter(a, line);
-    uint32_t seg = 0u, keys = 0u, vals = 0u, used[2] = {0u, 0u};
+    uint32_t seg = 0u, tiles = 0u, used0 = 0u, used1 = 0u;
     while (w.next(a)) {
-        const bool wide = w.wide();
-        const int n = (w.step1 - w.step0) * (wide ? 2 : 1);
-        if (!bar_wait(smem_u32(&bars->query_ready), seg & 1u, dead)) return;
-        uint32_t key_have = 0u, val_have = 0u;   // tiles of this segment that have been waited for
-        bool fine = true;
-        auto scores = [&](int i) {
-            const int slot = i & 1;
-            const uint32_t t = (uint32_t)(wide ? i >> 1 : i), st = (keys + t) & 1u;
-            if (key_have <= t) {
-                fine = fine && bar_wait(smem_u32(&bars->key_full[st]), ((keys + t) >> 1) & 1u, dead);
-                key_have = t + 1;
-                if (!fine) return;
-            }
+        const uint32_t wide = w.wide() ? 1u : 0u;
+        const int n = (w.step1 - w.step0) << wide;
+        if (!warp_wait(smem_u32(&bars->query_ready), seg & 1u, dead)) return;
+        // item i: slot i & 1; token tile i >> 1 if both slots share it, else i
+        auto scores = [&](uint32_t i) {
+            const uint32_t slot = i & 1u, t = tiles + (i >> wide), st = t & 1u;
+            if (!(wide & i) && !warp_wait(key_full + 8 * st, (t >> 1) & 1u, dead)) return false;
             fence_after();
-            const uint32_t qa = q_at + (wide ? slot : 0) * kTileBytes, ka = k_at + st * kTileBytes;
+            const uint64_t qa = q_desc + (wide & slot) * (kTileBytes >> 4), ka = k_desc + st * (kTileBytes >> 4);
+            const uint32_t d = tmem + slot * kTile;
+            if (elected()) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t by = (uint32_t)((ks >> 2) * (kTile * 128) + (ks & 3) * 32);
-                product_ss(tmem + slot * kTile, tile_desc(qa + by, 16, 1024), tile_desc(ka + by, 16, 1024), kScore, ks > 0);
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    constexpr uint32_t kBlock = kTile * 128 / 16;
+                    product_ss(d, qa + (ks >> 2) * kBlock + (ks & 3) * 2, ka + (ks >> 2) * kBlock + (ks & 3) * 2, kScore, ks > 0);
+                }
+                if (!wide || slot) commit_to(key_empty + 8 * st);
+                commit_to(score_full + 8 * slot);
             }
-            if (!wide || slot == 1) commit_to(smem_u32(&bars->key_empty[st]));
-            commit_to(smem_u32(&bars->score_full[slot]));
+            __syncwarp();
+            return true;
         };
-        auto outputs = [&](int i) {
-            const int slot = i & 1;
-            const uint32_t t = (uint32_t)(wide ? i >> 1 : i), st = (vals + t) & 1u;
-            fine = fine && bar_wait(smem_u32(&bars->weight_ready[slot]), used[slot] & 1u, dead);
-            ++used[slot];
-            if (fine && val_have <= t) {
-                fine = bar_wait(smem_u32(&bars->val_full[st]), ((vals + t) >> 1) & 1u, dead);
-                val_have = t + 1;
-            }
-            if (!fine) return;
+        auto outputs = [&](uint32_t i) {
+            const uint32_t slot = i & 1u, t = tiles + (i >> wide), st = t & 1u;
+            if (!warp_wait(weight_ready + 8 * slot, (slot ? used1 : used0) & 1u, dead)) return false;
+            if (slot) ++used1;
+            else ++used0;
+            if (!(wide & i) && !warp_wait(val_full + 8 * st, (t >> 1) & 1u, dead)) return false;
             fence_after();
-            const uint32_t va = v_at + st * kTileBytes;
+            const uint64_t va = v_desc + st * (kTileBytes >> 4);
+            const uint32_t d = tmem + 2 * kTile + slot * D, p = tmem + slot * kTile;
+            if (elected()) {
 #pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-                product_ts(tmem + 2 * kTile + slot * D, tmem + slot * kTile + ks * 8, tile_desc(va + ks * 2048, kTile * 128, 1024), kOut,
-                           i > 1 || ks > 0);
-            if (!wide || slot == 1) commit_to(smem_u32(&bars->val_empty[st]));
+                for (int ks = 0; ks < kTile / 16; ++ks) product_ts(d, p + ks * 8, va + ks * 128, kOut, i > 1u || ks > 0);
+                if (!wide || slot) commit_to(val_empty + 8 * st);
+            }
+            __syncwarp();
+            return true;
         };
-        scores(0);
-        if (n > 1 && fine) scores(1);
-        for (int i = 0; i < n && fine; ++i) {
-            outputs(i);
-            if (i + 2 < n && fine) scores(i + 2);
+        if (!scores(0u)) return;
+        if (n > 1 && !scores(1u)) return;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            if (!outputs(i)) return;
+            if (i + 2 < n && !scores(i + 2)) return;
         }
-        if (!fine) return;
-        commit_to(smem_u32(&bars->out_done));
-        keys += w.step1 - w.step0;
-        vals += w.step1 - w.step0;
+        if (elected()) commit_to(smem_u32(&bars->out_done));
+        __syncwarp();
+        tiles += w.step1 - w.step0;
         ++seg;
         w.leave(a);
     }
@@ -441,6 +446,22 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ void fma2(float &x, float &y, float s, float b) {      // both times s plus b
+    asm("{\n .reg .b64 v, m, a;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %2};\n mov.b64 a, {%3, %3};\n"
+        " fma.rn.f32x2 v, v, m, a;\n mov.b64 {%0, %1}, v;\n}" : "+f"(x), "+f"(y) : "f"(s), "f"(b));
+}
+__device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
+    asm("{\n .reg .b64 v, w;\n mov.b64 v, {%0, %1};\n mov.b64 w, {%2, %3};\n add.rn.f32x2 v, v, w;\n mov.b64 {%0, %1}, v;\n}"
+        : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ uint4 load_info(const uint32_t (&w)[4]) { return *reinterpret_cast<const uint4 *>(w); }
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int k) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
+
 template <int D>
 __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart &line, uint32_t tmem_all, uint32_t q_at, Bars *bars, const Info *info,
                                              float *s_m, float *s_l, volatile int *dead, int slot, int warp, int lane) {
@@ -448,7 +469,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
     const int me = warp * 32 + lane;                               // row of the slot's tile
     const uint32_t tmem = tmem_all + ((uint32_t)(warp * 32) << 16);
     const uint32_t s_at = tmem + slot * kTile, o_at = tmem + 2 * kTile + slot * D;
-    const float scale = fabsf(a.scale_log2);
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);          // a scale of 0 as one that no finite score is moved by
     Walk w;
     w.enter(a, line);
     uint32_t seg = 0u, used = 0u, tile_n = 0u;
@@ -488,14 +509,12 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             fence_after();
             const int t0 = (w.step0 + i) * kTile;
             const Info *inf = info + ((tile_n + i) & 3);
-            uint32_t hole = 0u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) hole |= ~inf->there[k] | inf->poison[k];
-            const bool part = __any_sync(0xFFFFFFFFu, hole != 0u || t0 + kTile > all);
-            // tokens of piece k (32 of them) that this row sees, and those of them that hold NaN
+            const uint4 there = load_info(inf->there), poison = load_info(inf->poison);
+            const bool part = t0 + kTile > all || ~(there.x & there.y & there.z & there.w) != 0u || (poison.x | poison.y | poison.z | poison.w) != 0u;
+            // tokens of piece k (32 of them) that this row sees
             auto seen = [&](int k) {
                 const int u0 = t0 + 32 * k;
-                uint32_t v = low_bits(lim - u0) & inf->there[k];
+                uint32_t v = low_bits(lim - u0) & word_of(there, k);
                 if (a.mask_kind == DSP_MASK_BITS && u0 + 32 > past && v) {
                     const int j0 = u0 - past;                      // new token that the piece's first place holds
                     const int w0 = j0 >> 5, sh = j0 & 31;
@@ -505,65 +524,72 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 }
                 return v;
             };
-            float x[32], top = -CUDART_INF_F;
+            if (__any_sync(0xFFFFFFFFu, part)) {                   // at the ends of what a tile's rows see: the scores once through the masks
+#pragma unroll 1
+                for (int k = 0; k < 4; ++k) {
+                    float x[32];
+                    tmem_load32(s_at + 32 * k, x);
+                    tmem_loaded(x);
+                    const uint32_t v = seen(k), nan = v & word_of(poison, k);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                tmem_load32(s_at + 32 * k, x);
-                tmem_loaded(x);
-                if (part) {
-                    const uint32_t v = seen(k);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = (v >> e) & 1u ? x[e] : -CUDART_INF_F;
+                    for (int e = 0; e < 32; ++e) {
+                        x[e] = (v >> e) & 1u ? x[e] : -CUDART_INF_F;
+                        if ((nan >> e) & 1u) x[e] = CUDART_NAN_F;
+                    }
+                    tmem_store32(s_at + 32 * k, x);
                 }
-#pragma unroll
-                for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+                tmem_stored();
             }
-            top *= scale;                                          // scale >= 0; 0 * -inf is NaN, which the next line takes for "no move"
-            bool move = top > (fresh ? -CUDART_INF_F : m + 8.0f) && top > m;
-            if (scale == 0.0f) move = fresh && m != 0.0f;
-            if (__any_sync(0xFFFFFFFFu, move)) {
-                const float to = move ? (scale == 0.0f ? 0.0f : top) : m;
-                const float keep = m == to ? 1.0f : ex2_approx(m - to);
+            // One pass over the scores against the maximum so far: weights (packed, held back), their sum, the scores' own
+            // maximum.  Only if that passes the one so far by 2^8 is the pass repeated against the new one; the scores are
+            // still there, since the weights that take their place are stored after it.
+            float sum;
+            uint32_t p[64];
+#pragma unroll 1
+            for (int again = 0; again < 2; ++again) {
+                const float base = m == -CUDART_INF_F ? 0.0f : m;
+                float tops[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F}, sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                float x[2][32];
+                tmem_load32(s_at, x[0]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float (&c)[32] = x[k & 1];
+                    tmem_loaded(c);
+                    if (k < 3) tmem_load32(s_at + 32 * (k + 1), x[(k + 1) & 1]);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], c[e], c[e + 1]);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        fma2(c[e], c[e + 1], scale, -base);
+                        c[e] = ex2_approx(c[e]);
+                        c[e + 1] = ex2_approx(c[e + 1]);
+                        add2(sums[e & 2], sums[(e & 2) + 1], c[e], c[e + 1]);
+                        p[k * 16 + (e >> 1)] = pack2(c[e], c[e + 1]);
+                    }
+                }
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
+                sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                const bool move = again == 0 && (top > m + 8.0f || (m == -CUDART_INF_F && top > m));
+                if (!__any_sync(0xFFFFFFFFu, move)) break;
+                const float to = move ? top : m, keep = m == to ? 1.0f : ex2_approx(m - to);
                 m = to;
                 l *= keep;
                 if (!fresh) {
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
-                        tmem_load32(o_at + 32 * k, x);
-                        tmem_loaded(x);
+                        float y[32];
+                        tmem_load32(o_at + 32 * k, y);
+                        tmem_loaded(y);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] *= keep;
-                        tmem_store32(o_at + 32 * k, x);
+                        for (int e = 0; e < 32; ++e) y[e] *= keep;
+                        tmem_store32(o_at + 32 * k, y);
                     }
                 }
             }
             fresh = false;
-            const float base = m == -CUDART_INF_F ? 0.0f : m;
+            l += sum;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                tmem_load32(s_at + 32 * k, x);
-                tmem_loaded(x);
-                if (part) {
-                    const uint32_t v = seen(k), nan = v & inf->poison[k];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float y = ex2_approx(fmaf(x[e], scale, -base));
-                        y = (v >> e) & 1u ? y : 0.0f;
-                        x[e] = (nan >> e) & 1u ? CUDART_NAN_F : y;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = ex2_approx(fmaf(x[e], scale, -base));
-                }
-                uint32_t p[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    l += x[2 * e];
-                    l += x[2 * e + 1];
-                    p[e] = pack2(x[2 * e], x[2 * e + 1]);
-                }
-                tmem_store16(s_at + 16 * k, p);
-            }
+            for (int k = 0; k < 4; ++k) tmem_store16(s_at + 16 * k, *reinterpret_cast<const uint32_t (*)[16]>(&p[16 * k]));
             tmem_stored();
             fence_before();
             __syncwarp();
@@ -663,8 +689,8 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         a.split[blockIdx.x].last_cta = -1;
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
-            bar_init(smem_u32(&s_bars.key_full[i]), kFillWarps / 2);
-            bar_init(smem_u32(&s_bars.val_full[i]), kFillWarps / 2);
+            bar_init(smem_u32(&s_bars.key_full[i]), kFillWarps);
+            bar_init(smem_u32(&s_bars.val_full[i]), kFillWarps);
             bar_init(smem_u32(&s_bars.key_empty[i]), 1);
             bar_init(smem_u32(&s_bars.val_empty[i]), 1);
             bar_init(smem_u32(&s_bars.score_full[i]), 1);
@@ -684,20 +710,14 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     const uint32_t tmem = s_tmem;
     if (s_line.begin < s_line.end) {
         if (warp < kSoftWarps) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kSoftRegs));
             softmax_role<D>(a, s_line, tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
         } else if (warp < kSoftWarps + kFillWarps) {
-            const int f = warp - kSoftWarps;
-            if (f < kFillWarps / 2) {
-                const uint32_t full[2] = {smem_u32(&s_bars.key_full[0]), smem_u32(&s_bars.key_full[1])};
-                const uint32_t empty[2] = {smem_u32(&s_bars.key_empty[0]), smem_u32(&s_bars.key_empty[1])};
-                fill_role<D, true>(a, s_line, k_at, s_info, full, empty, &s_dead, f, lane);
-            } else {
-                const uint32_t full[2] = {smem_u32(&s_bars.val_full[0]), smem_u32(&s_bars.val_full[1])};
-                const uint32_t empty[2] = {smem_u32(&s_bars.val_empty[0]), smem_u32(&s_bars.val_empty[1])};
-                fill_role<D, false>(a, s_line, v_at, s_info, full, empty, &s_dead, f - kFillWarps / 2, lane);
-            }
-        } else if (lane == 0) {
-            product_role<D>(a, s_line, tmem, q_at, k_at, v_at, &s_bars, &s_dead);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kFillRegs));
+            fill_role<D>(a, s_line, k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kProductRegs));
+            if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, tmem, q_at, k_at, v_at, &s_bars, &s_dead);
         }
     }
     __syncwarp();
