@@ -11,7 +11,7 @@
 //               back into the scores' columns as the second product's operand
 //   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
 //               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
-//   warp 16     one lane issues the products: S = Q K^T, O += P V (warps 17-19 only complete its warpgroup)
+//   warp 16     one lane issues the products: S = Q K^T, O += P V
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
@@ -28,11 +28,7 @@
 namespace dsp {
 namespace {
 
-constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 4) * 32;
-// Registers per thread: the block is launched with 96 for each of its 640 threads; of that sum the softmax
-// warpgroups take 144 (256 x 144), the fill warpgroups 72, the last one (whose first warp issues the products) 48.
-constexpr int kSoftRegs = 144, kFillRegs = 72, kProductRegs = 48;
-static_assert(256 * kSoftRegs + 256 * kFillRegs + 128 * kProductRegs <= kBlockThreads * 96, "register split");
+constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 1) * 32;
 constexpr int kTile = 128;                       // query rows of a slot, tokens of a tile
 constexpr int kRunsTile = kTile / 16;
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
@@ -248,15 +244,20 @@ template <int D> struct Fill {
     uint4 k[kVec], v[kVec];
     uint2 kp[2];                                 // scales and offsets of the tokens r and r + 8
     uint4 vp[2];                                 // of the tokens 2c, 2c+1 and 2c+8, 2c+9
-    bool ok;
-    __device__ __forceinline__ void load(const uint8_t *run, bool there, int lane) {
-        ok = there;
-        if (!ok) return;
+    bool ok_k, ok_v;
+    __device__ __forceinline__ void load_keys(const uint8_t *run, bool there, int lane) {
+        ok_k = there;
+        if (!there) return;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) k[i] = ldg_stream(run + i * 512 + lane * 16);
         const uint8_t *par = run + Kv4<D>::kParamOff;
         kp[0] = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2));
         kp[1] = __ldg(reinterpret_cast<const uint2 *>(par) + (lane >> 2) + 8);
+    }
+    __device__ __forceinline__ void load_values(const uint8_t *run, bool there, int lane) {
+        ok_v = there;
+        if (!there) return;
+        const uint8_t *par = run + Kv4<D>::kParamOff;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = ldg_stream(run + Kv4<D>::kValueOff + i * 512 + lane * 16);
         vp[0] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3));
@@ -270,7 +271,7 @@ template <int D> struct Fill {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const int t = r + 8 * hi;
-            const bool live = ok && t < left, nan = live && (not_finite(kp[hi].x) || not_finite(kp[hi].y));
+            const bool live = ok_k && t < left, nan = live && (not_finite(kp[hi].x) || not_finite(kp[hi].y));
             mark |= ((live ? 1u : 0u) | (nan ? 0x10000u : 0u)) << t;
             const bool use = live && !nan;
             const uint32_t s2 = use ? both_lo(kp[hi].x) : 0u, z2 = use ? both_hi(kp[hi].x) : 0u;
@@ -299,7 +300,7 @@ template <int D> struct Fill {
             for (int e = 0; e < 2; ++e) {
                 const int t = 2 * c + e + 8 * hi;
                 const uint32_t par = e ? vp[hi].w : vp[hi].y;
-                const bool use = ok && t < left && !not_finite(par);
+                const bool use = ok_v && t < left && !not_finite(par);
                 const uint32_t s2 = use ? both_lo(par) : 0u, z2 = use ? both_hi(par) : 0u;
                 if (D == 128) {
                     const uint4 u = v[D == 128 ? hi : 0];
@@ -340,9 +341,16 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             }
         };
         Fill<D> f;
-        auto load = [&]() { f.load(head + id * (head_bytes * a.Hkv) + (long long)sub * Kv4<D>::kRunBytes, id >= 0 && id < a.n_blocks, lane); };
+        const uint8_t *run = head;
+        bool there = false;
+        auto locate = [&]() {
+            there = id >= 0 && id < a.n_blocks;
+            run = head + id * (head_bytes * a.Hkv) + (long long)sub * Kv4<D>::kRunBytes;
+        };
         lookup(step);
-        load();
+        locate();
+        f.load_keys(run, there, lane);
+        f.load_values(run, there, lane);
         lookup(step + 1);
 #pragma unroll 1
         for (; step < step1; ++step, ++n) {
@@ -357,13 +365,15 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(key_full + 8 * st);
+            // the next tile's loads, keys and values each as soon as their registers are free
+            locate();
+            f.load_keys(run, there, lane);
             if (!warp_wait(val_empty + 8 * st, parity, dead)) return;
             f.put_values(v_at + st * kTileBytes, t0, left, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(val_full + 8 * st);
-            // the next tile's loads are in flight while its stage is waited for
-            load();
+            f.load_values(run, there, lane);
             lookup(step + 2);
         }
         w.leave(a);
@@ -540,56 +550,58 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 }
                 tmem_stored();
             }
-            // One pass over the scores against the maximum so far: weights (packed, held back), their sum, the scores' own
-            // maximum.  Only if that passes the one so far by 2^8 is the pass repeated against the new one; the scores are
-            // still there, since the weights that take their place are stored after it.
-            float sum;
-            uint32_t p[64];
-#pragma unroll 1
-            for (int again = 0; again < 2; ++again) {
-                const float base = m == -CUDART_INF_F ? 0.0f : m;
-                float tops[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F}, sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                float x[2][32];
-                tmem_load32(s_at, x[0]);
+            // the row's maximum; only where it passes the one so far by 2^8 does that move, and the output with it
+            float x[2][32];
+            float tops[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+            tmem_load32(s_at, x[0]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float (&c)[32] = x[k & 1];
-                    tmem_loaded(c);
-                    if (k < 3) tmem_load32(s_at + 32 * (k + 1), x[(k + 1) & 1]);
+            for (int k = 0; k < 4; ++k) {
+                float (&c)[32] = x[k & 1];
+                tmem_loaded(c);
+                tmem_load32(s_at + 32 * ((k + 1) & 3), x[(k + 1) & 1]);      // the last one is the first of the next pass
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], c[e], c[e + 1]);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        fma2(c[e], c[e + 1], scale, -base);
-                        c[e] = ex2_approx(c[e]);
-                        c[e + 1] = ex2_approx(c[e + 1]);
-                        add2(sums[e & 2], sums[(e & 2) + 1], c[e], c[e + 1]);
-                        p[k * 16 + (e >> 1)] = pack2(c[e], c[e + 1]);
-                    }
-                }
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
-                sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-                const bool move = again == 0 && (top > m + 8.0f || (m == -CUDART_INF_F && top > m));
-                if (!__any_sync(0xFFFFFFFFu, move)) break;
+                for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], c[e], c[e + 1]);
+            }
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
+            const bool move = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
+            if (__any_sync(0xFFFFFFFFu, move)) {
                 const float to = move ? top : m, keep = m == to ? 1.0f : ex2_approx(m - to);
                 m = to;
                 l *= keep;
                 if (!fresh) {
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
-                        float y[32];
-                        tmem_load32(o_at + 32 * k, y);
-                        tmem_loaded(y);
+                        tmem_loaded(x[1]);
+                        tmem_load32(o_at + 32 * k, x[1]);
+                        tmem_loaded(x[1]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] *= keep;
-                        tmem_store32(o_at + 32 * k, y);
+                        for (int e = 0; e < 32; ++e) x[1][e] *= keep;
+                        tmem_store32(o_at + 32 * k, x[1]);
                     }
                 }
             }
             fresh = false;
-            l += sum;
+            const float base = m == -CUDART_INF_F ? 0.0f : m;
+            float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) tmem_store16(s_at + 16 * k, *reinterpret_cast<const uint32_t (*)[16]>(&p[16 * k]));
+            for (int k = 0; k < 4; ++k) {
+                float (&c)[32] = x[k & 1];
+                tmem_loaded(c);
+                if (k < 3) tmem_load32(s_at + 32 * (k + 1), x[(k + 1) & 1]);
+                uint32_t p[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    fma2(c[e], c[e + 1], scale, -base);
+                    c[e] = ex2_approx(c[e]);
+                    c[e + 1] = ex2_approx(c[e + 1]);
+                    add2(sums[e & 2], sums[(e & 2) + 1], c[e], c[e + 1]);
+                    p[e >> 1] = pack2(c[e], c[e + 1]);
+                }
+                // weights over scores that have been read: piece k's end where piece k + 1 begins at the latest, and that one is in registers
+                if (k < 3) tmem_loaded(x[(k + 1) & 1]);
+                tmem_store16(s_at + 16 * k, p);
+            }
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_stored();
             fence_before();
             __syncwarp();
@@ -710,13 +722,10 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     const uint32_t tmem = s_tmem;
     if (s_line.begin < s_line.end) {
         if (warp < kSoftWarps) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kSoftRegs));
             softmax_role<D>(a, s_line, tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
         } else if (warp < kSoftWarps + kFillWarps) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kFillRegs));
             fill_role<D>(a, s_line, k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kProductRegs));
             if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, tmem, q_at, k_at, v_at, &s_bars, &s_dead);
         }
     }
