@@ -11,7 +11,7 @@
 //               back into the scores' columns as the second product's operand
 //   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
 //               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
-//   warp 16     one lane issues the products: S = Q K^T, O += P V
+//   warp 16     one lane issues the products: S = Q K^T, O += P V (warps 17-19 only complete its warpgroup)
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
@@ -28,7 +28,12 @@
 namespace dsp {
 namespace {
 
-constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 1) * 32;
+constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 4) * 32;
+// Registers per thread: the block is launched with 96 for each of its 640 threads; of that sum the softmax
+// warpgroups take 152 each thread (a whole row of scores), the fill warpgroups 64, the last one, whose
+// first warp issues the products, 48.
+constexpr int kLaunchRegs = 96, kSoftRegs = 152, kFillRegs = 64, kProductRegs = 48;
+static_assert(256 * kSoftRegs + 256 * kFillRegs + 128 * kProductRegs <= kBlockThreads * kLaunchRegs, "register split");
 constexpr int kTile = 128;                       // query rows of a slot, tokens of a tile
 constexpr int kRunsTile = kTile / 16;
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
@@ -102,10 +107,8 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const float (&x)[32]) 
                     "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]),
                     "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]), "f"(x[31]) : "memory");
 }
-__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 :: "r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]),
-                    "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
+__device__ __forceinline__ void tmem_store4(uint32_t at, const uint32_t (&x)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
 }
 // The registers pass through the wait, so that nothing uses them before it.
 __device__ __forceinline__ void tmem_loaded(float (&x)[32]) {
@@ -115,12 +118,23 @@ __device__ __forceinline__ void tmem_loaded(float (&x)[32]) {
                    "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]),
                    "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]) , "+f"(x[30]), "+f"(x[31]) :: "memory");
 }
+// Eight columns, waited for.
+__device__ __forceinline__ void tmem_load8(uint32_t at, float (&x)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n tcgen05.wait::ld.sync.aligned;"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const float (&x)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void pair_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 
 // ------------------------------------------------------------------------------- cut of the work
-// A request's units: tiles of 256 rows, for each tile its key heads.  Lengths are counted in tile
-// products (128 rows x 128 tokens): 2 for each token tile of a unit with more than 128 rows, else 1.
+// A request's units: tiles of 256 rows, for each tile its key heads.  A token tile of a unit with more
+// than 128 rows counts kWide on the line, of one with fewer kNarrow: it has half the products but the
+// same keys and values to expand (measured: 4350 against 5700 clocks).
+constexpr int kWide = 4, kNarrow = 3;
 struct BlockRequest {
     int b, n_new, kv, rows, row0, group, tiles;
     bool causal;
@@ -132,7 +146,7 @@ struct BlockRequest {
         causal = a.mask_kind == DSP_MASK_CAUSAL;
     }
     __device__ __forceinline__ int rows_of(int tile) const { return min(rows - tile * 2 * kTile, 2 * kTile); }
-    __device__ __forceinline__ int weight(int tile) const { return rows_of(tile) > kTile ? 2 : 1; }
+    __device__ __forceinline__ int weight(int tile) const { return rows_of(tile) > kTile ? kWide : kNarrow; }
     __device__ __forceinline__ int steps(int tile) const {
         const int last = (tile * 2 * kTile + rows_of(tile) - 1) / group;
         const int end = causal ? min(kv, kv - n_new + last + 1) : kv;
@@ -141,7 +155,7 @@ struct BlockRequest {
     __device__ __forceinline__ long long length(int Hkv) const {
         if (!causal) {
             const long long whole = rows / (2 * kTile), rest = rows - whole * 2 * kTile, n = max(1, (kv + kTile - 1) / kTile);
-            return Hkv * n * (2 * whole + (rest > kTile ? 2 : rest > 0 ? 1 : 0));
+            return Hkv * n * (kWide * whole + (rest > kTile ? kWide : rest > 0 ? kNarrow : 0));
         }
         long long n = 0;
         for (int t = 0; t < tiles; ++t) n += (long long)steps(t) * weight(t);
@@ -199,9 +213,25 @@ struct Walk {
             rq.load(a, rq.b + 1, 0, 0);
         } while (rq.tiles == 0);
     }
-    __device__ __forceinline__ bool wide() const { return weight == 2; }
+    __device__ __forceinline__ bool wide() const { return weight == kWide; }
     __device__ __forceinline__ int row_first() const { return tile * 2 * kTile; }
 };
+// Every warp has a walk of its own in shared memory (its state is not worth registers); lane 0 takes the steps.
+__device__ __forceinline__ void walk_enter(Walk &w, const AttnArgs &a, const LineStart &s, int lane) {
+    if (lane == 0) w.enter(a, s);
+    __syncwarp();
+}
+__device__ __forceinline__ bool walk_next(Walk &w, const AttnArgs &a, int lane) {
+    __syncwarp();
+    bool more = false;
+    if (lane == 0) more = w.next(a);
+    __syncwarp();
+    return __shfl_sync(0xFFFFFFFFu, more, 0);
+}
+__device__ __forceinline__ void walk_leave(Walk &w, const AttnArgs &a, int lane) {
+    __syncwarp();
+    if (lane == 0) w.leave(a);
+}
 
 struct Bars {
     uint64_t key_full[2], key_empty[2], val_full[2], val_empty[2], score_full[2], weight_ready[2], query_ready, out_done;
@@ -316,17 +346,16 @@ template <int D> struct Fill {
 };
 
 template <int D>
-__device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &line, uint32_t k_at, uint32_t v_at, Info *info, Bars *bars,
+__device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t k_at, uint32_t v_at, Info *info, Bars *bars,
                                           volatile int *dead, int warp, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
     const int runs_page = a.page >> 4;
     const long long head_bytes = (long long)runs_page * Kv4<D>::kRunBytes;
     const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
     const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
-    Walk w;
-    w.enter(a, line);
+    walk_enter(w, a, line, lane);
     uint32_t n = 0u;                             // tiles filled so far
-    while (w.next(a)) {
+    while (walk_next(w, a, lane)) {
         const int32_t *table = a.table + (long long)w.rq.b * a.table_stride;
         const uint8_t *head = a.cache + w.h * head_bytes;
         const int step1 = w.step1, kv = w.rq.kv;
@@ -376,27 +405,26 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             f.load_values(run, there, lane);
             lookup(step + 2);
         }
-        w.leave(a);
+        walk_leave(w, a, lane);
     }
 }
 
 // ---------------------------------------------------------------------------------------- products
 // The whole warp walks, one lane issues.
 template <int D>
-__device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, uint32_t tmem, uint32_t q_at, uint32_t k_at, uint32_t v_at,
-                                             Bars *bars, volatile int *dead) {
+__device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem, uint32_t q_at, uint32_t k_at,
+                                             uint32_t v_at, Bars *bars, volatile int *dead, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
     constexpr uint32_t kScore = kBf16Product | (uint32_t)(kTile >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
     const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
     const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
     const uint32_t score_full = smem_u32(bars->score_full), weight_ready = smem_u32(bars->weight_ready);
     const uint64_t q_desc = tile_desc(q_at, 16, 1024), k_desc = tile_desc(k_at, 16, 1024), v_desc = tile_desc(v_at, kTile * 128, 1024);
-    Walk w;
-    w.enter(a, line);
+    walk_enter(w, a, line, lane);
     uint32_t seg = 0u, tiles = 0u, used0 = 0u, used1 = 0u;
-    while (w.next(a)) {
+    while (walk_next(w, a, lane)) {
         const uint32_t wide = w.wide() ? 1u : 0u;
-        const int n = (w.step1 - w.step0) << wide;
+        const int n_tiles = w.step1 - w.step0, n = n_tiles << wide;
         if (!warp_wait(smem_u32(&bars->query_ready), seg & 1u, dead)) return;
         // item i: slot i & 1; token tile i >> 1 if both slots share it, else i
         auto scores = [&](uint32_t i) {
@@ -443,9 +471,9 @@ __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart 
         }
         if (elected()) commit_to(smem_u32(&bars->out_done));
         __syncwarp();
-        tiles += w.step1 - w.step0;
+        tiles += n_tiles;
         ++seg;
-        w.leave(a);
+        walk_leave(w, a, lane);
     }
 }
 
@@ -473,19 +501,18 @@ __device__ __forceinline__ uint4 load_info(const uint32_t (&w)[4]) { return *rei
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int k) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
 
 template <int D>
-__device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart &line, uint32_t tmem_all, uint32_t q_at, Bars *bars, const Info *info,
-                                             float *s_m, float *s_l, volatile int *dead, int slot, int warp, int lane) {
+__device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem_all, uint32_t q_at, Bars *bars,
+                                             const Info *info, float *s_m, float *s_l, volatile int *dead, int slot, int warp, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
     const int me = warp * 32 + lane;                               // row of the slot's tile
     const uint32_t tmem = tmem_all + ((uint32_t)(warp * 32) << 16);
     const uint32_t s_at = tmem + slot * kTile, o_at = tmem + 2 * kTile + slot * D;
     const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);          // a scale of 0 as one that no finite score is moved by
-    Walk w;
-    w.enter(a, line);
+    walk_enter(w, a, line, lane);
     uint32_t seg = 0u, used = 0u, tile_n = 0u;
-    while (w.next(a)) {
+    while (walk_next(w, a, lane)) {
         const bool wide = w.wide();
-        const int n = w.step1 - w.step0;
+        const int step0 = w.step0, n = w.step1 - step0;
         const int row = w.row_first() + (wide ? slot * kTile : 0) + me, qi = row / a.group;
         const bool live = row < w.rq.rows;
         const long long token = w.rq.row0 + qi;
@@ -507,8 +534,10 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         __syncwarp();
         if (lane == 0) bar_arrive(smem_u32(&bars->query_ready));
         const int past = w.rq.kv - w.rq.n_new;
-        const int lim = !live ? 0 : a.mask_kind == DSP_MASK_CAUSAL ? min(w.rq.kv, past + qi + 1) : w.rq.kv;
-        const int all = a.mask_kind == DSP_MASK_BITS ? min(past, lim) : lim;      // tokens below are seen without a look at the bits
+        // rows beyond the unit's see everything: what they hold is not used, and their tiles need no masks
+        const int lim = !live ? 0x7FFFFFFF : a.mask_kind == DSP_MASK_CAUSAL ? min(w.rq.kv, past + qi + 1) : w.rq.kv;
+        const int all = live && a.mask_kind == DSP_MASK_BITS ? min(past, lim) : lim;      // tokens below are seen without a look at the bits
+        const bool some = __any_sync(0xFFFFFFFFu, live);
         const uint32_t *bits = a.bits ? a.bits + token * a.words : nullptr;
         float m = -CUDART_INF_F, l = 0.0f;
         bool fresh = true;                                         // nothing of this slot is in its output yet
@@ -517,15 +546,19 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             if (!warp_wait(smem_u32(&bars->score_full[slot]), used & 1u, dead)) break;
             ++used;
             fence_after();
-            const int t0 = (w.step0 + i) * kTile;
+            if (!some) {                                           // a warp without rows: its part of the tile stays what it is
+                if (lane == 0) bar_arrive(smem_u32(&bars->weight_ready[slot]));
+                continue;
+            }
+            const int t0 = (step0 + i) * kTile;
             const Info *inf = info + ((tile_n + i) & 3);
             const uint4 there = load_info(inf->there), poison = load_info(inf->poison);
-            const bool part = t0 + kTile > all || ~(there.x & there.y & there.z & there.w) != 0u || (poison.x | poison.y | poison.z | poison.w) != 0u;
+            const bool part = live && (t0 + kTile > all || ~(there.x & there.y & there.z & there.w) != 0u || (poison.x | poison.y | poison.z | poison.w) != 0u);
             // tokens of piece k (32 of them) that this row sees
             auto seen = [&](int k) {
                 const int u0 = t0 + 32 * k;
                 uint32_t v = low_bits(lim - u0) & word_of(there, k);
-                if (a.mask_kind == DSP_MASK_BITS && u0 + 32 > past && v) {
+                if (live && a.mask_kind == DSP_MASK_BITS && u0 + 32 > past && v) {
                     const int j0 = u0 - past;                      // new token that the piece's first place holds
                     const int w0 = j0 >> 5, sh = j0 & 31;
                     const uint32_t lo = w0 >= 0 && w0 < a.words ? __ldg(bits + w0) : w0 < 0 ? 0xFFFFFFFFu : 0u;
@@ -551,16 +584,15 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 tmem_stored();
             }
             // the row's maximum; only where it passes the one so far by 2^8 does that move, and the output with it
-            float x[2][32];
+            float x[4][32];
             float tops[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-            tmem_load32(s_at, x[0]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tmem_load32(s_at + 32 * k, x[k]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float (&c)[32] = x[k & 1];
-                tmem_loaded(c);
-                tmem_load32(s_at + 32 * ((k + 1) & 3), x[(k + 1) & 1]);      // the last one is the first of the next pass
+                tmem_loaded(x[k]);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], c[e], c[e + 1]);
+                for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], x[k][e], x[k][e + 1]);
             }
             const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
             const bool move = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
@@ -570,13 +602,12 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 l *= keep;
                 if (!fresh) {
 #pragma unroll 1
-                    for (int k = 0; k < D / 32; ++k) {
-                        tmem_loaded(x[1]);
-                        tmem_load32(o_at + 32 * k, x[1]);
-                        tmem_loaded(x[1]);
+                    for (int k = 0; k < D / 8; ++k) {
+                        float y[8];
+                        tmem_load8(o_at + 8 * k, y);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[1][e] *= keep;
-                        tmem_store32(o_at + 32 * k, x[1]);
+                        for (int e = 0; e < 8; ++e) y[e] *= keep;
+                        tmem_store8(o_at + 8 * k, y);
                     }
                 }
             }
@@ -585,21 +616,20 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float (&c)[32] = x[k & 1];
-                tmem_loaded(c);
-                if (k < 3) tmem_load32(s_at + 32 * (k + 1), x[(k + 1) & 1]);
-                uint32_t p[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    fma2(c[e], c[e + 1], scale, -base);
-                    c[e] = ex2_approx(c[e]);
-                    c[e + 1] = ex2_approx(c[e + 1]);
-                    add2(sums[e & 2], sums[(e & 2) + 1], c[e], c[e + 1]);
-                    p[e >> 1] = pack2(c[e], c[e + 1]);
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t p[4];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        float a0 = x[k][8 * h + e], a1 = x[k][8 * h + e + 1];
+                        fma2(a0, a1, scale, -base);
+                        a0 = ex2_approx(a0);
+                        a1 = ex2_approx(a1);
+                        add2(sums[e & 2], sums[(e & 2) + 1], a0, a1);
+                        p[e >> 1] = pack2(a0, a1);
+                    }
+                    tmem_store4(s_at + 16 * k + 4 * h, p);         // over scores that are in registers
                 }
-                // weights over scores that have been read: piece k's end where piece k + 1 begins at the latest, and that one is in registers
-                if (k < 3) tmem_loaded(x[(k + 1) & 1]);
-                tmem_store16(s_at + 16 * k, p);
             }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_stored();
@@ -679,7 +709,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         fence_before();
         if (!wide) pair_barrier(1, kSoftWarps * 32);              // slot 1's output has been read, its sums too
         ++seg;
-        w.leave(a);
+        walk_leave(w, a, lane);
     }
 }
 
@@ -693,6 +723,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint32_t s_tmem;
+    __shared__ Walk s_walk[kSoftWarps + kFillWarps + 1];
     __shared__ int s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(s_raw) + 1023u) & ~1023u;
@@ -717,16 +748,19 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         fence_before();
     }
-    enter_line<BlockRequest>(a, 0, 0, 2, s_scan, &s_line);         // ends with a barrier of the CTA
+    enter_line<BlockRequest>(a, 0, 0, kWide, s_scan, &s_line);         // ends with a barrier of the CTA
     fence_after();
     const uint32_t tmem = s_tmem;
     if (s_line.begin < s_line.end) {
         if (warp < kSoftWarps) {
-            softmax_role<D>(a, s_line, tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kSoftRegs));
+            softmax_role<D>(a, s_line, s_walk[warp], tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
         } else if (warp < kSoftWarps + kFillWarps) {
-            fill_role<D>(a, s_line, k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kFillRegs));
+            fill_role<D>(a, s_line, s_walk[warp], k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
         } else {
-            if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, tmem, q_at, k_at, v_at, &s_bars, &s_dead);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kProductRegs));
+            if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, &s_dead, lane);
         }
     }
     __syncwarp();
