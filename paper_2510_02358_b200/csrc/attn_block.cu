@@ -4,14 +4,15 @@
 // One CTA per SM.  A unit is up to 256 query rows of one key head against a stretch of the cache; its
 // rows are two tiles of 128 that share every key and value tile, or, with at most 128 rows, one tile
 // whose even and odd token tiles go to the two halves of the CTA.  Either way there are two slots, each
-// with 128 x 128 scores and a 128 x D output in tensor memory (512 columns together), so that the tensor
-// cores work on one slot while the other's scores are exponentiated.
+// with a 128 x D output in tensor memory and two buffers of 128 x 64 scores (512 columns together): the
+// tensor cores form the scores of a slot's next half tile while its last one is exponentiated, so the
+// softmax warps, which are the slowest part, need not wait for them.
 //
 //   warps 0-7   softmax, four per slot, one thread per query row: maximum, exponentials, weights in bf16
 //               back into the scores' columns as the second product's operand
 //   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
 //               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
-//   warp 16     one lane issues the products: S = Q K^T, O += P V (warps 17-19 only complete its warpgroup)
+//   warp 16     one lane issues the products: S = Q K^T, O += P V
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
@@ -28,13 +29,9 @@
 namespace dsp {
 namespace {
 
-constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 4) * 32;
-// Registers per thread: the block is launched with 96 for each of its 640 threads; of that sum the softmax
-// warpgroups take 152 each thread (a whole row of scores), the fill warpgroups 64, the last one, whose
-// first warp issues the products, 48.
-constexpr int kLaunchRegs = 96, kSoftRegs = 152, kFillRegs = 64, kProductRegs = 48;
-static_assert(256 * kSoftRegs + 256 * kFillRegs + 128 * kProductRegs <= kBlockThreads * kLaunchRegs, "register split");
+constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 1) * 32;
 constexpr int kTile = 128;                       // query rows of a slot, tokens of a tile
+constexpr int kHalf = kTile / 2;                 // tokens whose scores are formed and exponentiated at once
 constexpr int kRunsTile = kTile / 16;
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
 
@@ -66,13 +63,17 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void commit_to(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
-}
-__device__ __forceinline__ bool elected() {
+// Products and commits are issued by the lane whose `lead` is set; the rest of the warp passes by.  The lane is picked by a
+// predicate and not by a branch: in a branch that only some lanes take, every operand has to be moved to the uniform registers
+// that these instructions want, one at a time (measured: 120 clocks per product instead of 40).
+__device__ __forceinline__ uint32_t elected() {
     uint32_t ok;
     asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
-    return ok != 0u;
+    return ok;
+}
+__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t lead) {
+    asm volatile("{\n .reg .pred e;\n setp.ne.u32 e, %1, 0;\n"
+                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" :: "r"(bar), "r"(lead) : "memory");
 }
 // Operand tiles lie in shared memory as blocks of 64 channels: [block][row][128 bytes], the 16-byte
 // pieces of a row exchanged by its number modulo 8 (the 128-byte swizzle).  The same bytes serve as an
@@ -82,13 +83,15 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead_bytes
            (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 constexpr uint32_t kBf16Product = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kTile >> 4) << 24;      // fp32 sums, bf16 operands, 128 rows
-__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, uint32_t lead) {
+    asm volatile("{\n .reg .pred p, e;\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 e, %5, 0;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add, uint32_t lead) {
+    asm volatile("{\n .reg .pred p, e;\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 e, %5, 0;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t at, float (&x)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -98,14 +101,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, float (&x)[32]) {
                    "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]),
                    "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
                  : "r"(at) : "memory");
-}
-__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&x)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 :: "r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]),
-                    "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]),
-                    "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]),
-                    "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]), "f"(x[31]) : "memory");
 }
 __device__ __forceinline__ void tmem_store4(uint32_t at, const uint32_t (&x)[4]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
@@ -234,7 +229,10 @@ __device__ __forceinline__ void walk_leave(Walk &w, const AttnArgs &a, int lane)
 }
 
 struct Bars {
-    uint64_t key_full[2], key_empty[2], val_full[2], val_empty[2], score_full[2], weight_ready[2], query_ready, out_done;
+    uint64_t key_full[2], key_empty[2], val_full[2], val_empty[2];
+    uint64_t score_full[4], weight_ready[4];     // [slot * 2 + buffer]
+    uint64_t out_free[2];                        // [slot] its last product with the weights has ended
+    uint64_t query_ready, out_done;
 };
 struct __align__(16) Info {                      // beside a token tile, one bit per token
     uint32_t there[4], poison[4];                // 16 bits from each fill warp
@@ -376,34 +374,49 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             there = id >= 0 && id < a.n_blocks;
             run = head + id * (head_bytes * a.Hkv) + (long long)sub * Kv4<D>::kRunBytes;
         };
+        const int t0 = warp * 16;
+        // keys of tile m, the segment's step s; false: the wait ran out
+        auto keys = [&](uint32_t m, int s) {
+            const uint32_t st = m & 1u;
+            if (!warp_wait(key_empty + 8 * st, ((m >> 1) & 1u) ^ 1u, dead)) return false;
+            const uint32_t mark = f.put_keys(k_at + st * kTileBytes, t0, kv - s * kTile - t0, lane);
+            if (lane == 0) {
+                reinterpret_cast<uint16_t *>(info[m & 3].there)[warp] = (uint16_t)mark;
+                reinterpret_cast<uint16_t *>(info[m & 3].poison)[warp] = (uint16_t)(mark >> 16);
+            }
+            fence_smem();
+            __syncwarp();
+            if (lane == 0) bar_arrive(key_full + 8 * st);
+            return true;
+        };
         lookup(step);
         locate();
         f.load_keys(run, there, lane);
         f.load_values(run, there, lane);
         lookup(step + 1);
+        if (!keys(n, step)) return;
+        locate();
+        f.load_keys(run, there, lane);
+        lookup(step + 2);
+        // Keys stay a tile ahead of the values: the products ask for the scores of up to two tiles on before they are done with
+        // a tile's values.  Each load is issued as soon as its registers are free.
 #pragma unroll 1
         for (; step < step1; ++step, ++n) {
-            const uint32_t st = n & 1u, parity = ((n >> 1) & 1u) ^ 1u;
-            const int t0 = warp * 16, left = kv - step * kTile - t0;
-            if (!warp_wait(key_empty + 8 * st, parity, dead)) return;
-            const uint32_t mark = f.put_keys(k_at + st * kTileBytes, t0, left, lane);
-            if (lane == 0) {
-                reinterpret_cast<uint16_t *>(info[n & 3].there)[warp] = (uint16_t)mark;
-                reinterpret_cast<uint16_t *>(info[n & 3].poison)[warp] = (uint16_t)(mark >> 16);
+            const uint8_t *val_run = run;
+            const bool val_there = there;
+            if (step + 1 < step1) {
+                if (!keys(n + 1, step + 1)) return;
+                locate();
+                f.load_keys(run, there, lane);
+                lookup(step + 3);
             }
-            fence_smem();
-            __syncwarp();
-            if (lane == 0) bar_arrive(key_full + 8 * st);
-            // the next tile's loads, keys and values each as soon as their registers are free
-            locate();
-            f.load_keys(run, there, lane);
-            if (!warp_wait(val_empty + 8 * st, parity, dead)) return;
-            f.put_values(v_at + st * kTileBytes, t0, left, lane);
+            const uint32_t st = n & 1u;
+            if (!warp_wait(val_empty + 8 * st, ((n >> 1) & 1u) ^ 1u, dead)) return;
+            f.put_values(v_at + st * kTileBytes, t0, kv - step * kTile - t0, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(val_full + 8 * st);
-            f.load_values(run, there, lane);
-            lookup(step + 2);
+            f.load_values(val_run, val_there, lane);
         }
         walk_leave(w, a, lane);
     }
@@ -415,63 +428,64 @@ template <int D>
 __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem, uint32_t q_at, uint32_t k_at,
                                              uint32_t v_at, Bars *bars, volatile int *dead, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
-    constexpr uint32_t kScore = kBf16Product | (uint32_t)(kTile >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
+    constexpr uint32_t kScore = kBf16Product | (uint32_t)(kHalf >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
     const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
     const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
     const uint32_t score_full = smem_u32(bars->score_full), weight_ready = smem_u32(bars->weight_ready);
+    const uint32_t out_free = smem_u32(bars->out_free);
     const uint64_t q_desc = tile_desc(q_at, 16, 1024), k_desc = tile_desc(k_at, 16, 1024), v_desc = tile_desc(v_at, kTile * 128, 1024);
     walk_enter(w, a, line, lane);
-    uint32_t seg = 0u, tiles = 0u, used0 = 0u, used1 = 0u;
+    const uint32_t lead = elected();
+    uint32_t seg = 0u, tiles = 0u, uses[2] = {0u, 0u};
     while (walk_next(w, a, lane)) {
-        const uint32_t wide = w.wide() ? 1u : 0u;
-        const int n_tiles = w.step1 - w.step0, n = n_tiles << wide;
+        // the same in every lane, which the compiler shall know
+        const uint32_t wide = __shfl_sync(0xFFFFFFFFu, w.wide() ? 1u : 0u, 0), n = __shfl_sync(0xFFFFFFFFu, (uint32_t)(w.step1 - w.step0), 0);
+        // token tiles of each slot in this segment
+        const uint32_t of0 = wide ? n : (n + 1) >> 1, of1 = wide ? n : n >> 1;
         if (!warp_wait(smem_u32(&bars->query_ready), seg & 1u, dead)) return;
-        // item i: slot i & 1; token tile i >> 1 if both slots share it, else i
+        // item i: slot i & 1, its half tile i >> 1; the slots take turns
+        auto exists = [&](uint32_t i) { return (i >> 2) < ((i & 1u) ? of1 : of0); };
         auto scores = [&](uint32_t i) {
-            const uint32_t slot = i & 1u, t = tiles + (i >> wide), st = t & 1u;
-            if (!(wide & i) && !warp_wait(key_full + 8 * st, (t >> 1) & 1u, dead)) return false;
+            const uint32_t slot = i & 1u, buf = (i >> 1) & 1u, t = tiles + (wide ? i >> 2 : 2u * (i >> 2) + slot), st = t & 1u;
+            if (buf == 0u && !(wide & slot) && !warp_wait(key_full + 8 * st, (t >> 1) & 1u, dead)) return false;
             fence_after();
-            const uint64_t qa = q_desc + (wide & slot) * (kTileBytes >> 4), ka = k_desc + st * (kTileBytes >> 4);
-            const uint32_t d = tmem + slot * kTile;
-            if (elected()) {
+            const uint64_t qa = q_desc + (wide & slot) * (kTileBytes >> 4), ka = k_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
+            const uint32_t d = tmem + slot * kTile + buf * kHalf;
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    constexpr uint32_t kBlock = kTile * 128 / 16;
-                    product_ss(d, qa + (ks >> 2) * kBlock + (ks & 3) * 2, ka + (ks >> 2) * kBlock + (ks & 3) * 2, kScore, ks > 0);
-                }
-                if (!wide || slot) commit_to(key_empty + 8 * st);
-                commit_to(score_full + 8 * slot);
+            for (int ks = 0; ks < D / 16; ++ks) {
+                constexpr uint32_t kBlock = kTile * 128 / 16;
+                product_ss(d, qa + (ks >> 2) * kBlock + (ks & 3) * 2, ka + (ks >> 2) * kBlock + (ks & 3) * 2, kScore, ks > 0, lead);
             }
-            __syncwarp();
+            if (buf && (!wide || slot)) commit_to(key_empty + 8 * st, lead);
+            commit_to(score_full + 8 * (slot * 2 + buf), lead);
             return true;
         };
         auto outputs = [&](uint32_t i) {
-            const uint32_t slot = i & 1u, t = tiles + (i >> wide), st = t & 1u;
-            if (!warp_wait(weight_ready + 8 * slot, (slot ? used1 : used0) & 1u, dead)) return false;
-            if (slot) ++used1;
-            else ++used0;
-            if (!(wide & i) && !warp_wait(val_full + 8 * st, (t >> 1) & 1u, dead)) return false;
+            const uint32_t slot = i & 1u, buf = (i >> 1) & 1u, t = tiles + (wide ? i >> 2 : 2u * (i >> 2) + slot), st = t & 1u;
+            if (!warp_wait(weight_ready + 8 * (slot * 2 + buf), ((slot ? uses[1] : uses[0]) + (i >> 2)) & 1u, dead)) return false;
+            if (buf == 0u && !(wide & slot) && !warp_wait(val_full + 8 * st, (t >> 1) & 1u, dead)) return false;
             fence_after();
-            const uint64_t va = v_desc + st * (kTileBytes >> 4);
-            const uint32_t d = tmem + 2 * kTile + slot * D, p = tmem + slot * kTile;
-            if (elected()) {
+            const uint64_t va = v_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
+            const uint32_t d = tmem + 2 * kTile + slot * D, p = tmem + slot * kTile + buf * kHalf;
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks) product_ts(d, p + ks * 8, va + ks * 128, kOut, i > 1u || ks > 0);
-                if (!wide || slot) commit_to(val_empty + 8 * st);
-            }
-            __syncwarp();
+            for (int ks = 0; ks < kHalf / 16; ++ks) product_ts(d, p + ks * 8, va + ks * 128, kOut, i > 1u || ks > 0, lead);
+            if (buf && (!wide || slot)) commit_to(val_empty + 8 * st, lead);
+            commit_to(out_free + 8 * slot, lead);
             return true;
         };
-        if (!scores(0u)) return;
-        if (n > 1 && !scores(1u)) return;
 #pragma unroll 1
-        for (int i = 0; i < n; ++i) {
+        for (uint32_t i = 0; i < 4u; ++i)
+            if (exists(i) && !scores(i)) return;
+#pragma unroll 1
+        for (uint32_t i = 0; (i >> 2) < of0; ++i) {
+            if (!exists(i)) continue;
             if (!outputs(i)) return;
-            if (i + 2 < n && !scores(i + 2)) return;
+            if (exists(i + 4u) && !scores(i + 4u)) return;
         }
-        if (elected()) commit_to(smem_u32(&bars->out_done));
-        __syncwarp();
-        tiles += n_tiles;
+        commit_to(smem_u32(&bars->out_done), lead);
+        tiles += n;
+        uses[0] += of0;
+        uses[1] += of1;
         ++seg;
         walk_leave(w, a, lane);
     }
@@ -497,8 +511,6 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
     asm("{\n .reg .b64 v, w;\n mov.b64 v, {%0, %1};\n mov.b64 w, {%2, %3};\n add.rn.f32x2 v, v, w;\n mov.b64 {%0, %1}, v;\n}"
         : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
-__device__ __forceinline__ uint4 load_info(const uint32_t (&w)[4]) { return *reinterpret_cast<const uint4 *>(w); }
-__device__ __forceinline__ uint32_t word_of(const uint4 &v, int k) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
 
 template <int D>
 __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem_all, uint32_t q_at, Bars *bars,
@@ -509,7 +521,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
     const uint32_t s_at = tmem + slot * kTile, o_at = tmem + 2 * kTile + slot * D;
     const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);          // a scale of 0 as one that no finite score is moved by
     walk_enter(w, a, line, lane);
-    uint32_t seg = 0u, used = 0u, tile_n = 0u;
+    uint32_t seg = 0u, used = 0u, freed = 0u, tile_n = 0u;
     while (walk_next(w, a, lane)) {
         const bool wide = w.wide();
         const int step0 = w.step0, n = w.step1 - step0;
@@ -541,66 +553,64 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         const uint32_t *bits = a.bits ? a.bits + token * a.words : nullptr;
         float m = -CUDART_INF_F, l = 0.0f;
         bool fresh = true;                                         // nothing of this slot is in its output yet
-        for (int i = wide ? 0 : slot; i < n; i += wide ? 1 : 2) {
-            if (*dead) break;
-            if (!warp_wait(smem_u32(&bars->score_full[slot]), used & 1u, dead)) break;
-            ++used;
+        const int halves = 2 * (wide ? n : (n + 1 - slot) >> 1);
+#pragma unroll 1
+        for (int i = 0; i < halves; ++i) {
+            const uint32_t buf = i & 1;
+            const uint32_t weight_bar = smem_u32(&bars->weight_ready[slot * 2 + buf]);
+            if (!warp_wait(smem_u32(&bars->score_full[slot * 2 + buf]), (used + (i >> 1)) & 1u, dead)) break;
             fence_after();
             if (!some) {                                           // a warp without rows: its part of the tile stays what it is
-                if (lane == 0) bar_arrive(smem_u32(&bars->weight_ready[slot]));
+                if (lane == 0) bar_arrive(weight_bar);
                 continue;
             }
-            const int t0 = (step0 + i) * kTile;
-            const Info *inf = info + ((tile_n + i) & 3);
-            const uint4 there = load_info(inf->there), poison = load_info(inf->poison);
-            const bool part = live && (t0 + kTile > all || ~(there.x & there.y & there.z & there.w) != 0u || (poison.x | poison.y | poison.z | poison.w) != 0u);
-            // tokens of piece k (32 of them) that this row sees
-            auto seen = [&](int k) {
-                const int u0 = t0 + 32 * k;
-                uint32_t v = low_bits(lim - u0) & word_of(there, k);
-                if (live && a.mask_kind == DSP_MASK_BITS && u0 + 32 > past && v) {
-                    const int j0 = u0 - past;                      // new token that the piece's first place holds
-                    const int w0 = j0 >> 5, sh = j0 & 31;
-                    const uint32_t lo = w0 >= 0 && w0 < a.words ? __ldg(bits + w0) : w0 < 0 ? 0xFFFFFFFFu : 0u;
-                    const uint32_t hi = w0 + 1 >= 0 && w0 + 1 < a.words ? __ldg(bits + w0 + 1) : 0u;
-                    v &= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
-                }
-                return v;
-            };
-            if (__any_sync(0xFFFFFFFFu, part)) {                   // at the ends of what a tile's rows see: the scores once through the masks
-#pragma unroll 1
-                for (int k = 0; k < 4; ++k) {
-                    float x[32];
-                    tmem_load32(s_at + 32 * k, x);
-                    tmem_loaded(x);
-                    const uint32_t v = seen(k), nan = v & word_of(poison, k);
+            const uint32_t at = s_at + buf * kHalf;
+            float x[2][32];
+            tmem_load32(at, x[0]);
+            tmem_load32(at + 32, x[1]);
+            const int tile = wide ? i >> 1 : 2 * (i >> 1) + slot, t0 = (step0 + tile) * kTile + (int)buf * kHalf;
+            const Info *inf = info + ((tile_n + tile) & 3);
+            const uint2 there = *reinterpret_cast<const uint2 *>(&inf->there[2 * buf]), poison = *reinterpret_cast<const uint2 *>(&inf->poison[2 * buf]);
+            const bool part = live && (t0 + kHalf > all || (there.x & there.y) != 0xFFFFFFFFu || (poison.x | poison.y) != 0u);
+            tmem_loaded(x[0]);
+            tmem_loaded(x[1]);
+            if (__any_sync(0xFFFFFFFFu, part)) {                   // at the ends of what a tile's rows see
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        x[e] = (v >> e) & 1u ? x[e] : -CUDART_INF_F;
-                        if ((nan >> e) & 1u) x[e] = CUDART_NAN_F;
+                for (int k = 0; k < 2; ++k) {
+                    const int u0 = t0 + 32 * k;
+                    uint32_t v = low_bits(lim - u0) & (k ? there.y : there.x);
+                    if (live && a.mask_kind == DSP_MASK_BITS && u0 + 32 > past && v) {
+                        const int j0 = u0 - past;                  // new token that the piece's first place holds
+                        const int w0 = j0 >> 5, sh = j0 & 31;
+                        const uint32_t lo = w0 >= 0 && w0 < a.words ? __ldg(bits + w0) : w0 < 0 ? 0xFFFFFFFFu : 0u;
+                        const uint32_t hi = w0 + 1 >= 0 && w0 + 1 < a.words ? __ldg(bits + w0 + 1) : 0u;
+                        v &= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
                     }
-                    tmem_store32(s_at + 32 * k, x);
+                    const uint32_t nan = v & (k ? poison.y : poison.x);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[k][e] = (v >> e) & 1u ? x[k][e] : -CUDART_INF_F;
+                    if (nan) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[k][e] = (nan >> e) & 1u ? CUDART_NAN_F : x[k][e];
+                    }
                 }
-                tmem_stored();
             }
             // the row's maximum; only where it passes the one so far by 2^8 does that move, and the output with it
-            float x[4][32];
             float tops[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) tmem_load32(s_at + 32 * k, x[k]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                tmem_loaded(x[k]);
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], x[k][e], x[k][e + 1]);
-            }
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
+            const float top = max3(fmaxf(tops[0], tops[1]), tops[2], tops[3]) * scale;
             const bool move = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float to = move ? top : m, keep = m == to ? 1.0f : ex2_approx(m - to);
                 m = to;
                 l *= keep;
+                // between the product with the weights before these, which may still be running, and the one with these
                 if (!fresh) {
+                    if (!warp_wait(smem_u32(&bars->out_free[slot]), (freed + i - 1) & 1u, dead)) break;
+                    fence_after();
 #pragma unroll 1
                     for (int k = 0; k < D / 8; ++k) {
                         float y[8];
@@ -615,7 +625,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             const float base = m == -CUDART_INF_F ? 0.0f : m;
             float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2; ++k) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     uint32_t p[4];
@@ -628,15 +638,17 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                         add2(sums[e & 2], sums[(e & 2) + 1], a0, a1);
                         p[e >> 1] = pack2(a0, a1);
                     }
-                    tmem_store4(s_at + 16 * k + 4 * h, p);         // over scores that are in registers
+                    tmem_store4(at + 16 * k + 4 * h, p);           // over scores that are in registers
                 }
             }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_stored();
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(smem_u32(&bars->weight_ready[slot]));
+            if (lane == 0) bar_arrive(weight_bar);
         }
+        used += halves >> 1;
+        freed += halves;
         tile_n += n;
         if (!*dead) warp_wait(smem_u32(&bars->out_done), seg & 1u, dead);
         fence_after();
@@ -725,7 +737,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     __shared__ uint32_t s_tmem;
     __shared__ Walk s_walk[kSoftWarps + kFillWarps + 1];
     __shared__ int s_dead;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(s_raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, k_at = base + 2 * kTileBytes, v_at = base + 4 * kTileBytes;
     if (threadIdx.x == 0) {
@@ -736,6 +748,9 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
             bar_init(smem_u32(&s_bars.val_full[i]), kFillWarps);
             bar_init(smem_u32(&s_bars.key_empty[i]), 1);
             bar_init(smem_u32(&s_bars.val_empty[i]), 1);
+            bar_init(smem_u32(&s_bars.out_free[i]), 1);
+        }
+        for (int i = 0; i < 4; ++i) {
             bar_init(smem_u32(&s_bars.score_full[i]), 1);
             bar_init(smem_u32(&s_bars.weight_ready[i]), kSoftWarps / 2);
         }
@@ -750,16 +765,13 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     }
     enter_line<BlockRequest>(a, 0, 0, kWide, s_scan, &s_line);         // ends with a barrier of the CTA
     fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem, 0);
     if (s_line.begin < s_line.end) {
         if (warp < kSoftWarps) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kSoftRegs));
             softmax_role<D>(a, s_line, s_walk[warp], tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
         } else if (warp < kSoftWarps + kFillWarps) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kFillRegs));
             fill_role<D>(a, s_line, s_walk[warp], k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
         } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kProductRegs));
             if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, &s_dead, lane);
         }
     }

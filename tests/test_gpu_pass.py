@@ -345,6 +345,27 @@ def test_attention_matches_the_definition(new, kv, Hq, Hkv, D, page, mask, sprea
 
 
 @gpu
+@pytest.mark.parametrize("new,Hq,Hkv,D", [(20, 8, 8, 128), (70, 8, 8, 64), (150, 8, 8, 128), (64, 20, 4, 64), (3, 16, 16, 128)])
+def test_attention_of_more_requests_than_the_gpu_has_places_for(new, Hq, Hkv, D):
+    """Units of many token tiles in a row on one SM, of one and of two tiles of rows; two requests are looked at closely."""
+    page, B = 64, 60
+    r = np.random.default_rng(new)
+    kv = [int(x) for x in r.integers(1400, 2300, B)]
+    width = -(-max(kv) // page)
+    cache = _cache_of(r, 200, Hkv, D, page)
+    table = r.integers(0, 200, (B, width)).astype(np.int32)       # requests may share blocks
+    q = torch.tensor(r.normal(size=(B * new, Hq, D)), dtype=torch.bfloat16)
+    cu = [new * b for b in range(B + 1)]
+    for mask in ("causal", "full"):
+        got = _attend(q, cache, table, kv, cu, new, mask)
+        for b in (0, B - 1):
+            rows = slice(cu[b], cu[b + 1])
+            want = ref.attend(ref.to_numpy(q[rows]), cache, page, D, [table[b].tolist()], [kv[b]], [0, new], D ** -0.5, mask)
+            _attn_close(got[rows], want)
+        assert torch.isfinite(got).all()
+
+
+@gpu
 @pytest.mark.parametrize("D,Hq,Hkv,new", [(128, 5, 1, 1), (64, 4, 2, 6), (128, 40, 8, 40), (64, 16, 2, 200)])
 def test_attention_ignores_what_it_must_not_see(D, Hq, Hkv, new):
     """Unwritten places of the pages, pages beyond the length, tokens that the mask hides: all NaN, all block numbers wild."""
