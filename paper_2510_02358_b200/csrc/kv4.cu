@@ -3,8 +3,8 @@
 // the 4-bit form of keys and values), in one pass over them.
 //
 // A head of a token is a row of D channels on D / 8 neighbouring lanes, eight channels a lane: the
-// row's sum of squares, extrema and the rotation's partner channels come from shuffles inside those
-// lanes, so nothing goes through shared memory and the pass is one read and one write of the rows.
+// row's sum of squares and extrema come from shuffles inside those lanes, so nothing goes through
+// shared memory and the pass is one read and one write of the rows.
 // A group of lanes takes kHeads heads of one token: their loads are in flight together, and the
 // token's angles are read once for them.
 //
@@ -30,8 +30,8 @@ struct NormArgs {
     const float *cos_sin;
     bool cs_vec;
     int max_pos, rot, interleaved;
-    int T, Hq, Hkv, heads;                       // heads: Hq + Hkv (norm) or Hq + 2 Hkv (append)
-    int chunks;                                  // groups of heads per token
+    int T, Hq, Hkv;
+    int chunks, q_chunks, k_chunks;              // groups of heads per token, of queries, of keys
     const int64_t *slot;
     uint8_t *cache;
     long long n_slots;
@@ -39,52 +39,66 @@ struct NormArgs {
     void *q_out, *k_out;
 };
 
-template <typename DT> struct Row8;
-template <> struct Row8<__nv_bfloat16> {
-    uint4 v;
+// Two fp32 numbers that go through the arithmetic together (each rounded for itself, as ever).
+struct Two {
+    float a, b;
+};
+__device__ __forceinline__ Two mul2(Two x, Two y) {
+    asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
+        : "+f"(x.a), "+f"(x.b) : "f"(y.a), "f"(y.b));
+    return x;
+}
+__device__ __forceinline__ Two add2(Two x, Two y) {
+    asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n add.rn.f32x2 u, u, v;\n mov.b64 {%0, %1}, u;\n}"
+        : "+f"(x.a), "+f"(x.b) : "f"(y.a), "f"(y.b));
+    return x;
+}
+
+// Four neighbouring channels of a row.
+template <typename DT> struct Quad;
+template <> struct Quad<__nv_bfloat16> {
+    uint2 v;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool vec) {
+        if (vec) {
+            asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+        } else {
+            const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
+            v.x = u[0] | (uint32_t)u[1] << 16;
+            v.y = u[2] | (uint32_t)u[3] << 16;
+        }
+    }
+    __device__ __forceinline__ void get(Two &x, Two &y) const {
+        x = {bf16_lo(v.x), bf16_hi(v.x)};
+        y = {bf16_lo(v.y), bf16_hi(v.y)};
+    }
+    static __device__ __forceinline__ uint32_t pack(Two x) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(x.a, x.b);
+        return *reinterpret_cast<const uint32_t *>(&p);
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16 *p, Two x, Two y) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack(x), pack(y));
+    }
+    static __device__ __forceinline__ Two rounded(Two x) {
+        const uint32_t w = pack(x);
+        return {bf16_lo(w), bf16_hi(w)};
+    }
+};
+template <> struct Quad<float> {
+    uint4 v;
+    __device__ __forceinline__ void load(const float *p, bool vec) {
         if (vec) {
             v = ldg_stream(p);
         } else {
-            const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
-            v.x = u[0] | (uint32_t)u[1] << 16; v.y = u[2] | (uint32_t)u[3] << 16;
-            v.z = u[4] | (uint32_t)u[5] << 16; v.w = u[6] | (uint32_t)u[7] << 16;
-        }
-    }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-        x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
-    }
-    static __device__ __forceinline__ uint32_t pack(float a, float b) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-        return *reinterpret_cast<const uint32_t *>(&p);
-    }
-    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&x)[8]) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(pack(x[0], x[1]), pack(x[2], x[3]), pack(x[4], x[5]), pack(x[6], x[7]));
-    }
-    static __device__ __forceinline__ float rounded(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
-};
-template <> struct Row8<float> {
-    uint4 a, b;
-    __device__ __forceinline__ void load(const float *p, bool vec) {
-        if (vec) {
-            a = ldg_stream(p);
-            b = ldg_stream(p + 4);
-        } else {
             const uint32_t *u = reinterpret_cast<const uint32_t *>(p);
-            a = make_uint4(u[0], u[1], u[2], u[3]);
-            b = make_uint4(u[4], u[5], u[6], u[7]);
+            v = make_uint4(u[0], u[1], u[2], u[3]);
         }
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
-        x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+    __device__ __forceinline__ void get(Two &x, Two &y) const {
+        x = {__uint_as_float(v.x), __uint_as_float(v.y)};
+        y = {__uint_as_float(v.z), __uint_as_float(v.w)};
     }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[8]) {
-        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-    }
-    static __device__ __forceinline__ float rounded(float x) { return x; }
+    static __device__ __forceinline__ void store(float *p, Two x, Two y) { *reinterpret_cast<float4 *>(p) = make_float4(x.a, x.b, y.a, y.b); }
+    static __device__ __forceinline__ Two rounded(Two x) { return x; }
 };
 
 __device__ __forceinline__ float bf16_down(float x) {
@@ -93,16 +107,17 @@ __device__ __forceinline__ float bf16_down(float x) {
 }
 __device__ __forceinline__ float bf16_up_nonneg(float x) { return __uint_as_float((__float_as_uint(x) + 0xFFFFu) & 0xFFFF0000u); }
 
-// One scale, one offset and eight codes of a lane's channels; kLanes lanes hold the row.
+// One scale and one offset for the row, and the codes of a lane's two quads as they lie in half a word
+// (bits 0-7: channels 0 and 2, bits 16-23: channels 1 and 3).  kLanes lanes hold the row.
 template <int kLanes>
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &params) {
-    float lo = x[0], hi = x[0];
-    bool fine = fabsf(x[0]) <= 3.402823466e38f;
+__device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2], uint32_t &params) {
+    float lo = x[0].a, hi = x[0].a;
+    bool fine = true;
 #pragma unroll
-    for (int e = 1; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        fine = fine && fabsf(x[e]) <= 3.402823466e38f;            // false for NaN too
+    for (int e = 0; e < 4; ++e) {
+        lo = fminf(lo, fminf(x[e].a, x[e].b));
+        hi = fmaxf(hi, fmaxf(x[e].a, x[e].b));
+        fine = fine && fabsf(x[e].a) <= 3.402823466e38f && fabsf(x[e].b) <= 3.402823466e38f;      // false for NaN too
     }
     hi = fine ? hi : CUDART_INF_F;                                 // carries the finding through the reduction
 #pragma unroll
@@ -114,163 +129,217 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &par
     float s = bf16_up_nonneg(__fdiv_rn(__fsub_rn(hi, z), 15.0f));
     const bool ok = hi <= 3.402823466e38f && z >= -3.402823466e38f && s <= 3.402823466e38f;
     s = s < 1.17549435e-38f ? 0.0f : s;
-    uint32_t w = 0u;
+    half[0] = half[1] = 0u;
     if (ok && s > 0.0f) {
+        auto code = [&](float v) { return min(__float2uint_rn(__fdiv_rn(__fsub_rn(v, z), s)), 15u); };
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t code = min(__float2uint_rn(__fdiv_rn(__fsub_rn(x[e], z), s)), 15u);
-            w |= code << (4 * (e >> 1) + 16 * (e & 1));
-        }
+        for (int k = 0; k < 2; ++k)
+            half[k] = code(x[2 * k].a) | code(x[2 * k + 1].a) << 4 | code(x[2 * k].b) << 16 | code(x[2 * k + 1].b) << 20;
     }
     params = ok ? (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xFFFF0000u) : 0x7FFF7FFFu;
-    return w;
 }
 
-template <typename DT, int D, bool kAppend, int kHeads>
-__global__ void __launch_bounds__(kNormThreads) norm_rope_kernel(const NormArgs a) {
+// A lane holds two quads of its row.  kPaired: such that the channels that the rotation mixes are in one lane (quads a and
+// b = a + rot/2; with rot = D / 2 the upper lanes hold the channels that are not turned, in the same way).  Otherwise, for
+// neighbouring pairs and for other values of rot, eight channels in a row.  Either way the lanes' sums of squares meet in the
+// order of a tree of neighbouring channels.
+//
+// kHeads heads of one kind (queries, keys or values) of one token per group of lanes.
+template <typename DT, int D, bool kAppend, int kHeads, bool kPaired>
+__global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 4 : 3) norm_rope_kernel(const NormArgs a) {
     constexpr int kLanes = D / 8;                                 // lanes of a row
     const int lane = threadIdx.x & (kLanes - 1);
     const uint32_t group = blockIdx.x * (kNormThreads / kLanes) + threadIdx.x / kLanes;
     const uint32_t t_raw = group / (uint32_t)a.chunks;
     const bool live = t_raw < (uint32_t)a.T;                      // whole groups: the shuffles below need every lane of the warp
     const int t = live ? (int)t_raw : a.T - 1;
-    const int h0 = (int)(group - t_raw * (uint32_t)a.chunks) * kHeads;
-    const int ch = lane * 8;
-    const bool rope = a.cos_sin != nullptr;
+    int chunk = (int)(group - t_raw * (uint32_t)a.chunks);
+    // the chunks of a token: queries, keys, values
+    const int kind = chunk < a.q_chunks ? 0 : !kAppend || chunk < a.q_chunks + a.k_chunks ? 1 : 2;
+    chunk -= kind == 0 ? 0 : kind == 1 ? a.q_chunks : a.q_chunks + a.k_chunks;
+    const int h0 = chunk * kHeads, heads = kind == 0 ? a.Hq : a.Hkv;
+    const DT *src = static_cast<const DT *>(kind == 0 ? a.q : kind == 1 ? a.k : a.v);
+    const long long st = kind == 0 ? a.q_t : kind == 1 ? a.k_t : a.v_t, sh = kind == 0 ? a.q_h : kind == 1 ? a.k_h : a.v_h;
+    const bool vec = kind == 0 ? a.q_vec : kind == 1 ? a.k_vec : a.v_vec;
+    const DT *weight = static_cast<const DT *>(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
+    const bool rope = a.cos_sin != nullptr;                       // the same for the whole grid
+    const int turning = rope && kPaired ? a.rot >> 3 : kLanes;    // kPaired: the lanes whose channels are turned
+    const int ch0 = !kPaired ? lane * 8 : lane < turning ? lane * 4 : 4 * lane + 4 * turning;
+    const int ch1 = ch0 + (!kPaired ? 4 : 4 * turning);
+    src += t * st;
 
-    Row8<DT> raw[kHeads];
+    Quad<DT> raw[kHeads][2], wraw[2];
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
-        const int h = min(h0 + i, a.heads - 1);
-        const DT *p;
-        bool vec;
-        if (h < a.Hq) {
-            p = static_cast<const DT *>(a.q) + t * a.q_t + h * a.q_h;
-            vec = a.q_vec;
-        } else if (!kAppend || h < a.Hq + a.Hkv) {
-            p = static_cast<const DT *>(a.k) + t * a.k_t + (h - a.Hq) * a.k_h;
-            vec = a.k_vec;
-        } else {
-            p = static_cast<const DT *>(a.v) + t * a.v_t + (h - a.Hq - a.Hkv) * a.v_h;
-            vec = a.v_vec;
-        }
-        raw[i].load(p + ch, vec);
+        const DT *row = src + min(h0 + i, heads - 1) * sh;
+        raw[i][0].load(row + ch0, vec);
+        raw[i][1].load(row + ch1, vec);
     }
     const int pos = a.positions ? a.positions[t] : 0;
+    if (weight) {
+        wraw[0].load(weight + ch0, a.w_vec);
+        wraw[1].load(weight + ch1, a.w_vec);
+    }
     const bool pad = pos < 0, beyond = rope && pos >= a.max_pos;
-    const bool turned = rope && ch < a.rot;
-    // the angles of this lane's channels: pairs (i, i + rot/2) or (2i, 2i+1)
-    float c[8], s[8];
+    const bool turned = rope && kind < 2 && (kPaired ? lane < turning : ch0 < a.rot);
+    // angles: kPaired, of the channels ch0 ..; neighbouring pairs, the lane's four; else of all eight channels
+    constexpr int kAngles = kPaired ? 2 : 4;
+    Two c[kAngles], s[kAngles];
     if (turned) {
-        const float *row = a.cos_sin + (long long)min(max(pos, 0), a.max_pos - 1) * a.rot;
         const int half = a.rot >> 1;
-        if (a.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                c[e] = __ldg(row + (ch >> 1) + e);
-                s[e] = __ldg(row + half + (ch >> 1) + e);
-            }
-        } else {
-            const int i0 = ch < half ? ch : ch - half;
+        const float *row = a.cos_sin + (long long)min(max(pos, 0), a.max_pos - 1) * a.rot;
+        row += kPaired ? ch0 : a.interleaved ? ch0 >> 1 : ch0 < half ? ch0 : ch0 - half;
+        auto angles = [&](const float *p, Two &x, Two &y) {
             if (a.cs_vec) {
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const float4 cv = __ldg(reinterpret_cast<const float4 *>(row + i0 + e));
-                    const float4 sv = __ldg(reinterpret_cast<const float4 *>(row + half + i0 + e));
-                    c[e] = cv.x; c[e + 1] = cv.y; c[e + 2] = cv.z; c[e + 3] = cv.w;
-                    s[e] = sv.x; s[e + 1] = sv.y; s[e + 2] = sv.z; s[e + 3] = sv.w;
-                }
+                const float4 v = __ldg(reinterpret_cast<const float4 *>(p));
+                x = {v.x, v.y};
+                y = {v.z, v.w};
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    c[e] = __ldg(row + i0 + e);
-                    s[e] = __ldg(row + half + i0 + e);
-                }
+                x = {__ldg(p), __ldg(p + 1)};
+                y = {__ldg(p + 2), __ldg(p + 3)};
             }
+        };
+        angles(row, c[0], c[1]);
+        angles(row + half, s[0], s[1]);
+        if (!kPaired && !a.interleaved) {
+            angles(row + 4, c[kAngles - 2], c[kAngles - 1]);
+            angles(row + half + 4, s[kAngles - 2], s[kAngles - 1]);
         }
     }
+    // Sums of squares of the chunk's heads, then 1 / sqrt once for all of them: each of the first lanes takes one head's.
+    // (Heads of all kinds may share a warp, and a warp's lanes go through the shuffles together.)
+    float r[kHeads];
+    {
+        Two sums[kHeads];                                          // of the two quads
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            Two x[4];
+            raw[i][0].get(x[0], x[1]);
+            raw[i][1].get(x[2], x[3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], x[e]);
+            const Two y = add2({x[0].a, x[2].a}, {x[0].b, x[2].b}), z = add2({x[1].a, x[3].a}, {x[1].b, x[3].b});
+            sums[i] = add2(y, z);
+        }
+        if (!kPaired) {
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) sums[i].a = __fadd_rn(sums[i].a, sums[i].b);
+        }
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) {
+            if (kPaired && o == turning) {                         // rot = D / 2: a lane's quads meet before its half meets the other
+#pragma unroll
+                for (int i = 0; i < kHeads; ++i) sums[i] = {__fadd_rn(sums[i].a, sums[i].b), 0.0f};
+            }
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                const float xa = __shfl_xor_sync(0xFFFFFFFFu, sums[i].a, o);
+                if (kPaired) sums[i] = add2(sums[i], {xa, __shfl_xor_sync(0xFFFFFFFFu, sums[i].b, o)});
+                else sums[i].a = __fadd_rn(sums[i].a, xa);
+            }
+        }
+        if (kPaired) {                                             // adds the zero where that has been done
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) sums[i].a = __fadd_rn(sums[i].a, sums[i].b);
+        }
+        float mine = sums[0].a;
+#pragma unroll
+        for (int i = 1; i < kHeads; ++i) mine = (lane & (kHeads - 1)) == i ? sums[i].a : mine;
+        mine = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(mine, 1.0f / D), a.eps)));
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) r[i] = kHeads == 1 ? mine : __shfl_sync(0xFFFFFFFFu, mine, i, kLanes);
+    }
+    Two w[4];
+    if (weight) {
+        wraw[0].get(w[0], w[1]);
+        wraw[1].get(w[2], w[3]);
+    }
+    const bool any_kept = kAppend && __any_sync(0xFFFFFFFFu, kind > 0);
+    const long long slot = kAppend && kind > 0 ? a.slot[t] : -1;
+    const bool kept = live && !pad && slot >= 0 && slot < a.n_slots;
+    const long long block = kept ? block_of(slot, a.page) : 0;
+    const int place = kept ? (int)(slot - block * a.page) : 0, tok = place & 15;
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
         const int h = h0 + i;
-        const bool mine = live && h < a.heads;
-        const int kind = h < a.Hq ? 0 : (!kAppend || h < a.Hq + a.Hkv) ? 1 : 2;
-        float x[8];
-        raw[i].get(x);
-        {   // heads of both kinds may share a warp: every lane takes part in the sum, values leave it unused
-            const DT *w = static_cast<const DT *>(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
-            float sq[8];
+        Two x[4];
+        raw[i][0].get(x[0], x[1]);
+        raw[i][1].get(x[2], x[3]);
+        if (weight) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq[e] = __fmul_rn(x[e], x[e]);
-            float sum = __fadd_rn(__fadd_rn(__fadd_rn(sq[0], sq[1]), __fadd_rn(sq[2], sq[3])),
-                                  __fadd_rn(__fadd_rn(sq[4], sq[5]), __fadd_rn(sq[6], sq[7])));
-#pragma unroll
-            for (int o = 1; o < kLanes; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
-            if (w) {
-                const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.eps)));
-                Row8<DT> wr;
-                wr.load(w + ch, a.w_vec);
-                float wv[8];
-                wr.get(wv);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], r), wv[e]);
-            }
+            for (int e = 0; e < 4; ++e) x[e] = mul2(mul2(x[e], {r[i], r[i]}), w[e]);
         }
-        if (rope) {                                               // uniform over the grid
-            float y[8];
-            if (a.interleaved) {
+        if (kPaired) {
+            if (turned) {
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    y[e] = __fsub_rn(__fmul_rn(x[e], c[e >> 1]), __fmul_rn(x[e + 1], s[e >> 1]));
-                    y[e + 1] = __fadd_rn(__fmul_rn(x[e + 1], c[e >> 1]), __fmul_rn(x[e], s[e >> 1]));
+                for (int e = 0; e < 2; ++e) {                      // a - b and a + (-b) are the same number
+                    const Two y = add2(mul2(x[e], c[e]), mul2(x[e + 2], {-s[e].a, -s[e].b}));
+                    x[e + 2] = add2(mul2(x[e + 2], c[e]), mul2(x[e], s[e]));
+                    x[e] = y;
+                }
+            }
+        } else if (rope) {
+            if (a.interleaved) {
+                if (turned) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ce = e & 1 ? c[e >> 1].b : c[e >> 1].a, se = e & 1 ? s[e >> 1].b : s[e >> 1].a;
+                        x[e] = add2(mul2(x[e], {ce, ce}), mul2({x[e].b, x[e].a}, {-se, se}));
+                    }
                 }
             } else {
                 const int hop = a.rot >> 4;                       // lanes between a channel and its partner
                 const bool first = lane < hop;
-                const int base = (threadIdx.x & 31) - lane;
-                const int src = base + (first ? lane + hop : lane < 2 * hop ? lane - hop : lane);
+                const int from = first ? lane + hop : lane < 2 * hop ? lane - hop : lane;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float o = __shfl_sync(0xFFFFFFFFu, x[e], src);
-                    const float xc = __fmul_rn(x[e], c[e]), os = __fmul_rn(o, s[e]);
-                    y[e] = first ? __fsub_rn(xc, os) : __fadd_rn(xc, os);
+                for (int e = 0; e < 4; ++e) {
+                    const Two o = {__shfl_sync(0xFFFFFFFFu, x[e].a, from, kLanes), __shfl_sync(0xFFFFFFFFu, x[e].b, from, kLanes)};
+                    if (turned) {
+                        const Two se = s[e < kAngles ? e : 0];
+                        x[e] = add2(mul2(x[e], c[e < kAngles ? e : 0]), mul2(o, first ? Two{-se.a, -se.b} : se));
+                    }
                 }
-            }
-            if (turned && kind < 2) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = y[e];
             }
         }
         if (kind < 2 && (pad || beyond)) {
+            const float v = pad ? 0.0f : CUDART_NAN_F;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = pad ? 0.0f : CUDART_NAN_F;
+            for (int e = 0; e < 4; ++e) x[e] = {v, v};
         }
-        if (kind == 0) {
-            if (mine && a.q_out) Row8<DT>::store(static_cast<DT *>(a.q_out) + ((long long)t * a.Hq + h) * D + ch, x);
-        } else if (!kAppend) {
-            if (mine) Row8<DT>::store(static_cast<DT *>(a.k_out) + ((long long)t * a.Hkv + (h - a.Hq)) * D + ch, x);
+        const bool mine = live && h < heads;
+        if (kind == 0 || !kAppend) {
+            DT *out = static_cast<DT *>(kind == 0 ? a.q_out : a.k_out);
+            if (mine && out) {
+                out += ((long long)t * heads + h) * D;
+                Quad<DT>::store(out + ch0, x[0], x[1]);
+                Quad<DT>::store(out + ch1, x[2], x[3]);
+            }
         }
-        if (kAppend) {
+        if (kAppend && any_kept) {
             if constexpr (D <= 128) {
-                // shuffles inside: every lane of the warp takes part, queries too when they share a warp with keys
-                const bool any = __any_sync(0xFFFFFFFFu, kind > 0);
-                if (any) {
-                    if (kind == 1) {
+                if (kind == 1) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = Row8<DT>::rounded(x[e]);
-                    }
-                    uint32_t params;
-                    const uint32_t w = quantise8<kLanes>(x, params);
-                    const long long slot = a.slot[t];
-                    if (mine && kind > 0 && !pad && slot >= 0 && slot < a.n_slots) {
-                        const long long block = block_of(slot, a.page);
-                        const int place = (int)(slot - block * a.page), tok = place & 15;
-                        const int hk = kind == 1 ? h - a.Hq : h - a.Hq - a.Hkv;
-                        uint8_t *run = a.cache + run_index(block, place, hk, a.Hkv, a.page) * Kv4<D>::kRunBytes;
-                        const int at = kind == 1 ? Kv4<D>::key_word(tok, lane) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, lane);
-                        *reinterpret_cast<uint32_t *>(run + at) = w;
-                        if (lane == 0)
-                            *reinterpret_cast<uint32_t *>(run + Kv4<D>::kParamOff + tok * 8 + (kind == 1 ? 0 : 4)) = params;
-                    }
+                    for (int e = 0; e < 4; ++e) x[e] = Quad<DT>::rounded(x[e]);
+                }
+                uint32_t half[2], params;
+                quantise<kLanes>(x, half, params);
+                // Two quads make a word: kPaired, this lane's first with its neighbour's first, its second with the neighbour's
+                // second, so of the two lanes one gets each; otherwise the lane's own.
+                uint32_t word;
+                int at;
+                if (kPaired) {
+                    const bool odd = lane & 1;
+                    const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, odd ? half[0] : half[1], 1);
+                    word = odd ? got | half[1] << 8 : half[0] | got << 8;
+                    at = (odd ? ch1 : ch0) >> 3;
+                } else {
+                    word = half[0] | half[1] << 8;
+                    at = lane;
+                }
+                if (kept && h < heads) {
+                    uint8_t *run = a.cache + run_index(block, place, h, a.Hkv, a.page) * Kv4<D>::kRunBytes;
+                    *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, at) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, at))) = word;
+                    if (lane == 0) *reinterpret_cast<uint32_t *>(run + Kv4<D>::kParamOff + tok * 8 + (kind == 1 ? 0 : 4)) = params;
                 }
             }
         }
@@ -310,8 +379,12 @@ __global__ void __launch_bounds__(kNormThreads) kv4_read_kernel(const ReadArgs a
             v[e] = fmaf((float)((vw >> sh) & 15u), bf16_lo(p.y), bf16_hi(p.y));
         }
     }
-    Row8<DT>::store(static_cast<DT *>(a.k_out) + row * D + lane * 8, k);
-    Row8<DT>::store(static_cast<DT *>(a.v_out) + row * D + lane * 8, v);
+    DT *k_out = static_cast<DT *>(a.k_out) + row * D + lane * 8, *v_out = static_cast<DT *>(a.v_out) + row * D + lane * 8;
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+        Quad<DT>::store(k_out + e, {k[e], k[e + 1]}, {k[e + 2], k[e + 3]});
+        Quad<DT>::store(v_out + e, {v[e], v[e + 1]}, {v[e + 2], v[e + 3]});
+    }
 }
 
 bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -334,16 +407,25 @@ bool strides_ok(int64_t st, int64_t sh, int32_t H, int32_t D) { return sh >= D &
 template <typename DT, int D, bool kAppend>
 cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
     constexpr int kGroups = kNormThreads / (D / 8);
-    // Four heads to a group of lanes once that still fills the GPU (148 SMs of 8 CTAs), one below:
-    // a short call is the latency of one group's chain, a long one wants loads in flight.
-    const bool wide = (long long)a.T * a.heads >= 4LL * 148 * 8 * kGroups;
-    a.chunks = wide ? (a.heads + 3) / 4 : a.heads;
+    // Four heads to a group of lanes once single heads would need more than one round of CTAs (148 SMs of about 1024
+    // threads): a short call is the latency of one group's chain, a long one wants loads in flight.
+    const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv);
+    const bool wide = rows * (D / 8) > 148LL * 1024;
+    const int per = wide ? 4 : 1;
+    a.q_chunks = (a.Hq + per - 1) / per;
+    a.k_chunks = (a.Hkv + per - 1) / per;
+    a.chunks = a.q_chunks + (kAppend ? 2 : 1) * a.k_chunks;
     const long long groups = (long long)a.T * a.chunks;
     const unsigned grid = (unsigned)((groups + kGroups - 1) / kGroups);
-    if (wide)
-        norm_rope_kernel<DT, D, kAppend, 4><<<grid, kNormThreads, 0, st>>>(a);
+    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2));
+    if (wide && paired)
+        norm_rope_kernel<DT, D, kAppend, 4, true><<<grid, kNormThreads, 0, st>>>(a);
+    else if (wide)
+        norm_rope_kernel<DT, D, kAppend, 4, false><<<grid, kNormThreads, 0, st>>>(a);
+    else if (paired)
+        norm_rope_kernel<DT, D, kAppend, 1, true><<<grid, kNormThreads, 0, st>>>(a);
     else
-        norm_rope_kernel<DT, D, kAppend, 1><<<grid, kNormThreads, 0, st>>>(a);
+        norm_rope_kernel<DT, D, kAppend, 1, false><<<grid, kNormThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -399,7 +481,6 @@ extern "C" int32_t dsp_qk_norm_rope(const void *q, const void *k, int32_t dtype,
     if (!strides_ok(q_stride_t, q_stride_h, Hq, D) || !strides_ok(k_stride_t, k_stride_h, Hkv, D)) return DSP_ERR_INVALID_ARG;
     NormArgs a = norm_args(q, k, nullptr, dtype, T, Hq, Hkv, q_stride_t, q_stride_h, k_stride_t, k_stride_h, 0, 0,
                            q_weight, k_weight, eps, positions, cos_sin, max_pos, rot, interleaved);
-    a.heads = Hq + Hkv;
     a.q_out = q_out; a.k_out = k_out;
     DSP_CUDA_TRY(launch_norm<false>(a, dtype, D, reinterpret_cast<cudaStream_t>(stream)));
     return DSP_OK;
@@ -429,7 +510,6 @@ extern "C" int32_t dsp_kv4_append(const void *q, const void *k, const void *v, i
     if (!strides_ok(k_stride_t, k_stride_h, Hkv, D) || !strides_ok(v_stride_t, v_stride_h, Hkv, D)) return DSP_ERR_INVALID_ARG;
     NormArgs a = norm_args(q, k, v, dtype, T, with_q ? Hq : 0, Hkv, q_stride_t, q_stride_h, k_stride_t, k_stride_h,
                            v_stride_t, v_stride_h, q_weight, k_weight, eps, positions, cos_sin, max_pos, rot, interleaved);
-    a.heads = a.Hq + 2 * Hkv;
     a.slot = slot;
     a.cache = static_cast<uint8_t *>(cache);
     a.n_slots = (long long)n_blocks * page_size;
