@@ -107,19 +107,31 @@ __device__ __forceinline__ float bf16_down(float x) {
 }
 __device__ __forceinline__ float bf16_up_nonneg(float x) { return __uint_as_float((__float_as_uint(x) + 0xFFFFu) & 0xFFFF0000u); }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float y;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
 // One scale and one offset for the row, and the codes of a lane's two quads as they lie in half a word
 // (bits 0-7: channels 0 and 2, bits 16-23: channels 1 and 3).  kLanes lanes hold the row.
+//
+// A code is (x - z) / s, rounded, then rounded to a whole number.  The product with 1 / s is within 2e-6 of the quotient (which
+// is at most 15), so it has the same whole number next to it unless it lies within that of the middle between two; only lanes
+// that hold such a number (1e-4 is taken) divide.
 template <int kLanes>
 __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2], uint32_t &params) {
-    float lo = x[0].a, hi = x[0].a;
-    bool fine = true;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        lo = fminf(lo, fminf(x[e].a, x[e].b));
-        hi = fmaxf(hi, fmaxf(x[e].a, x[e].b));
-        fine = fine && fabsf(x[e].a) <= 3.402823466e38f && fabsf(x[e].b) <= 3.402823466e38f;      // false for NaN too
-    }
-    hi = fine ? hi : CUDART_INF_F;                                 // carries the finding through the reduction
+    float lo = min3(min3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a), hi = max3(max3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a);
+    lo = min3(min3(lo, x[2].b, x[3].a), x[3].b, lo);
+    hi = max3(max3(hi, x[2].b, x[3].a), x[3].b, hi);
+    const Two zero = {0.0f, 0.0f};                                 // 0 * x is NaN for an infinity or a NaN
+    const Two odd = add2(add2(mul2(x[0], zero), mul2(x[1], zero)), add2(mul2(x[2], zero), mul2(x[3], zero)));
+    hi = odd.a + odd.b == 0.0f ? hi : CUDART_INF_F;                // carries the finding through the reduction
 #pragma unroll
     for (int o = 1; o < kLanes; o <<= 1) {
         lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
@@ -131,10 +143,23 @@ __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2],
     s = s < 1.17549435e-38f ? 0.0f : s;
     half[0] = half[1] = 0u;
     if (ok && s > 0.0f) {
-        auto code = [&](float v) { return min(__float2uint_rn(__fdiv_rn(__fsub_rn(v, z), s)), 15u); };
+        const float inv = __frcp_rn(s);
+        constexpr float kRound = 12582912.0f;                      // 1.5 * 2^23: adding it leaves the nearest whole number, ties to even
+        Two c[4];
+        float far = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            half[k] = code(x[2 * k].a) | code(x[2 * k + 1].a) << 4 | code(x[2 * k].b) << 16 | code(x[2 * k + 1].b) << 20;
+        for (int e = 0; e < 4; ++e) {
+            const Two q = mul2(add2(x[e], {-z, -z}), {inv, inv});
+            c[e] = add2(add2(q, {kRound, kRound}), {-kRound, -kRound});
+            far = max3(far, fabsf(q.a - c[e].a), fabsf(q.b - c[e].b));
+        }
+        if (far > 0.4999f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = {rintf(__fdiv_rn(__fsub_rn(x[e].a, z), s)), rintf(__fdiv_rn(__fsub_rn(x[e].b, z), s))};
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)                                // below 2^24: exact
+            half[k] = __float2uint_rz(fmaf(c[2 * k + 1].b, 1048576.0f, fmaf(c[2 * k].b, 65536.0f, fmaf(c[2 * k + 1].a, 16.0f, c[2 * k].a))));
     }
     params = ok ? (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xFFFF0000u) : 0x7FFF7FFFu;
 }
@@ -146,8 +171,9 @@ __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2],
 //
 // kHeads heads of one kind (queries, keys or values) of one token per group of lanes.
 template <typename DT, int D, bool kAppend, int kHeads, bool kPaired>
-__global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 4 : 3) norm_rope_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 && !kAppend ? 4 : 3) norm_rope_kernel(const NormArgs a) {
     constexpr int kLanes = D / 8;                                 // lanes of a row
+    constexpr int kRunBytes = 16 * (D + 8);
     const int lane = threadIdx.x & (kLanes - 1);
     const uint32_t group = blockIdx.x * (kNormThreads / kLanes) + threadIdx.x / kLanes;
     const uint32_t t_raw = group / (uint32_t)a.chunks;
@@ -209,8 +235,8 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 
     // Sums of squares of the chunk's heads, then 1 / sqrt once for all of them: each of the first lanes takes one head's.
     // (Heads of all kinds may share a warp, and a warp's lanes go through the shuffles together.)
     float r[kHeads];
-    {
-        Two sums[kHeads];                                          // of the two quads
+    if (__any_sync(0xFFFFFFFFu, weight != nullptr)) {
+        float sum0[kHeads], sum1[kHeads];                          // of the two quads
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
             Two x[4];
@@ -218,33 +244,28 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 
             raw[i][1].get(x[2], x[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], x[e]);
-            const Two y = add2({x[0].a, x[2].a}, {x[0].b, x[2].b}), z = add2({x[1].a, x[3].a}, {x[1].b, x[3].b});
-            sums[i] = add2(y, z);
-        }
-        if (!kPaired) {
-#pragma unroll
-            for (int i = 0; i < kHeads; ++i) sums[i].a = __fadd_rn(sums[i].a, sums[i].b);
+            sum0[i] = __fadd_rn(__fadd_rn(x[0].a, x[0].b), __fadd_rn(x[1].a, x[1].b));
+            sum1[i] = __fadd_rn(__fadd_rn(x[2].a, x[2].b), __fadd_rn(x[3].a, x[3].b));
+            if (!kPaired) sum0[i] = __fadd_rn(sum0[i], sum1[i]);
         }
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) {
             if (kPaired && o == turning) {                         // rot = D / 2: a lane's quads meet before its half meets the other
 #pragma unroll
-                for (int i = 0; i < kHeads; ++i) sums[i] = {__fadd_rn(sums[i].a, sums[i].b), 0.0f};
+                for (int i = 0; i < kHeads; ++i) { sum0[i] = __fadd_rn(sum0[i], sum1[i]); sum1[i] = 0.0f; }
             }
 #pragma unroll
             for (int i = 0; i < kHeads; ++i) {
-                const float xa = __shfl_xor_sync(0xFFFFFFFFu, sums[i].a, o);
-                if (kPaired) sums[i] = add2(sums[i], {xa, __shfl_xor_sync(0xFFFFFFFFu, sums[i].b, o)});
-                else sums[i].a = __fadd_rn(sums[i].a, xa);
+                sum0[i] = __fadd_rn(sum0[i], __shfl_xor_sync(0xFFFFFFFFu, sum0[i], o));
+                if (kPaired) sum1[i] = __fadd_rn(sum1[i], __shfl_xor_sync(0xFFFFFFFFu, sum1[i], o));
             }
         }
-        if (kPaired) {                                             // adds the zero where that has been done
+        float mine = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kHeads; ++i) sums[i].a = __fadd_rn(sums[i].a, sums[i].b);
+        for (int i = 0; i < kHeads; ++i) {
+            if (kPaired) sum0[i] = __fadd_rn(sum0[i], sum1[i]);    // adds the zero where that has been done
+            mine = i == 0 || (lane & (kHeads - 1)) == i ? sum0[i] : mine;
         }
-        float mine = sums[0].a;
-#pragma unroll
-        for (int i = 1; i < kHeads; ++i) mine = (lane & (kHeads - 1)) == i ? sums[i].a : mine;
         mine = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(mine, 1.0f / D), a.eps)));
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) r[i] = kHeads == 1 ? mine : __shfl_sync(0xFFFFFFFFu, mine, i, kLanes);
@@ -259,6 +280,9 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 
     const bool kept = live && !pad && slot >= 0 && slot < a.n_slots;
     const long long block = kept ? block_of(slot, a.page) : 0;
     const int place = kept ? (int)(slot - block * a.page) : 0, tok = place & 15;
+    // where this token lies in the cache: a head further is a page's worth of runs further
+    const long long head_bytes = kAppend ? (long long)(a.page >> 4) * kRunBytes : 0;
+    uint8_t *run0 = kAppend ? a.cache + (block * a.Hkv + h0) * head_bytes + (long long)(place >> 4) * kRunBytes : nullptr;
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
         const int h = h0 + i;
@@ -337,7 +361,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 ? 
                     at = lane;
                 }
                 if (kept && h < heads) {
-                    uint8_t *run = a.cache + run_index(block, place, h, a.Hkv, a.page) * Kv4<D>::kRunBytes;
+                    uint8_t *run = run0 + i * head_bytes;
                     *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, at) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, at))) = word;
                     if (lane == 0) *reinterpret_cast<uint32_t *>(run + Kv4<D>::kParamOff + tok * 8 + (kind == 1 ? 0 : 4)) = params;
                 }
