@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from functools import lru_cache
 from types import SimpleNamespace
 from typing import Optional
 
@@ -717,12 +718,12 @@ def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: to
         _ints("node_depth", node_depth, (B, N), i32, dev)
         mask_words = mask_words or (N + 32) // 32
     if out is None:
-        count, kv_len, status = torch.empty((3, B), dtype=i32, device=dev).unbind(0)
-        position, token_row = torch.empty((2, T), dtype=i32, device=dev).unbind(0)
-        out = SimpleNamespace(block_count=count, kv_len=kv_len, row_status=status, position=position, token_row=token_row,
-                              cu_new=torch.empty(B + 1, dtype=i32, device=dev), ring_pos=torch.empty(2, dtype=i64, device=dev),
-                              slot=torch.empty(T, dtype=i64, device=dev),
-                              mask=torch.empty((T, mask_words), dtype=i32, device=dev) if N else None)
+        e = torch.empty                        # a tensor each: views of one buffer take longer to make
+        out = SimpleNamespace(block_count=e(B, dtype=i32, device=dev), kv_len=e(B, dtype=i32, device=dev),
+                              row_status=e(B, dtype=i32, device=dev), cu_new=e(B + 1, dtype=i32, device=dev),
+                              ring_pos=e(2, dtype=i64, device=dev), slot=e(T, dtype=i64, device=dev),
+                              position=e(T, dtype=i32, device=dev), token_row=e(T, dtype=i32, device=dev),
+                              mask=e((T, mask_words), dtype=i32, device=dev) if N else None)
     _check("dsp_cache_plan", lib().dsp_cache_plan(
         seq_len.data_ptr(), new_len.data_ptr(), block_count.data_ptr(), ring_pos.data_ptr(), B, T, page_size, n_blocks, width,
         table, stride, free_ring.data_ptr(), _at(node_parent), _at(node_depth), N,
@@ -833,6 +834,11 @@ def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bf
     return k, v
 
 
+@lru_cache(maxsize=1024)
+def _attn_workspace(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int, device: int) -> int:
+    return dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new)      # a function of the sizes and the device's SM count
+
+
 def dsp_attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int) -> int:
     n = C.c_size_t(0)
     _check("dsp_attn_kv4_workspace_bytes", lib().dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new, C.byref(n)))
@@ -864,7 +870,7 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
     else:
         _ints("out", out, (T, Hq, D), dt, dev)
     if workspace is None:
-        workspace = alloc_workspace(dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new), dev)
+        workspace = alloc_workspace(_attn_workspace(B, T, Hq, Hkv, D, max_new, dev.index), dev)
     _check("dsp_attn_kv4", lib().dsp_attn_kv4(
         q.data_ptr(), _dtype(q), B, T, Hq, Hkv, D, qt, qh, cache.data_ptr(), n_blocks, page, table, stride, width,
         kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,

@@ -484,7 +484,8 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
 template <int D, int NT, int kW, int kCtas, int kStages>
 cudaError_t launch_stream(const AttnArgs &a, int grid, cudaStream_t st) {
     constexpr int ring = kW * kStages * kU * Kv4<D>::kRunBytes, outs = kW * NT * (D / 16) * 4 * 32 * 4, smem = ring > outs ? ring : outs;
-    cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, NT, kW, kCtas, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<unsigned long long> done{0};
+    cudaError_t e = allow_shared(attn_stream_kernel<D, NT, kW, kCtas, kStages>, smem, done);
     if (e != cudaSuccess) return e;
     attn_stream_kernel<D, NT, kW, kCtas, kStages><<<grid, kW * 32, smem, st>>>(a);
     e = cudaGetLastError();

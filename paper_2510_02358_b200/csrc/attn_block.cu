@@ -820,7 +820,8 @@ __global__ void __launch_bounds__(128) attn_block_join_kernel(const AttnArgs a) 
 template <int D>
 cudaError_t launch(const AttnArgs &a, int grid, cudaStream_t st) {
     constexpr int smem = 6 * D * 2 * kTile + 1024;
-    cudaError_t e = cudaFuncSetAttribute(attn_block_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<unsigned long long> done{0};
+    cudaError_t e = allow_shared(attn_block_kernel<D>, smem, done);
     if (e != cudaSuccess) return e;
     attn_block_kernel<D><<<grid, kBlockThreads, smem, st>>>(a);
     e = cudaGetLastError();

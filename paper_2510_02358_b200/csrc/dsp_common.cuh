@@ -6,6 +6,8 @@
 #include <math_constants.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "dsp.h"
 
 namespace dsp {
@@ -37,6 +39,20 @@ inline int32_t cuda_fail(cudaError_t e) {
         cudaError_t e__ = (expr);                            \
         if (e__ != cudaSuccess) return ::dsp::cuda_fail(e__); \
     } while (0)
+
+// Lets `kernel` use `bytes` of dynamic shared memory; asked of the runtime once per kernel and device (`done`: a
+// static of the caller, a bit per device).
+template <typename Kernel>
+inline cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<unsigned long long> &done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 __host__ __device__ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -123,7 +123,7 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
 //
 // A code is (x - z) / s, rounded, then rounded to a whole number.  The product with 1 / s is within 2e-6 of the quotient (which
 // is at most 15), so it has the same whole number next to it unless it lies within that of the middle between two; only lanes
-// that hold such a number (1e-4 is taken) divide.
+// that hold such a number (1e-5 is taken) divide.
 template <int kLanes>
 __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2], uint32_t &params) {
     float lo = min3(min3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a), hi = max3(max3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a);
@@ -153,7 +153,7 @@ __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2],
             c[e] = add2(add2(q, {kRound, kRound}), {-kRound, -kRound});
             far = max3(far, fabsf(q.a - c[e].a), fabsf(q.b - c[e].b));
         }
-        if (far > 0.4999f) {
+        if (far > 0.49999f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) c[e] = {rintf(__fdiv_rn(__fsub_rn(x[e].a, z), s)), rintf(__fdiv_rn(__fsub_rn(x[e].b, z), s))};
         }
