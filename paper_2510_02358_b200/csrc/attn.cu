@@ -21,6 +21,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
+// Pairs of fp32 numbers (two query rows) that go through the arithmetic together.
+__device__ __forceinline__ void fma2(float &da, float &db, float s, float xa, float xb, float ya, float yb) {      // d = s x + y
+    asm("{\n .reg .b64 s, x, y;\n mov.b64 s, {%2, %2};\n mov.b64 x, {%3, %4};\n mov.b64 y, {%5, %6};\n fma.rn.f32x2 y, s, x, y;\n mov.b64 {%0, %1}, y;\n}"
+        : "=f"(da), "=f"(db) : "f"(s), "f"(xa), "f"(xb), "f"(ya), "f"(yb));
+}
+__device__ __forceinline__ void mul2(float &xa, float &xb, float s) {
+    asm("{\n .reg .b64 s, x;\n mov.b64 s, {%2, %2};\n mov.b64 x, {%0, %1};\n mul.rn.f32x2 x, s, x;\n mov.b64 {%0, %1}, x;\n}" : "+f"(xa), "+f"(xb) : "f"(s));
+}
+__device__ __forceinline__ void add2(float &xa, float &xb, float ya, float yb) {
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "+f"(xa), "+f"(xb) : "f"(ya), "f"(yb));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
 // Two codes as bf16 numbers 128 + code (0x4300 is 128, whose last mantissa bit is worth 1): (w >> 4i & 0x000F000F) | 0x43004300.
 __device__ __forceinline__ uint32_t biased(uint32_t w, int i) {
     uint32_t y;
@@ -47,7 +64,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
 }
 
 constexpr float kBias = 128.0f;
-constexpr int kU = 2;                            // runs of 16 tokens a warp takes per iteration
 
 // A lane's codes of a run of 16 tokens, keys or values.
 template <int D> struct Codes {
@@ -82,20 +98,23 @@ template <int D> struct Codes {
 // matrix instruction with rows of ones (so the bias leaves exactly; 136 and the 8 s beside z centre
 // the codes, which keeps the rounding error that of a centred value).
 //
-// Each warp walks its own runs of 16 tokens with the next run's loads in flight, and keeps its own
+// Each warp walks its own runs of 16 tokens with the next ones' copies in flight, and keeps its own
 // running maximum: it moves only when a score passes it by 2^8 (the sums cannot overflow by that, and
 // the division at the end takes it out), so most runs need no exchange between lanes for it.
-template <int D, int NT, int kW, int kCtas, int kStages>
+// kW warps a CTA, kCtas CTAs an SM, kU runs an iteration, kStages iterations in the ring.
+template <int D, int NT, int kW, int kCtas, int kU, int kStages>
 __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnArgs a) {
+    constexpr bool kQueriesShared = NT * D > 256;                 // their fragments would not leave enough registers
     constexpr int kRows = 8 * NT, kStep = 16 * kU * kW, kKs = D / 16, kMt = D / 16;
     constexpr int kFrag = NT * kMt * 4 * 32;                      // floats of a partial output, in fragment order
     constexpr int kStage = kU * Kv4<D>::kRunBytes, kRing = kStages * kStage;
     // a ring of kStages iterations' codes for each warp; after a segment the same place takes its output
     extern __shared__ __align__(16) uint8_t s_dyn[];
     float (*s_o)[NT * kMt * 4][32] = reinterpret_cast<float (*)[NT * kMt * 4][32]>(s_dyn);
-    __shared__ float s_m[kW][kRows], s_l[kW][kRows];
+    __shared__ float s_m[kW][kRows], s_l[kW][kRows], s_top[kRows], s_sum[kRows];
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
+    __shared__ uint2 s_q[kQueriesShared ? NT : 1][kQueriesShared ? kKs : 1][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     if (threadIdx.x == 0) a.split[blockIdx.x].last_cta = -1;
     enter_line<Request>(a, kRows, kStep, 1, s_scan, &s_line);
@@ -115,11 +134,12 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         const int step1 = (int)min((long long)rq.steps, step0 + (end - at));
         const int row_first = tile * kRows, rows_here = min(rq.rows - row_first, kRows);
         // queries of lane's row r, its quarter of the channels in the cache's order
-        uint32_t q[NT][kKs * 2];
+        uint32_t q[kQueriesShared ? 1 : NT][kKs * 2];
         float qs[NT][2];
-        int lim[NT][2];                                           // tokens that rows 2c, 2c+1 see (before the bits)
+        if (kQueriesShared) __syncthreads();                      // the last segment's have been used
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            uint32_t (&x)[kKs * 2] = q[kQueriesShared ? 0 : t];
             const int row = row_first + t * 8 + r;
             float sum = 0.0f;
             if (row < rq.rows) {
@@ -128,39 +148,45 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                                                                    (long long)(h * a.group + row - i * a.group) * a.q_h + c * (D / 4));
 #pragma unroll
                 for (int k = 0; k < kKs / 2; ++k) {
-                    const uint4 x = __ldg(src + k);
-                    q[t][4 * k] = x.x; q[t][4 * k + 1] = x.y; q[t][4 * k + 2] = x.z; q[t][4 * k + 3] = x.w;
+                    const uint4 v = __ldg(src + k);
+                    x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < kKs * 2; ++k) q[t][k] = 0u;
+                for (int k = 0; k < kKs * 2; ++k) x[k] = 0u;
             }
 #pragma unroll
-            for (int k = 0; k < kKs * 2; ++k) sum += bf16_lo(q[t][k]) + bf16_hi(q[t][k]);
+            for (int k = 0; k < kKs * 2; ++k) sum += bf16_lo(x[k]) + bf16_hi(x[k]);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4);
-                const int row_e = row_first + t * 8 + 2 * c + e;
-                lim[t][e] = row_e >= rq.rows ? 0
-                            : a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, rq.kv - rq.n_new + row_e / a.group + 1) : rq.kv;
+            for (int e = 0; e < 2; ++e) qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4);
+            if (kQueriesShared && warp == t % kW) {
+#pragma unroll
+                for (int j = 0; j < kKs; ++j) s_q[kQueriesShared ? t : 0][kQueriesShared ? j : 0][lane] = make_uint2(x[2 * j], x[2 * j + 1]);
             }
         }
+        if (kQueriesShared) __syncthreads();
         // tokens below `safe` are seen by every row of the tile, none from `stop` on by any
         const int past = rq.kv - rq.n_new;                        // negative if more is new than there is
         const int i_first = row_first / a.group, i_last = (row_first + rows_here - 1) / a.group;
         const int safe = a.mask_kind == DSP_MASK_CAUSAL ? past + i_first + 1 : a.mask_kind == DSP_MASK_FULL ? rq.kv : past;
         const int stop = a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i_last + 1) : rq.kv;
 
-        float o[NT][kMt][4], ps[NT][4], m[NT][2], l[NT][2], zs[NT][2];
+        // Scores are formed relative to the rows' reference -nb (base 2).  `unset`: rows of this lane (bit 2t + e) that have none
+        // yet, because nothing of what they see has come; rows beyond the unit's keep 0.
+        float o[NT][kMt][4], ps[NT][4], nb[NT][2], l[NT][2], zs[NT][2];
+        uint32_t unset = 0u;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int j = 0; j < kMt; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.0f;
             ps[t][0] = ps[t][1] = ps[t][2] = ps[t][3] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { m[t][e] = -CUDART_INF_F; l[t][e] = 0.0f; zs[t][e] = 0.0f; }
+            for (int e = 0; e < 2; ++e) {
+                nb[t][e] = 0.0f; l[t][e] = 0.0f; zs[t][e] = 0.0f;
+                unset |= (row_first + t * 8 + 2 * c + e < rq.rows ? 1u : 0u) << (2 * t + e);
+            }
         }
         // this warp's runs: kU neighbouring ones an iteration, kW iterations' worth on from one to the next
         int run = (step0 * kW + warp) * kU;
@@ -227,7 +253,14 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     const int i = 2 * (j & 1);
                     const uint32_t a0 = biased(w0, i), a1 = biased(w1, i), a2 = biased(w0, i + 1), a3 = biased(w1, i + 1);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma_bf16(s[x][t], a0, a1, a2, a3, q[t][2 * j], q[t][2 * j + 1]);
+                    for (int t = 0; t < NT; ++t) {
+                        if (kQueriesShared) {
+                            const uint2 b = s_q[kQueriesShared ? t : 0][kQueriesShared ? j : 0][lane];
+                            mma_bf16(s[x][t], a0, a1, a2, a3, b.x, b.y);
+                        } else {
+                            mma_bf16(s[x][t], a0, a1, a2, a3, q[kQueriesShared ? 0 : t][2 * j], q[kQueriesShared ? 0 : t][2 * j + 1]);
+                        }
+                    }
                 }
                 // tokens r (e < 2) and r + 8: their scales, in base 2
 #pragma unroll
@@ -238,9 +271,11 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     va[x][y] = bf16_lo(p.y);
                     vz[x][y] = fmaf(8.0f, va[x][y], bf16_hi(p.y));
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) s[x][t][2 * y + e] = fmaf(ka, s[x][t][2 * y + e], kb * qs[t][e]);
+                    for (int t = 0; t < NT; ++t) {
+                        float c0, c1;
+                        fma2(c0, c1, kb, qs[t][0], qs[t][1], nb[t][0], nb[t][1]);
+                        fma2(s[x][t][2 * y], s[x][t][2 * y + 1], ka, s[x][t][2 * y], s[x][t][2 * y + 1], c0, c1);
+                    }
                 }
             }
             const bool whole = (run + kU) * 16 <= min(safe, run_end * 16) && (here & ((1u << kU) - 1)) == (1u << kU) - 1;
@@ -253,40 +288,41 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int u = (run + x) * 16 + r + 8 * (e >> 1);
-                            bool ok = ((here >> x) & 1u) && run + x < run_end && u < lim[t][e & 1];
+                            const int u = (run + x) * 16 + r + 8 * (e >> 1), row = row_first + t * 8 + 2 * c + (e & 1), i = row / a.group;
+                            const int lim = row >= rq.rows ? 0 : a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i + 1) : rq.kv;
+                            bool ok = ((here >> x) & 1u) && run + x < run_end && u < lim;
                             if (a.mask_kind == DSP_MASK_BITS && ok && u >= past) {
-                                const int j = u - past, i = (row_first + t * 8 + 2 * c + (e & 1)) / a.group;
+                                const int j = u - past;
                                 ok = j < a.words * 32 && ((__ldg(a.bits + (long long)(rq.row0 + i) * a.words + (j >> 5)) >> (j & 31)) & 1u);
                             }
                             if (!ok) s[x][t][e] = -CUDART_INF_F;
                             seen |= (ok ? 1u : 0u) << ((x * NT + t) * 4 + e);
                         }
             }
-            bool move = false;
+            // A reference moves when a score passes it by 2^8, and is set by the first score that its row sees.
+            float top = -CUDART_INF_F;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int x = 0; x < kU; ++x)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(s[0][t][e], s[0][t][e + 2]);
-#pragma unroll
-                    for (int x = 1; x < kU; ++x) top = fmaxf(top, fmaxf(s[x][t][e], s[x][t][e + 2]));
-                    move = move || top > m[t][e] + 8.0f;
-                }
-            if (__any_sync(0xFFFFFFFFu, move)) {
+                for (int t = 0; t < NT; ++t) top = max3(max3(top, s[x][t][0], s[x][t][1]), s[x][t][2], s[x][t][3]);
+            if (__any_sync(0xFFFFFFFFu, top > 8.0f || unset != 0u)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(s[0][t][e], s[0][t][e + 2]);
+                        float row = fmaxf(s[0][t][e], s[0][t][e + 2]);
 #pragma unroll
-                        for (int x = 1; x < kU; ++x) top = fmaxf(top, fmaxf(s[x][t][e], s[x][t][e + 2]));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                        top = fmaxf(top, m[t][e]);
-                        const float keep = m[t][e] == top ? 1.0f : ex2_approx(m[t][e] - top);
-                        m[t][e] = top;
+                        for (int x = 1; x < kU; ++x) row = max3(row, s[x][t][e], s[x][t][e + 2]);
+                        row = fmaxf(row, __shfl_xor_sync(0xFFFFFFFFu, row, 4));
+                        row = fmaxf(row, __shfl_xor_sync(0xFFFFFFFFu, row, 8));
+                        row = fmaxf(row, __shfl_xor_sync(0xFFFFFFFFu, row, 16));
+                        const bool first = (unset >> (2 * t + e)) & 1u;
+                        const float by = (first ? row > -CUDART_INF_F : row > 8.0f) ? row : 0.0f;
+                        const float keep = first ? 1.0f : ex2_approx(-by);      // a row without a reference has nothing to rescale
+                        if (row > -CUDART_INF_F) unset &= ~(1u << (2 * t + e));
+                        nb[t][e] -= by;
+#pragma unroll
+                        for (int x = 0; x < kU; ++x) { s[x][t][e] -= by; s[x][t][e + 2] -= by; }
                         l[t][e] *= keep;
                         zs[t][e] *= keep;
                         ps[t][e] *= keep;
@@ -301,16 +337,14 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                 for (int t = 0; t < NT; ++t) {
                     float w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float base = m[t][e & 1] == -CUDART_INF_F ? 0.0f : m[t][e & 1];
-                        w[e] = ex2_approx(s[x][t][e] - base);
-                        l[t][e & 1] += w[e];
-                    }
+                    for (int e = 0; e < 4; ++e) w[e] = ex2_approx(s[x][t][e]);
+                    add2(l[t][0], l[t][1], w[0], w[1]);
+                    add2(l[t][0], l[t][1], w[2], w[3]);
                     if (whole) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            zs[t][e & 1] = fmaf(w[e], vz[x][e >> 1], zs[t][e & 1]);
-                            w[e] *= va[x][e >> 1];
+                        for (int y = 0; y < 2; ++y) {
+                            fma2(zs[t][0], zs[t][1], vz[x][y], w[2 * y], w[2 * y + 1], zs[t][0], zs[t][1]);
+                            mul2(w[2 * y], w[2 * y + 1], va[x][y]);
                         }
                     } else {
 #pragma unroll
@@ -351,7 +385,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     zs[t][e] += __shfl_xor_sync(0xFFFFFFFFu, zs[t][e], x);
                 }
                 if (r == 0) {
-                    s_m[warp][t * 8 + 2 * c + e] = m[t][e];
+                    s_m[warp][t * 8 + 2 * c + e] = (unset >> (2 * t + e)) & 1u ? -CUDART_INF_F : -nb[t][e];
                     s_l[warp][t * 8 + 2 * c + e] = l[t][e];
                 }
             }
@@ -360,15 +394,23 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float top = s_m[0][t * 8 + 2 * c + e];
+                const int row = t * 8 + 2 * c + e;
+                float top = s_m[0][row];
 #pragma unroll
-                for (int w = 1; w < kW; ++w) top = fmaxf(top, s_m[w][t * 8 + 2 * c + e]);
-                const float keep = m[t][e] == top ? 1.0f : ex2_approx(m[t][e] - top);
+                for (int w = 1; w < kW; ++w) top = fmaxf(top, s_m[w][row]);
+                const float mine = s_m[warp][row], keep = mine == top ? 1.0f : ex2_approx(mine - top);
                 const float off = zs[t][e] - (kBias + 8.0f) * ps[t][e];
 #pragma unroll
                 for (int j = 0; j < kMt; ++j) {
                     s_o[warp][(t * kMt + j) * 4 + e][lane] = (o[t][j][e] + off) * keep;
                     s_o[warp][(t * kMt + j) * 4 + e + 2][lane] = (o[t][j][e + 2] + off) * keep;
+                }
+                if (warp == 0 && r == 0) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) sum += s_m[w][row] == top ? s_l[w][row] : s_l[w][row] * ex2_approx(s_m[w][row] - top);
+                    s_top[row] = top;
+                    s_sum[row] = sum;
                 }
             }
         __syncthreads();
@@ -377,18 +419,15 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         for (int i = threadIdx.x; i < NT * kMt * 2 * 32; i += kW * 32) {
             const int ln = i & 31, k = i >> 5, e = k & 1, tj = k >> 1, t = tj / kMt, j = tj - t * kMt;
             const int row = t * 8 + 2 * (ln & 3) + e;
-            float x = 0.0f, y = 0.0f, sum = 0.0f, top = s_m[0][row];
-#pragma unroll
-            for (int w = 1; w < kW; ++w) top = fmaxf(top, s_m[w][row]);
+            float x = 0.0f, y = 0.0f;
 #pragma unroll
             for (int w = 0; w < kW; ++w) {
                 x += s_o[w][tj * 4 + e][ln];
                 y += s_o[w][tj * 4 + e + 2][ln];
-                sum += s_m[w][row] == top ? s_l[w][row] : s_l[w][row] * ex2_approx(s_m[w][row] - top);
             }
             if (starts && ends) {
                 if (row < rows_here) {
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    const float sum = s_sum[row], inv = 1.0f / sum;
                     const int rr = row_first + row, q_i = rr / a.group;
                     const int ch = (ln >> 2) * (D / 8) + 8 * (j >> 2) + 2 * (j & 3);
                     *reinterpret_cast<uint32_t *>(a.out + ((long long)(rq.row0 + q_i) * a.Hq + h * a.group + rr - q_i * a.group) * D + ch) =
@@ -398,8 +437,8 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                 part[(tj * 4 + e) * 32 + ln] = x;
                 part[(tj * 4 + e + 2) * 32 + ln] = y;
                 if (j == 0 && (ln >> 2) == 0) {
-                    part[kFrag + row] = top;
-                    part[kFrag + kRows + row] = sum;
+                    part[kFrag + row] = s_top[row];
+                    part[kFrag + kRows + row] = s_sum[row];
                 }
             }
         }
@@ -452,7 +491,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs a) {
 // Launch shape of a call, from what the host knows of it.
 struct Shape {
     bool block;                                  // the kernel for many rows
-    int nt, warps, ctas_sm, grid;
+    int nt, warps, ctas_sm, unroll, grid;
     size_t part_bytes;
 };
 
@@ -465,29 +504,30 @@ int sm_count() {
 Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
     Shape s;
     const long long rows = (long long)max_new * (Hq / Hkv);
-    s.block = rows > 16;
+    s.block = rows > 32;
     if (s.block) {
-        s.nt = s.warps = 0;
+        s.nt = s.warps = s.unroll = 0;
         s.ctas_sm = 1;
         s.grid = sm_count();
         s.part_bytes = attn_block_part_bytes(D);
         return s;
     }
-    s.nt = rows <= 8 ? 1 : 2;
+    s.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
     s.warps = s.nt == 1 ? 8 : 4;
-    s.ctas_sm = s.nt == 1 ? 2 : 3;
+    s.ctas_sm = s.nt == 2 ? 3 : 2;
+    s.unroll = s.nt == 4 ? 1 : 2;
     s.grid = sm_count() * s.ctas_sm;
     s.part_bytes = ((size_t)s.nt * D * 8 + 16 * s.nt) * sizeof(float);
     return s;
 }
 
-template <int D, int NT, int kW, int kCtas, int kStages>
+template <int D, int NT, int kW, int kCtas, int kU, int kStages>
 cudaError_t launch_stream(const AttnArgs &a, int grid, cudaStream_t st) {
     constexpr int ring = kW * kStages * kU * Kv4<D>::kRunBytes, outs = kW * NT * (D / 16) * 4 * 32 * 4, smem = ring > outs ? ring : outs;
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = allow_shared(attn_stream_kernel<D, NT, kW, kCtas, kStages>, smem, done);
+    cudaError_t e = allow_shared(attn_stream_kernel<D, NT, kW, kCtas, kU, kStages>, smem, done);
     if (e != cudaSuccess) return e;
-    attn_stream_kernel<D, NT, kW, kCtas, kStages><<<grid, kW * 32, smem, st>>>(a);
+    attn_stream_kernel<D, NT, kW, kCtas, kU, kStages><<<grid, kW * 32, smem, st>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_dependent(attn_join_kernel<D, NT>, (unsigned)grid, 128, 0, st, a, true);
@@ -549,13 +589,15 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
         return DSP_OK;
     }
     const long long tokens = (long long)max_blocks * page_size, rows = (long long)a.max_new * a.group;
-    const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * kU * s.warps - 1) / (16 * kU * s.warps));
+    const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * s.unroll * s.warps - 1) / (16 * s.unroll * s.warps));
     const int grid = (int)(most < s.grid ? most : s.grid);
     cudaError_t e;
     if (D == 64)
-        e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 3>(a, grid, st) : launch_stream<64, 2, 4, 3, 3>(a, grid, st);
+        e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<64, 2, 4, 3, 2, 3>(a, grid, st)
+                      : launch_stream<64, 4, 4, 2, 1, 4>(a, grid, st);
     else
-        e = s.nt == 1 ? launch_stream<128, 1, 8, 2, 3>(a, grid, st) : launch_stream<128, 2, 4, 3, 3>(a, grid, st);
+        e = s.nt == 1 ? launch_stream<128, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<128, 2, 4, 3, 2, 3>(a, grid, st)
+                      : launch_stream<128, 4, 4, 2, 1, 4>(a, grid, st);
     DSP_CUDA_TRY(e);
     return DSP_OK;
 }
