@@ -104,7 +104,7 @@ template <int D> struct Codes {
 // kW warps a CTA, kCtas CTAs an SM, kU runs an iteration, kStages iterations in the ring.
 template <int D, int NT, int kW, int kCtas, int kU, int kStages>
 __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnArgs a) {
-    constexpr bool kQueriesShared = NT * D > 256;                 // their fragments would not leave enough registers
+    constexpr bool kQueriesShared = NT >= 4;                      // their fragments would not leave enough registers
     constexpr int kRows = 8 * NT, kStep = 16 * kU * kW, kKs = D / 16, kMt = D / 16;
     constexpr int kFrag = NT * kMt * 4 * 32;                      // floats of a partial output, in fragment order
     constexpr int kStage = kU * Kv4<D>::kRunBytes, kRing = kStages * kStage;
@@ -112,10 +112,13 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     extern __shared__ __align__(16) uint8_t s_dyn[];
     float (*s_o)[NT * kMt * 4][32] = reinterpret_cast<float (*)[NT * kMt * 4][32]>(s_dyn);
     __shared__ float s_m[kW][kRows], s_l[kW][kRows], s_top[kRows], s_sum[kRows];
+    __shared__ __nv_bfloat16 *s_out[kRows];
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint2 s_q[kQueriesShared ? NT : 1][kQueriesShared ? kKs : 1][32];
+    __shared__ float s_qs[kRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+    grid_launch_dependents();                                     // the join's CTAs may come as soon as there is room
     if (threadIdx.x == 0) a.split[blockIdx.x].last_cta = -1;
     enter_line<Request>(a, kRows, kStep, 1, s_scan, &s_line);
     long long at = s_line.begin;
@@ -133,61 +136,12 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         const int h = unit / rq.tiles, tile = unit - h * rq.tiles;
         const int step1 = (int)min((long long)rq.steps, step0 + (end - at));
         const int row_first = tile * kRows, rows_here = min(rq.rows - row_first, kRows);
-        // queries of lane's row r, its quarter of the channels in the cache's order
-        uint32_t q[kQueriesShared ? 1 : NT][kKs * 2];
-        float qs[NT][2];
-        if (kQueriesShared) __syncthreads();                      // the last segment's have been used
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            uint32_t (&x)[kKs * 2] = q[kQueriesShared ? 0 : t];
-            const int row = row_first + t * 8 + r;
-            float sum = 0.0f;
-            if (row < rq.rows) {
-                const int i = row / a.group;
-                const uint4 *src = reinterpret_cast<const uint4 *>(a.q + (long long)(rq.row0 + i) * a.q_t +
-                                                                   (long long)(h * a.group + row - i * a.group) * a.q_h + c * (D / 4));
-#pragma unroll
-                for (int k = 0; k < kKs / 2; ++k) {
-                    const uint4 v = __ldg(src + k);
-                    x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kKs * 2; ++k) x[k] = 0u;
-            }
-#pragma unroll
-            for (int k = 0; k < kKs * 2; ++k) sum += bf16_lo(x[k]) + bf16_hi(x[k]);
-            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4);
-            if (kQueriesShared && warp == t % kW) {
-#pragma unroll
-                for (int j = 0; j < kKs; ++j) s_q[kQueriesShared ? t : 0][kQueriesShared ? j : 0][lane] = make_uint2(x[2 * j], x[2 * j + 1]);
-            }
-        }
-        if (kQueriesShared) __syncthreads();
         // tokens below `safe` are seen by every row of the tile, none from `stop` on by any
         const int past = rq.kv - rq.n_new;                        // negative if more is new than there is
         const int i_first = row_first / a.group, i_last = (row_first + rows_here - 1) / a.group;
         const int safe = a.mask_kind == DSP_MASK_CAUSAL ? past + i_first + 1 : a.mask_kind == DSP_MASK_FULL ? rq.kv : past;
         const int stop = a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i_last + 1) : rq.kv;
 
-        // Scores are formed relative to the rows' reference -nb (base 2).  `unset`: rows of this lane (bit 2t + e) that have none
-        // yet, because nothing of what they see has come; rows beyond the unit's keep 0.
-        float o[NT][kMt][4], ps[NT][4], nb[NT][2], l[NT][2], zs[NT][2];
-        uint32_t unset = 0u;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int j = 0; j < kMt; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.0f;
-            ps[t][0] = ps[t][1] = ps[t][2] = ps[t][3] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                nb[t][e] = 0.0f; l[t][e] = 0.0f; zs[t][e] = 0.0f;
-                unset |= (row_first + t * 8 + 2 * c + e < rq.rows ? 1u : 0u) << (2 * t + e);
-            }
-        }
         // this warp's runs: kU neighbouring ones an iteration, kW iterations' worth on from one to the next
         int run = (step0 * kW + warp) * kU;
         const int run_end = min(step1 * kW * kU, (max(stop, 0) + 15) >> 4);
@@ -229,9 +183,71 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
             }
             copies_done();                                        // an empty group keeps the count of groups that of iterations
         };
-        int ahead = run, stage = 0;
+        int ahead = run, stage = 0;                               // the first copies are under way while the queries come
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i, ahead += kW * kU) fetch(i, ahead < run_end);
+        auto load_queries = [&](int t, uint32_t (&x)[kKs * 2]) {
+            const int row = row_first + t * 8 + r, i = row / a.group;
+            const uint4 *src = reinterpret_cast<const uint4 *>(a.q + (long long)(rq.row0 + i) * a.q_t +
+                                                               (long long)(h * a.group + row - i * a.group) * a.q_h + c * (D / 4));
+#pragma unroll
+            for (int k = 0; k < kKs / 2; ++k) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (row < rq.rows) v = __ldg(src + k);
+                x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
+            }
+        };
+        auto query_sum = [&](const uint32_t (&x)[kKs * 2]) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kKs * 2; ++k) sum += bf16_lo(x[k]) + bf16_hi(x[k]);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+            return sum + __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+        };
+        // queries of lane's row r, its quarter of the channels in the cache's order
+        uint32_t q[kQueriesShared ? 1 : NT][kKs * 2];
+        float qs[NT][2];
+        if (kQueriesShared) {
+            // as operand fragments, each by one warp
+            __syncthreads();                                      // the last segment's have been used
+#pragma unroll
+            for (int t = warp; t < NT; t += kW) {
+                load_queries(t, q[0]);
+#pragma unroll
+                for (int j = 0; j < kKs; ++j) s_q[kQueriesShared ? t : 0][kQueriesShared ? j : 0][lane] = make_uint2(q[0][2 * j], q[0][2 * j + 1]);
+                const float sum = query_sum(q[0]);
+                if (c == 0) s_qs[t * 8 + r] = sum;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) qs[t][e] = s_qs[t * 8 + 2 * c + e];
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) load_queries(t, q[kQueriesShared ? 0 : t]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float sum = query_sum(q[kQueriesShared ? 0 : t]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4);
+            }
+        }
+        // Scores are formed relative to the rows' reference -nb (base 2).  `unset`: rows of this lane (bit 2t + e) that have none
+        // yet, because nothing of what they see has come; rows beyond the unit's keep 0.
+        float o[NT][kMt][4], ps[NT][4], nb[NT][2], l[NT][2], zs[NT][2];
+        uint32_t unset = 0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < kMt; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.0f;
+            ps[t][0] = ps[t][1] = ps[t][2] = ps[t][3] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                nb[t][e] = 0.0f; l[t][e] = 0.0f; zs[t][e] = 0.0f;
+                unset |= (row_first + t * 8 + 2 * c + e < rq.rows ? 1u : 0u) << (2 * t + e);
+            }
+        }
         for (; run < run_end; run += kW * kU, ahead += kW * kU) {
             await_copies<kStages - 2>();
             __syncwarp();                                         // every lane's copies have landed, and all have read the stage before
@@ -405,37 +421,51 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     s_o[warp][(t * kMt + j) * 4 + e][lane] = (o[t][j][e] + off) * keep;
                     s_o[warp][(t * kMt + j) * 4 + e + 2][lane] = (o[t][j][e + 2] + off) * keep;
                 }
-                if (warp == 0 && r == 0) {
+                if (warp == t % kW && r == 0) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int w = 0; w < kW; ++w) sum += s_m[w][row] == top ? s_l[w][row] : s_l[w][row] * ex2_approx(s_m[w][row] - top);
+                    const int rr = row_first + row, q_i = rr / a.group;
                     s_top[row] = top;
                     s_sum[row] = sum;
+                    s_out[row] = row < rows_here ? a.out + ((long long)(rq.row0 + q_i) * a.Hq + h * a.group + rr - q_i * a.group) * D : nullptr;
                 }
             }
         __syncthreads();
         const bool starts = step0 == 0, ends = step1 == rq.steps;
         float *part = a.part + ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * (kFrag + 2 * kRows);
-        for (int i = threadIdx.x; i < NT * kMt * 2 * 32; i += kW * 32) {
-            const int ln = i & 31, k = i >> 5, e = k & 1, tj = k >> 1, t = tj / kMt, j = tj - t * kMt;
-            const int row = t * 8 + 2 * (ln & 3) + e;
-            float x = 0.0f, y = 0.0f;
+        // a thread takes kJ neighbouring channel pairs of a row
+        constexpr int kAll = NT * kMt * 64 / (kW * 32), kJ = kAll >= 4 ? 4 : kAll >= 2 ? 2 : 1;
 #pragma unroll
-            for (int w = 0; w < kW; ++w) {
-                x += s_o[w][tj * 4 + e][ln];
-                y += s_o[w][tj * 4 + e + 2][ln];
-            }
+        for (int i = threadIdx.x; i < NT * kMt * 64 / kJ; i += kW * 32) {
+            const int ln = i & 31, e = (i >> 5) & 1, tj = (i >> 6) * kJ, t = tj / kMt, j = tj % kMt;
+            const int row = t * 8 + 2 * (ln & 3) + e;
+            float x[kJ] = {}, y[kJ] = {};
+#pragma unroll
+            for (int w = 0; w < kW; ++w)
+#pragma unroll
+                for (int z = 0; z < kJ; ++z) {
+                    x[z] += s_o[w][(tj + z) * 4 + e][ln];
+                    y[z] += s_o[w][(tj + z) * 4 + e + 2][ln];
+                }
             if (starts && ends) {
-                if (row < rows_here) {
-                    const float sum = s_sum[row], inv = 1.0f / sum;
-                    const int rr = row_first + row, q_i = rr / a.group;
-                    const int ch = (ln >> 2) * (D / 8) + 8 * (j >> 2) + 2 * (j & 3);
-                    *reinterpret_cast<uint32_t *>(a.out + ((long long)(rq.row0 + q_i) * a.Hq + h * a.group + rr - q_i * a.group) * D + ch) =
-                        sum == 0.0f ? 0u : pack_bf16(x * inv, y * inv);
+                __nv_bfloat16 *out = s_out[row];
+                if (out) {
+                    const float sum = s_sum[row], inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
+                    uint32_t v[kJ];
+#pragma unroll
+                    for (int z = 0; z < kJ; ++z) v[z] = sum == 0.0f ? 0u : pack_bf16(x[z] * inv, y[z] * inv);
+                    out += (ln >> 2) * (D / 8) + 8 * (j >> 2) + 2 * (j & 3);
+                    if constexpr (kJ == 4) *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
+                    else if constexpr (kJ == 2) *reinterpret_cast<uint2 *>(out) = make_uint2(v[0], v[1]);
+                    else *reinterpret_cast<uint32_t *>(out) = v[0];
                 }
             } else {
-                part[(tj * 4 + e) * 32 + ln] = x;
-                part[(tj * 4 + e + 2) * 32 + ln] = y;
+#pragma unroll
+                for (int z = 0; z < kJ; ++z) {
+                    part[((tj + z) * 4 + e) * 32 + ln] = x[z];
+                    part[((tj + z) * 4 + e + 2) * 32 + ln] = y[z];
+                }
                 if (j == 0 && (ln >> 2) == 0) {
                     part[kFrag + row] = s_top[row];
                     part[kFrag + kRows + row] = s_sum[row];
@@ -458,33 +488,85 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     }
 }
 
-// Joins the partial results of one unit that crossed the shares of several CTAs, in their order.
+// Joins the partial results of one unit that crossed the shares of several CTAs, in their order.  A long request alone may
+// leave one from every CTA: they are taken 16 at a time, all loads of a turn in flight together.
+constexpr int kJoinThreads = 256, kJoinTurn = 16;
 template <int D, int NT>
-__global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs a) {
-    constexpr int kRows = 8 * NT, kMt = D / 16, kFrag = NT * kMt * 4 * 32;
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a) {
+    constexpr int kRows = 8 * NT, kMt = D / 16, kFrag = NT * kMt * 4 * 32, kPart = kFrag + 2 * kRows;
+    constexpr int kPairs = NT * kMt * 2 * 32 / kJoinThreads > 0 ? NT * kMt * 2 * 32 / kJoinThreads : 1;
+    __shared__ float s_f[kJoinTurn][kRows], s_keep[kRows], s_m[kRows], s_l[kRows];
     grid_dependency_wait();
     const SplitUnit u = a.split[blockIdx.x];
     if (u.last_cta < 0) return;
-    const int first = blockIdx.x, n = u.last_cta - first + 1;
+    const int first = blockIdx.x, n = u.last_cta - first + 1, tid = threadIdx.x;
     const int row0 = max(a.cu[u.b], 0), n_new = max(min(min(a.cu[u.b + 1], a.T) - row0, a.max_new), 0);
-    auto part_of = [&](int i) { return a.part + ((long long)(first + i) * 2 + (i == 0 ? 1 : 0)) * (kFrag + 2 * kRows); };
-    for (int i = threadIdx.x; i < NT * kMt * 2 * 32; i += 128) {
-        const int ln = i & 31, k = i >> 5, e = k & 1, tj = k >> 1, t = tj / kMt, j = tj - t * kMt;
-        const int row = t * 8 + 2 * (ln & 3) + e, rr = u.tile * kRows + row;
-        if (rr >= n_new * a.group) continue;
-        float top = -CUDART_INF_F, x = 0.0f, y = 0.0f, sum = 0.0f;
-        for (int w = 0; w < n; ++w) top = fmaxf(top, part_of(w)[kFrag + row]);
-        for (int w = 0; w < n; ++w) {
-            const float *p = part_of(w);
-            const float m = p[kFrag + row], f = m == top ? 1.0f : ex2_approx(m - top);
-            x = fmaf(p[(tj * 4 + e) * 32 + ln], f, x);
-            y = fmaf(p[(tj * 4 + e + 2) * 32 + ln], f, y);
-            sum = fmaf(p[kFrag + kRows + row], f, sum);
+    // part i: the unit's first CTA left its second place, the others their first
+    const float *base = a.part + (long long)first * 2 * kPart;
+    if (tid < kRows) {
+        s_m[tid] = -CUDART_INF_F;
+        s_l[tid] = 0.0f;
+    }
+    float x[kPairs] = {}, y[kPairs] = {};
+    for (int i0 = 0; i0 < n; i0 += kJoinTurn) {
+        __syncthreads();
+        for (int i = tid; i < kJoinTurn * kRows; i += kJoinThreads) {
+            const int w = i / kRows;
+            s_f[w][i % kRows] = i0 + w < n ? base[(long long)((i0 + w) * 2 + (i0 + w == 0 ? 1 : 0)) * kPart + kFrag + i % kRows] : -CUDART_INF_F;
         }
-        const float inv = 1.0f / sum;
+        __syncthreads();
+        if (tid < kRows) {
+            const float before = s_m[tid];
+            float top = before, l[kJoinTurn];
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                top = fmaxf(top, s_f[w][tid]);
+                l[w] = i0 + w < n ? base[(long long)((i0 + w) * 2 + (i0 + w == 0 ? 1 : 0)) * kPart + kFrag + kRows + tid] : 0.0f;
+            }
+            const float keep = before == top ? 1.0f : ex2_approx(before - top);
+            float sum = s_l[tid] * keep;
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                const float m = s_f[w][tid], f = i0 + w >= n ? 0.0f : m == top ? 1.0f : ex2_approx(m - top);
+                s_f[w][tid] = f;
+                sum = fmaf(l[w], f, sum);
+            }
+            s_keep[tid] = keep;
+            s_m[tid] = top;
+            s_l[tid] = sum;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+            const int i = tid + k * kJoinThreads, ln = i & 31, q = i >> 5, e = q & 1, tj = q >> 1;
+            if (tj >= NT * kMt) break;
+            const int row = (tj / kMt) * 8 + 2 * (ln & 3) + e, at = (tj * 4 + e) * 32 + ln;
+            float vx[kJoinTurn], vy[kJoinTurn];
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                const float *p = base + (long long)((i0 + w) * 2 + (i0 + w == 0 ? 1 : 0)) * kPart + at;
+                vx[w] = i0 + w < n ? __ldg(p) : 0.0f;
+                vy[w] = i0 + w < n ? __ldg(p + 64) : 0.0f;
+            }
+            x[k] *= s_keep[row];
+            y[k] *= s_keep[row];
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                x[k] = fmaf(vx[w], s_f[w][row], x[k]);
+                y[k] = fmaf(vy[w], s_f[w][row], y[k]);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+        const int i = tid + k * kJoinThreads, ln = i & 31, q = i >> 5, e = q & 1, tj = q >> 1, j = tj % kMt;
+        if (tj >= NT * kMt) break;
+        const int row = (tj / kMt) * 8 + 2 * (ln & 3) + e, rr = u.tile * kRows + row;
+        if (rr >= n_new * a.group) continue;
+        const float sum = s_l[row], inv = 1.0f / sum;
         const int q_i = rr / a.group, ch = (ln >> 2) * (D / 8) + 8 * (j >> 2) + 2 * (j & 3);
         *reinterpret_cast<uint32_t *>(a.out + ((long long)(row0 + q_i) * a.Hq + u.h * a.group + rr - q_i * a.group) * D + ch) =
-            sum == 0.0f ? 0u : pack_bf16(x * inv, y * inv);
+            sum == 0.0f ? 0u : pack_bf16(x[k] * inv, y[k] * inv);
     }
 }
 
@@ -514,7 +596,7 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
     }
     s.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
     s.warps = s.nt == 1 ? 8 : 4;
-    s.ctas_sm = s.nt == 2 ? 3 : 2;
+    s.ctas_sm = s.nt == 2 || (s.nt == 4 && D == 64) ? 3 : 2;
     s.unroll = s.nt == 4 ? 1 : 2;
     s.grid = sm_count() * s.ctas_sm;
     s.part_bytes = ((size_t)s.nt * D * 8 + 16 * s.nt) * sizeof(float);
@@ -530,7 +612,7 @@ cudaError_t launch_stream(const AttnArgs &a, int grid, cudaStream_t st) {
     attn_stream_kernel<D, NT, kW, kCtas, kU, kStages><<<grid, kW * 32, smem, st>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    return launch_dependent(attn_join_kernel<D, NT>, (unsigned)grid, 128, 0, st, a, true);
+    return launch_dependent(attn_join_kernel<D, NT>, (unsigned)grid, kJoinThreads, 0, st, a, true);
 }
 
 }  // namespace
@@ -594,7 +676,7 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     cudaError_t e;
     if (D == 64)
         e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<64, 2, 4, 3, 2, 3>(a, grid, st)
-                      : launch_stream<64, 4, 4, 2, 1, 4>(a, grid, st);
+                      : launch_stream<64, 4, 4, 3, 1, 4>(a, grid, st);
     else
         e = s.nt == 1 ? launch_stream<128, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<128, 2, 4, 3, 2, 3>(a, grid, st)
                       : launch_stream<128, 4, 4, 2, 1, 4>(a, grid, st);

@@ -740,6 +740,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(s_raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, k_at = base + 2 * kTileBytes, v_at = base + 4 * kTileBytes;
+    grid_launch_dependents();                                     // the join's CTAs may come as soon as there is room
     if (threadIdx.x == 0) {
         a.split[blockIdx.x].last_cta = -1;
         s_dead = 0;
@@ -784,11 +785,12 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     }
 }
 
-// Joins the partial results of one unit, 16 rows per CTA of 128 threads.
+// Joins the partial results of one unit: 16 rows per CTA of 256 threads, the parts of a turn loaded together.
+constexpr int kJoinThreads = 256, kJoinTurn = 4, kJoinRows = 16;
 template <int D>
-__global__ void __launch_bounds__(128) attn_block_join_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const AttnArgs a) {
     grid_dependency_wait();
-    constexpr int kPart = 2 * kTile * (D + 2), kChunks = 2 * kTile / 16;
+    constexpr int kPart = 2 * kTile * (D + 2), kChunks = 2 * kTile / kJoinRows, kVec = kJoinRows * (D / 4) / kJoinThreads;
     const int first = blockIdx.x / kChunks, chunk = blockIdx.x % kChunks;
     const SplitUnit u = a.split[first];
     if (u.last_cta < 0) return;
@@ -796,24 +798,55 @@ __global__ void __launch_bounds__(128) attn_block_join_kernel(const AttnArgs a) 
     BlockRequest rq;
     rq.load(a, u.b, 0, 0);
     const int rows = rq.rows_of(u.tile);
-    auto part_of = [&](int i) { return a.part + ((long long)(first + i) * 2 + (i == 0 ? 1 : 0)) * kPart; };
-    for (int i = threadIdx.x; i < 16 * (D / 4); i += 128) {
-        const int row = chunk * 16 + i / (D / 4), ch = (i % (D / 4)) * 4;
-        if (row >= rows) continue;
-        float top = -CUDART_INF_F, sum = 0.0f;
-        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = 0; w < n; ++w) top = fmaxf(top, part_of(w)[2 * kTile * D + row]);
-        for (int w = 0; w < n; ++w) {
-            const float *p = part_of(w);
-            const float m = p[2 * kTile * D + row], f = m == top ? 1.0f : ex2_approx(m - top);
-            const float4 y = *reinterpret_cast<const float4 *>(p + (long long)row * D + ch);
-            x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
-            sum = fmaf(p[2 * kTile * D + 2 * kTile + row], f, sum);
+    if (chunk * kJoinRows >= rows) return;
+    const float *base = a.part + (long long)first * 2 * kPart;
+    auto part_of = [&](int i) { return base + (long long)(2 * i + (i == 0 ? 1 : 0)) * kPart; };
+    float4 x[kVec];
+    float m[kVec], l[kVec];
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+        x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        m[k] = -CUDART_INF_F;
+        l[k] = 0.0f;
+    }
+    for (int i0 = 0; i0 < n; i0 += kJoinTurn) {
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) {
+            const int i = threadIdx.x + k * kJoinThreads, row = chunk * kJoinRows + i / (D / 4), ch = (i % (D / 4)) * 4;
+            float4 y[kJoinTurn];
+            float my[kJoinTurn], ly[kJoinTurn];
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                const bool ok = i0 + w < n && row < rows;
+                const float *p = part_of(i0 + w);
+                my[w] = ok ? __ldg(p + 2 * kTile * D + row) : -CUDART_INF_F;
+                ly[w] = ok ? __ldg(p + 2 * kTile * D + 2 * kTile + row) : 0.0f;
+                y[w] = ok ? __ldg(reinterpret_cast<const float4 *>(p + (long long)row * D + ch)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            float top = m[k];
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) top = fmaxf(top, my[w]);
+            const float keep = m[k] == top ? 1.0f : ex2_approx(m[k] - top);
+            m[k] = top;
+            x[k].x *= keep; x[k].y *= keep; x[k].z *= keep; x[k].w *= keep;
+            l[k] *= keep;
+#pragma unroll
+            for (int w = 0; w < kJoinTurn; ++w) {
+                const float f = my[w] == top ? 1.0f : ex2_approx(my[w] - top);
+                x[k].x = fmaf(y[w].x, f, x[k].x); x[k].y = fmaf(y[w].y, f, x[k].y);
+                x[k].z = fmaf(y[w].z, f, x[k].z); x[k].w = fmaf(y[w].w, f, x[k].w);
+                l[k] = fmaf(ly[w], f, l[k]);
+            }
         }
-        const float inv = 1.0f / sum;
+    }
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+        const int i = threadIdx.x + k * kJoinThreads, row = chunk * kJoinRows + i / (D / 4), ch = (i % (D / 4)) * 4;
+        if (row >= rows) continue;
+        const float inv = 1.0f / l[k];
         const int rr = u.tile * 2 * kTile + row, qi = rr / a.group;
         *reinterpret_cast<uint2 *>(a.out + ((long long)(rq.row0 + qi) * a.Hq + u.h * a.group + rr - qi * a.group) * D + ch) =
-            sum == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv));
+            l[k] == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack2(x[k].x * inv, x[k].y * inv), pack2(x[k].z * inv, x[k].w * inv));
     }
 }
 
@@ -826,7 +859,7 @@ cudaError_t launch(const AttnArgs &a, int grid, cudaStream_t st) {
     attn_block_kernel<D><<<grid, kBlockThreads, smem, st>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    return launch_dependent(attn_block_join_kernel<D>, (unsigned)grid * (2 * kTile / 16), 128, 0, st, a, true);
+    return launch_dependent(attn_block_join_kernel<D>, (unsigned)grid * (2 * kTile / kJoinRows), kJoinThreads, 0, st, a, true);
 }
 
 }  // namespace
