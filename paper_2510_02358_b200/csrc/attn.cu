@@ -489,11 +489,11 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
 }
 
 // Joins the partial results of one unit that crossed the shares of several CTAs, in their order.  A long request alone may
-// leave one from every CTA: they are taken 16 at a time, all loads of a turn in flight together.
-constexpr int kJoinThreads = 256, kJoinTurn = 16;
+// leave one from every CTA: they are taken 16 or 32 at a time, all loads of a turn in flight together.
+constexpr int kJoinThreads = 256;
 template <int D, int NT>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a) {
-    constexpr int kRows = 8 * NT, kMt = D / 16, kFrag = NT * kMt * 4 * 32, kPart = kFrag + 2 * kRows;
+    constexpr int kRows = 8 * NT, kMt = D / 16, kFrag = NT * kMt * 4 * 32, kPart = kFrag + 2 * kRows, kJoinTurn = NT == 1 ? 32 : 16;
     constexpr int kPairs = NT * kMt * 2 * 32 / kJoinThreads > 0 ? NT * kMt * 2 * 32 / kJoinThreads : 1;
     __shared__ float s_f[kJoinTurn][kRows], s_keep[kRows], s_m[kRows], s_l[kRows];
     grid_dependency_wait();
@@ -595,8 +595,8 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
         return s;
     }
     s.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-    s.warps = s.nt == 1 ? 8 : 4;
-    s.ctas_sm = s.nt == 2 || (s.nt == 4 && D == 64) ? 3 : 2;
+    s.warps = 4;
+    s.ctas_sm = s.nt == 1 ? 4 : s.nt == 2 || D == 64 ? 3 : 2;
     s.unroll = s.nt == 4 ? 1 : 2;
     s.grid = sm_count() * s.ctas_sm;
     s.part_bytes = ((size_t)s.nt * D * 8 + 16 * s.nt) * sizeof(float);
@@ -675,10 +675,10 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     const int grid = (int)(most < s.grid ? most : s.grid);
     cudaError_t e;
     if (D == 64)
-        e = s.nt == 1 ? launch_stream<64, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<64, 2, 4, 3, 2, 3>(a, grid, st)
+        e = s.nt == 1 ? launch_stream<64, 1, 4, 4, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<64, 2, 4, 3, 2, 3>(a, grid, st)
                       : launch_stream<64, 4, 4, 3, 1, 4>(a, grid, st);
     else
-        e = s.nt == 1 ? launch_stream<128, 1, 8, 2, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<128, 2, 4, 3, 2, 3>(a, grid, st)
+        e = s.nt == 1 ? launch_stream<128, 1, 4, 4, 2, 3>(a, grid, st) : s.nt == 2 ? launch_stream<128, 2, 4, 3, 2, 3>(a, grid, st)
                       : launch_stream<128, 4, 4, 2, 1, 4>(a, grid, st);
     DSP_CUDA_TRY(e);
     return DSP_OK;
