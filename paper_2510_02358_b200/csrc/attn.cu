@@ -44,14 +44,25 @@ __device__ __forceinline__ uint32_t biased(uint32_t w, int i) {
     asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(y) : "r"(w >> (4 * i)));
     return y;
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+// A bulk copy into this CTA's shared memory, counted by a barrier there.
+__device__ __forceinline__ void copy_bulk(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void await_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
+__device__ __forceinline__ bool bytes_here(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (true) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if (clock64() - t0 > kWaitClocks) return false;
+    }
+}
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -109,16 +120,20 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     constexpr int kFrag = NT * kMt * 4 * 32;                      // floats of a partial output, in fragment order
     constexpr int kStage = kU * Kv4<D>::kRunBytes, kRing = kStages * kStage;
     // a ring of kStages iterations' codes for each warp; after a segment the same place takes its output
-    extern __shared__ __align__(16) uint8_t s_dyn[];
+    extern __shared__ __align__(128) uint8_t s_dyn[];
     float (*s_o)[NT * kMt * 4][32] = reinterpret_cast<float (*)[NT * kMt * 4][32]>(s_dyn);
     __shared__ float s_m[kW][kRows], s_l[kW][kRows], s_top[kRows], s_sum[kRows];
     __shared__ __nv_bfloat16 *s_out[kRows];
+    __shared__ uint64_t s_bars[kW][kStages];
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint2 s_q[kQueriesShared ? NT : 1][kQueriesShared ? kKs : 1][32];
     __shared__ float s_qs[kRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     grid_launch_dependents();                                     // the join's CTAs may come as soon as there is room
+    if (threadIdx.x < kW * kStages)
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"((uint32_t)__cvta_generic_to_shared(&s_bars[0][0] + threadIdx.x)) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (threadIdx.x == 0) a.split[blockIdx.x].last_cta = -1;
     enter_line<Request>(a, kRows, kStep, 1, s_scan, &s_line);
     long long at = s_line.begin;
@@ -128,6 +143,9 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     const long long head_bytes = (long long)runs_page * Kv4<D>::kRunBytes, block_bytes = head_bytes * a.Hkv;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_dyn) + warp * kRing;
+    const uint32_t bars = (uint32_t)__cvta_generic_to_shared(&s_bars[warp][0]);
+    uint32_t phases = 0u;                                         // parity that each stage's barrier is waited for with
+    bool lost = false;
     Request rq;
     long long before = s_line.before;
     rq.load(a, s_line.b, kRows, kStep);
@@ -146,46 +164,57 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         int run = (step0 * kW + warp) * kU;
         const int run_end = min(step1 * kW * kU, (max(stop, 0) + 15) >> 4);
         const int32_t *table = a.table + (long long)rq.b * a.table_stride;
-        const uint8_t *head = a.cache + h * head_bytes + lane * 16;
-        // lane l looks up the run that is l / kU iterations ahead (its l % kU-th), the whole warp at once
-        int ids = -1, ids_sub = 0, ids_left = 0, ids_run = run;
+        const uint8_t *head = a.cache + h * head_bytes;
+        // lane l looks up the run that is l / kU iterations ahead (its l % kU-th), the whole warp at once and a turn ahead
+        int ids = -1, ids_sub = 0, ids_left = 0, next_ids = -1, next_sub = 0, next_run = run;
         auto lookup = [&]() {
-            const int mine = ids_run + (lane / kU) * (kW * kU) + lane % kU;
-            ids = -1;
+            ids = next_ids;
+            ids_sub = next_sub;
+            ids_left = 32;
+            const int mine = next_run + (lane / kU) * (kW * kU) + lane % kU;
+            next_ids = -1;
             if (mine < run_end) {
                 const int blk = runs_page == 1 ? mine : mine / runs_page;
-                ids = table[blk];
-                ids_sub = mine - blk * runs_page;
-                if (ids >= a.n_blocks) ids = -1;
+                next_ids = __ldg(table + blk);
+                next_sub = mine - blk * runs_page;
+                if (next_ids >= a.n_blocks) next_ids = -1;
             }
-            ids_run += (32 / kU) * (kW * kU);
-            ids_left = 32;
+            next_run += (32 / kU) * (kW * kU);
         };
+        lookup();
+        ids_left = 0;
         uint32_t there = 0u;                                      // per stage and run: whether its block exists
-        auto fetch = [&](int stage, bool more) {
-            if (more) {
-                if (ids_left == 0) lookup();
+        auto fetch = [&](int stage) {
+            if (ids_left == 0) lookup();
+            const uint32_t dst = ring + stage * kStage, bar = bars + 8 * stage;
+            int id[kU], sub[kU];
+            uint32_t bytes = 0u;
 #pragma unroll
-                for (int x = 0; x < kU; ++x) {
-                    const int from = 32 - ids_left + x;
-                    const int id = __shfl_sync(0xFFFFFFFFu, ids, from), sub = __shfl_sync(0xFFFFFFFFu, ids_sub, from);
-                    const uint32_t bit = 1u << (stage * kU + x), dst = ring + stage * kStage + x * Kv4<D>::kRunBytes + lane * 16;
-                    there &= ~bit;
-                    if (id >= 0) {
-                        there |= bit;
-                        const uint8_t *src = head + id * block_bytes + (long long)sub * Kv4<D>::kRunBytes;
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) copy16(dst + i * 512, src + i * 512);
-                        copy4(dst - lane * 12 + Kv4<D>::kParamOff, src - lane * 12 + Kv4<D>::kParamOff);
-                    }
-                }
-                ids_left -= kU;
+            for (int x = 0; x < kU; ++x) {
+                id[x] = __shfl_sync(0xFFFFFFFFu, ids, 32 - ids_left + x);
+                sub[x] = __shfl_sync(0xFFFFFFFFu, ids_sub, 32 - ids_left + x);
+                const uint32_t bit = 1u << (stage * kU + x);
+                there = id[x] >= 0 ? there | bit : there & ~bit;
+                bytes += id[x] >= 0 ? Kv4<D>::kRunBytes : 0;
             }
-            copies_done();                                        // an empty group keeps the count of groups that of iterations
+            ids_left -= kU;
+            if (lane == 0) {
+                expect_bytes(bar, bytes);
+                const uint8_t *src = head + id[0] * block_bytes + (long long)sub[0] * Kv4<D>::kRunBytes;
+                if (kU == 2 && id[0] >= 0 && id[0] == id[kU - 1]) {      // neighbours in a block: one piece
+                    copy_bulk(dst, src, kU * Kv4<D>::kRunBytes, bar);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < kU; ++x)
+                        if (id[x] >= 0)
+                            copy_bulk(dst + x * Kv4<D>::kRunBytes, head + id[x] * block_bytes + (long long)sub[x] * Kv4<D>::kRunBytes, Kv4<D>::kRunBytes, bar);
+                }
+            }
         };
         int ahead = run, stage = 0;                               // the first copies are under way while the queries come
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i, ahead += kW * kU) fetch(i, ahead < run_end);
+        for (int i = 0; i < kStages - 1; ++i, ahead += kW * kU)
+            if (ahead < run_end && !lost) fetch(i);
         auto load_queries = [&](int t, uint32_t (&x)[kKs * 2]) {
             const int row = row_first + t * 8 + r, i = row / a.group;
             const uint4 *src = reinterpret_cast<const uint4 *>(a.q + (long long)(rq.row0 + i) * a.q_t +
@@ -249,9 +278,16 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
             }
         }
         for (; run < run_end; run += kW * kU, ahead += kW * kU) {
-            await_copies<kStages - 2>();
-            __syncwarp();                                         // every lane's copies have landed, and all have read the stage before
-            fetch(stage == 0 ? kStages - 1 : stage - 1, ahead < run_end);
+            // the stage's bytes are here (a wait that has run out loses the row's sums, below, and is not waited for again)
+            if (!lost) lost = !__all_sync(0xFFFFFFFFu, bytes_here(bars + 8 * stage, (phases >> stage) & 1u));
+            phases ^= 1u << stage;
+            __syncwarp();                                         // all lanes have read the stage before
+            if (ahead < run_end && !lost) fetch(stage == 0 ? kStages - 1 : stage - 1);
+            if (lost) {                                           // what is still under way has to land before the CTA may end
+#pragma unroll 1
+                for (int i = 0; i < kStages; ++i) bytes_here(bars + 8 * i, (phases >> i) & 1u);
+                break;
+            }
             const uint32_t codes = ring + stage * kStage + lane * 16, params = ring + stage * kStage + Kv4<D>::kParamOff + r * 8;
             const uint32_t here = there >> (stage * kU);
             stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -400,6 +436,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     l[t][e] += __shfl_xor_sync(0xFFFFFFFFu, l[t][e], x);
                     zs[t][e] += __shfl_xor_sync(0xFFFFFFFFu, zs[t][e], x);
                 }
+                if (lost) l[t][e] = CUDART_NAN_F;
                 if (r == 0) {
                     s_m[warp][t * 8 + 2 * c + e] = (unset >> (2 * t + e)) & 1u ? -CUDART_INF_F : -nb[t][e];
                     s_l[warp][t * 8 + 2 * c + e] = l[t][e];
@@ -484,7 +521,9 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
             before += rq.length(a.Hkv);
             rq.load(a, rq.b + 1, kRows, kStep);
         }
-        __syncthreads();                                          // s_o and s_m are written anew
+        // the places of s_o, written and read as ordinary memory, are the copies' again
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
     }
 }
 
