@@ -54,13 +54,14 @@ __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
 }
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
 __device__ __forceinline__ bool bytes_here(uint32_t bar, uint32_t parity) {
-    const long long t0 = clock64();
+    long long t0 = 0;
     while (true) {
         uint32_t ok;
         asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
-        if (clock64() - t0 > kWaitClocks) return false;
+        if (t0 == 0) t0 = clock64();
+        else if (clock64() - t0 > kWaitClocks) return false;
     }
 }
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
@@ -165,51 +166,49 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         const int run_end = min(step1 * kW * kU, (max(stop, 0) + 15) >> 4);
         const int32_t *table = a.table + (long long)rq.b * a.table_stride;
         const uint8_t *head = a.cache + h * head_bytes;
-        // lane l looks up the run that is l / kU iterations ahead (its l % kU-th), the whole warp at once and a turn ahead
-        int ids = -1, ids_sub = 0, ids_left = 0, next_ids = -1, next_sub = 0, next_run = run;
+        // Lane l looks up the run that is l / kU iterations ahead (its l % kU-th), the whole warp at once and a turn ahead; `valid`
+        // and `joined` have a bit for each lane: its run's block exists, and the run after it lies next to it in the cache.
+        const uint8_t *place = nullptr, *next_place = nullptr;
+        int left = 0, next_run = run;
+        uint32_t valid = 0u, joined = 0u;
         auto lookup = [&]() {
-            ids = next_ids;
-            ids_sub = next_sub;
-            ids_left = 32;
+            place = next_place;
+            valid = __ballot_sync(0xFFFFFFFFu, place != nullptr);
+            const unsigned long long here = (unsigned long long)place;
+            joined = __ballot_sync(0xFFFFFFFFu, here + Kv4<D>::kRunBytes == __shfl_down_sync(0xFFFFFFFFu, here, 1));
+            left = 32;
             const int mine = next_run + (lane / kU) * (kW * kU) + lane % kU;
-            next_ids = -1;
+            next_place = nullptr;
             if (mine < run_end) {
-                const int blk = runs_page == 1 ? mine : mine / runs_page;
-                next_ids = __ldg(table + blk);
-                next_sub = mine - blk * runs_page;
-                if (next_ids >= a.n_blocks) next_ids = -1;
+                const int blk = runs_page == 1 ? mine : mine / runs_page, id = __ldg(table + blk);
+                if (id >= 0 && id < a.n_blocks) next_place = head + id * block_bytes + (long long)(mine - blk * runs_page) * Kv4<D>::kRunBytes;
             }
             next_run += (32 / kU) * (kW * kU);
         };
         lookup();
-        ids_left = 0;
+        left = 0;
         uint32_t there = 0u;                                      // per stage and run: whether its block exists
         auto fetch = [&](int stage) {
-            if (ids_left == 0) lookup();
-            const uint32_t dst = ring + stage * kStage, bar = bars + 8 * stage;
-            int id[kU], sub[kU];
-            uint32_t bytes = 0u;
-#pragma unroll
-            for (int x = 0; x < kU; ++x) {
-                id[x] = __shfl_sync(0xFFFFFFFFu, ids, 32 - ids_left + x);
-                sub[x] = __shfl_sync(0xFFFFFFFFu, ids_sub, 32 - ids_left + x);
-                const uint32_t bit = 1u << (stage * kU + x);
-                there = id[x] >= 0 ? there | bit : there & ~bit;
-                bytes += id[x] >= 0 ? Kv4<D>::kRunBytes : 0;
-            }
-            ids_left -= kU;
-            if (lane == 0) {
-                expect_bytes(bar, bytes);
-                const uint8_t *src = head + id[0] * block_bytes + (long long)sub[0] * Kv4<D>::kRunBytes;
-                if (kU == 2 && id[0] >= 0 && id[0] == id[kU - 1]) {      // neighbours in a block: one piece
-                    copy_bulk(dst, src, kU * Kv4<D>::kRunBytes, bar);
-                } else {
-#pragma unroll
-                    for (int x = 0; x < kU; ++x)
-                        if (id[x] >= 0)
-                            copy_bulk(dst + x * Kv4<D>::kRunBytes, head + id[x] * block_bytes + (long long)sub[x] * Kv4<D>::kRunBytes, Kv4<D>::kRunBytes, bar);
+            if (left == 0) lookup();
+            const int from = 32 - left;
+            constexpr uint32_t kAll = (1u << kU) - 1u;
+            const uint32_t dst = ring + stage * kStage, bar = bars + 8 * stage, ok = (valid >> from) & kAll;
+            there = (there & ~(kAll << (stage * kU))) | ok << (stage * kU);
+            const uint8_t *src = (const uint8_t *)__shfl_sync(0xFFFFFFFFu, (unsigned long long)place, from);
+            if (kU == 2 && ok == kAll && ((joined >> from) & 1u)) {      // neighbours: one piece
+                if (lane == 0) {
+                    expect_bytes(bar, kStage);
+                    copy_bulk(dst, src, kStage, bar);
+                }
+            } else {
+                const uint8_t *src2 = kU == 2 ? (const uint8_t *)__shfl_sync(0xFFFFFFFFu, (unsigned long long)place, from + kU - 1) : nullptr;
+                if (lane == 0) {
+                    expect_bytes(bar, __popc(ok) * Kv4<D>::kRunBytes);
+                    if (ok & 1u) copy_bulk(dst, src, Kv4<D>::kRunBytes, bar);
+                    if (kU == 2 && (ok & 2u)) copy_bulk(dst + Kv4<D>::kRunBytes, src2, Kv4<D>::kRunBytes, bar);
                 }
             }
+            left -= kU;
         };
         int ahead = run, stage = 0;                               // the first copies are under way while the queries come
 #pragma unroll
@@ -235,7 +234,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         };
         // queries of lane's row r, its quarter of the channels in the cache's order
         uint32_t q[kQueriesShared ? 1 : NT][kKs * 2];
-        float qs[NT][2];
+        float qs[NT][2];                                          // sums of the rows 2c, 2c + 1, times the scale
         if (kQueriesShared) {
             // as operand fragments, each by one warp
             __syncthreads();                                      // the last segment's have been used
@@ -251,7 +250,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) qs[t][e] = s_qs[t * 8 + 2 * c + e];
+                for (int e = 0; e < 2; ++e) qs[t][e] = s_qs[t * 8 + 2 * c + e] * a.scale_log2;
         } else {
 #pragma unroll
             for (int t = 0; t < NT; ++t) load_queries(t, q[kQueriesShared ? 0 : t]);
@@ -259,7 +258,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
             for (int t = 0; t < NT; ++t) {
                 const float sum = query_sum(q[kQueriesShared ? 0 : t]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4);
+                for (int e = 0; e < 2; ++e) qs[t][e] = __shfl_sync(0xFFFFFFFFu, sum, (2 * c + e) * 4) * a.scale_log2;
             }
         }
         // Scores are formed relative to the rows' reference -nb (base 2).  `unset`: rows of this lane (bit 2t + e) that have none
@@ -319,7 +318,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                 for (int y = 0; y < 2; ++y) {
                     const uint2 p = lds64(params + x * Kv4<D>::kRunBytes + y * 64);
                     const float ks = bf16_lo(p.x), kz = bf16_hi(p.x);
-                    const float ka = ks * a.scale_log2, kb = fmaf(-kBias, ks, kz) * a.scale_log2;
+                    const float ka = ks * a.scale_log2, kb = fmaf(-kBias, ks, kz);
                     va[x][y] = bf16_lo(p.y);
                     vz[x][y] = fmaf(8.0f, va[x][y], bf16_hi(p.y));
 #pragma unroll
