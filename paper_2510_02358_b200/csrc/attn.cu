@@ -126,6 +126,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     __shared__ float s_m[kW][kRows], s_l[kW][kRows], s_top[kRows], s_sum[kRows];
     __shared__ __nv_bfloat16 *s_out[kRows];
     __shared__ uint64_t s_bars[kW][kStages];
+    __shared__ int s_lim[kRows], s_query[kRows];                  // tokens that a row sees (before the bits), its query
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint2 s_q[kQueriesShared ? NT : 1][kQueriesShared ? kKs : 1][32];
@@ -158,6 +159,12 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         // tokens below `safe` are seen by every row of the tile, none from `stop` on by any
         const int past = rq.kv - rq.n_new;                        // negative if more is new than there is
         const int i_first = row_first / a.group, i_last = (row_first + rows_here - 1) / a.group;
+        if (threadIdx.x < kRows) {
+            const int row = row_first + threadIdx.x, i = row / a.group;
+            s_query[threadIdx.x] = i;
+            s_lim[threadIdx.x] = row >= rq.rows ? 0 : a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i + 1) : rq.kv;
+        }
+        __syncthreads();
         const int safe = a.mask_kind == DSP_MASK_CAUSAL ? past + i_first + 1 : a.mask_kind == DSP_MASK_FULL ? rq.kv : past;
         const int stop = a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i_last + 1) : rq.kv;
 
@@ -237,7 +244,6 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         float qs[NT][2];                                          // sums of the rows 2c, 2c + 1, times the scale
         if (kQueriesShared) {
             // as operand fragments, each by one warp
-            __syncthreads();                                      // the last segment's have been used
 #pragma unroll
             for (int t = warp; t < NT; t += kW) {
                 load_queries(t, q[0]);
@@ -265,6 +271,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         // yet, because nothing of what they see has come; rows beyond the unit's keep 0.
         float o[NT][kMt][4], ps[NT][4], nb[NT][2], l[NT][2], zs[NT][2];
         uint32_t unset = 0u;
+        bool started = false;                                     // nothing to rescale in the first iteration
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -339,12 +346,11 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int u = (run + x) * 16 + r + 8 * (e >> 1), row = row_first + t * 8 + 2 * c + (e & 1), i = row / a.group;
-                            const int lim = row >= rq.rows ? 0 : a.mask_kind == DSP_MASK_CAUSAL ? min(rq.kv, past + i + 1) : rq.kv;
-                            bool ok = ((here >> x) & 1u) && run + x < run_end && u < lim;
+                            const int u = (run + x) * 16 + r + 8 * (e >> 1), row = t * 8 + 2 * c + (e & 1);
+                            bool ok = ((here >> x) & 1u) && run + x < run_end && u < s_lim[row];
                             if (a.mask_kind == DSP_MASK_BITS && ok && u >= past) {
                                 const int j = u - past;
-                                ok = j < a.words * 32 && ((__ldg(a.bits + (long long)(rq.row0 + i) * a.words + (j >> 5)) >> (j & 31)) & 1u);
+                                ok = j < a.words * 32 && ((__ldg(a.bits + (long long)(rq.row0 + s_query[row]) * a.words + (j >> 5)) >> (j & 31)) & 1u);
                             }
                             if (!ok) s[x][t][e] = -CUDART_INF_F;
                             seen |= (ok ? 1u : 0u) << ((x * NT + t) * 4 + e);
@@ -374,13 +380,16 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                         nb[t][e] -= by;
 #pragma unroll
                         for (int x = 0; x < kU; ++x) { s[x][t][e] -= by; s[x][t][e + 2] -= by; }
-                        l[t][e] *= keep;
-                        zs[t][e] *= keep;
-                        ps[t][e] *= keep;
+                        if (started) {
+                            l[t][e] *= keep;
+                            zs[t][e] *= keep;
+                            ps[t][e] *= keep;
 #pragma unroll
-                        for (int j = 0; j < kMt; ++j) { o[t][j][e] *= keep; o[t][j][e + 2] *= keep; }
+                            for (int j = 0; j < kMt; ++j) { o[t][j][e] *= keep; o[t][j][e + 2] *= keep; }
+                        }
                     }
             }
+            started = true;
 #pragma unroll
             for (int x = 0; x < kU; ++x) {
                 uint32_t p[NT][2];
@@ -461,7 +470,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     float sum = 0.0f;
 #pragma unroll
                     for (int w = 0; w < kW; ++w) sum += s_m[w][row] == top ? s_l[w][row] : s_l[w][row] * ex2_approx(s_m[w][row] - top);
-                    const int rr = row_first + row, q_i = rr / a.group;
+                    const int rr = row_first + row, q_i = s_query[row];
                     s_top[row] = top;
                     s_sum[row] = sum;
                     s_out[row] = row < rows_here ? a.out + ((long long)(rq.row0 + q_i) * a.Hq + h * a.group + rr - q_i * a.group) * D : nullptr;
