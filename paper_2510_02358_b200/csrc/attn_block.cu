@@ -12,7 +12,7 @@
 //               back into the scores' columns as the second product's operand
 //   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
 //               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
-//   warp 16     one lane issues the products: S = Q K^T, O += P V
+//   warps 16-17 one lane each issues the products of a slot: S = Q K^T, O += P V
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
@@ -29,7 +29,8 @@
 namespace dsp {
 namespace {
 
-constexpr int kSoftWarps = 8, kFillWarps = 8, kBlockThreads = (kSoftWarps + kFillWarps + 1) * 32;
+constexpr int kSoftWarps = 8, kFillWarps = 8, kProductWarps = 2;
+constexpr int kBlockThreads = (kSoftWarps + kFillWarps + kProductWarps) * 32;
 constexpr int kTile = 128;                       // query rows of a slot, tokens of a tile
 constexpr int kHalf = kTile / 2;                 // tokens whose scores are formed and exponentiated at once
 constexpr int kRunsTile = kTile / 16;
@@ -423,69 +424,73 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
 }
 
 // ---------------------------------------------------------------------------------------- products
-// The whole warp walks, one lane issues.
+// One warp for each slot: the steps between two products (waits, commits) of one fall beside the products of the other.  The
+// whole warp walks, one lane issues.  A slot's own products are in the order of issue, which is all that its buffers need.
 template <int D>
 __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem, uint32_t q_at, uint32_t k_at,
-                                             uint32_t v_at, Bars *bars, volatile int *dead, int lane) {
-    constexpr uint32_t kTileBytes = D * 2 * kTile;
+                                             uint32_t v_at, Bars *bars, volatile int *dead, uint32_t slot, int lane) {
+    constexpr uint32_t kTileBytes = D * 2 * kTile, kBlock = kTile * 128 / 16;
     constexpr uint32_t kScore = kBf16Product | (uint32_t)(kHalf >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
     const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
     const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
-    const uint32_t score_full = smem_u32(bars->score_full), weight_ready = smem_u32(bars->weight_ready);
-    const uint32_t out_free = smem_u32(bars->out_free);
+    const uint32_t score_full = smem_u32(bars->score_full) + 16 * slot, weight_ready = smem_u32(bars->weight_ready) + 16 * slot;
+    const uint32_t out_free = smem_u32(bars->out_free) + 8 * slot;
     const uint64_t q_desc = tile_desc(q_at, 16, 1024), k_desc = tile_desc(k_at, 16, 1024), v_desc = tile_desc(v_at, kTile * 128, 1024);
-    walk_enter(w, a, line, lane);
+    const uint32_t s_at = tmem + slot * kTile, o_at = tmem + 2 * kTile + slot * D;
     const uint32_t lead = elected();
-    uint32_t seg = 0u, tiles = 0u, uses[2] = {0u, 0u};
+    walk_enter(w, a, line, lane);
+    uint32_t seg = 0u, tiles = 0u, uses = 0u;
     while (walk_next(w, a, lane)) {
         // the same in every lane, which the compiler shall know
         const uint32_t wide = __shfl_sync(0xFFFFFFFFu, w.wide() ? 1u : 0u, 0), n = __shfl_sync(0xFFFFFFFFu, (uint32_t)(w.step1 - w.step0), 0);
-        // token tiles of each slot in this segment
-        const uint32_t of0 = wide ? n : (n + 1) >> 1, of1 = wide ? n : n >> 1;
+        const uint32_t mine = wide ? n : (n + 1u - slot) >> 1;    // token tiles of this slot
         if (!warp_wait(smem_u32(&bars->query_ready), seg & 1u, dead)) return;
-        // item i: slot i & 1, its half tile i >> 1; the slots take turns
-        auto exists = [&](uint32_t i) { return (i >> 2) < ((i & 1u) ? of1 : of0); };
+        const uint64_t qa = q_desc + (wide & slot) * (kTileBytes >> 4);
+        // item i: half i & 1 of the slot's token tile i >> 1
         auto scores = [&](uint32_t i) {
-            const uint32_t slot = i & 1u, buf = (i >> 1) & 1u, t = tiles + (wide ? i >> 2 : 2u * (i >> 2) + slot), st = t & 1u;
-            if (buf == 0u && !(wide & slot) && !warp_wait(key_full + 8 * st, (t >> 1) & 1u, dead)) return false;
+            const uint32_t buf = i & 1u, t = tiles + (wide ? i >> 1 : 2u * (i >> 1) + slot), st = t & 1u;
+            if (buf == 0u && !warp_wait(key_full + 8 * st, (t >> 1) & 1u, dead)) return false;
             fence_after();
-            const uint64_t qa = q_desc + (wide & slot) * (kTileBytes >> 4), ka = k_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
-            const uint32_t d = tmem + slot * kTile + buf * kHalf;
+            const uint64_t ka = k_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
+            const uint32_t d = s_at + buf * kHalf;
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                constexpr uint32_t kBlock = kTile * 128 / 16;
+            for (int ks = 0; ks < D / 16; ++ks)
                 product_ss(d, qa + (ks >> 2) * kBlock + (ks & 3) * 2, ka + (ks >> 2) * kBlock + (ks & 3) * 2, kScore, ks > 0, lead);
+            commit_to(score_full + 8 * buf, lead);
+            if (buf) {                                             // a stage is free when both slots have used it, or one twice as much
+                commit_to(key_empty + 8 * st, lead);
+                if (!wide) commit_to(key_empty + 8 * st, lead);
             }
-            if (buf && (!wide || slot)) commit_to(key_empty + 8 * st, lead);
-            commit_to(score_full + 8 * (slot * 2 + buf), lead);
             return true;
         };
         auto outputs = [&](uint32_t i) {
-            const uint32_t slot = i & 1u, buf = (i >> 1) & 1u, t = tiles + (wide ? i >> 2 : 2u * (i >> 2) + slot), st = t & 1u;
-            if (!warp_wait(weight_ready + 8 * (slot * 2 + buf), ((slot ? uses[1] : uses[0]) + (i >> 2)) & 1u, dead)) return false;
-            if (buf == 0u && !(wide & slot) && !warp_wait(val_full + 8 * st, (t >> 1) & 1u, dead)) return false;
+            const uint32_t buf = i & 1u, t = tiles + (wide ? i >> 1 : 2u * (i >> 1) + slot), st = t & 1u;
+            if (buf == 0u && !warp_wait(val_full + 8 * st, (t >> 1) & 1u, dead)) return false;
+            if (!warp_wait(weight_ready + 8 * buf, (uses + (i >> 1)) & 1u, dead)) return false;
             fence_after();
             const uint64_t va = v_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
-            const uint32_t d = tmem + 2 * kTile + slot * D, p = tmem + slot * kTile + buf * kHalf;
+            const uint32_t p = s_at + buf * kHalf;
 #pragma unroll
-            for (int ks = 0; ks < kHalf / 16; ++ks) product_ts(d, p + ks * 8, va + ks * 128, kOut, i > 1u || ks > 0, lead);
-            if (buf && (!wide || slot)) commit_to(val_empty + 8 * st, lead);
-            commit_to(out_free + 8 * slot, lead);
+            for (int ks = 0; ks < kHalf / 16; ++ks) product_ts(o_at, p + ks * 8, va + ks * 128, kOut, i > 0u || ks > 0, lead);
+            commit_to(out_free, lead);
+            if (buf) {
+                commit_to(val_empty + 8 * st, lead);
+                if (!wide) commit_to(val_empty + 8 * st, lead);
+            }
             return true;
         };
+        const uint32_t items = 2u * mine;
 #pragma unroll 1
-        for (uint32_t i = 0; i < 4u; ++i)
-            if (exists(i) && !scores(i)) return;
+        for (uint32_t i = 0; i < min(items, 2u); ++i)
+            if (!scores(i)) return;
 #pragma unroll 1
-        for (uint32_t i = 0; (i >> 2) < of0; ++i) {
-            if (!exists(i)) continue;
+        for (uint32_t i = 0; i < items; ++i) {
             if (!outputs(i)) return;
-            if (exists(i + 4u) && !scores(i + 4u)) return;
+            if (i + 2u < items && !scores(i + 2u)) return;
         }
         commit_to(smem_u32(&bars->out_done), lead);
         tiles += n;
-        uses[0] += of0;
-        uses[1] += of1;
+        uses += mine;
         ++seg;
         walk_leave(w, a, lane);
     }
@@ -735,7 +740,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint32_t s_tmem;
-    __shared__ Walk s_walk[kSoftWarps + kFillWarps + 1];
+    __shared__ Walk s_walk[kBlockThreads / 32];
     __shared__ int s_dead;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t base = (smem_u32(s_raw) + 1023u) & ~1023u;
@@ -747,8 +752,8 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_u32(&s_bars.key_full[i]), kFillWarps);
             bar_init(smem_u32(&s_bars.val_full[i]), kFillWarps);
-            bar_init(smem_u32(&s_bars.key_empty[i]), 1);
-            bar_init(smem_u32(&s_bars.val_empty[i]), 1);
+            bar_init(smem_u32(&s_bars.key_empty[i]), kProductWarps);
+            bar_init(smem_u32(&s_bars.val_empty[i]), kProductWarps);
             bar_init(smem_u32(&s_bars.out_free[i]), 1);
         }
         for (int i = 0; i < 4; ++i) {
@@ -756,7 +761,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
             bar_init(smem_u32(&s_bars.weight_ready[i]), kSoftWarps / 2);
         }
         bar_init(smem_u32(&s_bars.query_ready), kSoftWarps);
-        bar_init(smem_u32(&s_bars.out_done), 1);
+        bar_init(smem_u32(&s_bars.out_done), kProductWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kSoftWarps + kFillWarps) {
@@ -773,7 +778,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         } else if (warp < kSoftWarps + kFillWarps) {
             fill_role<D>(a, s_line, s_walk[warp], k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
         } else {
-            if (warp == kSoftWarps + kFillWarps) product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, &s_dead, lane);
+            product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, &s_dead, (uint32_t)(warp - kSoftWarps - kFillWarps), lane);
         }
     }
     __syncwarp();
