@@ -2,11 +2,10 @@
 // projections and the attention (the norm of each query and key head, the rotation by position,
 // the 4-bit form of keys and values), in one pass over them.
 //
-// A head of a token is a row of D channels on D / 8 neighbouring lanes, eight channels a lane: the
-// row's sum of squares and extrema come from shuffles inside those lanes, so nothing goes through
-// shared memory and the pass is one read and one write of the rows.
-// A group of lanes takes kHeads heads of one token: their loads are in flight together, and the
-// token's angles are read once for them.
+// A head of a token is a row of D channels on a few neighbouring lanes: the row's sum of squares and
+// extrema come from shuffles inside those lanes, so nothing goes through shared memory and the pass is
+// one read and one write of the rows.  A group of lanes takes kHeads heads of one token: their loads
+// are in flight together, and the token's angles are read once for them.
 //
 // What is written is a function of the row alone: the sum of squares is a tree of neighbouring
 // channels (in a lane, then over the lanes by xor 1, 2, 4, 8), and no product is fused with a sum,
@@ -101,6 +100,47 @@ template <> struct Quad<float> {
     static __device__ __forceinline__ Two rounded(Two x) { return x; }
 };
 
+// Eight neighbouring channels: pairs (0,1) (2,3) (4,5) (6,7).
+template <typename DT> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool vec) {
+        if (vec) {
+            v = ldg_stream(p);
+        } else {
+            const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
+            v = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+        }
+    }
+    __device__ __forceinline__ void get(Two (&x)[4]) const {
+        x[0] = {bf16_lo(v.x), bf16_hi(v.x)}; x[1] = {bf16_lo(v.y), bf16_hi(v.y)};
+        x[2] = {bf16_lo(v.z), bf16_hi(v.z)}; x[3] = {bf16_lo(v.w), bf16_hi(v.w)};
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const Two (&x)[4]) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(Quad<__nv_bfloat16>::pack(x[0]), Quad<__nv_bfloat16>::pack(x[1]),
+                                                   Quad<__nv_bfloat16>::pack(x[2]), Quad<__nv_bfloat16>::pack(x[3]));
+    }
+};
+template <> struct Eight<float> {
+    Quad<float> q[2];
+    __device__ __forceinline__ void load(const float *p, bool vec) { q[0].load(p, vec); q[1].load(p + 4, vec); }
+    __device__ __forceinline__ void get(Two (&x)[4]) const { q[0].get(x[0], x[1]); q[1].get(x[2], x[3]); }
+    static __device__ __forceinline__ void store(float *p, const Two (&x)[4]) {
+        Quad<float>::store(p, x[0], x[1]);
+        Quad<float>::store(p + 4, x[2], x[3]);
+    }
+};
+// Sum of eight squares as a tree of neighbours.
+__device__ __forceinline__ float square_sum(const Two (&x)[4]) {
+    float s[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const Two q = mul2(x[e], x[e]);
+        s[e] = __fadd_rn(q.a, q.b);
+    }
+    return __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
+}
+
 __device__ __forceinline__ float bf16_down(float x) {
     const uint32_t b = __float_as_uint(x);
     return __uint_as_float((int32_t)b < 0 ? (b + 0xFFFFu) & 0xFFFF0000u : b & 0xFFFF0000u);
@@ -118,32 +158,49 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
     return y;
 }
 
-// One scale and one offset for the row, and the codes of a lane's two quads as they lie in half a word
-// (bits 0-7: channels 0 and 2, bits 16-23: channels 1 and 3).  kLanes lanes hold the row.
+// One scale and one offset for a row that lies on kLanes lanes, and the codes of eight channels as a word.
 //
 // A code is (x - z) / s, rounded, then rounded to a whole number.  The product with 1 / s is within 2e-6 of the quotient (which
 // is at most 15), so it has the same whole number next to it unless it lies within that of the middle between two; only lanes
 // that hold such a number (1e-5 is taken) divide.
-template <int kLanes>
-__device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2], uint32_t &params) {
-    float lo = min3(min3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a), hi = max3(max3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a);
-    lo = min3(min3(lo, x[2].b, x[3].a), x[3].b, lo);
-    hi = max3(max3(hi, x[2].b, x[3].a), x[3].b, hi);
-    const Two zero = {0.0f, 0.0f};                                 // 0 * x is NaN for an infinity or a NaN
-    const Two odd = add2(add2(mul2(x[0], zero), mul2(x[1], zero)), add2(mul2(x[2], zero), mul2(x[3], zero)));
-    hi = odd.a + odd.b == 0.0f ? hi : CUDART_INF_F;                // carries the finding through the reduction
-#pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
+struct Extrema {
+    float lo, hi;
+    bool fine;
+    __device__ __forceinline__ Extrema(const Two (&x)[4]) {
+        lo = min3(min3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a);
+        hi = max3(max3(x[0].a, x[0].b, x[1].a), x[1].b, x[2].a);
+        lo = fminf(min3(lo, x[2].b, x[3].a), x[3].b);
+        hi = fmaxf(max3(hi, x[2].b, x[3].a), x[3].b);
+        const Two zero = {0.0f, 0.0f};                             // 0 * x is NaN for an infinity or a NaN
+        const Two odd = add2(add2(mul2(x[0], zero), mul2(x[1], zero)), add2(mul2(x[2], zero), mul2(x[3], zero)));
+        fine = odd.a + odd.b == 0.0f;
     }
-    const float z = bf16_down(lo);
-    float s = bf16_up_nonneg(__fdiv_rn(__fsub_rn(hi, z), 15.0f));
-    const bool ok = hi <= 3.402823466e38f && z >= -3.402823466e38f && s <= 3.402823466e38f;
-    s = s < 1.17549435e-38f ? 0.0f : s;
-    half[0] = half[1] = 0u;
-    if (ok && s > 0.0f) {
-        const float inv = __frcp_rn(s);
+};
+struct Scale {
+    float s, z, inv;
+    bool live;                                                     // codes are not all 0
+    uint32_t params;
+    template <int kLanes> __device__ __forceinline__ void reduce(float lo, float hi, bool fine) {
+        hi = fine ? hi : CUDART_INF_F;                             // carries the finding through the reduction
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) {
+            lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
+            hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
+        }
+        z = bf16_down(lo);
+        s = bf16_up_nonneg(__fdiv_rn(__fsub_rn(hi, z), 15.0f));
+        const bool ok = hi <= 3.402823466e38f && z >= -3.402823466e38f && s <= 3.402823466e38f;
+        s = s < 1.17549435e-38f ? 0.0f : s;
+        live = ok && s > 0.0f;
+        inv = __frcp_rn(s);
+        params = ok ? (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xFFFF0000u) : 0x7FFF7FFFu;
+    }
+    // a quad's codes: bits 0-7 channels 0 and 2, bits 16-23 channels 1 and 3
+    static __device__ __forceinline__ uint32_t half_word(Two c, Two d) {
+        return __float2uint_rz(fmaf(d.b, 1048576.0f, fmaf(c.b, 65536.0f, fmaf(d.a, 16.0f, c.a))));      // below 2^24: exact
+    }
+    __device__ __forceinline__ uint32_t word(const Two (&x)[4]) const {
+        if (!live) return 0u;
         constexpr float kRound = 12582912.0f;                      // 1.5 * 2^23: adding it leaves the nearest whole number, ties to even
         Two c[4];
         float far = 0.0f;
@@ -157,20 +214,22 @@ __device__ __forceinline__ void quantise(const Two (&x)[4], uint32_t (&half)[2],
 #pragma unroll
             for (int e = 0; e < 4; ++e) c[e] = {rintf(__fdiv_rn(__fsub_rn(x[e].a, z), s)), rintf(__fdiv_rn(__fsub_rn(x[e].b, z), s))};
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)                                // below 2^24: exact
-            half[k] = __float2uint_rz(fmaf(c[2 * k + 1].b, 1048576.0f, fmaf(c[2 * k].b, 65536.0f, fmaf(c[2 * k + 1].a, 16.0f, c[2 * k].a))));
+        return half_word(c[0], c[1]) | half_word(c[2], c[3]) << 8;
     }
-    params = ok ? (__float_as_uint(s) >> 16) | (__float_as_uint(z) & 0xFFFF0000u) : 0x7FFF7FFFu;
+};
+template <int kLanes> __device__ __forceinline__ void quantise_pair(const Two (&x)[4], const Two (&y)[4], uint32_t (&words)[2], uint32_t &params) {
+    const Extrema ex(x), ey(y);
+    Scale sc;
+    sc.reduce<kLanes>(fminf(ex.lo, ey.lo), fmaxf(ex.hi, ey.hi), ex.fine && ey.fine);
+    words[0] = sc.word(x);
+    words[1] = sc.word(y);
+    params = sc.params;
 }
 
-// A lane holds two quads of its row.  kPaired: such that the channels that the rotation mixes are in one lane (quads a and
-// b = a + rot/2; with rot = D / 2 the upper lanes hold the channels that are not turned, in the same way).  Otherwise, for
-// neighbouring pairs and for other values of rot, eight channels in a row.  Either way the lanes' sums of squares meet in the
-// order of a tree of neighbouring channels.
+// The rotations that mix channels of other lanes or neighbouring ones: a lane holds eight channels in a row.
 //
 // kHeads heads of one kind (queries, keys or values) of one token per group of lanes.
-template <typename DT, int D, bool kAppend, int kHeads, bool kPaired>
+template <typename DT, int D, bool kAppend, int kHeads>
 __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 && !kAppend ? 4 : 3) norm_rope_kernel(const NormArgs a) {
     constexpr int kLanes = D / 8;                                 // lanes of a row
     constexpr int kRunBytes = 16 * (D + 8);
@@ -189,9 +248,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
     const bool vec = kind == 0 ? a.q_vec : kind == 1 ? a.k_vec : a.v_vec;
     const DT *weight = static_cast<const DT *>(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
     const bool rope = a.cos_sin != nullptr;                       // the same for the whole grid
-    const int turning = rope && kPaired ? a.rot >> 3 : kLanes;    // kPaired: the lanes whose channels are turned
-    const int ch0 = !kPaired ? lane * 8 : lane < turning ? lane * 4 : 4 * lane + 4 * turning;
-    const int ch1 = ch0 + (!kPaired ? 4 : 4 * turning);
+    const int ch0 = lane * 8, ch1 = ch0 + 4;
     src += t * st;
 
     Quad<DT> raw[kHeads][2], wraw[2];
@@ -207,14 +264,12 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
         wraw[1].load(weight + ch1, a.w_vec);
     }
     const bool pad = pos < 0, beyond = rope && pos >= a.max_pos;
-    const bool turned = rope && kind < 2 && (kPaired ? lane < turning : ch0 < a.rot);
-    // angles: kPaired, of the channels ch0 ..; neighbouring pairs, the lane's four; else of all eight channels
-    constexpr int kAngles = kPaired ? 2 : 4;
-    Two c[kAngles], s[kAngles];
+    const bool turned = rope && kind < 2 && ch0 < a.rot;
+    Two c[4], s[4];                                               // angles: neighbouring pairs, the lane's four; else of all eight channels
     if (turned) {
         const int half = a.rot >> 1;
         const float *row = a.cos_sin + (long long)min(max(pos, 0), a.max_pos - 1) * a.rot;
-        row += kPaired ? ch0 : a.interleaved ? ch0 >> 1 : ch0 < half ? ch0 : ch0 - half;
+        row += a.interleaved ? ch0 >> 1 : ch0 < half ? ch0 : ch0 - half;
         auto angles = [&](const float *p, Two &x, Two &y) {
             if (a.cs_vec) {
                 const float4 v = __ldg(reinterpret_cast<const float4 *>(p));
@@ -227,16 +282,16 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
         };
         angles(row, c[0], c[1]);
         angles(row + half, s[0], s[1]);
-        if (!kPaired && !a.interleaved) {
-            angles(row + 4, c[kAngles - 2], c[kAngles - 1]);
-            angles(row + half + 4, s[kAngles - 2], s[kAngles - 1]);
+        if (!a.interleaved) {
+            angles(row + 4, c[2], c[3]);
+            angles(row + half + 4, s[2], s[3]);
         }
     }
     // Sums of squares of the chunk's heads, then 1 / sqrt once for all of them: each of the first lanes takes one head's.
     // (Heads of all kinds may share a warp, and a warp's lanes go through the shuffles together.)
     float r[kHeads];
     if (__any_sync(0xFFFFFFFFu, weight != nullptr)) {
-        float sum0[kHeads], sum1[kHeads];                          // of the two quads
+        float sum[kHeads];
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
             Two x[4];
@@ -244,28 +299,16 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
             raw[i][1].get(x[2], x[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], x[e]);
-            sum0[i] = __fadd_rn(__fadd_rn(x[0].a, x[0].b), __fadd_rn(x[1].a, x[1].b));
-            sum1[i] = __fadd_rn(__fadd_rn(x[2].a, x[2].b), __fadd_rn(x[3].a, x[3].b));
-            if (!kPaired) sum0[i] = __fadd_rn(sum0[i], sum1[i]);
+            sum[i] = __fadd_rn(__fadd_rn(__fadd_rn(x[0].a, x[0].b), __fadd_rn(x[1].a, x[1].b)),
+                               __fadd_rn(__fadd_rn(x[2].a, x[2].b), __fadd_rn(x[3].a, x[3].b)));
         }
 #pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) {
-            if (kPaired && o == turning) {                         // rot = D / 2: a lane's quads meet before its half meets the other
+        for (int o = 1; o < kLanes; o <<= 1)
 #pragma unroll
-                for (int i = 0; i < kHeads; ++i) { sum0[i] = __fadd_rn(sum0[i], sum1[i]); sum1[i] = 0.0f; }
-            }
-#pragma unroll
-            for (int i = 0; i < kHeads; ++i) {
-                sum0[i] = __fadd_rn(sum0[i], __shfl_xor_sync(0xFFFFFFFFu, sum0[i], o));
-                if (kPaired) sum1[i] = __fadd_rn(sum1[i], __shfl_xor_sync(0xFFFFFFFFu, sum1[i], o));
-            }
-        }
+            for (int i = 0; i < kHeads; ++i) sum[i] = __fadd_rn(sum[i], __shfl_xor_sync(0xFFFFFFFFu, sum[i], o));
         float mine = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kHeads; ++i) {
-            if (kPaired) sum0[i] = __fadd_rn(sum0[i], sum1[i]);    // adds the zero where that has been done
-            mine = i == 0 || (lane & (kHeads - 1)) == i ? sum0[i] : mine;
-        }
+        for (int i = 0; i < kHeads; ++i) mine = i == 0 || (lane & (kHeads - 1)) == i ? sum[i] : mine;
         mine = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(mine, 1.0f / D), a.eps)));
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) r[i] = kHeads == 1 ? mine : __shfl_sync(0xFFFFFFFFu, mine, i, kLanes);
@@ -293,16 +336,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = mul2(mul2(x[e], {r[i], r[i]}), w[e]);
         }
-        if (kPaired) {
-            if (turned) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {                      // a - b and a + (-b) are the same number
-                    const Two y = add2(mul2(x[e], c[e]), mul2(x[e + 2], {-s[e].a, -s[e].b}));
-                    x[e + 2] = add2(mul2(x[e + 2], c[e]), mul2(x[e], s[e]));
-                    x[e] = y;
-                }
-            }
-        } else if (rope) {
+        if (rope) {
             if (a.interleaved) {
                 if (turned) {
 #pragma unroll
@@ -319,8 +353,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
                 for (int e = 0; e < 4; ++e) {
                     const Two o = {__shfl_sync(0xFFFFFFFFu, x[e].a, from, kLanes), __shfl_sync(0xFFFFFFFFu, x[e].b, from, kLanes)};
                     if (turned) {
-                        const Two se = s[e < kAngles ? e : 0];
-                        x[e] = add2(mul2(x[e], c[e < kAngles ? e : 0]), mul2(o, first ? Two{-se.a, -se.b} : se));
+                        x[e] = add2(mul2(x[e], c[e]), mul2(o, first ? Two{-s[e].a, -s[e].b} : s[e]));      // a - b and a + (-b) are the same number
                     }
                 }
             }
@@ -345,24 +378,165 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = Quad<DT>::rounded(x[e]);
                 }
-                uint32_t half[2], params;
-                quantise<kLanes>(x, half, params);
-                // Two quads make a word: kPaired, this lane's first with its neighbour's first, its second with the neighbour's
-                // second, so of the two lanes one gets each; otherwise the lane's own.
-                uint32_t word;
-                int at;
-                if (kPaired) {
-                    const bool odd = lane & 1;
-                    const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, odd ? half[0] : half[1], 1);
-                    word = odd ? got | half[1] << 8 : half[0] | got << 8;
-                    at = (odd ? ch1 : ch0) >> 3;
-                } else {
-                    word = half[0] | half[1] << 8;
-                    at = lane;
-                }
+                const Extrema ex(x);
+                Scale sc;
+                sc.reduce<kLanes>(ex.lo, ex.hi, ex.fine);
+                const uint32_t word = sc.word(x), params = sc.params;
                 if (kept && h < heads) {
                     uint8_t *run = run0 + i * head_bytes;
-                    *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, at) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, at))) = word;
+                    *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, lane) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, lane))) = word;
+                    if (lane == 0) *reinterpret_cast<uint32_t *>(run + Kv4<D>::kParamOff + tok * 8 + (kind == 1 ? 0 : 4)) = params;
+                }
+            }
+        }
+    }
+}
+
+// The usual case: no rotation, or one of all channels or their first half with pairs half of that apart.  A lane holds the eight
+// channels from ch0 and the eight that the rotation pairs with them (with rot = D / 2 the upper lanes hold the channels that are
+// not turned in the same way), so a row takes D / 16 lanes, loads and stores are whole 16-byte vectors, nothing but the row's sum
+// and extrema goes through shuffles, and each eight channels are a word of codes.  The lanes' sums meet in the order of a tree of
+// neighbouring channels: up to `turning` lanes of either eight, then the two, then the rest.
+template <typename DT, int D, bool kAppend, int kHeads>
+__global__ void __launch_bounds__(kNormThreads, 3) norm_rope_paired_kernel(const NormArgs a) {
+    constexpr int kLanes = D / 16;                                // lanes of a row
+    constexpr int kRunBytes = 16 * (D + 8);
+    const int lane = threadIdx.x & (kLanes - 1);
+    const uint32_t group = blockIdx.x * (kNormThreads / kLanes) + threadIdx.x / kLanes;
+    const uint32_t t_raw = group / (uint32_t)a.chunks;
+    const bool live = t_raw < (uint32_t)a.T;                      // whole groups: the shuffles below need every lane of the warp
+    const int t = live ? (int)t_raw : a.T - 1;
+    int chunk = (int)(group - t_raw * (uint32_t)a.chunks);
+    // the chunks of a token: queries, keys, values
+    const int kind = chunk < a.q_chunks ? 0 : !kAppend || chunk < a.q_chunks + a.k_chunks ? 1 : 2;
+    chunk -= kind == 0 ? 0 : kind == 1 ? a.q_chunks : a.q_chunks + a.k_chunks;
+    const int h0 = chunk * kHeads, heads = kind == 0 ? a.Hq : a.Hkv;
+    const DT *src = static_cast<const DT *>(kind == 0 ? a.q : kind == 1 ? a.k : a.v);
+    const long long st = kind == 0 ? a.q_t : kind == 1 ? a.k_t : a.v_t, sh = kind == 0 ? a.q_h : kind == 1 ? a.k_h : a.v_h;
+    const bool vec = kind == 0 ? a.q_vec : kind == 1 ? a.k_vec : a.v_vec;
+    const DT *weight = static_cast<const DT *>(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
+    const bool rope = a.cos_sin != nullptr;                       // the same for the whole grid
+    const int turning = rope ? a.rot >> 4 : kLanes;               // lanes whose channels are turned
+    const int ch0 = lane < turning ? lane * 8 : 8 * lane + 8 * turning, ch1 = ch0 + 8 * turning;
+
+    Eight<DT> raw[kHeads][2], wraw[2];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+        const DT *row = src + t * st + min(h0 + i, heads - 1) * sh;
+        raw[i][0].load(row + ch0, vec);
+        raw[i][1].load(row + ch1, vec);
+    }
+    const int pos = a.positions ? a.positions[t] : 0;
+    if (weight) {
+        wraw[0].load(weight + ch0, a.w_vec);
+        wraw[1].load(weight + ch1, a.w_vec);
+    }
+    const bool pad = pos < 0, beyond = rope && pos >= a.max_pos;
+    const bool turned = rope && kind < 2 && lane < turning;
+    Two c[4], s[4];
+    if (turned) {
+        const float *row = a.cos_sin + (long long)min(max(pos, 0), a.max_pos - 1) * a.rot + ch0;
+        Eight<float> cv, sv;
+        cv.load(row, a.cs_vec);
+        sv.load(row + (a.rot >> 1), a.cs_vec);
+        cv.get(c);
+        sv.get(s);
+    }
+    float r[kHeads];
+    if (__any_sync(0xFFFFFFFFu, weight != nullptr)) {
+        float sum0[kHeads], sum1[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            Two x[4];
+            raw[i][0].get(x);
+            sum0[i] = square_sum(x);
+            raw[i][1].get(x);
+            sum1[i] = square_sum(x);
+        }
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) {
+            if (o == turning) {
+#pragma unroll
+                for (int i = 0; i < kHeads; ++i) { sum0[i] = __fadd_rn(sum0[i], sum1[i]); sum1[i] = 0.0f; }
+            }
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                sum0[i] = __fadd_rn(sum0[i], __shfl_xor_sync(0xFFFFFFFFu, sum0[i], o));
+                sum1[i] = __fadd_rn(sum1[i], __shfl_xor_sync(0xFFFFFFFFu, sum1[i], o));
+            }
+        }
+        // 1 / sqrt once for all heads: each of the first lanes takes one head's
+        float mine = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            sum0[i] = __fadd_rn(sum0[i], sum1[i]);                 // adds the zero where that has been done
+            mine = i == 0 || (lane & (kHeads - 1)) == i ? sum0[i] : mine;
+        }
+        mine = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(mine, 1.0f / D), a.eps)));
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) r[i] = kHeads == 1 ? mine : __shfl_sync(0xFFFFFFFFu, mine, i, kLanes);
+    }
+    const bool any_kept = kAppend && __any_sync(0xFFFFFFFFu, kind > 0);
+    const long long slot = kAppend && kind > 0 ? a.slot[t] : -1;
+    const bool kept = live && !pad && slot >= 0 && slot < a.n_slots;
+    const long long block = kept ? block_of(slot, a.page) : 0;
+    const int place = kept ? (int)(slot - block * a.page) : 0, tok = place & 15;
+    // where this token lies in the cache: a head further is a page's worth of runs further
+    const long long head_bytes = kAppend ? (long long)(a.page >> 4) * kRunBytes : 0;
+    uint8_t *run0 = kAppend ? a.cache + (block * a.Hkv + h0) * head_bytes + (long long)(place >> 4) * kRunBytes : nullptr;
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+        const int h = h0 + i;
+        const bool mine = live && h < heads;
+        Two x[4], y[4];
+        raw[i][0].get(x);
+        raw[i][1].get(y);
+        if (weight) {
+            Two w[4];
+            wraw[0].get(w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = mul2(mul2(x[e], {r[i], r[i]}), w[e]);
+            wraw[1].get(w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = mul2(mul2(y[e], {r[i], r[i]}), w[e]);
+        }
+        if (turned) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {                          // a - b and a + (-b) are the same number
+                const Two z = add2(mul2(x[e], c[e]), mul2(y[e], {-s[e].a, -s[e].b}));
+                y[e] = add2(mul2(y[e], c[e]), mul2(x[e], s[e]));
+                x[e] = z;
+            }
+        }
+        if (kind < 2 && (pad || beyond)) {
+            const float v = pad ? 0.0f : CUDART_NAN_F;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = y[e] = {v, v};
+        }
+        if (kind == 0 || !kAppend) {
+            DT *out = static_cast<DT *>(kind == 0 ? a.q_out : a.k_out);
+            if (mine && out) {
+                out += ((long long)t * heads + h) * D;
+                Eight<DT>::store(out + ch0, x);
+                Eight<DT>::store(out + ch1, y);
+            }
+        }
+        if (kAppend && any_kept) {
+            if constexpr (D <= 128) {
+                if (kind == 1) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = Quad<DT>::rounded(x[e]);
+                        y[e] = Quad<DT>::rounded(y[e]);
+                    }
+                }
+                uint32_t words[2], params;
+                quantise_pair<kLanes>(x, y, words, params);
+                if (kept && h < heads) {
+                    uint8_t *run = run0 + i * head_bytes;
+                    const int w0 = ch0 >> 3, w1 = ch1 >> 3;
+                    *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, w0) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, w0))) = words[0];
+                    *reinterpret_cast<uint32_t *>(run + (kind == 1 ? Kv4<D>::key_word(tok, w1) : Kv4<D>::kValueOff + Kv4<D>::value_word(tok, w1))) = words[1];
                     if (lane == 0) *reinterpret_cast<uint32_t *>(run + Kv4<D>::kParamOff + tok * 8 + (kind == 1 ? 0 : 4)) = params;
                 }
             }
@@ -430,26 +604,26 @@ bool strides_ok(int64_t st, int64_t sh, int32_t H, int32_t D) { return sh >= D &
 
 template <typename DT, int D, bool kAppend>
 cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
-    constexpr int kGroups = kNormThreads / (D / 8);
-    // Four heads to a group of lanes once single heads would need more than one round of CTAs (148 SMs of about 1024
+    // Several heads to a group of lanes once single heads would need more than one round of CTAs (148 SMs of about 1024
     // threads): a short call is the latency of one group's chain, a long one wants loads in flight.
+    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2));
+    const int lanes = paired ? D / 16 : D / 8;
     const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv);
-    const bool wide = rows * (D / 8) > 148LL * 1024;
-    const int per = wide ? 4 : 1;
+    const bool wide = rows * lanes > 148LL * 1024;
+    const int per = !wide ? 1 : paired ? 2 : 4;
     a.q_chunks = (a.Hq + per - 1) / per;
     a.k_chunks = (a.Hkv + per - 1) / per;
     a.chunks = a.q_chunks + (kAppend ? 2 : 1) * a.k_chunks;
-    const long long groups = (long long)a.T * a.chunks;
-    const unsigned grid = (unsigned)((groups + kGroups - 1) / kGroups);
-    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2));
-    if (wide && paired)
-        norm_rope_kernel<DT, D, kAppend, 4, true><<<grid, kNormThreads, 0, st>>>(a);
-    else if (wide)
-        norm_rope_kernel<DT, D, kAppend, 4, false><<<grid, kNormThreads, 0, st>>>(a);
+    const long long groups = (long long)a.T * a.chunks, per_cta = kNormThreads / lanes;
+    const unsigned grid = (unsigned)((groups + per_cta - 1) / per_cta);
+    if (paired && wide)
+        norm_rope_paired_kernel<DT, D, kAppend, 2><<<grid, kNormThreads, 0, st>>>(a);
     else if (paired)
-        norm_rope_kernel<DT, D, kAppend, 1, true><<<grid, kNormThreads, 0, st>>>(a);
+        norm_rope_paired_kernel<DT, D, kAppend, 1><<<grid, kNormThreads, 0, st>>>(a);
+    else if (wide)
+        norm_rope_kernel<DT, D, kAppend, 4><<<grid, kNormThreads, 0, st>>>(a);
     else
-        norm_rope_kernel<DT, D, kAppend, 1, false><<<grid, kNormThreads, 0, st>>>(a);
+        norm_rope_kernel<DT, D, kAppend, 1><<<grid, kNormThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 
