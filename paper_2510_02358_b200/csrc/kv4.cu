@@ -604,6 +604,15 @@ bool strides_ok(int64_t st, int64_t sh, int32_t H, int32_t D) { return sh >= D &
 
 template <typename DT, int D, bool kAppend>
 cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
+    // A long append is two launches: its queries alone need fewer registers and less code than keys and values, and so run
+    // faster (8192 tokens of 40 + 2 x 8 heads of 128: 85 us together); a short one is bound by the launch.
+    if (kAppend && a.Hq > 0 && (long long)a.T * (a.Hq + 2 * a.Hkv) * (D / 16) > 148LL * 2048) {
+        NormArgs q = a;
+        q.Hkv = 0;
+        const cudaError_t e = launch_norm_heads<DT, D, false>(q, st);
+        if (e != cudaSuccess) return e;
+        a.Hq = 0;
+    }
     // Several heads to a group of lanes once single heads would need more than one round of CTAs (148 SMs of about 1024
     // threads): a short call is the latency of one group's chain, a long one wants loads in flight.
     const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2));
