@@ -53,6 +53,12 @@ __device__ __forceinline__ Two add2(Two x, Two y) {
     return x;
 }
 
+__device__ __forceinline__ Two fma2(Two x, Two y, Two z) {
+    asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mov.b64 w, {%4, %5};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
+        : "+f"(x.a), "+f"(x.b) : "f"(y.a), "f"(y.b), "f"(z.a), "f"(z.b));
+    return x;
+}
+
 // Four neighbouring channels of a row.
 template <typename DT> struct Quad;
 template <> struct Quad<__nv_bfloat16> {
@@ -160,9 +166,10 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
 
 // One scale and one offset for a row that lies on kLanes lanes, and the codes of eight channels as a word.
 //
-// A code is (x - z) / s, rounded, then rounded to a whole number.  The product with 1 / s is within 2e-6 of the quotient (which
-// is at most 15), so it has the same whole number next to it unless it lies within that of the middle between two; only lanes
-// that hold such a number (1e-5 is taken) divide.
+// A code is (x - z) / s, rounded to fp32, then to a whole number.  The quotient comes from the correctly rounded reciprocal and one
+// step with the exact remainder (Markstein's method): q = d * inv, q + (d - q s) * inv.  That is within 2^-46 of d / s before its
+// own rounding, and d / s cannot be nearer than 2^-33 to the middle between two fp32 numbers, since s has 8 bits: so it is the
+// rounded quotient.  (Only where neither the remainder nor the reciprocal leaves the normal range; elsewhere the lanes divide.)
 struct Extrema {
     float lo, hi;
     bool fine;
@@ -203,14 +210,14 @@ struct Scale {
         if (!live) return 0u;
         constexpr float kRound = 12582912.0f;                      // 1.5 * 2^23: adding it leaves the nearest whole number, ties to even
         Two c[4];
-        float far = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const Two q = mul2(add2(x[e], {-z, -z}), {inv, inv});
+            const Two d = add2(x[e], {-z, -z});
+            Two q = mul2(d, {inv, inv});
+            q = fma2(fma2(q, {-s, -s}, d), {inv, inv}, q);
             c[e] = add2(add2(q, {kRound, kRound}), {-kRound, -kRound});
-            far = max3(far, fabsf(q.a - c[e].a), fabsf(q.b - c[e].b));
         }
-        if (far > 0.49999f) {
+        if (!(s > 1e-27f && s < 1e30f)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) c[e] = {rintf(__fdiv_rn(__fsub_rn(x[e].a, z), s)), rintf(__fdiv_rn(__fsub_rn(x[e].b, z), s))};
         }
