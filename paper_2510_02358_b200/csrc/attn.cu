@@ -52,6 +52,12 @@ __device__ __forceinline__ void copy_bulk(uint32_t dst, const void *src, uint32_
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
+// The same without their bias, and centred: code - 8, exactly.
+__device__ __forceinline__ uint32_t centred(uint32_t x) {
+    uint32_t y;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(0x43084308u));
+    return y;
+}
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
 __device__ __forceinline__ bool bytes_here(uint32_t bar, uint32_t parity) {
     long long t0 = 0;
@@ -107,8 +113,9 @@ template <int D> struct Codes {
 //     q . k = s (q . (128 + code)) + (z - 128 s) sum(q),
 //     sum_u p v = sum_u (p s)(128 + code) - 136 sum_u (p s) + sum_u p (z + 8 s)
 // where p s is rounded to bf16 as an operand and sum (p s) is formed from the rounded numbers by a
-// matrix instruction with rows of ones (so the bias leaves exactly; 136 and the 8 s beside z centre
-// the codes, which keeps the rounding error that of a centred value).
+// matrix instruction with rows of ones (136 and the 8 s beside z centre the codes, which keeps the
+// rounding error that of a centred value).  The bias leaves in every iteration: over a long stretch it
+// would grow to thousands of times an output that averages over many tokens, and take its last bits.
 //
 // Each warp walks its own runs of 16 tokens with the next ones' copies in flight, and keeps its own
 // running maximum: it moves only when a score passes it by 2^8 (the sums cannot overflow by that, and
@@ -116,6 +123,9 @@ template <int D> struct Codes {
 // kW warps a CTA, kCtas CTAs an SM, kU runs an iteration, kStages iterations in the ring.
 template <int D, int NT, int kW, int kCtas, int kU, int kStages>
 __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnArgs a) {
+    // how the values' bias leaves (see above): by a subtraction in the operand, once a code, or from the sums, once an output and
+    // iteration; the latter is less work for few rows
+    constexpr bool kCentred = NT >= 4;
     constexpr bool kQueriesShared = NT >= 4;                      // their fragments would not leave enough registers
     constexpr int kRows = 8 * NT, kStep = 16 * kU * kW, kKs = D / 16, kMt = D / 16;
     constexpr int kFrag = NT * kMt * 4 * 32;                      // floats of a partial output, in fragment order
@@ -269,14 +279,13 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         }
         // Scores are formed relative to the rows' reference -nb (base 2).  `unset`: rows of this lane (bit 2t + e) that have none
         // yet, because nothing of what they see has come; rows beyond the unit's keep 0.
-        float o[NT][kMt][4], ps[NT][4], nb[NT][2], l[NT][2], zs[NT][2];
+        float o[NT][kMt][4], ps[kCentred ? 1 : NT][4] = {}, nb[NT][2], l[NT][2], zs[NT][2];
         uint32_t unset = 0u;
         bool started = false;                                     // nothing to rescale in the first iteration
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int j = 0; j < kMt; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.0f;
-            ps[t][0] = ps[t][1] = ps[t][2] = ps[t][3] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 nb[t][e] = 0.0f; l[t][e] = 0.0f; zs[t][e] = 0.0f;
@@ -383,7 +392,6 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                         if (started) {
                             l[t][e] *= keep;
                             zs[t][e] *= keep;
-                            ps[t][e] *= keep;
 #pragma unroll
                             for (int j = 0; j < kMt; ++j) { o[t][j][e] *= keep; o[t][j][e + 2] *= keep; }
                         }
@@ -416,7 +424,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     }
                     p[t][0] = transpose8x8(pack_bf16(w[0], w[1]));
                     p[t][1] = transpose8x8(pack_bf16(w[2], w[3]));
-                    mma_bf16(ps[t], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, p[t][0], p[t][1]);
+                    if (!kCentred) mma_bf16(ps[kCentred ? 0 : t], 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u, p[t][0], p[t][1]);
                 }
                 Codes<D> v;
                 v.load(codes + x * Kv4<D>::kRunBytes + Kv4<D>::kValueOff);
@@ -426,10 +434,23 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                     const uint32_t e1 = __byte_perm(v.val(i, 1, 0), v.val(i, 1, 1), 0x5410), o1 = __byte_perm(v.val(i, 1, 0), v.val(i, 1, 1), 0x7632);
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
-                        const uint32_t a0 = biased(e0, y), a1 = biased(o0, y), a2 = biased(e1, y), a3 = biased(o1, y);
+                        uint32_t a0 = biased(e0, y), a1 = biased(o0, y), a2 = biased(e1, y), a3 = biased(o1, y);
+                        if (kCentred) { a0 = centred(a0); a1 = centred(a1); a2 = centred(a2); a3 = centred(a3); }
 #pragma unroll
                         for (int t = 0; t < NT; ++t) mma_bf16(o[t][4 * i + y], a0, a1, a2, a3, p[t][0], p[t][1]);
                     }
+                }
+            }
+            if (!kCentred) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float (&sum)[4] = ps[kCentred ? 0 : t];
+#pragma unroll
+                    for (int j = 0; j < kMt; ++j) {
+                        fma2(o[t][j][0], o[t][j][1], -(kBias + 8.0f), sum[0], sum[1], o[t][j][0], o[t][j][1]);
+                        fma2(o[t][j][2], o[t][j][3], -(kBias + 8.0f), sum[0], sum[1], o[t][j][2], o[t][j][3]);
+                    }
+                    sum[0] = sum[1] = sum[2] = sum[3] = 0.0f;
                 }
             }
         }
@@ -460,7 +481,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
 #pragma unroll
                 for (int w = 1; w < kW; ++w) top = fmaxf(top, s_m[w][row]);
                 const float mine = s_m[warp][row], keep = mine == top ? 1.0f : ex2_approx(mine - top);
-                const float off = zs[t][e] - (kBias + 8.0f) * ps[t][e];
+                const float off = zs[t][e];
 #pragma unroll
                 for (int j = 0; j < kMt; ++j) {
                     s_o[warp][(t * kMt + j) * 4 + e][lane] = (o[t][j][e] + off) * keep;

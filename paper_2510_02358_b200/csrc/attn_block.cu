@@ -14,15 +14,22 @@
 //               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
 //   warps 16-17 one lane each issues the products of a slot: S = Q K^T, O += P V
 //
-// Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole bf16 value on the way
+// Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
-// does, would cost each score more than that.
+// does, would cost each score more than that.  The operands are fp16, whose 11 bits leave the result's
+// own rounding to bf16 as the only error that counts (0.0017 of an output in the mean; with bf16 operands
+// it was 0.0035).  What fp16's range does not hold is brought into it by powers of two: a row of queries
+// by its largest number, taken back with the softmax scale; a key whose largest number lies outside
+// 2^-4 .. 2^15 by that, its scores being multiplied back (k_mul).  Values are multiplied by 64, and the 16
+// tokens of a run that holds one outside 2^-10 .. 2^9 go through bf16 operands instead (wide_runs).
 //
 // The running maximum moves only when a row's scores pass it by 2^8, and only then is the output in
 // tensor memory rescaled (by the softmax warps, between two products of their slot).
 //
 // Tokens that nobody may see (beyond the length, of a missing block) become zeros, and those whose scale
 // or offset is NaN too, with a bit beside the tile: the rows that see such a token get a NaN score.
+#include <cuda_fp16.h>
+
 #include "attn.cuh"
 #include "attn_block.h"
 
@@ -83,7 +90,8 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead_bytes
     return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(lead_bytes >> 4) << 16 | (uint64_t)(stride_bytes >> 4) << 32 |
            (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-constexpr uint32_t kBf16Product = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kTile >> 4) << 24;      // fp32 sums, bf16 operands, 128 rows
+constexpr uint32_t kProduct = 1u << 4 | (uint32_t)(kTile >> 4) << 24;      // fp32 sums, fp16 operands, 128 rows
+constexpr uint32_t kWithBf16 = 1u << 7 | 1u << 10;                         // bf16 operands instead
 __device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, uint32_t lead) {
     asm volatile("{\n .reg .pred p, e;\n setp.ne.u32 p, %4, 0;\n setp.ne.u32 e, %5, 0;\n"
                  " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
@@ -236,31 +244,62 @@ struct Bars {
     uint64_t query_ready, out_done;
 };
 struct __align__(16) Info {                      // beside a token tile, one bit per token
-    uint32_t there[4], poison[4];                // 16 bits from each fill warp
+    uint32_t there[4], poison[4], scaled[4];     // 16 bits from each fill warp: there is such a token, it holds NaN, its k_mul is not 1
+    float k_mul[kTile];
+    uint8_t wide_runs[8];                        // whether a run's values are bf16
+    uint8_t odd[8];                              // whether anything of the above is other than usual in a run
 };
 
 // ------------------------------------------------------------------------------- codes to values
-__device__ __forceinline__ uint32_t biased_pair(uint32_t w, int i) {
-    uint32_t y;
-    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(y) : "r"(w >> (4 * i)));
-    return y;
+// Scale and offset of a token, both in both halves; fp16 numbers take a second scale for the codes that come 16 times as large.
+struct Affine {
+    uint32_t s, s16, z;
+};
+__device__ __forceinline__ uint32_t twice_f16(float x) {
+    const __half2 h = __float2half2_rn(x);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
-// Eight channels: (128 + code) - 128 is exact, then code * s + z is rounded once.
-__device__ __forceinline__ uint4 values8(uint32_t w, uint32_t s2, uint32_t z2) {
+__device__ __forceinline__ uint32_t twice_bf16(float x) {
+    const __nv_bfloat162 h = __float2bfloat162_rn(x);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// Eight channels.  fp16: 0x6400 is 1024 and its last bit is worth 1, so a masked OR makes 1024 + code or 1024 + 16 code; taking
+// 1024 off is exact, and code * s + z is rounded once.
+__device__ __forceinline__ uint4 values_f16(uint32_t w, const Affine &a) {
     uint32_t v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t code;
-        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(code) : "r"(biased_pair(w, i)), "r"(0x43004300u));
-        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(code), "r"(s2), "r"(z2));
+        uint32_t c;
+        if (i & 1) asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(c) : "r"(w));
+        else asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(c) : "r"(w));
+        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(c) : "r"(c), "r"(0x64006400u));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(i & 1 ? a.s16 : a.s), "r"(a.z));
+        if (i == 1) w >>= 8;
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// bf16: the same with 128 + code.
+__device__ __forceinline__ uint4 values_bf16(uint32_t w, const Affine &a) {
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t c;
+        asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(c) : "r"(w >> (4 * i)));
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(c), "r"(0x43004300u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(a.s), "r"(a.z));
     }
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 __device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ uint32_t both_lo(uint32_t p) { return __byte_perm(p, p, 0x1010); }
-__device__ __forceinline__ uint32_t both_hi(uint32_t p) { return __byte_perm(p, p, 0x3232); }
+// The largest number that a head of scale and offset p (bf16 each) may hold, in magnitude.
+__device__ __forceinline__ float largest(uint32_t p) { return fmaxf(fabsf(bf16_hi(p)), fabsf(fmaf(15.0f, bf16_lo(p), bf16_hi(p)))); }
+constexpr float kValueMul = 64.0f;               // values are multiplied by it on the way in, outputs by its inverse on the way out
+__device__ __forceinline__ bool value_fits(uint32_t p) {
+    const float top = largest(p);
+    return top == 0.0f || (top >= 0.0009765625f && top < 512.0f);
+}
 __device__ __forceinline__ bool not_finite(uint32_t p) { return (p & 0x7FFFu) >= 0x7F80u || (p & 0x7FFF0000u) >= 0x7F800000u; }
 // Where the 16-byte piece `piece` (channels 8 piece ..) of row t lies in an operand tile.
 __device__ __forceinline__ uint32_t piece_at(int t, int piece) {
@@ -292,36 +331,57 @@ template <int D> struct Fill {
         vp[0] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3));
         vp[1] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3) + 4);
     }
-    // Keys into the tile at shared address `tile`; `left`: tokens of the request from the run's first on.  Returns the run's
-    // tokens that are there (low half) and those of them that hold NaN (high half).
-    __device__ __forceinline__ uint32_t put_keys(uint32_t tile, int t0, int left, int lane) const {
-        const int r = lane >> 2, c = lane & 3;
-        uint32_t mark = 0u;
+    // Keys into the tile at shared address `tile`, what is known of its tokens into `info`; `left`: tokens of the request from the
+    // run's first on.
+    __device__ __forceinline__ void put_keys(uint32_t tile, Info *info, int warp, int left, int lane) const {
+        const int r = lane >> 2, c = lane & 3, t0 = warp * 16;
+        uint32_t mark = 0u, scaled = 0u;
+        bool fits = true;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const int t = r + 8 * hi;
             const bool live = ok_k && t < left, nan = live && (not_finite(kp[hi].x) || not_finite(kp[hi].y));
             mark |= ((live ? 1u : 0u) | (nan ? 0x10000u : 0u)) << t;
             const bool use = live && !nan;
-            const uint32_t s2 = use ? both_lo(kp[hi].x) : 0u, z2 = use ? both_hi(kp[hi].x) : 0u;
+            float s = use ? bf16_lo(kp[hi].x) : 0.0f, z = use ? bf16_hi(kp[hi].x) : 0.0f;
+            fits = fits && (!use || value_fits(kp[hi].y));
+            const float top = use ? largest(kp[hi].x) : 0.0f;
+            if (top != 0.0f && !(top >= 0.0625f && top < 32768.0f)) {
+                const int ex = min(max((int)(__float_as_uint(top) >> 23), 2), 252);
+                const float down = __uint_as_float((uint32_t)(254 - ex) << 23);
+                s *= down;
+                z *= down;
+                scaled |= 1u << t;
+                if (c == 0) info->k_mul[t0 + t] = __uint_as_float((uint32_t)ex << 23);
+            }
+            const Affine a = {twice_f16(s), twice_f16(s * 0.0625f), twice_f16(z)};
             if (D == 128) {
                 // the lanes c and c + 2 write to the same banks: the upper two take their words the other way round
                 const uint4 u = k[D == 128 ? hi : 0];
                 const bool swap = (c & 2) != 0;
                 const uint32_t w0 = swap ? u.z : u.x, w1 = swap ? u.w : u.y, w2 = swap ? u.x : u.z, w3 = swap ? u.y : u.w;
                 const int p0 = 4 * c + (swap ? 2 : 0), p2 = 4 * c + (swap ? 0 : 2);
-                store16(tile + piece_at(t0 + t, p0), values8(w0, s2, z2));
-                store16(tile + piece_at(t0 + t, p0 + 1), values8(w1, s2, z2));
-                store16(tile + piece_at(t0 + t, p2), values8(w2, s2, z2));
-                store16(tile + piece_at(t0 + t, p2 + 1), values8(w3, s2, z2));
+                store16(tile + piece_at(t0 + t, p0), values_f16(w0, a));
+                store16(tile + piece_at(t0 + t, p0 + 1), values_f16(w1, a));
+                store16(tile + piece_at(t0 + t, p2), values_f16(w2, a));
+                store16(tile + piece_at(t0 + t, p2 + 1), values_f16(w3, a));
             } else {
-                store16(tile + piece_at(t0 + t, 2 * c), values8(hi ? k[0].z : k[0].x, s2, z2));
-                store16(tile + piece_at(t0 + t, 2 * c + 1), values8(hi ? k[0].w : k[0].y, s2, z2));
+                store16(tile + piece_at(t0 + t, 2 * c), values_f16(hi ? k[0].z : k[0].x, a));
+                store16(tile + piece_at(t0 + t, 2 * c + 1), values_f16(hi ? k[0].w : k[0].y, a));
             }
         }
-        return __reduce_or_sync(0xFFFFFFFFu, mark);
+        mark = __reduce_or_sync(0xFFFFFFFFu, mark);
+        scaled = __reduce_or_sync(0xFFFFFFFFu, scaled);
+        fits = __all_sync(0xFFFFFFFFu, fits);
+        if (lane == 0) {
+            reinterpret_cast<uint16_t *>(info->there)[warp] = (uint16_t)mark;
+            reinterpret_cast<uint16_t *>(info->poison)[warp] = (uint16_t)(mark >> 16);
+            reinterpret_cast<uint16_t *>(info->scaled)[warp] = (uint16_t)scaled;
+            info->wide_runs[warp] = fits ? 0 : 1;
+            info->odd[warp] = mark != 0xFFFFu || scaled != 0u || !fits ? 1 : 0;
+        }
     }
-    __device__ __forceinline__ void put_values(uint32_t tile, int t0, int left, int lane) const {
+    __device__ __forceinline__ void put_values(uint32_t tile, int t0, int left, bool wide, int lane) const {
         const int r = lane >> 2, c = lane & 3;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
@@ -330,15 +390,25 @@ template <int D> struct Fill {
                 const int t = 2 * c + e + 8 * hi;
                 const uint32_t par = e ? vp[hi].w : vp[hi].y;
                 const bool use = ok_v && t < left && !not_finite(par);
-                const uint32_t s2 = use ? both_lo(par) : 0u, z2 = use ? both_hi(par) : 0u;
+                const float s = use ? bf16_lo(par) * kValueMul : 0.0f, z = use ? bf16_hi(par) * kValueMul : 0.0f;
+                uint32_t w0, w1 = 0u;
                 if (D == 128) {
                     const uint4 u = v[D == 128 ? hi : 0];
-                    const uint32_t a0 = e ? u.z : u.x, a1 = e ? u.w : u.y;
-                    const bool swap = (r & 1) != 0;                  // as above: odd r the other way round
-                    store16(tile + piece_at(t0 + t, 2 * r + (swap ? 1 : 0)), values8(swap ? a1 : a0, s2, z2));
-                    store16(tile + piece_at(t0 + t, 2 * r + (swap ? 0 : 1)), values8(swap ? a0 : a1, s2, z2));
+                    w0 = e ? u.z : u.x;
+                    w1 = e ? u.w : u.y;
                 } else {
-                    store16(tile + piece_at(t0 + t, r), values8(hi ? (e ? v[0].w : v[0].z) : (e ? v[0].y : v[0].x), s2, z2));
+                    w0 = hi ? (e ? v[0].w : v[0].z) : (e ? v[0].y : v[0].x);
+                }
+                const bool swap = D == 128 && (r & 1) != 0;          // as above: odd r the other way round
+                const int at = D == 128 ? 2 * r : r;
+                if (!wide) {
+                    const Affine a = {twice_f16(s), twice_f16(s * 0.0625f), twice_f16(z)};
+                    store16(tile + piece_at(t0 + t, at + (swap ? 1 : 0)), values_f16(swap ? w1 : w0, a));
+                    if (D == 128) store16(tile + piece_at(t0 + t, at + (swap ? 0 : 1)), values_f16(swap ? w0 : w1, a));
+                } else {
+                    const Affine a = {twice_bf16(s), 0u, twice_bf16(z)};
+                    store16(tile + piece_at(t0 + t, at + (swap ? 1 : 0)), values_bf16(swap ? w1 : w0, a));
+                    if (D == 128) store16(tile + piece_at(t0 + t, at + (swap ? 0 : 1)), values_bf16(swap ? w0 : w1, a));
                 }
             }
     }
@@ -380,11 +450,7 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
         auto keys = [&](uint32_t m, int s) {
             const uint32_t st = m & 1u;
             if (!warp_wait(key_empty + 8 * st, ((m >> 1) & 1u) ^ 1u, dead)) return false;
-            const uint32_t mark = f.put_keys(k_at + st * kTileBytes, t0, kv - s * kTile - t0, lane);
-            if (lane == 0) {
-                reinterpret_cast<uint16_t *>(info[m & 3].there)[warp] = (uint16_t)mark;
-                reinterpret_cast<uint16_t *>(info[m & 3].poison)[warp] = (uint16_t)(mark >> 16);
-            }
+            f.put_keys(k_at + st * kTileBytes, info + (m & 3), warp, kv - s * kTile - t0, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(key_full + 8 * st);
@@ -413,7 +479,7 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             }
             const uint32_t st = n & 1u;
             if (!warp_wait(val_empty + 8 * st, ((n >> 1) & 1u) ^ 1u, dead)) return;
-            f.put_values(v_at + st * kTileBytes, t0, kv - step * kTile - t0, lane);
+            f.put_values(v_at + st * kTileBytes, t0, kv - step * kTile - t0, info[n & 3].wide_runs[warp] != 0, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(val_full + 8 * st);
@@ -428,9 +494,9 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
 // whole warp walks, one lane issues.  A slot's own products are in the order of issue, which is all that its buffers need.
 template <int D>
 __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem, uint32_t q_at, uint32_t k_at,
-                                             uint32_t v_at, Bars *bars, volatile int *dead, uint32_t slot, int lane) {
+                                             uint32_t v_at, Bars *bars, const Info *info, volatile int *dead, uint32_t slot, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile, kBlock = kTile * 128 / 16;
-    constexpr uint32_t kScore = kBf16Product | (uint32_t)(kHalf >> 3) << 17, kOut = kBf16Product | 1u << 16 | (uint32_t)(D >> 3) << 17;
+    constexpr uint32_t kScore = kProduct | (uint32_t)(kHalf >> 3) << 17, kOut = kProduct | 1u << 16 | (uint32_t)(D >> 3) << 17;
     const uint32_t key_full = smem_u32(bars->key_full), key_empty = smem_u32(bars->key_empty);
     const uint32_t val_full = smem_u32(bars->val_full), val_empty = smem_u32(bars->val_empty);
     const uint32_t score_full = smem_u32(bars->score_full) + 16 * slot, weight_ready = smem_u32(bars->weight_ready) + 16 * slot;
@@ -470,8 +536,15 @@ __device__ __forceinline__ void product_role(const AttnArgs &a, const LineStart 
             fence_after();
             const uint64_t va = v_desc + st * (kTileBytes >> 4) + buf * (kHalf * 128 / 16);
             const uint32_t p = s_at + buf * kHalf;
+            const uint32_t odd = __shfl_sync(0xFFFFFFFFu, *reinterpret_cast<const uint32_t *>(&info[t & 3].wide_runs[4 * buf]), 0);
+            if (odd == 0u) {
 #pragma unroll
-            for (int ks = 0; ks < kHalf / 16; ++ks) product_ts(o_at, p + ks * 8, va + ks * 128, kOut, i > 0u || ks > 0, lead);
+                for (int ks = 0; ks < kHalf / 16; ++ks) product_ts(o_at, p + ks * 8, va + ks * 128, kOut, i > 0u || ks > 0, lead);
+            } else {                                               // a run of 16 tokens each
+#pragma unroll
+                for (int ks = 0; ks < kHalf / 16; ++ks)
+                    product_ts(o_at, p + ks * 8, va + ks * 128, (odd >> (8 * ks)) & 1u ? kOut | kWithBf16 : kOut, i > 0u || ks > 0, lead);
+            }
             commit_to(out_free, lead);
             if (buf) {
                 commit_to(val_empty + 8 * st, lead);
@@ -503,6 +576,10 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi) {
+    const __half2 p = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float y;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
@@ -519,12 +596,11 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
 
 template <int D>
 __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart &line, Walk &w, uint32_t tmem_all, uint32_t q_at, Bars *bars,
-                                             const Info *info, float *s_m, float *s_l, volatile int *dead, int slot, int warp, int lane) {
+                                             const Info *info, float *s_m, float *s_l, float *s_back, volatile int *dead, int slot, int warp, int lane) {
     constexpr uint32_t kTileBytes = D * 2 * kTile;
     const int me = warp * 32 + lane;                               // row of the slot's tile
     const uint32_t tmem = tmem_all + ((uint32_t)(warp * 32) << 16);
     const uint32_t s_at = tmem + slot * kTile, o_at = tmem + 2 * kTile + slot * D;
-    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);          // a scale of 0 as one that no finite score is moved by
     walk_enter(w, a, line, lane);
     uint32_t seg = 0u, used = 0u, freed = 0u, tile_n = 0u;
     while (walk_next(w, a, lane)) {
@@ -535,21 +611,45 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         const long long token = w.rq.row0 + qi;
         const int head = w.h * a.group + row - qi * a.group;
         // queries into shared memory (the products of the segment before are done: out_done was waited for)
+        float back = 1.0f;
+        bool lost_row = false;                                     // an infinity or a NaN among its queries
         if (wide || slot == 0) {
             const uint32_t dst = q_at + (wide ? slot : 0) * kTileBytes;
-            const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;      // the scale's sign goes into the queries
             const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_t + (long long)head * a.q_h);
+            auto load = [&](int i) { return live ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u); };
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {                      // read twice: the second time from the first-level cache
+                const uint4 x = load(i);
+                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float f = bf16_lo(v[e]), g = bf16_hi(v[e]);
+                    top = max3(top, fabsf(f), fabsf(g));
+                    lost_row = lost_row || !(fabsf(f) <= 3.402823466e38f) || !(fabsf(g) <= 3.402823466e38f);
+                }
+            }
+            // the row's largest number to 1 .. 2, with the scale's sign; taken back below
+            const int ex = min(max((int)(__float_as_uint(top) >> 23), 27), 227);
+            const float up = copysignf(__uint_as_float((uint32_t)(254 - ex) << 23), a.scale_log2);
+            back = __uint_as_float((uint32_t)ex << 23);
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (live) x = __ldg(src + i);
-                x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
-                store16(dst + piece_at(me, i), x);
+                const uint4 x = load(i);
+                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = pack2_f16(bf16_lo(v[e]) * up, bf16_hi(v[e]) * up);
+                store16(dst + piece_at(me, i), make_uint4(h[0], h[1], h[2], h[3]));
             }
             fence_smem();
+            s_back[slot * kTile + me] = lost_row ? CUDART_NAN_F : back;
         }
         __syncwarp();
         if (lane == 0) bar_arrive(smem_u32(&bars->query_ready));
+        // what a product with the row's queries is multiplied with; a unit of one tile has them from slot 0
+        if (!wide) pair_barrier(1, kSoftWarps * 32);
+        const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f) * s_back[(wide ? slot * kTile : 0) + me];      // 0 as one that moves nothing
         const int past = w.rq.kv - w.rq.n_new;
         // rows beyond the unit's see everything: what they hold is not used, and their tiles need no masks
         const int lim = !live ? 0x7FFFFFFF : a.mask_kind == DSP_MASK_CAUSAL ? min(w.rq.kv, past + qi + 1) : w.rq.kv;
@@ -575,11 +675,13 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             tmem_load32(at + 32, x[1]);
             const int tile = wide ? i >> 1 : 2 * (i >> 1) + slot, t0 = (step0 + tile) * kTile + (int)buf * kHalf;
             const Info *inf = info + ((tile_n + tile) & 3);
-            const uint2 there = *reinterpret_cast<const uint2 *>(&inf->there[2 * buf]), poison = *reinterpret_cast<const uint2 *>(&inf->poison[2 * buf]);
-            const bool part = live && (t0 + kHalf > all || (there.x & there.y) != 0xFFFFFFFFu || (poison.x | poison.y) != 0u);
+            const uint32_t odd = *reinterpret_cast<const uint32_t *>(&inf->odd[4 * buf]);
+            const bool part = live && (t0 + kHalf > all || odd != 0u);
             tmem_loaded(x[0]);
             tmem_loaded(x[1]);
             if (__any_sync(0xFFFFFFFFu, part)) {                   // at the ends of what a tile's rows see
+                const uint2 there = *reinterpret_cast<const uint2 *>(&inf->there[2 * buf]), poison = *reinterpret_cast<const uint2 *>(&inf->poison[2 * buf]);
+                const uint2 scaled = *reinterpret_cast<const uint2 *>(&inf->scaled[2 * buf]);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int u0 = t0 + 32 * k;
@@ -591,7 +693,12 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                         const uint32_t hi = w0 + 1 >= 0 && w0 + 1 < a.words ? __ldg(bits + w0 + 1) : 0u;
                         v &= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
                     }
-                    const uint32_t nan = v & (k ? poison.y : poison.x);
+                    const uint32_t nan = v & (k ? poison.y : poison.x), mul = k ? scaled.y : scaled.x;
+                    if (mul) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if ((mul >> e) & 1u) x[k][e] *= inf->k_mul[kHalf * buf + 32 * k + e];
+                    }
 #pragma unroll
                     for (int e = 0; e < 32; ++e) x[k][e] = (v >> e) & 1u ? x[k][e] : -CUDART_INF_F;
                     if (nan) {
@@ -641,12 +748,30 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                         a0 = ex2_approx(a0);
                         a1 = ex2_approx(a1);
                         add2(sums[e & 2], sums[(e & 2) + 1], a0, a1);
-                        p[e >> 1] = pack2(a0, a1);
+                        p[e >> 1] = pack2_f16(a0, a1);
                     }
                     tmem_store4(at + 16 * k + 4 * h, p);           // over scores that are in registers
                 }
             }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            if (odd) {                                             // weights of runs whose values are bf16: as bf16 too
+                const uint32_t wide_runs = *reinterpret_cast<const uint32_t *>(&inf->wide_runs[4 * buf]);
+                if (wide_runs) tmem_stored();
+#pragma unroll 1
+                for (int k = 0; k < 4; ++k) {
+                    if (!((wide_runs >> (8 * k)) & 1u)) continue;
+                    float y[8];
+                    uint32_t p[4];
+                    tmem_load8(at + 8 * k, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t both = __float_as_uint(y[e]);
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&both));
+                        p[e & 3] = pack2(f.x, f.y);
+                        if ((e & 3) == 3) tmem_store4(at + 8 * k + e - 3, p);
+                    }
+                }
+            }
             tmem_stored();
             fence_before();
             __syncwarp();
@@ -677,7 +802,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             float sum = two ? fmaf(l1, f1, l * f0) : l;
             if (*dead) sum = CUDART_NAN_F;
             const bool whole = w.step0 == 0 && w.step1 == w.steps;
-            const float inv = sum == 0.0f ? 0.0f : whole ? 1.0f / sum : 1.0f;
+            const float inv = sum == 0.0f ? 0.0f : whole ? 1.0f / (sum * kValueMul) : 1.0f / kValueMul;
             const int part_row = (wide ? slot * kTile : 0) + me;
             float *part = a.part + ((long long)blockIdx.x * 2 + (w.step0 == 0 ? 1 : 0)) * (2 * kTile * (D + 2));
 #pragma unroll 1
@@ -709,7 +834,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 } else {
                     float4 *dst = reinterpret_cast<float4 *>(part + (long long)part_row * D + 32 * k);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) dst[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                    for (int e = 0; e < 8; ++e) dst[e] = make_float4(x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv);
                 }
             }
             if (!whole) {
@@ -736,7 +861,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     extern __shared__ uint8_t s_raw[];
     __shared__ Bars s_bars;
     __shared__ Info s_info[4];
-    __shared__ float s_m[kTile], s_l[kTile];
+    __shared__ float s_m[kTile], s_l[kTile], s_back[2 * kTile];
     __shared__ long long s_scan[32];
     __shared__ LineStart s_line;
     __shared__ uint32_t s_tmem;
@@ -774,11 +899,11 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem, 0);
     if (s_line.begin < s_line.end) {
         if (warp < kSoftWarps) {
-            softmax_role<D>(a, s_line, s_walk[warp], tmem, q_at, &s_bars, s_info, s_m, s_l, &s_dead, warp >> 2, warp & 3, lane);
+            softmax_role<D>(a, s_line, s_walk[warp], tmem, q_at, &s_bars, s_info, s_m, s_l, s_back, &s_dead, warp >> 2, warp & 3, lane);
         } else if (warp < kSoftWarps + kFillWarps) {
             fill_role<D>(a, s_line, s_walk[warp], k_at, v_at, s_info, &s_bars, &s_dead, warp - kSoftWarps, lane);
         } else {
-            product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, &s_dead, (uint32_t)(warp - kSoftWarps - kFillWarps), lane);
+            product_role<D>(a, s_line, s_walk[warp], tmem, q_at, k_at, v_at, &s_bars, s_info, &s_dead, (uint32_t)(warp - kSoftWarps - kFillWarps), lane);
         }
     }
     __syncwarp();

@@ -366,6 +366,43 @@ def test_attention_of_more_requests_than_the_gpu_has_places_for(new, Hq, Hkv, D)
 
 
 @gpu
+@pytest.mark.parametrize("new,D", [(1, 128), (1, 64), (4, 128), (9, 64), (9, 128), (40, 128), (40, 64)])
+def test_attention_averages_over_long_contexts_without_losing_bits(new, D):
+    """Diffuse weights over 20000 tokens: the output is a hundredth of a value, sums of anything larger must not eat into it."""
+    Hq, Hkv, page, kv = 3, 1, 64, 20000
+    r, q, cache, table, cu = _attn_case(21, [new], [kv], Hq, Hkv, D, page)
+    want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, 0.2 * D ** -0.5, "causal")
+    got = ref.to_numpy(_attend(q, cache, table, [kv], cu, new, "causal", scale=0.2 * D ** -0.5))
+    assert np.linalg.norm(got - want) <= 5e-3 * np.linalg.norm(want)
+
+
+@gpu
+@pytest.mark.parametrize("new,D", [(1, 128), (5, 64), (10, 64), (40, 128), (200, 64)])
+@pytest.mark.parametrize("key_mul,value_mul,some", [(1e-7, 1.0, False), (1e6, 1.0, False), (1.0, 1e-7, False), (1.0, 1e6, False), (1e5, 3e-5, True),
+                                                    (1e-6, 1e5, True), (2.0 ** 100, 2.0 ** 100, False), (2.0 ** -90, 2.0 ** -90, True)])
+def test_attention_at_the_ends_of_the_number_range(new, D, key_mul, value_mul, some):
+    """Keys and values far from 1, of all tokens or of every seventh; the queries bring the scores back to the usual size."""
+    Hq, Hkv, page, kv = 4, 2, 32, 700
+    r, q, cache, table, cu = _attn_case(31, [new], [kv], Hq, Hkv, D, page)
+    runs = cache.reshape(len(cache), Hkv, page // 16, 16 * (D + 8))
+    num = runs[..., 16 * D:].copy().view(np.uint16).astype(np.uint32) << 16
+    num = num.view(np.float32).reshape(*runs.shape[:3], 16, 4).astype(np.float64)
+    which = (np.arange(16) % 7 == 3) if some else np.ones(16, dtype=bool)
+    num[..., which, 0:2] *= key_mul
+    num[..., which, 2:4] *= value_mul
+    bits = (np.ascontiguousarray(num.astype(np.float32)).view(np.uint32) >> 16).astype(np.uint16)
+    runs[..., 16 * D:] = np.ascontiguousarray(bits).view(np.uint8).reshape(*runs.shape[:3], 128)
+    back = 1.0 / key_mul if not some or key_mul > 1 else 1.0
+    q = (q.double() * back).to(torch.bfloat16)
+    args = (ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, D ** -0.5, "causal")
+    want = ref.attend(*args)
+    got = ref.to_numpy(_attend(q, cache, table, [kv], cu, new, "causal"))
+    assert np.isfinite(got).all()
+    # against each output's own size: columns of a row may be of any
+    assert np.linalg.norm(got - want) <= 5e-3 * np.linalg.norm(want)
+
+
+@gpu
 @pytest.mark.parametrize("D,Hq,Hkv,new", [(128, 5, 1, 1), (64, 4, 2, 6), (128, 40, 8, 40), (64, 16, 2, 200)])
 def test_attention_ignores_what_it_must_not_see(D, Hq, Hkv, new):
     """Unwritten places of the pages, pages beyond the length, tokens that the mask hides: all NaN, all block numbers wild."""
