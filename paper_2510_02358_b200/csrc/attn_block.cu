@@ -137,8 +137,10 @@ __device__ __forceinline__ void pair_barrier(int id, int threads) { asm volatile
 // ------------------------------------------------------------------------------- cut of the work
 // A request's units: tiles of 256 rows, for each tile its key heads.  A token tile of a unit with more
 // than 128 rows counts kWide on the line, of one with fewer kNarrow: it has half the products but the
-// same keys and values to expand (measured: 4350 against 5700 clocks).
-constexpr int kWide = 4, kNarrow = 3;
+// same keys and values to expand (measured: 4350 against 5700 clocks).  Before its first token a unit has kEnter places of the line
+// for what every unit costs, its queries and its output: with none the shares of many short units took longer than others (16
+// requests of 65 new tokens over 8192, 40 heads on 8: 167 us instead of 153; 24 places: 157).
+constexpr int kWide = 4, kNarrow = 3, kEnter = 12;
 struct BlockRequest {
     int b, n_new, kv, rows, row0, group, tiles;
     bool causal;
@@ -156,13 +158,14 @@ struct BlockRequest {
         const int end = causal ? min(kv, kv - n_new + last + 1) : kv;
         return max(1, (end + kTile - 1) / kTile);
     }
+    __device__ __forceinline__ int places(int tile) const { return steps(tile) * weight(tile) + kEnter; }
     __device__ __forceinline__ long long length(int Hkv) const {
         if (!causal) {
             const long long whole = rows / (2 * kTile), rest = rows - whole * 2 * kTile, n = max(1, (kv + kTile - 1) / kTile);
-            return Hkv * n * (kWide * whole + (rest > kTile ? kWide : rest > 0 ? kNarrow : 0));
+            return Hkv * (n * (kWide * whole + (rest > kTile ? kWide : rest > 0 ? kNarrow : 0)) + (long long)kEnter * tiles);
         }
         long long n = 0;
-        for (int t = 0; t < tiles; ++t) n += (long long)steps(t) * weight(t);
+        for (int t = 0; t < tiles; ++t) n += places(t);
         return n * Hkv;
     }
 };
@@ -181,12 +184,12 @@ struct Walk {
         rq.load(a, s.b, 0, 0);
         long long rest = at - s.before;
         while (true) {
-            const long long len = (long long)rq.steps(tile) * rq.weight(tile) * a.Hkv;
+            const long long len = (long long)rq.places(tile) * a.Hkv;
             if (rest < len) break;
             rest -= len;
             ++tile;
         }
-        const int unit = rq.steps(tile) * rq.weight(tile);
+        const int unit = rq.places(tile);
         h = (int)(rest / unit);
         off = (int)(rest - (long long)h * unit);
     }
@@ -195,9 +198,9 @@ struct Walk {
         while (at < end) {
             steps = rq.steps(tile);
             weight = rq.weight(tile);
-            const int len = steps * weight, take = (int)min((long long)(len - off), end - at);
-            step0 = off / weight;
-            step1 = off + take == len ? steps : (off + take) / weight;
+            const int len = steps * weight + kEnter, take = (int)min((long long)(len - off), end - at);
+            step0 = max(off - kEnter, 0) / weight;
+            step1 = max(off + take - kEnter, 0) / weight;
             at += take;
             off += take;
             if (step1 > step0) return true;
@@ -292,6 +295,11 @@ __device__ __forceinline__ uint4 values_bf16(uint32_t w, const Affine &a) {
 }
 __device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
 }
 // The largest number that a head of scale and offset p (bf16 each) may hold, in magnitude.
 __device__ __forceinline__ float largest(uint32_t p) { return fmaxf(fabsf(bf16_hi(p)), fabsf(fmaf(15.0f, bf16_lo(p), bf16_hi(p)))); }
@@ -610,40 +618,41 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         const bool live = row < w.rq.rows;
         const long long token = w.rq.row0 + qi;
         const int head = w.h * a.group + row - qi * a.group;
-        // queries into shared memory (the products of the segment before are done: out_done was waited for)
-        float back = 1.0f;
-        bool lost_row = false;                                     // an infinity or a NaN among its queries
+        // queries into shared memory (the products of the segment before are done: out_done was waited for); kRowLanes lanes share a
+        // row, so that a load takes whole rows and a store all banks
+        constexpr int kRowLanes = D / 8, kRowsTurn = 32 / kRowLanes;
         if (wide || slot == 0) {
-            const uint32_t dst = q_at + (wide ? slot : 0) * kTileBytes;
-            const uint4 *src = reinterpret_cast<const uint4 *>(a.q + token * a.q_t + (long long)head * a.q_h);
-            auto load = [&](int i) { return live ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u); };
-            float top = 0.0f;
+            const uint32_t q_tile = q_at + slot * kTileBytes;
+            const unsigned long long src = (unsigned long long)(a.q + token * a.q_t + (long long)head * a.q_h);
+            const uint32_t lives = __ballot_sync(0xFFFFFFFFu, live);
+            const int piece = lane % kRowLanes;
+            uint4 x[kRowLanes];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {                      // read twice: the second time from the first-level cache
-                const uint4 x = load(i);
-                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float f = bf16_lo(v[e]), g = bf16_hi(v[e]);
-                    top = max3(top, fabsf(f), fabsf(g));
-                    lost_row = lost_row || !(fabsf(f) <= 3.402823466e38f) || !(fabsf(g) <= 3.402823466e38f);
-                }
+            for (int i = 0; i < kRowLanes; ++i) {
+                const int rr = i * kRowsTurn + lane / kRowLanes;
+                const uint4 *from = reinterpret_cast<const uint4 *>(__shfl_sync(0xFFFFFFFFu, src, rr)) + piece;
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if ((lives >> rr) & 1u) x[i] = __ldg(from);
             }
-            // the row's largest number to 1 .. 2, with the scale's sign; taken back below
-            const int ex = min(max((int)(__float_as_uint(top) >> 23), 27), 227);
-            const float up = copysignf(__uint_as_float((uint32_t)(254 - ex) << 23), a.scale_log2);
-            back = __uint_as_float((uint32_t)ex << 23);
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                const uint4 x = load(i);
-                const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+            for (int i = 0; i < kRowLanes; ++i) {
+                const int rr = warp * 32 + i * kRowsTurn + lane / kRowLanes;
+                // the largest magnitude, as bits: infinities and NaN lie above all numbers
+                uint32_t top = __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+#pragma unroll
+                for (int o = 1; o < kRowLanes; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                top = max(top & 0xFFFFu, top >> 16);
+                // the row's largest number to 1 .. 2, with the scale's sign; taken back below
+                const int ex = min(max((int)(top >> 7), 27), 227);
+                const float up = copysignf(__uint_as_float((uint32_t)(254 - ex) << 23), a.scale_log2);
+                const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
                 uint32_t h[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[e] = pack2_f16(bf16_lo(v[e]) * up, bf16_hi(v[e]) * up);
-                store16(dst + piece_at(me, i), make_uint4(h[0], h[1], h[2], h[3]));
+                store16(q_tile + piece_at(rr, piece), make_uint4(h[0], h[1], h[2], h[3]));
+                if (piece == 0) s_back[slot * kTile + rr] = top >= 0x7F80u ? CUDART_NAN_F : __uint_as_float((uint32_t)ex << 23);
             }
             fence_smem();
-            s_back[slot * kTile + me] = lost_row ? CUDART_NAN_F : back;
         }
         __syncwarp();
         if (lane == 0) bar_arrive(smem_u32(&bars->query_ready));
@@ -803,7 +812,8 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
             if (*dead) sum = CUDART_NAN_F;
             const bool whole = w.step0 == 0 && w.step1 == w.steps;
             const float inv = sum == 0.0f ? 0.0f : whole ? 1.0f / (sum * kValueMul) : 1.0f / kValueMul;
-            const int part_row = (wide ? slot * kTile : 0) + me;
+            const int part_row = slot * kTile + me;
+            const uint32_t q_tile = q_at + slot * kTileBytes;
             float *part = a.part + ((long long)blockIdx.x * 2 + (w.step0 == 0 ? 1 : 0)) * (2 * kTile * (D + 2));
 #pragma unroll 1
             for (int k = 0; k < D / 32; ++k) {
@@ -823,19 +833,31 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
 #pragma unroll
                     for (int e = 0; e < 32; ++e) x[e] = CUDART_NAN_F;
                 }
-                if (!live) continue;
-                if (whole) {
-                    uint4 *dst = reinterpret_cast<uint4 *>(a.out + (token * a.Hq + head) * D + 32 * k);
+                if (whole) {                                       // by way of the queries' place, whose products are done
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        dst[e] = sum == 0.0f ? make_uint4(0u, 0u, 0u, 0u)
-                                             : make_uint4(pack2(x[8 * e] * inv, x[8 * e + 1] * inv), pack2(x[8 * e + 2] * inv, x[8 * e + 3] * inv),
-                                                          pack2(x[8 * e + 4] * inv, x[8 * e + 5] * inv), pack2(x[8 * e + 6] * inv, x[8 * e + 7] * inv));
-                } else {
-                    float4 *dst = reinterpret_cast<float4 *>(part + (long long)part_row * D + 32 * k);
+                        store16(q_tile + piece_at(me, 4 * k + e),
+                                sum == 0.0f ? make_uint4(0u, 0u, 0u, 0u)
+                                            : make_uint4(pack2(x[8 * e] * inv, x[8 * e + 1] * inv), pack2(x[8 * e + 2] * inv, x[8 * e + 3] * inv),
+                                                         pack2(x[8 * e + 4] * inv, x[8 * e + 5] * inv), pack2(x[8 * e + 6] * inv, x[8 * e + 7] * inv)));
+                } else {                                           // rows lie next to each other, as the lanes do
+                    float4 *dst = reinterpret_cast<float4 *>(part) + 8 * k * (2 * kTile) + part_row;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) dst[e] = make_float4(x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv);
+                    for (int e = 0; e < 8; ++e) dst[e * (2 * kTile)] = make_float4(x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv);
                 }
+            }
+            if (whole) {
+                const int row2 = w.row_first() + part_row, q2 = row2 / a.group;       // once more: registers are short
+                const unsigned long long dst =
+                    row2 < w.rq.rows ? (unsigned long long)(a.out + ((long long)(w.rq.row0 + q2) * a.Hq + w.h * a.group + row2 - q2 * a.group) * D) : 0ULL;
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < kRowLanes; ++i) {
+                    const int rr = i * kRowsTurn + lane / kRowLanes, piece = lane % kRowLanes;
+                    uint4 *to = reinterpret_cast<uint4 *>(__shfl_sync(0xFFFFFFFFu, dst, rr));
+                    if (to) to[piece] = load16(q_tile + piece_at(warp * 32 + rr, piece));
+                }
+                __syncwarp();                                      // before the next segment's queries take the place
             }
             if (!whole) {
                 part[2 * kTile * D + part_row] = top;
@@ -843,7 +865,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 if (w.step0 == 0 && me == 0 && slot == 0) {
                     SplitUnit u;
                     u.b = w.rq.b; u.h = w.h; u.tile = w.tile;
-                    u.last_cta = cta_of(w.at - w.off + (long long)w.steps * w.weight - 1, w.total, w.ctas);
+                    u.last_cta = cta_of(w.at - w.off + (long long)w.steps * w.weight + kEnter - 1, w.total, w.ctas);
                     a.split[blockIdx.x] = u;
                 }
             }
@@ -930,6 +952,9 @@ __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const Att
     const int rows = rq.rows_of(u.tile);
     if (chunk * kJoinRows >= rows) return;
     const float *base = a.part + (long long)first * 2 * kPart;
+    // a warp takes four rows and eight pieces of four channels: whole sectors of the parts, where rows are neighbours, and of the output
+    auto row_of = [&](int i) { return chunk * kJoinRows + ((i >> 5) & 3) * 4 + (i & 3); };
+    auto piece_of = [&](int i) { return (i >> 7) * 8 + ((i >> 2) & 7); };
     auto part_of = [&](int i) { return base + (long long)(2 * i + (i == 0 ? 1 : 0)) * kPart; };
     float4 x[kVec];
     float m[kVec], l[kVec];
@@ -942,7 +967,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const Att
     for (int i0 = 0; i0 < n; i0 += kJoinTurn) {
 #pragma unroll
         for (int k = 0; k < kVec; ++k) {
-            const int i = threadIdx.x + k * kJoinThreads, row = chunk * kJoinRows + i / (D / 4), ch = (i % (D / 4)) * 4;
+            const int i = threadIdx.x + k * kJoinThreads, row = row_of(i), piece = piece_of(i);
             float4 y[kJoinTurn];
             float my[kJoinTurn], ly[kJoinTurn];
 #pragma unroll
@@ -951,7 +976,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const Att
                 const float *p = part_of(i0 + w);
                 my[w] = ok ? __ldg(p + 2 * kTile * D + row) : -CUDART_INF_F;
                 ly[w] = ok ? __ldg(p + 2 * kTile * D + 2 * kTile + row) : 0.0f;
-                y[w] = ok ? __ldg(reinterpret_cast<const float4 *>(p + (long long)row * D + ch)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                y[w] = ok ? __ldg(reinterpret_cast<const float4 *>(p) + piece * (2 * kTile) + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
             float top = m[k];
 #pragma unroll
@@ -971,7 +996,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const Att
     }
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-        const int i = threadIdx.x + k * kJoinThreads, row = chunk * kJoinRows + i / (D / 4), ch = (i % (D / 4)) * 4;
+        const int i = threadIdx.x + k * kJoinThreads, row = row_of(i), ch = piece_of(i) * 4;
         if (row >= rows) continue;
         const float inv = 1.0f / l[k];
         const int rr = u.tile * 2 * kTile + row, qi = rr / a.group;
