@@ -666,7 +666,8 @@ def dsp_breadth_update(state: BreadthState, params: BreadthParams, entropy, acce
 
 
 # ---- the model pass around the step: paged 4-bit cache and attention over it ----
-# These calls are made once per layer, so their checks are kept short.
+# These calls are made once per layer, so their checks are kept short (and sizes of new tensors are passed one by one:
+# 1.5 us on the host, where a tuple takes 2.2).
 
 def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
@@ -718,12 +719,13 @@ def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: to
         _ints("node_depth", node_depth, (B, N), i32, dev)
         mask_words = mask_words or (N + 32) // 32
     if out is None:
-        e = torch.empty                        # a tensor each: views of one buffer take longer to make
-        out = SimpleNamespace(block_count=e(B, dtype=i32, device=dev), kv_len=e(B, dtype=i32, device=dev),
-                              row_status=e(B, dtype=i32, device=dev), cu_new=e(B + 1, dtype=i32, device=dev),
+        # six views of one buffer: 3.9 us on the host, where six tensors take 8.5
+        e = torch.empty
+        count, kv, status, cu, position, row = torch.unsafe_split_with_sizes(
+            e(4 * B + 1 + 2 * T, dtype=i32, device=dev), (B, B, B, B + 1, T, T))
+        out = SimpleNamespace(block_count=count, kv_len=kv, row_status=status, cu_new=cu,
                               ring_pos=e(2, dtype=i64, device=dev), slot=e(T, dtype=i64, device=dev),
-                              position=e(T, dtype=i32, device=dev), token_row=e(T, dtype=i32, device=dev),
-                              mask=e((T, mask_words), dtype=i32, device=dev) if N else None)
+                              position=position, token_row=row, mask=e(T, mask_words, dtype=i32, device=dev) if N else None)
     _check("dsp_cache_plan", lib().dsp_cache_plan(
         seq_len.data_ptr(), new_len.data_ptr(), block_count.data_ptr(), ring_pos.data_ptr(), B, T, page_size, n_blocks, width,
         table, stride, free_ring.data_ptr(), _at(node_parent), _at(node_depth), N,
@@ -772,7 +774,7 @@ def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[tor
     Hkv, kt, kh = _heads("k", k, T, D, dt, dev)
     wq, wk, pos, cs, rows, rot = _rope(q_weight, k_weight, positions, cos_sin, T, D, dt, dev)
     if out is None:
-        q_out, k_out = torch.empty((T, Hq, D), dtype=dt, device=dev), torch.empty((T, Hkv, D), dtype=dt, device=dev)
+        q_out, k_out = torch.empty(T, Hq, D, dtype=dt, device=dev), torch.empty(T, Hkv, D, dtype=dt, device=dev)
     else:
         q_out, k_out = _ints("out[0]", out[0], (T, Hq, D), dt, dev), _ints("out[1]", out[1], (T, Hkv, D), dt, dev)
     _check("dsp_qk_norm_rope", lib().dsp_qk_norm_rope(
@@ -811,7 +813,7 @@ def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
     if q is None:
         out = None
     elif out is None:
-        out = torch.empty((T, Hq, D), dtype=dt, device=dev)
+        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
     else:
         _ints("out", out, (T, Hq, D), dt, dev)
     _check("dsp_kv4_append", lib().dsp_kv4_append(
@@ -826,7 +828,7 @@ def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bf
     n_blocks, page = _cache(cache, Hkv, D, dev)
     _ints("slot", slot, (T,), torch.int64, dev)
     if out is None:
-        k, v = torch.empty((T, Hkv, D), dtype=dtype, device=dev), torch.empty((T, Hkv, D), dtype=dtype, device=dev)
+        k, v = torch.empty(T, Hkv, D, dtype=dtype, device=dev), torch.empty(T, Hkv, D, dtype=dtype, device=dev)
     else:
         k, v = (_ints("out", t, (T, Hkv, D), dtype, dev) for t in out)
     _check("dsp_kv4_read", lib().dsp_kv4_read(cache.data_ptr(), n_blocks, page, Hkv, D, slot.data_ptr(), T, _dtype(k),
@@ -836,7 +838,7 @@ def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bf
 
 @lru_cache(maxsize=1024)
 def _attn_workspace(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int, device: int) -> int:
-    return dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new)      # a function of the sizes and the device's SM count
+    return max(256, dsp_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D, max_new))      # a function of the sizes and the device's SM count
 
 
 def dsp_attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_new: int) -> int:
@@ -866,11 +868,11 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
         words = mask.shape[-1]
         bits = _ints("mask", mask, (T, words), torch.int32, dev)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=dt, device=dev)
+        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
     else:
         _ints("out", out, (T, Hq, D), dt, dev)
     if workspace is None:
-        workspace = alloc_workspace(_attn_workspace(B, T, Hq, Hkv, D, max_new, dev.index), dev)
+        workspace = torch.empty(_attn_workspace(B, T, Hq, Hkv, D, max_new, dev.index), dtype=torch.uint8, device=dev)
     _check("dsp_attn_kv4", lib().dsp_attn_kv4(
         q.data_ptr(), _dtype(q), B, T, Hq, Hkv, D, qt, qh, cache.data_ptr(), n_blocks, page, table, stride, width,
         kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,
