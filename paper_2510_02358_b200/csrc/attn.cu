@@ -159,8 +159,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     if (threadIdx.x == 0) a.split[blockIdx.x].last_cta = -1;
     enter_line<StreamRequest>(a, kRows, kStep, 1, s_scan, &s_line);
     long long at = s_line.begin;
-    const long long end = s_line.end, total = s_line.total;
-    if (at >= end) return;
+    if (at >= s_line.end) return;
     const int runs_page = a.page >> 4;
     const long long head_bytes = (long long)runs_page * Kv4<D>::kRunBytes, block_bytes = head_bytes * a.Hkv;
 
@@ -174,7 +173,7 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
     while (true) {
         const int unit = (int)((at - before) / rq.places()), off = (int)(at - before - (long long)unit * rq.places());
         const int h = unit / rq.tiles, tile = unit - h * rq.tiles;
-        const int take = (int)min((long long)rq.places() - off, end - at);
+        const int take = (int)min((long long)rq.places() - off, s_line.end - at);
         const int step0 = max(off - kEnter, 0), step1 = max(off + take - kEnter, 0);
         at += take;
         if (step0 == step1) break;                                // only places of the way in are left: the next CTA's unit
@@ -554,10 +553,10 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
         if (starts && !ends && threadIdx.x == 0) {
             SplitUnit u;
             u.b = rq.b; u.h = h; u.tile = tile;
-            u.last_cta = cta_of(at - off - take + rq.places() - 1, total, s_line.ctas);
+            u.last_cta = cta_of(before + (long long)(h * rq.tiles + tile + 1) * rq.places() - 1, s_line.total, s_line.ctas);
             a.split[blockIdx.x] = u;
         }
-        if (at >= end) break;
+        if (at >= s_line.end) break;
         while (at >= before + rq.length(a.Hkv)) {
             before += rq.length(a.Hkv);
             rq.load(a, rq.b + 1, kRows, kStep);
