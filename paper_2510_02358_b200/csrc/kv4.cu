@@ -612,20 +612,26 @@ bool strides_ok(int64_t st, int64_t sh, int32_t H, int32_t D) { return sh >= D &
 template <typename DT, int D, bool kAppend>
 cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
     // A long append is two launches: its queries alone need fewer registers and less code than keys and values, and so run
-    // faster (8192 tokens of 40 + 2 x 8 heads of 128: 85 us together); a short one is bound by the launch.
-    if (kAppend && a.Hq > 0 && (long long)a.T * (a.Hq + 2 * a.Hkv) * (D / 16) > 148LL * 2048) {
+    // faster (8192 tokens of 40 + 2 x 8 heads of 128: 64 us instead of 74; 2048: 19.8 and 20.3; 1024: 12.4 and 12.1).
+    if (kAppend && a.Hq > 0 && (long long)a.T * (a.Hq + 2 * a.Hkv) * (D / 16) > 148LL * 4096) {
         NormArgs q = a;
         q.Hkv = 0;
         const cudaError_t e = launch_norm_heads<DT, D, false>(q, st);
         if (e != cudaSuccess) return e;
         a.Hq = 0;
     }
-    // Several heads to a group of lanes once single heads would need more than one round of CTAs (148 SMs of about 1024
-    // threads): a short call is the latency of one group's chain, a long one wants loads in flight.
-    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2));
+    // Several heads to a group of lanes where there is more than a round or two of groups: a short call is the latency of one
+    // group's chain, a long one wants loads in flight.  40 + 8 heads of 128, several and one: 64 tokens 2.5 and 2.4 us, 272: 3.5 and
+    // 3.6, 512: 4.6 and 5.4, 8192: 46 and 70.  With the codes the chain is longer and registers are dearer: 512 tokens 8.1 and 7.2, 800: 11.3
+    // and 11.2, 8192: 64 and 89.
+    // Half-head rotations split a row's loads into pieces of D / 4 channels, and pairs pay less in long calls, by size and type (8192
+    // tokens, paired and not; bf16, 40 heads of 64: 18.7 and 20.8 us, 48 of 128: 67 and 53, 20 of 256: 39 and 45;
+    // fp32, 40 of 64: 65 and 33, 20 of 128: 37 and 33).  Short ones keep them (64 tokens, bf16, 48 of 128: 3.0 and 3.3).
+    const bool halves = sizeof(DT) == 2 && D != 128;
+    const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv), limit = 148LL * (kAppend ? 2048 : 512);
+    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || (a.rot == D / 2 && (halves || rows * (D / 16) <= limit))));
     const int lanes = paired ? D / 16 : D / 8;
-    const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv);
-    const bool wide = rows * lanes > 148LL * 1024;
+    const bool wide = rows * lanes > limit;
     const int per = !wide ? 1 : paired ? 2 : 4;
     a.q_chunks = (a.Hq + per - 1) / per;
     a.k_chunks = (a.Hkv + per - 1) / per;

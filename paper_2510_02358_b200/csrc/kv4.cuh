@@ -37,7 +37,4 @@ __device__ __forceinline__ long long block_of(long long slot, int page) {
     return (slot >> 32) ? slot / page : (long long)((uint32_t)slot / (uint32_t)page);
 }
 
-// Codes of the channels 2i (nibble i) and 2i + 1 (nibble i + 4) of a word.
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) { return (w >> (4 * i)) & 0x000F000Fu; }
-
 }  // namespace dsp
