@@ -627,12 +627,13 @@ cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
     // group's chain, a long one wants loads in flight.  40 + 8 heads of 128, several and one: 64 tokens 2.5 and 2.4 us, 272: 3.5 and
     // 3.6, 512: 4.6 and 5.4, 8192: 46 and 70.  With the codes the chain is longer and registers are dearer: 512 tokens 8.1 and 7.2, 800: 11.3
     // and 11.2, 8192: 64 and 89.
-    // Half-head rotations split a row's loads into pieces of D / 4 channels, and pairs pay less in long calls, by size and type (8192
-    // tokens, paired and not; bf16, 40 heads of 64: 18.7 and 20.8 us, 48 of 128: 67 and 53, 20 of 256: 39 and 45;
-    // fp32, 40 of 64: 65 and 33, 20 of 128: 37 and 33).  Short ones keep them (64 tokens, bf16, 48 of 128: 3.0 and 3.3).
-    const bool halves = sizeof(DT) == 2 && D != 128;
+    // Pairs save shuffles and read both halves of a row at once, which in long calls pays in bf16 only, and not where half of a head of
+    // 128 is turned (8192 tokens, paired and not; bf16: 48 heads of 128 45 and 54 us, half turned 67 and 53; 40 of 64 18.8 and 21.0, half
+    // turned 18.7 and 20.8; 20 of 256, half turned 39 and 45.  fp32: 40 of 64 35 and 33, half turned 65 and 33; 20 of 128 38 and 35).
+    // Short calls are always better paired (64 tokens, bf16, 48 of 128: 2.5 and 3.3, half turned 3.0 and 3.3).
     const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv), limit = 148LL * (kAppend ? 2048 : 512);
-    const bool paired = !a.cos_sin || (!a.interleaved && (a.rot == D || (a.rot == D / 2 && (halves || rows * (D / 16) <= limit))));
+    const bool apart = sizeof(DT) == 4 || (D == 128 && a.cos_sin && a.rot == D / 2);
+    const bool paired = (!apart || rows * (D / 16) <= limit) && (!a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2)));
     const int lanes = paired ? D / 16 : D / 8;
     const bool wide = rows * lanes > limit;
     const int per = !wide ? 1 : paired ? 2 : 4;
@@ -641,9 +642,9 @@ cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
     a.chunks = a.q_chunks + (kAppend ? 2 : 1) * a.k_chunks;
     const long long groups = (long long)a.T * a.chunks, per_cta = kNormThreads / lanes;
     const unsigned grid = (unsigned)((groups + per_cta - 1) / per_cta);
-    if (paired && wide)
-        norm_rope_paired_kernel<DT, D, kAppend, 2><<<grid, kNormThreads, 0, st>>>(a);
-    else if (paired)
+    if (paired && wide) {
+        if constexpr (sizeof(DT) == 2) norm_rope_paired_kernel<DT, D, kAppend, 2><<<grid, kNormThreads, 0, st>>>(a);
+    } else if (paired)
         norm_rope_paired_kernel<DT, D, kAppend, 1><<<grid, kNormThreads, 0, st>>>(a);
     else if (wide)
         norm_rope_kernel<DT, D, kAppend, 4><<<grid, kNormThreads, 0, st>>>(a);

@@ -188,6 +188,33 @@ def test_unaligned_and_strided_rows_give_the_same_bits(bf16):
 
 
 @gpu
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("D,rot,inter", [(64, 64, False), (64, 32, False), (64, 64, True), (64, 0, False), (128, 128, False), (128, 64, False),
+                                         (128, 128, True), (128, 48, False), (128, 0, False), (256, 256, False), (256, 128, False), (256, 64, True)])
+def test_long_calls_give_the_bits_of_short_ones(D, rot, inter, bf16):
+    """However a call's length cuts it, rows, codes and what is read back are those of calls of a few tokens."""
+    dt = torch.bfloat16 if bf16 else torch.float32
+    T, Hq, Hkv, part = 2500, 23, 5, 50
+    g = torch.Generator(device=DEV).manual_seed(D + rot + bf16)
+    q, k, v = torch.randn(T, Hq + 2 * Hkv, D, generator=g, device=DEV).to(dt).split([Hq, Hkv, Hkv], 1)
+    w = torch.randn(D, generator=g, device=DEV).to(dt)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    rope = dict(q_weight=w, k_weight=w, cos_sin=_angles(T, rot) if rot else None, interleaved=inter)
+    norm_q, norm_k = dsp.dsp_qk_norm_rope(q, k, positions=pos, **rope)
+    few = [dsp.dsp_qk_norm_rope(q[i:i + part], k[i:i + part], positions=pos[i:i + part], **rope) for i in range(0, T, part)]
+    assert torch.equal(norm_q, torch.cat([x for x, _ in few])) and torch.equal(norm_k, torch.cat([y for _, y in few]))
+    if D == 256:
+        return
+    slot = torch.randperm(2560, generator=g, device=DEV)[:T]
+    caches = [dsp.kv4_cache(40, Hkv, D, 64, DEV) for _ in range(2)]
+    one = dsp.dsp_kv4_append(q, k, v, slot, caches[0], positions=pos, **rope)
+    for i in range(0, T, part):
+        s = slice(i, i + part)
+        assert torch.equal(one[s], dsp.dsp_kv4_append(q[s], k[s], v[s], slot[s], caches[1], positions=pos[s], **rope))
+    assert torch.equal(one, norm_q) and torch.equal(caches[0], caches[1])
+
+
+@gpu
 @pytest.mark.parametrize("T,Hq,Hkv,D,page,bf16", [(1, 4, 1, 128, 16, True), (1, 1, 1, 64, 16, False), (37, 10, 2, 64, 48, True),
                                                   (61, 5, 5, 128, 32, False), (900, 28, 4, 128, 64, True), (513, 24, 8, 64, 16, True)])
 def test_append_stores_what_the_definition_says(T, Hq, Hkv, D, page, bf16):
