@@ -12,8 +12,8 @@
 // so the same row gives the same bits (and, right on the edge between two codes, the same code)
 // from every call shape, and dsp_kv4_append's keys are those of dsp_qk_norm_rope.
 //
-// Measured, 8192 tokens: norm and rotation of 40 + 8 heads of 128 in bf16 45 us (201 MB, 4.5 TB/s), with keys and values stored 64 us (219
-// MB, 3.4 TB/s: the codes' arithmetic is the larger part of the second launch); 8 tokens 2.1 and 2.6 us, a launch's latency.
+// Measured, 8192 tokens: norm and rotation of 40 + 8 heads of 128 in bf16 45 us (201 MB, 4.5 TB/s), with keys and values stored 66 us (219
+// MB, 3.3 TB/s: the codes' arithmetic is the larger part of the second launch); 8 tokens 2.1 and 2.6 us, a launch's latency.
 #include "kv4.cuh"
 
 namespace dsp {
@@ -55,6 +55,10 @@ __device__ __forceinline__ Two add2(Two x, Two y) {
         : "+f"(x.a), "+f"(x.b) : "f"(y.a), "f"(y.b));
     return x;
 }
+
+// Sum of two products, each rounded for itself.  The additions are single ones: a packed product and the packed sum that takes it
+// are built as one fused step, although both ask for a rounding of their own (tenths of the rotated numbers then had another last bit, and a key's code, once in some 10^4 heads, was another).
+__device__ __forceinline__ Two add_products(Two x, Two y) { return {__fadd_rn(x.a, y.a), __fadd_rn(x.b, y.b)}; }
 
 __device__ __forceinline__ Two fma2(Two x, Two y, Two z) {
     asm("{\n .reg .b64 u, v, w;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mov.b64 w, {%4, %5};\n fma.rn.f32x2 u, u, v, w;\n mov.b64 {%0, %1}, u;\n}"
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float ce = e & 1 ? c[e >> 1].b : c[e >> 1].a, se = e & 1 ? s[e >> 1].b : s[e >> 1].a;
-                        x[e] = add2(mul2(x[e], {ce, ce}), mul2({x[e].b, x[e].a}, {-se, se}));
+                        x[e] = add_products(mul2(x[e], {ce, ce}), mul2({x[e].b, x[e].a}, {-se, se}));
                     }
                 }
             } else {
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(kNormThreads, kHeads > 1 && sizeof(DT) == 2 &&
                 for (int e = 0; e < 4; ++e) {
                     const Two o = {__shfl_sync(0xFFFFFFFFu, x[e].a, from, kLanes), __shfl_sync(0xFFFFFFFFu, x[e].b, from, kLanes)};
                     if (turned) {
-                        x[e] = add2(mul2(x[e], c[e]), mul2(o, first ? Two{-s[e].a, -s[e].b} : s[e]));      // a - b and a + (-b) are the same number
+                        x[e] = add_products(mul2(x[e], c[e]), mul2(o, first ? Two{-s[e].a, -s[e].b} : s[e]));      // a - b and a + (-b) are the same number
                     }
                 }
             }
@@ -513,8 +517,8 @@ __global__ void __launch_bounds__(kNormThreads, 3) norm_rope_paired_kernel(const
         if (turned) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {                          // a - b and a + (-b) are the same number
-                const Two z = add2(mul2(x[e], c[e]), mul2(y[e], {-s[e].a, -s[e].b}));
-                y[e] = add2(mul2(y[e], c[e]), mul2(x[e], s[e]));
+                const Two z = add_products(mul2(x[e], c[e]), mul2(y[e], {-s[e].a, -s[e].b}));
+                y[e] = add_products(mul2(y[e], c[e]), mul2(x[e], s[e]));
                 x[e] = z;
             }
         }
