@@ -8,16 +8,16 @@
 // tensor cores form the scores of a slot's next half tile while its last one is exponentiated, so the
 // softmax warps, which are the slowest part, need not wait for them.
 //
-//   warps 0-7   softmax, four per slot, one thread per query row: maximum, exponentials, weights in bf16
+//   warps 0-7   softmax, four per slot, one thread per query row: maximum, exponentials, weights in fp16
 //               back into the scores' columns as the second product's operand
 //   warps 8-15  the tiles' codes (a run of 16 tokens each, keys then values): 16-byte loads one tile
-//               ahead in registers, four bits to bf16 values, swizzled stores; two stages of each
+//               ahead in registers, four bits to fp16 values, swizzled stores; two stages of each
 //   warps 16-17 one lane each issues the products of a slot: S = Q K^T, O += P V
 //
 // Here a cached number is expanded once for 128 or 256 rows, so it becomes a whole value on the way
 // (code * scale + offset, one rounding): folding the scales into the sums, as the kernel for few rows
 // does, would cost each score more than that.  The operands are fp16, whose 11 bits leave the result's
-// own rounding to bf16 as the only error that counts (0.0017 of an output in the mean; with bf16 operands
+// own rounding to bf16 as the error that counts (0.0017 of an output in the mean; with bf16 operands
 // it was 0.0035).  What fp16's range does not hold is brought into it by powers of two: a row of queries
 // by its largest number, taken back with the softmax scale; a key whose largest number lies outside
 // 2^-4 .. 2^15 by that, its scores being multiplied back (k_mul).  Values are multiplied by 64, and the 16
@@ -48,6 +48,10 @@ constexpr int kTile = 128;                       // query rows of a slot, tokens
 constexpr int kHalf = kTile / 2;                 // tokens whose scores are formed and exponentiated at once
 constexpr int kRunsTile = kTile / 16;
 constexpr long long kWaitClocks = 4000000000LL;  // about two seconds: a wait that long has failed
+// Weights are formed as 2^(score - maximum + 7): at most 2^15, since a score passes the maximum by no more than 2^8, and whole fp16
+// numbers down to 2^-21 of it.  Beside one dominant token the others' weights are small, and without the 7 they lost their last bits
+// (at 2^-25 of it 1.3% of the output).  Sums and outputs carry the same 2^7, so it leaves with the division.
+constexpr float kWeightUp = 7.0f;
 
 // ---------------------------------------------------------------- tensor cores and barriers (PTX)
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -749,7 +753,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 }
             }
             fresh = false;
-            const float base = m == -CUDART_INF_F ? 0.0f : m;
+            const float base = m == -CUDART_INF_F ? 0.0f : m - kWeightUp;
             float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < 2; ++k) {

@@ -1,0 +1,78 @@
+"""dsp_attn_kv4 where masks, lengths, weights and numbers are at their ends, against the plain 64-bit definition.
+
+Tolerances (2-norm of the difference over the 2-norm of the output).  The output's own rounding to bf16 makes
+1.7e-3.  Up to 32 query rows a key head: weight times value scale is rounded to bf16, another 1.7e-3, so 2.4e-3;
+3.5e-3 is allowed.  More rows: queries, keys, weights and values are fp16 (2.8e-4 each at most, small against the
+rest), so 1.8e-3; 2.5e-3 is allowed.
+"""
+import numpy as np
+import pytest
+import torch
+
+import pass_reference as ref
+from paper_2510_02358_b200 import binding as dsp
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _allowed(rows):
+    return 3.5e-3 if rows <= 32 else 2.5e-3
+
+
+def _off(got, want):
+    return np.linalg.norm(ref.to_numpy(got) - want) / np.linalg.norm(want)
+
+
+def _case(seed, new, kv, Hq, Hkv, D, page, centred=False):
+    """Random codes of unit spread, every request with blocks of its own."""
+    r = np.random.default_rng(seed)
+    B, width = len(new), max(1, max(-(-n // page) for n in kv)) + 1
+    n_blocks = B * width + 2
+    table = r.permutation(n_blocks)[:B * width].reshape(B, width).astype(np.int32)
+    cache = r.integers(0, 256, (n_blocks, Hkv, page // 16, 16 * (D + 8)), dtype=np.uint8)
+    s = r.uniform(0.15, 0.3, (n_blocks, Hkv, page // 16, 16, 2))
+    z = -7.5 * s + (0.0 if centred else 0.2) * r.normal(size=s.shape)
+    cache[..., 16 * D:] = _bytes(np.stack([s, z], -1).reshape(*s.shape[:-1], 4)).reshape(*cache.shape[:3], 128)
+    q = torch.tensor(r.normal(size=(sum(new), Hq, D)), dtype=torch.bfloat16)
+    return r, q, cache.reshape(n_blocks, Hkv, -1), table, np.cumsum([0] + list(new)).tolist()
+
+
+def _bytes(numbers):
+    """Numbers as bf16 (cut off), byte by byte along a last axis that is twice as long."""
+    with np.errstate(over="ignore"):
+        bits = (np.ascontiguousarray(numbers, dtype=np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    return np.ascontiguousarray(bits).view(np.uint8)
+
+
+def _set(cache, page, D, table, u, key=None, value=None):
+    """Scale and offset of a request's token u, of all heads."""
+    run = cache[table[u // page]].reshape(cache.shape[1], page // 16, 16 * (D + 8))[:, u % page // 16]
+    at = 16 * D + 8 * (u % 16)
+    if key is not None:
+        run[:, at:at + 4] = _bytes(np.array(key))
+    if value is not None:
+        run[:, at + 4:at + 8] = _bytes(np.array(value))
+
+
+def _attend(q, cache, table, kv, cu, max_new, mask="causal", **kw):
+    return dsp.dsp_attn_kv4(q.to(DEV), torch.tensor(cache, device=DEV), i32(table), i32(kv), i32(cu), max_new, mask=mask, **kw)
+
+
+# ------------------------------------------------------------------------------------ weights
+@gpu
+@pytest.mark.parametrize("new,D", [(1, 128), (12, 64), (30, 128), (40, 128), (70, 64), (150, 128)])
+@pytest.mark.parametrize("above", [18, 20, 22, 25])
+@pytest.mark.parametrize("place", [0, 5000])
+def test_small_weights_beside_a_dominant_token_count(new, D, above, place):
+    """One token's weight is 2^above of the others' and its value 0: the output is what the others leave."""
+    page, kv = 64, 8192
+    r, q, cache, table, cu = _case(above, [new], [kv], 1, 1, D, page, centred=True)
+    q = (0.5 + 0.5 * q.float()).to(torch.bfloat16)
+    _set(cache, page, D, table[0], place, key=[0.0, above * np.log(2.0) / (0.5 * D * D ** -0.5)], value=[0.0, 0.0])
+    want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, D ** -0.5, "causal")
+    assert _off(_attend(q, cache, table, [kv], cu, new), want) <= _allowed(new)
