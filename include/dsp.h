@@ -854,8 +854,10 @@ int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int
  * Request b's tokens are those of block_table[b] up to kv_len[b], its new ones the
  * last cu_new[b+1] - cu_new[b] of them (dsp_kv4_append has stored them); what of
  * them a query sees goes by `mask_kind`.  A query that sees nothing, or whose
- * scores are all -inf, gets 0.  Tokens that are not seen are not multiplied by
- * anything: whatever their bytes hold, NaN included, changes nothing.
+ * scores are all -inf, gets 0.  Tokens that are not seen have no part in an output,
+ * whatever their bytes hold, NaN included.  (Above 32 query rows a key head a finite
+ * value outside 2^-10 .. 2^9 makes the values of its run of 16 tokens bf16 operands
+ * instead of fp16, which shows in the last bits of rows that see others of the run.)
  *
  * q bf16 [T,Hq,D] (strides in elements, rows 16-byte aligned); out bf16 [T,Hq,D]
  * contiguous; rows from cu_new[B] on are not written.  block_table int32 [B,

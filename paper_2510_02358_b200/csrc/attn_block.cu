@@ -350,8 +350,9 @@ template <int D> struct Fill {
         vp[1] = __ldg(reinterpret_cast<const uint4 *>(par) + (lane & 3) + 4);
     }
     // Keys into the tile at shared address `tile`, what is known of its tokens into `info`; `left`: tokens of the request from the
-    // run's first on.
-    __device__ __forceinline__ void put_keys(uint32_t tile, Info *info, int warp, int left, int lane) const {
+    // run's first on.  Returns what put_values needs to know: a bit for each token that holds NaN, and kWideRun.
+    static constexpr uint32_t kWideRun = 0x10000u;
+    __device__ __forceinline__ uint32_t put_keys(uint32_t tile, Info *info, int warp, int left, int lane) const {
         const int r = lane >> 2, c = lane & 3, t0 = warp * 16;
         uint32_t mark = 0u, scaled = 0u;
         bool fits = true;
@@ -398,8 +399,12 @@ template <int D> struct Fill {
             info->wide_runs[warp] = fits ? 0 : 1;
             info->odd[warp] = mark != 0xFFFFu || scaled != 0u || !fits ? 1 : 0;
         }
+        return mark >> 16 | (fits ? 0u : kWideRun);
     }
-    __device__ __forceinline__ void put_values(uint32_t tile, int t0, int left, bool wide, int lane) const {
+    // `odd`: as put_keys returned it.  Whoever sees a token of NaN gets NaN by its score, so its value is left out whole: a finite one
+    // beside a key of NaN was not looked at for whether fp16 holds it.
+    __device__ __forceinline__ void put_values(uint32_t tile, int t0, int left, uint32_t odd, int lane) const {
+        const bool wide = (odd & kWideRun) != 0u;
         const int r = lane >> 2, c = lane & 3;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
@@ -407,7 +412,7 @@ template <int D> struct Fill {
             for (int e = 0; e < 2; ++e) {
                 const int t = 2 * c + e + 8 * hi;
                 const uint32_t par = e ? vp[hi].w : vp[hi].y;
-                const bool use = ok_v && t < left && !not_finite(par);
+                const bool use = ok_v && t < left && !((odd >> t) & 1u);
                 const float s = use ? bf16_lo(par) * kValueMul : 0.0f, z = use ? bf16_hi(par) * kValueMul : 0.0f;
                 uint32_t w0, w1 = 0u;
                 if (D == 128) {
@@ -464,11 +469,12 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             run = head + id * (head_bytes * a.Hkv) + (long long)sub * Kv4<D>::kRunBytes;
         };
         const int t0 = warp * 16;
+        uint32_t odd_next = 0u;                                    // of the run whose keys were put last
         // keys of tile m, the segment's step s; false: the wait ran out
         auto keys = [&](uint32_t m, int s) {
             const uint32_t st = m & 1u;
             if (!warp_wait(key_empty + 8 * st, ((m >> 1) & 1u) ^ 1u, dead)) return false;
-            f.put_keys(k_at + st * kTileBytes, info + (m & 3), warp, kv - s * kTile - t0, lane);
+            odd_next = f.put_keys(k_at + st * kTileBytes, info + (m & 3), warp, kv - s * kTile - t0, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(key_full + 8 * st);
@@ -489,6 +495,7 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
         for (; step < step1; ++step, ++n) {
             const uint8_t *val_run = run;
             const bool val_there = there;
+            const uint32_t odd = odd_next;
             if (step + 1 < step1) {
                 if (!keys(n + 1, step + 1)) return;
                 locate();
@@ -497,7 +504,7 @@ __device__ __forceinline__ void fill_role(const AttnArgs &a, const LineStart &li
             }
             const uint32_t st = n & 1u;
             if (!warp_wait(val_empty + 8 * st, ((n >> 1) & 1u) ^ 1u, dead)) return;
-            f.put_values(v_at + st * kTileBytes, t0, kv - step * kTile - t0, info[n & 3].wide_runs[warp] != 0, lane);
+            f.put_values(v_at + st * kTileBytes, t0, kv - step * kTile - t0, odd, lane);
             fence_smem();
             __syncwarp();
             if (lane == 0) bar_arrive(val_full + 8 * st);

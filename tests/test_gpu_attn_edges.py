@@ -76,3 +76,33 @@ def test_small_weights_beside_a_dominant_token_count(new, D, above, place):
     _set(cache, page, D, table[0], place, key=[0.0, above * np.log(2.0) / (0.5 * D * D ** -0.5)], value=[0.0, 0.0])
     want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, D ** -0.5, "causal")
     assert _off(_attend(q, cache, table, [kv], cu, new), want) <= _allowed(new)
+
+
+# ------------------------------------------------------------------------------- hidden tokens
+NAN = float("nan")
+HIDDEN = [([NAN, NAN], [2000.0, 3000.0]), ([NAN, 0.0], [1e4, -3e4]), ([0.2, -1.5], [NAN, 0.0]), ([NAN, NAN], [2.0 ** 40, 1.0]), ([NAN, 0.1], [1e-30, 1e-30])]
+
+
+@gpu
+@pytest.mark.parametrize("new,Hq,Hkv,D", [(2, 4, 1, 128), (20, 1, 1, 64), (40, 2, 2, 128), (200, 4, 2, 64)])
+@pytest.mark.parametrize("key,value", HIDDEN)
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_hidden_token_changes_nothing_whatever_it_holds(new, Hq, Hkv, D, key, value, tree):
+    """New token 1 is seen by later rows only (causal), or by none but row 1 (tree): the others have their usual bits."""
+    page, kv = 32, 170 + new
+    r, q, cache, table, cu = _case(3, [new], [kv], Hq, Hkv, D, page)
+    mask = "causal"
+    if tree:
+        bits = np.zeros((new, new), dtype=bool)
+        bits[np.arange(new), np.arange(new)] = True
+        bits[:, 0] = True
+        words = -(-new // 32)
+        packed = np.packbits(np.pad(bits, ((0, 0), (0, 32 * words - new))), axis=1, bitorder="little").view(np.uint32)
+        mask = torch.tensor(packed.view(np.int32).copy(), device=DEV)
+    before = _attend(q, cache, table, [kv], cu, new, mask)
+    assert torch.isfinite(before).all()
+    _set(cache, page, D, table[0], kv - new + 1, key=key, value=value)
+    after = _attend(q, cache, table, [kv], cu, new, mask)
+    blind = [i for i in range(new) if i != 1] if tree else [0]
+    assert torch.equal(before[blind], after[blind])
+    assert after[1].isnan().all()
