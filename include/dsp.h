@@ -865,7 +865,8 @@ int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int
  * new tokens (more are not answered).  mask_bits uint32 [T, mask_words] for
  * DSP_MASK_BITS, else null; new tokens from 32 * mask_words on are not seen.
  * A block number outside 0..n_blocks-1 hides its tokens.  Lengths outside what the
- * table holds are clipped.  Scores, sums and outputs are accumulated in fp32.
+ * table holds are clipped.  Scores, sums and outputs are accumulated in fp32, which
+ * holds weighted sums of values up to 2^80 for any number of tokens.
  * workspace: dsp_attn_kv4_workspace_bytes(...), 256-byte aligned; garbage before
  * and after.
  * Errors : INVALID_ARG (null pointer, negative sizes, Hq not a multiple of Hkv,

@@ -21,7 +21,8 @@
 // it was 0.0035).  What fp16's range does not hold is brought into it by powers of two: a row of queries
 // by its largest number, taken back with the softmax scale; a key whose largest number lies outside
 // 2^-4 .. 2^15 by that, its scores being multiplied back (k_mul).  Values are multiplied by 64, and the 16
-// tokens of a run that holds one outside 2^-10 .. 2^9 go through bf16 operands instead (wide_runs).
+// tokens of a run that holds one outside 2^-10 .. 2^9 go through bf16 operands instead (wide_runs), with the
+// 64 in their weights.
 //
 // The running maximum moves only when a row's scores pass it by 2^8, and only then is the output in
 // tensor memory rescaled (by the softmax warps, between two products of their slot).
@@ -303,6 +304,15 @@ __device__ __forceinline__ uint4 values_bf16(uint32_t w, const Affine &a) {
     }
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
+// Four pairs of bf16 numbers without infinities: the sum of a scale and an offset near the range's end may pass it, and rows that do
+// not see the token multiply it by 0.
+__device__ __forceinline__ uint4 finite_bf16(uint4 v) {
+    uint32_t *p = &v.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm("min.bf16x2 %0, %0, %1;\n max.bf16x2 %0, %0, %2;" : "+r"(p[i]) : "r"(0x7F7F7F7Fu), "r"(0xFF7FFF7Fu));
+    return v;
+}
 __device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -313,7 +323,9 @@ __device__ __forceinline__ uint4 load16(uint32_t at) {
 }
 // The largest number that a head of scale and offset p (bf16 each) may hold, in magnitude.
 __device__ __forceinline__ float largest(uint32_t p) { return fmaxf(fabsf(bf16_hi(p)), fabsf(fmaf(15.0f, bf16_lo(p), bf16_hi(p)))); }
-constexpr float kValueMul = 64.0f;               // values are multiplied by it on the way in, outputs by its inverse on the way out
+// Values are multiplied by it on the way in (those of bf16 runs, which may lie near the range's end, through their weights), outputs by
+// its inverse on the way out.
+constexpr float kValueMul = 64.0f;
 __device__ __forceinline__ bool value_fits(uint32_t p) {
     const float top = largest(p);
     return top == 0.0f || (top >= 0.0009765625f && top < 512.0f);
@@ -413,7 +425,7 @@ template <int D> struct Fill {
                 const int t = 2 * c + e + 8 * hi;
                 const uint32_t par = e ? vp[hi].w : vp[hi].y;
                 const bool use = ok_v && t < left && !((odd >> t) & 1u);
-                const float s = use ? bf16_lo(par) * kValueMul : 0.0f, z = use ? bf16_hi(par) * kValueMul : 0.0f;
+                float s = use ? bf16_lo(par) : 0.0f, z = use ? bf16_hi(par) : 0.0f;
                 uint32_t w0, w1 = 0u;
                 if (D == 128) {
                     const uint4 u = v[D == 128 ? hi : 0];
@@ -425,13 +437,15 @@ template <int D> struct Fill {
                 const bool swap = D == 128 && (r & 1) != 0;          // as above: odd r the other way round
                 const int at = D == 128 ? 2 * r : r;
                 if (!wide) {
+                    s *= kValueMul;
+                    z *= kValueMul;
                     const Affine a = {twice_f16(s), twice_f16(s * 0.0625f), twice_f16(z)};
                     store16(tile + piece_at(t0 + t, at + (swap ? 1 : 0)), values_f16(swap ? w1 : w0, a));
                     if (D == 128) store16(tile + piece_at(t0 + t, at + (swap ? 0 : 1)), values_f16(swap ? w0 : w1, a));
                 } else {
                     const Affine a = {twice_bf16(s), 0u, twice_bf16(z)};
-                    store16(tile + piece_at(t0 + t, at + (swap ? 1 : 0)), values_bf16(swap ? w1 : w0, a));
-                    if (D == 128) store16(tile + piece_at(t0 + t, at + (swap ? 0 : 1)), values_bf16(swap ? w0 : w1, a));
+                    store16(tile + piece_at(t0 + t, at + (swap ? 1 : 0)), finite_bf16(values_bf16(swap ? w1 : w0, a)));
+                    if (D == 128) store16(tile + piece_at(t0 + t, at + (swap ? 0 : 1)), finite_bf16(values_bf16(swap ? w0 : w1, a)));
                 }
             }
     }
@@ -780,7 +794,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                 }
             }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-            if (odd) {                                             // weights of runs whose values are bf16: as bf16 too
+            if (odd) {                                             // weights of runs whose values are bf16: as bf16 too, with the values' factor
                 const uint32_t wide_runs = *reinterpret_cast<const uint32_t *>(&inf->wide_runs[4 * buf]);
                 if (wide_runs) tmem_stored();
 #pragma unroll 1
@@ -793,7 +807,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
                     for (int e = 0; e < 8; ++e) {
                         const uint32_t both = __float_as_uint(y[e]);
                         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&both));
-                        p[e & 3] = pack2(f.x, f.y);
+                        p[e & 3] = pack2(f.x * kValueMul, f.y * kValueMul);
                         if ((e & 3) == 3) tmem_store4(at + 8 * k + e - 3, p);
                     }
                 }

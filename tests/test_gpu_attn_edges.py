@@ -106,3 +106,18 @@ def test_a_hidden_token_changes_nothing_whatever_it_holds(new, Hq, Hkv, D, key, 
     blind = [i for i in range(new) if i != 1] if tree else [0]
     assert torch.equal(before[blind], after[blind])
     assert after[1].isnan().all()
+
+
+@gpu
+@pytest.mark.parametrize("new,Hq,Hkv,D", [(2, 4, 1, 128), (20, 1, 1, 64), (40, 2, 2, 128), (200, 4, 2, 64)])
+@pytest.mark.parametrize("key,value", [([0.2, -1.5], [2.0 ** 123, 2.0 ** 120]), ([0.2, -1.5], [3.3e38, 3.3e38]), ([0.2, -1.5], [-3.3e38, -3.3e38]),
+                                       ([3.3e38, 3.3e38], [0.2, -1.5]), ([2.0 ** 125, -2.0 ** 125], [2.0 ** 123, -2.0 ** 126])])
+def test_a_hidden_token_at_the_end_of_the_number_range_reaches_no_other_row(new, Hq, Hkv, D, key, value):
+    page, kv = 32, 170 + new
+    r, q, cache, table, cu = _case(4, [new], [kv], Hq, Hkv, D, page)
+    want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, D ** -0.5, "causal")
+    u = kv - new // 2                                                               # rows of the first half do not see it
+    _set(cache, page, D, table[0], u, key=key, value=value)
+    got = _attend(q, cache, table, [kv], cu, new)
+    rows = slice(0, new - new // 2)
+    assert _off(got[rows], want[rows]) <= _allowed(new * Hq // Hkv)
