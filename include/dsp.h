@@ -862,7 +862,8 @@ int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int
  * q bf16 [T,Hq,D] (strides in elements, rows 16-byte aligned); out bf16 [T,Hq,D]
  * contiguous; rows from cu_new[B] on are not written.  block_table int32 [B,
  * max_blocks]; kv_len int32 [B]; cu_new int32 [B+1]; max_new: no request has more
- * new tokens (more are not answered).  mask_bits uint32 [T, mask_words] for
+ * new tokens (of one that has, only the first max_new are answered, and of one that
+ * reaches beyond T only those before).  mask_bits uint32 [T, mask_words] for
  * DSP_MASK_BITS, else null; new tokens from 32 * mask_words on are not seen.
  * A block number outside 0..n_blocks-1 hides its tokens.  Lengths outside what the
  * table holds are clipped.  Scores, sums and outputs are accumulated in fp32, which

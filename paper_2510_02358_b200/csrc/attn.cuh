@@ -38,15 +38,15 @@ struct SplitUnit {
 
 // A request's place on that line.
 struct Request {
-    int b, n_new, kv, rows;                      // new tokens, tokens in all, query rows per key head
+    int b, n_new, kv, rows;                      // new tokens, tokens in all (may be fewer), query rows per key head
     int row0;                                    // first row of q
     int tiles, steps;                            // query tiles, steps of each unit
     __device__ __forceinline__ void load(const AttnArgs &a, int b_, int tile_rows, int step_tokens) {
         b = b_;
         row0 = max(a.cu[b], 0);
-        n_new = max(min(min(a.cu[b + 1], a.T) - row0, a.max_new), 0);
+        n_new = max(a.cu[b + 1] - row0, 0);
         kv = (int)max(0LL, min((long long)a.kv_len[b], min((long long)a.max_blocks * a.page, 0x7FFFFF00LL)));
-        rows = n_new * a.group;
+        rows = max(min(min(n_new, a.T - row0), a.max_new), 0) * a.group;      // of the tokens that the call answers
         tiles = (rows + tile_rows - 1) / tile_rows;
         steps = max(1, (kv + step_tokens - 1) / step_tokens);
     }

@@ -121,3 +121,25 @@ def test_a_hidden_token_at_the_end_of_the_number_range_reaches_no_other_row(new,
     got = _attend(q, cache, table, [kv], cu, new)
     rows = slice(0, new - new // 2)
     assert _off(got[rows], want[rows]) <= _allowed(new * Hq // Hkv)
+
+
+# ------------------------------------------------------------------------- more than is answered
+@gpu
+@pytest.mark.parametrize("mask", ["causal", "full", "tree"])
+@pytest.mark.parametrize("new,max_new,T,Hq,Hkv,D", [([5], 1, 5, 4, 1, 128), ([9, 20], 4, 29, 2, 2, 64), ([9, 20], 20, 16, 2, 1, 128), ([30, 90], 40, 120, 4, 4, 128),
+                                                    ([200], 200, 130, 4, 2, 64), ([70, 300], 100, 333, 8, 1, 128)])
+def test_requests_with_more_new_tokens_than_are_answered(new, max_new, T, Hq, Hkv, D, mask):
+    """The rows that are answered see what they see in a call that answers all; the others are left alone."""
+    page, kv = 16, [100 + 3 * n for n in new]
+    r, q, cache, table, cu = _case(6, new, kv, Hq, Hkv, D, page)
+    bits, words, m = None, 0, mask
+    if mask == "tree":
+        words = -(-max(new) // 32)
+        bits = [int.from_bytes(r.bytes(4 * words), "little") & ((1 << n) - 1) | 1 for n in new for _ in range(n)]
+        m = torch.tensor(np.array([[b >> 32 * w & 0xFFFFFFFF for w in range(words)] for b in bits[:T]], dtype=np.uint32).view(np.int32), device=DEV)
+    want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), kv, cu, D ** -0.5, bits if bits is not None else mask, words)
+    out = torch.full((T, Hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    _attend(q[:T], cache, table, kv, cu, max_new, m, out=out)
+    answered = np.concatenate([np.arange(n) < max_new for n in new])[:T]
+    assert _off(out[torch.tensor(answered, device=DEV)], want[:T][answered]) <= _allowed(max_new * Hq // Hkv)
+    assert (out[torch.tensor(~answered, device=DEV)] == 7.0).all()
