@@ -854,7 +854,8 @@ int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int
  * Request b's tokens are those of block_table[b] up to kv_len[b], its new ones the
  * last cu_new[b+1] - cu_new[b] of them (dsp_kv4_append has stored them); what of
  * them a query sees goes by `mask_kind`.  A query that sees nothing, or whose
- * scores are all -inf, gets 0.  Tokens that are not seen have no part in an output,
+ * scores are all -inf, gets 0; one that holds NaN or an infinity and sees something
+ * gets NaN (or 0, if its scores all come out as -inf).  Tokens that are not seen have no part in an output,
  * whatever their bytes hold, NaN included.  (Above 32 query rows a key head a finite
  * value outside 2^-10 .. 2^9 makes the values of its run of 16 tokens bf16 operands
  * instead of fp16, which shows in the last bits of rows that see others of the run.)
@@ -872,7 +873,7 @@ int32_t dsp_kv4_read(const void *cache, int32_t n_blocks, int32_t page_size, int
  * and after.
  * Errors : INVALID_ARG (null pointer, negative sizes, Hq not a multiple of Hkv,
  *          max_new < 1, max_blocks < 1, strides, page_size not a multiple of 16,
- *          alignment, scale not finite, mask), UNSUPPORTED (dtype not DSP_BF16,
+ *          alignment, scale * log2(e) not finite, mask), UNSUPPORTED (dtype not DSP_BF16,
  *          D not 64 / 128, B > 65535, more than 2^24 tokens or 4096 heads), WORKSPACE, CUDA.
  */
 int32_t dsp_attn_kv4_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_new,

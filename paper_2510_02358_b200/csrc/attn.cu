@@ -728,7 +728,7 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     if (rc != DSP_OK) return rc;
     if (dtype != DSP_BF16) return DSP_ERR_UNSUPPORTED;
     if (n_blocks < 1 || page_size < 16 || page_size % 16 != 0 || max_blocks < 1 || table_stride < max_blocks) return DSP_ERR_INVALID_ARG;
-    if (!isfinite(scale)) return DSP_ERR_INVALID_ARG;
+    if (!isfinite(scale * kLog2e)) return DSP_ERR_INVALID_ARG;
     if (mask_kind != DSP_MASK_CAUSAL && mask_kind != DSP_MASK_FULL && mask_kind != DSP_MASK_BITS) return DSP_ERR_INVALID_ARG;
     if (B == 0 || T == 0) return DSP_OK;
     if (!q || !cache || !block_table || !kv_len || !cu_new || !out || !workspace) return DSP_ERR_INVALID_ARG;

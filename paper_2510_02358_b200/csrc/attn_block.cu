@@ -668,7 +668,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
 #pragma unroll
             for (int i = 0; i < kRowLanes; ++i) {
                 const int rr = warp * 32 + i * kRowsTurn + lane / kRowLanes;
-                // the largest magnitude, as bits: infinities and NaN lie above all numbers
+                // the largest magnitude, as bits (infinities and NaN lie above all numbers, and stay what they are below)
                 uint32_t top = __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
 #pragma unroll
                 for (int o = 1; o < kRowLanes; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -681,7 +681,7 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[e] = pack2_f16(bf16_lo(v[e]) * up, bf16_hi(v[e]) * up);
                 store16(q_tile + piece_at(rr, piece), make_uint4(h[0], h[1], h[2], h[3]));
-                if (piece == 0) s_back[slot * kTile + rr] = top >= 0x7F80u ? CUDART_NAN_F : __uint_as_float((uint32_t)ex << 23);
+                if (piece == 0) s_back[slot * kTile + rr] = __uint_as_float((uint32_t)ex << 23);
             }
             fence_smem();
         }
@@ -689,7 +689,8 @@ __device__ __forceinline__ void softmax_role(const AttnArgs &a, const LineStart 
         if (lane == 0) bar_arrive(smem_u32(&bars->query_ready));
         // what a product with the row's queries is multiplied with; a unit of one tile has them from slot 0
         if (!wide) pair_barrier(1, kSoftWarps * 32);
-        const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f) * s_back[(wide ? slot * kTile : 0) + me];      // 0 as one that moves nothing
+        // (never 0, which would make NaN of the -infinity of what is not seen; the smallest normal number moves nothing)
+        const float scale = fmaxf(fabsf(a.scale_log2) * s_back[(wide ? slot * kTile : 0) + me], 1.17549435e-38f);
         const int past = w.rq.kv - w.rq.n_new;
         // rows beyond the unit's see everything: what they hold is not used, and their tiles need no masks
         const int lim = !live ? 0x7FFFFFFF : a.mask_kind == DSP_MASK_CAUSAL ? min(w.rq.kv, past + qi + 1) : w.rq.kv;

@@ -143,3 +143,39 @@ def test_requests_with_more_new_tokens_than_are_answered(new, max_new, T, Hq, Hk
     answered = np.concatenate([np.arange(n) < max_new for n in new])[:T]
     assert _off(out[torch.tensor(answered, device=DEV)], want[:T][answered]) <= _allowed(max_new * Hq // Hkv)
     assert (out[torch.tensor(~answered, device=DEV)] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------ queries and scale
+SHAPES = [(1, 4, 1, 128), (6, 2, 1, 64), (30, 1, 1, 128), (40, 2, 2, 128), (70, 4, 2, 64), (200, 4, 2, 64)]
+
+
+@gpu
+@pytest.mark.parametrize("new,Hq,Hkv,D", SHAPES)
+def test_queries_with_nan_or_infinity_keep_to_their_rows(new, Hq, Hkv, D):
+    """A row of NaN that sees something gets NaN, one that sees nothing 0, and the rows beside it what they always get."""
+    page, kv = 16, 150 + new
+    r, q, cache, table, cu = _case(8, [new], [kv], Hq, Hkv, D, page)
+    clean = _attend(q, cache, table, [kv], cu, new)
+    odd = [i for i in range(new) if i % 3 == 0]
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bad = q.clone()
+        bad[odd, :, 5] = value
+        got = _attend(bad, cache, table, [kv], cu, new)
+        assert torch.equal(got[[i for i in range(new) if i % 3]], clean[[i for i in range(new) if i % 3]])
+        assert got[odd].isnan().all()                                               # keys of both signs: never -inf alone
+        missing = np.full_like(table, -1)
+        assert not _attend(bad, cache, missing, [kv], cu, new).any()
+        none = torch.zeros((new, -(-new // 32)), dtype=torch.int32, device=DEV)
+        assert not _attend(bad, cache, table, [new], cu, new, none).any()
+
+
+@gpu
+@pytest.mark.parametrize("new,Hq,Hkv,D", SHAPES)
+@pytest.mark.parametrize("scale,size", [(0.0, 0.0), (0.0, 1.0), (0.0, 1e-25), (0.125, 0.0), (1e-30, 1e-25), (-0.1, 1.0), (1e-42, 0.0), (3e-4, 300.0)])
+def test_scales_and_queries_of_any_size(new, Hq, Hkv, D, scale, size):
+    page, kv = 16, 190 + new
+    r, q, cache, table, cu = _case(9, [new], [kv], Hq, Hkv, D, page)
+    q = (q.float() * size).to(torch.bfloat16)
+    table[0, 2] = -1                                                                # tokens that are not there among those that are
+    want = ref.attend(ref.to_numpy(q), cache, page, D, table.tolist(), [kv], cu, scale, "causal")
+    assert _off(_attend(q, cache, table, [kv], cu, new, scale=scale), want) <= _allowed(new * Hq // Hkv)
