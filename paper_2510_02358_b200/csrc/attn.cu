@@ -572,7 +572,8 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
 }
 
 // Joins the partial results of one unit that crossed the shares of several CTAs, in their order.  A long request alone may
-// leave one from every CTA: they are taken 16 or 32 at a time, all loads of a turn in flight together.
+// leave one from every CTA: they are taken 16 or 32 at a time, all loads of a turn in flight together.  (Ordinary loads: the parts are
+// written while this kernel's CTAs already wait, and a read-only load is for what nobody writes as long as its kernel runs.)
 constexpr int kJoinThreads = 256;
 template <int D, int NT>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs a) {
@@ -628,8 +629,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnArgs 
 #pragma unroll
             for (int w = 0; w < kJoinTurn; ++w) {
                 const float *p = base + (long long)((i0 + w) * 2 + (i0 + w == 0 ? 1 : 0)) * kPart + at;
-                vx[w] = i0 + w < n ? __ldg(p) : 0.0f;
-                vy[w] = i0 + w < n ? __ldg(p + 64) : 0.0f;
+                vx[w] = i0 + w < n ? p[0] : 0.0f;
+                vy[w] = i0 + w < n ? p[64] : 0.0f;
             }
             x[k] *= s_keep[row];
             y[k] *= s_keep[row];

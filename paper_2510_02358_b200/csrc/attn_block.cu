@@ -969,7 +969,8 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
     }
 }
 
-// Joins the partial results of one unit: 16 rows per CTA of 256 threads, the parts of a turn loaded together.
+// Joins the partial results of one unit: 16 rows per CTA of 256 threads, the parts of a turn loaded together (by ordinary loads: they
+// are written while this kernel's CTAs already wait).
 constexpr int kJoinThreads = 256, kJoinTurn = 4, kJoinRows = 16;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const AttnArgs a) {
@@ -1006,9 +1007,9 @@ __global__ void __launch_bounds__(kJoinThreads) attn_block_join_kernel(const Att
             for (int w = 0; w < kJoinTurn; ++w) {
                 const bool ok = i0 + w < n && row < rows;
                 const float *p = part_of(i0 + w);
-                my[w] = ok ? __ldg(p + 2 * kTile * D + row) : -CUDART_INF_F;
-                ly[w] = ok ? __ldg(p + 2 * kTile * D + 2 * kTile + row) : 0.0f;
-                y[w] = ok ? __ldg(reinterpret_cast<const float4 *>(p) + piece * (2 * kTile) + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                my[w] = ok ? p[2 * kTile * D + row] : -CUDART_INF_F;
+                ly[w] = ok ? p[2 * kTile * D + 2 * kTile + row] : 0.0f;
+                y[w] = ok ? reinterpret_cast<const float4 *>(p)[piece * (2 * kTile) + row] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
             float top = m[k];
 #pragma unroll
