@@ -3,6 +3,7 @@
 
 #include "attn.cuh"
 #include "attn_block.h"
+#include "copy_ring.h"
 
 namespace dsp {
 namespace {
@@ -169,8 +170,8 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_dyn) + warp * kRing;
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(&s_bars[warp][0]);
-    uint32_t phases = 0u;                                         // parity that each stage's barrier is waited for with
-    bool lost = false;
+    CopyRing<kStages> order;
+    bool lost = false;                                            // a copy has not come in time: the warp's rows get NaN, and nothing is fetched any more
     StreamRequest rq;
     long long before = s_line.before;
     rq.load(a, s_line.b, kRows, kStep);
@@ -243,7 +244,8 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
             }
             left -= kU;
         };
-        int ahead = run, stage = 0;                               // the first copies are under way while the queries come
+        int ahead = run;                                          // the first copies are under way while the queries come
+        order.restart();
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i, ahead += kW * kU)
             if (ahead < run_end && !lost) fetch(i);
@@ -308,20 +310,20 @@ __global__ void __launch_bounds__(kW * 32, kCtas) attn_stream_kernel(const AttnA
                 unset |= (row_first + t * 8 + 2 * c + e < rq.rows ? 1u : 0u) << (2 * t + e);
             }
         }
-        for (; run < run_end; run += kW * kU, ahead += kW * kU) {
-            // the stage's bytes are here (a wait that has run out loses the row's sums, below, and is not waited for again)
-            if (!lost) lost = !__all_sync(0xFFFFFFFFu, bytes_here(bars + 8 * stage, (phases >> stage) & 1u));
-            phases ^= 1u << stage;
-            __syncwarp();                                         // all lanes have read the stage before
-            if (ahead < run_end && !lost) fetch(stage == 0 ? kStages - 1 : stage - 1);
-            if (lost) {                                           // what is still under way has to land before the CTA may end
+        for (; run < run_end && !lost; run += kW * kU, ahead += kW * kU) {
+            // the stage's bytes are here; where a wait runs out, what is still under way has to land before its place is used otherwise
+            lost = !__all_sync(0xFFFFFFFFu, bytes_here(bars + 8 * order.stage, order.parity()));
+            if (lost) {
 #pragma unroll 1
-                for (int i = 0; i < kStages; ++i) bytes_here(bars + 8 * i, (phases >> i) & 1u);
+                for (int left = order.under_way(run, ahead, run_end, kW * kU); left > 0; --left, order.used())
+                    bytes_here(bars + 8 * order.stage, order.parity());
                 break;
             }
-            const uint32_t codes = ring + stage * kStage + lane * 16, params = ring + stage * kStage + Kv4<D>::kParamOff + r * 8;
-            const uint32_t here = there >> (stage * kU);
-            stage = stage == kStages - 1 ? 0 : stage + 1;
+            __syncwarp();                                         // all lanes have read the stage before
+            if (ahead < run_end) fetch(order.before());
+            const uint32_t codes = ring + order.stage * kStage + lane * 16, params = ring + order.stage * kStage + Kv4<D>::kParamOff + r * 8;
+            const uint32_t here = there >> (order.stage * kU);
+            order.used();
             // a run beyond the end or of no block leaves its operands at whatever the ring holds (codes are finite) and is not seen
             float s[kU][NT][4], va[kU][2], vz[kU][2];
 #pragma unroll
