@@ -256,6 +256,7 @@ struct Bars {
     uint64_t score_full[4], weight_ready[4];     // [slot * 2 + buffer]
     uint64_t out_free[2];                        // [slot] its last product with the weights has ended
     uint64_t query_ready, out_done;
+    uint64_t ended;                              // every product that was issued
 };
 struct __align__(16) Info {                      // beside a token tile, one bit per token
     uint32_t there[4], poison[4], scaled[4];     // 16 bits from each fill warp: there is such a token, it holds NaN, its k_mul is not 1
@@ -941,6 +942,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         }
         bar_init(smem_u32(&s_bars.query_ready), kSoftWarps);
         bar_init(smem_u32(&s_bars.out_done), kProductWarps);
+        bar_init(smem_u32(&s_bars.ended), kProductWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kSoftWarps + kFillWarps) {
@@ -961,9 +963,14 @@ __global__ void __launch_bounds__(kBlockThreads, 1) attn_block_kernel(const Attn
         }
     }
     __syncwarp();
+    // by the lane that issued them: where a wait ran out, products may still be under way, which read this CTA's memory
+    if (warp >= kSoftWarps + kFillWarps) commit_to(smem_u32(&s_bars.ended), elected());
     fence_before();
     __syncthreads();
     if (warp == kSoftWarps + kFillWarps) {
+        const long long t0 = clock64();
+        while (!bar_test(smem_u32(&s_bars.ended), 0u) && clock64() - t0 < kWaitClocks) {}
+        __syncwarp();
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
     }

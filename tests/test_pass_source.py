@@ -91,3 +91,13 @@ def test_the_ring_of_copies_waits_for_what_is_under_way_and_for_nothing_else(tmp
     assert subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.strip() == "0"
     text = open(os.path.join(CSRC, "attn.cu")).read()              # the kernel goes by this bookkeeping and has none of its own
     assert "CopyRing<kStages> order" in text and "phases" not in text
+
+
+def test_tensor_memory_is_given_back_after_the_last_product():
+    """Also where a wait ran out: the products commit to a barrier of their own, which is waited for (with a limit) before the CTA ends."""
+    text = open(os.path.join(CSRC, "attn_block.cu")).read()
+    end = text[text.index("attn_block_kernel(const AttnArgs a) {"):]
+    end = end[end.index("product_role<D>("):end.index("tcgen05.dealloc")]
+    assert re.search(r"commit_to\(smem_u32\(&s_bars\.ended\), elected\(\)\);.*__syncthreads\(\);.*while \(!bar_test\(smem_u32\(&s_bars\.ended\), 0u\) && clock64\(\) - t0 < kWaitClocks\)",
+                     end, flags=re.S)
+    assert "bar_init(smem_u32(&s_bars.ended), kProductWarps)" in text
