@@ -9,8 +9,9 @@ CUDA library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import inspect
 import os
-from functools import lru_cache
+from functools import lru_cache, wraps
 from types import SimpleNamespace
 from typing import Optional
 
@@ -116,6 +117,21 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def _on_stream(call):
+    """A call with ``stream=s`` is one made under ``torch.cuda.stream(s)``: outputs and workspaces that it allocates belong to that
+    stream too.  Memory of the current stream could be another call's as soon as this one returns, while ``s`` still works on it."""
+    at = list(inspect.signature(call).parameters).index("stream")
+
+    @wraps(call)
+    def placed(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return placed
+
+
 def _logits3(t: torch.Tensor, name: str):
     if t.dim() != 3 or not t.is_cuda or t.stride(2) != 1:
         raise ValueError("%s must be a CUDA tensor [B, L, V] with a contiguous vocabulary dimension" % name)
@@ -172,6 +188,7 @@ def lattice_outputs(B: int, L: int, K_max: int, eos_id: int, device) -> SimpleNa
         gen_len=e((B,), torch.int32), row_status=e((B,), torch.int32))
 
 
+@_on_stream
 def dsp_lattice_build(draft: torch.Tensor, K_max: int, tau: float = 0.0, eos_id: int = -1,
                       out: Optional[SimpleNamespace] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> SimpleNamespace:
@@ -189,6 +206,7 @@ def dsp_lattice_build(draft: torch.Tensor, K_max: int, tau: float = 0.0, eos_id:
     return out
 
 
+@_on_stream
 def dsp_lattice_build_static(draft: torch.Tensor, K_max: int, tau: float = 0.0, eos_id: int = -1,
                              out: Optional[SimpleNamespace] = None, stream=None) -> SimpleNamespace:
     """``dsp_lattice_build`` with the scratch held inside the library: for callers that cannot
@@ -216,6 +234,7 @@ def cps_outputs(B: int, L: int, W: int, device, beams: bool = True) -> SimpleNam
         beam_cum=e((B, W), torch.float32) if beams else None)
 
 
+@_on_stream
 def dsp_cps_search(lat: SimpleNamespace, prev_token: torch.Tensor, table: torch.Tensor, *, W: int,
                    lam: float, eos_id: int = -1, proxy_kind: int = 0, table_log2: int = 0,
                    hash_seed: int = 0, V: int = 1, out: Optional[SimpleNamespace] = None,
@@ -233,6 +252,7 @@ def dsp_cps_search(lat: SimpleNamespace, prev_token: torch.Tensor, table: torch.
     return out
 
 
+@_on_stream
 def dsp_cps_search_biased(lat: SimpleNamespace, prev_token: torch.Tensor, table: torch.Tensor, *, W: int,
                           lam: float, ver_score: Optional[torch.Tensor], mu: float, eos_id: int = -1,
                           proxy_kind: int = 0, table_log2: int = 0, hash_seed: int = 0, V: int = 1,
@@ -261,6 +281,7 @@ def verify_outputs(B: int, L: int, Lt: int, device) -> SimpleNamespace:
         tgt_lse=e((B, Lt), torch.float32))
 
 
+@_on_stream
 def dsp_verify(target: torch.Tensor, draft: Optional[torch.Tensor], cps: SimpleNamespace,
                lat: Optional[SimpleNamespace], *, mode: Optional[torch.Tensor] = None,
                u: Optional[torch.Tensor] = None, eos_id: int = -1, all_greedy: bool = False,
@@ -323,6 +344,7 @@ def _step_call(draft, target, prev_token, table, K_max, W, lam, tau, eos_id, pro
     return args, lat, cps, ver, keep
 
 
+@_on_stream
 def dsp_draft_verify_step(draft: torch.Tensor, target: torch.Tensor, prev_token: torch.Tensor,
                           table: torch.Tensor, *, K_max: int, W: int, lam: float, tau: float = 0.0,
                           eos_id: int = -1, proxy_kind: int = 0, table_log2: int = 0, hash_seed: int = 0,
@@ -387,6 +409,7 @@ def dsp_shard_workspace_bytes(B: int, L: int, Vs: int, dtype: int, K_max: int) -
     return n.value
 
 
+@_on_stream
 def dsp_lattice_shard(logits: torch.Tensor, vocab_offset: int, K_max: int, eos_id: int = -1, *,
                       out: Optional[SimpleNamespace] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> SimpleNamespace:
@@ -408,6 +431,7 @@ def dsp_lattice_shard(logits: torch.Tensor, vocab_offset: int, K_max: int, eos_i
     return out
 
 
+@_on_stream
 def dsp_lattice_merge(sums: torch.Tensor, keys: torch.Tensor, status: torch.Tensor, V: int, K_max: int,
                       tau: float = 0.0, eos_id: int = -1, *, out: Optional[SimpleNamespace] = None,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
@@ -433,6 +457,7 @@ def dsp_lattice_merge(sums: torch.Tensor, keys: torch.Tensor, status: torch.Tens
     return out
 
 
+@_on_stream
 def dsp_target_shard(logits: torch.Tensor, vocab_offset: int, cps: SimpleNamespace, *,
                      out: Optional[SimpleNamespace] = None, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> SimpleNamespace:
@@ -454,6 +479,7 @@ def dsp_target_shard(logits: torch.Tensor, vocab_offset: int, cps: SimpleNamespa
     return out
 
 
+@_on_stream
 def dsp_verify_merge(sums: torch.Tensor, keys: torch.Tensor, status: torch.Tensor, cps: SimpleNamespace,
                      lat: Optional[SimpleNamespace], *, mode: Optional[torch.Tensor] = None,
                      u: Optional[torch.Tensor] = None, eos_id: int = -1, all_greedy: bool = False,
@@ -483,6 +509,7 @@ def dsp_verify_merge(sums: torch.Tensor, keys: torch.Tensor, status: torch.Tenso
     return out
 
 
+@_on_stream
 def dsp_residual_sample(target_rows: torch.Tensor, draft_rows: torch.Tensor, ver: SimpleNamespace,
                         lat: SimpleNamespace, u: torch.Tensor, L: int, *,
                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
@@ -504,6 +531,7 @@ def dsp_residual_sample(target_rows: torch.Tensor, draft_rows: torch.Tensor, ver
         _ptr(workspace), C.c_size_t(workspace.numel()), _stream(stream)))
 
 
+@_on_stream
 def dsp_beam_tree(cps: SimpleNamespace, stream=None) -> SimpleNamespace:
     """Token tree of the beams in ``cps`` (beam_ids [B,W,L], path_len [B])."""
     B, W, L = cps.beam_ids.shape
@@ -517,6 +545,7 @@ def dsp_beam_tree(cps: SimpleNamespace, stream=None) -> SimpleNamespace:
     return out
 
 
+@_on_stream
 def dsp_verify_tree(target: torch.Tensor, tree: SimpleNamespace, L: int, *,
                     workspace: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
     """Greedy verification of the token tree; ``target`` is [B, 1 + N, V]."""
@@ -541,6 +570,7 @@ def dsp_verify_tree(target: torch.Tensor, tree: SimpleNamespace, L: int, *,
     return out
 
 
+@_on_stream
 def dsp_verify_tree_stochastic(target: torch.Tensor, draft: torch.Tensor, tree: SimpleNamespace, u: torch.Tensor, *,
                                workspace: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
     """Stochastic verification of the token tree; ``target`` [B, 1 + N, V], ``draft`` [B, L, V], ``u`` fp32 [B, N + 1]."""
@@ -588,6 +618,7 @@ def dsp_unmask_workspace_bytes(B: int, L: int, V: int, dtype: int) -> int:
     return n.value
 
 
+@_on_stream
 def dsp_unmask_step(logits: torch.Tensor, tokens: torch.Tensor, masked: torch.Tensor, n_update: int, *,
                     out: Optional[SimpleNamespace] = None, workspace: Optional[torch.Tensor] = None,
                     stream=None) -> SimpleNamespace:
@@ -693,6 +724,7 @@ def _table(t: torch.Tensor, B: int, dev):
     return t.data_ptr(), (t.stride(0) if B > 1 else width), width
 
 
+@_on_stream
 def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: torch.Tensor, ring_pos: torch.Tensor,
                    block_table: torch.Tensor, free_ring: torch.Tensor, page_size: int, T: int, *,
                    node_parent: Optional[torch.Tensor] = None, node_depth: Optional[torch.Tensor] = None,
@@ -764,6 +796,7 @@ def _rope(q_weight, k_weight, positions, cos_sin, T: int, D: int, dtype, dev):
     return _at(q_weight), _at(k_weight), positions.data_ptr(), cos_sin.data_ptr(), rows, rot
 
 
+@_on_stream
 def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[torch.Tensor] = None,
                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                      positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
@@ -796,6 +829,7 @@ def _cache(cache: torch.Tensor, Hkv: int, D: int, dev):
     raise ValueError("cache must be a contiguous uint8 [n_blocks, Hkv, page_size * (D + 8)] tensor on the inputs' device")
 
 
+@_on_stream
 def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, cache: torch.Tensor, *,
                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                    positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
@@ -822,6 +856,7 @@ def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
     return out
 
 
+@_on_stream
 def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bfloat16, *, out=None, stream=None):
     """The keys and values, [T, Hkv, D] each, that ``cache`` holds for the tokens in ``slot``."""
     T, Hkv, dev = slot.shape[0], cache.shape[1], cache.device
@@ -847,6 +882,7 @@ def dsp_attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_
     return n.value
 
 
+@_on_stream
 def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
                  cu_new: torch.Tensor, max_new: int, *, scale: Optional[float] = None, mask="causal",
                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
