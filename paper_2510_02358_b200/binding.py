@@ -704,11 +704,12 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _queue(stream, dev: torch.device) -> int:
-    """Raw handle of the stream that a call goes to: torch's current one on the tensors' device."""
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+def _queue(dev: torch.device) -> int:
+    """Raw handle of torch's current stream on the tensors' device, which has to be the current one: kernels are launched there."""
+    index = dev.index                                              # None in host memory
+    if index is None or index != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on %s, which is not the current CUDA device" % dev)
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _ints(name: str, t: torch.Tensor, shape, dtype, dev) -> torch.Tensor:
@@ -763,7 +764,7 @@ def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: to
         table, stride, free_ring.data_ptr(), _at(node_parent), _at(node_depth), N,
         out.block_count.data_ptr(), out.ring_pos.data_ptr(), out.cu_new.data_ptr(), out.kv_len.data_ptr(),
         out.slot.data_ptr(), out.position.data_ptr(), _at(out.token_row), _at(out.mask), mask_words if N else 0,
-        out.row_status.data_ptr(), _queue(stream, dev)))
+        out.row_status.data_ptr(), _queue(dev)))
     return out
 
 
@@ -812,7 +813,7 @@ def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[tor
         q_out, k_out = _ints("out[0]", out[0], (T, Hq, D), dt, dev), _ints("out[1]", out[1], (T, Hkv, D), dt, dev)
     _check("dsp_qk_norm_rope", lib().dsp_qk_norm_rope(
         q.data_ptr(), k.data_ptr(), _dtype(q), T, Hq, Hkv, D, qt, qh, kt, kh, wq, wk, eps, pos, cs, rows, rot,
-        interleaved, q_out.data_ptr(), k_out.data_ptr(), _queue(stream, dev)))
+        interleaved, q_out.data_ptr(), k_out.data_ptr(), _queue(dev)))
     return q_out, k_out
 
 
@@ -824,9 +825,9 @@ def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device) -> torch.
 def _cache(cache: torch.Tensor, Hkv: int, D: int, dev):
     if cache.dim() == 3:
         n_blocks, H, size = cache.shape
-        if H == Hkv and size % (D + 8) == 0 and cache.dtype == torch.uint8 and cache.device == dev and cache.is_contiguous():
+        if H == Hkv and size % (D + 8) == 0 and cache.dtype == torch.uint8 and cache.device == dev and cache.is_cuda and cache.is_contiguous():
             return n_blocks, size // (D + 8)
-    raise ValueError("cache must be a contiguous uint8 [n_blocks, Hkv, page_size * (D + 8)] tensor on the inputs' device")
+    raise ValueError("cache must be a contiguous uint8 CUDA tensor [n_blocks, Hkv, page_size * (D + 8)] on the inputs' device")
 
 
 @_on_stream
@@ -852,7 +853,7 @@ def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
         _ints("out", out, (T, Hq, D), dt, dev)
     _check("dsp_kv4_append", lib().dsp_kv4_append(
         _at(q), k.data_ptr(), v.data_ptr(), _dtype(k), T, Hq, Hkv, D, qt, qh, kt, kh, vt, vh, wq, wk, eps, pos, cs, rows, rot,
-        interleaved, slot.data_ptr(), cache.data_ptr(), n_blocks, page, _at(out), _queue(stream, dev)))
+        interleaved, slot.data_ptr(), cache.data_ptr(), n_blocks, page, _at(out), _queue(dev)))
     return out
 
 
@@ -867,7 +868,7 @@ def dsp_kv4_read(cache: torch.Tensor, slot: torch.Tensor, D: int, dtype=torch.bf
     else:
         k, v = (_ints("out", t, (T, Hkv, D), dtype, dev) for t in out)
     _check("dsp_kv4_read", lib().dsp_kv4_read(cache.data_ptr(), n_blocks, page, Hkv, D, slot.data_ptr(), T, _dtype(k),
-                                              k.data_ptr(), v.data_ptr(), _queue(stream, dev)))
+                                              k.data_ptr(), v.data_ptr(), _queue(dev)))
     return k, v
 
 
@@ -907,10 +908,11 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
         out = torch.empty(T, Hq, D, dtype=dt, device=dev)
     else:
         _ints("out", out, (T, Hq, D), dt, dev)
+    queue = _queue(dev)                                            # before the workspace, whose size goes by the current device
     if workspace is None:
         workspace = torch.empty(_attn_workspace(B, T, Hq, Hkv, D, max_new, dev.index), dtype=torch.uint8, device=dev)
     _check("dsp_attn_kv4", lib().dsp_attn_kv4(
         q.data_ptr(), _dtype(q), B, T, Hq, Hkv, D, qt, qh, cache.data_ptr(), n_blocks, page, table, stride, width,
         kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,
-        out.data_ptr(), workspace.data_ptr(), workspace.numel(), _queue(stream, dev)))
+        out.data_ptr(), workspace.data_ptr(), workspace.numel(), queue))
     return out

@@ -91,3 +91,35 @@ def test_step_calls_on_another_stream_own_their_memory():
     for name in ("cand_id", "cand_logit", "lse64"):
         assert torch.equal(getattr(got, name), getattr(want, name))
     assert np.isfinite(got.lse64.cpu().numpy()).all()
+
+
+# ---------------------------------------------------------------------------------------- devices
+def test_the_tensors_device_has_to_be_the_current_one(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i)
+    assert dsp._queue(torch.device("cuda", 0)) == 100
+    for dev in (torch.device("cuda", 1), torch.device("cpu")):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            dsp._queue(dev)
+
+
+def test_read_refuses_a_cache_in_host_memory(monkeypatch):
+    """On whatever stream: the address would go to the kernel."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(dsp, "lib", lambda: pytest.fail("called"))
+    cache, slot = dsp.kv4_cache(2, 2, 64, 16, "cpu"), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError):
+        dsp.dsp_kv4_read(cache, slot, 64)
+
+
+@pytest.mark.gpu
+def test_calls_refuse_tensors_of_another_device(monkeypatch):
+    args = _attention(1)
+    q, cache = args[0], args[1]
+    plan = [torch.zeros(3, dtype=torch.int32, device=DEV) for _ in range(3)] + [torch.tensor([0, 8], device=DEV), args[2], torch.arange(8, dtype=torch.int32, device=DEV)]
+    slot = torch.zeros(3, dtype=torch.int64, device=DEV)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in (lambda: dsp.dsp_attn_kv4(*args), lambda: dsp.dsp_qk_norm_rope(q, q[:, :2]), lambda: dsp.dsp_kv4_read(cache, slot, 128),
+                 lambda: dsp.dsp_kv4_append(None, q[:, :2], q[:, :2], slot, cache), lambda: dsp.dsp_cache_plan(*plan, 32, 3)):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
