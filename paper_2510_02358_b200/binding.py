@@ -759,6 +759,16 @@ def dsp_cache_plan(seq_len: torch.Tensor, new_len: torch.Tensor, block_count: to
         out = SimpleNamespace(block_count=count, kv_len=kv, row_status=status, cu_new=cu,
                               ring_pos=e(2, dtype=i64, device=dev), slot=e(T, dtype=i64, device=dev),
                               position=position, token_row=row, mask=e(T, mask_words, dtype=i32, device=dev) if N else None)
+    else:
+        for name, n, dt in (("block_count", B, i32), ("kv_len", B, i32), ("row_status", B, i32), ("cu_new", B + 1, i32), ("ring_pos", 2, i64),
+                            ("slot", T, i64), ("position", T, i32)):
+            _ints("out." + name, getattr(out, name), (n,), dt, dev)
+        if out.token_row is not None:
+            _ints("out.token_row", out.token_row, (T,), i32, dev)
+        if N:
+            if out.mask is None:
+                raise ValueError("out.mask is needed with a tree")
+            _ints("out.mask", out.mask, (T, mask_words), i32, dev)
     _check("dsp_cache_plan", lib().dsp_cache_plan(
         seq_len.data_ptr(), new_len.data_ptr(), block_count.data_ptr(), ring_pos.data_ptr(), B, T, page_size, n_blocks, width,
         table, stride, free_ring.data_ptr(), _at(node_parent), _at(node_depth), N,
@@ -911,8 +921,10 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
     queue = _queue(dev)                                            # before the workspace, whose size goes by the current device
     if workspace is None:
         workspace = torch.empty(_attn_workspace(B, T, Hq, Hkv, D, max_new, dev.index), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % dev)
     _check("dsp_attn_kv4", lib().dsp_attn_kv4(
         q.data_ptr(), _dtype(q), B, T, Hq, Hkv, D, qt, qh, cache.data_ptr(), n_blocks, page, table, stride, width,
         kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,
-        out.data_ptr(), workspace.data_ptr(), workspace.numel(), queue))
+        out.data_ptr(), workspace.data_ptr(), workspace.nbytes, queue))
     return out
