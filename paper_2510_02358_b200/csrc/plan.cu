@@ -241,7 +241,7 @@ extern "C" int32_t dsp_cache_plan(const int32_t *seq_len, const int32_t *new_len
     using namespace dsp;
     const bool tree = node_parent || node_depth;
     if (B < 0 || T < 0 || page_size < 1 || n_blocks < 1 || max_blocks < 1 || table_stride < max_blocks) return DSP_ERR_INVALID_ARG;
-    if (tree && (!node_parent || !node_depth || N < 1 || !mask || (long long)mask_words * 32 < (long long)N + 1))
+    if (tree && (!node_parent || !node_depth || N < 1 || (T > 0 && !mask) || (long long)mask_words * 32 < (long long)N + 1))
         return DSP_ERR_INVALID_ARG;
     if (B > DSP_MAX_PLAN_ROWS || (tree && N + 1 > DSP_MAX_L)) return DSP_ERR_UNSUPPORTED;
     if (B == 0 && T == 0) return DSP_OK;
