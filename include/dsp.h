@@ -828,7 +828,8 @@ int32_t dsp_qk_norm_rope(const void *q, const void *k, int32_t dtype, int32_t T,
  * dsp_kv4_append: q, k, v as in dsp_qk_norm_rope (v is neither normed nor rotated);
  * q_out like there; token t's key and value enter slot[t] (int64; block * page_size
  * + place).  A slot outside 0 .. n_blocks * page_size - 1 or a negative position
- * stores nothing.  Of two tokens with the same slot, either may win.  (After a tree
+ * stores nothing.  No two tokens of a call may have the same slot: the place would
+ * hold codes of one beside the scale or codes of the other.  (After a tree
  * was verified, the accepted nodes' rows are appended again at the slots of their
  * final places, with slot -1 for the others.)  q and q_out null: keys and values only.
  * dsp_kv4_read: the values that the cache holds for the tokens in slot [T], in

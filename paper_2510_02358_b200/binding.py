@@ -845,7 +845,8 @@ def dsp_kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                    positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
                    interleaved: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
-    """Norm and rotation like dsp_qk_norm_rope; keys and values enter ``cache`` at ``slot`` (int64 [T]); returns q_out."""
+    """Norm and rotation like dsp_qk_norm_rope; keys and values enter ``cache`` at ``slot`` (int64 [T], no
+    slot twice; outside of the cache: not stored); returns q_out."""
     T, D, dt, dev = k.shape[0], k.shape[-1], k.dtype, k.device
     Hkv, kt, kh = _heads("k", k, T, D, dt, dev)
     Hv, vt, vh = _heads("v", v, T, D, dt, dev)
