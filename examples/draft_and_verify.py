@@ -1,6 +1,7 @@
 """Draft-and-verify decoding with a small target and a small drafter, both with random weights.
 
-One step, everything on the device: the drafter sees its block of masks from both sides over its cache
+One step, whose lengths stay on the device (the host reads the emitted tokens, and with a tree whether any
+accepted node lies off the first beam): the drafter sees its block of masks from both sides over its cache
 ("full" attention), its logits become a lattice and a path (or the beams' token tree), the target passes
 over the path ("causal") or the tree (the plan's visibility bits) once, the verification accepts a part,
 and the lengths move by it; what was drafted beyond is written over by the next step.

@@ -105,7 +105,7 @@ template <int D> struct Codes {
     }
 };
 
-// The kernel for few query rows (a token, a short chain): bound by the bytes of the cache.
+// The kernel for few query rows (a token, a short chain): the work that each byte of the cache needs is about as long as its way.
 //
 // Keys are the 16 rows of the matrix instruction and query rows its 8 columns: S^T = K Q^T, then
 // O^T = V^T P^T with 16 value channels as rows, so 8 query rows fill an instruction, and the codes
@@ -123,13 +123,16 @@ template <int D> struct Codes {
 // the division at the end takes it out), so most runs need no exchange between lanes for it.
 // kW warps a CTA, kCtas CTAs an SM, kU runs an iteration, kStages iterations in the ring.
 //
-// Measured: one new token of 64 requests over up to 16384 tokens, 40 heads on 8 of 128: 180 us for 752 MB, 4.2 TB/s of the cache.
-// The copies alone take 131 us; with about 285 instructions of a warp for a run's 2176 bytes the unpacking is what bounds it.  64 drafts
-// of 32 tokens over 1023, 16 heads of 64: 64 us, bound by latency (three CTAs an SM; a fourth spills: 72 us).
+// Measured: one new token of 64 requests over up to 16384 tokens, 40 heads on 8 of 128: 179 us for 752 MB, 4.2 TB/s of the cache;
+// the copies alone take 131.  A run's 2176 bytes need 273 instructions of a warp, which would be 84 us if one were issued every clock:
+// the counters say one every second (51 %).  Sixteen warps an SM, as many as the registers hold, do not cover what an instruction waits
+// for: per issue 1.6 warps wait for a result of the fixed kind, 1.1 for the ALU (60 % busy, the most of all units), 0.7 for memory.  64
+// drafts of 32 tokens over 1023, 16 heads of 64: 64 us, bound by latency too (three CTAs an SM; a fourth spills: 72 us).  Some registers
+// go to memory as it is: 8 rows of 128 44 bytes a thread, 16 rows 236, 32 rows 8 (of 64: 24).
 //
 // Before its first step a unit has kEnter places of the line for what every unit costs (queries, the first copies, the join of the
 // warps): with none the CTAs that get many short units end last (64 requests of 32 new tokens over 1023, 16 heads of 64: 76 us
-// instead of 65; one new token over 16384: 184 instead of 182).
+// instead of 65; where units are long they cost a little: one new token over 16384 177 us with none, 179 with them).
 constexpr int kEnter = 4;
 struct StreamRequest : Request {
     __device__ __forceinline__ int places() const { return steps + kEnter; }
@@ -673,8 +676,8 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
     Shape s;
     const long long rows = (long long)max_new * (Hq / Hkv);
     // Query rows are columns of the matrix instruction in the kernel for few rows, which unpacks codes in every warp, and a tile of 128 in
-    // the other.  32 rows over 8192 tokens, 16 requests, 8 key heads of 128: 70 us there, 99 here (of 64: 48 and 77); beyond 32 the sums
-    // no longer fit the registers (64 rows: 107 us here, against twice 70).
+    // the other.  32 rows over 8192 tokens, 16 requests, 8 key heads of 128: 71 us for few rows, 97 for many (of 64: 48 and 75).  Beyond 32
+    // the sums no longer fit the registers, and the codes are unpacked once for every 32 rows: 64 rows 122 and 104 (of 64: 85 and 92).
     s.block = rows > 32;
     if (s.block) {
         s.nt = s.warps = s.unroll = 0;
@@ -683,7 +686,7 @@ Shape shape_of(int32_t D, int32_t Hq, int32_t Hkv, int32_t max_new) {
         s.part_bytes = attn_block_part_bytes(D);
         return s;
     }
-    // 64 requests over 8192, 8 key heads of 128: 8 rows 105 us in one column group, 135 in two; 16 rows 131 us in two, 219 in four
+    // 64 requests over 8192, 8 key heads of 128: 8 rows 104 us in one column group, 131 in two; 16 rows 127 us in two, 214 in four
     s.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
     s.warps = 4;
     s.ctas_sm = s.nt == 1 ? 4 : s.nt == 2 || D == 64 ? 3 : 2;
@@ -754,12 +757,12 @@ extern "C" int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t
     a.out = static_cast<__nv_bfloat16 *>(out);
     a.split = static_cast<SplitUnit *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + align_up(s.grid * sizeof(SplitUnit), 256));
-    // no more CTAs than the line can have steps, as far as the host knows the lengths
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (s.block) {
         DSP_CUDA_TRY(attn_block_launch(a, D, s.grid, st));
         return DSP_OK;
     }
+    // no more CTAs than the line can have steps, as far as the host knows the lengths
     const long long tokens = (long long)max_blocks * page_size, rows = (long long)a.max_new * a.group;
     const long long most = (long long)B * Hkv * ((rows + 8 * s.nt - 1) / (8 * s.nt)) * ((tokens + 16 * s.unroll * s.warps - 1) / (16 * s.unroll * s.warps));
     const int grid = (int)(most < s.grid ? most : s.grid);

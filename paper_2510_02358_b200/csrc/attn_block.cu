@@ -27,11 +27,12 @@
 // The running maximum moves only when a row's scores pass it by 2^8, and only then is the output in
 // tensor memory rescaled (by the softmax warps, between two products of their slot).
 //
-// Measured: a chunk of 2 x 2048 new tokens over 8200, 40 heads on 8 of 128: 674 us, 832 TFLOP/s (half the rate of a plain matrix
-// product); trees of 65 over 8192, 16 requests: 153 us.  A wide token tile takes about 5000 clocks, of which the tensor cores need 2560 (a
-// product of 64 scores columns 48, bound by shared memory, one with the weights 64), the softmax warps 3900 and the fill warps 3400; a
-// copy without exponentials takes as long, one without unpacking 626 us.  The loop from weights over the output's product and the next
-// scores to the next weights is what bounds it: scores and weights of a half tile share their columns, and tensor memory has no others.
+// Measured: a chunk of 2 x 2048 new tokens over 8200, 40 heads on 8 of 128: 719 us among other calls, 780 TFLOP/s, and 656 us, 855
+// TFLOP/s, where it alone is repeated (a plain matrix product: 1670); trees of 65 over 8192, 16 requests: 151 us.  A wide token tile takes
+// about 5000 clocks, of which the tensor cores need 2560 (a product of 64 scores columns 48, bound by shared memory, one with the weights
+// 64), the softmax warps 3900 and the fill warps 3400; of a form that took 674 us a copy without exponentials took as long, one without
+// unpacking 626.  The loop from weights over the output's product and the next scores to the next weights is what bounds it: scores and
+// weights of a half tile share their columns, and tensor memory has no others.  (96 registers a thread; 12 bytes of them go to memory.)
 //
 // Tokens that nobody may see (beyond the length, of a missing block) become zeros, and those whose scale
 // or offset is NaN too, with a bit beside the tile: the rows that see such a token get a NaN score.
@@ -150,7 +151,7 @@ __device__ __forceinline__ void pair_barrier(int id, int threads) { asm volatile
 // than 128 rows counts kWide on the line, of one with fewer kNarrow: it has half the products but the
 // same keys and values to expand (measured: about 4000 clocks against 5000).  Before its first token a unit has kEnter places of the line
 // for what every unit costs, its queries and its output: with none the shares of many short units took longer than others (16
-// requests of 65 new tokens over 8192, 40 heads on 8: 172 us instead of 153; 24 places: 157).
+// requests of 65 new tokens over 8192, 40 heads on 8: 167 us instead of 150; the chunk of 2 x 2048 over 8200: 658 and 657).
 constexpr int kWide = 4, kNarrow = 3, kEnter = 12;
 struct BlockRequest {
     int b, n_new, kv, rows, row0, group, tiles;

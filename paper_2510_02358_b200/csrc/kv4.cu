@@ -12,8 +12,9 @@
 // so the same row gives the same bits (and, right on the edge between two codes, the same code)
 // from every call shape, and dsp_kv4_append's keys are those of dsp_qk_norm_rope.
 //
-// Measured, 8192 tokens: norm and rotation of 40 + 8 heads of 128 in bf16 45 us (201 MB, 4.5 TB/s), with keys and values stored 66 us (219
-// MB, 3.3 TB/s: the codes' arithmetic is the larger part of the second launch); 8 tokens 2.1 and 2.6 us, a launch's latency.
+// Measured, 8192 tokens: norm and rotation of 40 + 8 heads of 128 in bf16 45 us (201 MB, 4.5 TB/s), with keys and values stored 65 us (219
+// MB, 3.4 TB/s: 27 of them for the keys and values, by the codes' arithmetic and by stores of 4 bytes); 8 tokens 2.3 and 2.8 us, a launch's
+// latency.
 #include "kv4.cuh"
 
 namespace dsp {
@@ -566,7 +567,8 @@ struct ReadArgs {
     long long n_slots;
 };
 
-// One word of key codes and one of value codes per lane: eight channels each.  8192 tokens of 8 heads of 128: 12 us for 42 MB written and read.
+// One word of key codes and one of value codes per lane: eight channels each.  8192 tokens of 8 heads of 128: 10 to 12 us for 42 MB read and
+// written (6.5 at the copy's rate): a lane has one load of each in flight before it can store.
 template <typename DT, int D>
 __global__ void __launch_bounds__(kNormThreads) kv4_read_kernel(const ReadArgs a) {
     constexpr int kLanes = D / 8;
@@ -619,7 +621,7 @@ bool strides_ok(int64_t st, int64_t sh, int32_t H, int32_t D) { return sh >= D &
 template <typename DT, int D, bool kAppend>
 cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
     // A long append is two launches: its queries alone need fewer registers and less code than keys and values, and so run
-    // faster (8192 tokens of 40 + 2 x 8 heads of 128: 64 us instead of 74; 2048: 19.8 and 20.3; 1024: 12.4 and 12.1).
+    // faster (8192 tokens of 40 + 2 x 8 heads of 128: 65 us instead of 74; 2048: 19.8 and 20.4; 1024: 12.5 and 12.2).
     if (kAppend && a.Hq > 0 && (long long)a.T * (a.Hq + 2 * a.Hkv) * (D / 16) > 148LL * 4096) {
         NormArgs q = a;
         q.Hkv = 0;
@@ -628,13 +630,13 @@ cudaError_t launch_norm_heads(NormArgs a, cudaStream_t st) {
         a.Hq = 0;
     }
     // Several heads to a group of lanes where there is more than a round or two of groups: a short call is the latency of one
-    // group's chain, a long one wants loads in flight.  40 + 8 heads of 128, several and one: 64 tokens 2.5 and 2.4 us, 272: 3.5 and
-    // 3.6, 512: 4.6 and 5.4, 8192: 46 and 70.  With the codes the chain is longer and registers are dearer: 512 tokens 8.1 and 7.2, 800: 11.3
-    // and 11.2, 8192: 64 and 89.
+    // group's chain, a long one wants loads in flight.  40 + 8 heads of 128, several and one: 64 tokens 2.5 and 2.3 us, 272: 3.5 and
+    // 3.7, 512: 4.6 and 5.4, 8192: 47 and 71.  With the codes the chain is longer and registers are dearer (the forms of several heads keep 24
+    // to 100 bytes a thread in memory): 512 tokens 8.1 and 7.2, 800: 9.8 and 10.5, 8192: 65 and 90.
     // Pairs save shuffles and read both halves of a row at once, which in long calls pays in bf16 only, and not where half of a head of
-    // 128 is turned (8192 tokens, paired and not; bf16: 48 heads of 128 45 and 54 us, half turned 67 and 53; 40 of 64 18.8 and 21.0, half
-    // turned 18.7 and 20.8; 20 of 256, half turned 39 and 45.  fp32: 40 of 64 35 and 33, half turned 65 and 33; 20 of 128 38 and 35).
-    // Short calls are always better paired (64 tokens, bf16, 48 of 128: 2.5 and 3.3, half turned 3.0 and 3.3).
+    // 128 is turned (8192 tokens, paired and not; bf16: 48 heads of 128 45 and 54 us, half turned 67 and 53; 40 of 64 19.1 and 21.1, half
+    // turned 19.2 and 21.4; 20 of 256, half turned 40 and 46.  fp32: 40 of 64 35 and 33, half turned 65 and 33; 20 of 128 38 and 35).
+    // Short calls are always better paired (64 tokens, bf16, 48 of 128: 2.6 and 3.3, half turned 3.0 and 3.2).
     const long long rows = (long long)a.T * (a.Hq + (kAppend ? 2 : 1) * a.Hkv), limit = 148LL * (kAppend ? 2048 : 512);
     const bool apart = sizeof(DT) == 4 || (D == 128 && a.cos_sin && a.rot == D / 2);
     const bool paired = (!apart || rows * (D / 16) <= limit) && (!a.cos_sin || (!a.interleaved && (a.rot == D || a.rot == D / 2)));

@@ -9,7 +9,8 @@
 // table and the ring are only written where no CTA reads (entries of blocks taken now are looked up
 // in the ring, and a block given back goes behind the ring's tail).
 //
-// Bound by its latency: 8 requests of 17 tokens 4.9 us, 1024 of 32 (1.1 MB) 11.2 us, of which the scans and their barriers are most.
+// Bound by its latency: 8 requests of 17 tokens 4.8 us, 1024 of 32 (1.1 MB) 11.0 us, most of it what every CTA does for all requests: three
+// passes that each load a request's numbers and divide (in 64 bits), and four scans with their barriers.
 #include "dsp_common.cuh"
 
 namespace dsp {
@@ -257,8 +258,8 @@ extern "C" int32_t dsp_cache_plan(const int32_t *seq_len, const int32_t *new_len
     a.count = block_count; a.ring_pos = ring_pos; a.cu = cu_new; a.kv_len = kv_len;
     a.slot = slot; a.position = position; a.token_row = token_row;
     a.mask = mask; a.words = mask_words; a.status = row_status;
-    // a request's lengths are scanned by every CTA: few threads have the short barrier (1024 requests of 32 new tokens: 11.4 us with
-    // 256 threads, 12.7 with 1024), many the short loop (4096 requests of 8: 44 and 21 us)
+    // a request's lengths are scanned by every CTA: few threads have the short barrier (1024 requests of 32 new tokens: 11.0 us with
+    // 256 threads, 12.4 with 1024), many the short loop (4096 requests of 8: 44 and 21 us)
     const unsigned threads = B <= 1024 ? 256u : 1024u;
     const size_t smem = ((size_t)3 * (B + 1) + a.N) * sizeof(int32_t);
     if (smem > 40 * 1024)
