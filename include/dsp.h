@@ -887,6 +887,161 @@ int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t
                      int32_t mask_kind, const uint32_t *mask_bits, int32_t mask_words,
                      void *out, void *workspace, size_t workspace_bytes, dsp_stream_t stream);
 
+/* -------------------------------------------------------------------------
+ * After a verified step: tokens are scored, the drafter learns from the target,
+ * and the cache follows what was accepted and which requests go on.
+ */
+
+/* Log-probabilities of given tokens, entropy and the best alternatives.
+ *
+ * With z = x / temperature for every row (b,l), l < row_len[b], of logits [B,L,V]:
+ *   lse = log sum_v exp(z_v),  entropy = lse - sum_v z_v exp(z_v - lse)    (nats; -inf logits add 0)
+ *   logp[b,l,g] = z[tokens[b,l,g]] - lse;  -inf for a token outside 0..V-1
+ *   rank[b,l] = number of tokens that come before tokens[b,l,0] in the total order
+ *               (0: it is the argmax); -1 for a token outside 0..V-1
+ *   the K best tokens in the total order with their logits x and log-probabilities;
+ *   -inf logits are not among them, unused slots (K > V) are id -1, logit and logp -inf.
+ * Rows from row_len[b] on (clipped to 0..L) are not read: logp and lse -inf, rank -1,
+ * entropy 0, no alternatives.  Everything but the scalars of a row is read once.
+ * Any V and any row start run at full speed: what lies outside of whole 16-byte pieces
+ * of a row is read by element.
+ *
+ * The scores fit the library's other calls: logp of a lattice's candidates (tokens =
+ * cand_id, G = KC) under a verifier's row is dsp_cps_search_biased's ver_score, and
+ * top_id, top_logit and lse are what dsp_distill takes of a teacher.
+ *
+ * Inputs : logits (dtype, strides in elements, as for dsp_lattice_build); row_len int32
+ *          [B] (nullable: all rows); tokens int32 [B,L,G] (null with G = 0);
+ *          1e-3 <= temperature <= 1e3; 0 <= K <= DSP_MAX_K, G >= 0.
+ * Outputs: logp float [B,L,G]; rank int32 [B,L] (nullable; needs G >= 1); top_id int32, top_logit,
+ *          top_logp float [B,L,K] (null with K = 0); lse float [B,L]; entropy float [B,L]
+ *          (nullable); row_status uint32 [B] (written): DSP_ROW_NONFINITE_INPUT (that row:
+ *          logp of its tokens, lse and entropy NaN), DSP_ROW_TIMEOUT.
+ * workspace: dsp_token_logprobs_workspace_bytes(B, L, V, dtype), 256-byte aligned.
+ * Errors : INVALID_ARG (null pointer, sizes, strides, alignment, temperature),
+ *          UNSUPPORTED (dtype, K > DSP_MAX_K, G > DSP_MAX_SCORED, V > 2^30, more than 2^24 rows), WORKSPACE, CUDA.
+ *          B == 0 is a no-op returning DSP_OK.
+ */
+#define DSP_MAX_SCORED 1024         /* largest G of dsp_token_logprobs */
+int32_t dsp_token_logprobs_workspace_bytes(int32_t B, int32_t L, int32_t V, int32_t dtype,
+                                           size_t *bytes /* host, out */);
+int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                           int64_t stride_b, int64_t stride_l, const int32_t *row_len,
+                           const int32_t *tokens, int32_t G, float temperature, int32_t K,
+                           float *logp, int32_t *rank, int32_t *top_id, float *top_logit, float *top_logp,
+                           float *lse, float *entropy, uint32_t *row_status,
+                           void *workspace, size_t workspace_bytes, dsp_stream_t stream);
+
+/* Distillation of a drafter from a teacher's top logits: loss and gradient.
+ *
+ * Of the teacher's row the caller has K tokens with their logits t_k, and either the
+ * log-sum-exp of its whole row at this temperature T (teacher_lse) or nothing more:
+ *   teacher_lse given: p_k = exp(t_k / T - teacher_lse), and r = max(0, 1 - sum_k p_k) is the mass of all other tokens;
+ *   teacher_lse null : p   = softmax of t / T over the K tokens, r = 0.
+ * With q = softmax(x / T) of the student's whole row and s = the mass that q gives to all other tokens:
+ *   loss   = sum_k p_k (log p_k - log q_k) + r (log r - log s)             (nats; 0 log 0 = 0)
+ *   accept = sum_k min(p_k, q_k) + min(r, s)    (the best acceptance rate that these masses allow)
+ *   lse    = log sum_v exp(x_v / T)
+ *   dloss / dx_v = (q_v - p_v) / T for the teacher's tokens, q_v (1 - r / s) / T for all others
+ * (the gradient of others is 0 where s is 0).  A slot takes no part if it is at or beyond teacher_count, its id
+ * is outside 0..V-1, or an earlier slot has the same id.  A row without any such token, or with
+ * teacher_lse null and no finite t_k, has loss 0 and gradient 0.  loss is +inf where p_k > 0 = q_k; the gradient stays finite.
+ *
+ * dsp_distill computes the loss, and with `grad` also weight * dloss/dx in the same pass: the row
+ * is read once, stays in the shared memory of a cluster of CTAs (rows up to 1.7 MB), and its gradient is written
+ * once.  A row of weight 0 is not read: loss, accept 0, lse -inf, gradient 0.
+ * dsp_distill_grad computes row_grad * dloss/dx from the student's logits and what dsp_distill left in
+ * `state`, for callers whose factor comes later (an autograd graph); row_grad 0 gives 0 without reading the row.
+ * The gradient has the logits' dtype, one rounding; sums, statistics and factors are kept in 32 bits or more.
+ * grad may be the logits themselves (same address and strides) and must not overlap them otherwise.
+ *
+ * Inputs : student_logits [B,L,V] (dtype, strides in elements, as for dsp_lattice_build); teacher_id
+ *          int32, teacher_logit float [B,L,K]; teacher_lse float [B,L] (nullable);
+ *          teacher_count int32 [B,L] (nullable: K); weight, row_grad float [B,L] (weight nullable: 1);
+ *          1e-3 <= temperature <= 1e3.
+ * Outputs: loss, accept, lse float [B,L] (accept and lse nullable); state float [B,L,K+4] (nullable: dsp_distill_grad's input, 16-byte
+ *          aligned; its layout is the library's own); grad [B,L,V] (dtype, strides in elements; nullable);
+ *          row_status uint32 [B] (nullable): flags OR-ed into existing content, DSP_ROW_NONFINITE_INPUT
+ *          (NaN or +inf logit of a row that is read, no finite logit, or a NaN or +inf among the teacher's values: that
+ *          row's outputs are NaN or unspecified), DSP_ROW_TIMEOUT.
+ * Errors : INVALID_ARG (null pointer, sizes, strides, alignment, temperature, K < 1), UNSUPPORTED (dtype,
+ *          K > DSP_MAX_TEACHER, V > 2^30, more than 2^24 rows), CUDA.  B == 0 is a no-op returning DSP_OK.
+ */
+#define DSP_MAX_TEACHER 256         /* largest K of dsp_distill */
+int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                    int64_t stride_b, int64_t stride_l, const int32_t *teacher_id, const float *teacher_logit,
+                    const float *teacher_lse, const int32_t *teacher_count, int32_t K, float temperature,
+                    const float *weight, float *loss, float *accept, float *lse, float *state,
+                    void *grad, int64_t grad_stride_b, int64_t grad_stride_l,
+                    uint32_t *row_status, dsp_stream_t stream);
+int32_t dsp_distill_grad(const void *student_logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                         int64_t stride_b, int64_t stride_l, const int32_t *teacher_id, int32_t K,
+                         const float *state, float temperature, const float *row_grad,
+                         void *grad, int64_t grad_stride_b, int64_t grad_stride_l, dsp_stream_t stream);
+
+/* Requests that fork, shrink, move or end: new block tables from old ones, with shared blocks.
+ *
+ * Output row r holds the first keep_len[r] tokens of input row src_row[r] (keep_len null: all of its
+ * seq_len_in); -1: the row is empty.  Several rows may continue one.  Blocks that are full of kept tokens are
+ * shared by all rows that keep them.  A block that is partly filled belongs to one row, because the row's next tokens go there: where
+ * other rows hold it too, the row that holds all of it, else the lowest of the rows that hold a part, keeps it, and each
+ * other row takes a block from the free list, into which its tokens have to be copied
+ * (copy_src, copy_dst, copy_len; dsp_kv4_copy, once for all layers of a cache).  Blocks that input rows hold
+ * (block_count_in of each, those of rejected drafts among them) and no output row does go back to the free list, each
+ * once, in the order of the input rows, then of the table; so src_row -1 frees a request and keep_len alone shortens it.  The
+ * ring is used as in dsp_cache_plan: blocks that return are free from the next call on.
+ * All requests that share blocks with one of the call have to be in it.  dsp_cache_plan gives surplus blocks back without
+ * looking at who else holds them: a request with shared blocks is shortened by this call, not by a smaller seq_len there
+ * (the blocks that it adds for new tokens are never shared).
+ * A row that cannot be served comes out empty and says why in row_status: DSP_ROW_BAD_LENGTH (src_row outside
+ * -1..B_in-1, keep_len or seq_len_in negative, keep_len beyond seq_len_in, or more blocks needed than block_count_in), DSP_ROW_BAD_BLOCK (a block number
+ * outside 0..n_blocks-1 among those kept), DSP_ROW_NO_BLOCKS (rows that need a block from the first on whose need,
+ * counted over the rows, passes the free ones).  A call may be repeated on its inputs.
+ *
+ * Inputs : src_row, keep_len int32 [B_out]; seq_len_in, block_count_in int32 [B_in]; ring_pos_in int64 [2];
+ *          block_table_in int32 [B_in, max_blocks] (stride table_in_stride).
+ * In/out : free_ring int32 [n_blocks].
+ * Outputs: block_table int32 [B_out, max_blocks] (stride table_stride; must not overlap the input table; entries beyond a
+ *          row's count are left as they are), block_count, seq_len int32 [B_out], ring_pos int64 [2], copy_src, copy_dst (block
+ *          numbers, -1: nothing to copy) and copy_len (tokens) int32 [B_out], row_status uint32 [B_out]; none may overlap an input.
+ * workspace: dsp_cache_fork_workspace_bytes(B_in, B_out, n_blocks), 256-byte aligned.
+ * Errors : INVALID_ARG (null pointer, B_in < 0, B_out < 0, page_size < 1, n_blocks < 1, max_blocks < 1, strides, overlap of
+ *          tables or ring positions), UNSUPPORTED (B_in or B_out > DSP_MAX_PLAN_ROWS, rows * max_blocks > 2^30), WORKSPACE, CUDA.
+ */
+#define DSP_ROW_BAD_BLOCK  1024u   /* dsp_cache_fork: a kept table entry is no block of the pool */
+int32_t dsp_cache_fork_workspace_bytes(int32_t B_in, int32_t B_out, int32_t n_blocks, size_t *bytes /* host, out */);
+int32_t dsp_cache_fork(const int32_t *src_row, const int32_t *keep_len, int32_t B_out,
+                       const int32_t *seq_len_in, const int32_t *block_count_in, const int64_t *ring_pos_in,
+                       const int32_t *block_table_in, int64_t table_in_stride, int32_t B_in,
+                       int32_t page_size, int32_t n_blocks, int32_t max_blocks, int32_t *free_ring,
+                       int32_t *block_table, int64_t table_stride, int32_t *block_count, int32_t *seq_len,
+                       int64_t *ring_pos, int32_t *copy_src, int32_t *copy_dst, int32_t *copy_len,
+                       uint32_t *row_status, void *workspace, size_t workspace_bytes, dsp_stream_t stream);
+
+/* Copies of blocks and moves of tokens in the 4-bit cache, for all layers of a model at once.
+ *
+ * cache: layer i is a cache of dsp_kv4_append (uint8 [n_blocks, Hkv, page_size * (D + 8)]) at cache + i * layer_stride
+ * bytes (a multiple of 16; not read with one layer).
+ * dsp_kv4_copy: block copy_src[i] to block copy_dst[i] for i < N: the runs of 16 tokens that hold its first copy_len[i]
+ * tokens (copy_len null: the whole block).  An entry with a block outside 0..n_blocks-1 is skipped.  No block may be the
+ * target of two entries, or the target of one and the source of another.
+ * dsp_kv4_compact: after a tree was verified (new tokens as dsp_cache_plan lays them out: the last kept token at seq_len[b],
+ * node n at seq_len[b] + 1 + n), the accepted nodes' keys and values move behind the last kept token: node accepted_node[b,i] to
+ * seq_len[b] + 1 + i, for i < accepted_len[b] (clipped to 0..L).  accepted_node is dsp_verify_tree's: int32 [B,L], growing
+ * along i (other orders move something unspecified within the request).  A move whose source or target lies before the
+ * tree, beyond the table, or in a block outside 0..n_blocks-1 is skipped.
+ * Errors : INVALID_ARG (null pointer, negative sizes, layers < 1, n_blocks < 1, Hkv < 1, page_size not a multiple of 16, alignment, layer_stride
+ *          shorter than a layer, table_stride < max_blocks), UNSUPPORTED (D not 64 / 128, layers > 65535, Hkv > 4096,
+ *          B or N > 2^24), CUDA.  B, N or L = 0 is a no-op returning DSP_OK.
+ */
+int32_t dsp_kv4_copy(void *cache, int32_t layers, int64_t layer_stride, int32_t n_blocks, int32_t page_size,
+                     int32_t Hkv, int32_t D, const int32_t *copy_src, const int32_t *copy_dst,
+                     const int32_t *copy_len, int32_t N, dsp_stream_t stream);
+int32_t dsp_kv4_compact(void *cache, int32_t layers, int64_t layer_stride, int32_t n_blocks, int32_t page_size,
+                        int32_t Hkv, int32_t D, const int32_t *block_table, int64_t table_stride, int32_t max_blocks,
+                        const int32_t *seq_len, const int32_t *accepted_node, const int32_t *accepted_len,
+                        int32_t B, int32_t L, dsp_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,10 +26,11 @@ DSP_STATIC_WS_BYTES = 4 << 20
 DSP_F32, DSP_BF16 = 0, 1
 ROW_NONFINITE_INPUT, ROW_ZERO_RESIDUAL, ROW_NO_BONUS_ROW, ROW_EOS_ACCEPTED, ROW_EOS_STOPPED = 1, 2, 4, 8, 16
 ROW_TIMEOUT = 32
-ROW_NO_BLOCKS, ROW_TABLE_FULL, ROW_PLAN_FULL, ROW_BAD_LENGTH = 64, 128, 256, 512
+ROW_NO_BLOCKS, ROW_TABLE_FULL, ROW_PLAN_FULL, ROW_BAD_LENGTH, ROW_BAD_BLOCK = 64, 128, 256, 512, 1024
 DSP_MASK_CAUSAL, DSP_MASK_FULL, DSP_MASK_BITS = 0, 1, 2
 DSP_MAX_PLAN_ROWS = 8192
 DSP_MAX_K, DSP_MAX_W, DSP_MAX_L = 32, 32, 1024
+DSP_MAX_SCORED, DSP_MAX_TEACHER = 1024, 256
 
 EXPORTS = ["dsp_strerror", "dsp_last_cuda_error", "dsp_version", "dsp_profile_events", "dsp_read_probe", "dsp_lattice_workspace_bytes",
            "dsp_lattice_build", "dsp_lattice_build_static", "dsp_cps_search", "dsp_cps_search_biased", "dsp_verify_workspace_bytes", "dsp_verify", "dsp_draft_verify_step",
@@ -41,6 +42,8 @@ EXPORTS = ["dsp_strerror", "dsp_last_cuda_error", "dsp_version", "dsp_profile_ev
            "dsp_beam_tree", "dsp_verify_tree_workspace_bytes", "dsp_verify_tree", "dsp_verify_tree_stochastic",
            "dsp_cache_plan", "dsp_qk_norm_rope", "dsp_kv4_append", "dsp_kv4_read",
            "dsp_attn_kv4_workspace_bytes", "dsp_attn_kv4",
+           "dsp_token_logprobs_workspace_bytes", "dsp_token_logprobs", "dsp_distill", "dsp_distill_grad",
+           "dsp_cache_fork_workspace_bytes", "dsp_cache_fork", "dsp_kv4_copy", "dsp_kv4_compact",
            "dsp_adl_init", "dsp_adl_update", "dsp_breadth_init", "dsp_breadth_update"]
 
 
@@ -70,6 +73,12 @@ _SIGNATURES = {
     "dsp_kv4_append": "pppiiiiillllllppfppiiippiipp",
     "dsp_kv4_read": "piiiipiippp",
     "dsp_attn_kv4": "piiiiiillpiiplippifipippzp",
+    "dsp_token_logprobs": "piiiill" "ppifi" "pppppppp" "pzp",
+    "dsp_distill": "piiiill" "ppppif" "p" "pppp" "pll" "pp",
+    "dsp_distill_grad": "piiiill" "pipfp" "pllp",
+    "dsp_cache_fork": "ppi" "ppppliiii" "pplppp" "pppp" "pzp",
+    "dsp_kv4_copy": "piliiii" "pppip",
+    "dsp_kv4_compact": "piliiii" "plipppiip",
 }
 
 _lib = None
@@ -929,3 +938,233 @@ def dsp_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor
         kv_len.data_ptr(), cu_new.data_ptr(), max_new, D ** -0.5 if scale is None else scale, kind, _at(bits), words,
         out.data_ptr(), workspace.data_ptr(), workspace.nbytes, queue))
     return out
+
+
+# ---- after a verified step: scores of tokens, distillation of the drafter, forks and moves of the cache ----
+
+def _rows(name: str, t: torch.Tensor, like=None):
+    """Sizes and strides of logits [B, L, V] with a contiguous vocabulary (strides of single rows are free)."""
+    if t.dim() != 3 or not t.is_cuda or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError("%s must be a CUDA tensor [B, L, V] with a contiguous vocabulary dimension" % name)
+    B, L, V = t.shape
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError("%s must have the logits' shape, dtype and device" % name)
+    sl = t.stride(1) if L > 1 else V
+    return B, L, V, (t.stride(0) if B > 1 else L * sl), sl
+
+
+def _maybe(name: str, t: Optional[torch.Tensor], shape, dtype, dev):
+    return None if t is None else _ints(name, t, shape, dtype, dev).data_ptr()
+
+
+def dsp_token_logprobs_workspace_bytes(B: int, L: int, V: int, dtype: int) -> int:
+    n = C.c_size_t(0)
+    _check("dsp_token_logprobs_workspace_bytes", lib().dsp_token_logprobs_workspace_bytes(B, L, V, dtype, C.byref(n)))
+    return n.value
+
+
+@lru_cache(maxsize=1024)
+def _score_workspace(B: int, L: int, V: int, dtype: int, device: int) -> int:
+    return max(256, dsp_token_logprobs_workspace_bytes(B, L, V, dtype))      # a function of the sizes and the device's SM count
+
+
+@_on_stream
+def dsp_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, K: int = 0, temperature: float = 1.0,
+                       row_len: Optional[torch.Tensor] = None, out: Optional[SimpleNamespace] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
+    """Log-probabilities ``logp`` of ``tokens`` (int32 [B, L] or [B, L, G]) under ``logits`` / temperature, the first token's
+    ``rank``, ``lse``, ``entropy`` and the K best alternatives (``top_id``, ``top_logit``, ``top_logp``, [B, L, K]) of the rows
+    before ``row_len`` (int32 [B])."""
+    B, L, V, sb, sl = _rows("logits", logits)
+    dt, dev = _dtype(logits), logits.device
+    i32, f32 = torch.int32, torch.float32
+    G, shape = 0, (B, L, 0)
+    if tokens is not None:
+        if tokens.dim() not in (2, 3):
+            raise ValueError("tokens must be int32 [B, L] or [B, L, G]")
+        G = tokens.shape[2] if tokens.dim() == 3 else 1
+        shape = (B, L) + tuple(tokens.shape[2:])
+        _ints("tokens", tokens, shape, i32, dev)
+    lens = _maybe("row_len", row_len, (B,), i32, dev)
+    if out is None:
+        e = torch.empty
+        out = SimpleNamespace(logp=e(shape, dtype=f32, device=dev) if G else None, rank=e(B, L, dtype=i32, device=dev) if G else None,
+                              top_id=e(B, L, K, dtype=i32, device=dev) if K else None, top_logit=e(B, L, K, dtype=f32, device=dev) if K else None,
+                              top_logp=e(B, L, K, dtype=f32, device=dev) if K else None, lse=e(B, L, dtype=f32, device=dev),
+                              entropy=e(B, L, dtype=f32, device=dev), row_status=e(B, dtype=i32, device=dev))
+    else:
+        if G:
+            _ints("out.logp", out.logp, shape, f32, dev)
+            _maybe("out.rank", out.rank, (B, L), i32, dev)
+        if K:
+            _ints("out.top_id", out.top_id, (B, L, K), i32, dev)
+            _ints("out.top_logit", out.top_logit, (B, L, K), f32, dev)
+            _ints("out.top_logp", out.top_logp, (B, L, K), f32, dev)
+        _ints("out.lse", out.lse, (B, L), f32, dev)
+        _maybe("out.entropy", out.entropy, (B, L), f32, dev)
+        _ints("out.row_status", out.row_status, (B,), i32, dev)
+    queue = _queue(dev)                                            # before the workspace, whose size goes by the current device
+    if workspace is None:
+        workspace = torch.empty(_score_workspace(B, L, V, dt, dev.index), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % dev)
+    _check("dsp_token_logprobs", lib().dsp_token_logprobs(
+        logits.data_ptr(), dt, B, L, V, sb, sl, lens, _at(tokens) if G else None, G, temperature, K,
+        out.logp.data_ptr() if G else None, _at(out.rank) if G else None, _at(out.top_id) if K else None,
+        _at(out.top_logit) if K else None, _at(out.top_logp) if K else None, out.lse.data_ptr(), _at(out.entropy),
+        out.row_status.data_ptr(), workspace.data_ptr(), workspace.nbytes, queue))
+    return out
+
+
+def _grad_rows(grad, logits: torch.Tensor):
+    """(tensor, strides) of the gradient that a call writes: a new one for True, else the caller's (the logits themselves, if wanted)."""
+    if grad is True:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _, _, _, sb, sl = _rows("grad", grad, logits)
+    return grad, sb, sl
+
+
+@_on_stream
+def dsp_distill(student: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor, *,
+                teacher_lse: Optional[torch.Tensor] = None, teacher_count: Optional[torch.Tensor] = None,
+                weight: Optional[torch.Tensor] = None, temperature: float = 1.0, grad=None, state=None,
+                row_status: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
+    """Loss of ``student`` logits [B, L, V] against a teacher's top tokens ``teacher_id`` (int32 [B, L, K]) with ``teacher_logit``
+    (float) and, for the mass of all others, ``teacher_lse`` (float [B, L]).  Returns ``loss``, ``accept``, ``lse`` [B, L].
+    ``grad``: True or a tensor like the logits (or the logits themselves) takes ``weight`` * dloss/dlogits in the same pass.
+    ``state`` (by default kept where no gradient is asked for) is what dsp_distill_grad needs."""
+    B, L, V, sb, sl = _rows("student", student)
+    dt, dev, f32 = _dtype(student), student.device, torch.float32
+    if teacher_id.dim() != 3:
+        raise ValueError("teacher_id must be int32 [B, L, K]")
+    K = teacher_id.shape[2]
+    _ints("teacher_id", teacher_id, (B, L, K), torch.int32, dev)
+    _ints("teacher_logit", teacher_logit, (B, L, K), f32, dev)
+    lse_in = _maybe("teacher_lse", teacher_lse, (B, L), f32, dev)
+    count = _maybe("teacher_count", teacher_count, (B, L), torch.int32, dev)
+    w = _maybe("weight", weight, (B, L), f32, dev)
+    status = _maybe("row_status", row_status, (B,), torch.int32, dev)
+    grad = None if grad is False else grad
+    gb, gl = 0, 0
+    if grad is not None:
+        grad, gb, gl = _grad_rows(grad, student)
+    if state is None and grad is None or state is True:
+        state = torch.empty(B, L, K + 4, dtype=f32, device=dev)
+    elif state is None or state is False:
+        state = None
+    else:
+        _ints("state", state, (B, L, K + 4), f32, dev)
+    e = torch.empty
+    loss, accept, lse = e(B, L, dtype=f32, device=dev), e(B, L, dtype=f32, device=dev), e(B, L, dtype=f32, device=dev)
+    _check("dsp_distill", lib().dsp_distill(
+        student.data_ptr(), dt, B, L, V, sb, sl, teacher_id.data_ptr(), teacher_logit.data_ptr(), lse_in, count, K, temperature, w,
+        loss.data_ptr(), accept.data_ptr(), lse.data_ptr(), _at(state), _at(grad), gb, gl, status, _queue(dev)))
+    return SimpleNamespace(loss=loss, accept=accept, lse=lse, state=state, grad=grad)
+
+
+@_on_stream
+def dsp_distill_grad(student: torch.Tensor, teacher_id: torch.Tensor, state: torch.Tensor, row_grad: torch.Tensor, *,
+                     temperature: float = 1.0, grad=True, stream=None) -> torch.Tensor:
+    """``row_grad`` (float [B, L]) * dloss/dlogits from the logits, ids and temperature of a dsp_distill call and its ``state``;
+    ``grad``: True for a new tensor, else one like the logits (or the logits themselves)."""
+    B, L, V, sb, sl = _rows("student", student)
+    dt, dev = _dtype(student), student.device
+    if teacher_id.dim() != 3:
+        raise ValueError("teacher_id must be int32 [B, L, K]")
+    K = teacher_id.shape[2]
+    _ints("teacher_id", teacher_id, (B, L, K), torch.int32, dev)
+    _ints("state", state, (B, L, K + 4), torch.float32, dev)
+    _ints("row_grad", row_grad, (B, L), torch.float32, dev)
+    grad, gb, gl = _grad_rows(grad, student)
+    _check("dsp_distill_grad", lib().dsp_distill_grad(
+        student.data_ptr(), dt, B, L, V, sb, sl, teacher_id.data_ptr(), K, state.data_ptr(), temperature, row_grad.data_ptr(),
+        grad.data_ptr(), gb, gl, _queue(dev)))
+    return grad
+
+
+def dsp_cache_fork_workspace_bytes(B_in: int, B_out: int, n_blocks: int) -> int:
+    n = C.c_size_t(0)
+    _check("dsp_cache_fork_workspace_bytes", lib().dsp_cache_fork_workspace_bytes(B_in, B_out, n_blocks, C.byref(n)))
+    return n.value
+
+
+@_on_stream
+def dsp_cache_fork(src_row: torch.Tensor, keep_len: Optional[torch.Tensor], seq_len: torch.Tensor, block_count: torch.Tensor,
+                   ring_pos: torch.Tensor, block_table: torch.Tensor, free_ring: torch.Tensor, page_size: int, new_table: torch.Tensor, *,
+                   out: Optional[SimpleNamespace] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> SimpleNamespace:
+    """The tables of requests that continue others: row r of ``new_table`` (int32 [B_out, max_blocks]) holds the first ``keep_len[r]``
+    tokens of row ``src_row[r]`` of ``block_table`` (-1: none).  ``free_ring`` is updated in place; returned are ``block_count``,
+    ``seq_len``, ``ring_pos`` of the new rows, the blocks to copy (``copy_src``, ``copy_dst``, ``copy_len``, for dsp_kv4_copy) and
+    ``row_status``."""
+    dev, i32, i64 = src_row.device, torch.int32, torch.int64
+    if not src_row.is_cuda:
+        raise ValueError("src_row must be a CUDA tensor")
+    Bo, Bi, n_blocks = src_row.shape[0], seq_len.shape[0], free_ring.numel()
+    _ints("src_row", src_row, (Bo,), i32, dev)
+    keep = _maybe("keep_len", keep_len, (Bo,), i32, dev)
+    _ints("seq_len", seq_len, (Bi,), i32, dev)
+    _ints("block_count", block_count, (Bi,), i32, dev)
+    _ints("ring_pos", ring_pos, (2,), i64, dev)
+    _ints("free_ring", free_ring, (n_blocks,), i32, dev)
+    old, old_stride, width = _table(block_table, Bi, dev)
+    new, new_stride, new_width = _table(new_table, Bo, dev)
+    if width != new_width:
+        raise ValueError("new_table must be as wide as block_table")
+    if out is None:
+        count, seq, status, src, dst, n = torch.unsafe_split_with_sizes(torch.empty(6 * Bo, dtype=i32, device=dev), (Bo,) * 6)
+        out = SimpleNamespace(block_count=count, seq_len=seq, row_status=status, copy_src=src, copy_dst=dst, copy_len=n,
+                              ring_pos=torch.empty(2, dtype=i64, device=dev))
+    else:
+        for name in ("block_count", "seq_len", "row_status", "copy_src", "copy_dst", "copy_len"):
+            _ints("out." + name, getattr(out, name), (Bo,), i32, dev)
+        _ints("out.ring_pos", out.ring_pos, (2,), i64, dev)
+    queue = _queue(dev)
+    if workspace is None:
+        workspace = torch.empty(dsp_cache_fork_workspace_bytes(Bi, Bo, n_blocks), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % dev)
+    _check("dsp_cache_fork", lib().dsp_cache_fork(
+        src_row.data_ptr(), keep, Bo, seq_len.data_ptr(), block_count.data_ptr(), ring_pos.data_ptr(), old, old_stride, Bi, page_size,
+        n_blocks, width, free_ring.data_ptr(), new, new_stride, out.block_count.data_ptr(), out.seq_len.data_ptr(),
+        out.ring_pos.data_ptr(), out.copy_src.data_ptr(), out.copy_dst.data_ptr(), out.copy_len.data_ptr(), out.row_status.data_ptr(),
+        workspace.data_ptr(), workspace.nbytes, queue))
+    return out
+
+
+def _layers(cache: torch.Tensor, D: int):
+    """(address, layers, bytes from layer to layer, blocks, page, heads) of one layer's cache, or of [layers, ...] of them."""
+    one = cache[0] if cache.dim() == 4 and cache.shape[0] > 0 else cache
+    if one.dim() != 3 or cache.dtype != torch.uint8 or not cache.is_cuda or not one.is_contiguous() or one.shape[2] % (D + 8) != 0:
+        raise ValueError("cache must be a uint8 CUDA tensor [n_blocks, Hkv, page_size * (D + 8)] or [layers, ...] of contiguous ones")
+    n_blocks, Hkv, size = one.shape
+    layers = cache.shape[0] if cache.dim() == 4 else 1
+    return cache.data_ptr(), layers, (cache.stride(0) if layers > 1 else 0), n_blocks, size // (D + 8), Hkv, D
+
+
+@_on_stream
+def dsp_kv4_copy(cache: torch.Tensor, D: int, copy_src: torch.Tensor, copy_dst: torch.Tensor,
+                 copy_len: Optional[torch.Tensor] = None, *, stream=None) -> None:
+    """Blocks ``copy_src`` to ``copy_dst`` (int32 [N], -1: nothing) of ``cache`` ([n_blocks, Hkv, bytes], or [layers, ...] of them): the
+    runs of 16 tokens that hold the first ``copy_len`` tokens, or all of them."""
+    where, dev, N = _layers(cache, D), cache.device, copy_src.shape[0]
+    _ints("copy_src", copy_src, (N,), torch.int32, dev)
+    _ints("copy_dst", copy_dst, (N,), torch.int32, dev)
+    _check("dsp_kv4_copy", lib().dsp_kv4_copy(*where, copy_src.data_ptr(), copy_dst.data_ptr(),
+                                              _maybe("copy_len", copy_len, (N,), torch.int32, dev), N, _queue(dev)))
+
+
+@_on_stream
+def dsp_kv4_compact(cache: torch.Tensor, D: int, block_table: torch.Tensor, seq_len: torch.Tensor, accepted_node: torch.Tensor,
+                    accepted_len: torch.Tensor, *, stream=None) -> None:
+    """The accepted nodes of verified trees (``accepted_node`` int32 [B, L], ``accepted_len`` [B] of dsp_verify_tree) move right behind the
+    last kept token, which is at ``seq_len`` (the length that the trees were planned with), in ``cache`` as in dsp_kv4_copy."""
+    where, dev, B = _layers(cache, D), cache.device, seq_len.shape[0]
+    table, stride, width = _table(block_table, B, dev)
+    if accepted_node.dim() != 2:
+        raise ValueError("accepted_node must be int32 [B, L]")
+    L = accepted_node.shape[1]
+    _ints("seq_len", seq_len, (B,), torch.int32, dev)
+    _ints("accepted_node", accepted_node, (B, L), torch.int32, dev)
+    _ints("accepted_len", accepted_len, (B,), torch.int32, dev)
+    _check("dsp_kv4_compact", lib().dsp_kv4_compact(*where, table, stride, width, seq_len.data_ptr(), accepted_node.data_ptr(),
+                                                    accepted_len.data_ptr(), B, L, _queue(dev)))

@@ -9,7 +9,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdsp.so")
 SOURCES = ["api.cu", "lattice.cu", "cps.cu", "verify.cu", "step.cu", "step_graph.cu", "unmask.cu", "shard.cu", "tree.cu", "tree_stochastic.cu",
-           "plan.cu", "kv4.cu", "attn.cu", "attn_block.cu"]
+           "plan.cu", "kv4.cu", "attn.cu", "attn_block.cu", "score.cu", "distill.cu", "fork.cu", "kv4_move.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "8"]
 

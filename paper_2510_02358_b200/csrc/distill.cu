@@ -1,0 +1,687 @@
+// dsp_distill, dsp_distill_grad: a drafter learns from the teacher's top logits (loss and gradient: dsp.h).
+//
+// Everything but K values of a row follows from two numbers.  With e_v = 2^(x_v log2e/T - c), c the largest exponent
+// among the tokens that the teacher does not name, and S their sum of e_v:
+//   q_v = e_v 2^(c - c_all) / S_all,   s = S 2^(c - c_all) / S_all,   dloss/dx_v = e_v * f,
+//   f = (2^(c - c_all) / S_all - r / S) / T,
+// so the gradient of a row is one exponential and one product per element, with K elements put in afterwards.  S is
+// summed over the other tokens alone (the teacher's are taken out of the row before the sum), because s and r / s cannot be had from 1 - sum q
+// where the teacher's tokens hold nearly all of the mass.
+//
+// The floor is one read and one write of the row.  A row is cut into equal slices for a cluster of CTAs, a slice stays in
+// its CTA's shared memory between the sums and the gradient (bulk copies in and out), and the CTAs exchange five numbers each
+// over distributed shared memory.  The CTAs of an SM belong to different rows, so one loads while another sums.
+#include "stream_core.cuh"
+
+namespace dsp {
+namespace {
+
+constexpr int kDT = 256;                        // threads of a CTA: one per teacher slot
+static_assert(kDT == DSP_MAX_TEACHER && kDT == kThreads, "one thread per slot");
+constexpr int kMaxCluster = 8;
+constexpr int kSliceVecs = 2560;                 // a CTA's share of a row, 40 KB, unless the cluster is at its largest
+constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no part
+
+struct DistillArgs {
+    const void *x;
+    long long sb, sl;
+    int L, V, K, C;                             // C: CTAs of a row
+    int buf_vecs;                               // 16-byte vectors that a CTA's buffer holds
+    const int32_t *id, *count;
+    const float *val, *tlse, *weight;
+    double scale, inv_t;                        // log2(e) / T, 1 / T
+    float s_hi, s_lo;                           // scale = s_hi + s_lo, s_lo > 0: both products of -inf are then -inf
+    float *loss, *accept, *lse, *state;
+    void *g;
+    long long gsb, gsl;
+    uint32_t *status;
+};
+
+// What a CTA knows of its slice, handed to all CTAs of the row.
+struct Part {
+    double S, E, P, H;       // sums: other tokens (against c), the teacher's tokens (against ct), p, p (log p - z)
+    float c, ct;
+};
+struct Found {               // what follows for the row
+    double c_all, inv_all;
+    float c, fw;             // reference of the others, their factor with the row's weight
+    float rest;              // min(r, s)
+    int none;                // the list says nothing: no gradient
+};
+struct CopyBar {
+    uint64_t bar;
+    int timed_out;
+};
+struct Shared : CopyBar {
+    Part part[kMaxCluster];
+    float accept[kMaxCluster];
+    Found found;
+    __align__(16) int id[kDT];
+    double red[kWarps][3];
+    float redc[kWarps], redt[kWarps];
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void *p, int rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, uint64_t v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void bulk_store(void *dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_store_read_wait() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
+// A row in 16-byte pieces: piece i holds the elements [i N - h, (i + 1) N - h), h the row's distance from the boundary before it.
+// Pieces lo .. hi-1 lie inside the row; of the first and the last a part may lie outside, which is neither read nor written.
+template <typename DT>
+struct Pieces {
+    static constexpr int N = Elem<DT>::N;
+    int h, n, lo, hi;
+    __device__ __forceinline__ Pieces(const DT *row, int V) {
+        h = (int)((reinterpret_cast<uintptr_t>(row) / sizeof(DT)) % N);
+        n = (h + V + N - 1) / N;
+        lo = h ? 1 : 0;
+        hi = (h + V) / N;
+    }
+};
+// Calls at(element, place) for the elements of the partly outside pieces among [a, b), one element a thread; outside: element -1.
+template <typename DT, typename At>
+__device__ __forceinline__ void edges(const Pieces<DT> &p, int V, int a, int b, At at) {
+    constexpr int N = Elem<DT>::N;
+    const int tid = threadIdx.x;
+    auto one = [&](int piece, int e) {
+        const int v = piece * N + e - p.h;
+        at(v >= 0 && v < V ? v : -1, (piece - a) * N + e);
+    };
+    if (p.lo == 1 && a == 0 && tid < N) one(0, tid);
+    if (p.hi < p.n && p.n - 1 >= p.lo && p.n == b && tid >= 32 && tid < 32 + N) one(p.n - 1, tid - 32);
+}
+
+// Pieces [a, b) of the row into the buffer.  Thread 0 sends the copies; a barrier of the CTA lies between the last use of the buffer
+// (fenced) and this call.  Complete after take_copies and a barrier of the CTA.
+template <typename DT>
+__device__ __forceinline__ void send_copies(const DT *row, const Pieces<DT> &p, int V, int a, int b, DT *buf, CopyBar &sh) {
+    constexpr int N = Elem<DT>::N;
+    if (threadIdx.x == 0) {
+        const int l = max(a, p.lo), u = min(b, p.hi);
+        const uint32_t bytes = u > l ? (uint32_t)(u - l) * 16u : 0u;
+        mbar_expect_tx(&sh.bar, bytes);
+        const char *src = reinterpret_cast<const char *>(row + ((long long)l * N - p.h));
+        char *dst = reinterpret_cast<char *>(buf + (size_t)(l - a) * N);
+        constexpr uint32_t kPiece = 16384;
+        for (uint32_t o = 0; o < bytes; o += kPiece) bulk_load(dst + o, src + o, min(kPiece, bytes - o), &sh.bar);
+    }
+    edges<DT>(p, V, a, b, [&](int v, int place) {
+        if (v >= 0) buf[place] = row[v];
+        else if constexpr (N == 8) reinterpret_cast<unsigned short *>(buf)[place] = 0xFF80u;
+        else reinterpret_cast<uint32_t *>(buf)[place] = 0xFF800000u;
+    });
+}
+__device__ __forceinline__ void take_copies(CopyBar &sh, uint32_t parity) {
+    volatile int *abort = &sh.timed_out;
+    if (mbar_wait(&sh.bar, parity, abort)) return;
+    sh.timed_out = 1;                           // once more, so that no copy is under way into a buffer that is used again
+    const long long t0 = clock64();
+    while (!mbar_try(smem_addr(&sh.bar), parity) && clock64() - t0 < kWaitCycles) {}
+}
+
+template <typename DT> __device__ __forceinline__ float elem_of(const DT *buf, int i) { return Elem<DT>::load1(buf + i); }
+template <typename DT> __device__ __forceinline__ void hide(DT *buf, int i) {
+    if constexpr (sizeof(DT) == 2) reinterpret_cast<unsigned short *>(buf)[i] = 0xFF80u;
+    else reinterpret_cast<uint32_t *>(buf)[i] = 0xFF800000u;
+}
+template <typename DT> __device__ __forceinline__ DT rounded(float v) {
+    if constexpr (sizeof(DT) == 2) return __float2bfloat16(v);
+    else return v;
+}
+
+// Sum of 2^(x s - c) over the buffer's pieces, by this thread's share, against its own running reference c.
+template <typename DT>
+__device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s_hi, float s_lo, float &c, unsigned long long &S2) {
+    constexpr int N = Elem<DT>::N, kU = 4;
+    const uint32_t nw = Elem<DT>::kNegInfWord;
+    const unsigned long long hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo);
+    for (int i0 = threadIdx.x; i0 < n; i0 += kU * kDT) {
+        uint4 v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) v[u] = i0 + u * kDT < n ? buf[i0 + u * kDT] : make_uint4(nw, nw, nw, nw);
+        const float tm = fmaxf(fmaxf(Elem<DT>::vmax(v[0]), Elem<DT>::vmax(v[1])), fmaxf(Elem<DT>::vmax(v[2]), Elem<DT>::vmax(v[3])));
+        const float ts = tm * s_hi;
+        if (ts > c) {
+            const float sc = ex2_approx(c - ts);
+            S2 = mul2(S2, pack2(sc, sc));
+            c = ts;
+        }
+        const unsigned long long nc2 = pack2(-c, -c);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const unsigned long long x2 = pack2(Elem<DT>::get(v[u], e), Elem<DT>::get(v[u], e + 1));
+                const unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
+                float a0, a1;
+                unpack2(a2, a0, a1);
+                S2 = add2(S2, pack2(ex2_approx(a0), ex2_approx(a1)));
+            }
+        }
+    }
+}
+
+// The buffer's logits become f * 2^(x s - c), in place, rounded once.
+template <typename DT>
+__device__ __forceinline__ void turn_pieces(uint4 *buf, int n, float s_hi, float s_lo, float c, float f) {
+    constexpr int N = Elem<DT>::N;
+    const unsigned long long hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo), nc2 = pack2(-c, -c), f2 = pack2(f, f);
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n; i += kDT) {
+        const uint4 v = buf[i];
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const unsigned long long x2 = pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1));
+            const unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
+            float a0, a1;
+            unpack2(a2, a0, a1);
+            unpack2(mul2(pack2(ex2_approx(a0), ex2_approx(a1)), f2), a0, a1);
+            if constexpr (N == 8) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(a0, a1);
+                w[e / 2] = *reinterpret_cast<const uint32_t *>(&b);
+            } else {
+                w[e] = __float_as_uint(a0);
+                w[e + 1] = __float_as_uint(a1);
+            }
+        }
+        buf[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// The buffer as pieces [a, b) of the gradient's row.  Ends with the stores sent; thread 0 waits for them (bulk_store_read_wait) before
+// the buffer is used again or the CTA ends.
+template <typename DT>
+__device__ __forceinline__ void store_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf) {
+    constexpr int N = Elem<DT>::N;
+    const bool same = (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % N) == p.h;
+    if (same) {
+        fence_async();
+        __syncthreads();
+        const int l = max(a, p.lo), u = min(b, p.hi);
+        if (threadIdx.x == 0 && u > l) {
+            bulk_store(grow + ((long long)l * N - p.h), buf + (size_t)(l - a) * N, (uint32_t)(u - l) * 16u);
+            bulk_store_commit();
+        }
+        edges<DT>(p, V, a, b, [&](int v, int place) {
+            if (v >= 0) grow[v] = buf[place];
+        });
+    } else {                                    // the gradient's rows start elsewhere within 16 bytes: element by element
+        __syncthreads();
+        const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
+        for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = buf[v + p.h - a * N];
+    }
+}
+
+// Zeros as the gradient of pieces [a, b).
+template <typename DT>
+__device__ void store_zeros(DT *grow, int v0, int v1) {
+    constexpr int N = Elem<DT>::N;
+    const int h = (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % N);
+    const int first = min(v1, (v0 + h + N - 1) / N * N - h), last = max(first, (v1 + h) / N * N - h);
+    for (int v = v0 + threadIdx.x; v < first; v += kDT) grow[v] = rounded<DT>(0.f);
+    for (int v = last + threadIdx.x; v < v1; v += kDT) grow[v] = rounded<DT>(0.f);
+    uint4 *g4 = reinterpret_cast<uint4 *>(grow + first);
+    for (int i = threadIdx.x; i < (last - first) / N; i += kDT) g4[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+__device__ __forceinline__ double max_over(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+
+template <typename DT, bool GRAD>
+__global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
+    constexpr int N = Elem<DT>::N;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ Shared sh;
+    DT *buf = reinterpret_cast<DT *>(ring);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = a.C, rank = C > 1 ? (int)cluster_rank() : 0;
+    const long long row = blockIdx.x / (unsigned)C;
+    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L);
+    const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
+    DT *g = GRAD ? reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl : nullptr;
+    const Pieces<DT> p(x, a.V);
+    const int p0 = (int)((long long)p.n * rank / C), p1 = (int)((long long)p.n * (rank + 1) / C);
+    const float w = a.weight ? a.weight[row] : 1.f;
+    float *state = a.state ? a.state + row * (a.K + 4) : nullptr;
+
+    if (w == 0.f) {                             // the whole cluster alike
+        if (GRAD) store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
+        if (rank == 0) {
+            if (tid == 0) {
+                a.loss[row] = 0.f;
+                if (a.accept) a.accept[row] = 0.f;
+                if (a.lse) a.lse[row] = -CUDART_INF_F;
+                if (state) { state[0] = -kRefFloor; state[1] = 0.f; state[2] = 0.f; state[3] = 0.f; }
+            }
+            if (state && tid < a.K) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+        }
+        return;
+    }
+    if (tid == 0) {
+        mbar_init(&sh.bar, 1);
+        mbar_init_fence();
+        sh.timed_out = 0;
+    }
+    __syncthreads();
+    if (C > 1) cluster_arrive();
+    const int chunks = (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
+    int q0 = p0, q1 = min(p1, p0 + a.buf_vecs);
+    uint32_t parity = 0;
+    send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+
+    // ---- the teacher's list, one slot a thread: while the copies are under way ----
+    int id = -1;
+    float t = -CUDART_INF_F;
+    if (tid < a.K) {
+        id = a.id[row * a.K + tid];
+        t = a.val[row * a.K + tid];
+        const int n = a.count ? a.count[row] : a.K;
+        if (tid >= n || id < 0 || id >= a.V) id = -1;
+    }
+    sh.id[tid] = id;
+    __syncthreads();
+    if (id >= 0) {                              // of equal ids the first slot counts
+        bool twice = false;
+        const int4 *ids = reinterpret_cast<const int4 *>(sh.id);
+        for (int j = 0; j < tid >> 2; ++j) {
+            const int4 o = ids[j];
+            twice |= o.x == id || o.y == id || o.z == id || o.w == id;
+        }
+        for (int j = tid & ~3; j < tid; ++j) twice |= sh.id[j] == id;
+        if (twice) id = -1;
+    }
+    const bool tail = a.tlse != nullptr;
+    double lp = -CUDART_INF, pk = 0.0;          // log p_k, p_k
+    if (tail) {
+        if (id >= 0) lp = (double)t * a.inv_t - (double)a.tlse[row];
+    } else {                                    // softmax over the K tokens
+        const double m0 = max_over(id >= 0 ? (double)t : -CUDART_INF);
+        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
+        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : m0;
+        __syncthreads();
+        double m = sh.red[0][0];
+        for (int i = 1; i < kWarps; ++i) {
+            const double o = sh.red[i][0];
+            if (m == m && !(o <= m)) m = o;     // a NaN stays
+        }
+        const double e = id >= 0 && m > -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
+        const double z0 = warp_sum(m != m ? m : e);
+        if (lane == 0) sh.red[warp][1] = z0;
+        __syncthreads();
+        double z = 0.0;
+        for (int i = 0; i < kWarps; ++i) z += sh.red[i][1];
+        if (id >= 0 && z != 0.0) lp = ((double)t - m) * a.inv_t - log(z);
+    }
+    if (id >= 0) pk = exp(lp);
+    const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
+    const bool mine = piece >= p0 && piece < p1;
+
+    // ---- the slice: the teacher's tokens taken out, the others summed ----
+    float xk = 0.f, c = kRefFloor;
+    unsigned long long S2 = pack2(0.f, 0.f);
+    for (int k = 0;;) {
+        take_copies(sh, parity);
+        parity ^= 1u;
+        __syncthreads();                        // the edges are in place too
+        if (piece >= q0 && piece < q1) {
+            const int at = p.h + id - q0 * N;
+            xk = elem_of<DT>(buf, at);
+            hide<DT>(buf, at);
+        }
+        __syncthreads();
+        sum_pieces<DT>(reinterpret_cast<const uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, c, S2);
+        if (++k >= chunks) break;
+        fence_async();
+        __syncthreads();
+        q0 = q1;
+        q1 = min(p1, q1 + a.buf_vecs);
+        send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+    }
+
+    // ---- what the CTA knows, to every CTA of the row ----
+    const double zs = (double)xk * a.scale;     // the token's exponent
+    {
+        float s0, s1;
+        unpack2(S2, s0, s1);
+        const float cw = warp_max(c);
+        const float aw = ex2_approx(c - cw);
+        const double Sw = warp_sum(aw == 0.f && s0 + s1 < CUDART_INF_F ? 0.0 : (double)(s0 + s1) * (double)aw);
+        const float zf = warp_max(mine && (float)zs > kRefFloor ? (float)zs : kRefFloor);
+        if (lane == 0) { sh.redc[warp] = cw; sh.redt[warp] = zf; sh.red[warp][0] = Sw; }
+    }
+    __syncthreads();
+    float ct = sh.redt[0];
+    for (int i = 1; i < kWarps; ++i) ct = fmaxf(ct, sh.redt[i]);
+    double S = 0.0;
+    float cb = kRefFloor;
+    if (warp == 0) {
+        const double Sw = lane < kWarps ? sh.red[lane][0] : 0.0;
+        const float cw = lane < kWarps ? sh.redc[lane] : kRefFloor;
+        cb = warp_max(cw);
+        S = warp_sum(Sw != 0.0 ? Sw * exp2((double)cw - (double)cb) : 0.0);
+    }
+    __syncthreads();                            // sh.red is free again
+    double E = 0.0, P = 0.0, H = 0.0;
+    if (warp * 32 < a.K) {                      // the first warps have the slots
+        E = warp_sum(mine ? exp2(zs - (double)ct) : 0.0);
+        P = warp_sum(pk);
+        H = warp_sum(mine && pk != 0.0 ? pk * (lp - (double)xk * a.inv_t) : 0.0);
+    }
+    if (lane == 0) { sh.red[warp][0] = E; sh.red[warp][1] = P; sh.red[warp][2] = H; }
+    __syncthreads();
+    if (C > 1) cluster_wait();                  // the other CTAs are there
+    if (warp == 0) {
+        E = P = H = 0.0;
+        for (int i = 0; i < kWarps; ++i) { E += sh.red[i][0]; P += sh.red[i][1]; H += sh.red[i][2]; }
+        if (C > 1) {
+            if (lane < C) {
+                const Part *to = &sh.part[rank];
+                put_remote(at_rank(&to->S, lane), (uint64_t)__double_as_longlong(S));
+                put_remote(at_rank(&to->E, lane), (uint64_t)__double_as_longlong(E));
+                put_remote(at_rank(&to->P, lane), (uint64_t)__double_as_longlong(P));
+                put_remote(at_rank(&to->H, lane), (uint64_t)__double_as_longlong(H));
+                put_remote(at_rank(&to->c, lane), cb);
+                put_remote(at_rank(&to->ct, lane), ct);
+            }
+        } else if (lane == 0) {
+            sh.part[0] = Part{S, E, P, H, cb, ct};
+        }
+        __syncwarp();
+    }
+    if (C > 1) { cluster_arrive(); cluster_wait(); }
+
+    // ---- the row ----
+    if (warp == 0) {
+        const bool there = lane < C;
+        const Part q = sh.part[there ? lane : 0];
+        const float cs = warp_max(there ? q.c : kRefFloor), cl = warp_max(there ? q.ct : kRefFloor);
+        S = warp_sum(there && q.S != 0.0 ? q.S * exp2((double)q.c - (double)cs) : 0.0);
+        E = warp_sum(there && q.E != 0.0 ? q.E * exp2((double)q.ct - (double)cl) : 0.0);
+        H = warp_sum(there ? q.H : 0.0);
+        P = q.P;                                // formed by every CTA from the whole list
+        if (lane == 0) {
+            const double c_all = fmax((double)cs, (double)cl);
+            const double to_all = exp2((double)cs - c_all);
+            const double all = (S != 0.0 ? S * to_all : 0.0) + (E != 0.0 ? E * exp2((double)cl - c_all) : 0.0);
+            const bool ok = all > 0.0 && all < CUDART_INF && c_all > (double)kRefFloor && c_all < CUDART_INF;
+            const double lse = ok ? kLn2 * (c_all + log2(all)) : CUDART_NAN;
+            double r = tail ? 1.0 - P : 0.0;
+            r = r < 0.0 ? 0.0 : r;              // NaN stays
+            const bool none = !tail && P == 0.0;
+            double loss = none ? 0.0 : H + P * lse;
+            if (r != 0.0) loss += r * (log(r) - (kLn2 * ((double)cs + log2(S)) - lse));
+            const double f = none || S == 0.0 ? 0.0 : (to_all / all - r / S) * a.inv_t;
+            const double s = S * to_all / all;
+            sh.found.c_all = c_all;
+            sh.found.inv_all = 1.0 / all;
+            sh.found.c = S != 0.0 ? cs : -kRefFloor;      // nothing to scale: every exponential is 0
+            sh.found.fw = (float)(f * (double)w);
+            sh.found.rest = (float)(r < s ? r : s);
+            sh.found.none = none;
+            const bool bad = !ok || !(P < CUDART_INF);
+            if (rank == 0) {
+                a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
+                if (a.lse) a.lse[row] = (float)lse;
+                if (state) { state[0] = sh.found.c; state[1] = (float)f; state[2] = 0.f; state[3] = 0.f; }
+            }
+            const uint32_t flags = (bad && rank == 0 ? DSP_ROW_NONFINITE_INPUT : 0u) | (sh.timed_out ? DSP_ROW_TIMEOUT : 0u);
+            if (a.status && flags) atomicOr(&a.status[b], flags);
+        }
+    }
+    __syncthreads();
+    const Found fd = sh.found;
+    float gk = 0.f;                             // the slot's gradient, with the row's weight
+    double acc = 0.0;
+    if (mine) {
+        const double qk = exp2(zs - fd.c_all) * fd.inv_all;
+        const double gu = fd.none ? 0.0 : (qk - pk) * a.inv_t;
+        gk = (float)(gu * (double)w);
+        acc = pk < qk ? pk : qk;
+        if (state) state[4 + tid] = (float)gu;
+    } else if (state && rank == 0 && tid < a.K && id < 0) {
+        reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+    }
+    if (a.accept) {
+        if (warp * 32 < a.K) acc = warp_sum(acc);
+        if (lane == 0) sh.red[warp][0] = acc;
+        __syncthreads();
+        if (tid == 0) {
+            acc = 0.0;
+            for (int i = 0; i < kWarps; ++i) acc += sh.red[i][0];
+            if (C > 1) put_remote(at_rank(&sh.accept[rank], 0), (float)acc);
+            else sh.accept[0] = (float)acc;
+        }
+        __syncwarp();
+    }
+    if (C > 1) cluster_arrive();
+    if constexpr (GRAD) {
+        for (int k = 0;;) {
+            // one chunk: it is in the buffer still, without the teacher's tokens; several: once more from the first on
+            if (chunks > 1) {
+                q0 = p0 + k * a.buf_vecs;
+                q1 = min(p1, q0 + a.buf_vecs);
+                if (tid == 0) bulk_store_read_wait();
+                fence_async();
+                __syncthreads();
+                send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+                take_copies(sh, parity);
+                parity ^= 1u;
+                __syncthreads();
+                if (piece >= q0 && piece < q1) hide<DT>(buf, p.h + id - q0 * N);
+                __syncthreads();
+            }
+            turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, fd.c, fd.fw);
+            __syncthreads();
+            if (piece >= q0 && piece < q1) buf[p.h + id - q0 * N] = rounded<DT>(gk);
+            store_pieces<DT>(g, p, a.V, q0, q1, buf);
+            if (++k >= chunks) break;
+        }
+        if (tid == 0) bulk_store_read_wait();
+    }
+    if (C > 1) cluster_wait();
+    if (rank == 0 && tid == 0 && a.accept) {
+        acc = (double)fd.rest;
+        for (int i = 0; i < C; ++i) acc += (double)sh.accept[i];
+        a.accept[row] = (float)acc;
+    }
+}
+
+// The gradient from what dsp_distill left of the row: c, f and the K elements.
+struct DistillGradArgs {
+    const void *x;
+    long long sb, sl;
+    int L, V, K, slices;
+    const int32_t *id;
+    const float *state, *factor;
+    float s_hi, s_lo;
+    void *g;
+    long long gsb, gsl;
+};
+constexpr int kGradVecs = 2048;                 // 32 KB of a row for a CTA
+
+template <typename DT>
+__global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs a) {
+    constexpr int N = Elem<DT>::N;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ CopyBar sh;
+    DT *buf = reinterpret_cast<DT *>(ring);
+    const int tid = threadIdx.x;
+    const long long row = blockIdx.x / (unsigned)a.slices;
+    const int slice = (int)(blockIdx.x - row * a.slices);
+    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L);
+    const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
+    DT *g = reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl;
+    const Pieces<DT> p(x, a.V);
+    const int p0 = (int)((long long)p.n * slice / a.slices), p1 = (int)((long long)p.n * (slice + 1) / a.slices);
+    const float w = a.factor[row];
+    if (w == 0.f) {
+        store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
+        return;
+    }
+    if (tid == 0) {
+        mbar_init(&sh.bar, 1);
+        mbar_init_fence();
+        sh.timed_out = 0;
+    }
+    __syncthreads();
+    send_copies<DT>(x, p, a.V, p0, p1, buf, sh);
+    const float *state = a.state + row * (a.K + 4);
+    const float c = state[0], f = state[1] * w;
+    int at = -1;
+    float gk = 0.f;
+    if (tid < a.K && __float_as_uint(state[4 + tid]) != kNoEntry) {
+        const int id = a.id[row * a.K + tid];
+        const int piece = (p.h + id) / N;
+        if (id >= 0 && id < a.V && piece >= p0 && piece < p1) {
+            at = p.h + id - p0 * N;
+            gk = state[4 + tid] * w;
+        }
+    }
+    take_copies(sh, 0u);
+    __syncthreads();
+    turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), p1 - p0, a.s_hi, a.s_lo, c, sh.timed_out ? CUDART_NAN_F : f);
+    __syncthreads();
+    if (at >= 0) buf[at] = rounded<DT>(gk);
+    store_pieces<DT>(g, p, a.V, p0, p1, buf);
+    if (tid == 0) bulk_store_read_wait();
+}
+
+inline int pieces_at_most(int V, int N) { return (int)(((long long)V + 2 * N - 2) / N); }
+
+constexpr int kMaxBufVecs = 216 * 1024 / 16;
+
+template <typename DT, bool GRAD>
+int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
+    constexpr int N = Elem<DT>::N;
+    const int n = pieces_at_most(a.V, N);
+    int C = 1;
+    while (C < kMaxCluster && (long long)n > (long long)C * kSliceVecs) C *= 2;
+    while (C < kMaxCluster && rows * C < device_sm_count() && n >= 2 * C * 256) C *= 2;
+    a.C = C;
+    const int per = (n + C - 1) / C;
+    a.buf_vecs = per < kMaxBufVecs ? per : kMaxBufVecs;
+    if (rows * C > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
+    static std::atomic<unsigned long long> smem_done{0};
+    DSP_CUDA_TRY(allow_shared(distill_kernel<DT, GRAD>, kMaxBufVecs * 16, smem_done));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * C));
+    cfg.blockDim = dim3(kDT);
+    cfg.dynamicSmemBytes = (size_t)a.buf_vecs * 16;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = C > 1 ? 1 : 0;
+    DSP_CUDA_TRY(cudaLaunchKernelEx(&cfg, distill_kernel<DT, GRAD>, (const DistillArgs)a));
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
+template <typename DT>
+int32_t launch_distill_grad(DistillGradArgs &a, long long rows, cudaStream_t st) {
+    const int n = pieces_at_most(a.V, Elem<DT>::N);
+    a.slices = (n + kGradVecs - 1) / kGradVecs;
+    if (rows * a.slices > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
+    const int per = (n + a.slices - 1) / a.slices;
+    distill_grad_kernel<DT><<<(unsigned)(rows * a.slices), kDT, (size_t)per * 16, st>>>(a);
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
+int32_t check_rows(int32_t dtype, int32_t B, int32_t L, int32_t V, int32_t K, float temperature) {
+    if (B < 0 || L < 1 || V < 1 || K < 1 || !(temperature >= 1e-3f && temperature <= 1e3f)) return DSP_ERR_INVALID_ARG;
+    if ((dtype != DSP_F32 && dtype != DSP_BF16) || K > DSP_MAX_TEACHER || V > (1 << 30) || (long long)B * L > (1 << 24))
+        return DSP_ERR_UNSUPPORTED;
+    return DSP_OK;
+}
+bool rows_fit(const void *p, size_t es, int64_t sb, int64_t sl, int32_t B, int32_t L, int32_t V) {
+    if ((reinterpret_cast<uintptr_t>(p) & (es - 1)) != 0 || sl < V || sb < 0) return false;
+    return B == 1 || sb >= (int64_t)(L - 1) * sl + V;
+}
+
+}  // namespace
+}  // namespace dsp
+
+extern "C" int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                               int64_t stride_b, int64_t stride_l, const int32_t *teacher_id, const float *teacher_logit,
+                               const float *teacher_lse, const int32_t *teacher_count, int32_t K, float temperature,
+                               const float *weight, float *loss, float *accept, float *lse, float *state,
+                               void *grad, int64_t grad_stride_b, int64_t grad_stride_l,
+                               uint32_t *row_status, dsp_stream_t stream) {
+    using namespace dsp;
+    const int32_t rc = check_rows(dtype, B, L, V, K, temperature);
+    if (rc != DSP_OK) return rc;
+    if (B == 0) return DSP_OK;
+    const size_t es = dtype == DSP_BF16 ? 2 : 4;
+    if (!student_logits || !teacher_id || !teacher_logit || !loss) return DSP_ERR_INVALID_ARG;
+    if (!rows_fit(student_logits, es, stride_b, stride_l, B, L, V)) return DSP_ERR_INVALID_ARG;
+    if (grad && !rows_fit(grad, es, grad_stride_b, grad_stride_l, B, L, V)) return DSP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(state) & 15) != 0) return DSP_ERR_INVALID_ARG;
+    DistillArgs a = {};
+    a.x = student_logits; a.sb = stride_b; a.sl = stride_l;
+    a.L = L; a.V = V; a.K = K;
+    a.id = teacher_id; a.count = teacher_count; a.val = teacher_logit; a.tlse = teacher_lse; a.weight = weight;
+    a.inv_t = 1.0 / (double)temperature;
+    a.scale = a.inv_t / kLn2;
+    split_scale(a.scale, a.s_hi, a.s_lo);
+    a.loss = loss; a.accept = accept; a.lse = lse; a.state = state;
+    a.g = grad; a.gsb = grad_stride_b; a.gsl = grad_stride_l;
+    a.status = row_status;
+    const long long rows = (long long)B * L;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (dtype == DSP_BF16)
+        return grad ? launch_distill<__nv_bfloat16, true>(a, rows, st) : launch_distill<__nv_bfloat16, false>(a, rows, st);
+    return grad ? launch_distill<float, true>(a, rows, st) : launch_distill<float, false>(a, rows, st);
+}
+
+extern "C" int32_t dsp_distill_grad(const void *student_logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                                    int64_t stride_b, int64_t stride_l, const int32_t *teacher_id, int32_t K,
+                                    const float *state, float temperature, const float *row_grad,
+                                    void *grad, int64_t grad_stride_b, int64_t grad_stride_l, dsp_stream_t stream) {
+    using namespace dsp;
+    const int32_t rc = check_rows(dtype, B, L, V, K, temperature);
+    if (rc != DSP_OK) return rc;
+    if (B == 0) return DSP_OK;
+    const size_t es = dtype == DSP_BF16 ? 2 : 4;
+    if (!student_logits || !teacher_id || !state || !row_grad || !grad) return DSP_ERR_INVALID_ARG;
+    if (!rows_fit(student_logits, es, stride_b, stride_l, B, L, V) || !rows_fit(grad, es, grad_stride_b, grad_stride_l, B, L, V))
+        return DSP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(state) & 15) != 0) return DSP_ERR_INVALID_ARG;
+    DistillGradArgs a = {};
+    a.x = student_logits; a.sb = stride_b; a.sl = stride_l;
+    a.L = L; a.V = V; a.K = K;
+    a.id = teacher_id; a.state = state; a.factor = row_grad;
+    split_scale(1.0 / (double)temperature / kLn2, a.s_hi, a.s_lo);
+    a.g = grad; a.gsb = grad_stride_b; a.gsl = grad_stride_l;
+    const long long rows = (long long)B * L;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return dtype == DSP_BF16 ? launch_distill_grad<__nv_bfloat16>(a, rows, st) : launch_distill_grad<float>(a, rows, st);
+}

@@ -276,10 +276,10 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
 // Whatever an earlier kernel of the launch chain prepared (zeroed tickets and status words, see
 // launch_prepare) is first touched after the stream: the kernel may start before that kernel
 // has ended (programmatic launch) and waits for it here.
-template <typename DT>
+template <typename DT, typename Pass>
 __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums, long long row, int slice,
                            int nslices, int ntiles_row, int nstages, const RowScratch &ws, unsigned *status_word,
-                           StreamBars &bars, unsigned char *ring, RowResult &res) {
+                           StreamBars &bars, unsigned char *ring, RowResult &res, Pass &pass) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int s0, s1;
     slice_range<DT>(slice, nslices, ntiles_row, V, s0, s1);
@@ -287,8 +287,8 @@ __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums,
     ColTop top;
     ColSums cs;
     cs.c = kRefFloor; cs.S = 0.f; cs.T = 0.f;
-    if (sums) stream_slice<DT, true>(rowp, s0, s1, nstages, bars, ring, top, cs);
-    else      stream_slice<DT, false>(rowp, s0, s1, nstages, bars, ring, top, cs);
+    if (sums) stream_slice<DT, true>(rowp, s0, s1, nstages, bars, ring, top, cs, pass);
+    else      stream_slice<DT, false>(rowp, s0, s1, nstages, bars, ring, top, cs, pass);
 
     // masked (-inf) logits leave 0 * -inf in T only: such columns are summed once more, clamped
     const bool poisoned = sums && cs.T != cs.T && cs.S == cs.S && cs.S < CUDART_INF_F;
@@ -296,6 +296,7 @@ __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums,
         if (poisoned) redo_column_sums<DT>(rowp, s0, s1, tid, cs);
     }
     grid_dependency_wait();
+    if constexpr (Pass::kCount) pass.hand_in();
     if (tid == 0 && bars.timed_out) atomicOr(status_word, (unsigned)DSP_ROW_TIMEOUT);
     if (sums) {
         const WarpPartial p = warp_partial(cs);
@@ -320,6 +321,14 @@ __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums,
         stash[tid] = mine;
     }
     return row_finish<DT>(rowp, V, K, sums, row, nslices, ntiles_row, ws, nslices > 1 ? nullptr : bars.wp, ring, res);
+}
+
+template <typename DT>
+__device__ __forceinline__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums, long long row, int slice,
+                                           int nslices, int ntiles_row, int nstages, const RowScratch &ws, unsigned *status_word,
+                                           StreamBars &bars, unsigned char *ring, RowResult &res) {
+    PlainPass nothing;
+    return row_engine<DT, PlainPass>(rowp, V, K, sums, row, slice, nslices, ntiles_row, nstages, ws, status_word, bars, ring, res, nothing);
 }
 
 // Global scratch of a launch over `nrows` rows cut into `nslices` slices each.

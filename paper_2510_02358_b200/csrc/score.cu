@@ -1,0 +1,379 @@
+// dsp_token_logprobs: log-probabilities of given tokens, entropy, rank and the best alternatives of every row.
+//
+// One pass over the logits by the row engine (stream_core.cuh, row_engine.cuh): slices stream through shared memory, the CTA that is
+// through with a row last finishes it.  Its own parts are the sums at a temperature (TokenPass::sums), the rank of the first token
+// (TokenPass::count) and rows that start or end inside a 16-byte piece: the whole pieces between are streamed, and what lies outside of
+// them (fewer than two pieces, one element a lane) joins the result when the row is finished, so an odd vocabulary costs nothing.
+//
+// The rank needs one comparison per logit and no index: a token that precedes token t in the vocabulary comes before it with an equal
+// logit, a later one does not, so pieces before t's count what exceeds the next smaller number and the others what exceeds t's logit.
+#include "dsp_internal.h"
+#include "row_engine.cuh"
+
+namespace dsp {
+namespace {
+
+struct ScoreArgs {
+    const void *logits;
+    int B, L, V;
+    long long stride_b, stride_l;
+    const int32_t *row_len, *tokens;
+    int G, K;
+    double scale, inv_t;      // log2(e) / T, 1 / T
+    float s_hi, s_lo;         // scale = s_hi + s_lo, s_lo > 0: both products of -inf are then -inf
+    float *logp;
+    int32_t *rank, *top_id;
+    float *top_logit, *top_logp, *lse, *entropy;
+    uint32_t *row_status;
+    int inner;                // elements of a row that are streamed: a multiple of a piece's
+    int nslices, ntiles_row, nstages;
+    RowScratch rs;
+    unsigned *rank_acc;       // [rows] zeroed per call
+};
+
+// The number just below x (NaN below -inf: everything exceeds it).
+__device__ __forceinline__ uint32_t below_bits(float x) {
+    const uint32_t b = __float_as_uint(x);
+    if (x == 0.f) return 0x80000001u;
+    if (b == 0xFF800000u) return 0x7FFFFFFFu;
+    return (b & 0x80000000u) ? b + 1u : b - 1u;
+}
+__device__ __forceinline__ uint32_t below_bits_bf16(float x) {
+    const uint32_t b = __float_as_uint(x) >> 16;
+    if (x == 0.f) return 0x8001u;
+    if (b == 0xFF80u) return 0x7FFFu;
+    return (b & 0x8000u) ? b + 1u : b - 1u;
+}
+
+template <typename DT>
+struct TokenPass {
+    static constexpr bool kOwnSums = true, kCount = true;
+    const DT *row;            // the whole row
+    const int32_t *token;     // the first token of the row, or null
+    unsigned *acc;
+    float s_hi, s_lo;
+    int V, head, inner;
+    bool masked = false;      // -inf logits seen: exponents are clamped from there on
+    // rank
+    int tok = -1, vec = 0;    // token, and the streamed piece it lies in (pieces: beyond, 0: before)
+    float xt = 0.f;
+    uint32_t ge = 0u, gt = 0u;
+    int n = 0;
+
+    __device__ __forceinline__ void begin() {
+        constexpr int N = Elem<DT>::N;
+        tok = token ? *token : -1;
+        if (tok < 0 || tok >= V) { tok = -1; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
+        xt = Elem<DT>::load1(row + tok);
+        vec = tok < head ? 0 : min((tok - head) / N, inner / N);
+        if constexpr (N == 8) {
+            gt = (__float_as_uint(xt) >> 16) * 0x10001u;
+            ge = below_bits_bf16(xt) * 0x10001u;
+        } else {
+            gt = __float_as_uint(xt);
+            ge = below_bits(xt);
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void count(const uint4 (&v)[kVpt], int base) {
+        constexpr int N = Elem<DT>::N;
+        const int v0 = base / N + (int)threadIdx.x;
+        if constexpr (N == 8) {
+            __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f);          // at most 4 kVpt a half: exact
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j) {
+                const uint32_t w = v0 + j * kThreads < vec ? ge : gt;
+                const __nv_bfloat162 lim = *reinterpret_cast<const __nv_bfloat162 *>(&w);
+                const uint32_t q[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum = __hadd2(sum, __hgtu2(*reinterpret_cast<const __nv_bfloat162 *>(&q[i]), lim));
+            }
+            n += (int)(__low2float(sum) + __high2float(sum));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j) {
+                const float lim = __uint_as_float(v0 + j * kThreads < vec ? ge : gt);
+#pragma unroll
+                for (int e = 0; e < N; ++e) n += Elem<DT>::get(v[j], e) <= lim ? 0 : 1;
+            }
+        }
+    }
+    // The exponents x s - c of one tile into S = sum 2^a and T = sum 2^a a.  A masked logit leaves 0 * -inf in T: the tile is summed
+    // again with its exponents clamped, and later tiles at once.
+    template <typename T, bool RAGGED>
+    __device__ __forceinline__ void sums(const float (&x)[kVpt][Elem<DT>::N], int nvec, int tid, float tm, float &c,
+                                         unsigned long long &S2, unsigned long long &T2) {
+        const float ts = tm * s_hi;
+        if (ts > c) {
+            const float d = c - ts;
+            const float sc = ex2_approx(d);
+            const unsigned long long sc2 = pack2(sc, sc);
+            T2 = mul2(fma2(S2, pack2(d, d), T2), sc2);
+            S2 = mul2(S2, sc2);
+            c = ts;
+        }
+        const unsigned long long S0 = S2, T0 = T2;
+        if (!masked) {
+            add<RAGGED, false>(x, nvec, tid, c, S2, T2);
+            float t0, t1;
+            unpack2(T2, t0, t1);
+            if (t0 + t1 == t0 + t1) return;
+            masked = true;
+        }
+        S2 = S0;
+        T2 = T0;
+        add<RAGGED, true>(x, nvec, tid, c, S2, T2);
+    }
+    template <bool RAGGED, bool CLAMP>
+    __device__ __forceinline__ void add(const float (&x)[kVpt][Elem<DT>::N], int nvec, int tid, float c, unsigned long long &S2,
+                                        unsigned long long &T2) {
+        const unsigned long long nc2 = pack2(-c, -c), hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo);
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) {
+            if (RAGGED && j * kThreads + tid >= nvec) continue;
+#pragma unroll
+            for (int e = 0; e < Elem<DT>::N; e += 2) {
+                const unsigned long long x2 = pack2(x[j][e], x[j][e + 1]);
+                unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
+                float a0, a1;
+                unpack2(a2, a0, a1);
+                if (CLAMP) {
+                    a0 = fmaxf(a0, -1000.f);
+                    a1 = fmaxf(a1, -1000.f);
+                    a2 = pack2(a0, a1);
+                }
+                const unsigned long long e2 = pack2(ex2_approx(a0), ex2_approx(a1));
+                S2 = add2(S2, e2);
+                T2 = fma2(e2, a2, T2);
+            }
+        }
+    }
+    // The slice's count, after the preparation has ended and before the row's ticket.
+    __device__ __forceinline__ void hand_in() {
+        if (!token) return;
+        const int all = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
+        if ((threadIdx.x & 31) == 0 && all) atomicAdd(acc, (unsigned)all);
+    }
+};
+
+// A row that is not read.
+__device__ void score_nothing(const ScoreArgs &a, long long row, int lane) {
+    for (int i = lane; i < a.G; i += 32) a.logp[row * a.G + i] = -CUDART_INF_F;
+    if (lane < a.K) {
+        a.top_id[row * a.K + lane] = -1;
+        a.top_logit[row * a.K + lane] = -CUDART_INF_F;
+        a.top_logp[row * a.K + lane] = -CUDART_INF_F;
+    }
+    if (lane == 0) {
+        if (a.rank) a.rank[row] = -1;
+        a.lse[row] = -CUDART_INF_F;
+        if (a.entropy) a.entropy[row] = 0.f;
+    }
+}
+
+// The finish of a row by one warp: the elements outside of the streamed pieces join, and everything is written.
+template <typename DT>
+__device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *rowp, int head, const TokenPass<DT> &pass, RowResult r,
+                          int lane) {
+    constexpr int N = Elem<DT>::N;
+    // one element a lane: before the streamed pieces, then behind them
+    const int extra = a.V - a.inner;
+    const int v = lane < head ? lane : a.inner + lane;
+    const float x = lane < extra ? Elem<DT>::load1(rowp + v) : -CUDART_INF_F;
+    bool bad = __any_sync(0xFFFFFFFFu, !(x < CUDART_INF_F)) || r.nonfinite;
+    unsigned long long key = lane < a.K && r.key ? r.key - (unsigned)head : 0ull;      // ids count from the streamed part
+    double c = r.c, S = r.S, T = r.T;
+    if (extra > 0) {
+        key = merge_top32(key, sort32_desc(x > -CUDART_INF_F ? make_key(x, v) : 0ull, lane), lane);
+        const double e = (double)x * a.scale;
+        const float cm = fmaxf(S != 0.0 ? r.c : kRefFloor, warp_max((float)e > kRefFloor ? (float)e : kRefFloor));
+        const double d = c - (double)cm, w = S != 0.0 ? exp2(d) : 0.0;
+        const double p = x > -CUDART_INF_F ? exp2(e - (double)cm) : 0.0;
+        const double S1 = warp_sum(p), T1 = warp_sum(p != 0.0 ? p * (e - (double)cm) : 0.0);
+        T = (S != 0.0 ? (T + S * d) * w : 0.0) + T1;
+        S = S * w + S1;
+        c = cm;
+    }
+    bad |= !(S > 0.0) || !(S < CUDART_INF) || !(T == T) || !(c > (double)kRefFloor) || !(c < CUDART_INF);
+    const double log_s = log2(S);
+    const double lse = bad ? CUDART_NAN : kLn2 * (c + log_s);
+    for (int i = lane; i < a.G; i += 32) {
+        const int t = a.tokens[row * a.G + i];
+        const bool in = t >= 0 && t < a.V;
+        a.logp[row * a.G + i] = in ? (float)((double)Elem<DT>::load1(rowp + t) * a.inv_t - lse) : -CUDART_INF_F;
+    }
+    if (lane < a.K) {
+        const bool some = key != 0ull;
+        const float xv = some ? key_value(key) : -CUDART_INF_F;
+        a.top_id[row * a.K + lane] = some ? key_id(key) : -1;
+        a.top_logit[row * a.K + lane] = xv;
+        a.top_logp[row * a.K + lane] = some ? (float)((double)xv * a.inv_t - lse) : -CUDART_INF_F;
+    }
+    if (a.rank) {
+        int rank = -1;
+        if (pass.tok >= 0) {
+            // before the token: of the outer elements, and of its own piece (counted without equals)
+            int n = lane < extra && (x > pass.xt || (x == pass.xt && v < pass.tok)) ? 1 : 0;
+            const int u = head + pass.vec * N + lane;
+            if (pass.tok >= head && pass.tok < head + a.inner && lane < N && u < pass.tok && Elem<DT>::load1(rowp + u) == pass.xt) ++n;
+            rank = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
+            if (lane == 0) rank += (int)atomicAdd(pass.acc, 0u);
+        }
+        if (lane == 0) a.rank[row] = rank;
+    }
+    if (lane == 0) {
+        a.lse[row] = (float)lse;
+        if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : (float)(kLn2 * (log_s - T / S));
+        if (bad) atomicOr(&a.row_status[b], DSP_ROW_NONFINITE_INPUT);
+    }
+}
+
+template <typename DT>
+__global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
+    constexpr int N = Elem<DT>::N;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ StreamBars bars;
+    const long long row = blockIdx.x / (unsigned)a.nslices;
+    const int slice = (int)(blockIdx.x - row * a.nslices);
+    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L), lane = threadIdx.x & 31;
+    if (a.row_len && l >= a.row_len[b]) {                // whole CTA alike
+        if (slice == 0 && threadIdx.x < 32) score_nothing(a, row, lane);
+        return;
+    }
+    const DT *rowp = reinterpret_cast<const DT *>(a.logits) + b * a.stride_b + l * a.stride_l;
+    const int head = a.inner == a.V ? 0 : (int)((N - (reinterpret_cast<uintptr_t>(rowp) / sizeof(DT)) % N) % N);
+    TokenPass<DT> pass;
+    pass.row = rowp;
+    pass.token = a.rank ? a.tokens + row * a.G : nullptr;
+    pass.acc = a.rank_acc + row;
+    pass.s_hi = a.s_hi; pass.s_lo = a.s_lo;
+    pass.V = a.V; pass.head = a.inner ? head : 0; pass.inner = a.inner;
+    RowResult r;
+    if (a.inner) {
+        stream_begin(bars, a.nstages);
+        if (!row_engine<DT>(rowp + head, a.inner, a.K > 0 ? a.K : 1, true, row, slice, a.nslices, a.ntiles_row, a.nstages, a.rs,
+                            &a.row_status[b], bars, ring, r, pass))
+            return;
+    } else {                                             // a row shorter than two pieces: one element a lane
+        if (threadIdx.x >= 32) return;
+        pass.begin();
+        grid_dependency_wait();
+        r.key = 0ull; r.c = kRefFloor; r.S = 0.0; r.T = 0.0; r.nonfinite = false;
+    }
+    score_row<DT>(a, row, b, rowp, pass.head, pass, r, lane);
+}
+
+struct ScoreWs {
+    size_t off_ticket, off_rank, zero_bytes;
+    RowScratchLayout rs;
+};
+ScoreWs score_ws_layout(long long rows, int nslices) {
+    ScoreWs w;
+    size_t o = 0;
+    w.off_ticket = o; o += align_up((size_t)rows * 4, 256);
+    w.off_rank = o;   o += align_up((size_t)rows * 4, 256);
+    w.zero_bytes = o;
+    w.rs = row_scratch_layout(o, rows, nslices);
+    return w;
+}
+
+// Elements of a row that are streamed whatever its start: all of it where every row starts on 16 bytes, else the pieces that lie inside
+// it at any start.  Slices are planned for rows that do not start on 16 bytes too, so that the workspace's size does not go by the address.
+template <typename DT>
+int inner_elems(const void *base, int V, long long stride_b, long long stride_l) {
+    constexpr int N = Elem<DT>::N;
+    if (base && stream_layout_ok<DT>(base, V, stride_b, stride_l)) return V;
+    return V < 2 * N ? 0 : (V - (N - 1)) / N * N;
+}
+template <typename DT>
+SlicePlan score_plan(long long rows, int inner) {
+    return plan_slices<DT>(rows, inner, slice_target_ctas());
+}
+
+template <typename DT>
+int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
+    const long long rows = (long long)a.B * a.L;
+    a.inner = inner_elems<DT>(a.logits, a.V, a.stride_b, a.stride_l);
+    const SlicePlan plan = score_plan<DT>(rows, a.inner);
+    a.nslices = plan.nslices;
+    a.ntiles_row = (a.inner + tile_elems<DT>() - 1) / tile_elems<DT>();
+    const ScoreWs w = score_ws_layout(rows, a.nslices);
+    if (workspace_bytes < w.rs.end) return DSP_ERR_WORKSPACE;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    a.rs.row_ticket = reinterpret_cast<unsigned *>(ws + w.off_ticket);
+    a.rs.cols = reinterpret_cast<uint2 *>(ws + w.rs.off_cols);
+    a.rs.wpart = reinterpret_cast<WarpPartial *>(ws + w.rs.off_wpart);
+    a.rank_acc = reinterpret_cast<unsigned *>(ws + w.off_rank);
+    const long long nblocks = rows * a.nslices;
+    if (nblocks > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
+    PrepareArgs prep = PrepareArgs();                    // tickets, counts and status words start at zero
+    prep.zero_a = reinterpret_cast<uint32_t *>(ws); prep.n_a = (long long)(w.zero_bytes / 4);
+    prep.zero_b = a.row_status; prep.n_b = a.B;
+    DSP_CUDA_TRY(launch_prepare(prep, st));
+    static RingSmemDone smem_done;                       // one per element type
+    DSP_CUDA_TRY(allow_ring_smem(score_kernel<DT>, smem_done));
+    a.nstages = ring_stages(nblocks);
+    DSP_CUDA_TRY(launch_dependent(score_kernel<DT>, (unsigned)nblocks, kThreads, (size_t)a.nstages * kTileBytes, st, a, true));
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
+template <typename DT>
+size_t score_ws_bytes(int B, int L, int V) {
+    const long long rows = (long long)B * L;
+    const size_t whole = score_ws_layout(rows, score_plan<DT>(rows, V).nslices).rs.end;
+    const size_t part = score_ws_layout(rows, score_plan<DT>(rows, inner_elems<DT>(nullptr, V, 0, 0)).nslices).rs.end;
+    return whole > part ? whole : part;
+}
+
+int32_t check_score(int32_t B, int32_t L, int32_t V, int32_t dtype) {
+    if (B < 0 || L < 1 || V < 1) return DSP_ERR_INVALID_ARG;
+    if ((dtype != DSP_F32 && dtype != DSP_BF16) || V > (1 << 30) || (long long)B * L > (1 << 24)) return DSP_ERR_UNSUPPORTED;
+    return DSP_OK;
+}
+
+}  // namespace
+}  // namespace dsp
+
+extern "C" int32_t dsp_token_logprobs_workspace_bytes(int32_t B, int32_t L, int32_t V, int32_t dtype, size_t *bytes) {
+    using namespace dsp;
+    if (!bytes) return DSP_ERR_INVALID_ARG;
+    const int32_t rc = check_score(B, L, V, dtype);
+    if (rc != DSP_OK) return rc;
+    const int Bq = B > 0 ? B : 1;
+    *bytes = dtype == DSP_BF16 ? score_ws_bytes<__nv_bfloat16>(Bq, L, V) : score_ws_bytes<float>(Bq, L, V);
+    return DSP_OK;
+}
+
+extern "C" int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t L, int32_t V,
+                                      int64_t stride_b, int64_t stride_l, const int32_t *row_len,
+                                      const int32_t *tokens, int32_t G, float temperature, int32_t K,
+                                      float *logp, int32_t *rank, int32_t *top_id, float *top_logit, float *top_logp,
+                                      float *lse, float *entropy, uint32_t *row_status,
+                                      void *workspace, size_t workspace_bytes, dsp_stream_t stream) {
+    using namespace dsp;
+    const int32_t rc = check_score(B, L, V, dtype);
+    if (rc != DSP_OK) return rc;
+    if (G < 0 || K < 0 || !(temperature >= 1e-3f && temperature <= 1e3f)) return DSP_ERR_INVALID_ARG;
+    if (K > DSP_MAX_K || G > DSP_MAX_SCORED) return DSP_ERR_UNSUPPORTED;
+    if (B == 0) return DSP_OK;
+    if (!logits || !lse || !row_status || !workspace) return DSP_ERR_INVALID_ARG;
+    if ((G > 0 && (!tokens || !logp)) || (rank && G < 1) || (K > 0 && (!top_id || !top_logit || !top_logp))) return DSP_ERR_INVALID_ARG;
+    if (stride_l < V || stride_b < 0 || (B > 1 && stride_b < (int64_t)(L - 1) * stride_l + V)) return DSP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return DSP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(logits) & (dtype == DSP_BF16 ? 1 : 3)) != 0) return DSP_ERR_INVALID_ARG;
+    ScoreArgs a = {};
+    a.logits = logits;
+    a.B = B; a.L = L; a.V = V;
+    a.stride_b = stride_b; a.stride_l = stride_l;
+    a.row_len = row_len; a.tokens = tokens;
+    a.G = G; a.K = K;
+    a.inv_t = 1.0 / (double)temperature;
+    a.scale = a.inv_t / kLn2;
+    split_scale(a.scale, a.s_hi, a.s_lo);
+    a.logp = logp; a.rank = rank; a.top_id = top_id; a.top_logit = top_logit; a.top_logp = top_logp;
+    a.lse = lse; a.entropy = entropy; a.row_status = row_status;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return dtype == DSP_BF16 ? launch_score<__nv_bfloat16>(a, workspace, workspace_bytes, st)
+                             : launch_score<float>(a, workspace, workspace_bytes, st);
+}

@@ -167,11 +167,18 @@ struct ColSums {    // S = sum 2^(x*kLog2e - c), T = sum 2^(x*kLog2e - c) * (x*k
     float c, S, T;
 };
 
+// What a kernel may add to the pass over its rows (score.cu does): nothing.
+struct PlainPass {
+    static constexpr bool kOwnSums = false;       // sums() instead of the loop below
+    static constexpr bool kCount = false;         // count() sees every tile
+    __device__ __forceinline__ void begin() {}    // the first copies are under way
+};
+
 // One tile from shared memory into the thread's running values.  nvec: 16-byte vectors of the
 // tile that exist (RAGGED: fewer than a whole tile; the missing ones take no part in anything).
-template <typename DT, bool SUMS, bool RAGGED>
+template <typename DT, bool SUMS, bool RAGGED, typename Pass>
 __device__ __forceinline__ void scan_tile(const uint4 *__restrict__ sp, int nvec, int t, int tid, ColTop &top,
-                                          float &c, unsigned long long &S2, unsigned long long &T2) {
+                                          float &c, unsigned long long &S2, unsigned long long &T2, Pass &pass, int base) {
     constexpr int N = Elem<DT>::N;
     uint4 v[kVpt];
     if constexpr (!RAGGED) {
@@ -212,7 +219,10 @@ __device__ __forceinline__ void scan_tile(const uint4 *__restrict__ sp, int nvec
     top.rm1 = gt ? tm : top.rm1;
     top.seen = max2_nan(top.seen, tm);
 
-    if constexpr (SUMS) {
+    if constexpr (Pass::kCount) pass.template count<DT>(v, base);
+    if constexpr (Pass::kOwnSums) {
+        pass.template sums<DT, RAGGED>(x, nvec, tid, tm, c, S2, T2);
+    } else if constexpr (SUMS) {
         const float ts = tm * kLog2e;                 // the reference exponent bounds every logit seen
         if (ts > c) {                                  // both halves move to the new reference exponent
             const float d = c - ts;
@@ -272,9 +282,9 @@ __device__ void redo_column_sums(const DT *__restrict__ row, int s0, int s1, int
 // Streams [s0, s1) of `row` through the ring (all kThreads threads of the CTA; `nstages` stages of
 // kTileBytes in `ring`).  On return `top` holds the thread's column record and, with SUMS, `cs`
 // its sums (c = kRefFloor, S = 0 if the thread saw no finite logit).
-template <typename DT, bool SUMS>
+template <typename DT, bool SUMS, typename Pass>
 __device__ void stream_slice(const DT *__restrict__ row, int s0, int s1, int nstages, StreamBars &bars,
-                             unsigned char *ring, ColTop &top, ColSums &cs) {
+                             unsigned char *ring, ColTop &top, ColSums &cs, Pass &pass) {
     constexpr int VT = kTileBytes / 16;
     static_assert(VT == kThreads * kVpt && tile_elems<DT>() * (int)sizeof(DT) == kTileBytes, "tile geometry");
     const int tid = threadIdx.x, lane = tid & 31;
@@ -292,6 +302,7 @@ __device__ void stream_slice(const DT *__restrict__ row, int s0, int s1, int nst
     if (tid == 0) {
         for (int tt = 0; tt < min(nstages, ntiles); ++tt) issue_tile(src, nbytes, tt, tt, ring, bars);
     }
+    pass.begin();
     int s = 0;                                       // stage of tile t: t % nstages
     uint32_t ph = 0u;                                // phase parity of tile t in its stage: (t / nstages) & 1
     for (int t = 0; t < ntiles; ++t) {
@@ -304,8 +315,9 @@ __device__ void stream_slice(const DT *__restrict__ row, int s0, int s1, int nst
         if (!mbar_wait(&bars.full[s], ph, abort)) bars.timed_out = 1;
         const int nvec = min(kTileBytes, nbytes - t * kTileBytes) >> 4;
         const uint4 *sp = reinterpret_cast<const uint4 *>(ring + (size_t)s * kTileBytes);
-        if (nvec == VT) scan_tile<DT, SUMS, false>(sp, nvec, t, tid, top, c, S2, T2);
-        else            scan_tile<DT, SUMS, true>(sp, nvec, t, tid, top, c, S2, T2);
+        const int base = s0 + t * tile_elems<DT>();
+        if (nvec == VT) scan_tile<DT, SUMS, false>(sp, nvec, t, tid, top, c, S2, T2, pass, base);
+        else            scan_tile<DT, SUMS, true>(sp, nvec, t, tid, top, c, S2, T2, pass, base);
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.empty[s]);   // the stage has been read: release it
         if (++s == nstages) { s = 0; ph ^= 1u; }

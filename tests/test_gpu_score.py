@@ -1,0 +1,160 @@
+"""dsp_token_logprobs against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import after_reference as ref
+from paper_2510_02358_b200 import binding as dsp
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def rows(B, L, V, dtype, seed, masked=0.0, offset=0, pitch=0):
+    """Logits [B, L, V] with a few likely tokens; `offset` elements into a buffer, rows `pitch` elements longer than V apart."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = 2.0 * torch.randn(B, L, V, generator=g, device="cuda")
+    x.scatter_add_(2, torch.randint(0, V, (B, L, 4), generator=g, device="cuda"), 5 + 3 * torch.rand(B, L, 4, generator=g, device="cuda"))
+    if masked:
+        x.masked_fill_(torch.rand(B, L, V, generator=g, device="cuda") < masked, -math.inf)
+        x[..., V // 2] = 1.0                                              # one logit stays
+    buf = torch.empty(B * L * (V + pitch) + offset, dtype=dtype, device="cuda")
+    out = buf[offset:].view(B, L, V + pitch)[..., :V]
+    out.copy_(x)
+    return out, g
+
+
+def tokens_of(g, B, L, G, V):
+    t = torch.randint(0, V, (B, L, G), generator=g, device="cuda", dtype=torch.int32)
+    if G > 1:
+        t[..., -1] = V - 1
+    if G > 2:
+        t[..., 1] = 0
+    return t
+
+
+def close(got, want, tol, what):
+    got, want = got.double(), want.double()
+    same = (got == want) | ((got - want).abs() <= tol + 2.0 ** -24 * want.abs())
+    assert same.all(), (what, (got - want).abs()[~same].max().item(), int((~same).sum()))
+
+
+def check(x, T, tokens, K, row_len=None, got=None):
+    got = got or dsp.dsp_token_logprobs(x, tokens, K=K, temperature=T, row_len=row_len)
+    three = tokens if tokens.dim() == 3 else tokens[..., None]
+    logp, rank, lse, entropy, top_id, top_x, top_p = ref.score(x, T, three, K, row_len)
+    err = ref.exponent_error(x, T, ref.terms(x.shape[-1]))
+    assert torch.equal(got.rank.long(), rank), "rank"
+    close(got.lse, lse, err, "lse")
+    close(got.logp.view(three.shape), logp, err[..., None], "logp")
+    # T / S: every term's error again, times |a| <= log2 V + 1 in the mean
+    close(got.entropy, entropy, err * (2 + math.log2(x.shape[-1] + 1)), "entropy")
+    if K:
+        assert torch.equal(got.top_id.long(), top_id) and torch.equal(got.top_logit.double(), top_x), "alternatives"
+        close(got.top_logp, top_p, err[..., None], "top_logp")
+    assert not got.row_status.any()
+    return got
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [1, 2, 7, 15, 16, 17, 23, 33, 1000, 12288, 12289, 12303, 32003, 152064, 300001])
+def test_sizes(V, dtype):
+    x, g = rows(3, 2, V, dtype, V)
+    check(x, 1.0, tokens_of(g, 3, 2, 3, V), min(5, 32))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("offset", range(9))
+def test_rows_that_start_anywhere(dtype, offset):
+    x, g = rows(2, 3, 5003, dtype, offset, offset=offset, pitch=offset % 3)
+    t = tokens_of(g, 2, 3, 1, 5003)
+    for first in (0, 1, 6, 7, 8, 9, 4994, 4995, 4996, 5001, 5002):       # tokens outside of the whole pieces, and next to them
+        t[:, :, 0] = first
+        check(x, 1.0, t, 3)
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.7])
+@pytest.mark.parametrize("B,L,V,dtype,G,K", [(1, 1, 152064, BF, 1, 5), (16, 17, 32000, BF, 1, 20), (64, 8, 4001, F32, 33, 0),
+                                             (1, 300, 32000, BF, 2, 32), (2, 1100, 1000, F32, 1, 1)])
+def test_shapes_and_temperatures(B, L, V, dtype, G, K, T):
+    x, g = rows(B, L, V, dtype, G)
+    check(x, T, tokens_of(g, B, L, G, V), K)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("masked", [0.1, 0.9, 1.0])
+@pytest.mark.parametrize("V", [20, 999, 32000, 152064])
+def test_masked_vocabularies(V, masked, dtype):
+    x, g = rows(2, 3, V, dtype, 5, masked=masked)
+    t = tokens_of(g, 2, 3, 2, V)
+    t[0, 0, 0] = V // 2
+    check(x, 0.8, t, 32)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_ties_and_zeros_of_both_signs(dtype):
+    V = 4099
+    x = torch.zeros(1, 4, V, dtype=dtype, device="cuda")
+    x[0, 1, ::2] = -0.0
+    x[0, 2] = torch.randint(0, 3, (V,), device="cuda").to(dtype)
+    tiny = torch.finfo(dtype).smallest_normal / 4                         # below the smallest normal number
+    x[0, 3] = tiny * torch.randint(-2, 3, (V,), device="cuda").to(dtype)
+    for tok in (0, 1, 5, 2048, 4097, 4098):
+        check(x, 1.0, torch.full((1, 4), tok, dtype=torch.int32, device="cuda"), 32)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_ragged_rows_and_tokens_outside(dtype):
+    x, g = rows(4, 5, 2000, dtype, 2)
+    x[1, 3:] = math.nan                                                   # rows that are not read
+    n = torch.tensor([5, 3, 0, 7], dtype=torch.int32, device="cuda")
+    t = tokens_of(g, 4, 5, 3, 2000)
+    t[0, 0], t[3, 1, 0] = torch.tensor([-1, 2000, 7], device="cuda"), 1 << 30
+    got = dsp.dsp_token_logprobs(x, t, K=4, row_len=n)
+    y = x.clone()
+    y[1, 3:] = 0.0
+    check(y, 1.0, t, 4, n.clamp(max=5), got)
+
+
+def test_a_bad_row_is_named_and_alone():
+    x, g = rows(3, 2, 32000, F32, 3)
+    t = tokens_of(g, 3, 2, 1, 32000)
+    want = dsp.dsp_token_logprobs(x, t, K=2)
+    x[1, 0, 77], x[2, 1, 31999] = math.nan, math.inf
+    got = dsp.dsp_token_logprobs(x, t, K=2)
+    assert got.row_status.tolist() == [0, 1, 1]
+    assert got.lse.isnan().tolist() == [[False, False], [True, False], [False, True]]
+    assert got.logp[1, 0].isnan().all() and got.entropy[2, 1].isnan()
+    keep = torch.tensor([[True, True], [False, True], [True, False]], device="cuda")
+    for name in ("lse", "entropy", "rank", "top_id", "top_logp"):
+        assert torch.equal(getattr(got, name)[keep], getattr(want, name)[keep]), name
+    x[0] = -math.inf
+    assert dsp.dsp_token_logprobs(x, t).row_status.tolist() == [1, 1, 1]
+
+
+def test_far_logits():
+    x = torch.full((1, 2, 9000), -9e36, device="cuda")
+    x[0, 0, 5], x[0, 1, 8999] = 1e6, 1e6 - 0.5
+    x[0, 1, 3] = 1e6
+    check(x, 1.0, torch.tensor([[5, 3]], dtype=torch.int32, device="cuda"), 2)
+
+
+def test_only_what_is_asked_for():
+    x, g = rows(2, 2, 1000, BF, 8)
+    got = dsp.dsp_token_logprobs(x)
+    assert got.logp is None and got.rank is None and got.top_id is None
+    full = dsp.dsp_token_logprobs(x, tokens_of(g, 2, 2, 1, 1000)[..., 0], K=3)
+    assert torch.equal(got.lse, full.lse) and torch.equal(got.entropy, full.entropy) and full.logp.shape == (2, 2)
+    assert dsp.dsp_token_logprobs(x[:0]).lse.shape == (0, 2)
+
+
+def test_calls_give_the_same_bits_and_agree_with_the_lattice():
+    x, g = rows(4, 8, 152064, BF, 9)
+    t = tokens_of(g, 4, 8, 1, 152064)
+    a, b = (dsp.dsp_token_logprobs(x, t, K=16) for _ in range(2))
+    for name in vars(a):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    lat = dsp.dsp_lattice_build(x, 16)
+    assert torch.equal(lat.cand_id, a.top_id) and torch.equal(lat.cand_logit, a.top_logit)
+    close(lat.lse, a.lse, 2 * ref.exponent_error(x, 1.0, ref.terms(152064)), "lse")
