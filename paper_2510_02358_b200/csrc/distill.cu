@@ -39,26 +39,20 @@ struct DistillArgs {
 
 // What a CTA knows of its slice, handed to all CTAs of the row.
 struct Part {
-    double S, E, P, H;       // sums: other tokens (against c), the teacher's tokens (against ct), p, p (log p - z)
-    float c, ct;
-};
-struct Found {               // what follows for the row
-    double c_all, inv_all;
-    float c, fw;             // reference of the others, their factor with the row's weight
-    float rest;              // min(r, s)
-    int none;                // the list says nothing: no gradient
+    float c, S;              // the other tokens: reference, sum against it
+    float ct, E;             // the teacher's tokens of this slice: the same
 };
 struct CopyBar {
     uint64_t bar;
     int timed_out;
 };
 struct Shared : CopyBar {
-    Part part[kMaxCluster];
+    __align__(16) Part warp_part[kWarps];
+    __align__(16) Part part[kMaxCluster];
+    double H[kMaxCluster];                      // sum p (log p - z) of a CTA's tokens
     float accept[kMaxCluster];
-    Found found;
     __align__(16) int id[kDT];
-    double red[kWarps][3];
-    float redc[kWarps], redt[kWarps];
+    double red[kWarps][2];
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -74,8 +68,16 @@ __device__ __forceinline__ uint32_t at_rank(const void *p, int rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void put_remote(uint32_t addr, uint64_t v) {
-    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+__device__ __forceinline__ void put_remote(uint32_t addr, double v) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, float v0, float v1, float v2, float v3) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v0), "f"(v1), "f"(v2), "f"(v3) : "memory");
+}
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
 }
 __device__ __forceinline__ void put_remote(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
@@ -247,14 +249,20 @@ __device__ void store_zeros(DT *grow, int v0, int v1) {
     for (int i = threadIdx.x; i < (last - first) / N; i += kDT) g4[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-__device__ __forceinline__ double max_over(double v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
+// The parts of the lanes of a warp as one.
+__device__ __forceinline__ Part merged_warp(Part p) {
+    Part m;
+    m.c = warp_max(p.c);
+    m.ct = warp_max(p.ct);
+    const float w = ex2_approx(p.c - m.c);
+    // far below the reference: nothing, but NaN and infinite sums stay visible
+    m.S = warp_add(w == 0.f && p.S < CUDART_INF_F ? 0.f : p.S * w);
+    m.E = warp_add(p.E != 0.f ? p.E * ex2_approx(p.ct - m.ct) : 0.f);
+    return m;
 }
 
 template <typename DT, bool GRAD>
-__global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
+__global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     constexpr int N = Elem<DT>::N;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ Shared sh;
@@ -283,17 +291,16 @@ __global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
         }
         return;
     }
+    const int chunks = (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
+    int q0 = p0, q1 = min(p1, p0 + a.buf_vecs);
+    uint32_t parity = 0;
     if (tid == 0) {
         mbar_init(&sh.bar, 1);
         mbar_init_fence();
         sh.timed_out = 0;
     }
-    __syncthreads();
-    if (C > 1) cluster_arrive();
-    const int chunks = (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
-    int q0 = p0, q1 = min(p1, p0 + a.buf_vecs);
-    uint32_t parity = 0;
     send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+    if (C > 1) cluster_arrive();
 
     // ---- the teacher's list, one slot a thread: while the copies are under way ----
     int id = -1;
@@ -317,28 +324,37 @@ __global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
         if (twice) id = -1;
     }
     const bool tail = a.tlse != nullptr;
-    double lp = -CUDART_INF, pk = 0.0;          // log p_k, p_k
+    double lp = -CUDART_INF, pk = 0.0, P;       // log p_k, p_k, their sum
     if (tail) {
         if (id >= 0) lp = (double)t * a.inv_t - (double)a.tlse[row];
+        if (id >= 0) pk = exp(lp);
+        const double p1w = warp * 32 < a.K ? warp_sum(pk) : 0.0;
+        if (lane == 0) sh.red[warp][0] = p1w;
+        __syncthreads();
+        P = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
     } else {                                    // softmax over the K tokens
-        const double m0 = max_over(id >= 0 ? (double)t : -CUDART_INF);
+        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
         const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
-        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : m0;
+        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
         __syncthreads();
         double m = sh.red[0][0];
-        for (int i = 1; i < kWarps; ++i) {
+        for (int i = 1; i * 32 < a.K; ++i) {
             const double o = sh.red[i][0];
             if (m == m && !(o <= m)) m = o;     // a NaN stays
         }
-        const double e = id >= 0 && m > -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
-        const double z0 = warp_sum(m != m ? m : e);
+        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
+        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
         if (lane == 0) sh.red[warp][1] = z0;
         __syncthreads();
         double z = 0.0;
-        for (int i = 0; i < kWarps; ++i) z += sh.red[i][1];
-        if (id >= 0 && z != 0.0) lp = ((double)t - m) * a.inv_t - log(z);
+        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
+        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
+        if (id >= 0 && z != 0.0) {
+            pk = e / z;
+            lp = ((double)t - m) * a.inv_t - log(z);
+        }
     }
-    if (id >= 0) pk = exp(lp);
     const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
     const bool mine = piece >= p0 && piece < p1;
 
@@ -364,122 +380,57 @@ __global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
         send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
     }
 
-    // ---- what the CTA knows, to every CTA of the row ----
+    // ---- what the CTA knows, to every CTA of the row: all that the gradient waits for is in single precision ----
     const double zs = (double)xk * a.scale;     // the token's exponent
     {
         float s0, s1;
         unpack2(S2, s0, s1);
-        const float cw = warp_max(c);
-        const float aw = ex2_approx(c - cw);
-        const double Sw = warp_sum(aw == 0.f && s0 + s1 < CUDART_INF_F ? 0.0 : (double)(s0 + s1) * (double)aw);
-        const float zf = warp_max(mine && (float)zs > kRefFloor ? (float)zs : kRefFloor);
-        if (lane == 0) { sh.redc[warp] = cw; sh.redt[warp] = zf; sh.red[warp][0] = Sw; }
+        Part w1 = {c, s0 + s1, mine && (float)zs > kRefFloor ? (float)zs : kRefFloor, 0.f};
+        w1.E = mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f;
+        w1 = merged_warp(w1);
+        if (lane == 0) sh.warp_part[warp] = w1;
     }
     __syncthreads();
-    float ct = sh.redt[0];
-    for (int i = 1; i < kWarps; ++i) ct = fmaxf(ct, sh.redt[i]);
-    double S = 0.0;
-    float cb = kRefFloor;
     if (warp == 0) {
-        const double Sw = lane < kWarps ? sh.red[lane][0] : 0.0;
-        const float cw = lane < kWarps ? sh.redc[lane] : kRefFloor;
-        cb = warp_max(cw);
-        S = warp_sum(Sw != 0.0 ? Sw * exp2((double)cw - (double)cb) : 0.0);
-    }
-    __syncthreads();                            // sh.red is free again
-    double E = 0.0, P = 0.0, H = 0.0;
-    if (warp * 32 < a.K) {                      // the first warps have the slots
-        E = warp_sum(mine ? exp2(zs - (double)ct) : 0.0);
-        P = warp_sum(pk);
-        H = warp_sum(mine && pk != 0.0 ? pk * (lp - (double)xk * a.inv_t) : 0.0);
-    }
-    if (lane == 0) { sh.red[warp][0] = E; sh.red[warp][1] = P; sh.red[warp][2] = H; }
-    __syncthreads();
-    if (C > 1) cluster_wait();                  // the other CTAs are there
-    if (warp == 0) {
-        E = P = H = 0.0;
-        for (int i = 0; i < kWarps; ++i) { E += sh.red[i][0]; P += sh.red[i][1]; H += sh.red[i][2]; }
+        const Part mine1 = merged_warp(lane < kWarps ? sh.warp_part[lane] : Part{kRefFloor, 0.f, kRefFloor, 0.f});
         if (C > 1) {
+            cluster_wait();                     // (every warp) the other CTAs are there
             if (lane < C) {
-                const Part *to = &sh.part[rank];
-                put_remote(at_rank(&to->S, lane), (uint64_t)__double_as_longlong(S));
-                put_remote(at_rank(&to->E, lane), (uint64_t)__double_as_longlong(E));
-                put_remote(at_rank(&to->P, lane), (uint64_t)__double_as_longlong(P));
-                put_remote(at_rank(&to->H, lane), (uint64_t)__double_as_longlong(H));
-                put_remote(at_rank(&to->c, lane), cb);
-                put_remote(at_rank(&to->ct, lane), ct);
+                const uint32_t to = at_rank(&sh.part[rank], lane);
+                put_remote(to, mine1.c, mine1.S, mine1.ct, mine1.E);
             }
+            __syncwarp();
         } else if (lane == 0) {
-            sh.part[0] = Part{S, E, P, H, cb, ct};
+            sh.part[0] = mine1;
         }
-        __syncwarp();
+    } else if (C > 1) {
+        cluster_wait();
     }
     if (C > 1) { cluster_arrive(); cluster_wait(); }
+    else __syncthreads();
 
-    // ---- the row ----
-    if (warp == 0) {
-        const bool there = lane < C;
-        const Part q = sh.part[there ? lane : 0];
-        const float cs = warp_max(there ? q.c : kRefFloor), cl = warp_max(there ? q.ct : kRefFloor);
-        S = warp_sum(there && q.S != 0.0 ? q.S * exp2((double)q.c - (double)cs) : 0.0);
-        E = warp_sum(there && q.E != 0.0 ? q.E * exp2((double)q.ct - (double)cl) : 0.0);
-        H = warp_sum(there ? q.H : 0.0);
-        P = q.P;                                // formed by every CTA from the whole list
-        if (lane == 0) {
-            const double c_all = fmax((double)cs, (double)cl);
-            const double to_all = exp2((double)cs - c_all);
-            const double all = (S != 0.0 ? S * to_all : 0.0) + (E != 0.0 ? E * exp2((double)cl - c_all) : 0.0);
-            const bool ok = all > 0.0 && all < CUDART_INF && c_all > (double)kRefFloor && c_all < CUDART_INF;
-            const double lse = ok ? kLn2 * (c_all + log2(all)) : CUDART_NAN;
-            double r = tail ? 1.0 - P : 0.0;
-            r = r < 0.0 ? 0.0 : r;              // NaN stays
-            const bool none = !tail && P == 0.0;
-            double loss = none ? 0.0 : H + P * lse;
-            if (r != 0.0) loss += r * (log(r) - (kLn2 * ((double)cs + log2(S)) - lse));
-            const double f = none || S == 0.0 ? 0.0 : (to_all / all - r / S) * a.inv_t;
-            const double s = S * to_all / all;
-            sh.found.c_all = c_all;
-            sh.found.inv_all = 1.0 / all;
-            sh.found.c = S != 0.0 ? cs : -kRefFloor;      // nothing to scale: every exponential is 0
-            sh.found.fw = (float)(f * (double)w);
-            sh.found.rest = (float)(r < s ? r : s);
-            sh.found.none = none;
-            const bool bad = !ok || !(P < CUDART_INF);
-            if (rank == 0) {
-                a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
-                if (a.lse) a.lse[row] = (float)lse;
-                if (state) { state[0] = sh.found.c; state[1] = (float)f; state[2] = 0.f; state[3] = 0.f; }
-            }
-            const uint32_t flags = (bad && rank == 0 ? DSP_ROW_NONFINITE_INPUT : 0u) | (sh.timed_out ? DSP_ROW_TIMEOUT : 0u);
-            if (a.status && flags) atomicOr(&a.status[b], flags);
-        }
+    // ---- the row, by every thread for itself ----
+    float cs = kRefFloor, cl = kRefFloor;
+    for (int i = 0; i < C; ++i) { cs = fmaxf(cs, sh.part[i].c); cl = fmaxf(cl, sh.part[i].ct); }
+    float S = 0.f, E = 0.f;
+    for (int i = 0; i < C; ++i) {
+        const Part q = sh.part[i];
+        if (q.S != 0.f) S += q.S * ex2_approx(q.c - cs);
+        if (q.E != 0.f) E += q.E * ex2_approx(q.ct - cl);
     }
-    __syncthreads();
-    const Found fd = sh.found;
-    float gk = 0.f;                             // the slot's gradient, with the row's weight
-    double acc = 0.0;
+    const float c_all = fmaxf(cs, cl);
+    const float to_all = ex2_approx(cs - c_all);
+    const float all = (S != 0.f ? S * to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - c_all) : 0.f);
+    double r = tail ? 1.0 - P : 0.0;
+    r = r < 0.0 ? 0.0 : r;                      // NaN stays
+    const bool none = !tail && P == 0.0;        // the list says nothing: no gradient
+    const float f = none || S == 0.f ? 0.f : (float)(((double)(to_all / all) - r / (double)S) * a.inv_t);
+    const float c_f = S != 0.f ? cs : -kRefFloor;         // nothing to scale: every exponential is 0
+    float gk = 0.f, qk = 0.f;                   // the slot's gradient for a weight of 1, and q_k
     if (mine) {
-        const double qk = exp2(zs - fd.c_all) * fd.inv_all;
-        const double gu = fd.none ? 0.0 : (qk - pk) * a.inv_t;
-        gk = (float)(gu * (double)w);
-        acc = pk < qk ? pk : qk;
-        if (state) state[4 + tid] = (float)gu;
-    } else if (state && rank == 0 && tid < a.K && id < 0) {
-        reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+        qk = ex2_approx((float)(zs - (double)c_all)) / all;
+        gk = none ? 0.f : (float)(((double)qk - pk) * a.inv_t);
     }
-    if (a.accept) {
-        if (warp * 32 < a.K) acc = warp_sum(acc);
-        if (lane == 0) sh.red[warp][0] = acc;
-        __syncthreads();
-        if (tid == 0) {
-            acc = 0.0;
-            for (int i = 0; i < kWarps; ++i) acc += sh.red[i][0];
-            if (C > 1) put_remote(at_rank(&sh.accept[rank], 0), (float)acc);
-            else sh.accept[0] = (float)acc;
-        }
-        __syncwarp();
-    }
-    if (C > 1) cluster_arrive();
     if constexpr (GRAD) {
         for (int k = 0;;) {
             // one chunk: it is in the buffer still, without the teacher's tokens; several: once more from the first on
@@ -496,19 +447,53 @@ __global__ void __launch_bounds__(kDT) distill_kernel(const DistillArgs a) {
                 if (piece >= q0 && piece < q1) hide<DT>(buf, p.h + id - q0 * N);
                 __syncthreads();
             }
-            turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, fd.c, fd.fw);
+            turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, c_f, f * w);
             __syncthreads();
-            if (piece >= q0 && piece < q1) buf[p.h + id - q0 * N] = rounded<DT>(gk);
+            if (piece >= q0 && piece < q1) buf[p.h + id - q0 * N] = rounded<DT>(gk * w);
             store_pieces<DT>(g, p, a.V, q0, q1, buf);
             if (++k >= chunks) break;
         }
-        if (tid == 0) bulk_store_read_wait();
     }
-    if (C > 1) cluster_wait();
-    if (rank == 0 && tid == 0 && a.accept) {
-        acc = (double)fd.rest;
-        for (int i = 0; i < C; ++i) acc += (double)sh.accept[i];
-        a.accept[row] = (float)acc;
+    // ---- loss and what else the row is told: while the stores are under way ----
+    if (warp * 32 < a.K) {
+        const double h = warp_sum(mine && pk != 0.0 ? pk * (lp - (double)xk * a.inv_t) : 0.0);
+        const double m = warp_sum(mine ? fmin(pk, (double)qk) : 0.0);
+        if (lane == 0) { sh.red[warp][0] = h; sh.red[warp][1] = m; }
+    }
+    if (state && mine) state[4 + tid] = gk;
+    if (state && rank == 0 && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+    __syncthreads();
+    if (tid == 0) {
+        double h = 0.0, m = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) { h += sh.red[i][0]; m += sh.red[i][1]; }
+        if (C > 1) {
+            put_remote(at_rank(&sh.H[rank], 0), h);
+            put_remote(at_rank(&sh.accept[rank], 0), (float)m);
+        } else {
+            sh.H[0] = h;
+            sh.accept[0] = (float)m;
+        }
+    }
+    __syncwarp();
+    if (C > 1) { cluster_arrive(); cluster_wait(); }
+    if (tid == 0) {
+        uint32_t flags = sh.timed_out ? DSP_ROW_TIMEOUT : 0u;
+        if (rank == 0) {
+            double H = 0.0, accept = 0.0;
+            for (int i = 0; i < C; ++i) { H += sh.H[i]; accept += (double)sh.accept[i]; }
+            const bool ok = all > 0.f && all < CUDART_INF_F && c_all > kRefFloor && c_all < CUDART_INF_F;
+            const double lse = ok ? kLn2 * ((double)c_all + log2((double)all)) : CUDART_NAN;
+            double loss = none ? 0.0 : H + P * lse;
+            if (r != 0.0) loss += r * (log(r) - (kLn2 * ((double)cs + log2((double)S)) - lse));
+            const double s = (double)S * (double)to_all / (double)all;
+            a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
+            if (a.lse) a.lse[row] = (float)lse;
+            if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
+            if (state) { state[0] = c_f; state[1] = f; state[2] = 0.f; state[3] = 0.f; }
+            if (!ok || !(P < CUDART_INF)) flags |= DSP_ROW_NONFINITE_INPUT;
+        }
+        if (a.status && flags) atomicOr(&a.status[b], flags);
+        if (GRAD) bulk_store_read_wait();
     }
 }
 
