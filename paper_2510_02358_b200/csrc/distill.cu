@@ -25,12 +25,12 @@ constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no p
 struct DistillArgs {
     const void *x;
     long long sb, sl;
-    int L, V, K, C;                             // C: CTAs of a row
+    int L, V, K, C, log2_c;                     // C: CTAs of a row
     int buf_vecs;                               // 16-byte vectors that a CTA's buffer holds
     const int32_t *id, *count;
     const float *val, *tlse, *weight;
-    double scale, inv_t;                        // log2(e) / T, 1 / T
-    float s_hi, s_lo;                           // scale = s_hi + s_lo, s_lo > 0: both products of -inf are then -inf
+    double inv_t, inv_s;                        // 1 / T, and back from exponents: 1 / (s T)
+    float s;                                    // log2(e) / T in 32 bits: all exponents of a row are multiples of it
     float *loss, *accept, *lse, *state;
     void *g;
     long long gsb, gsl;
@@ -49,8 +49,7 @@ struct CopyBar {
 struct Shared : CopyBar {
     __align__(16) Part warp_part[kWarps];
     __align__(16) Part part[kMaxCluster];
-    double H[kMaxCluster];                      // sum p (log p - z) of a CTA's tokens
-    float accept[kMaxCluster];
+    float xk[kDT];                              // first CTA: the teacher's tokens under the student
     __align__(16) int id[kDT];
     double red[kWarps][2];
 };
@@ -61,6 +60,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_empty() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t at_rank(const void *p, int rank) {
@@ -68,26 +68,13 @@ __device__ __forceinline__ uint32_t at_rank(const void *p, int rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void put_remote(uint32_t addr, double v) {
-    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
-}
 __device__ __forceinline__ void put_remote(uint32_t addr, float v0, float v1, float v2, float v3) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v0), "f"(v1), "f"(v2), "f"(v3) : "memory");
-}
-__device__ __forceinline__ float warp_add(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    return v;
 }
 __device__ __forceinline__ void put_remote(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void bulk_store(void *dst, const void *src, uint32_t bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bulk_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_store_read_wait() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
 // A row in 16-byte pieces: piece i holds the elements [i N - h, (i + 1) N - h), h the row's distance from the boundary before it.
 // Pieces lo .. hi-1 lie inside the row; of the first and the last a part may lie outside, which is neither read nor written.
@@ -153,84 +140,139 @@ template <typename DT> __device__ __forceinline__ DT rounded(float v) {
     else return v;
 }
 
-// Sum of 2^(x s - c) over the buffer's pieces, by this thread's share, against its own running reference c.
+// Sum of 2^(x s - c) over the buffer's pieces, by this thread's share.  The reference c of a thread is the largest exponent of its
+// first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where the sum passes 2^64 (or a
+// logit is not finite) the share is summed once more against its true maximum, so that no sum is lost below another thread's reference.
 template <typename DT>
-__device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s_hi, float s_lo, float &c, unsigned long long &S2) {
-    constexpr int N = Elem<DT>::N, kU = 4;
+__device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2, unsigned long long nc2, unsigned long long &S2) {
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::N; e += 2) {
+        const unsigned long long a2 = fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2);
+        float a0, a1;
+        unpack2(a2, a0, a1);
+        S2 = add2(S2, pack2(ex2_approx(a0), ex2_approx(a1)));
+    }
+}
+template <typename DT>
+__device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, float &c, float &S) {
+    constexpr int kU = 4;
     const uint32_t nw = Elem<DT>::kNegInfWord;
-    const unsigned long long hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo);
-    for (int i0 = threadIdx.x; i0 < n; i0 += kU * kDT) {
-        uint4 v[kU];
-#pragma unroll
-        for (int u = 0; u < kU; ++u) v[u] = i0 + u * kDT < n ? buf[i0 + u * kDT] : make_uint4(nw, nw, nw, nw);
-        const float tm = fmaxf(fmaxf(Elem<DT>::vmax(v[0]), Elem<DT>::vmax(v[1])), fmaxf(Elem<DT>::vmax(v[2]), Elem<DT>::vmax(v[3])));
-        const float ts = tm * s_hi;
-        if (ts > c) {
-            const float sc = ex2_approx(c - ts);
-            S2 = mul2(S2, pack2(sc, sc));
-            c = ts;
-        }
-        const unsigned long long nc2 = pack2(-c, -c);
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-#pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                const unsigned long long x2 = pack2(Elem<DT>::get(v[u], e), Elem<DT>::get(v[u], e + 1));
-                const unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
-                float a0, a1;
-                unpack2(a2, a0, a1);
-                S2 = add2(S2, pack2(ex2_approx(a0), ex2_approx(a1)));
-            }
-        }
+    const unsigned long long s2 = pack2(s, s);
+    float m = -CUDART_INF_F;
+    int i = threadIdx.x;
+    for (int u = 0; u < kU; ++u) m = fmaxf(m, i + u * kDT < n ? Elem<DT>::vmax(buf[i + u * kDT]) : m);
+    float c1 = fmaxf(m * s, kRefFloor), s0, s1;
+    unsigned long long S2 = pack2(0.f, 0.f), T2 = S2, nc2 = pack2(-c1, -c1);
+    for (; i + kDT < n; i += 2 * kDT) {
+        const uint4 v = buf[i], w = buf[i + kDT];
+        add_piece<DT>(v, s2, nc2, S2);
+        add_piece<DT>(w, s2, nc2, T2);
     }
+    add_piece<DT>(i < n ? buf[i] : make_uint4(nw, nw, nw, nw), s2, nc2, S2);
+    unpack2(add2(S2, T2), s0, s1);
+    if (!(s0 + s1 < 0x1p64f)) {
+        for (i = threadIdx.x; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
+        c1 = fmaxf(m * s, kRefFloor);
+        nc2 = pack2(-c1, -c1);
+        S2 = pack2(0.f, 0.f);
+        for (i = threadIdx.x; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, S2);
+        unpack2(S2, s0, s1);
+    }
+    // with what the chunks before gave
+    const float cn = fmaxf(c, c1);
+    S = (S != 0.f ? S * ex2_approx(c - cn) : 0.f) + ((s0 + s1) != 0.f ? (s0 + s1) * ex2_approx(c1 - cn) : 0.f);
+    c = cn;
 }
 
-// The buffer's logits become f * 2^(x s - c), in place, rounded once.
-template <typename DT>
-__device__ __forceinline__ void turn_pieces(uint4 *buf, int n, float s_hi, float s_lo, float c, float f) {
-    constexpr int N = Elem<DT>::N;
-    const unsigned long long hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo), nc2 = pack2(-c, -c), f2 = pack2(f, f);
-#pragma unroll 2
-    for (int i = threadIdx.x; i < n; i += kDT) {
-        const uint4 v = buf[i];
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-            const unsigned long long x2 = pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1));
-            const unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
-            float a0, a1;
-            unpack2(a2, a0, a1);
-            unpack2(mul2(pack2(ex2_approx(a0), ex2_approx(a1)), f2), a0, a1);
-            if constexpr (N == 8) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(a0, a1);
-                w[e / 2] = *reinterpret_cast<const uint32_t *>(&b);
-            } else {
-                w[e] = __float_as_uint(a0);
-                w[e + 1] = __float_as_uint(a1);
-            }
-        }
-        buf[i] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+// 2^a of two exponents a > -126 by the FMA units: 2^n times a cubic in the fraction within half of 0, the least relative error of any
+// (2^-13.7; half a step of bf16 is 2^-9 to 2^-8).  Coefficients: Remez exchange on the relative error.
+__device__ __forceinline__ unsigned long long exp2_cubic(unsigned long long a2) {
+    const float kC0 = 0.99992806f, kC1 = 0.69326097f, kC2 = 0.24261113f, kC3 = 0.05517167f;
+    const float kMagic = 12582912.f;                     // 1.5 * 2^23: the sum's last bits are the exponent rounded to a whole number
+    const unsigned long long t2 = add2(a2, pack2(kMagic, kMagic));
+    const unsigned long long x2 = fma2(add2(t2, pack2(-kMagic, -kMagic)), pack2(-1.f, -1.f), a2);
+    unsigned long long p2 = fma2(x2, pack2(kC3, kC3), pack2(kC2, kC2));
+    p2 = fma2(p2, x2, pack2(kC1, kC1));
+    p2 = fma2(p2, x2, pack2(kC0, kC0));
+    float t0, t1, p0, p1;
+    unpack2(t2, t0, t1);
+    unpack2(p2, p0, p1);
+    return pack2(__uint_as_float((__float_as_uint(t0) << 23) + __float_as_uint(p0)),
+                 __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(p1)));
 }
 
-// The buffer as pieces [a, b) of the gradient's row.  Ends with the stores sent; thread 0 waits for them (bulk_store_read_wait) before
-// the buffer is used again or the CTA ends.
+// Products below the normal numbers become 0: what a masked logit leaves of the clamped exponent above.
+__device__ __forceinline__ unsigned long long mul2_flush(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// f * 2^(x s - c) of a piece, rounded once (bf16: to the nearest, halves away from 0).  bf16: the exponentials of both passes and the conversions
+// would fill the special function units for nearly as long as memory takes, so a quarter of the exponentials goes to the FMA units and
+// the rounding to the integer ones.
 template <typename DT>
-__device__ __forceinline__ void store_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf) {
+__device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, unsigned long long nc2, unsigned long long f2) {
     constexpr int N = Elem<DT>::N;
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        unsigned long long a2 = fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2);
+        float a0, a1;
+        unpack2(a2, a0, a1);
+        if (N == 8 && e == 6) {
+            a2 = exp2_cubic(pack2(fmaxf(a0, -126.f), fmaxf(a1, -126.f)));
+        } else {
+            a2 = pack2(ex2_approx(a0), ex2_approx(a1));
+        }
+        unpack2(mul2_flush(a2, f2), a0, a1);
+        if constexpr (N == 8) {
+            w[e / 2] = __byte_perm(__float_as_uint(a0) + 0x8000u, __float_as_uint(a1) + 0x8000u, 0x7632);
+        } else {
+            w[e] = __float_as_uint(a0);
+            w[e + 1] = __float_as_uint(a1);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The gradient of pieces [a, b) from their logits in the buffer, the teacher's tokens aside.  Rows of the gradient that start where the
+// logits' do within 16 bytes take whole pieces, others are written element by element.
+template <typename DT>
+__device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf, float s, float c, float f) {
+    constexpr int N = Elem<DT>::N;
+    const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c), f2 = pack2(f, f);
+    uint4 *bp = reinterpret_cast<uint4 *>(buf);
+    if (!(fabsf(f) < CUDART_INF_F)) {           // a row that is not finite: the integer rounding would hide it
+        const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
+        for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = rounded<DT>(CUDART_NAN_F);
+        return;
+    }
     const bool same = (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % N) == p.h;
     if (same) {
-        fence_async();
-        __syncthreads();
         const int l = max(a, p.lo), u = min(b, p.hi);
-        if (threadIdx.x == 0 && u > l) {
-            bulk_store(grow + ((long long)l * N - p.h), buf + (size_t)(l - a) * N, (uint32_t)(u - l) * 16u);
-            bulk_store_commit();
+        uint4 *gp = reinterpret_cast<uint4 *>(grow + ((long long)l * N - p.h));
+        const uint4 *from = bp + (l - a);
+        int i = threadIdx.x;
+        for (; i + kDT < u - l; i += 2 * kDT) {
+            const uint4 v0 = from[i], v1 = from[i + kDT];
+            gp[i] = turned<DT>(v0, s2, nc2, f2);
+            gp[i + kDT] = turned<DT>(v1, s2, nc2, f2);
         }
+        if (i < u - l) gp[i] = turned<DT>(from[i], s2, nc2, f2);
         edges<DT>(p, V, a, b, [&](int v, int place) {
-            if (v >= 0) grow[v] = buf[place];
+            if (v < 0) return;
+            const uint4 t = turned<DT>(bp[place / N], s2, nc2, f2);
+            const int e = place % N;
+            if constexpr (N == 8) {
+                const uint32_t w = e < 2 ? t.x : e < 4 ? t.y : e < 6 ? t.z : t.w;
+                reinterpret_cast<unsigned short *>(grow)[v] = (unsigned short)(e & 1 ? w >> 16 : w);
+            } else {
+                grow[v] = Elem<DT>::get(t, e);
+            }
         });
-    } else {                                    // the gradient's rows start elsewhere within 16 bytes: element by element
+    } else {
+        for (int i = threadIdx.x; i < b - a; i += kDT) bp[i] = turned<DT>(bp[i], s2, nc2, f2);
         __syncthreads();
         const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
         for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = buf[v + p.h - a * N];
@@ -249,15 +291,21 @@ __device__ void store_zeros(DT *grow, int v0, int v1) {
     for (int i = threadIdx.x; i < (last - first) / N; i += kDT) g4[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// The parts of the lanes of a warp as one.
-__device__ __forceinline__ Part merged_warp(Part p) {
-    Part m;
-    m.c = warp_max(p.c);
-    m.ct = warp_max(p.ct);
+// The parts of n neighbouring lanes (a power of two) as one.
+__device__ __forceinline__ Part merged_among(const Part &p, int n) {
+    Part m = p;
+    for (int o = 1; o < n; o <<= 1) {
+        m.c = fmaxf(m.c, __shfl_xor_sync(0xFFFFFFFFu, m.c, o));
+        m.ct = fmaxf(m.ct, __shfl_xor_sync(0xFFFFFFFFu, m.ct, o));
+    }
     const float w = ex2_approx(p.c - m.c);
     // far below the reference: nothing, but NaN and infinite sums stay visible
-    m.S = warp_add(w == 0.f && p.S < CUDART_INF_F ? 0.f : p.S * w);
-    m.E = warp_add(p.E != 0.f ? p.E * ex2_approx(p.ct - m.ct) : 0.f);
+    m.S = w == 0.f && p.S < CUDART_INF_F ? 0.f : p.S * w;
+    m.E = p.E != 0.f ? p.E * ex2_approx(p.ct - m.ct) : 0.f;
+    for (int o = 1; o < n; o <<= 1) {
+        m.S += __shfl_xor_sync(0xFFFFFFFFu, m.S, o);
+        m.E += __shfl_xor_sync(0xFFFFFFFFu, m.E, o);
+    }
     return m;
 }
 
@@ -269,12 +317,12 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     DT *buf = reinterpret_cast<DT *>(ring);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = a.C, rank = C > 1 ? (int)cluster_rank() : 0;
-    const long long row = blockIdx.x / (unsigned)C;
-    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L);
+    const unsigned row32 = blockIdx.x >> a.log2_c, b = row32 / (unsigned)a.L, l = row32 - b * (unsigned)a.L;
+    const long long row = row32;
     const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
     DT *g = GRAD ? reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl : nullptr;
     const Pieces<DT> p(x, a.V);
-    const int p0 = (int)((long long)p.n * rank / C), p1 = (int)((long long)p.n * (rank + 1) / C);
+    const int p0 = (int)(((unsigned)p.n * (unsigned)rank) >> a.log2_c), p1 = (int)(((unsigned)p.n * (unsigned)(rank + 1)) >> a.log2_c);
     const float w = a.weight ? a.weight[row] : 1.f;
     float *state = a.state ? a.state + row * (a.K + 4) : nullptr;
 
@@ -291,7 +339,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         }
         return;
     }
-    const int chunks = (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
+    const int chunks = p1 - p0 <= a.buf_vecs ? 1 : (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
     int q0 = p0, q1 = min(p1, p0 + a.buf_vecs);
     uint32_t parity = 0;
     if (tid == 0) {
@@ -300,7 +348,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         sh.timed_out = 0;
     }
     send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
-    if (C > 1) cluster_arrive();
+    if (C > 1) cluster_arrive_empty();
 
     // ---- the teacher's list, one slot a thread: while the copies are under way ----
     int id = -1;
@@ -359,10 +407,9 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     const bool mine = piece >= p0 && piece < p1;
 
     // ---- the slice: the teacher's tokens taken out, the others summed ----
-    float xk = 0.f, c = kRefFloor;
-    unsigned long long S2 = pack2(0.f, 0.f);
+    float xk = 0.f, c = kRefFloor, Sc = 0.f;
     for (int k = 0;;) {
-        take_copies(sh, parity);
+        if (warp == 0) take_copies(sh, parity);
         parity ^= 1u;
         __syncthreads();                        // the edges are in place too
         if (piece >= q0 && piece < q1) {
@@ -371,7 +418,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
             hide<DT>(buf, at);
         }
         __syncthreads();
-        sum_pieces<DT>(reinterpret_cast<const uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, c, S2);
+        sum_pieces<DT>(reinterpret_cast<const uint4 *>(buf), q1 - q0, a.s, c, Sc);
         if (++k >= chunks) break;
         fence_async();
         __syncthreads();
@@ -381,130 +428,114 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     }
 
     // ---- what the CTA knows, to every CTA of the row: all that the gradient waits for is in single precision ----
-    const double zs = (double)xk * a.scale;     // the token's exponent
+    const double zs = (double)xk * (double)a.s; // the token's exponent
     {
-        float s0, s1;
-        unpack2(S2, s0, s1);
-        Part w1 = {c, s0 + s1, mine && (float)zs > kRefFloor ? (float)zs : kRefFloor, 0.f};
+        Part w1 = {c, Sc, mine && (float)zs > kRefFloor ? (float)zs : kRefFloor, 0.f};
         w1.E = mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f;
-        w1 = merged_warp(w1);
+        w1 = merged_among(w1, 32);
         if (lane == 0) sh.warp_part[warp] = w1;
+    }
+    if (C > 1) cluster_wait();                  // the other CTAs are there
+    if (mine) {
+        if (C > 1) put_remote(at_rank(&sh.xk[tid], 0), xk);
+        else sh.xk[tid] = xk;
     }
     __syncthreads();
     if (warp == 0) {
-        const Part mine1 = merged_warp(lane < kWarps ? sh.warp_part[lane] : Part{kRefFloor, 0.f, kRefFloor, 0.f});
+        const Part all1 = merged_among(sh.warp_part[lane & (kWarps - 1)], kWarps);
         if (C > 1) {
-            cluster_wait();                     // (every warp) the other CTAs are there
-            if (lane < C) {
-                const uint32_t to = at_rank(&sh.part[rank], lane);
-                put_remote(to, mine1.c, mine1.S, mine1.ct, mine1.E);
-            }
-            __syncwarp();
+            if (lane < C) put_remote(at_rank(&sh.part[rank], lane), all1.c, all1.S, all1.ct, all1.E);
         } else if (lane == 0) {
-            sh.part[0] = mine1;
+            sh.part[0] = all1;
         }
-    } else if (C > 1) {
-        cluster_wait();
+        __syncwarp();
     }
-    if (C > 1) { cluster_arrive(); cluster_wait(); }
-    else __syncthreads();
+    if (C > 1) {
+        if (warp * 32 < a.K) cluster_arrive();  // the warps that have put something
+        else cluster_arrive_empty();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
 
     // ---- the row, by every thread for itself ----
-    float cs = kRefFloor, cl = kRefFloor;
-    for (int i = 0; i < C; ++i) { cs = fmaxf(cs, sh.part[i].c); cl = fmaxf(cl, sh.part[i].ct); }
-    float S = 0.f, E = 0.f;
-    for (int i = 0; i < C; ++i) {
-        const Part q = sh.part[i];
-        if (q.S != 0.f) S += q.S * ex2_approx(q.c - cs);
-        if (q.E != 0.f) E += q.E * ex2_approx(q.ct - cl);
-    }
+    const Part q = merged_among(sh.part[lane & (C - 1)], C);
+    const float cs = q.c, S = q.S, cl = q.ct, E = q.E;
     const float c_all = fmaxf(cs, cl);
     const float to_all = ex2_approx(cs - c_all);
     const float all = (S != 0.f ? S * to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - c_all) : 0.f);
     double r = tail ? 1.0 - P : 0.0;
     r = r < 0.0 ? 0.0 : r;                      // NaN stays
     const bool none = !tail && P == 0.0;        // the list says nothing: no gradient
-    const float f = none || S == 0.f ? 0.f : (float)(((double)(to_all / all) - r / (double)S) * a.inv_t);
+    const float f = none || S == 0.f ? 0.f : (to_all / all - (float)r / S) * (float)a.inv_t;
     const float c_f = S != 0.f ? cs : -kRefFloor;         // nothing to scale: every exponential is 0
     float gk = 0.f, qk = 0.f;                   // the slot's gradient for a weight of 1, and q_k
     if (mine) {
         qk = ex2_approx((float)(zs - (double)c_all)) / all;
         gk = none ? 0.f : (float)(((double)qk - pk) * a.inv_t);
     }
+    if (state && mine) state[4 + tid] = gk;
     if constexpr (GRAD) {
         for (int k = 0;;) {
             // one chunk: it is in the buffer still, without the teacher's tokens; several: once more from the first on
             if (chunks > 1) {
                 q0 = p0 + k * a.buf_vecs;
                 q1 = min(p1, q0 + a.buf_vecs);
-                if (tid == 0) bulk_store_read_wait();
                 fence_async();
                 __syncthreads();
                 send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
-                take_copies(sh, parity);
+                if (warp == 0) take_copies(sh, parity);
                 parity ^= 1u;
                 __syncthreads();
-                if (piece >= q0 && piece < q1) hide<DT>(buf, p.h + id - q0 * N);
-                __syncthreads();
             }
-            turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), q1 - q0, a.s_hi, a.s_lo, c_f, f * w);
-            __syncthreads();
-            if (piece >= q0 && piece < q1) buf[p.h + id - q0 * N] = rounded<DT>(gk * w);
-            store_pieces<DT>(g, p, a.V, q0, q1, buf);
+            write_pieces<DT>(g, p, a.V, q0, q1, buf, a.s, c_f, f * w);
+            __syncthreads();                    // the token's own element comes after the piece that it lies in
+            if (piece >= q0 && piece < q1) g[id] = rounded<DT>(gk * w);
             if (++k >= chunks) break;
         }
     }
-    // ---- loss and what else the row is told: while the stores are under way ----
-    if (warp * 32 < a.K) {
-        const double h = warp_sum(mine && pk != 0.0 ? pk * (lp - (double)xk * a.inv_t) : 0.0);
-        const double m = warp_sum(mine ? fmin(pk, (double)qk) : 0.0);
-        if (lane == 0) { sh.red[warp][0] = h; sh.red[warp][1] = m; }
-    }
-    if (state && mine) state[4 + tid] = gk;
-    if (state && rank == 0 && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
-    __syncthreads();
-    if (tid == 0) {
-        double h = 0.0, m = 0.0;
-        for (int i = 0; i * 32 < a.K; ++i) { h += sh.red[i][0]; m += sh.red[i][1]; }
-        if (C > 1) {
-            put_remote(at_rank(&sh.H[rank], 0), h);
-            put_remote(at_rank(&sh.accept[rank], 0), (float)m);
-        } else {
-            sh.H[0] = h;
-            sh.accept[0] = (float)m;
+    // ---- loss and what else the row is told: the first CTA, while the stores are under way ----
+    if (rank == 0) {
+        const float xt = tid < a.K && id >= 0 ? sh.xk[tid] : 0.f;
+        if (warp * 32 < a.K) {
+            double h = 0.0, m = 0.0;
+            if (id >= 0) {
+                if (pk != 0.0) h = pk * (lp - (double)xt * a.inv_t);
+                m = fmin(pk, (double)(ex2_approx((float)((double)xt * (double)a.s - (double)c_all)) / all));
+            }
+            h = warp_sum(h);
+            m = warp_sum(m);
+            if (lane == 0) { sh.red[warp][0] = h; sh.red[warp][1] = m; }
         }
-    }
-    __syncwarp();
-    if (C > 1) { cluster_arrive(); cluster_wait(); }
-    if (tid == 0) {
-        uint32_t flags = sh.timed_out ? DSP_ROW_TIMEOUT : 0u;
-        if (rank == 0) {
+        if (state && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+        __syncthreads();
+        if (tid == 0) {
             double H = 0.0, accept = 0.0;
-            for (int i = 0; i < C; ++i) { H += sh.H[i]; accept += (double)sh.accept[i]; }
+            for (int i = 0; i * 32 < a.K; ++i) { H += sh.red[i][0]; accept += sh.red[i][1]; }
             const bool ok = all > 0.f && all < CUDART_INF_F && c_all > kRefFloor && c_all < CUDART_INF_F;
-            const double lse = ok ? kLn2 * ((double)c_all + log2((double)all)) : CUDART_NAN;
+            const double ln_all = kLn2 * log2((double)all);
+            const double lse = ok ? (double)c_all * a.inv_s + ln_all : CUDART_NAN;
             double loss = none ? 0.0 : H + P * lse;
-            if (r != 0.0) loss += r * (log(r) - (kLn2 * ((double)cs + log2((double)S)) - lse));
+            if (r != 0.0) loss += r * (log(r) - ((double)cs * a.inv_s + kLn2 * log2((double)S) - lse));
             const double s = (double)S * (double)to_all / (double)all;
             a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
             if (a.lse) a.lse[row] = (float)lse;
             if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
             if (state) { state[0] = c_f; state[1] = f; state[2] = 0.f; state[3] = 0.f; }
-            if (!ok || !(P < CUDART_INF)) flags |= DSP_ROW_NONFINITE_INPUT;
+            if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[b], DSP_ROW_NONFINITE_INPUT);
         }
-        if (a.status && flags) atomicOr(&a.status[b], flags);
-        if (GRAD) bulk_store_read_wait();
     }
+    if (tid == 0 && sh.timed_out && a.status) atomicOr(&a.status[b], DSP_ROW_TIMEOUT);
 }
 
 // The gradient from what dsp_distill left of the row: c, f and the K elements.
 struct DistillGradArgs {
     const void *x;
     long long sb, sl;
-    int L, V, K, slices;
+    int L, V, K, slices, per;                   // pieces of a slice
     const int32_t *id;
     const float *state, *factor;
-    float s_hi, s_lo;
+    float s;
     void *g;
     long long gsb, gsl;
 };
@@ -517,13 +548,13 @@ __global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs
     __shared__ CopyBar sh;
     DT *buf = reinterpret_cast<DT *>(ring);
     const int tid = threadIdx.x;
-    const long long row = blockIdx.x / (unsigned)a.slices;
-    const int slice = (int)(blockIdx.x - row * a.slices);
-    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L);
+    const unsigned row32 = blockIdx.x / (unsigned)a.slices, slice = blockIdx.x - row32 * (unsigned)a.slices;
+    const unsigned b = row32 / (unsigned)a.L, l = row32 - b * (unsigned)a.L;
+    const long long row = row32;
     const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
     DT *g = reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl;
     const Pieces<DT> p(x, a.V);
-    const int p0 = (int)((long long)p.n * slice / a.slices), p1 = (int)((long long)p.n * (slice + 1) / a.slices);
+    const int p0 = (int)min(slice * (unsigned)a.per, (unsigned)p.n), p1 = (int)min((slice + 1) * (unsigned)a.per, (unsigned)p.n);
     const float w = a.factor[row];
     if (w == 0.f) {
         store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
@@ -544,17 +575,15 @@ __global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs
         const int id = a.id[row * a.K + tid];
         const int piece = (p.h + id) / N;
         if (id >= 0 && id < a.V && piece >= p0 && piece < p1) {
-            at = p.h + id - p0 * N;
+            at = id;
             gk = state[4 + tid] * w;
         }
     }
-    take_copies(sh, 0u);
+    if (tid < 32) take_copies(sh, 0u);
     __syncthreads();
-    turn_pieces<DT>(reinterpret_cast<uint4 *>(buf), p1 - p0, a.s_hi, a.s_lo, c, sh.timed_out ? CUDART_NAN_F : f);
-    __syncthreads();
-    if (at >= 0) buf[at] = rounded<DT>(gk);
-    store_pieces<DT>(g, p, a.V, p0, p1, buf);
-    if (tid == 0) bulk_store_read_wait();
+    write_pieces<DT>(g, p, a.V, p0, p1, buf, a.s, c, sh.timed_out ? CUDART_NAN_F : f);
+    __syncthreads();                            // the token's own element comes after the piece that it lies in
+    if (at >= 0) g[at] = rounded<DT>(gk);
 }
 
 inline int pieces_at_most(int V, int N) { return (int)(((long long)V + 2 * N - 2) / N); }
@@ -569,6 +598,7 @@ int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     while (C < kMaxCluster && (long long)n > (long long)C * kSliceVecs) C *= 2;
     while (C < kMaxCluster && rows * C < device_sm_count() && n >= 2 * C * 256) C *= 2;
     a.C = C;
+    while ((1 << a.log2_c) < C) ++a.log2_c;
     const int per = (n + C - 1) / C;
     a.buf_vecs = per < kMaxBufVecs ? per : kMaxBufVecs;
     if (rows * C > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
@@ -595,8 +625,8 @@ int32_t launch_distill_grad(DistillGradArgs &a, long long rows, cudaStream_t st)
     const int n = pieces_at_most(a.V, Elem<DT>::N);
     a.slices = (n + kGradVecs - 1) / kGradVecs;
     if (rows * a.slices > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
-    const int per = (n + a.slices - 1) / a.slices;
-    distill_grad_kernel<DT><<<(unsigned)(rows * a.slices), kDT, (size_t)per * 16, st>>>(a);
+    a.per = (n + a.slices - 1) / a.slices;
+    distill_grad_kernel<DT><<<(unsigned)(rows * a.slices), kDT, (size_t)a.per * 16, st>>>(a);
     DSP_CUDA_TRY(cudaGetLastError());
     return DSP_OK;
 }
@@ -635,8 +665,8 @@ extern "C" int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_
     a.L = L; a.V = V; a.K = K;
     a.id = teacher_id; a.count = teacher_count; a.val = teacher_logit; a.tlse = teacher_lse; a.weight = weight;
     a.inv_t = 1.0 / (double)temperature;
-    a.scale = a.inv_t / kLn2;
-    split_scale(a.scale, a.s_hi, a.s_lo);
+    a.s = (float)(a.inv_t / kLn2);
+    a.inv_s = a.inv_t / (double)a.s;
     a.loss = loss; a.accept = accept; a.lse = lse; a.state = state;
     a.g = grad; a.gsb = grad_stride_b; a.gsl = grad_stride_l;
     a.status = row_status;
@@ -664,7 +694,7 @@ extern "C" int32_t dsp_distill_grad(const void *student_logits, int32_t dtype, i
     a.x = student_logits; a.sb = stride_b; a.sl = stride_l;
     a.L = L; a.V = V; a.K = K;
     a.id = teacher_id; a.state = state; a.factor = row_grad;
-    split_scale(1.0 / (double)temperature / kLn2, a.s_hi, a.s_lo);
+    a.s = (float)(1.0 / (double)temperature / kLn2);
     a.g = grad; a.gsb = grad_stride_b; a.gsl = grad_stride_l;
     const long long rows = (long long)B * L;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
