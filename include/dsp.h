@@ -900,7 +900,7 @@ int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t
  *   rank[b,l] = number of tokens that come before tokens[b,l,0] in the total order
  *               (0: it is the argmax); -1 for a token outside 0..V-1
  *   the K best tokens in the total order with their logits x and log-probabilities;
- *   -inf logits are not among them, unused slots (K > V) are id -1, logit and logp -inf.
+ *   -inf logits are not among them (finite ones must exceed -1e38 * temperature, too), unused slots (K > V) are id -1, logit and logp -inf.
  * Rows from row_len[b] on (clipped to 0..L) are not read: logp and lse -inf, rank -1,
  * entropy 0, no alternatives.  Everything but the scalars of a row is read once.
  * Any V and any row start run at full speed: what lies outside of whole 16-byte pieces

@@ -3,7 +3,6 @@
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
-#include <math.h>
 #include <math_constants.h>
 #include <stdint.h>
 
@@ -56,13 +55,6 @@ inline cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<unsigned l
 }
 
 __host__ __device__ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// log2(e) / T as a sum of two floats with a positive second one.
-inline void split_scale(double scale, float &hi, float &lo) {
-    hi = (float)scale;
-    if ((double)hi >= scale) hi = nextafterf(hi, 0.f);
-    lo = (float)(scale - (double)hi);
-}
 
 // ---- programmatic dependent launch: a kernel that only consumes what the kernel before it in
 // the stream produced is launched with launch_dependent; the device may then place its CTAs as

@@ -296,7 +296,7 @@ __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums,
         if (poisoned) redo_column_sums<DT>(rowp, s0, s1, tid, cs);
     }
     grid_dependency_wait();
-    if constexpr (Pass::kCount) pass.hand_in();
+    pass.hand_in();
     if (tid == 0 && bars.timed_out) atomicOr(status_word, (unsigned)DSP_ROW_TIMEOUT);
     if (sums) {
         const WarpPartial p = warp_partial(cs);

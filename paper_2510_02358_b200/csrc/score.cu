@@ -7,6 +7,8 @@
 //
 // The rank needs one comparison per logit and no index: a token that precedes token t in the vocabulary comes before it with an equal
 // logit, a later one does not, so pieces before t's count what exceeds the next smaller number and the others what exceeds t's logit.
+#include <string.h>
+
 #include "dsp_internal.h"
 #include "row_engine.cuh"
 
@@ -19,8 +21,10 @@ struct ScoreArgs {
     long long stride_b, stride_l;
     const int32_t *row_len, *tokens;
     int G, K;
-    double scale, inv_t;      // log2(e) / T, 1 / T
-    float s_hi, s_lo;         // scale = s_hi + s_lo, s_lo > 0: both products of -inf are then -inf
+    double inv_t, inv_s;      // 1 / T, and back from exponents: 1 / (s T)
+    float s;                  // log2(e) / T in 32 bits: all exponents are multiples of it
+    uint32_t low;             // the lowest logit that counts, as a word of the logits' type (twice for bf16)
+    float low_s;              // and its exponent
     float *logp;
     int32_t *rank, *top_id;
     float *top_logit, *top_logp, *lse, *entropy;
@@ -47,13 +51,13 @@ __device__ __forceinline__ uint32_t below_bits_bf16(float x) {
 
 template <typename DT>
 struct TokenPass {
-    static constexpr bool kOwnSums = true, kCount = true;
+    static constexpr bool kOwnTile = true;
     const DT *row;            // the whole row
     const int32_t *token;     // the first token of the row, or null
     unsigned *acc;
-    float s_hi, s_lo;
+    float s;
+    uint32_t low;             // what masked logits are raised to in the sums, as a word of DT
     int V, head, inner;
-    bool masked = false;      // -inf logits seen: exponents are clamped from there on
     // rank
     int tok = -1, vec = 0;    // token, and the streamed piece it lies in (pieces: beyond, 0: before)
     float xt = 0.f;
@@ -63,7 +67,7 @@ struct TokenPass {
     __device__ __forceinline__ void begin() {
         constexpr int N = Elem<DT>::N;
         tok = token ? *token : -1;
-        if (tok < 0 || tok >= V) { tok = -1; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
+        if (tok < 0 || tok >= V) { tok = -1; xt = CUDART_INF_F; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
         xt = Elem<DT>::load1(row + tok);
         vec = tok < head ? 0 : min((tok - head) / N, inner / N);
         if constexpr (N == 8) {
@@ -74,7 +78,7 @@ struct TokenPass {
             ge = below_bits(xt);
         }
     }
-    template <typename T>
+    // Logits of a tile that come before the token: looked for only where the tile's largest reaches it.
     __device__ __forceinline__ void count(const uint4 (&v)[kVpt], int base) {
         constexpr int N = Elem<DT>::N;
         const int v0 = base / N + (int)threadIdx.x;
@@ -83,10 +87,9 @@ struct TokenPass {
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
                 const uint32_t w = v0 + j * kThreads < vec ? ge : gt;
-                const __nv_bfloat162 lim = *reinterpret_cast<const __nv_bfloat162 *>(&w);
                 const uint32_t q[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum = __hadd2(sum, __hgtu2(*reinterpret_cast<const __nv_bfloat162 *>(&q[i]), lim));
+                for (int i = 0; i < 4; ++i) sum = __hadd2(sum, __hgtu2(as_bf162(q[i]), as_bf162(w)));
             }
             n += (int)(__low2float(sum) + __high2float(sum));
         } else {
@@ -98,12 +101,36 @@ struct TokenPass {
             }
         }
     }
-    // The exponents x s - c of one tile into S = sum 2^a and T = sum 2^a a.  A masked logit leaves 0 * -inf in T: the tile is summed
-    // again with its exponents clamped, and later tiles at once.
-    template <typename T, bool RAGGED>
-    __device__ __forceinline__ void sums(const float (&x)[kVpt][Elem<DT>::N], int nvec, int tid, float tm, float &c,
-                                         unsigned long long &S2, unsigned long long &T2) {
-        const float ts = tm * s_hi;
+    static __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); }
+    static __device__ __forceinline__ uint32_t word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+    static __device__ __forceinline__ float max_of(const uint4 (&v)[kVpt]) {
+        if constexpr (Elem<DT>::N == 8) {
+            __nv_bfloat162 m[kVpt];
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j)
+                m[j] = __hmax2_nan(__hmax2_nan(as_bf162(v[j].x), as_bf162(v[j].y)), __hmax2_nan(as_bf162(v[j].z), as_bf162(v[j].w)));
+#pragma unroll
+            for (int j = 1; j < kVpt; ++j) m[0] = __hmax2_nan(m[0], m[j]);
+            return max2_nan(bf16_lo(word(m[0])), bf16_hi(word(m[0])));
+        } else {
+            float m = __uint_as_float(v[0].x);
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j) {
+                m = max3_nan(m, __uint_as_float(v[j].x), __uint_as_float(v[j].y));
+                m = max3_nan(m, __uint_as_float(v[j].z), __uint_as_float(v[j].w));
+            }
+            return m;
+        }
+    }
+    // One tile's share of a thread: S = sum 2^a and T = sum 2^a a over the exponents a = x s - c.  A masked logit counts as `low`: its
+    // power is 0, and so is the product (0 * -inf is not).
+    template <bool RAGGED>
+    __device__ __forceinline__ float tile(const uint4 (&v)[kVpt], int nvec, int tid, int base, float &c, unsigned long long &S2,
+                                          unsigned long long &T2) {
+        constexpr int N = Elem<DT>::N;
+        const float tm = max_of(v);
+        if (!(tm < xt)) count(v, base);
+        const float ts = fmaxf(tm, N == 8 ? bf16_hi(low) : __uint_as_float(low)) * s;
         if (ts > c) {
             const float d = c - ts;
             const float sc = ex2_approx(d);
@@ -112,41 +139,31 @@ struct TokenPass {
             S2 = mul2(S2, sc2);
             c = ts;
         }
-        const unsigned long long S0 = S2, T0 = T2;
-        if (!masked) {
-            add<RAGGED, false>(x, nvec, tid, c, S2, T2);
-            float t0, t1;
-            unpack2(T2, t0, t1);
-            if (t0 + t1 == t0 + t1) return;
-            masked = true;
-        }
-        S2 = S0;
-        T2 = T0;
-        add<RAGGED, true>(x, nvec, tid, c, S2, T2);
-    }
-    template <bool RAGGED, bool CLAMP>
-    __device__ __forceinline__ void add(const float (&x)[kVpt][Elem<DT>::N], int nvec, int tid, float c, unsigned long long &S2,
-                                        unsigned long long &T2) {
-        const unsigned long long nc2 = pack2(-c, -c), hi2 = pack2(s_hi, s_hi), lo2 = pack2(s_lo, s_lo);
+        const unsigned long long nc2 = pack2(-c, -c), s2 = pack2(s, s);
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
             if (RAGGED && j * kThreads + tid >= nvec) continue;
+            const uint32_t q[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
-            for (int e = 0; e < Elem<DT>::N; e += 2) {
-                const unsigned long long x2 = pack2(x[j][e], x[j][e + 1]);
-                unsigned long long a2 = fma2(x2, hi2, fma2(x2, lo2, nc2));
+            for (int i = 0; i < 4; i += N == 8 ? 1 : 2) {
+                float x0, x1;
+                if constexpr (N == 8) {
+                    const uint32_t w = word(__hmax2_nan(as_bf162(q[i]), as_bf162(low)));
+                    x0 = bf16_lo(w);
+                    x1 = bf16_hi(w);
+                } else {
+                    x0 = max2_nan(__uint_as_float(q[i]), __uint_as_float(low));
+                    x1 = max2_nan(__uint_as_float(q[i + 1]), __uint_as_float(low));
+                }
+                const unsigned long long a2 = fma2(pack2(x0, x1), s2, nc2);
                 float a0, a1;
                 unpack2(a2, a0, a1);
-                if (CLAMP) {
-                    a0 = fmaxf(a0, -1000.f);
-                    a1 = fmaxf(a1, -1000.f);
-                    a2 = pack2(a0, a1);
-                }
                 const unsigned long long e2 = pack2(ex2_approx(a0), ex2_approx(a1));
                 S2 = add2(S2, e2);
                 T2 = fma2(e2, a2, T2);
             }
         }
+        return tm;
     }
     // The slice's count, after the preparation has ended and before the row's ticket.
     __device__ __forceinline__ void hand_in() {
@@ -185,7 +202,7 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
     double c = r.c, S = r.S, T = r.T;
     if (extra > 0) {
         key = merge_top32(key, sort32_desc(x > -CUDART_INF_F ? make_key(x, v) : 0ull, lane), lane);
-        const double e = (double)x * a.scale;
+        const double e = (double)x * (double)a.s;
         const float cm = fmaxf(S != 0.0 ? r.c : kRefFloor, warp_max((float)e > kRefFloor ? (float)e : kRefFloor));
         const double d = c - (double)cm, w = S != 0.0 ? exp2(d) : 0.0;
         const double p = x > -CUDART_INF_F ? exp2(e - (double)cm) : 0.0;
@@ -194,9 +211,9 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
         S = S * w + S1;
         c = cm;
     }
-    bad |= !(S > 0.0) || !(S < CUDART_INF) || !(T == T) || !(c > (double)kRefFloor) || !(c < CUDART_INF);
+    bad |= !(S > 0.0) || !(S < CUDART_INF) || !(T == T) || !(c > (double)a.low_s) || !(c < CUDART_INF);
     const double log_s = log2(S);
-    const double lse = bad ? CUDART_NAN : kLn2 * (c + log_s);
+    const double lse = bad ? CUDART_NAN : c * a.inv_s + kLn2 * log_s;
     for (int i = lane; i < a.G; i += 32) {
         const int t = a.tokens[row * a.G + i];
         const bool in = t >= 0 && t < a.V;
@@ -223,7 +240,7 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
     }
     if (lane == 0) {
         a.lse[row] = (float)lse;
-        if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : (float)(kLn2 * (log_s - T / S));
+        if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : (float)(kLn2 * log_s - T / S * a.inv_s);
         if (bad) atomicOr(&a.row_status[b], DSP_ROW_NONFINITE_INPUT);
     }
 }
@@ -233,9 +250,10 @@ __global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
     constexpr int N = Elem<DT>::N;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ StreamBars bars;
-    const long long row = blockIdx.x / (unsigned)a.nslices;
-    const int slice = (int)(blockIdx.x - row * a.nslices);
-    const int b = (int)(row / a.L), l = (int)(row - (long long)b * a.L), lane = threadIdx.x & 31;
+    const unsigned row32 = blockIdx.x / (unsigned)a.nslices;
+    const long long row = row32;
+    const int slice = (int)(blockIdx.x - row32 * (unsigned)a.nslices);
+    const int b = (int)(row32 / (unsigned)a.L), l = (int)(row32 - (unsigned)b * (unsigned)a.L), lane = threadIdx.x & 31;
     if (a.row_len && l >= a.row_len[b]) {                // whole CTA alike
         if (slice == 0 && threadIdx.x < 32) score_nothing(a, row, lane);
         return;
@@ -246,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
     pass.row = rowp;
     pass.token = a.rank ? a.tokens + row * a.G : nullptr;
     pass.acc = a.rank_acc + row;
-    pass.s_hi = a.s_hi; pass.s_lo = a.s_lo;
+    pass.s = a.s; pass.low = a.low;
     pass.V = a.V; pass.head = a.inner ? head : 0; pass.inner = a.inner;
     RowResult r;
     if (a.inner) {
@@ -369,8 +387,16 @@ extern "C" int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t
     a.row_len = row_len; a.tokens = tokens;
     a.G = G; a.K = K;
     a.inv_t = 1.0 / (double)temperature;
-    a.scale = a.inv_t / kLn2;
-    split_scale(a.scale, a.s_hi, a.s_lo);
+    a.s = (float)(a.inv_t / kLn2);
+    a.inv_s = a.inv_t / (double)a.s;
+    // -1e37, or less where its exponent would leave the number range; one that bf16 holds, for both types
+    const float low = a.s > 20.f ? -2e38f / a.s : -1e37f;
+    memcpy(&a.low, &low, 4);
+    a.low &= 0xFFFF0000u;
+    float held;
+    memcpy(&held, &a.low, 4);
+    a.low_s = held * a.s;
+    if (dtype == DSP_BF16) a.low |= a.low >> 16;
     a.logp = logp; a.rank = rank; a.top_id = top_id; a.top_logit = top_logit; a.top_logp = top_logp;
     a.lse = lse; a.entropy = entropy; a.row_status = row_status;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -167,11 +167,21 @@ struct ColSums {    // S = sum 2^(x*kLog2e - c), T = sum 2^(x*kLog2e - c) * (x*k
     float c, S, T;
 };
 
+// A tile's largest logit `tm` enters a thread's record of its column: the best tile and the best of the others (a NaN maximum changes
+// neither).
+__device__ __forceinline__ void note_tile(ColTop &top, float tm, int t) {
+    const bool gt = tm > top.rm1;
+    top.rm2 = gt ? top.rm1 : fmaxf(top.rm2, tm);
+    top.t1 = gt ? t : top.t1;
+    top.rm1 = gt ? tm : top.rm1;
+    top.seen = max2_nan(top.seen, tm);
+}
+
 // What a kernel may add to the pass over its rows (score.cu does): nothing.
 struct PlainPass {
-    static constexpr bool kOwnSums = false;       // sums() instead of the loop below
-    static constexpr bool kCount = false;         // count() sees every tile
+    static constexpr bool kOwnTile = false;       // tile() returns a tile's largest logit (NaN if it holds one) and adds its sums
     __device__ __forceinline__ void begin() {}    // the first copies are under way
+    __device__ __forceinline__ void hand_in() {}  // the slice is through, what an earlier kernel prepared may be touched
 };
 
 // One tile from shared memory into the thread's running values.  nvec: 16-byte vectors of the
@@ -192,59 +202,55 @@ __device__ __forceinline__ void scan_tile(const uint4 *__restrict__ sp, int nvec
             v[j] = vi < nvec ? sp[vi] : make_uint4(nw, nw, nw, nw);
         }
     }
-    float x[kVpt][N];
-    float vm[kVpt];
-#pragma unroll
-    for (int j = 0; j < kVpt; ++j) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[j][e] = Elem<DT>::get(v[j], e);
-        if constexpr (N == 8) {
-            vm[j] = max3_nan(max3_nan(x[j][0], x[j][1], x[j][2]), max3_nan(x[j][3], x[j][4], x[j][5]),
-                             max2_nan(x[j][6], x[j][7]));
-        } else {
-            vm[j] = max2_nan(max3_nan(x[j][0], x[j][1], x[j][2]), x[j][3]);
-        }
-    }
-    float tm = vm[0];
-    if constexpr (kVpt == 6) {
-        tm = max2_nan(max3_nan(vm[0], vm[1], vm[2]), max3_nan(vm[3], vm[4], vm[5]));
+    if constexpr (Pass::kOwnTile) {
+        note_tile(top, pass.template tile<RAGGED>(v, nvec, tid, base, c, S2, T2), t);
     } else {
-#pragma unroll
-        for (int j = 1; j < kVpt; ++j) tm = max2_nan(tm, vm[j]);
-    }
-    // the column's best tile and the best of the others (a NaN maximum changes neither)
-    const bool gt = tm > top.rm1;
-    top.rm2 = gt ? top.rm1 : fmaxf(top.rm2, tm);
-    top.t1 = gt ? t : top.t1;
-    top.rm1 = gt ? tm : top.rm1;
-    top.seen = max2_nan(top.seen, tm);
-
-    if constexpr (Pass::kCount) pass.template count<DT>(v, base);
-    if constexpr (Pass::kOwnSums) {
-        pass.template sums<DT, RAGGED>(x, nvec, tid, tm, c, S2, T2);
-    } else if constexpr (SUMS) {
-        const float ts = tm * kLog2e;                 // the reference exponent bounds every logit seen
-        if (ts > c) {                                  // both halves move to the new reference exponent
-            const float d = c - ts;
-            const float sc = ex2_approx(d);
-            const unsigned long long sc2 = pack2(sc, sc);
-            T2 = mul2(fma2(S2, pack2(d, d), T2), sc2);
-            S2 = mul2(S2, sc2);
-            c = ts;
-        }
-        // two logits per instruction: a = x * log2(e) - c, S += 2^a, T += 2^a * a
-        const unsigned long long nc2 = pack2(-c, -c), l2e2 = pack2(kLog2e, kLog2e);
+        float x[kVpt][N];
+        float vm[kVpt];
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
-            if (RAGGED && j * kThreads + tid >= nvec) continue;
 #pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                const unsigned long long a2 = fma2(pack2(x[j][e], x[j][e + 1]), l2e2, nc2);
-                float a0, a1;
-                unpack2(a2, a0, a1);
-                const unsigned long long e2 = pack2(ex2_approx(a0), ex2_approx(a1));
-                S2 = add2(S2, e2);
-                T2 = fma2(e2, a2, T2);
+            for (int e = 0; e < N; ++e) x[j][e] = Elem<DT>::get(v[j], e);
+            if constexpr (N == 8) {
+                vm[j] = max3_nan(max3_nan(x[j][0], x[j][1], x[j][2]), max3_nan(x[j][3], x[j][4], x[j][5]),
+                                 max2_nan(x[j][6], x[j][7]));
+            } else {
+                vm[j] = max2_nan(max3_nan(x[j][0], x[j][1], x[j][2]), x[j][3]);
+            }
+        }
+        float tm = vm[0];
+        if constexpr (kVpt == 6) {
+            tm = max2_nan(max3_nan(vm[0], vm[1], vm[2]), max3_nan(vm[3], vm[4], vm[5]));
+        } else {
+#pragma unroll
+            for (int j = 1; j < kVpt; ++j) tm = max2_nan(tm, vm[j]);
+        }
+        note_tile(top, tm, t);
+
+        if constexpr (SUMS) {
+            const float ts = tm * kLog2e;                 // the reference exponent bounds every logit seen
+            if (ts > c) {                                  // both halves move to the new reference exponent
+                const float d = c - ts;
+                const float sc = ex2_approx(d);
+                const unsigned long long sc2 = pack2(sc, sc);
+                T2 = mul2(fma2(S2, pack2(d, d), T2), sc2);
+                S2 = mul2(S2, sc2);
+                c = ts;
+            }
+            // two logits per instruction: a = x * log2(e) - c, S += 2^a, T += 2^a * a
+            const unsigned long long nc2 = pack2(-c, -c), l2e2 = pack2(kLog2e, kLog2e);
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j) {
+                if (RAGGED && j * kThreads + tid >= nvec) continue;
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const unsigned long long a2 = fma2(pack2(x[j][e], x[j][e + 1]), l2e2, nc2);
+                    float a0, a1;
+                    unpack2(a2, a0, a1);
+                    const unsigned long long e2 = pack2(ex2_approx(a0), ex2_approx(a1));
+                    S2 = add2(S2, e2);
+                    T2 = fma2(e2, a2, T2);
+                }
             }
         }
     }
