@@ -53,7 +53,9 @@ template <typename DT>
 struct TokenPass {
     static constexpr bool kOwnTile = true;
     const DT *row;            // the whole row
-    const int32_t *token;     // the first token of the row, or null
+    const int32_t *tokens;    // the row's tokens
+    int G;
+    bool ranked;
     unsigned *acc;
     float s;
     uint32_t low;             // what masked logits are raised to in the sums, as a word of DT
@@ -63,10 +65,21 @@ struct TokenPass {
     float xt = 0.f;
     uint32_t ge = 0u, gt = 0u;
     int n = 0;
+    // what the row's finish needs of the row, loaded by the first warp while the row streams: a token a lane, the elements outside of
+    // the streamed pieces, the piece of the first token
+    int mine = -1;
+    float x_mine = 0.f, x_outer = 0.f, x_piece = 0.f;
 
+    __device__ __forceinline__ int outer_at(int lane) const { return lane < head ? lane : inner + lane; }
     __device__ __forceinline__ void begin() {
         constexpr int N = Elem<DT>::N;
-        tok = token ? *token : -1;
+        const int lane = threadIdx.x;
+        if (lane < 32) {
+            if (lane < G) mine = tokens[lane];
+            if (mine >= 0 && mine < V) x_mine = Elem<DT>::load1(row + mine);
+            x_outer = lane < V - inner ? Elem<DT>::load1(row + outer_at(lane)) : -CUDART_INF_F;
+        }
+        tok = ranked ? tokens[0] : -1;
         if (tok < 0 || tok >= V) { tok = -1; xt = CUDART_INF_F; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
         xt = Elem<DT>::load1(row + tok);
         vec = tok < head ? 0 : min((tok - head) / N, inner / N);
@@ -77,6 +90,7 @@ struct TokenPass {
             gt = __float_as_uint(xt);
             ge = below_bits(xt);
         }
+        if (lane < N && tok >= head && tok < head + inner) x_piece = Elem<DT>::load1(row + head + vec * N + lane);
     }
     // Logits of a tile that come before the token: looked for only where the tile's largest reaches it.
     __device__ __forceinline__ void count(const uint4 (&v)[kVpt], int base) {
@@ -167,7 +181,7 @@ struct TokenPass {
     }
     // The slice's count, after the preparation has ended and before the row's ticket.
     __device__ __forceinline__ void hand_in() {
-        if (!token) return;
+        if (!ranked) return;
         const int all = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
         if ((threadIdx.x & 31) == 0 && all) atomicAdd(acc, (unsigned)all);
     }
@@ -195,8 +209,8 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
     constexpr int N = Elem<DT>::N;
     // one element a lane: before the streamed pieces, then behind them
     const int extra = a.V - a.inner;
-    const int v = lane < head ? lane : a.inner + lane;
-    const float x = lane < extra ? Elem<DT>::load1(rowp + v) : -CUDART_INF_F;
+    const int v = pass.outer_at(lane);
+    const float x = pass.x_outer;
     bool bad = __any_sync(0xFFFFFFFFu, !(x < CUDART_INF_F)) || r.nonfinite;
     unsigned long long key = lane < a.K && r.key ? r.key - (unsigned)head : 0ull;      // ids count from the streamed part
     double c = r.c, S = r.S, T = r.T;
@@ -215,9 +229,10 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
     const double log_s = log2(S);
     const double lse = bad ? CUDART_NAN : c * a.inv_s + kLn2 * log_s;
     for (int i = lane; i < a.G; i += 32) {
-        const int t = a.tokens[row * a.G + i];
+        const int t = i < 32 ? pass.mine : a.tokens[row * a.G + i];
         const bool in = t >= 0 && t < a.V;
-        a.logp[row * a.G + i] = in ? (float)((double)Elem<DT>::load1(rowp + t) * a.inv_t - lse) : -CUDART_INF_F;
+        const float xi = !in || i < 32 ? pass.x_mine : Elem<DT>::load1(rowp + t);
+        a.logp[row * a.G + i] = in ? (float)((double)xi * a.inv_t - lse) : -CUDART_INF_F;
     }
     if (lane < a.K) {
         const bool some = key != 0ull;
@@ -232,7 +247,7 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
             // before the token: of the outer elements, and of its own piece (counted without equals)
             int n = lane < extra && (x > pass.xt || (x == pass.xt && v < pass.tok)) ? 1 : 0;
             const int u = head + pass.vec * N + lane;
-            if (pass.tok >= head && pass.tok < head + a.inner && lane < N && u < pass.tok && Elem<DT>::load1(rowp + u) == pass.xt) ++n;
+            if (pass.tok >= head && pass.tok < head + a.inner && lane < N && u < pass.tok && pass.x_piece == pass.xt) ++n;
             rank = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
             if (lane == 0) rank += (int)atomicAdd(pass.acc, 0u);
         }
@@ -243,6 +258,53 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
         if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : (float)(kLn2 * log_s - T / S * a.inv_s);
         if (bad) atomicOr(&a.row_status[b], DSP_ROW_NONFINITE_INPUT);
     }
+}
+
+// The sums of a row whose best tokens nobody asks for: as row_engine, without the selection.  True in warp 0 of the CTA that is through last.
+template <typename DT>
+__device__ bool score_sums(const ScoreArgs &a, const DT *inner, long long row, int slice, int b, StreamBars &bars, unsigned char *ring,
+                           TokenPass<DT> &pass, RowResult &r) {
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int s0, s1;
+    slice_range<DT>(slice, a.nslices, a.ntiles_row, a.inner, s0, s1);
+    ColTop top;
+    ColSums cs;
+    stream_slice<DT, true>(inner, s0, s1, a.nstages, bars, ring, top, cs, pass);
+    if (!(top.seen < CUDART_INF_F)) cs.S = CUDART_NAN_F;         // NaN or +inf: the row's sum says so
+    const WarpPartial p = warp_partial(cs);
+    grid_dependency_wait();
+    pass.hand_in();
+    if (lane == 0) {
+        if (a.nslices > 1) {
+            a.rs.wpart[(row * a.nslices + slice) * kWarps + warp] = p;
+            __threadfence();
+        } else {
+            bars.wp[warp] = p;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        if (bars.timed_out) atomicOr(&a.row_status[b], (unsigned)DSP_ROW_TIMEOUT);
+        s_last = a.nslices == 1 || atomicAdd(&a.rs.row_ticket[row], 1u) == (unsigned)a.nslices - 1;
+    }
+    if (warp != 0) return false;
+    __syncwarp();
+    if (!s_last) return false;
+    if (a.nslices > 1) {
+        __threadfence();
+        const WarpPartial *wp = a.rs.wpart + row * a.nslices * kWarps;
+        warp_merge_partials([&](int i) {
+            WarpPartial q;
+            q.S = __ldcg(&wp[i].S); q.T = __ldcg(&wp[i].T); q.c = __ldcg(&wp[i].c); q.pad = 0;
+            return q;
+        }, a.nslices * kWarps, lane, r.c, r.S, r.T);
+    } else {
+        warp_merge_partials([&](int i) { return bars.wp[i]; }, kWarps, lane, r.c, r.S, r.T);
+    }
+    r.key = 0ull;
+    r.nonfinite = false;
+    return true;
 }
 
 template <typename DT>
@@ -262,14 +324,19 @@ __global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
     const int head = a.inner == a.V ? 0 : (int)((N - (reinterpret_cast<uintptr_t>(rowp) / sizeof(DT)) % N) % N);
     TokenPass<DT> pass;
     pass.row = rowp;
-    pass.token = a.rank ? a.tokens + row * a.G : nullptr;
+    pass.tokens = a.tokens + row * a.G;
+    pass.G = a.G;
+    pass.ranked = a.rank != nullptr;
     pass.acc = a.rank_acc + row;
     pass.s = a.s; pass.low = a.low;
     pass.V = a.V; pass.head = a.inner ? head : 0; pass.inner = a.inner;
     RowResult r;
-    if (a.inner) {
+    if (a.inner && a.K == 0) {
         stream_begin(bars, a.nstages);
-        if (!row_engine<DT>(rowp + head, a.inner, a.K > 0 ? a.K : 1, true, row, slice, a.nslices, a.ntiles_row, a.nstages, a.rs,
+        if (!score_sums<DT>(a, rowp + head, row, slice, b, bars, ring, pass, r)) return;
+    } else if (a.inner) {
+        stream_begin(bars, a.nstages);
+        if (!row_engine<DT>(rowp + head, a.inner, a.K, true, row, slice, a.nslices, a.ntiles_row, a.nstages, a.rs,
                             &a.row_status[b], bars, ring, r, pass))
             return;
     } else {                                             // a row shorter than two pieces: one element a lane
