@@ -117,6 +117,22 @@ def test_ragged_rows_and_tokens_outside(dtype):
     check(y, 1.0, t, 4, n.clamp(max=5), got)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [16, 100, 6150, 20000, 50257])
+def test_many_rows(V, dtype):
+    """More rows than CTAs: each takes several in turn, some of them unread."""
+    B, L = 23, 41
+    x, g = rows(B, L, V, dtype, V, offset=1, pitch=1)
+    t = tokens_of(g, B, L, 3, V)
+    n = torch.randint(0, L + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    n[3], n[4:9] = L, 0
+    check(x, 1.3, t, 0, n)
+    x[3, 7, V // 2], x[5, 1, 0] = math.nan, math.nan                     # one that is read, one that is not
+    got = dsp.dsp_token_logprobs(x, t, temperature=1.3, row_len=n)
+    assert got.row_status.tolist() == [int(b == 3) for b in range(B)] and got.lse.isnan().sum() == 1 and got.lse[3, 7].isnan()
+    check(x[3:4, 8:12], 1.3, t[3:4, 8:12].contiguous(), 2)               # few rows, cut into slices: other sums, the same bounds
+
+
 def test_a_bad_row_is_named_and_alone():
     x, g = rows(3, 2, 32000, F32, 3)
     t = tokens_of(g, 3, 2, 1, 32000)
