@@ -37,18 +37,17 @@ struct DistillArgs {
     uint32_t *status;
 };
 
-// What a CTA knows of its slice, handed to all CTAs of the row.
+// What a warp knows of its share of the row, handed to all CTAs of the row.
 struct Part {
     float c, S;              // the other tokens: reference, sum against it
-    float ct, E;             // the teacher's tokens of this slice: the same
+    float ct, E;             // the teacher's tokens that the warp's slots name in this slice: the same
 };
 struct CopyBar {
     uint64_t bar;
     int timed_out;
 };
 struct Shared : CopyBar {
-    __align__(16) Part warp_part[kWarps];
-    __align__(16) Part part[kMaxCluster];
+    __align__(16) Part part[kMaxCluster * kWarps];
     float xk[kDT];                              // first CTA: the teacher's tokens under the student
     __align__(16) int id[kDT];
     double red[kWarps][2];
@@ -140,9 +139,21 @@ template <typename DT> __device__ __forceinline__ DT rounded(float v) {
     else return v;
 }
 
-// Sum of 2^(x s - c) over the buffer's pieces, by this thread's share.  The reference c of a thread is the largest exponent of its
-// first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where the sum passes 2^64 (or a
-// logit is not finite) the share is summed once more against its true maximum, so that no sum is lost below another thread's reference.
+// Largest of a warp (NaN aside) and sum over it.
+__device__ __forceinline__ float max_of_warp(float v) {
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
+__device__ __forceinline__ float sum_of_warp(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Sum of 2^(x s - c) over the buffer's pieces, by this thread's share.  The reference c of a warp is the largest exponent of its
+// first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where a sum passes 2^64 (or a
+// logit is not finite) the warp sums once more against its true maximum, so that no sum is lost below another warp's reference.
 template <typename DT>
 __device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2, unsigned long long nc2, unsigned long long &S2) {
 #pragma unroll
@@ -161,7 +172,7 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     float m = -CUDART_INF_F;
     int i = threadIdx.x;
     for (int u = 0; u < kU; ++u) m = fmaxf(m, i + u * kDT < n ? Elem<DT>::vmax(buf[i + u * kDT]) : m);
-    float c1 = fmaxf(m * s, kRefFloor), s0, s1;
+    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0, s1;
     unsigned long long S2 = pack2(0.f, 0.f), T2 = S2, nc2 = pack2(-c1, -c1);
     for (; i + kDT < n; i += 2 * kDT) {
         const uint4 v = buf[i], w = buf[i + kDT];
@@ -170,9 +181,9 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     }
     add_piece<DT>(i < n ? buf[i] : make_uint4(nw, nw, nw, nw), s2, nc2, S2);
     unpack2(add2(S2, T2), s0, s1);
-    if (!(s0 + s1 < 0x1p64f)) {
+    if (__any_sync(0xFFFFFFFFu, !(s0 + s1 < 0x1p64f))) {
         for (i = threadIdx.x; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
-        c1 = fmaxf(m * s, kRefFloor);
+        c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
         nc2 = pack2(-c1, -c1);
         S2 = pack2(0.f, 0.f);
         for (i = threadIdx.x; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, S2);
@@ -291,24 +302,6 @@ __device__ void store_zeros(DT *grow, int v0, int v1) {
     for (int i = threadIdx.x; i < (last - first) / N; i += kDT) g4[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// The parts of n neighbouring lanes (a power of two) as one.
-__device__ __forceinline__ Part merged_among(const Part &p, int n) {
-    Part m = p;
-    for (int o = 1; o < n; o <<= 1) {
-        m.c = fmaxf(m.c, __shfl_xor_sync(0xFFFFFFFFu, m.c, o));
-        m.ct = fmaxf(m.ct, __shfl_xor_sync(0xFFFFFFFFu, m.ct, o));
-    }
-    const float w = ex2_approx(p.c - m.c);
-    // far below the reference: nothing, but NaN and infinite sums stay visible
-    m.S = w == 0.f && p.S < CUDART_INF_F ? 0.f : p.S * w;
-    m.E = p.E != 0.f ? p.E * ex2_approx(p.ct - m.ct) : 0.f;
-    for (int o = 1; o < n; o <<= 1) {
-        m.S += __shfl_xor_sync(0xFFFFFFFFu, m.S, o);
-        m.E += __shfl_xor_sync(0xFFFFFFFFu, m.E, o);
-    }
-    return m;
-}
-
 template <typename DT, bool GRAD>
 __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     constexpr int N = Elem<DT>::N;
@@ -353,6 +346,8 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     // ---- the teacher's list, one slot a thread: while the copies are under way ----
     int id = -1;
     float t = -CUDART_INF_F;
+    const bool tail = a.tlse != nullptr;
+    const float t_lse = tail ? a.tlse[row] : 0.f;
     if (tid < a.K) {
         id = a.id[row * a.K + tid];
         t = a.val[row * a.K + tid];
@@ -370,38 +365,6 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         }
         for (int j = tid & ~3; j < tid; ++j) twice |= sh.id[j] == id;
         if (twice) id = -1;
-    }
-    const bool tail = a.tlse != nullptr;
-    double lp = -CUDART_INF, pk = 0.0, P;       // log p_k, p_k, their sum
-    if (tail) {
-        if (id >= 0) lp = (double)t * a.inv_t - (double)a.tlse[row];
-        if (id >= 0) pk = exp(lp);
-        const double p1w = warp * 32 < a.K ? warp_sum(pk) : 0.0;
-        if (lane == 0) sh.red[warp][0] = p1w;
-        __syncthreads();
-        P = 0.0;
-        for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
-    } else {                                    // softmax over the K tokens
-        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
-        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
-        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
-        __syncthreads();
-        double m = sh.red[0][0];
-        for (int i = 1; i * 32 < a.K; ++i) {
-            const double o = sh.red[i][0];
-            if (m == m && !(o <= m)) m = o;     // a NaN stays
-        }
-        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
-        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
-        if (lane == 0) sh.red[warp][1] = z0;
-        __syncthreads();
-        double z = 0.0;
-        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
-        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
-        if (id >= 0 && z != 0.0) {
-            pk = e / z;
-            lp = ((double)t - m) * a.inv_t - log(z);
-        }
     }
     const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
     const bool mine = piece >= p0 && piece < p1;
@@ -427,51 +390,94 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
     }
 
-    // ---- what the CTA knows, to every CTA of the row: all that the gradient waits for is in single precision ----
+    // ---- what the warp knows, to every CTA of the row: all that the gradient waits for is in single precision ----
     const double zs = (double)xk * (double)a.s; // the token's exponent
-    {
-        Part w1 = {c, Sc, mine && (float)zs > kRefFloor ? (float)zs : kRefFloor, 0.f};
-        w1.E = mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f;
-        w1 = merged_among(w1, 32);
-        if (lane == 0) sh.warp_part[warp] = w1;
-    }
-    if (C > 1) cluster_wait();                  // the other CTAs are there
-    if (mine) {
-        if (C > 1) put_remote(at_rank(&sh.xk[tid], 0), xk);
-        else sh.xk[tid] = xk;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        const Part all1 = merged_among(sh.warp_part[lane & (kWarps - 1)], kWarps);
-        if (C > 1) {
-            if (lane < C) put_remote(at_rank(&sh.part[rank], lane), all1.c, all1.S, all1.ct, all1.E);
-        } else if (lane == 0) {
-            sh.part[0] = all1;
-        }
-        __syncwarp();
+    Part w1 = {c, sum_of_warp(Sc), kRefFloor, 0.f};
+    if (warp * 32 < a.K) {                      // the warps that have slots
+        w1.ct = max_of_warp(mine && (float)zs > kRefFloor ? (float)zs : kRefFloor);
+        w1.E = sum_of_warp(mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f);
     }
     if (C > 1) {
-        if (warp * 32 < a.K) cluster_arrive();  // the warps that have put something
-        else cluster_arrive_empty();
-        cluster_wait();
+        cluster_wait();                         // the other CTAs are there
+        if (mine) put_remote(at_rank(&sh.xk[tid], 0), xk);
+        if (lane < C) put_remote(at_rank(&sh.part[rank * kWarps + warp], lane), w1.c, w1.S, w1.ct, w1.E);
+        __syncwarp();
+        cluster_arrive();
     } else {
-        __syncthreads();
+        if (mine) sh.xk[tid] = xk;
+        if (lane == 0) sh.part[warp] = w1;
     }
 
+    // ---- the list's probabilities, while the others arrive ----
+    double lp = -CUDART_INF, pk = 0.0, P = 0.0; // log p_k, p_k, their sum
+    if (tail) {
+        if (id >= 0) lp = (double)t * a.inv_t - (double)t_lse;
+        if (id >= 0) pk = exp(lp);
+        if (warp * 32 < a.K) {
+            const double Pw = warp_sum(pk);
+            if (lane == 0) sh.red[warp][0] = Pw;
+        }
+    } else {                                    // softmax over the K tokens
+        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
+        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
+        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
+        __syncthreads();
+        double m = sh.red[0][0];
+        for (int i = 1; i * 32 < a.K; ++i) {
+            const double o = sh.red[i][0];
+            if (m == m && !(o <= m)) m = o;     // a NaN stays
+        }
+        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
+        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
+        if (lane == 0) sh.red[warp][1] = z0;
+        __syncthreads();
+        double z = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
+        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
+        if (id >= 0 && z != 0.0) {
+            pk = e / z;
+            lp = ((double)t - m) * a.inv_t - log(z);
+        }
+    }
+    if (C > 1) cluster_wait();
+    __syncthreads();
+    if (tail)
+        for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
+
     // ---- the row, by every thread for itself ----
-    const Part q = merged_among(sh.part[lane & (C - 1)], C);
-    const float cs = q.c, S = q.S, cl = q.ct, E = q.E;
+    Part q[kMaxCluster * kWarps / 32];
+    float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+        q[i] = lane + 32 * i < C * kWarps ? sh.part[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
+        cs = fmaxf(cs, q[i].c);
+        cl = fmaxf(cl, q[i].ct);
+    }
+    cs = max_of_warp(cs);
+    cl = max_of_warp(cl);
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+        const float w2 = ex2_approx(q[i].c - cs);
+        // far below the reference: nothing, but NaN and infinite sums stay visible
+        S += w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2;
+        E += q[i].E != 0.f ? q[i].E * ex2_approx(q[i].ct - cl) : 0.f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
+        E += __shfl_xor_sync(0xFFFFFFFFu, E, o);
+    }
     const float c_all = fmaxf(cs, cl);
     const float to_all = ex2_approx(cs - c_all);
     const float all = (S != 0.f ? S * to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - c_all) : 0.f);
     double r = tail ? 1.0 - P : 0.0;
     r = r < 0.0 ? 0.0 : r;                      // NaN stays
     const bool none = !tail && P == 0.0;        // the list says nothing: no gradient
-    const float f = none || S == 0.f ? 0.f : (to_all / all - (float)r / S) * (float)a.inv_t;
+    const float f = none || S == 0.f ? 0.f : (__fdividef(to_all, all) - __fdividef((float)r, S)) * (float)a.inv_t;
     const float c_f = S != 0.f ? cs : -kRefFloor;         // nothing to scale: every exponential is 0
     float gk = 0.f, qk = 0.f;                   // the slot's gradient for a weight of 1, and q_k
     if (mine) {
-        qk = ex2_approx((float)(zs - (double)c_all)) / all;
+        qk = __fdividef(ex2_approx((float)(zs - (double)c_all)), all);
         gk = none ? 0.f : (float)(((double)qk - pk) * a.inv_t);
     }
     if (state && mine) state[4 + tid] = gk;
