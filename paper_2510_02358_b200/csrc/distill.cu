@@ -121,12 +121,18 @@ __device__ __forceinline__ void send_copies(const DT *row, const Pieces<DT> &p, 
         else reinterpret_cast<uint32_t *>(buf)[place] = 0xFF800000u;
     });
 }
+// Waits for a buffer's copies, asleep for a microsecond at a time: other CTAs of the SM have the issue slots meanwhile.
 __device__ __forceinline__ void take_copies(CopyBar &sh, uint32_t parity) {
-    volatile int *abort = &sh.timed_out;
-    if (mbar_wait(&sh.bar, parity, abort)) return;
-    sh.timed_out = 1;                           // once more, so that no copy is under way into a buffer that is used again
     const long long t0 = clock64();
-    while (!mbar_try(smem_addr(&sh.bar), parity) && clock64() - t0 < kWaitCycles) {}
+    for (int turn = 0; turn < 2; ++turn) {
+        do {
+            uint32_t ok;
+            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(ok) : "r"(smem_addr(&sh.bar)), "r"(parity), "r"(1000u) : "memory");
+            if (ok) return;
+        } while (clock64() - t0 < (turn + 1) * kWaitCycles);
+        sh.timed_out = 1;                       // once more, so that no copy is under way into a buffer that is used again
+    }
 }
 
 template <typename DT> __device__ __forceinline__ float elem_of(const DT *buf, int i) { return Elem<DT>::load1(buf + i); }
@@ -166,27 +172,29 @@ __device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2,
 }
 template <typename DT>
 __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, float &c, float &S) {
-    constexpr int kU = 4;
-    const uint32_t nw = Elem<DT>::kNegInfWord;
     const unsigned long long s2 = pack2(s, s);
+    const int tid = threadIdx.x, full = n / kDT, rest = n % kDT;       // whole rounds of the CTA, pieces of the last one
+    const uint4 *at = buf + tid;
     float m = -CUDART_INF_F;
-    int i = threadIdx.x;
-    for (int u = 0; u < kU; ++u) m = fmaxf(m, i + u * kDT < n ? Elem<DT>::vmax(buf[i + u * kDT]) : m);
+    if (tid < n) m = Elem<DT>::vmax(at[0]);
+    if (tid + kDT < n) m = fmaxf(m, Elem<DT>::vmax(at[kDT]));
     float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0, s1;
     unsigned long long S2 = pack2(0.f, 0.f), T2 = S2, nc2 = pack2(-c1, -c1);
-    for (; i + kDT < n; i += 2 * kDT) {
-        const uint4 v = buf[i], w = buf[i + kDT];
+    int k = full;
+    for (; k >= 2; k -= 2, at += 2 * kDT) {
+        const uint4 v = at[0], w = at[kDT];
         add_piece<DT>(v, s2, nc2, S2);
         add_piece<DT>(w, s2, nc2, T2);
     }
-    add_piece<DT>(i < n ? buf[i] : make_uint4(nw, nw, nw, nw), s2, nc2, S2);
+    if (k) { add_piece<DT>(at[0], s2, nc2, S2); at += kDT; }
+    if (tid < rest) add_piece<DT>(at[0], s2, nc2, T2);
     unpack2(add2(S2, T2), s0, s1);
     if (__any_sync(0xFFFFFFFFu, !(s0 + s1 < 0x1p64f))) {
-        for (i = threadIdx.x; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
+        for (int i = tid; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
         c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
         nc2 = pack2(-c1, -c1);
         S2 = pack2(0.f, 0.f);
-        for (i = threadIdx.x; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, S2);
+        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, S2);
         unpack2(S2, s0, s1);
     }
     // with what the chunks before gave
@@ -264,13 +272,17 @@ __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int 
         const int l = max(a, p.lo), u = min(b, p.hi);
         uint4 *gp = reinterpret_cast<uint4 *>(grow + ((long long)l * N - p.h));
         const uint4 *from = bp + (l - a);
-        int i = threadIdx.x;
-        for (; i + kDT < u - l; i += 2 * kDT) {
-            const uint4 v0 = from[i], v1 = from[i + kDT];
-            gp[i] = turned<DT>(v0, s2, nc2, f2);
-            gp[i + kDT] = turned<DT>(v1, s2, nc2, f2);
+        const int tid = threadIdx.x, rest = (u - l) % kDT;
+        from += tid;
+        gp += tid;
+        int k = (u - l) / kDT;
+        for (; k >= 2; k -= 2, from += 2 * kDT, gp += 2 * kDT) {
+            const uint4 v0 = from[0], v1 = from[kDT];
+            gp[0] = turned<DT>(v0, s2, nc2, f2);
+            gp[kDT] = turned<DT>(v1, s2, nc2, f2);
         }
-        if (i < u - l) gp[i] = turned<DT>(from[i], s2, nc2, f2);
+        if (k) { gp[0] = turned<DT>(from[0], s2, nc2, f2); from += kDT; gp += kDT; }
+        if (tid < rest) gp[0] = turned<DT>(from[0], s2, nc2, f2);
         edges<DT>(p, V, a, b, [&](int v, int place) {
             if (v < 0) return;
             const uint4 t = turned<DT>(bp[place / N], s2, nc2, f2);
