@@ -46,7 +46,14 @@ struct CopyBar {
     uint64_t bar;
     int timed_out;
 };
+struct Place {               // of a CTA's slice: worked out by one thread
+    const void *x;
+    void *g;
+    int h, n, lo, hi, p0, p1;
+    float w;
+};
 struct Shared : CopyBar {
+    Place place;
     __align__(16) Part part[kMaxCluster * kWarps];
     float xk[kDT];                              // first CTA: the teacher's tokens under the student
     __align__(16) int id[kDT];
@@ -81,6 +88,7 @@ template <typename DT>
 struct Pieces {
     static constexpr int N = Elem<DT>::N;
     int h, n, lo, hi;
+    Pieces() = default;
     __device__ __forceinline__ Pieces(const DT *row, int V) {
         h = (int)((reinterpret_cast<uintptr_t>(row) / sizeof(DT)) % N);
         n = (h + V + N - 1) / N;
@@ -101,26 +109,30 @@ __device__ __forceinline__ void edges(const Pieces<DT> &p, int V, int a, int b, 
     if (p.hi < p.n && p.n - 1 >= p.lo && p.n == b && tid >= 32 && tid < 32 + N) one(p.n - 1, tid - 32);
 }
 
-// Pieces [a, b) of the row into the buffer.  Thread 0 sends the copies; a barrier of the CTA lies between the last use of the buffer
-// (fenced) and this call.  Complete after take_copies and a barrier of the CTA.
+// Pieces [a, b) of the row into the buffer: one thread sends the copies of whole pieces, the elements of the others are read one a thread
+// (outside of the row: -inf).  A barrier of the CTA lies between the last use of the buffer (fenced) and the copies; complete after
+// take_copies and a barrier of the CTA.
 template <typename DT>
-__device__ __forceinline__ void send_copies(const DT *row, const Pieces<DT> &p, int V, int a, int b, DT *buf, CopyBar &sh) {
+__device__ __forceinline__ void send_copies(const DT *row, const Pieces<DT> &p, int a, int b, DT *buf, CopyBar &sh) {
     constexpr int N = Elem<DT>::N;
-    if (threadIdx.x == 0) {
-        const int l = max(a, p.lo), u = min(b, p.hi);
-        const uint32_t bytes = u > l ? (uint32_t)(u - l) * 16u : 0u;
-        mbar_expect_tx(&sh.bar, bytes);
-        const char *src = reinterpret_cast<const char *>(row + ((long long)l * N - p.h));
-        char *dst = reinterpret_cast<char *>(buf + (size_t)(l - a) * N);
-        constexpr uint32_t kPiece = 16384;
-        for (uint32_t o = 0; o < bytes; o += kPiece) bulk_load(dst + o, src + o, min(kPiece, bytes - o), &sh.bar);
-    }
+    const int l = max(a, p.lo), u = min(b, p.hi);
+    const uint32_t bytes = u > l ? (uint32_t)(u - l) * 16u : 0u;
+    mbar_expect_tx(&sh.bar, bytes);
+    const char *src = reinterpret_cast<const char *>(row + ((long long)l * N - p.h));
+    char *dst = reinterpret_cast<char *>(buf + (size_t)(l - a) * N);
+    constexpr uint32_t kPiece = 16384;
+    for (uint32_t o = 0; o < bytes; o += kPiece) bulk_load(dst + o, src + o, min(kPiece, bytes - o), &sh.bar);
+}
+template <typename DT>
+__device__ __forceinline__ void read_edges(const DT *row, const Pieces<DT> &p, int V, int a, int b, DT *buf) {
+    if (p.lo == 0 && p.hi == p.n) return;
     edges<DT>(p, V, a, b, [&](int v, int place) {
         if (v >= 0) buf[place] = row[v];
-        else if constexpr (N == 8) reinterpret_cast<unsigned short *>(buf)[place] = 0xFF80u;
+        else if constexpr (Elem<DT>::N == 8) reinterpret_cast<unsigned short *>(buf)[place] = 0xFF80u;
         else reinterpret_cast<uint32_t *>(buf)[place] = 0xFF800000u;
     });
 }
+
 // Waits for a buffer's copies, asleep for a microsecond at a time: other CTAs of the SM have the issue slots meanwhile.
 __device__ __forceinline__ void take_copies(CopyBar &sh, uint32_t parity) {
     const long long t0 = clock64();
@@ -283,6 +295,7 @@ __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int 
         }
         if (k) { gp[0] = turned<DT>(from[0], s2, nc2, f2); from += kDT; gp += kDT; }
         if (tid < rest) gp[0] = turned<DT>(from[0], s2, nc2, f2);
+        if (p.lo == 0 && p.hi == p.n) return;
         edges<DT>(p, V, a, b, [&](int v, int place) {
             if (v < 0) return;
             const uint4 t = turned<DT>(bp[place / N], s2, nc2, f2);
@@ -322,15 +335,45 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     DT *buf = reinterpret_cast<DT *>(ring);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = a.C, rank = C > 1 ? (int)cluster_rank() : 0;
-    const unsigned row32 = blockIdx.x >> a.log2_c, b = row32 / (unsigned)a.L, l = row32 - b * (unsigned)a.L;
+    const unsigned row32 = blockIdx.x >> a.log2_c;
     const long long row = row32;
-    const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
-    DT *g = GRAD ? reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl : nullptr;
-    const Pieces<DT> p(x, a.V);
-    const int p0 = (int)(((unsigned)p.n * (unsigned)rank) >> a.log2_c), p1 = (int)(((unsigned)p.n * (unsigned)(rank + 1)) >> a.log2_c);
-    const float w = a.weight ? a.weight[row] : 1.f;
+    if (tid == 0) {
+        Place &at = sh.place;
+        const float w0 = a.weight ? a.weight[row] : 1.f;
+        const unsigned b0 = row32 / (unsigned)a.L, l0 = row32 - b0 * (unsigned)a.L;
+        const DT *x0 = reinterpret_cast<const DT *>(a.x) + b0 * a.sb + l0 * a.sl;
+        const Pieces<DT> p(x0, a.V);
+        at.x = x0;
+        if (GRAD) at.g = reinterpret_cast<DT *>(a.g) + b0 * a.gsb + l0 * a.gsl;
+        at.h = p.h; at.n = p.n; at.lo = p.lo; at.hi = p.hi;
+        at.p0 = (int)(((unsigned)p.n * (unsigned)rank) >> a.log2_c);
+        at.p1 = (int)(((unsigned)p.n * (unsigned)(rank + 1)) >> a.log2_c);
+        at.w = w0;
+        sh.timed_out = 0;
+        mbar_init(&sh.bar, 1);
+        mbar_init_fence();
+        if (w0 != 0.f) send_copies<DT>(x0, p, at.p0, min(at.p1, at.p0 + a.buf_vecs), buf, sh);
+    }
+    // ---- the teacher's list, one slot a thread ----
+    int id = -1;
+    float t = -CUDART_INF_F;
+    const bool tail = a.tlse != nullptr;
+    const float t_lse = tail ? a.tlse[row] : 0.f;
+    if (tid < a.K) {
+        id = a.id[row * a.K + tid];
+        t = a.val[row * a.K + tid];
+        const int n = a.count ? a.count[row] : a.K;
+        if (tid >= n || id < 0 || id >= a.V) id = -1;
+    }
+    sh.id[tid] = id;
+    __syncthreads();
+    const DT *x = reinterpret_cast<const DT *>(sh.place.x);
+    DT *g = reinterpret_cast<DT *>(sh.place.g);
+    Pieces<DT> p;
+    p.h = sh.place.h; p.n = sh.place.n; p.lo = sh.place.lo; p.hi = sh.place.hi;
+    const int p0 = sh.place.p0, p1 = sh.place.p1;
+    const float w = sh.place.w;
     float *state = a.state ? a.state + row * (a.K + 4) : nullptr;
-
     if (w == 0.f) {                             // the whole cluster alike
         if (GRAD) store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
         if (rank == 0) {
@@ -344,30 +387,15 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         }
         return;
     }
+    if (C > 1) cluster_arrive_empty();
     const int chunks = p1 - p0 <= a.buf_vecs ? 1 : (p1 - p0 + a.buf_vecs - 1) / a.buf_vecs;
     int q0 = p0, q1 = min(p1, p0 + a.buf_vecs);
     uint32_t parity = 0;
-    if (tid == 0) {
-        mbar_init(&sh.bar, 1);
-        mbar_init_fence();
-        sh.timed_out = 0;
-    }
-    send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
-    if (C > 1) cluster_arrive_empty();
-
-    // ---- the teacher's list, one slot a thread: while the copies are under way ----
-    int id = -1;
-    float t = -CUDART_INF_F;
-    const bool tail = a.tlse != nullptr;
-    const float t_lse = tail ? a.tlse[row] : 0.f;
-    if (tid < a.K) {
-        id = a.id[row * a.K + tid];
-        t = a.val[row * a.K + tid];
-        const int n = a.count ? a.count[row] : a.K;
-        if (tid >= n || id < 0 || id >= a.V) id = -1;
-    }
-    sh.id[tid] = id;
-    __syncthreads();
+    read_edges<DT>(x, p, a.V, q0, q1, buf);
+    auto send = [&]() {
+        if (tid == 0) send_copies<DT>(x, p, q0, q1, buf, sh);
+        read_edges<DT>(x, p, a.V, q0, q1, buf);
+    };
     if (id >= 0) {                              // of equal ids the first slot counts
         bool twice = false;
         const int4 *ids = reinterpret_cast<const int4 *>(sh.id);
@@ -399,7 +427,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         __syncthreads();
         q0 = q1;
         q1 = min(p1, q1 + a.buf_vecs);
-        send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+        send();
     }
 
     // ---- what the warp knows, to every CTA of the row: all that the gradient waits for is in single precision ----
@@ -501,7 +529,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
                 q1 = min(p1, q0 + a.buf_vecs);
                 fence_async();
                 __syncthreads();
-                send_copies<DT>(x, p, a.V, q0, q1, buf, sh);
+                send();
                 if (warp == 0) take_copies(sh, parity);
                 parity ^= 1u;
                 __syncthreads();
@@ -540,10 +568,10 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
             if (a.lse) a.lse[row] = (float)lse;
             if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
             if (state) { state[0] = c_f; state[1] = f; state[2] = 0.f; state[3] = 0.f; }
-            if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[b], DSP_ROW_NONFINITE_INPUT);
+            if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[row32 / (unsigned)a.L], DSP_ROW_NONFINITE_INPUT);
         }
     }
-    if (tid == 0 && sh.timed_out && a.status) atomicOr(&a.status[b], DSP_ROW_TIMEOUT);
+    if (tid == 0 && sh.timed_out && a.status) atomicOr(&a.status[row32 / (unsigned)a.L], DSP_ROW_TIMEOUT);
 }
 
 // The gradient from what dsp_distill left of the row: c, f and the K elements.
@@ -584,7 +612,8 @@ __global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs
         sh.timed_out = 0;
     }
     __syncthreads();
-    send_copies<DT>(x, p, a.V, p0, p1, buf, sh);
+    if (tid == 0) send_copies<DT>(x, p, p0, p1, buf, sh);
+    read_edges<DT>(x, p, a.V, p0, p1, buf);
     const float *state = a.state + row * (a.K + 4);
     const float c = state[0], f = state[1] * w;
     int at = -1;
