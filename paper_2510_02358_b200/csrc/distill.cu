@@ -173,13 +173,14 @@ __device__ __forceinline__ float sum_of_warp(float v) {
 // first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where a sum passes 2^64 (or a
 // logit is not finite) the warp sums once more against its true maximum, so that no sum is lost below another warp's reference.
 template <typename DT>
-__device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2, unsigned long long nc2, unsigned long long &S2) {
+__device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2, unsigned long long nc2, float &S0, float &S1) {
 #pragma unroll
     for (int e = 0; e < Elem<DT>::N; e += 2) {
         const unsigned long long a2 = fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2);
         float a0, a1;
         unpack2(a2, a0, a1);
-        S2 = add2(S2, pack2(ex2_approx(a0), ex2_approx(a1)));
+        S0 += ex2_approx(a0);
+        S1 += ex2_approx(a1);
     }
 }
 template <typename DT>
@@ -190,28 +191,28 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     float m = -CUDART_INF_F;
     if (tid < n) m = Elem<DT>::vmax(at[0]);
     if (tid + kDT < n) m = fmaxf(m, Elem<DT>::vmax(at[kDT]));
-    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0, s1;
-    unsigned long long S2 = pack2(0.f, 0.f), T2 = S2, nc2 = pack2(-c1, -c1);
+    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    unsigned long long nc2 = pack2(-c1, -c1);
     int k = full;
     for (; k >= 2; k -= 2, at += 2 * kDT) {
         const uint4 v = at[0], w = at[kDT];
-        add_piece<DT>(v, s2, nc2, S2);
-        add_piece<DT>(w, s2, nc2, T2);
+        add_piece<DT>(v, s2, nc2, s0, s1);
+        add_piece<DT>(w, s2, nc2, t0, t1);
     }
-    if (k) { add_piece<DT>(at[0], s2, nc2, S2); at += kDT; }
-    if (tid < rest) add_piece<DT>(at[0], s2, nc2, T2);
-    unpack2(add2(S2, T2), s0, s1);
-    if (__any_sync(0xFFFFFFFFu, !(s0 + s1 < 0x1p64f))) {
+    if (k) { add_piece<DT>(at[0], s2, nc2, s0, s1); at += kDT; }
+    if (tid < rest) add_piece<DT>(at[0], s2, nc2, t0, t1);
+    float sum = (s0 + s1) + (t0 + t1);
+    if (__any_sync(0xFFFFFFFFu, !(sum < 0x1p64f))) {
         for (int i = tid; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
         c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
         nc2 = pack2(-c1, -c1);
-        S2 = pack2(0.f, 0.f);
-        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, S2);
-        unpack2(S2, s0, s1);
+        s0 = s1 = 0.f;
+        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, s0, s1);
+        sum = s0 + s1;
     }
     // with what the chunks before gave
     const float cn = fmaxf(c, c1);
-    S = (S != 0.f ? S * ex2_approx(c - cn) : 0.f) + ((s0 + s1) != 0.f ? (s0 + s1) * ex2_approx(c1 - cn) : 0.f);
+    S = (S != 0.f ? S * ex2_approx(c - cn) : 0.f) + (sum != 0.f ? sum * ex2_approx(c1 - cn) : 0.f);
     c = cn;
 }
 
@@ -243,7 +244,8 @@ __device__ __forceinline__ unsigned long long mul2_flush(unsigned long long a, u
 // would fill the special function units for nearly as long as memory takes, so a quarter of the exponentials goes to the FMA units and
 // the rounding to the integer ones.
 template <typename DT>
-__device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, unsigned long long nc2, unsigned long long f2) {
+__device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, unsigned long long nc2, float f) {
+    const unsigned long long f2 = pack2(f, f);
     constexpr int N = Elem<DT>::N;
     uint32_t w[4];
 #pragma unroll
@@ -254,9 +256,14 @@ __device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, u
         if (N == 8 && e == 6) {
             a2 = exp2_cubic(pack2(fmaxf(a0, -126.f), fmaxf(a1, -126.f)));
         } else {
-            a2 = pack2(ex2_approx(a0), ex2_approx(a1));
+            a2 = 0ull;
         }
-        unpack2(mul2_flush(a2, f2), a0, a1);
+        if (N == 8 && e == 6) {
+            unpack2(mul2_flush(a2, f2), a0, a1);
+        } else {
+            a0 = ex2_approx(a0) * f;
+            a1 = ex2_approx(a1) * f;
+        }
         if constexpr (N == 8) {
             w[e / 2] = __byte_perm(__float_as_uint(a0) + 0x8000u, __float_as_uint(a1) + 0x8000u, 0x7632);
         } else {
@@ -272,7 +279,7 @@ __device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, u
 template <typename DT>
 __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf, float s, float c, float f) {
     constexpr int N = Elem<DT>::N;
-    const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c), f2 = pack2(f, f);
+    const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c);
     uint4 *bp = reinterpret_cast<uint4 *>(buf);
     if (!(fabsf(f) < CUDART_INF_F)) {           // a row that is not finite: the integer rounding would hide it
         const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
@@ -290,15 +297,15 @@ __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int 
         int k = (u - l) / kDT;
         for (; k >= 2; k -= 2, from += 2 * kDT, gp += 2 * kDT) {
             const uint4 v0 = from[0], v1 = from[kDT];
-            gp[0] = turned<DT>(v0, s2, nc2, f2);
-            gp[kDT] = turned<DT>(v1, s2, nc2, f2);
+            gp[0] = turned<DT>(v0, s2, nc2, f);
+            gp[kDT] = turned<DT>(v1, s2, nc2, f);
         }
-        if (k) { gp[0] = turned<DT>(from[0], s2, nc2, f2); from += kDT; gp += kDT; }
-        if (tid < rest) gp[0] = turned<DT>(from[0], s2, nc2, f2);
+        if (k) { gp[0] = turned<DT>(from[0], s2, nc2, f); from += kDT; gp += kDT; }
+        if (tid < rest) gp[0] = turned<DT>(from[0], s2, nc2, f);
         if (p.lo == 0 && p.hi == p.n) return;
         edges<DT>(p, V, a, b, [&](int v, int place) {
             if (v < 0) return;
-            const uint4 t = turned<DT>(bp[place / N], s2, nc2, f2);
+            const uint4 t = turned<DT>(bp[place / N], s2, nc2, f);
             const int e = place % N;
             if constexpr (N == 8) {
                 const uint32_t w = e < 2 ? t.x : e < 4 ? t.y : e < 6 ? t.z : t.w;
@@ -308,7 +315,7 @@ __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int 
             }
         });
     } else {
-        for (int i = threadIdx.x; i < b - a; i += kDT) bp[i] = turned<DT>(bp[i], s2, nc2, f2);
+        for (int i = threadIdx.x; i < b - a; i += kDT) bp[i] = turned<DT>(bp[i], s2, nc2, f);
         __syncthreads();
         const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
         for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = buf[v + p.h - a * N];
@@ -354,7 +361,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         mbar_init_fence();
         if (w0 != 0.f) send_copies<DT>(x0, p, at.p0, min(at.p1, at.p0 + a.buf_vecs), buf, sh);
     }
-    // ---- the teacher's list, one slot a thread ----
+    // ---- the teacher's list, one slot a thread: its probabilities are formed while the copies are under way ----
     int id = -1;
     float t = -CUDART_INF_F;
     const bool tail = a.tlse != nullptr;
@@ -406,6 +413,36 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         for (int j = tid & ~3; j < tid; ++j) twice |= sh.id[j] == id;
         if (twice) id = -1;
     }
+    double lp = -CUDART_INF, pk = 0.0, P = 0.0; // log p_k, p_k, their sum
+    if (tail) {
+        if (id >= 0) lp = (double)t * a.inv_t - (double)t_lse;
+        if (id >= 0) pk = exp(lp);
+        if (warp * 32 < a.K) {
+            const double Pw = warp_sum(pk);
+            if (lane == 0) sh.red[warp][0] = Pw;
+        }
+    } else {                                    // softmax over the K tokens
+        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
+        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
+        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
+        __syncthreads();
+        double m = sh.red[0][0];
+        for (int i = 1; i * 32 < a.K; ++i) {
+            const double o = sh.red[i][0];
+            if (m == m && !(o <= m)) m = o;     // a NaN stays
+        }
+        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
+        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
+        if (lane == 0) sh.red[warp][1] = z0;
+        __syncthreads();
+        double z = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
+        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
+        if (id >= 0 && z != 0.0) {
+            pk = e / z;
+            lp = ((double)t - m) * a.inv_t - log(z);
+        }
+    }
     const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
     const bool mine = piece >= p0 && piece < p1;
 
@@ -448,39 +485,8 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         if (lane == 0) sh.part[warp] = w1;
     }
 
-    // ---- the list's probabilities, while the others arrive ----
-    double lp = -CUDART_INF, pk = 0.0, P = 0.0; // log p_k, p_k, their sum
-    if (tail) {
-        if (id >= 0) lp = (double)t * a.inv_t - (double)t_lse;
-        if (id >= 0) pk = exp(lp);
-        if (warp * 32 < a.K) {
-            const double Pw = warp_sum(pk);
-            if (lane == 0) sh.red[warp][0] = Pw;
-        }
-    } else {                                    // softmax over the K tokens
-        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
-        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
-        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
-        __syncthreads();
-        double m = sh.red[0][0];
-        for (int i = 1; i * 32 < a.K; ++i) {
-            const double o = sh.red[i][0];
-            if (m == m && !(o <= m)) m = o;     // a NaN stays
-        }
-        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
-        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
-        if (lane == 0) sh.red[warp][1] = z0;
-        __syncthreads();
-        double z = 0.0;
-        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
-        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
-        if (id >= 0 && z != 0.0) {
-            pk = e / z;
-            lp = ((double)t - m) * a.inv_t - log(z);
-        }
-    }
     if (C > 1) cluster_wait();
-    __syncthreads();
+    else __syncthreads();
     if (tail)
         for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
 
