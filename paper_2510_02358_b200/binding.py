@@ -1088,6 +1088,11 @@ def dsp_cache_fork_workspace_bytes(B_in: int, B_out: int, n_blocks: int) -> int:
     return n.value
 
 
+@lru_cache(maxsize=1024)
+def _fork_workspace(B_in: int, B_out: int, n_blocks: int) -> int:
+    return max(256, dsp_cache_fork_workspace_bytes(B_in, B_out, n_blocks))
+
+
 @_on_stream
 def dsp_cache_fork(src_row: torch.Tensor, keep_len: Optional[torch.Tensor], seq_len: torch.Tensor, block_count: torch.Tensor,
                    ring_pos: torch.Tensor, block_table: torch.Tensor, free_ring: torch.Tensor, page_size: int, new_table: torch.Tensor, *,
@@ -1120,7 +1125,7 @@ def dsp_cache_fork(src_row: torch.Tensor, keep_len: Optional[torch.Tensor], seq_
         _ints("out.ring_pos", out.ring_pos, (2,), i64, dev)
     queue = _queue(dev)
     if workspace is None:
-        workspace = torch.empty(dsp_cache_fork_workspace_bytes(Bi, Bo, n_blocks), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(_fork_workspace(Bi, Bo, n_blocks), dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on %s" % dev)
     _check("dsp_cache_fork", lib().dsp_cache_fork(
