@@ -1137,13 +1137,19 @@ def dsp_cache_fork(src_row: torch.Tensor, keep_len: Optional[torch.Tensor], seq_
 
 
 def _layers(cache: torch.Tensor, D: int):
-    """(address, layers, bytes from layer to layer, blocks, page, heads) of one layer's cache, or of [layers, ...] of them."""
-    one = cache[0] if cache.dim() == 4 and cache.shape[0] > 0 else cache
-    if one.dim() != 3 or cache.dtype != torch.uint8 or not cache.is_cuda or not one.is_contiguous() or one.shape[2] % (D + 8) != 0:
-        raise ValueError("cache must be a uint8 CUDA tensor [n_blocks, Hkv, page_size * (D + 8)] or [layers, ...] of contiguous ones")
-    n_blocks, Hkv, size = one.shape
-    layers = cache.shape[0] if cache.dim() == 4 else 1
-    return cache.data_ptr(), layers, (cache.stride(0) if layers > 1 else 0), n_blocks, size // (D + 8), Hkv, D
+    """(address, layers, bytes from layer to layer, blocks, page, heads, D) of one layer's cache, or of [layers, ...] of them."""
+    shape = cache.shape
+    if len(shape) in (3, 4) and cache.dtype == torch.uint8 and cache.is_cuda:
+        n_blocks, Hkv, size = shape[-3:]
+        if len(shape) == 3:
+            layers, stride, whole = 1, 0, cache.is_contiguous()
+        else:
+            layers = shape[0]
+            stride, block, head, byte = cache.stride()
+            whole = layers > 0 and byte == 1 and (head == size or Hkv == 1) and (block == Hkv * size or n_blocks == 1)
+        if whole and size % (D + 8) == 0:
+            return cache.data_ptr(), layers, stride if layers > 1 else 0, n_blocks, size // (D + 8), Hkv, D
+    raise ValueError("cache must be a uint8 CUDA tensor [n_blocks, Hkv, page_size * (D + 8)] or [layers, ...] of contiguous ones")
 
 
 @_on_stream
