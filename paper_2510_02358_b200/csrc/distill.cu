@@ -52,7 +52,14 @@ struct Place {               // of a CTA's slice: worked out by one thread
     int h, n, lo, hi, p0, p1;
     float w;
 };
+struct Known {               // of the row, after the exchange
+    float cs, S, c_all, to_all, all;
+    float f, c_f;            // gradient of the others: f 2^(x s - c_f)
+    double r;
+    int none;
+};
 struct Shared : CopyBar {
+    Known known;
     Place place;
     __align__(16) Part part[kMaxCluster * kWarps];
     float xk[kDT];                              // first CTA: the teacher's tokens under the student
@@ -173,41 +180,35 @@ __device__ __forceinline__ float sum_of_warp(float v) {
 // first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where a sum passes 2^64 (or a
 // logit is not finite) the warp sums once more against its true maximum, so that no sum is lost below another warp's reference.
 template <typename DT>
-__device__ __forceinline__ void add_piece(const uint4 &v, unsigned long long s2, unsigned long long nc2, float &S0, float &S1) {
+__device__ __forceinline__ void add_piece(const uint4 &v, float s, float c, float &S0, float &S1) {
 #pragma unroll
     for (int e = 0; e < Elem<DT>::N; e += 2) {
-        const unsigned long long a2 = fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2);
-        float a0, a1;
-        unpack2(a2, a0, a1);
-        S0 += ex2_approx(a0);
-        S1 += ex2_approx(a1);
+        S0 += ex2_approx(fmaf(Elem<DT>::get(v, e), s, -c));
+        S1 += ex2_approx(fmaf(Elem<DT>::get(v, e + 1), s, -c));
     }
 }
 template <typename DT>
 __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, float &c, float &S) {
-    const unsigned long long s2 = pack2(s, s);
     const int tid = threadIdx.x, full = n / kDT, rest = n % kDT;       // whole rounds of the CTA, pieces of the last one
     const uint4 *at = buf + tid;
     float m = -CUDART_INF_F;
     if (tid < n) m = Elem<DT>::vmax(at[0]);
     if (tid + kDT < n) m = fmaxf(m, Elem<DT>::vmax(at[kDT]));
     float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
-    unsigned long long nc2 = pack2(-c1, -c1);
     int k = full;
     for (; k >= 2; k -= 2, at += 2 * kDT) {
         const uint4 v = at[0], w = at[kDT];
-        add_piece<DT>(v, s2, nc2, s0, s1);
-        add_piece<DT>(w, s2, nc2, t0, t1);
+        add_piece<DT>(v, s, c1, s0, s1);
+        add_piece<DT>(w, s, c1, t0, t1);
     }
-    if (k) { add_piece<DT>(at[0], s2, nc2, s0, s1); at += kDT; }
-    if (tid < rest) add_piece<DT>(at[0], s2, nc2, t0, t1);
+    if (k) { add_piece<DT>(at[0], s, c1, s0, s1); at += kDT; }
+    if (tid < rest) add_piece<DT>(at[0], s, c1, t0, t1);
     float sum = (s0 + s1) + (t0 + t1);
     if (__any_sync(0xFFFFFFFFu, !(sum < 0x1p64f))) {
         for (int i = tid; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
         c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
-        nc2 = pack2(-c1, -c1);
         s0 = s1 = 0.f;
-        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s2, nc2, s0, s1);
+        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s, c1, s0, s1);
         sum = s0 + s1;
     }
     // with what the chunks before gave
@@ -216,56 +217,18 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     c = cn;
 }
 
-// 2^a of two exponents a > -126 by the FMA units: 2^n times a cubic in the fraction within half of 0, the least relative error of any
-// (2^-13.7; half a step of bf16 is 2^-9 to 2^-8).  Coefficients: Remez exchange on the relative error.
-__device__ __forceinline__ unsigned long long exp2_cubic(unsigned long long a2) {
-    const float kC0 = 0.99992806f, kC1 = 0.69326097f, kC2 = 0.24261113f, kC3 = 0.05517167f;
-    const float kMagic = 12582912.f;                     // 1.5 * 2^23: the sum's last bits are the exponent rounded to a whole number
-    const unsigned long long t2 = add2(a2, pack2(kMagic, kMagic));
-    const unsigned long long x2 = fma2(add2(t2, pack2(-kMagic, -kMagic)), pack2(-1.f, -1.f), a2);
-    unsigned long long p2 = fma2(x2, pack2(kC3, kC3), pack2(kC2, kC2));
-    p2 = fma2(p2, x2, pack2(kC1, kC1));
-    p2 = fma2(p2, x2, pack2(kC0, kC0));
-    float t0, t1, p0, p1;
-    unpack2(t2, t0, t1);
-    unpack2(p2, p0, p1);
-    return pack2(__uint_as_float((__float_as_uint(t0) << 23) + __float_as_uint(p0)),
-                 __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(p1)));
-}
-
-// Products below the normal numbers become 0: what a masked logit leaves of the clamped exponent above.
-__device__ __forceinline__ unsigned long long mul2_flush(unsigned long long a, unsigned long long b) {
-    unsigned long long d;
-    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
-// f * 2^(x s - c) of a piece, rounded once (bf16: to the nearest, halves away from 0).  bf16: the exponentials of both passes and the conversions
-// would fill the special function units for nearly as long as memory takes, so a quarter of the exponentials goes to the FMA units and
-// the rounding to the integer ones.
+// f * 2^(x s - c) of a piece, rounded once.
 template <typename DT>
-__device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, unsigned long long nc2, float f) {
-    const unsigned long long f2 = pack2(f, f);
+__device__ __forceinline__ uint4 turned(const uint4 &v, float s, float c, float f) {
     constexpr int N = Elem<DT>::N;
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
-        unsigned long long a2 = fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2);
-        float a0, a1;
-        unpack2(a2, a0, a1);
-        if (N == 8 && e == 6) {
-            a2 = exp2_cubic(pack2(fmaxf(a0, -126.f), fmaxf(a1, -126.f)));
-        } else {
-            a2 = 0ull;
-        }
-        if (N == 8 && e == 6) {
-            unpack2(mul2_flush(a2, f2), a0, a1);
-        } else {
-            a0 = ex2_approx(a0) * f;
-            a1 = ex2_approx(a1) * f;
-        }
+        const float a0 = ex2_approx(fmaf(Elem<DT>::get(v, e), s, -c)) * f;
+        const float a1 = ex2_approx(fmaf(Elem<DT>::get(v, e + 1), s, -c)) * f;
         if constexpr (N == 8) {
-            w[e / 2] = __byte_perm(__float_as_uint(a0) + 0x8000u, __float_as_uint(a1) + 0x8000u, 0x7632);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(a0, a1);
+            w[e / 2] = *reinterpret_cast<const uint32_t *>(&b);
         } else {
             w[e] = __float_as_uint(a0);
             w[e + 1] = __float_as_uint(a1);
@@ -274,18 +237,22 @@ __device__ __forceinline__ uint4 turned(const uint4 &v, unsigned long long s2, u
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Element e of a piece, to memory.
+template <typename DT>
+__device__ __forceinline__ void put_one(DT *to, const uint4 &t, int e) {
+    if constexpr (Elem<DT>::N == 8) {
+        const uint32_t w = e < 2 ? t.x : e < 4 ? t.y : e < 6 ? t.z : t.w;
+        *reinterpret_cast<unsigned short *>(to) = (unsigned short)(e & 1 ? w >> 16 : w);
+    } else {
+        *to = Elem<DT>::get(t, e);
+    }
+}
 // The gradient of pieces [a, b) from their logits in the buffer, the teacher's tokens aside.  Rows of the gradient that start where the
 // logits' do within 16 bytes take whole pieces, others are written element by element.
 template <typename DT>
 __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf, float s, float c, float f) {
     constexpr int N = Elem<DT>::N;
-    const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c);
     uint4 *bp = reinterpret_cast<uint4 *>(buf);
-    if (!(fabsf(f) < CUDART_INF_F)) {           // a row that is not finite: the integer rounding would hide it
-        const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
-        for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = rounded<DT>(CUDART_NAN_F);
-        return;
-    }
     const bool same = (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % N) == p.h;
     if (same) {
         const int l = max(a, p.lo), u = min(b, p.hi);
@@ -297,25 +264,18 @@ __device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int 
         int k = (u - l) / kDT;
         for (; k >= 2; k -= 2, from += 2 * kDT, gp += 2 * kDT) {
             const uint4 v0 = from[0], v1 = from[kDT];
-            gp[0] = turned<DT>(v0, s2, nc2, f);
-            gp[kDT] = turned<DT>(v1, s2, nc2, f);
+            gp[0] = turned<DT>(v0, s, c, f);
+            gp[kDT] = turned<DT>(v1, s, c, f);
         }
-        if (k) { gp[0] = turned<DT>(from[0], s2, nc2, f); from += kDT; gp += kDT; }
-        if (tid < rest) gp[0] = turned<DT>(from[0], s2, nc2, f);
+        if (k) { gp[0] = turned<DT>(from[0], s, c, f); from += kDT; gp += kDT; }
+        if (tid < rest) gp[0] = turned<DT>(from[0], s, c, f);
         if (p.lo == 0 && p.hi == p.n) return;
         edges<DT>(p, V, a, b, [&](int v, int place) {
             if (v < 0) return;
-            const uint4 t = turned<DT>(bp[place / N], s2, nc2, f);
-            const int e = place % N;
-            if constexpr (N == 8) {
-                const uint32_t w = e < 2 ? t.x : e < 4 ? t.y : e < 6 ? t.z : t.w;
-                reinterpret_cast<unsigned short *>(grow)[v] = (unsigned short)(e & 1 ? w >> 16 : w);
-            } else {
-                grow[v] = Elem<DT>::get(t, e);
-            }
+            put_one<DT>(grow + v, turned<DT>(bp[place / N], s, c, f), place % N);
         });
     } else {
-        for (int i = threadIdx.x; i < b - a; i += kDT) bp[i] = turned<DT>(bp[i], s2, nc2, f);
+        for (int i = threadIdx.x; i < b - a; i += kDT) bp[i] = turned<DT>(bp[i], s, c, f);
         __syncthreads();
         const int v0 = max(0, a * N - p.h), v1 = min(V, b * N - p.h);
         for (int v = v0 + threadIdx.x; v < v1; v += kDT) grow[v] = buf[v + p.h - a * N];
@@ -487,45 +447,51 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
 
     if (C > 1) cluster_wait();
     else __syncthreads();
-    if (tail)
-        for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
 
-    // ---- the row, by every thread for itself ----
-    Part q[kMaxCluster * kWarps / 32];
-    float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
+    // ---- the row, by one warp for all ----
+    if (warp == 0) {
+        Part q[kMaxCluster * kWarps / 32];
+        float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
-        q[i] = lane + 32 * i < C * kWarps ? sh.part[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
-        cs = fmaxf(cs, q[i].c);
-        cl = fmaxf(cl, q[i].ct);
-    }
-    cs = max_of_warp(cs);
-    cl = max_of_warp(cl);
+        for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+            q[i] = lane + 32 * i < C * kWarps ? sh.part[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
+            cs = fmaxf(cs, q[i].c);
+            cl = fmaxf(cl, q[i].ct);
+        }
+        cs = max_of_warp(cs);
+        cl = max_of_warp(cl);
 #pragma unroll
-    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
-        const float w2 = ex2_approx(q[i].c - cs);
-        // far below the reference: nothing, but NaN and infinite sums stay visible
-        S += w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2;
-        E += q[i].E != 0.f ? q[i].E * ex2_approx(q[i].ct - cl) : 0.f;
-    }
+        for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+            const float w2 = ex2_approx(q[i].c - cs);
+            // far below the reference: nothing, but NaN and infinite sums stay visible
+            S += w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2;
+            E += q[i].E != 0.f ? q[i].E * ex2_approx(q[i].ct - cl) : 0.f;
+        }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
-        E += __shfl_xor_sync(0xFFFFFFFFu, E, o);
+        for (int o = 16; o > 0; o >>= 1) {
+            S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
+            E += __shfl_xor_sync(0xFFFFFFFFu, E, o);
+        }
+        Known kn;
+        kn.cs = cs;
+        kn.S = S;
+        kn.c_all = fmaxf(cs, cl);
+        kn.to_all = ex2_approx(cs - kn.c_all);
+        kn.all = (S != 0.f ? S * kn.to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - kn.c_all) : 0.f);
+        if (tail)
+            for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
+        const double r = tail ? 1.0 - P : 0.0;
+        kn.r = r < 0.0 ? 0.0 : r;               // NaN stays
+        kn.none = !tail && P == 0.0;            // the list says nothing: no gradient
+        kn.f = kn.none || S == 0.f ? 0.f : (__fdividef(kn.to_all, kn.all) - __fdividef((float)kn.r, S)) * (float)a.inv_t;
+        kn.c_f = S != 0.f ? cs : -kRefFloor;    // nothing to scale: every exponential is 0
+        if (lane == 0) sh.known = kn;
     }
-    const float c_all = fmaxf(cs, cl);
-    const float to_all = ex2_approx(cs - c_all);
-    const float all = (S != 0.f ? S * to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - c_all) : 0.f);
-    double r = tail ? 1.0 - P : 0.0;
-    r = r < 0.0 ? 0.0 : r;                      // NaN stays
-    const bool none = !tail && P == 0.0;        // the list says nothing: no gradient
-    const float f = none || S == 0.f ? 0.f : (__fdividef(to_all, all) - __fdividef((float)r, S)) * (float)a.inv_t;
-    const float c_f = S != 0.f ? cs : -kRefFloor;         // nothing to scale: every exponential is 0
-    float gk = 0.f, qk = 0.f;                   // the slot's gradient for a weight of 1, and q_k
-    if (mine) {
-        qk = __fdividef(ex2_approx((float)(zs - (double)c_all)), all);
-        gk = none ? 0.f : (float)(((double)qk - pk) * a.inv_t);
-    }
+    __syncthreads();
+    const float c_all = sh.known.c_all, all = sh.known.all, f = sh.known.f, c_f = sh.known.c_f;
+    const bool none = sh.known.none;
+    float gk = 0.f;                             // the slot's gradient for a weight of 1
+    if (mine) gk = none ? 0.f : (float)(((double)__fdividef(ex2_approx((float)(zs - (double)c_all)), all) - pk) * a.inv_t);
     if (state && mine) state[4 + tid] = gk;
     if constexpr (GRAD) {
         for (int k = 0;;) {
@@ -567,6 +533,8 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
             const bool ok = all > 0.f && all < CUDART_INF_F && c_all > kRefFloor && c_all < CUDART_INF_F;
             const double ln_all = kLn2 * log2((double)all);
             const double lse = ok ? (double)c_all * a.inv_s + ln_all : CUDART_NAN;
+            const float cs = sh.known.cs, S = sh.known.S, to_all = sh.known.to_all;
+            const double r = sh.known.r;
             double loss = none ? 0.0 : H + P * lse;
             if (r != 0.0) loss += r * (log(r) - ((double)cs * a.inv_s + kLn2 * log2((double)S) - lse));
             const double s = (double)S * (double)to_all / (double)all;

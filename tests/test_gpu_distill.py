@@ -79,8 +79,7 @@ def check(x, ids, val, T, lse=None, count=None, weight=None, grad=True, two=Fals
     size = (logq.exp() + rest[..., None] * share).scatter_add(-1, at, torch.where(use, p, torch.zeros_like(p)))
     tol = (2 * rel + one + 4 * small)[..., None] * size * (w / T)[..., None] + torch.finfo(x.dtype).eps / 2 * g.abs() * 1.001 + 1e-37
     if x.dtype == BF:
-        # a quarter of the exponentials is a cubic within 2^-13.7 of them (the maximum of |p(x) / 2^x - 1|), before the one rounding
-        tol = (tol + 2.0 ** -13.6 * size * (w / T)[..., None]) * (1 + 2.0 ** -8)
+        tol = tol * (1 + 2.0 ** -8)
     near(got, g, tol, "gradient")
     return r
 
