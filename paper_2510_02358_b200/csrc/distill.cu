@@ -294,6 +294,139 @@ __device__ void store_zeros(DT *grow, int v0, int v1) {
     for (int i = threadIdx.x; i < (last - first) / N; i += kDT) g4[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// The list of a row, one slot a thread (ids: all slots', complete): of equal ids the first slot counts; its probability.  The sum of all: P, or
+// with the teacher's log-sum-exp of each warp in red[warp][0].  Every thread of the CTA.
+__device__ __forceinline__ void probabilities(const DistillArgs &a, int &id, float t, float t_lse, const int *ids, double (*red)[2], double &lp,
+                                              double &pk, double &P) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (id >= 0) {                              // of equal ids the first slot counts
+        bool twice = false;
+        const int4 *quads = reinterpret_cast<const int4 *>(ids);
+        for (int j = 0; j < tid >> 2; ++j) {
+            const int4 o = quads[j];
+            twice |= o.x == id || o.y == id || o.z == id || o.w == id;
+        }
+        for (int j = tid & ~3; j < tid; ++j) twice |= ids[j] == id;
+        if (twice) id = -1;
+    }
+    lp = -CUDART_INF;
+    pk = P = 0.0;
+    if (a.tlse) {
+        if (id >= 0) lp = (double)t * a.inv_t - (double)t_lse;
+        if (id >= 0) pk = exp(lp);
+        if (warp * 32 < a.K) {
+            const double Pw = warp_sum(pk);
+            if (lane == 0) red[warp][0] = Pw;
+        }
+    } else {                                    // softmax over the K tokens
+        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
+        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
+        if (lane == 0) red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
+        __syncthreads();
+        double m = red[0][0];
+        for (int i = 1; i * 32 < a.K; ++i) {
+            const double o = red[i][0];
+            if (m == m && !(o <= m)) m = o;     // a NaN stays
+        }
+        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
+        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
+        if (lane == 0) red[warp][1] = z0;
+        __syncthreads();
+        double z = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) z += red[i][1];
+        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
+        if (id >= 0 && z != 0.0) {
+            pk = e / z;
+            lp = ((double)t - m) * a.inv_t - log(z);
+        }
+    }
+}
+
+// Loss and what else a row is told, by every thread of a CTA; x: the slot's token under the student.
+__device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int id, double lp, double pk, double P, float xt, const Known &kn,
+                                         double (*red)[2]) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float *state = a.state ? a.state + (long long)row * (a.K + 4) : nullptr;
+    if (warp * 32 < a.K) {
+        double h = 0.0, m = 0.0;
+        if (id >= 0) {
+            if (pk != 0.0) h = pk * (lp - (double)xt * a.inv_t);
+            m = fmin(pk, (double)(ex2_approx((float)((double)xt * (double)a.s - (double)kn.c_all)) / kn.all));
+        }
+        h = warp_sum(h);
+        m = warp_sum(m);
+        if (lane == 0) { red[warp][0] = h; red[warp][1] = m; }
+    }
+    if (state && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+    __syncthreads();
+    if (tid == 0) {
+        double H = 0.0, accept = 0.0;
+        for (int i = 0; i * 32 < a.K; ++i) { H += red[i][0]; accept += red[i][1]; }
+        const bool ok = kn.all > 0.f && kn.all < CUDART_INF_F && kn.c_all > kRefFloor && kn.c_all < CUDART_INF_F;
+        const double ln_all = kLn2 * log2((double)kn.all);
+        const double lse = ok ? (double)kn.c_all * a.inv_s + ln_all : CUDART_NAN;
+        const float cs = kn.cs, S = kn.S, to_all = kn.to_all;
+        const double r = kn.r;
+        double loss = kn.none ? 0.0 : H + P * lse;
+        if (r != 0.0) loss += r * (log(r) - ((double)cs * a.inv_s + kLn2 * log2((double)S) - lse));
+        const double s = (double)S * (double)to_all / (double)kn.all;
+        a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
+        if (a.lse) a.lse[row] = (float)lse;
+        if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
+        if (state) { state[0] = kn.c_f; state[1] = kn.f; state[2] = 0.f; state[3] = 0.f; }
+        if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[row / (unsigned)a.L], DSP_ROW_NONFINITE_INPUT);
+    }
+}
+// A row that is not read.
+__device__ __forceinline__ void tell_nothing(const DistillArgs &a, unsigned row) {
+    const int tid = threadIdx.x;
+    float *state = a.state ? a.state + (long long)row * (a.K + 4) : nullptr;
+    if (tid == 0) {
+        a.loss[row] = 0.f;
+        if (a.accept) a.accept[row] = 0.f;
+        if (a.lse) a.lse[row] = -CUDART_INF_F;
+        if (state) { state[0] = -kRefFloor; state[1] = 0.f; state[2] = 0.f; state[3] = 0.f; }
+    }
+    if (state && tid < a.K) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
+}
+// What follows from the sums of a row's n parts, by one warp (P: the list's sum).
+__device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, int lane) {
+    Part q[kMaxCluster * kWarps / 32];
+    float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+        q[i] = lane + 32 * i < n ? parts[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
+        cs = fmaxf(cs, q[i].c);
+        cl = fmaxf(cl, q[i].ct);
+    }
+    cs = max_of_warp(cs);
+    cl = max_of_warp(cl);
+#pragma unroll
+    for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+        const float w2 = ex2_approx(q[i].c - cs);
+        // far below the reference: nothing, but NaN and infinite sums stay visible
+        S += w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2;
+        E += q[i].E != 0.f ? q[i].E * ex2_approx(q[i].ct - cl) : 0.f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
+        E += __shfl_xor_sync(0xFFFFFFFFu, E, o);
+    }
+    Known kn;
+    kn.cs = cs;
+    kn.S = S;
+    kn.c_all = fmaxf(cs, cl);
+    kn.to_all = ex2_approx(cs - kn.c_all);
+    kn.all = (S != 0.f ? S * kn.to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - kn.c_all) : 0.f);
+    const double r = a.tlse ? 1.0 - P : 0.0;
+    kn.r = r < 0.0 ? 0.0 : r;               // NaN stays
+    kn.none = !a.tlse && P == 0.0;           // the list says nothing: no gradient
+    kn.f = kn.none || S == 0.f ? 0.f : (__fdividef(kn.to_all, kn.all) - __fdividef((float)kn.r, S)) * (float)a.inv_t;
+    kn.c_f = S != 0.f ? cs : -kRefFloor;    // nothing to scale: every exponential is 0
+    return kn;
+}
+
 template <typename DT, bool GRAD>
 __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     constexpr int N = Elem<DT>::N;
@@ -343,15 +476,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     float *state = a.state ? a.state + row * (a.K + 4) : nullptr;
     if (w == 0.f) {                             // the whole cluster alike
         if (GRAD) store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
-        if (rank == 0) {
-            if (tid == 0) {
-                a.loss[row] = 0.f;
-                if (a.accept) a.accept[row] = 0.f;
-                if (a.lse) a.lse[row] = -CUDART_INF_F;
-                if (state) { state[0] = -kRefFloor; state[1] = 0.f; state[2] = 0.f; state[3] = 0.f; }
-            }
-            if (state && tid < a.K) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
-        }
+        if (rank == 0) tell_nothing(a, row32);
         return;
     }
     if (C > 1) cluster_arrive_empty();
@@ -363,46 +488,8 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         if (tid == 0) send_copies<DT>(x, p, q0, q1, buf, sh);
         read_edges<DT>(x, p, a.V, q0, q1, buf);
     };
-    if (id >= 0) {                              // of equal ids the first slot counts
-        bool twice = false;
-        const int4 *ids = reinterpret_cast<const int4 *>(sh.id);
-        for (int j = 0; j < tid >> 2; ++j) {
-            const int4 o = ids[j];
-            twice |= o.x == id || o.y == id || o.z == id || o.w == id;
-        }
-        for (int j = tid & ~3; j < tid; ++j) twice |= sh.id[j] == id;
-        if (twice) id = -1;
-    }
-    double lp = -CUDART_INF, pk = 0.0, P = 0.0; // log p_k, p_k, their sum
-    if (tail) {
-        if (id >= 0) lp = (double)t * a.inv_t - (double)t_lse;
-        if (id >= 0) pk = exp(lp);
-        if (warp * 32 < a.K) {
-            const double Pw = warp_sum(pk);
-            if (lane == 0) sh.red[warp][0] = Pw;
-        }
-    } else {                                    // softmax over the K tokens
-        const float m0 = warp_max(id >= 0 ? t : -CUDART_INF_F);
-        const bool nan0 = __any_sync(0xFFFFFFFFu, id >= 0 && t != t);
-        if (lane == 0) sh.red[warp][0] = nan0 ? CUDART_NAN : (double)m0;
-        __syncthreads();
-        double m = sh.red[0][0];
-        for (int i = 1; i * 32 < a.K; ++i) {
-            const double o = sh.red[i][0];
-            if (m == m && !(o <= m)) m = o;     // a NaN stays
-        }
-        const double e = id >= 0 && m != -CUDART_INF ? exp(((double)t - m) * a.inv_t) : 0.0;
-        const double z0 = warp * 32 < a.K ? warp_sum(m != m ? m : e) : 0.0;
-        if (lane == 0) sh.red[warp][1] = z0;
-        __syncthreads();
-        double z = 0.0;
-        for (int i = 0; i * 32 < a.K; ++i) z += sh.red[i][1];
-        P = z == 0.0 ? 0.0 : z / z;             // 1, or NaN
-        if (id >= 0 && z != 0.0) {
-            pk = e / z;
-            lp = ((double)t - m) * a.inv_t - log(z);
-        }
-    }
+    double lp, pk, P;                           // log p_k, p_k, their sum (tail: of the warp's, in sh.red)
+    probabilities(a, id, t, t_lse, sh.id, sh.red, lp, pk, P);
     const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
     const bool mine = piece >= p0 && piece < p1;
 
@@ -450,41 +537,9 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
 
     // ---- the row, by one warp for all ----
     if (warp == 0) {
-        Part q[kMaxCluster * kWarps / 32];
-        float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
-#pragma unroll
-        for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
-            q[i] = lane + 32 * i < C * kWarps ? sh.part[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
-            cs = fmaxf(cs, q[i].c);
-            cl = fmaxf(cl, q[i].ct);
-        }
-        cs = max_of_warp(cs);
-        cl = max_of_warp(cl);
-#pragma unroll
-        for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
-            const float w2 = ex2_approx(q[i].c - cs);
-            // far below the reference: nothing, but NaN and infinite sums stay visible
-            S += w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2;
-            E += q[i].E != 0.f ? q[i].E * ex2_approx(q[i].ct - cl) : 0.f;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
-            E += __shfl_xor_sync(0xFFFFFFFFu, E, o);
-        }
-        Known kn;
-        kn.cs = cs;
-        kn.S = S;
-        kn.c_all = fmaxf(cs, cl);
-        kn.to_all = ex2_approx(cs - kn.c_all);
-        kn.all = (S != 0.f ? S * kn.to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - kn.c_all) : 0.f);
         if (tail)
             for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
-        const double r = tail ? 1.0 - P : 0.0;
-        kn.r = r < 0.0 ? 0.0 : r;               // NaN stays
-        kn.none = !tail && P == 0.0;            // the list says nothing: no gradient
-        kn.f = kn.none || S == 0.f ? 0.f : (__fdividef(kn.to_all, kn.all) - __fdividef((float)kn.r, S)) * (float)a.inv_t;
-        kn.c_f = S != 0.f ? cs : -kRefFloor;    // nothing to scale: every exponential is 0
+        const Known kn = known_of(a, sh.part, C * kWarps, P, lane);
         if (lane == 0) sh.known = kn;
     }
     __syncthreads();
@@ -513,39 +568,186 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         }
     }
     // ---- loss and what else the row is told: the first CTA, while the stores are under way ----
-    if (rank == 0) {
-        const float xt = tid < a.K && id >= 0 ? sh.xk[tid] : 0.f;
-        if (warp * 32 < a.K) {
-            double h = 0.0, m = 0.0;
-            if (id >= 0) {
-                if (pk != 0.0) h = pk * (lp - (double)xt * a.inv_t);
-                m = fmin(pk, (double)(ex2_approx((float)((double)xt * (double)a.s - (double)c_all)) / all));
-            }
-            h = warp_sum(h);
-            m = warp_sum(m);
-            if (lane == 0) { sh.red[warp][0] = h; sh.red[warp][1] = m; }
-        }
-        if (state && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
-        __syncthreads();
-        if (tid == 0) {
-            double H = 0.0, accept = 0.0;
-            for (int i = 0; i * 32 < a.K; ++i) { H += sh.red[i][0]; accept += sh.red[i][1]; }
-            const bool ok = all > 0.f && all < CUDART_INF_F && c_all > kRefFloor && c_all < CUDART_INF_F;
-            const double ln_all = kLn2 * log2((double)all);
-            const double lse = ok ? (double)c_all * a.inv_s + ln_all : CUDART_NAN;
-            const float cs = sh.known.cs, S = sh.known.S, to_all = sh.known.to_all;
-            const double r = sh.known.r;
-            double loss = none ? 0.0 : H + P * lse;
-            if (r != 0.0) loss += r * (log(r) - ((double)cs * a.inv_s + kLn2 * log2((double)S) - lse));
-            const double s = (double)S * (double)to_all / (double)all;
-            a.loss[row] = ok ? (float)loss : CUDART_NAN_F;
-            if (a.lse) a.lse[row] = (float)lse;
-            if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
-            if (state) { state[0] = c_f; state[1] = f; state[2] = 0.f; state[3] = 0.f; }
-            if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[row32 / (unsigned)a.L], DSP_ROW_NONFINITE_INPUT);
-        }
-    }
+    if (rank == 0) tell_row(a, row32, id, lp, pk, P, tid < a.K && id >= 0 ? sh.xk[tid] : 0.f, sh.known, sh.red);
     if (tid == 0 && sh.timed_out && a.status) atomicOr(&a.status[row32 / (unsigned)a.L], DSP_ROW_TIMEOUT);
+}
+
+// ---- the loss alone, of many rows: nothing has to stay, so a CTA streams a row of its own (stream_core.cuh) ----
+
+// Takes element e out of a piece and returns it.
+template <typename DT>
+__device__ __forceinline__ float take_out(uint4 &v, int e) {
+    float x = 0.f;
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < Elem<DT>::N; ++i) {
+        if (i != e) continue;
+        x = Elem<DT>::get(v, i);
+        if constexpr (Elem<DT>::N == 8) w[i >> 1] = (i & 1) ? (w[i >> 1] & 0x0000FFFFu) | 0xFF800000u : (w[i >> 1] & 0xFFFF0000u) | 0xFF80u;
+        else w[i] = 0xFF800000u;
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+    return x;
+}
+
+// The sums of a row without the teacher's tokens.  These are sorted by place; every warp walks through them with the tiles, and the thread
+// that has a token takes it out and notes it.
+template <typename DT, typename List>
+struct LossPass {
+    static constexpr bool kOwnTile = true;
+    List &make_list;          // forms the list while the first tiles are under way
+    const int *place;         // elements of the streamed part, ascending, then one behind all
+    float *xk;
+    float s;
+    int token = 0, next = 0;
+    float c = kRefFloor, S = 0.f, ct = kRefFloor, E = 0.f;
+    bool first = true;
+
+    __device__ __forceinline__ LossPass(List &list, const int *pl, float *x, float scale) : make_list(list), place(pl), xk(x), s(scale) {}
+    __device__ __forceinline__ void begin() {
+        make_list();
+        next = place[0];
+    }
+    __device__ __forceinline__ void hand_in() {}
+    __device__ __forceinline__ void add_token(float x) {
+        const float c1 = fmaxf(ct, x * s);
+        E = (E != 0.f ? E * ex2_approx(ct - c1) : 0.f) + ex2_approx((float)((double)x * (double)s - (double)c1));
+        ct = c1;
+    }
+    template <bool RAGGED>
+    __device__ __forceinline__ float tile(const uint4 (&t)[kVpt], int, int tid, int base, float &, unsigned long long &, unsigned long long &) {
+        constexpr int N = Elem<DT>::N;
+        uint4 v[kVpt];
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) v[j] = t[j];
+        for (; next < base + tile_elems<DT>(); next = place[++token]) {
+            const int q = (next - base) / N;                     // the token's piece of the tile
+            if (q % kThreads != tid) continue;
+            float x = 0.f;
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j)
+                if (q / kThreads == j) x = take_out<DT>(v[j], next % N);
+            xk[token] = x;
+            add_token(x);
+        }
+        if (first) {
+            first = false;
+            c = fmaxf(max_of_warp(fmaxf(Elem<DT>::vmax(v[0]), Elem<DT>::vmax(v[1]))) * s, kRefFloor);
+        }
+        float s0 = S, s1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) add_piece<DT>(v[j], s, c, s0, s1);
+        if (__any_sync(0xFFFFFFFFu, !(s0 + s1 < 0x1p64f))) {     // against a new reference, as in sum_pieces
+            float m = Elem<DT>::vmax(v[0]);
+#pragma unroll
+            for (int j = 1; j < kVpt; ++j) m = fmaxf(m, Elem<DT>::vmax(v[j]));
+            const float c1 = fmaxf(max_of_warp(m) * s, c);
+            s0 = S != 0.f ? S * ex2_approx(c - c1) : 0.f;
+            s1 = 0.f;
+#pragma unroll
+            for (int j = 0; j < kVpt; ++j) add_piece<DT>(v[j], s, c1, s0, s1);
+            c = c1;
+        }
+        S = s0 + s1;
+        return 0.f;
+    }
+};
+
+// Shared memory behind the ring: ids, places, logits of the list.
+__host__ __device__ inline int loss_list_words(int K) { return (K + 3) / 4 * 4 + (K + 4) / 4 * 4 + K; }
+
+template <typename DT>
+__global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const DistillArgs a, int inner) {
+    constexpr int N = Elem<DT>::N;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ StreamBars bars;
+    __shared__ __align__(16) Part s_part[kWarps];
+    __shared__ Known s_known;
+    __shared__ double s_red[kWarps][2];
+    __shared__ unsigned s_outer;                 // which of the elements outside of the streamed part are the teacher's
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned row32 = blockIdx.x;
+    const long long row = row32;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        tell_nothing(a, row32);
+        return;
+    }
+    int *ids = reinterpret_cast<int *>(ring + kMinStages * kTileBytes), *place = ids + (a.K + 3) / 4 * 4;
+    float *xk = reinterpret_cast<float *>(place + (a.K + 4) / 4 * 4);
+    const unsigned b = row32 / (unsigned)a.L, l = row32 - b * (unsigned)a.L;
+    const DT *x = reinterpret_cast<const DT *>(a.x) + b * a.sb + l * a.sl;
+    const int head = inner == a.V ? 0 : (int)((N - (reinterpret_cast<uintptr_t>(x) / sizeof(DT)) % N) % N);
+    if (tid == 0) s_outer = 0u;
+    stream_begin(bars, kMinStages);
+
+    int id = -1, rank = -1;
+    float outer_x = -CUDART_INF_F, x_mine = 0.f; // an element outside of the streamed part; the slot's token, if it is one of those
+    double lp, pk, P;
+    auto list = [&]() {
+        float t = -CUDART_INF_F;
+        const float t_lse = a.tlse ? a.tlse[row] : 0.f;
+        if (tid < a.K) {
+            id = a.id[row * a.K + tid];
+            t = a.val[row * a.K + tid];
+            const int n = a.count ? a.count[row] : a.K;
+            if (tid >= n || id < 0 || id >= a.V) id = -1;
+        }
+        if (tid < a.V - inner) outer_x = Elem<DT>::load1(x + (tid < head ? tid : inner + tid));
+        if (tid < (a.K + 3) / 4 * 4) ids[tid] = id;
+        __syncthreads();
+        probabilities(a, id, t, t_lse, ids, s_red, lp, pk, P);
+        __syncthreads();
+        const bool in = id >= head && id < head + inner;
+        if (tid < (a.K + 3) / 4 * 4) ids[tid] = in ? id : 0x7FFFFFFF;
+        if (id >= 0 && !in) {
+            atomicOr(&s_outer, 1u << (id < head ? id : id - inner));
+            x_mine = Elem<DT>::load1(x + id);
+        }
+        __syncthreads();
+        if (in) {
+            const int4 *all = reinterpret_cast<const int4 *>(ids);
+            rank = 0;
+            for (int j = 0; j * 4 < a.K; ++j) {
+                const int4 o = all[j];
+                rank += (o.x < id) + (o.y < id) + (o.z < id) + (o.w < id);
+            }
+            place[rank] = id - head;
+        }
+        const int used = __syncthreads_count(in);
+        if (tid == 0) place[used] = 0x7FFFFFFF;
+        __syncthreads();
+    };
+    LossPass<DT, decltype(list)> pass(list, place, xk, a.s);
+    ColTop top;
+    ColSums cs;
+    stream_slice<DT, true>(x + head, 0, inner, kMinStages, bars, ring, top, cs, pass);
+    if (id >= 0 && rank < 0) pass.add_token(x_mine);
+    if (warp == 0) {                             // the elements outside of the streamed part
+        const bool other = lane < a.V - inner && !(s_outer >> lane & 1u);
+        const float c1 = fmaxf(max_of_warp(other ? outer_x * a.s : kRefFloor), pass.c);
+        pass.S = pass.S != 0.f ? pass.S * ex2_approx(pass.c - c1) : 0.f;
+        if (other) pass.S += ex2_approx(fmaf(outer_x, a.s, -c1));
+        pass.c = c1;
+    }
+    Part part = {pass.c, sum_of_warp(pass.S), max_of_warp(pass.ct), 0.f};
+    part.E = sum_of_warp(pass.E != 0.f ? pass.E * ex2_approx(pass.ct - part.ct) : 0.f);
+    if (lane == 0) s_part[warp] = part;
+    __syncthreads();
+    if (warp == 0) {
+        if (a.tlse)
+            for (int i = 0; i * 32 < a.K; ++i) P += s_red[i][0];
+        const Known kn = known_of(a, s_part, kWarps, P, lane);
+        if (lane == 0) s_known = kn;
+    }
+    __syncthreads();
+    const float xt = id < 0 ? 0.f : rank < 0 ? x_mine : xk[rank];
+    if (a.state && id >= 0) {
+        const float q = __fdividef(ex2_approx((float)((double)xt * (double)a.s - (double)s_known.c_all)), s_known.all);
+        a.state[row * (a.K + 4) + 4 + tid] = s_known.none ? 0.f : (float)(((double)q - pk) * a.inv_t);
+    }
+    tell_row(a, row32, id, lp, pk, P, xt, s_known, s_red);
+    if (tid == 0 && bars.timed_out && a.status) atomicOr(&a.status[b], DSP_ROW_TIMEOUT);
 }
 
 // The gradient from what dsp_distill left of the row: c, f and the K elements.
@@ -641,6 +843,19 @@ int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     return DSP_OK;
 }
 
+constexpr int kLongRow = 75000;
+int32_t launch_distill_loss(const DistillArgs &a, long long rows, cudaStream_t st) {
+    using DT = __nv_bfloat16;
+    constexpr int N = Elem<DT>::N;
+    // elements of a row that are streamed: all of it where every row starts on 16 bytes, else the pieces that lie inside it at any start
+    const int inner = stream_layout_ok<DT>(a.x, a.V, a.sb, a.sl) ? a.V : (a.V - (N - 1)) / N * N;
+    static std::atomic<unsigned long long> smem_done{0};
+    DSP_CUDA_TRY(allow_shared(distill_loss_kernel<DT>, kMinStages * kTileBytes + loss_list_words(DSP_MAX_TEACHER) * 4, smem_done));
+    distill_loss_kernel<DT><<<(unsigned)rows, kThreads, (size_t)(kMinStages * kTileBytes + loss_list_words(a.K) * 4), st>>>(a, inner);
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
 template <typename DT>
 int32_t launch_distill_grad(DistillGradArgs &a, long long rows, cudaStream_t st) {
     const int n = pieces_at_most(a.V, Elem<DT>::N);
@@ -693,6 +908,10 @@ extern "C" int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_
     a.status = row_status;
     const long long rows = (long long)B * L;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    // The loss alone of many long bf16 rows streams each in a CTA; measured with the gradient's call behind it, K = 16 (us, streamed / by
+    // clusters): 600 rows of 100000 76 / 90, of 200000 131 / 146, of 64000 57 / 55; 148 rows of 152064 32 / 33, 32 rows 22 / 13;
+    // fp32 (half the logits for the same bytes, the same work a tile) 600 rows of 100000 152 / 137.
+    if (!grad && dtype == DSP_BF16 && rows >= device_sm_count() && V >= kLongRow) return launch_distill_loss(a, rows, st);
     if (dtype == DSP_BF16)
         return grad ? launch_distill<__nv_bfloat16, true>(a, rows, st) : launch_distill<__nv_bfloat16, false>(a, rows, st);
     return grad ? launch_distill<float, true>(a, rows, st) : launch_distill<float, false>(a, rows, st);
