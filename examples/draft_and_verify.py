@@ -3,16 +3,20 @@
 One step, whose lengths stay on the device (the host reads the emitted tokens, and with a tree whether any
 accepted node lies off the first beam): the drafter sees its block of masks from both sides over its cache
 ("full" attention), its logits become a lattice and a path (or the beams' token tree), the target passes
-over the path ("causal") or the tree (the plan's visibility bits) once, the verification accepts a part,
-and the lengths move by it; what was drafted beyond is written over by the next step.
+over the path ("causal") or the tree (the plan's visibility bits) once, the verification accepts a part (a
+tree's accepted nodes move behind the last kept token), and the lengths move by it; what was drafted beyond is
+written over by the next step.  Between steps a request may fork or end (`fork`), and the drafter may learn from
+the target's rows of the last verification (`lesson`).
 
     dsp_cache_plan -> projections -> dsp_kv4_append -> dsp_attn_kv4 -> ... -> logits
-    dsp_lattice_build -> dsp_cps_search (-> dsp_beam_tree) -> dsp_verify / dsp_verify_tree
+    dsp_lattice_build -> dsp_cps_search (-> dsp_beam_tree) -> dsp_verify / dsp_verify_tree (-> dsp_kv4_compact)
+    dsp_cache_fork -> dsp_kv4_copy
+    dsp_token_logprobs (the teacher's list) -> dsp_distill (loss and gradient)
 
 The projections are PyTorch matrix products.  Both models lean towards one fixed chain of tokens, which
 stands in for what training would have taught them to agree on.
 
-    python examples/draft_and_verify.py [--tree] [--steps 16] [--batch 4]
+    python examples/draft_and_verify.py [--tree] [--fork] [--learn] [--steps 16] [--batch 4]
 """
 from __future__ import annotations
 
@@ -41,13 +45,22 @@ class Pool:
         self.block_table, self.free_ring = torch.zeros((B, width), **i32), torch.arange(n, **i32)
         self.ring_pos = torch.tensor([0, n], dtype=torch.int64, device=dev)
         self.block_count, self.seq_len = torch.zeros(B, **i32), torch.zeros(B, **i32)
-        self.layers = [dsp.kv4_cache(n, HKV, D, PAGE, dev) for _ in range(LAYERS)]
+        self.cache = dsp.kv4_cache(n, HKV, D, PAGE, dev, LAYERS)
+        self.layers = list(self.cache)
 
     def plan(self, new_len: torch.Tensor, T: int, tree: SimpleNamespace = None) -> SimpleNamespace:
         p = dsp.dsp_cache_plan(self.seq_len, new_len, self.block_count, self.ring_pos, self.block_table, self.free_ring, PAGE, T,
                                node_parent=tree.node_parent if tree else None, node_depth=tree.node_depth if tree else None)
         self.block_count, self.ring_pos = p.block_count, p.ring_pos
         return p
+
+    def fork(self, src: torch.Tensor):
+        """Row r continues what row src[r] holds (-1: it ends)."""
+        table = torch.empty_like(self.block_table)
+        f = dsp.dsp_cache_fork(src, None, self.seq_len, self.block_count, self.ring_pos, self.block_table, self.free_ring, PAGE, table)
+        dsp.dsp_kv4_copy(self.cache, D, f.copy_src, f.copy_dst, f.copy_len)
+        self.block_table, self.block_count, self.seq_len, self.ring_pos = table, f.block_count, f.seq_len, f.ring_pos
+        return f
 
 
 class Model:
@@ -83,7 +96,8 @@ class Model:
             x = x + o.view(B * n, HQ * D) @ w.out
             x = x + torch.nn.functional.silu(self.norm(x) @ w.up) @ w.down
         at = (p.cu_new[:-1, None] + torch.arange(n, device=tokens.device)).clamp_max(B * n - 1).long()
-        return self.norm(x)[at].float() @ self.head
+        self.hidden = self.norm(x)[at].float()
+        return self.hidden @ self.head
 
     def leaning(self, logits: torch.Tensor, to: torch.Tensor) -> torch.Tensor:
         return logits.scatter_add(-1, to[..., None].long(), torch.full(to.shape + (1,), self.lean, device=to.device))
@@ -137,6 +151,7 @@ class Decoder:
             guess.append(self.chain[guess[-1].long()])
         logits = logits.gather(1, block[..., None].expand(-1, -1, VOCAB))
         logits = self.drafter.leaning(logits, torch.stack(guess, 1))
+        self.drafted = logits, self.drafter.hidden.gather(1, block[..., None].expand(-1, -1, WIDTH))
         lat = dsp.dsp_lattice_build(logits, self.K)
         cps = dsp.dsp_cps_search(lat, self.last, self.proxy, W=self.W, lam=0.9, table_log2=10, V=VOCAB, row_status=lat.row_status)
         return lat, cps
@@ -149,7 +164,7 @@ class Decoder:
             tokens = torch.cat([last, cps.path.clamp_min(0)], 1)
             logits = self.target.leaning(self.target.forward(tokens, 1 + cps.path_len), self.chain[tokens.long()])
             ver = dsp.dsp_verify(logits, None, cps, None, all_greedy=True, row_status=lat.row_status)
-            accepted, path, in_place = ver.accepted_len, cps.path, ver.accepted_len
+            accepted, path = ver.accepted_len, cps.path
         else:
             t = dsp.dsp_beam_tree(cps)
             tokens = torch.cat([last, t.node_token.clamp_min(0)], 1)
@@ -157,18 +172,34 @@ class Decoder:
             ver = dsp.dsp_verify_tree(logits, t, self.L)
             accepted = ver.accepted_len
             path = t.node_token.gather(1, ver.accepted_node.clamp_min(0).long())
-            i = torch.arange(self.L, device=self.dev)
-            in_place = ((ver.accepted_node == i) & (i < accepted[:, None])).int().cumprod(1).sum(1).int()
-        pool.seq_len = pool.seq_len + 1 + in_place
-        if tree:                                                                   # accepted nodes off the first beam: passed over once more
-            rest = accepted - in_place
-            if int(rest.max()) > 0:
-                at = (in_place[:, None] + torch.arange(self.L, device=self.dev)).clamp_max(self.L - 1)
-                self.target.forward(path.gather(1, at.long()).clamp_min(0), rest)
-                pool.seq_len = pool.seq_len + rest
+            dsp.dsp_kv4_compact(pool.cache, D, pool.block_table, pool.seq_len, ver.accepted_node, accepted)
+        self.rows, self.path, self.right = logits[:, :self.L], cps.path, (cps.path == path).int().cumprod(1).sum(1).minimum(accepted)
+        pool.seq_len = pool.seq_len + 1 + accepted
         new = torch.cat([path.clamp_min(0), path[:, :1]], 1).scatter(1, accepted[:, None].long(), ver.next_token[:, None])
         self.emit(new, accepted + 1)
         return accepted
+
+
+    def fork(self, src):
+        """Request r goes on from where request src[r] is (-1: it ends, and its place stays empty)."""
+        src_t = torch.tensor(src, dtype=torch.int32, device=self.dev)
+        for pool in (self.target.pool, self.drafter.pool):
+            pool.fork(src_t)
+        at = src_t.clamp_min(0).long()
+        self.last, self.pending, self.pending_len = self.last[at], self.pending[at], self.pending_len[at]
+        self.texts = [list(self.texts[s]) if s >= 0 else [] for s in src]
+        self.margins = [list(self.margins[s]) if s >= 0 else [] for s in src]
+
+    def lesson(self, K: int = 16, temperature: float = 1.0) -> SimpleNamespace:
+        """What the drafter can learn from the last step: its block against the target's rows of the best path, whose positions count up to
+        the first token that the target did not take.  Returns loss and accept [B, L] and the gradient for the drafter's head."""
+        logits, hidden = self.drafted
+        n = (self.right + 1).clamp_max(self.L).int()                               # rows that follow accepted tokens
+        teacher = dsp.dsp_token_logprobs(self.rows, self.path, K=K, temperature=temperature, row_len=n)
+        weight = (torch.arange(self.L, device=self.dev) < n[:, None]).float() / n.sum()
+        r = dsp.dsp_distill(logits, teacher.top_id, teacher.top_logit, teacher_lse=teacher.lse, weight=weight, temperature=temperature, grad=True)
+        return SimpleNamespace(loss=r.loss, accept=r.accept, weight=weight, teacher=teacher, grad=r.grad,
+                               head=hidden.flatten(0, 1).t() @ r.grad.flatten(0, 1))
 
 
 def prompts(B: int, longest: int, seed: int, dev="cuda"):
@@ -182,13 +213,21 @@ def prompts(B: int, longest: int, seed: int, dev="cuda"):
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--tree", action="store_true", help="verify the beams' token tree instead of the best path")
+    ap.add_argument("--fork", action="store_true", help="halfway, the last request ends and its place goes on from the first one")
+    ap.add_argument("--learn", action="store_true", help="after every step the drafter's head learns from the target's rows")
     ap.add_argument("--steps", type=int, default=16)
     ap.add_argument("--batch", type=int, default=4)
     a = ap.parse_args()
     d = Decoder(a.batch, 128 + a.steps * 9 + 64)
     d.prompt(*prompts(a.batch, 100, 7))
     for s in range(a.steps):
+        if a.fork and s == a.steps // 2:
+            d.fork(list(range(a.batch - 1)) + [0])
         print("step %2d: accepted %s" % (s, d.step(a.tree).tolist()))
+        if a.learn:
+            r = d.lesson()
+            d.drafter.head -= 0.5 * r.head
+            print("         loss %.4f, acceptance within %.3f" % (float((r.loss * r.weight).sum()), float((r.accept * r.weight).sum())))
     for b, text in enumerate(d.texts):
         print("request %d: %d tokens in %d steps: %s ..." % (b, len(text), a.steps, text[:12]))
 

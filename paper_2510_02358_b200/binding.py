@@ -836,9 +836,10 @@ def dsp_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, *, q_weight: Optional[tor
     return q_out, k_out
 
 
-def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device) -> torch.Tensor:
-    """An empty 4-bit cache."""
-    return torch.zeros((n_blocks, Hkv, page_size * (D + 8)), dtype=torch.uint8, device=device)
+def kv4_cache(n_blocks: int, Hkv: int, D: int, page_size: int, device, layers: Optional[int] = None) -> torch.Tensor:
+    """An empty 4-bit cache, or ``layers`` of them in one tensor (for dsp_kv4_copy and dsp_kv4_compact; [i] is layer i's)."""
+    one = (n_blocks, Hkv, page_size * (D + 8))
+    return torch.zeros(one if layers is None else (layers,) + one, dtype=torch.uint8, device=device)
 
 
 def _cache(cache: torch.Tensor, Hkv: int, D: int, dev):
