@@ -6,15 +6,20 @@
 //      order does not matter); every input entry marks the first place that names the block;
 //   2. each output row sees whether its partly filled block is its own, each input row counts the blocks that nobody holds;
 //   3. a prefix sum over the rows (formed by every CTA) gives the places in the ring; tables and lists are written.
-// A warp takes a row at a time, with four table entries a lane under way.  Few entries and blocks: one CTA runs all parts, with the marks in
+// A warp takes a row at a time, with four table entries a lane under way.  Few rows and blocks: one CTA runs all parts, with the marks in
 // shared memory and barriers between; many: a fill and three launches, each started early and waiting for the one before.
+//
+// The bytes are nothing (512 requests of 8192 tokens: 0.6 MB); what bounds the call is the chain of dependent reads (row, table, mark) in each
+// part and the launches.  Measured: 4 requests 5.0 us, 16 7.6, 64 9.3, 500 10.6.
 #include "dsp_common.cuh"
 
 namespace dsp {
 namespace {
 
 constexpr int kNobody = 0x7F7F7F7F;              // what a fill with bytes leaves
-constexpr long long kOneCtaSteps = 32 * 16;      // rows times warp-wide table reads up to which one CTA is taken
+// Rows (old and new ones) up to which one CTA is taken: two rounds of its 32 warps.  Measured (us, one CTA / launches): 4 + 4 rows of 500 tokens
+// 5.0 / 10.3, 16 + 16 of 8000 12.8 / 27.8, 32 + 32 of 500 9.5 / 9.3, of 2000 10.3 / 12.2, 40 + 40 of 500 11.2 / 9.3, 64 + 64 13.2 / 9.5, 500 + 500 67 / 10.6.
+constexpr long long kOneCtaRows = 64;
 constexpr int kOneCtaShared = 200 * 1024;
 constexpr int kU = 4;                            // entries a lane has under way
 
@@ -260,7 +265,7 @@ ForkWs fork_ws(int Bi, int Bo, int n_blocks) {
 int32_t launch_fork(const ForkArgs &a, size_t mark_bytes, cudaStream_t st) {
     const long long rows = (long long)a.Bi + a.Bo;
     const long long one = one_cta_bytes(a.Bi, a.Bo, a.n_blocks);
-    if (rows * ((a.width + 31) / 32) <= kOneCtaSteps && one <= kOneCtaShared) {
+    if (rows <= kOneCtaRows && one <= kOneCtaShared) {
         static std::atomic<unsigned long long> done{0};
         if (one > 48 * 1024) DSP_CUDA_TRY(allow_shared(fork_kernel, kOneCtaShared, done));
         const unsigned threads = rows <= 8 ? 256u : 1024u;       // a warp for each row
