@@ -1,6 +1,6 @@
 // dsp_kv4_copy, dsp_kv4_compact: bytes of the 4-bit cache move, for all layers of a model in one launch.
 //
-// A copy of a block is one piece of memory a head (the runs up to the copied tokens), moved by a warp 16 bytes a lane.  A token is no
+// A copy of a block is one piece of memory a head (the runs up to the copied tokens); a warp moves a run, 16 bytes a lane.  A token is no
 // such piece: its codes are cut into the places of a matrix instruction's fragments (kv4.cuh), D / 4 words of 4 bytes and its scales and
 // offsets.  The same lane always takes the same word of a token, so the moves of a request need no barrier: a lane's reads and writes of
 // one address come in its own order, and since the accepted nodes grow along the path no target lies behind a later source.
@@ -14,50 +14,47 @@ constexpr int kMoveThreads = 256;
 struct CopyArgs {
     uint8_t *cache;
     long long layer_stride, head_bytes;      // bytes from layer to layer; of one head of one block
-    int layers, n_blocks, page, Hkv, run_bytes;
+    int layers, n_blocks, page, Hkv, runs;   // runs of a block
     const int32_t *src, *dst, *len;
     int N;
 };
 
-// A warp looks at 32 units (entry, layer, head) at a time, which lie a grid apart, and copies those that name two blocks.
+// A unit is a run of 16 tokens of an entry, layer and head.  A warp looks at 32 units at a time, which lie a grid apart, and copies those
+// that count, each with all of its reads under way at once.
+template <int D>
 __global__ void __launch_bounds__(kMoveThreads) kv4_copy_kernel(const CopyArgs a) {
+    constexpr int kVecs = Kv4<D>::kRunBytes / 16, kU = (kVecs + 31) / 32;
     const int lane = threadIdx.x & 31;
     const long long warp = ((long long)blockIdx.x * kMoveThreads + threadIdx.x) >> 5, warps = ((long long)gridDim.x * kMoveThreads) >> 5;
-    const int per = a.layers * a.Hkv;
-    const long long units = (long long)a.N * per;
+    const long long per = (long long)a.layers * a.Hkv * a.runs, units = a.N * per;
     for (long long u0 = warp; u0 < units; u0 += warps * 32) {
         const long long u = u0 + warps * lane;
         const uint8_t *from = nullptr;
         uint8_t *to = nullptr;
-        int vecs = 0;
         if (u < units) {
-            const int i = (int)(u / per), rest = (int)(u - (long long)i * per), layer = rest / a.Hkv, h = rest - layer * a.Hkv;
-            const int s = a.src[i], d = a.dst[i];
-            if (s >= 0 && s < a.n_blocks && d >= 0 && d < a.n_blocks) {
-                const int n = a.len ? min(max(a.len[i], 0), a.page) : a.page;
-                uint8_t *base = a.cache + layer * a.layer_stride + h * a.head_bytes;
-                from = base + s * a.head_bytes * a.Hkv;
-                to = base + d * a.head_bytes * a.Hkv;
-                vecs = (n + 15) / 16 * (a.run_bytes / 16);
+            const int i = (int)(u / per);
+            const unsigned rest = (unsigned)(u - i * per), unit = rest / (unsigned)a.runs;
+            const int run = (int)(rest - unit * (unsigned)a.runs), layer = (int)(unit / (unsigned)a.Hkv), h = (int)unit - layer * a.Hkv;
+            const int s = a.src[i], d = a.dst[i], n = a.len ? a.len[i] : a.page;
+            if (s >= 0 && s < a.n_blocks && d >= 0 && d < a.n_blocks && run * 16 < n) {
+                uint8_t *base = a.cache + layer * a.layer_stride + (long long)run * Kv4<D>::kRunBytes;
+                from = base + ((long long)s * a.Hkv + h) * a.head_bytes;
+                to = base + ((long long)d * a.Hkv + h) * a.head_bytes;
             }
         }
-        unsigned some = __ballot_sync(0xFFFFFFFFu, vecs > 0);
+        unsigned some = __ballot_sync(0xFFFFFFFFu, from != nullptr);
         while (some) {
             const int k = __ffs(some) - 1;
             some &= some - 1;
-            const int n = __shfl_sync(0xFFFFFFFFu, vecs, k);
-            const uint4 *p = reinterpret_cast<const uint4 *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(from), k));
-            uint4 *q = reinterpret_cast<uint4 *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), k));
-            constexpr int kU = 8;
-            for (int v0 = lane; v0 < n; v0 += 32 * kU) {
-                uint4 r[kU];
+            const uint4 *p = reinterpret_cast<const uint4 *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(from), k)) + lane;
+            uint4 *q = reinterpret_cast<uint4 *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), k)) + lane;
+            uint4 r[kU];
 #pragma unroll
-                for (int j = 0; j < kU; ++j)
-                    if (v0 + 32 * j < n) r[j] = p[v0 + 32 * j];
+            for (int j = 0; j < kU; ++j)
+                if (lane + 32 * j < kVecs) r[j] = p[32 * j];
 #pragma unroll
-                for (int j = 0; j < kU; ++j)
-                    if (v0 + 32 * j < n) q[v0 + 32 * j] = r[j];
-            }
+            for (int j = 0; j < kU; ++j)
+                if (lane + 32 * j < kVecs) q[32 * j] = r[j];
         }
     }
 }
@@ -162,12 +159,15 @@ extern "C" int32_t dsp_kv4_copy(void *cache, int32_t layers, int64_t layer_strid
     a.cache = static_cast<uint8_t *>(cache);
     a.layer_stride = layers > 1 ? layer_stride : 0;
     a.head_bytes = (long long)page_size * (D + 8);
-    a.layers = layers; a.n_blocks = n_blocks; a.page = page_size; a.Hkv = Hkv; a.run_bytes = 16 * (D + 8);
+    a.layers = layers; a.n_blocks = n_blocks; a.page = page_size; a.Hkv = Hkv; a.runs = page_size / 16;
     a.src = copy_src; a.dst = copy_dst; a.len = copy_len; a.N = N;
-    const long long warps = (long long)N * layers * Hkv;
+    if ((long long)layers * Hkv * a.runs > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
+    const long long warps = (long long)N * layers * Hkv * a.runs;
     long long grid = (warps + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     if (grid > 148 * 4) grid = 148 * 4;
-    kv4_copy_kernel<<<(unsigned)grid, kMoveThreads, 0, reinterpret_cast<cudaStream_t>(stream)>>>(a);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (D == 64) kv4_copy_kernel<64><<<(unsigned)grid, kMoveThreads, 0, st>>>(a);
+    else kv4_copy_kernel<128><<<(unsigned)grid, kMoveThreads, 0, st>>>(a);
     DSP_CUDA_TRY(cudaGetLastError());
     return DSP_OK;
 }
