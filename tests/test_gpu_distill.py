@@ -266,3 +266,20 @@ def test_an_autograd_function_over_the_two_calls():
     # each is within (2 rel + one + 4 half steps) of q + p (and of r times the others' share, below q + p here): twice that apart
     rel, one = bounds(x, 1.0, 2000)
     assert ((leaf.grad - want).abs().double() <= 2 * (2 * rel + one + 2.0 ** -22)[..., None] * up.double()[..., None]).all()
+
+
+@pytest.mark.parametrize("B,L,V,dtype,grad", [(3, 20, 32003, F32, True), (3, 20, 32003, BF, False), (1, 16, 152064, BF, True), (4, 64, 80000, BF, False)])
+def test_small_losses_are_exact(B, L, V, dtype, grad):
+    """A drafter next to its teacher: dloss = (s - r) dS / S for an error dS of the other tokens' sum, the list's own part is formed in 64 bits,
+    and the result is rounded to 32."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    t = 2.0 * torch.randn(B, L, V, generator=g, device="cuda")
+    t.scatter_add_(2, torch.randint(0, V, (B, L, 3), generator=g, device="cuda"), 6 + 3 * torch.rand(B, L, 3, generator=g, device="cuda"))
+    top = t.topk(8, -1)
+    ids, val, lse = top.indices.int(), top.values, t.double().logsumexp(-1).float()
+    x = (t + 0.1 * torch.randn(B, L, V, generator=g, device="cuda")).to(dtype)
+    want = ref.distill(x, ids, val, 1.0, lse)[0]
+    r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=grad)
+    _, use, rest = ref.teacher(val, 1.0, ids, V, lse)
+    q = torch.log_softmax(x.double(), -1).gather(-1, ids.long()).exp().sum(-1)
+    near(r.loss, want, (1 - q - rest).abs() * bounds(x, 1.0, V)[0] + 2.0 ** -24 * want.abs() + 1e-12, "loss")
