@@ -954,6 +954,11 @@ def _rows(name: str, t: torch.Tensor, like=None):
     return B, L, V, (t.stride(0) if B > 1 else L * sl), sl
 
 
+def _alike(n: int, dtype, dev, B: int, *rest: int):
+    """n tensors of one shape from one allocation (on the host, half the time of n)."""
+    return torch.empty(n * B, *rest, dtype=dtype, device=dev).unsafe_split_with_sizes((B,) * n)
+
+
 def _maybe(name: str, t: Optional[torch.Tensor], shape, dtype, dev):
     return None if t is None else _ints(name, t, shape, dtype, dev).data_ptr()
 
@@ -989,10 +994,20 @@ def dsp_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = No
     lens = _maybe("row_len", row_len, (B,), i32, dev)
     if out is None:
         e = torch.empty
-        out = SimpleNamespace(logp=e(shape, dtype=f32, device=dev) if G else None, rank=e(B, L, dtype=i32, device=dev) if G else None,
-                              top_id=e(B, L, K, dtype=i32, device=dev) if K else None, top_logit=e(B, L, K, dtype=f32, device=dev) if K else None,
-                              top_logp=e(B, L, K, dtype=f32, device=dev) if K else None, lse=e(B, L, dtype=f32, device=dev),
-                              entropy=e(B, L, dtype=f32, device=dev), row_status=e(B, dtype=i32, device=dev))
+        logp = rank = top_id = top_logit = top_logp = None
+        if len(shape) == 2:
+            lse, entropy, logp = _alike(3, f32, dev, B, L)
+        else:
+            lse, entropy = _alike(2, f32, dev, B, L)
+            if G:
+                logp = e(shape, dtype=f32, device=dev)
+        if G:
+            rank = e(B, L, dtype=i32, device=dev)
+        if K:
+            top_id = e(B, L, K, dtype=i32, device=dev)
+            top_logit, top_logp = _alike(2, f32, dev, B, L, K)
+        out = SimpleNamespace(logp=logp, rank=rank, top_id=top_id, top_logit=top_logit, top_logp=top_logp, lse=lse, entropy=entropy,
+                              row_status=e(B, dtype=i32, device=dev))
     else:
         if G:
             _ints("out.logp", out.logp, shape, f32, dev)
@@ -1020,7 +1035,8 @@ def dsp_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = No
 def _grad_rows(grad, logits: torch.Tensor):
     """(tensor, strides) of the gradient that a call writes: a new one for True, else the caller's (the logits themselves, if wanted)."""
     if grad is True:
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        _, L, V = logits.shape
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), L * V, V
     _, _, _, sb, sl = _rows("grad", grad, logits)
     return grad, sb, sl
 
@@ -1055,8 +1071,7 @@ def dsp_distill(student: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
         state = None
     else:
         _ints("state", state, (B, L, K + 4), f32, dev)
-    e = torch.empty
-    loss, accept, lse = e(B, L, dtype=f32, device=dev), e(B, L, dtype=f32, device=dev), e(B, L, dtype=f32, device=dev)
+    loss, accept, lse = _alike(3, f32, dev, B, L)
     _check("dsp_distill", lib().dsp_distill(
         student.data_ptr(), dt, B, L, V, sb, sl, teacher_id.data_ptr(), teacher_logit.data_ptr(), lse_in, count, K, temperature, w,
         loss.data_ptr(), accept.data_ptr(), lse.data_ptr(), _at(state), _at(grad), gb, gl, status, _queue(dev)))
