@@ -11,6 +11,7 @@
 //
 // The bytes are nothing (512 requests of 8192 tokens: 0.6 MB); what bounds the call is the chain of dependent reads (row, table, mark) in each
 // part and the launches.  Measured: 4 requests 5.0 us, 16 7.6, 64 9.3, 500 10.6.
+// A cluster of 16 CTAs instead of the fill and the launches: 512 requests of 8192 tokens 21 us instead of 15.
 #include "dsp_common.cuh"
 
 namespace dsp {
