@@ -98,7 +98,7 @@ __device__ __forceinline__ int warp_scan_incl(int v, int lane) {
 
 // The finish of a row by all threads of a CTA.  On entry stash[s * kThreads + tid] holds the column
 // records of every slice (behind the FinishSmem in `smem`), the row's warp sums are in wp_own
-// (a row of one slice, shared memory) or in ws.wpart (global memory), and a block-wide barrier
+// (shared memory, all slices') or, wp_own null, in ws.wpart (global memory), and a block-wide barrier
 // lies between this call and the last use of `smem` for anything else.  Returns true in warp 0.
 template <typename DT>
 __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums, long long row, int nslices,
@@ -136,7 +136,7 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
         float c;
         double S, T;
         if (wp_own) {
-            warp_merge_partials([&](int i) { return wp_own[i]; }, kWarps, lane, c, S, T);
+            warp_merge_partials([&](int i) { return wp_own[i]; }, nslices * kWarps, lane, c, S, T);
         } else {
             const WarpPartial *wp = ws.wpart + row * nslices * kWarps;
             warp_merge_partials([&](int i) {

@@ -33,6 +33,7 @@ struct ScoreArgs {
     int nslices, ntiles_row, nstages;
     RowScratch rs;
     unsigned *rank_acc;       // [rows] zeroed per call
+    bool own_status;          // a row is all of its status word: written, else OR-ed into
 };
 
 // The number just below x (NaN below -inf: everything exceeds it).
@@ -189,6 +190,7 @@ struct TokenPass {
 
 // A row that is not read.
 __device__ void score_nothing(const ScoreArgs &a, long long row, int lane) {
+    if (a.own_status && lane == 0) a.row_status[row] = 0u;
     for (int i = lane; i < a.G; i += 32) a.logp[row * a.G + i] = -CUDART_INF_F;
     if (lane < a.K) {
         a.top_id[row * a.K + lane] = -1;
@@ -202,10 +204,11 @@ __device__ void score_nothing(const ScoreArgs &a, long long row, int lane) {
     }
 }
 
-// The finish of a row by one warp: the elements outside of the streamed pieces join, and everything is written.
+// The finish of a row by one warp: the elements outside of the streamed pieces join, and everything is written (counted: of the streamed
+// logits, how many come before the first token; trouble: status bits so far).
 template <typename DT>
 __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *rowp, int head, const TokenPass<DT> &pass, RowResult r,
-                          int lane) {
+                          unsigned counted, uint32_t trouble, int lane) {
     constexpr int N = Elem<DT>::N;
     // one element a lane: before the streamed pieces, then behind them
     const int extra = a.V - a.inner;
@@ -248,15 +251,16 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
             int n = lane < extra && (x > pass.xt || (x == pass.xt && v < pass.tok)) ? 1 : 0;
             const int u = head + pass.vec * N + lane;
             if (pass.tok >= head && pass.tok < head + a.inner && lane < N && u < pass.tok && pass.x_piece == pass.xt) ++n;
-            rank = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
-            if (lane == 0) rank += (int)atomicAdd(pass.acc, 0u);
+            rank = (int)(__reduce_add_sync(0xFFFFFFFFu, (unsigned)n) + counted);
         }
         if (lane == 0) a.rank[row] = rank;
     }
     if (lane == 0) {
         a.lse[row] = (float)lse;
         if (a.entropy) a.entropy[row] = bad ? CUDART_NAN_F : (float)(kLn2 * log_s - T / S * a.inv_s);
-        if (bad) atomicOr(&a.row_status[b], DSP_ROW_NONFINITE_INPUT);
+        if (bad) trouble |= DSP_ROW_NONFINITE_INPUT;
+        if (a.own_status) a.row_status[b] = trouble;
+        else if (trouble) atomicOr(&a.row_status[b], trouble);
     }
 }
 
@@ -345,7 +349,95 @@ __global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
         grid_dependency_wait();
         r.key = 0ull; r.c = kRefFloor; r.S = 0.0; r.T = 0.0; r.nonfinite = false;
     }
-    score_row<DT>(a, row, b, rowp, pass.head, pass, r, lane);
+    const unsigned counted = pass.ranked && pass.tok >= 0 && a.inner && lane == 0 ? atomicAdd(pass.acc, 0u) : 0u;
+    score_row<DT>(a, row, b, rowp, pass.head, pass, r, counted, 0u, lane);
+}
+
+// ---- few rows: the CTAs of a row are a cluster and hand what they found to the first one, which finishes the row; no tickets, so nothing
+// has to be prepared where a status word belongs to one row ----
+constexpr int kMaxCluster = 8;
+constexpr int kClusterTiles = 4;             // tiles of a CTA, all in its ring at once
+constexpr int kFinishArea = kFinishBytes + kMaxCluster * kThreads * 8;
+struct HandIn {                              // in the first CTA
+    __align__(8) WarpPartial wp[kMaxCluster * kWarps];
+    unsigned counted[kMaxCluster * kWarps];
+    unsigned timed_out[kMaxCluster];
+};
+__device__ __forceinline__ void put_remote(uint32_t addr, unsigned long long v) {
+    asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, unsigned v) {
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+template <typename DT>
+__global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreArgs a) {
+    constexpr int N = Elem<DT>::N;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ StreamBars bars;
+    __shared__ HandIn hand;
+    const unsigned C = (unsigned)a.nslices, row32 = blockIdx.x / C, rank = cluster_rank();
+    const long long row = row32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int b = (int)(row32 / (unsigned)a.L), l = (int)(row32 - (unsigned)b * (unsigned)a.L);
+    if (a.row_len && l >= a.row_len[b]) {                // the whole cluster alike
+        if (rank == 0 && warp == 0) score_nothing(a, row, lane);
+        return;
+    }
+    cluster_arrive_empty();
+    const DT *rowp = reinterpret_cast<const DT *>(a.logits) + b * a.stride_b + l * a.stride_l;
+    const int head = a.inner == a.V ? 0 : (int)((N - (reinterpret_cast<uintptr_t>(rowp) / sizeof(DT)) % N) % N);
+    TokenPass<DT> pass;
+    pass.row = rowp;
+    pass.tokens = a.tokens + row * a.G;
+    pass.G = a.G;
+    pass.ranked = a.rank != nullptr;
+    pass.acc = nullptr;
+    pass.s = a.s; pass.low = a.low;
+    pass.V = a.V; pass.head = head; pass.inner = a.inner;
+    stream_begin(bars, a.nstages);
+    int s0, s1;
+    slice_range<DT>((int)rank, (int)C, a.ntiles_row, a.inner, s0, s1);
+    ColTop top;
+    ColSums cs;
+    stream_slice<DT, true>(rowp + head, s0, s1, a.nstages, bars, ring, top, cs, pass);
+    if (a.K == 0 && !(top.seen < CUDART_INF_F)) cs.S = CUDART_NAN_F;      // NaN or +inf: the row's sum says so
+    const WarpPartial p = warp_partial(cs);
+    const unsigned counted = __reduce_add_sync(0xFFFFFFFFu, (unsigned)pass.n);
+    unsigned char *area = ring + a.nstages * kTileBytes;
+    cluster_wait();                                      // the first CTA is there
+    if (a.K) {
+        const uint2 col = pack_col(top);
+        put_remote(at_rank(area + kFinishBytes + (rank * kThreads + tid) * 8, 0), (unsigned long long)col.y << 32 | col.x);
+    }
+    if (lane == 0) {
+        const uint32_t to = at_rank(&hand.wp[rank * kWarps + warp], 0);
+        put_remote(to, (unsigned long long)__double_as_longlong(p.S));
+        put_remote(to + 8, (unsigned long long)__double_as_longlong(p.T));
+        put_remote(to + 16, __float_as_uint(p.c));
+        put_remote(at_rank(&hand.counted[rank * kWarps + warp], 0), counted);
+    }
+    __syncthreads();                                     // every warp's waits are over
+    if (tid == 0) put_remote(at_rank(&hand.timed_out[rank], 0), bars.timed_out ? (unsigned)DSP_ROW_TIMEOUT : 0u);
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+    RowResult r;
+    if (a.K) {
+        if (!row_finish<DT>(rowp + head, a.inner, a.K, true, row, (int)C, a.ntiles_row, a.rs, hand.wp, area, r)) return;
+    } else {
+        if (warp != 0) return;
+        warp_merge_partials([&](int i) { return hand.wp[i]; }, (int)C * kWarps, lane, r.c, r.S, r.T);
+        r.key = 0ull;
+        r.nonfinite = false;
+    }
+    unsigned before = 0u, trouble = lane < (int)C ? hand.timed_out[lane] : 0u;
+    for (unsigned i = lane; i < C * kWarps; i += 32) before += hand.counted[i];
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    trouble = __reduce_or_sync(0xFFFFFFFFu, trouble);
+    grid_dependency_wait();                              // status words that several rows share are zeroed
+    score_row<DT>(a, row, b, rowp, head, pass, r, before, trouble, lane);
 }
 
 struct ScoreWs {
@@ -376,6 +468,36 @@ SlicePlan score_plan(long long rows, int inner) {
 }
 
 template <typename DT>
+int32_t launch_score_cluster(ScoreArgs &a, long long rows, int C, cudaStream_t st) {
+    a.nslices = C;
+    a.nstages = (a.ntiles_row + C - 1) / C;
+    a.own_status = a.L == 1;
+    if (!a.own_status) {
+        PrepareArgs prep = PrepareArgs();
+        prep.zero_b = a.row_status; prep.n_b = a.B;
+        DSP_CUDA_TRY(launch_prepare(prep, st));
+    }
+    static std::atomic<unsigned long long> smem_done{0};
+    DSP_CUDA_TRY(allow_shared(score_cluster_kernel<DT>, kClusterTiles * kTileBytes + kFinishArea, smem_done));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * C));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)(a.nstages * kTileBytes + kFinishArea);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.own_status ? 1 : 2;
+    DSP_CUDA_TRY(cudaLaunchKernelEx(&cfg, score_cluster_kernel<DT>, (const ScoreArgs)a));
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
+template <typename DT>
 int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
     const long long rows = (long long)a.B * a.L;
     a.inner = inner_elems<DT>(a.logits, a.V, a.stride_b, a.stride_l);
@@ -384,6 +506,12 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     a.ntiles_row = (a.inner + tile_elems<DT>() - 1) / tile_elems<DT>();
     const ScoreWs w = score_ws_layout(rows, a.nslices);
     if (workspace_bytes < w.rs.end) return DSP_ERR_WORKSPACE;
+    const int C = a.ntiles_row < kMaxCluster ? a.ntiles_row : kMaxCluster;
+    // Few rows go to clusters, as long as an SM gets two or three tiles.  Measured (us, cluster / slices and tickets; bf16, 5 alternatives if
+    // not said otherwise): 1 row of 152064 11.5 / 15.8, without alternatives 6.4 / 10.3, fp32 11.9 / 21.5; 17 rows 13.7 / 15.0, fp32 18.3 / 16.6;
+    // 34 rows 17.6 / 16.0; of 32003 68 rows 11.6 / 13.2, 136 rows 16.0 / 14.1.
+    if (C > 1 && a.ntiles_row <= kClusterTiles * kMaxCluster && 2 * rows * a.ntiles_row <= 5 * device_sm_count())
+        return launch_score_cluster<DT>(a, rows, C, st);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.rs.row_ticket = reinterpret_cast<unsigned *>(ws + w.off_ticket);
     a.rs.cols = reinterpret_cast<uint2 *>(ws + w.rs.off_cols);

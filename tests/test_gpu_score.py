@@ -174,3 +174,38 @@ def test_calls_give_the_same_bits_and_agree_with_the_lattice():
     lat = dsp.dsp_lattice_build(x, 16)
     assert torch.equal(lat.cand_id, a.top_id) and torch.equal(lat.cand_logit, a.top_logit)
     close(lat.lse, a.lse, 2 * ref.exponent_error(x, 1.0, ref.terms(152064)), "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,L,V,K,offset", [(1, 1, 12304, 5, 0), (3, 1, 24577, 32, 1), (1, 3, 50000, 0, 3), (2, 2, 98304, 1, 0), (5, 1, 110001, 20, 5),
+                                            (1, 1, 290000, 7, 0), (1, 4, 147459, 0, 2), (8, 1, 32003, 32, 0)])
+def test_few_rows(B, L, V, K, offset, dtype):
+    """A cluster's rows, of every number of tiles, with rows that are not read beside them; nothing is left of the outputs' old contents."""
+    x, g = rows(B, L, V, dtype, seed=V + K, offset=offset, masked=0.2)
+    tokens = tokens_of(g, B, L, 4, V)
+    tokens[..., 0] = x.argmax(-1).int()
+    tokens[0, 0, 0] = V - 1
+    check(x, 1.0, tokens, K)
+    lens = torch.tensor([0] + [L] * (B - 1) if B > 1 else [max(1, L - 1)], dtype=torch.int32, device="cuda")
+    old = dsp.dsp_token_logprobs(x, tokens, K=K)
+    for name in vars(old):
+        if getattr(old, name) is not None:
+            getattr(old, name).fill_(77)
+    check(x, 0.7, tokens, K, row_len=lens, got=dsp.dsp_token_logprobs(x, tokens, K=K, temperature=0.7, row_len=lens, out=old))
+
+
+@pytest.mark.parametrize("L", [1, 2])
+@pytest.mark.parametrize("K", [0, 8])
+def test_bad_and_flat_rows_of_few(K, L):
+    """NaN and +inf are named in their own status word only; a row of one value (no list is long enough for it) has its first tokens on top."""
+    B, V = 4, 40000
+    x, g = rows(B, L, V, BF, seed=3)
+    x[1, L - 1, 39999], x[2, 0, 0] = math.nan, math.inf
+    x[3] = 0.25
+    tokens = tokens_of(g, B, L, 1, V)
+    got = dsp.dsp_token_logprobs(x, tokens, K=K)
+    assert got.row_status.tolist() == [0, dsp.ROW_NONFINITE_INPUT, dsp.ROW_NONFINITE_INPUT, 0]
+    assert got.lse[1, L - 1].isnan() and got.lse[2, 0].isnan() and got.logp[2, 0].isnan().all()
+    good = torch.tensor([0, 3], device="cuda")
+    part = type(got)(**{k: None if v is None else v[good].contiguous() for k, v in vars(got).items()})
+    check(x[good], 1.0, tokens[good].contiguous(), K, got=part)
