@@ -830,8 +830,8 @@ int32_t dsp_qk_norm_rope(const void *q, const void *k, int32_t dtype, int32_t T,
  * + place).  A slot outside 0 .. n_blocks * page_size - 1 or a negative position
  * stores nothing.  No two tokens of a call may have the same slot: the place would
  * hold codes of one beside the scale or codes of the other.  (After a tree
- * was verified, the accepted nodes' rows are appended again at the slots of their
- * final places, with slot -1 for the others.)  q and q_out null: keys and values only.
+ * was verified, dsp_kv4_compact moves the accepted nodes; where their keys and values
+ * are at hand they may also be appended again at the slots of their final places, with slot -1 for the others.)  q and q_out null: keys and values only.
  * dsp_kv4_read: the values that the cache holds for the tokens in slot [T], in
  * `dtype`, [T,Hkv,D] contiguous, 16-byte aligned; an outside slot reads as 0.
  * Errors : as dsp_qk_norm_rope; INVALID_ARG (n_blocks < 1, page_size not a multiple
@@ -900,7 +900,8 @@ int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t
  *   rank[b,l] = number of tokens that come before tokens[b,l,0] in the total order
  *               (0: it is the argmax); -1 for a token outside 0..V-1
  *   the K best tokens in the total order with their logits x and log-probabilities;
- *   -inf logits are not among them (finite ones must exceed -1e38 * temperature, too), unused slots (K > V) are id -1, logit and logp -inf.
+ *   -inf logits are not among them, unused slots (fewer tokens than K) are id -1, logit and logp -inf.
+ *   In the sums, logits below -1e37 (or -1e38 * temperature, if that is higher) count as -inf.
  * Rows from row_len[b] on (clipped to 0..L) are not read: logp and lse -inf, rank -1,
  * entropy 0, no alternatives.  Everything but the scalars of a row is read once.
  * Any V and any row start run at full speed: what lies outside of whole 16-byte pieces
@@ -996,7 +997,7 @@ int32_t dsp_distill_grad(const void *student_logits, int32_t dtype, int32_t B, i
  * A row that cannot be served comes out empty and says why in row_status: DSP_ROW_BAD_LENGTH (src_row outside
  * -1..B_in-1, keep_len or seq_len_in negative, keep_len beyond seq_len_in, or more blocks needed than block_count_in), DSP_ROW_BAD_BLOCK (a block number
  * outside 0..n_blocks-1 among those kept), DSP_ROW_NO_BLOCKS (rows that need a block from the first on whose need,
- * counted over the rows, passes the free ones).  A call may be repeated on its inputs.
+ * counted over the rows, passes the free ones; its blocks stay with the rows that share them).  A call may be repeated on its inputs.
  *
  * Inputs : src_row, keep_len int32 [B_out]; seq_len_in, block_count_in int32 [B_in]; ring_pos_in int64 [2];
  *          block_table_in int32 [B_in, max_blocks] (stride table_in_stride).

@@ -4,6 +4,10 @@
 // such piece: its codes are cut into the places of a matrix instruction's fragments (kv4.cuh), D / 4 words of 4 bytes and its scales and
 // offsets.  The same lane always takes the same word of a token, so the moves of a request need no barrier: a lane's reads and writes of
 // one address come in its own order, and since the accepted nodes grow along the path no target lies behind a later source.
+//
+// Both are bound by latency, not by their bytes: 96 forks of 8704-byte heads in 4 layers 9.5 us with the launch, 64 trees of up to 16 accepted nodes in 16
+// layers of 8 heads 9.4 us (7 MB, 1.1 us at a copy's rate), one tree 4.6 us.  A warp a head for a tree: 8192 warps, each with a chain of table, node
+// and word reads; a warp a block and head instead of a run and head for the copies: 11.5 us.
 #include "kv4.cuh"
 
 namespace dsp {

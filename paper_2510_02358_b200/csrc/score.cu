@@ -7,6 +7,13 @@
 //
 // The rank needs one comparison per logit and no index: a token that precedes token t in the vocabulary comes before it with an equal
 // logit, a later one does not, so pieces before t's count what exceeds the next smaller number and the others what exceeds t's logit.
+// It is looked for only in tiles whose largest logit reaches the token's.
+//
+// The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 86 us = 5.4 TB/s, 0.84 of a
+// plain copy's rate; 272 rows with 20 alternatives 28 us (0.36: the selection, by one CTA a row, is 5 of them, the rest is that 272 rows are less than
+// two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 47 us (0.63: a row is six tiles, and while one warp finishes it the CTA's ring is
+// empty: 17 of 24 warps are active, 38% of the issue slots and 26% of the exponential unit are taken).  CTAs that stay and take row after row
+// measured 50 us there and 94 on the first: rows that are not read leave some of them idle.
 #include <string.h>
 
 #include "dsp_internal.h"

@@ -283,3 +283,24 @@ def test_small_losses_are_exact(B, L, V, dtype, grad):
     _, use, rest = ref.teacher(val, 1.0, ids, V, lse)
     q = torch.log_softmax(x.double(), -1).gather(-1, ids.long()).exp().sum(-1)
     near(r.loss, want, (1 - q - rest).abs() * bounds(x, 1.0, V)[0] + 2.0 ** -24 * want.abs() + 1e-12, "loss")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,L,V", [(2, 3, 33000), (1, 200, 80000)])
+def test_masks_of_the_lowest_number(B, L, V, dtype):
+    """Logits of the type's lowest value: no mass and no gradient among the others; in the list a loss that is next to infinite, not NaN."""
+    x, ids, val, lse = problem(B, L, V, 8, dtype, seed=12)
+    low = torch.finfo(dtype).min
+    x.masked_fill_(torch.rand(B, L, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) < 0.5, low)
+    x.scatter_(-1, ids.long(), torch.ones(B, L, 8, dtype=dtype, device="cuda"))
+    masked = x == low
+    x0 = x.masked_fill(masked, -math.inf)
+    for grad in (True, False):
+        a = dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=grad)
+        b = dsp.dsp_distill(x0, ids, val, teacher_lse=lse, grad=grad)
+        assert torch.equal(a.loss, b.loss) and torch.equal(a.accept, b.accept) and torch.equal(a.lse, b.lse)
+        ga, gb = (a.grad, b.grad) if grad else [dsp.dsp_distill_grad(t, ids, r.state, torch.ones(B, L, device="cuda")) for t, r in ((x, a), (x0, b))]
+        assert torch.equal(ga, gb) and not ga[masked].any() and torch.isfinite(ga).all()
+    x.scatter_(-1, ids[..., :1].long(), torch.full((B, L, 1), low, dtype=dtype, device="cuda"))
+    r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=True)
+    assert (r.loss > 1e30).all() and torch.isfinite(r.grad).all() and not r.accept.isnan().any()

@@ -209,3 +209,24 @@ def test_bad_and_flat_rows_of_few(K, L):
     good = torch.tensor([0, 3], device="cuda")
     part = type(got)(**{k: None if v is None else v[good].contiguous() for k, v in vars(got).items()})
     check(x[good], 1.0, tokens[good].contiguous(), K, got=part)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,L,V", [(2, 3, 33000), (3, 200, 5001), (2, 2, 11)])
+def test_masks_of_the_lowest_number(B, L, V, dtype):
+    """Masks of the type's lowest value are finite logits: they weigh nothing, and stand behind all others among the alternatives."""
+    x, g = rows(B, L, V, dtype, seed=8)
+    x.masked_fill_(torch.rand(B, L, V, generator=g, device="cuda") < 0.5, torch.finfo(dtype).min)
+    x[0, 0] = torch.finfo(dtype).min
+    x[0, 0, V - 2], x[0, 0, 4] = 1.5, 0.5
+    tokens = tokens_of(g, B, L, 2, V)
+    got = dsp.dsp_token_logprobs(x, tokens, K=6)
+    logp, rank, lse, entropy, top_id, top_x, top_p = ref.score(x, 1.0, tokens, 6)
+    err = ref.exponent_error(x.masked_fill(x < -1e30, 0.0), 1.0, ref.terms(V))
+    assert not got.row_status.any() and torch.equal(got.rank.long(), rank)
+    assert torch.equal(got.top_id.long(), top_id) and torch.equal(got.top_logit.double(), top_x)
+    for a, b, tol in ((got.lse, lse, err), (got.logp, logp, err[..., None]), (got.top_logp, top_p, err[..., None]),
+                      (got.entropy, entropy, err * (2 + math.log2(V + 1)))):
+        close(a, b, tol, "masked")
+    x.fill_(torch.finfo(dtype).min)                                       # nothing is left: named, not answered
+    assert (dsp.dsp_token_logprobs(x, tokens, K=6).row_status & dsp.ROW_NONFINITE_INPUT).bool().all()
