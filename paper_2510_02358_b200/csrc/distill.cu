@@ -375,7 +375,7 @@ __device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int
         if (a.lse) a.lse[row] = (float)lse;
         if (a.accept) a.accept[row] = (float)(accept + (r < s ? r : s));
         if (state) { state[0] = kn.c_f; state[1] = kn.f; state[2] = 0.f; state[3] = 0.f; }
-        if (a.status && (!ok || !(P < CUDART_INF))) atomicOr(&a.status[row / (unsigned)a.L], DSP_ROW_NONFINITE_INPUT);
+        if (a.status && (!ok || !(P < CUDART_INF) || (a.tlse && !(a.tlse[row] < CUDART_INF_F)))) atomicOr(&a.status[row / (unsigned)a.L], DSP_ROW_NONFINITE_INPUT);
     }
 }
 // A row that is not read.

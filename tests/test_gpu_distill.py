@@ -304,3 +304,32 @@ def test_masks_of_the_lowest_number(B, L, V, dtype):
     x.scatter_(-1, ids[..., :1].long(), torch.full((B, L, 1), low, dtype=dtype, device="cuda"))
     r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=True)
     assert (r.loss > 1e30).all() and torch.isfinite(r.grad).all() and not r.accept.isnan().any()
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("grad", [True, False])
+def test_a_bad_log_sum_exp_of_the_teacher_is_named(value, grad):
+    for B, L, V, dtype in ((3, 1, 5000, F32), (3, 60, 80000, BF)):
+        x, ids, val, lse = problem(B, L, V, 4, dtype, seed=2)
+        lse[1, L - 1] = value
+        status = torch.zeros(B, dtype=torch.int32, device="cuda")
+        dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=grad, row_status=status)
+        assert status.tolist() == [0, dsp.ROW_NONFINITE_INPUT, 0]
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_rows_beyond_32_bits(grad):
+    """Logits of more than 2^31 elements: the last rows, in place."""
+    V, L = 160001, 14000
+    x = torch.empty(1, L, V, dtype=BF, device="cuda")
+    small, ids_s, val_s, lse_s = problem(1, 3, V, 4, BF, seed=4)
+    x[:, -3:] = small
+    ids, val, lse, w = (torch.zeros(1, L, 4, dtype=torch.int32, device="cuda"), torch.zeros(1, L, 4, device="cuda"), torch.zeros(1, L, device="cuda"),
+                        torch.zeros(1, L, device="cuda"))
+    ids[:, -3:], val[:, -3:], lse[:, -3:], w[:, -3:] = ids_s, val_s, lse_s, 1.0
+    r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, weight=w, grad=x if grad else None)
+    got = x[:, -3:] if grad else dsp.dsp_distill_grad(x, ids, r.state, w, grad=x)[:, -3:]
+    want = dsp.dsp_distill(small.clone(), ids_s, val_s, teacher_lse=lse_s, grad=True)
+    near(r.loss[:, -3:], want.loss, 1e-5, "loss")
+    near(got, want.grad.double(), 2.0 ** -8 * want.grad.double().abs() + 1e-9, "gradient")     # a last bit may differ between the forms
+    assert not r.loss[:, :-3].any() and not x[0, 0].any() and not x[0, L - 4].any()

@@ -188,3 +188,21 @@ def test_compaction_of_a_single_layer_moves_what_the_cache_holds():
             for i in range(length[b]):
                 want[b, seq[b] + 1 + i] = x[b, seq[b] + 1 + node[b][i]]
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("layers", [1, 2])
+def test_moves_beyond_32_bits(layers):
+    """A cache of more than 2^32 bytes a layer: copies to and from its end, and a tree in its last blocks."""
+    D, page, H, blocks = 64, 16, 1, 3800000
+    cache = torch.empty(layers, blocks, H, page * (D + 8), dtype=torch.uint8, device="cuda")
+    small = random_cache(layers, 4, H, page, D, seed=3).cuda()
+    at = torch.tensor([0, 1, blocks - 2, blocks - 1], device="cuda")
+    cache[:, at] = small
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    dsp.dsp_kv4_copy(cache, D, ints(0, blocks - 1), ints(blocks - 3, 7), None)
+    assert torch.equal(cache[:, blocks - 3], small[:, 0]) and torch.equal(cache[:, 7], small[:, 3])
+    table = ints(0, blocks - 2, blocks - 1).view(1, 3)
+    seq, node, n = [page + 2], [[0, 9, 10, 20]], [4]
+    dsp.dsp_kv4_compact(cache, D, table, ints(*seq), ints(*node[0]).view(1, 4), ints(*n))
+    want = ref.compact(small.cpu(), D, [[0, 2, 3]], seq, node, n)
+    assert torch.equal(cache[:, at].cpu(), want)

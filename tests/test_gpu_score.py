@@ -230,3 +230,16 @@ def test_masks_of_the_lowest_number(B, L, V, dtype):
         close(a, b, tol, "masked")
     x.fill_(torch.finfo(dtype).min)                                       # nothing is left: named, not answered
     assert (dsp.dsp_token_logprobs(x, tokens, K=6).row_status & dsp.ROW_NONFINITE_INPUT).bool().all()
+
+
+def test_rows_beyond_32_bits():
+    V, L = 160001, 14000
+    x = torch.empty(1, L, V, dtype=BF, device="cuda")
+    small, g = rows(1, 3, V, BF, seed=4)
+    x[:, -3:] = small
+    tokens = torch.zeros(1, L, 2, dtype=torch.int32, device="cuda")
+    tokens[:, -3:] = tokens_of(g, 1, 3, 2, V)
+    got = dsp.dsp_token_logprobs(x, tokens, K=4)
+    part = type(got)(**{k: v if k == "row_status" else v[:, -3:].contiguous() for k, v in vars(got).items()})
+    part.row_status = torch.zeros_like(part.row_status)                   # the other rows are not initialised
+    check(x[:, -3:], 1.0, tokens[:, -3:].contiguous(), 4, got=part)
