@@ -70,6 +70,7 @@ struct TokenPass {
     int V, head, inner;
     // rank
     int tok = -1, vec = 0;    // token, and the streamed piece it lies in (pieces: beyond, 0: before)
+    bool apart = false;       // it lies in the streamed part: taken out of the sums, score_row adds it
     float xt = 0.f;
     uint32_t ge = 0u, gt = 0u;
     int n = 0;
@@ -78,14 +79,19 @@ struct TokenPass {
     int mine = -1;
     float x_mine = 0.f, x_outer = 0.f, x_piece = 0.f;
 
-    __device__ __forceinline__ int outer_at(int lane) const { return lane < head ? lane : inner + lane; }
+    // the outer element of a lane (lanes 16 and up), -1: none
+    __device__ __forceinline__ int outer_at(int lane) const {
+        const int i = lane - 16;
+        return i < 0 || i >= V - inner ? -1 : i < head ? i : inner + i;
+    }
     __device__ __forceinline__ void begin() {
         constexpr int N = Elem<DT>::N;
         const int lane = threadIdx.x;
         if (lane < 32) {
             if (lane < G) mine = tokens[lane];
             if (mine >= 0 && mine < V) x_mine = Elem<DT>::load1(row + mine);
-            x_outer = lane < V - inner ? Elem<DT>::load1(row + outer_at(lane)) : -CUDART_INF_F;
+            const int v = outer_at(lane);
+            x_outer = v >= 0 ? Elem<DT>::load1(row + v) : -CUDART_INF_F;
         }
         tok = ranked ? tokens[0] : -1;
         if (tok < 0 || tok >= V) { tok = -1; xt = CUDART_INF_F; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
@@ -98,7 +104,8 @@ struct TokenPass {
             gt = __float_as_uint(xt);
             ge = below_bits(xt);
         }
-        if (lane < N && tok >= head && tok < head + inner) x_piece = Elem<DT>::load1(row + head + vec * N + lane);
+        apart = tok >= head && tok < head + inner;
+        if (lane < N && apart) x_piece = Elem<DT>::load1(row + head + vec * N + lane);
     }
     // Logits of a tile that come before the token: looked for only where the tile's largest reaches it.
     __device__ __forceinline__ void count(const uint4 (&v)[kVpt], int base) {
@@ -123,6 +130,16 @@ struct TokenPass {
             }
         }
     }
+    // Element e of a piece becomes -inf.
+    static __device__ __forceinline__ void hide(uint4 &v, int e) {
+        const int at = Elem<DT>::N == 8 ? e >> 1 : e;
+        const uint32_t mask = Elem<DT>::N == 4 ? 0xFFFFFFFFu : e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+        const uint32_t word = (Elem<DT>::N == 8 ? 0xFF80FF80u : 0xFF800000u) & mask;
+        if (at == 0) v.x = (v.x & ~mask) | word;
+        if (at == 1) v.y = (v.y & ~mask) | word;
+        if (at == 2) v.z = (v.z & ~mask) | word;
+        if (at == 3) v.w = (v.w & ~mask) | word;
+    }
     static __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); }
     static __device__ __forceinline__ uint32_t word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
     static __device__ __forceinline__ float max_of(const uint4 (&v)[kVpt]) {
@@ -145,13 +162,25 @@ struct TokenPass {
         }
     }
     // One tile's share of a thread: S = sum 2^a and T = sum 2^a a over the exponents a = x s - c.  A masked logit counts as `low`: its
-    // power is 0, and so is the product (0 * -inf is not).
+    // power is 0, and so is the product (0 * -inf is not).  The first token is left out: next to a token that holds nearly all of the mass an fp32
+    // sum has no room for the others, which are all that its log-probability and the entropy are made of then.
     template <bool RAGGED>
-    __device__ __forceinline__ float tile(const uint4 (&v)[kVpt], int nvec, int tid, int base, float &c, unsigned long long &S2,
+    __device__ __forceinline__ float tile(const uint4 (&t)[kVpt], int nvec, int tid, int base, float &c, unsigned long long &S2,
                                           unsigned long long &T2) {
         constexpr int N = Elem<DT>::N;
+        uint4 v[kVpt];
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) v[j] = t[j];
         const float tm = max_of(v);
-        if (!(tm < xt)) count(v, base);
+        if (!(tm < xt)) {
+            count(v, base);
+            const int at = vec - base / N - tid;
+            if (apart && at >= 0 && at % kThreads == 0) {
+#pragma unroll
+                for (int j = 0; j < kVpt; ++j)
+                    if (at == j * kThreads) hide(v[j], (tok - head) % N);
+            }
+        }
         const float ts = fmaxf(tm, N == 8 ? bf16_hi(low) : __uint_as_float(low)) * s;
         if (ts > c) {
             const float d = c - ts;
@@ -211,11 +240,33 @@ __device__ void score_nothing(const ScoreArgs &a, long long row, int lane) {
     }
 }
 
-// The finish of a row by one warp: the elements outside of the streamed pieces join, and everything is written (counted: of the streamed
-// logits, how many come before the first token; trouble: status bits so far).
+// The logit that a lane adds to the sums by itself: one outside of the streamed pieces, the first token (lane 31), or none (-inf).
+template <typename DT>
+__device__ __forceinline__ float apart_of(const TokenPass<DT> &pass, int lane) {
+    static_assert(2 * Elem<DT>::N <= 16, "fewer than 15 outer elements: lane 31 is free");
+    return lane == 31 && pass.apart ? pass.xt : pass.x_outer;
+}
+// The sums of a row from its n partials and those logits, by one warp.
+template <typename DT, typename At>
+__device__ __forceinline__ void merge_row(const ScoreArgs &a, const TokenPass<DT> &pass, At at, int n, int lane, RowResult &r) {
+    const int last = n <= 16 ? 0 : (n + 31) / 32 * 32;   // a lane's last entry is its own logit (up to 16 partials leave room in one round)
+    const double e = (double)apart_of(pass, lane) * (double)a.s;
+    const float ce = (float)e;
+    const double res = (e - (double)ce) * kLn2;          // below 2^-16: 2^res is 1 + res + res^2 / 2 to 2^-50
+    WarpPartial own;
+    own.S = ce > kRefFloor ? 1.0 + res + 0.5 * res * res : 0.0;
+    own.c = ce; own.T = own.S * (e - (double)ce); own.pad = 0;
+    if (!(own.S > 0.0)) { own.S = own.T = 0.0; own.c = kRefFloor; }
+    WarpPartial none;
+    none.S = none.T = 0.0; none.c = kRefFloor; none.pad = 0;
+    warp_merge_partials([&](int i) { return i < n ? at(i) : i >= last ? own : none; }, last + 32, lane, r.c, r.S, r.T);
+}
+
+// The finish of a row by one warp: the first token and the elements outside of the streamed pieces join (joined: the sums have them), and everything is
+// written (counted: of the streamed logits, how many come before the first token; trouble: status bits so far).
 template <typename DT>
 __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *rowp, int head, const TokenPass<DT> &pass, RowResult r,
-                          unsigned counted, uint32_t trouble, int lane) {
+                          bool joined, unsigned counted, uint32_t trouble, int lane) {
     constexpr int N = Elem<DT>::N;
     // one element a lane: before the streamed pieces, then behind them
     const int extra = a.V - a.inner;
@@ -224,12 +275,13 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
     bool bad = __any_sync(0xFFFFFFFFu, !(x < CUDART_INF_F)) || r.nonfinite;
     unsigned long long key = lane < a.K && r.key ? r.key - (unsigned)head : 0ull;      // ids count from the streamed part
     double c = r.c, S = r.S, T = r.T;
-    if (extra > 0) {
-        key = merge_top32(key, sort32_desc(x > -CUDART_INF_F ? make_key(x, v) : 0ull, lane), lane);
-        const double e = (double)x * (double)a.s;
+    if (extra > 0) key = merge_top32(key, sort32_desc(x > -CUDART_INF_F ? make_key(x, v) : 0ull, lane), lane);
+    if (!joined && (extra > 0 || pass.apart)) {
+        const float y = apart_of(pass, lane);
+        const double e = (double)y * (double)a.s;
         const float cm = fmaxf(S != 0.0 ? r.c : kRefFloor, warp_max((float)e > kRefFloor ? (float)e : kRefFloor));
         const double d = c - (double)cm, w = S != 0.0 ? exp2(d) : 0.0;
-        const double p = x > -CUDART_INF_F ? exp2(e - (double)cm) : 0.0;
+        const double p = y > -CUDART_INF_F ? exp2(e - (double)cm) : 0.0;
         const double S1 = warp_sum(p), T1 = warp_sum(p != 0.0 ? p * (e - (double)cm) : 0.0);
         T = (S != 0.0 ? (T + S * d) * w : 0.0) + T1;
         S = S * w + S1;
@@ -255,7 +307,7 @@ __device__ void score_row(const ScoreArgs &a, long long row, int b, const DT *ro
         int rank = -1;
         if (pass.tok >= 0) {
             // before the token: of the outer elements, and of its own piece (counted without equals)
-            int n = lane < extra && (x > pass.xt || (x == pass.xt && v < pass.tok)) ? 1 : 0;
+            int n = v >= 0 && (x > pass.xt || (x == pass.xt && v < pass.tok)) ? 1 : 0;
             const int u = head + pass.vec * N + lane;
             if (pass.tok >= head && pass.tok < head + a.inner && lane < N && u < pass.tok && pass.x_piece == pass.xt) ++n;
             rank = (int)(__reduce_add_sync(0xFFFFFFFFu, (unsigned)n) + counted);
@@ -305,13 +357,13 @@ __device__ bool score_sums(const ScoreArgs &a, const DT *inner, long long row, i
     if (a.nslices > 1) {
         __threadfence();
         const WarpPartial *wp = a.rs.wpart + row * a.nslices * kWarps;
-        warp_merge_partials([&](int i) {
+        merge_row(a, pass, [&](int i) {
             WarpPartial q;
             q.S = __ldcg(&wp[i].S); q.T = __ldcg(&wp[i].T); q.c = __ldcg(&wp[i].c); q.pad = 0;
             return q;
-        }, a.nslices * kWarps, lane, r.c, r.S, r.T);
+        }, a.nslices * kWarps, lane, r);
     } else {
-        warp_merge_partials([&](int i) { return bars.wp[i]; }, kWarps, lane, r.c, r.S, r.T);
+        merge_row(a, pass, [&](int i) { return bars.wp[i]; }, kWarps, lane, r);
     }
     r.key = 0ull;
     r.nonfinite = false;
@@ -357,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
         r.key = 0ull; r.c = kRefFloor; r.S = 0.0; r.T = 0.0; r.nonfinite = false;
     }
     const unsigned counted = pass.ranked && pass.tok >= 0 && a.inner && lane == 0 ? atomicAdd(pass.acc, 0u) : 0u;
-    score_row<DT>(a, row, b, rowp, pass.head, pass, r, counted, 0u, lane);
+    score_row<DT>(a, row, b, rowp, pass.head, pass, r, a.inner && a.K == 0, counted, 0u, lane);
 }
 
 // ---- few rows: the CTAs of a row are a cluster and hand what they found to the first one, which finishes the row; no tickets, so nothing
@@ -435,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
         if (!row_finish<DT>(rowp + head, a.inner, a.K, true, row, (int)C, a.ntiles_row, a.rs, hand.wp, area, r)) return;
     } else {
         if (warp != 0) return;
-        warp_merge_partials([&](int i) { return hand.wp[i]; }, (int)C * kWarps, lane, r.c, r.S, r.T);
+        merge_row(a, pass, [&](int i) { return hand.wp[i]; }, (int)C * kWarps, lane, r);
         r.key = 0ull;
         r.nonfinite = false;
     }
@@ -444,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
     before = __reduce_add_sync(0xFFFFFFFFu, before);
     trouble = __reduce_or_sync(0xFFFFFFFFu, trouble);
     grid_dependency_wait();                              // status words that several rows share are zeroed
-    score_row<DT>(a, row, b, rowp, head, pass, r, before, trouble, lane);
+    score_row<DT>(a, row, b, rowp, head, pass, r, a.K == 0, before, trouble, lane);
 }
 
 struct ScoreWs {

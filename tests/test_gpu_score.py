@@ -243,3 +243,24 @@ def test_rows_beyond_32_bits():
     part = type(got)(**{k: v if k == "row_status" else v[:, -3:].contiguous() for k, v in vars(got).items()})
     part.row_status = torch.zeros_like(part.row_status)                   # the other rows are not initialised
     check(x[:, -3:], 1.0, tokens[:, -3:].contiguous(), 4, got=part)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("L,V,K,boost", [(1, 152064, 5, 24.0), (300, 32003, 0, 20.0), (40, 50001, 3, 30.0), (3, 15, 2, 30.0), (2, 1000, 0, 18.0)])
+def test_a_token_with_nearly_all_of_the_mass(L, V, K, boost, dtype):
+    """Its log-probability is made of the other tokens' sum, relative to its own exponent: an error of that sum counts times 1 - p, and in the entropy
+    times the others' share of it."""
+    x, g = rows(1, L, V, dtype, seed=int(boost))
+    x = x.clamp(max=6.0)
+    tokens = torch.randint(0, V, (1, L, 1), generator=g, device="cuda", dtype=torch.int32)
+    tokens[0, 0] = V - 1
+    x.scatter_(2, tokens.long(), torch.full((1, L, 1), boost, dtype=dtype, device="cuda"))
+    got = dsp.dsp_token_logprobs(x, tokens, K=K)
+    logp, rank, _, entropy, _, _, top_p = ref.score(x, 1.0, tokens, K)
+    err = ref.exponent_error(x, 1.0, ref.terms(V))
+    other = -torch.expm1(logp[..., 0])
+    assert (other < 0.2).all()
+    close(got.logp, logp, (err * other)[..., None] + 1e-13, "logp")
+    close(got.entropy, entropy, 2 * err * (entropy + 2 * other) + 1e-13, "entropy")
+    if K:
+        close(got.top_logp[..., 0], top_p[..., 0], err * other + 1e-13, "top_logp")
