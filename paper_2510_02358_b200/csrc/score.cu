@@ -10,7 +10,7 @@
 // It is looked for only in tiles whose largest logit reaches the token's.
 //
 // The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 86 us = 5.4 TB/s, 0.84 of a
-// plain copy's rate; 272 rows with 20 alternatives 28 us (0.36: the selection, by one CTA a row, is 5 of them, the rest is that 272 rows are less than
+// plain copy's rate; 272 rows with 20 alternatives 29 us (0.34: the selection, by one CTA a row, is 6 of them, the rest is that 272 rows are less than
 // two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 47 us (0.63: a row is six tiles, and while one warp finishes it the CTA's ring is
 // empty: 17 of 24 warps are active, 38% of the issue slots and 26% of the exponential unit are taken).  CTAs that stay and take row after row
 // measured 50 us there and 94 on the first: rows that are not read leave some of them idle.
@@ -567,8 +567,8 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     if (workspace_bytes < w.rs.end) return DSP_ERR_WORKSPACE;
     const int C = a.ntiles_row < kMaxCluster ? a.ntiles_row : kMaxCluster;
     // Few rows go to clusters, as long as an SM gets two or three tiles.  Measured (us, cluster / slices and tickets; bf16, 5 alternatives if
-    // not said otherwise): 1 row of 152064 11.5 / 15.8, without alternatives 6.4 / 10.3, fp32 11.9 / 21.5; 17 rows 13.7 / 15.0, fp32 18.3 / 16.6;
-    // 34 rows 17.6 / 16.0; of 32003 68 rows 11.6 / 13.2, 136 rows 16.0 / 14.1.
+    // not said otherwise): 1 row of 152064 12.1 / 16.9, without alternatives 7.1 / 10.0, fp32 12.6 / 22.6; 17 rows 14.5 / 16.4, fp32 18.9 / 17.9;
+    // 34 rows 18.5 / 16.8; of 32003 68 rows 12.0 / 13.6, 136 rows 16.5 / 14.3.
     if (C > 1 && a.ntiles_row <= kClusterTiles * kMaxCluster && 2 * rows * a.ntiles_row <= 5 * device_sm_count())
         return launch_score_cluster<DT>(a, rows, C, st);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
