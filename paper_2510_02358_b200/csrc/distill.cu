@@ -176,13 +176,21 @@ __device__ __forceinline__ float sum_of_warp(float v) {
 // Sum of 2^(x s - c) over the buffer's pieces, by this thread's share.  The reference c of a warp is the largest exponent of its
 // first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where a sum passes 2^64 (or a
 // logit is not finite) the warp sums once more against its true maximum, so that no sum is lost below another warp's reference.
+// Two logits an instruction where the hardware has one (2048 rows of 152064 bf16: 256 to 252 us).
 template <typename DT>
-__device__ __forceinline__ void add_piece(const uint4 &v, float s, float c, float &S0, float &S1) {
+__device__ __forceinline__ void add_piece(const uint4 &v, float s, float c, unsigned long long &S) {
+    const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c);
 #pragma unroll
     for (int e = 0; e < Elem<DT>::N; e += 2) {
-        S0 += ex2_approx(fmaf(Elem<DT>::get(v, e), s, -c));
-        S1 += ex2_approx(fmaf(Elem<DT>::get(v, e + 1), s, -c));
+        float a0, a1;
+        unpack2(fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), s2, nc2), a0, a1);
+        S = add2(S, pack2(ex2_approx(a0), ex2_approx(a1)));
     }
+}
+__device__ __forceinline__ float both(unsigned long long S) {
+    float a, b;
+    unpack2(S, a, b);
+    return a + b;
 }
 template <typename DT>
 __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, float &c, float &S) {
@@ -191,22 +199,23 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     float m = -CUDART_INF_F;
     if (tid < n) m = Elem<DT>::vmax(at[0]);
     if (tid + kDT < n) m = fmaxf(m, Elem<DT>::vmax(at[kDT]));
-    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor), s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
+    unsigned long long s0 = 0ull, t0 = 0ull;             // pairs of sums
     int k = full;
     for (; k >= 2; k -= 2, at += 2 * kDT) {
         const uint4 v = at[0], w = at[kDT];
-        add_piece<DT>(v, s, c1, s0, s1);
-        add_piece<DT>(w, s, c1, t0, t1);
+        add_piece<DT>(v, s, c1, s0);
+        add_piece<DT>(w, s, c1, t0);
     }
-    if (k) { add_piece<DT>(at[0], s, c1, s0, s1); at += kDT; }
-    if (tid < rest) add_piece<DT>(at[0], s, c1, t0, t1);
-    float sum = (s0 + s1) + (t0 + t1);
+    if (k) { add_piece<DT>(at[0], s, c1, s0); at += kDT; }
+    if (tid < rest) add_piece<DT>(at[0], s, c1, t0);
+    float sum = both(add2(s0, t0));
     if (__any_sync(0xFFFFFFFFu, !(sum < 0x1p64f))) {
         for (int i = tid; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
         c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
-        s0 = s1 = 0.f;
-        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s, c1, s0, s1);
-        sum = s0 + s1;
+        s0 = 0ull;
+        for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s, c1, s0);
+        sum = both(s0);
     }
     // with what the chunks before gave
     const float cn = fmaxf(c, c1);
@@ -221,8 +230,9 @@ __device__ __forceinline__ uint4 turned(const uint4 &v, float s, float c, float 
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
-        const float a0 = ex2_approx(fmaf(Elem<DT>::get(v, e), s, -c)) * f;
-        const float a1 = ex2_approx(fmaf(Elem<DT>::get(v, e + 1), s, -c)) * f;
+        float a0, a1;
+        unpack2(fma2(pack2(Elem<DT>::get(v, e), Elem<DT>::get(v, e + 1)), pack2(s, s), pack2(-c, -c)), a0, a1);
+        unpack2(mul2(pack2(ex2_approx(a0), ex2_approx(a1)), pack2(f, f)), a0, a1);
         if constexpr (N == 8) {
             const __nv_bfloat162 b = __floats2bfloat162_rn(a0, a1);
             w[e / 2] = *reinterpret_cast<const uint32_t *>(&b);
@@ -592,6 +602,16 @@ __device__ __forceinline__ float take_out(uint4 &v, int e) {
     return x;
 }
 
+// As add_piece, without the register pairs, which cost this kernel spills (512 rows of 152064 in two calls 91 us, with them 93).
+template <typename DT>
+__device__ __forceinline__ void add_single(const uint4 &v, float s, float c, float &S0, float &S1) {
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::N; e += 2) {
+        S0 += ex2_approx(fmaf(Elem<DT>::get(v, e), s, -c));
+        S1 += ex2_approx(fmaf(Elem<DT>::get(v, e + 1), s, -c));
+    }
+}
+
 // The sums of a row without the teacher's tokens.  These are sorted by place; every warp walks through them with the tiles, and the thread
 // that has a token takes it out and notes it.
 template <typename DT, typename List>
@@ -638,7 +658,7 @@ struct LossPass {
         }
         float s0 = S, s1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < kVpt; ++j) add_piece<DT>(v[j], s, c, s0, s1);
+        for (int j = 0; j < kVpt; ++j) add_single<DT>(v[j], s, c, s0, s1);
         if (__any_sync(0xFFFFFFFFu, !(s0 + s1 < 0x1p64f))) {     // against a new reference, as in sum_pieces
             float m = Elem<DT>::vmax(v[0]);
 #pragma unroll
@@ -647,7 +667,7 @@ struct LossPass {
             s0 = S != 0.f ? S * ex2_approx(c - c1) : 0.f;
             s1 = 0.f;
 #pragma unroll
-            for (int j = 0; j < kVpt; ++j) add_piece<DT>(v[j], s, c1, s0, s1);
+            for (int j = 0; j < kVpt; ++j) add_single<DT>(v[j], s, c1, s0, s1);
             c = c1;
         }
         S = s0 + s1;
