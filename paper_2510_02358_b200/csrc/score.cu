@@ -9,11 +9,11 @@
 // logit, a later one does not, so pieces before t's count what exceeds the next smaller number and the others what exceeds t's logit.
 // It is looked for only in tiles whose largest logit reaches the token's.
 //
-// The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 86 us = 5.4 TB/s, 0.84 of a
+// The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 85 us = 5.5 TB/s, 0.85 of a
 // plain copy's rate; 272 rows with 20 alternatives 29 us (0.34: the selection, by one CTA a row, is 6 of them, the rest is that 272 rows are less than
-// two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 47 us (0.63: a row is six tiles, and while one warp finishes it the CTA's ring is
-// empty: 17 of 24 warps are active, 38% of the issue slots and 26% of the exponential unit are taken).  CTAs that stay and take row after row
-// measured 50 us there and 94 on the first: rows that are not read leave some of them idle.
+// two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 45 us (0.67: a row is six tiles, and while one warp finishes it the CTA's ring is
+// empty; with three CTAs an SM 17 of 24 warps were active, 38% of the issue slots and 26% of the exponential unit taken).  CTAs that stay and take row
+// after row measured 50 us there and 94 on the first: rows that are not read leave some of them idle.
 #include <string.h>
 
 #include "dsp_internal.h"
@@ -370,8 +370,9 @@ __device__ bool score_sums(const ScoreArgs &a, const DT *inner, long long row, i
     return true;
 }
 
-template <typename DT>
-__global__ void __launch_bounds__(kThreads, 3) score_kernel(const ScoreArgs a) {
+// CTAS: of an SM.
+template <typename DT, int CTAS>
+__global__ void __launch_bounds__(kThreads, CTAS) score_kernel(const ScoreArgs a) {
     constexpr int N = Elem<DT>::N;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ StreamBars bars;
@@ -556,6 +557,13 @@ int32_t launch_score_cluster(ScoreArgs &a, long long rows, int C, cudaStream_t s
     return DSP_OK;
 }
 
+template <typename Kernel>
+int32_t launch_score_rows(Kernel kernel, long long nblocks, const ScoreArgs &a, cudaStream_t st) {
+    DSP_CUDA_TRY(launch_dependent(kernel, (unsigned)nblocks, kThreads, (size_t)a.nstages * kTileBytes, st, a, true));
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
 template <typename DT>
 int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cudaStream_t st) {
     const long long rows = (long long)a.B * a.L;
@@ -582,12 +590,19 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     prep.zero_a = reinterpret_cast<uint32_t *>(ws); prep.n_a = (long long)(w.zero_bytes / 4);
     prep.zero_b = a.row_status; prep.n_b = a.B;
     DSP_CUDA_TRY(launch_prepare(prep, st));
-    static RingSmemDone smem_done;                       // one per element type
-    DSP_CUDA_TRY(allow_ring_smem(score_kernel<DT>, smem_done));
+    // More than three CTAs an SM: four, with fewer registers and a ring of two tiles, if the finish has room in it.  Measured with three (us,
+    // four / three, bf16): 2048 rows of 152064 84.7 / 86.5, 500 with 20 alternatives 45.5 / 53.7; 2000 of 8000 with 5 alternatives 37 / 43; 2048 of
+    // 32003 fp32 45.0 / 47.4; five, with one tile: 102.7 for the first and 52.1 for the last.  272 rows, for which three are room enough: 30.1 / 29.2.
+    if (nblocks > 3ll * device_sm_count() && kFinishBytes + a.nslices * kThreads * 8 <= 2 * kTileBytes) {
+        a.nstages = 2;
+        static RingSmemDone done;                        // one per kernel
+        DSP_CUDA_TRY(allow_ring_smem(score_kernel<DT, 4>, done));
+        return launch_score_rows(score_kernel<DT, 4>, nblocks, a, st);
+    }
     a.nstages = ring_stages(nblocks);
-    DSP_CUDA_TRY(launch_dependent(score_kernel<DT>, (unsigned)nblocks, kThreads, (size_t)a.nstages * kTileBytes, st, a, true));
-    DSP_CUDA_TRY(cudaGetLastError());
-    return DSP_OK;
+    static RingSmemDone done;
+    DSP_CUDA_TRY(allow_ring_smem(score_kernel<DT, 3>, done));
+    return launch_score_rows(score_kernel<DT, 3>, nblocks, a, st);
 }
 
 template <typename DT>

@@ -264,3 +264,15 @@ def test_a_token_with_nearly_all_of_the_mass(L, V, K, boost, dtype):
     close(got.entropy, entropy, 2 * err * (entropy + 2 * other) + 1e-13, "entropy")
     if K:
         close(got.top_logp[..., 0], top_p[..., 0], err * other + 1e-13, "top_logp")
+
+
+@pytest.mark.parametrize("L,V", [(18, 10000003), (36, 5000000), (500, 40000)])
+def test_many_long_rows(L, V):
+    """Rows of many slices, with a CTA count beyond three an SM: a ring of three tiles where the finish needs it, of two elsewhere."""
+    g = torch.Generator(device="cuda").manual_seed(L)
+    x = torch.randn(1, L, V, generator=g, device="cuda", dtype=torch.bfloat16)
+    tokens = torch.randint(0, V, (1, L, 1), generator=g, device="cuda", dtype=torch.int32)
+    tokens[0, -1] = x[0, -1].argmax().int()
+    got = dsp.dsp_token_logprobs(x, tokens, K=3)
+    part = type(got)(**{k: v if k == "row_status" else v[:, -3:].contiguous() for k, v in vars(got).items()})
+    check(x[:, -3:], 1.0, tokens[:, -3:].contiguous(), 3, got=part)
