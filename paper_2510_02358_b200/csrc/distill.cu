@@ -15,9 +15,9 @@
 //
 // Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 252 us, which is
 // 4.7 TB/s or 0.73 of a plain copy's rate; 999 rows of 32003 fp32 61 us (0.65); 512 rows of 152064 bf16 in two calls 91 us (0.79; the gradient's
-// call alone 46 us, a copy's rate); 16 rows 9 us.  What bounds the one call is issue: with the kernel cut off after each phase, of
-// 83 us for 512 rows the load alone took 27, the sums 10 more, the exchange 9, the row's factors 5, the gradient the rest; now 75 under the profiler, with 49% of the issue slots and 56% of
-// the exponential unit are taken, half of the instructions belong to a row and not to its logits.  Other forms measured on 2048 rows: clusters that
+// call alone 46 us, a copy's rate); 16 rows 9 us.  Of 512 rows in one call, 75 us under the profiler, 49% of the issue slots and 56% of the
+// exponential unit are taken, half of the 1100 instructions a warp belong to the row and not to its logits, and 41% of the warps' waits are at
+// barriers, for the copies and the exchange, which five CTAs an SM cover in part.  Other forms measured on 2048 rows: clusters that
 // stay and load the next row into a second buffer 434 us, a row in one CTA with what does not fit read again from L2 276 us; a cubic for part
 // of the exponentials: within 2%.
 #include "stream_core.cuh"
