@@ -170,6 +170,7 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
             t0 = kb <= ord_bits(-CUDART_INF_F) ? -CUDART_INF_F : ord_value(kb);    // fewer than K finite maxima: everything finite
         }
         // ---- 2. shares ----
+        const int my_first = slice_first_tile(min(lane, nslices), nslices, ntiles_row);     // lane s: slice s's (a division, so once)
         for (int col0 = warp * 32; col0 < kThreads; col0 += nsel) {
             const int col = col0 + lane;
             for (int s = 0; s < nslices; ++s) {
@@ -177,7 +178,7 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
                 const float rm1 = col_rm1(r);
                 const bool in = rm1 >= t0 && rm1 > -CUDART_INF_F;
                 const bool whole = in && col_rm2(r) >= t0;     // more than one tile of this column may hold a top-K logit
-                const int tb = slice_first_tile(s, nslices, ntiles_row);
+                const int tb = __shfl_sync(0xFFFFFFFFu, my_first, s);
                 const unsigned m = __ballot_sync(0xFFFFFFFFu, in && !whole);
                 if (m) {                                       // one tile each: one counter update per warp
                     int base = 0;
