@@ -170,29 +170,46 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
             t0 = kb <= ord_bits(-CUDART_INF_F) ? -CUDART_INF_F : ord_value(kb);    // fewer than K finite maxima: everything finite
         }
         // ---- 2. shares ----
-        const int my_first = slice_first_tile(min(lane, nslices), nslices, ntiles_row);     // lane s: slice s's (a division, so once)
         for (int col0 = warp * 32; col0 < kThreads; col0 += nsel) {
             const int col = col0 + lane;
+            unsigned one = 0u, all = 0u;                       // slices of which the best tile, or every tile, may hold a top-K logit
+            int t1 = 0;                                        // that tile of the last such slice, within the slice
+#pragma unroll 2
             for (int s = 0; s < nslices; ++s) {
                 const uint2 r = stash[s * kThreads + col];
                 const float rm1 = col_rm1(r);
-                const bool in = rm1 >= t0 && rm1 > -CUDART_INF_F;
-                const bool whole = in && col_rm2(r) >= t0;     // more than one tile of this column may hold a top-K logit
-                const int tb = __shfl_sync(0xFFFFFFFFu, my_first, s);
-                const unsigned m = __ballot_sync(0xFFFFFFFFu, in && !whole);
-                if (m) {                                       // one tile each: one counter update per warp
-                    int base = 0;
-                    if (lane == 0) base = atomicAdd(&fs.nshares, __popc(m));
-                    base = __shfl_sync(0xFFFFFFFFu, base, 0);
-                    const int pos = base + __popc(m & ((1u << lane) - 1u));
-                    if (in && !whole && pos < kShareCap) fs.shares[pos] = ((uint32_t)(tb + col_t1(r)) << 8) | (uint32_t)col;
+                if (rm1 >= t0 && rm1 > -CUDART_INF_F) {
+                    (col_rm2(r) >= t0 ? all : one) |= 1u << s; // more than one tile of this column: all
+                    t1 = col_t1(r);
                 }
-                if (whole) {
-                    const int te = slice_first_tile(s + 1, nslices, ntiles_row);
-                    const int pos = atomicAdd(&fs.nshares, te - tb);
-                    for (int t = tb; t < te; ++t)
-                        if (pos + (t - tb) < kShareCap) fs.shares[pos + (t - tb)] = ((uint32_t)t << 8) | (uint32_t)col;
+            }
+            const unsigned some = __ballot_sync(0xFFFFFFFFu, (one | all) != 0u);
+            if (!some) continue;
+            int base = 0;
+            if (!__any_sync(0xFFFFFFFFu, all != 0u || (one & (one - 1u)) != 0u)) {     // one share a lane at most: the usual case
+                if (lane == 0) base = atomicAdd(&fs.nshares, __popc(some));
+                const int pos = __shfl_sync(0xFFFFFFFFu, base, 0) + __popc(some & ((1u << lane) - 1u));
+                if (one && pos < kShareCap)
+                    fs.shares[pos] = ((uint32_t)((nslices == 1 ? 0 : slice_first_tile(__ffs(one) - 1, nslices, ntiles_row)) + t1) << 8) | (uint32_t)col;
+                continue;
+            }
+            int n = __popc(one);
+            for (unsigned m = all; m; m &= m - 1) {
+                const int s = __ffs(m) - 1;
+                n += slice_first_tile(s + 1, nslices, ntiles_row) - slice_first_tile(s, nslices, ntiles_row);
+            }
+            const int incl = warp_scan_incl(n, lane);
+            if (lane == 31) base = atomicAdd(&fs.nshares, incl);
+            int pos = __shfl_sync(0xFFFFFFFFu, base, 31) + incl - n;
+            for (unsigned m = one | all; m; m &= m - 1) {
+                const int s = __ffs(m) - 1;
+                int t = slice_first_tile(s, nslices, ntiles_row), te = slice_first_tile(s + 1, nslices, ntiles_row);
+                if (one >> s & 1u) {
+                    t += col_t1(stash[s * kThreads + col]);
+                    te = t + 1;
                 }
+                for (; t < te; ++t, ++pos)
+                    if (pos < kShareCap) fs.shares[pos] = ((uint32_t)t << 8) | (uint32_t)col;
             }
         }
         select_barrier(nsel);

@@ -144,7 +144,7 @@ __device__ __forceinline__ void stream_begin(StreamBars &bars, int nstages) {
 // The tiles of a row dealt to its slices as evenly as whole tiles allow: slice s of n covers the
 // tiles [s * T / n, (s + 1) * T / n) of the row's T tiles (n <= T, so no slice is empty).
 __host__ __device__ __forceinline__ int slice_first_tile(int slice, int nslices, int ntiles_row) {
-    return (int)((long long)slice * ntiles_row / nslices);
+    return (int)((unsigned)slice * (unsigned)ntiles_row / (unsigned)nslices);      // at most 32 slices of 2^31 / 6144 tiles
 }
 template <typename DT>
 __device__ __forceinline__ void slice_range(int slice, int nslices, int ntiles_row, int V, int &s0, int &s1) {
