@@ -9,9 +9,9 @@
 // logit, a later one does not, so pieces before t's count what exceeds the next smaller number and the others what exceeds t's logit.
 // It is looked for only in tiles whose largest logit reaches the token's.
 //
-// The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 85 us = 5.5 TB/s, 0.85 of a
-// plain copy's rate; 272 rows with 20 alternatives 29 us (0.34: the selection, by one CTA a row, is 6 of them, the rest is that 272 rows are less than
-// two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 45 us (0.67: a row is six tiles, and while one warp finishes it the CTA's ring is
+// The floor is one read of the rows.  Measured (device time): 2048 rows of 152064 bf16 of which 25% are not read, 84 us = 5.5 TB/s, 0.86 of a
+// plain copy's rate; 272 rows with 20 alternatives 30 us (0.34: the selection, by one CTA a row, is 7 of them, the rest is that 272 rows are less than
+// two waves); 2048 rows of 32003 fp32, 26% not read, nine tokens a row, 44 us (0.68: a row is six tiles, and while one warp finishes it the CTA's ring is
 // empty; with three CTAs an SM 17 of 24 warps were active, 38% of the issue slots and 26% of the exponential unit taken).  CTAs that stay and take row
 // after row measured 50 us there and 94 on the first: rows that are not read leave some of them idle.
 #include <string.h>
@@ -575,8 +575,8 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     if (workspace_bytes < w.rs.end) return DSP_ERR_WORKSPACE;
     const int C = a.ntiles_row < kMaxCluster ? a.ntiles_row : kMaxCluster;
     // Few rows go to clusters, as long as an SM gets two or three tiles.  Measured (us, cluster / slices and tickets; bf16, 5 alternatives if
-    // not said otherwise): 1 row of 152064 12.1 / 16.9, without alternatives 7.1 / 10.0, fp32 12.6 / 22.6; 17 rows 14.5 / 16.4, fp32 18.9 / 17.9;
-    // 34 rows 18.5 / 16.8; of 32003 68 rows 12.0 / 13.6, 136 rows 16.5 / 14.3.
+    // not said otherwise): 1 row of 152064 9.5 / 13.2, without alternatives 6.6 / 9.6, fp32 9.8 / 15.0; 17 rows 11.6 / 14.3, fp32 15.9 / 14.9;
+    // 34 rows 15.5 / 15.3; of 32003 68 rows 11.1 / 12.9, 136 rows 15.6 / 14.2.
     if (C > 1 && a.ntiles_row <= kClusterTiles * kMaxCluster && 2 * rows * a.ntiles_row <= 5 * device_sm_count())
         return launch_score_cluster<DT>(a, rows, C, st);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
@@ -591,8 +591,8 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     prep.zero_b = a.row_status; prep.n_b = a.B;
     DSP_CUDA_TRY(launch_prepare(prep, st));
     // More than three CTAs an SM: four, with fewer registers and a ring of two tiles, if the finish has room in it.  Measured with three (us,
-    // four / three, bf16): 2048 rows of 152064 84.7 / 86.5, 500 with 20 alternatives 45.5 / 53.7; 2000 of 8000 with 5 alternatives 37 / 43; 2048 of
-    // 32003 fp32 45.0 / 47.4; five, with one tile: 102.7 for the first and 52.1 for the last.  272 rows, for which three are room enough: 30.1 / 29.2.
+    // four / three, bf16): 2048 rows of 152064 84.2 / 85.8, 500 with 20 alternatives 46.6 / 53.1; 2000 of 8000 with 5 alternatives 36 / 43; 2048 of
+    // 32003 fp32 43.6 / 45.8; five, with one tile: 102.7 for the first and 52.1 for the last.
     if (nblocks > 3ll * device_sm_count() && kFinishBytes + a.nslices * kThreads * 8 <= 2 * kTileBytes) {
         a.nstages = 2;
         static RingSmemDone done;                        // one per kernel
