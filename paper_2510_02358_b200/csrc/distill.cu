@@ -305,7 +305,7 @@ __device__ void store_zeros(DT *grow, int v0, int v1) {
 // with the teacher's log-sum-exp of each warp in red[warp][0].  Every thread of the CTA.
 __device__ __forceinline__ void probabilities(const DistillArgs &a, int &id, float t, float t_lse, const int *ids, double (*red)[3], double &lp,
                                               double &pk, double &P) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     if (id >= 0) {                              // of equal ids the first slot counts
         bool twice = false;
         const int4 *quads = reinterpret_cast<const int4 *>(ids);
@@ -354,7 +354,7 @@ __device__ __forceinline__ void probabilities(const DistillArgs &a, int &id, flo
 // the drafter is near the teacher, one of E does not (mean error of losses around 0.03: 1e-6 of themselves with 32 bits).
 __device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int id, double lp, double pk, double P, float xt, const Known &kn,
                                          double (*red)[3]) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     float *state = a.state ? a.state + (long long)row * (a.K + 4) : nullptr;
     if (warp * 32 < a.K) {
         double h = 0.0, m = 0.0, e = 0.0;
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ Shared sh;
     DT *buf = reinterpret_cast<DT *>(ring);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     const int C = a.C, rank = C > 1 ? (int)cluster_rank() : 0;
     const unsigned row32 = blockIdx.x >> a.log2_c;
     const long long row = row32;
@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const Distill
     __shared__ Known s_known;
     __shared__ double s_red[kWarps][3];
     __shared__ unsigned s_outer;                 // which of the elements outside of the streamed part are the teacher's
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     const unsigned row32 = blockIdx.x;
     const long long row = row32;
     const float w = a.weight ? a.weight[row] : 1.f;

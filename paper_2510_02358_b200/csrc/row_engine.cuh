@@ -106,7 +106,7 @@ __device__ bool row_finish(const DT *__restrict__ rowp, int V, int K, bool sums,
                            RowResult &res) {
     constexpr int N = Elem<DT>::N;
     constexpr int TE = tile_elems<DT>();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     FinishSmem &fs = *reinterpret_cast<FinishSmem *>(smem);
     const uint2 *stash = reinterpret_cast<const uint2 *>(smem + kFinishBytes);
 
@@ -298,7 +298,7 @@ template <typename DT, typename Pass>
 __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums, long long row, int slice,
                            int nslices, int ntiles_row, int nstages, const RowScratch &ws, unsigned *status_word,
                            StreamBars &bars, unsigned char *ring, RowResult &res, Pass &pass) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     int s0, s1;
     slice_range<DT>(slice, nslices, ntiles_row, V, s0, s1);
 

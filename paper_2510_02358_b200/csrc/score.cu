@@ -328,7 +328,7 @@ template <typename DT>
 __device__ bool score_sums(const ScoreArgs &a, const DT *inner, long long row, int slice, int b, StreamBars &bars, unsigned char *ring,
                            TokenPass<DT> &pass, RowResult &r) {
     __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     int s0, s1;
     slice_range<DT>(slice, a.nslices, a.ntiles_row, a.inner, s0, s1);
     ColTop top;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
     __shared__ HandIn hand;
     const unsigned C = (unsigned)a.nslices, row32 = blockIdx.x / C, rank = cluster_rank();
     const long long row = row32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     const int b = (int)(row32 / (unsigned)a.L), l = (int)(row32 - (unsigned)b * (unsigned)a.L);
     if (a.row_len && l >= a.row_len[b]) {                // the whole cluster alike
         if (rank == 0 && warp == 0) score_nothing(a, row, lane);

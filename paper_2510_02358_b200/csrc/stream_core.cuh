@@ -73,6 +73,10 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
         : "memory");
 }
 
+// The thread's warp, in a form that the compiler knows to be the same for all of its lanes: shuffles and votes in code that one warp
+// alone runs are then single instructions.
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0); }
+
 // Clusters of CTAs: place in the cluster; a barrier of all its threads, whose writes before arrive are seen after wait (arrive_empty: nothing
 // is ordered).
 __device__ __forceinline__ uint32_t cluster_rank() {
