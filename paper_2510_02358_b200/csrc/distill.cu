@@ -70,6 +70,7 @@ struct Known {               // of the row, after the exchange
     int none;
 };
 struct Shared : CopyBar {
+    uint64_t got;                               // clusters: what the row's CTAs send has arrived
     Known known;
     Place place;
     __align__(16) Part part[kMaxCluster * kWarps];
@@ -78,11 +79,14 @@ struct Shared : CopyBar {
     double red[kWarps][3];
 };
 
-__device__ __forceinline__ void put_remote(uint32_t addr, float v0, float v1, float v2, float v3) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v0), "f"(v1), "f"(v2), "f"(v3) : "memory");
+// Stores into another CTA of the cluster that are counted, in bytes, by a barrier there: no fence is needed on either side.  For launches with
+// clusters alone.
+__device__ __forceinline__ void send_counted(uint32_t addr, uint32_t bar, float v0, float v1, float v2, float v3) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(addr), "f"(v0), "f"(v1), "f"(v2), "f"(v3), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void put_remote(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+__device__ __forceinline__ void send_counted(uint32_t addr, uint32_t bar, float v) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(addr), "f"(v), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -137,19 +141,21 @@ __device__ __forceinline__ void read_edges(const DT *row, const Pieces<DT> &p, i
     });
 }
 
-// Waits for a buffer's copies, asleep for a microsecond at a time: other CTAs of the SM have the issue slots meanwhile.
-__device__ __forceinline__ void take_copies(CopyBar &sh, uint32_t parity) {
+// Waits for a buffer's copies (or what `bar` counts), asleep for a microsecond at a time: other CTAs of the SM have the issue slots meanwhile.
+__device__ __forceinline__ void take(uint64_t &bar, CopyBar &sh, uint32_t parity) {
     const long long t0 = clock64();
     for (int turn = 0; turn < 2; ++turn) {
         do {
             uint32_t ok;
             asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
-                         : "=r"(ok) : "r"(smem_addr(&sh.bar)), "r"(parity), "r"(1000u) : "memory");
+                         : "=r"(ok) : "r"(smem_addr(&bar)), "r"(parity), "r"(1000u) : "memory");
             if (ok) return;
         } while (clock64() - t0 < (turn + 1) * kWaitCycles);
         sh.timed_out = 1;                       // once more, so that no copy is under way into a buffer that is used again
     }
 }
+
+__device__ __forceinline__ void take_copies(CopyBar &sh, uint32_t parity) { take(sh.bar, sh, parity); }
 
 template <typename DT> __device__ __forceinline__ float elem_of(const DT *buf, int i) { return Elem<DT>::load1(buf + i); }
 template <typename DT> __device__ __forceinline__ void hide(DT *buf, int i) {
@@ -449,7 +455,18 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     const int C = a.C, rank = C > 1 ? (int)cluster_rank() : 0;
     const unsigned row32 = blockIdx.x >> a.log2_c;
     const long long row = row32;
-    if (tid == 0) {
+    // ---- the teacher's list, one slot a thread: its probabilities are formed while the copies are under way ----
+    int id = -1;
+    float t = -CUDART_INF_F;
+    const bool tail = a.tlse != nullptr;
+    const float t_lse = tail ? a.tlse[row] : 0.f;
+    if (tid < a.K) {
+        id = a.id[row * a.K + tid];
+        t = a.val[row * a.K + tid];
+        const int n = a.count ? a.count[row] : a.K;
+        if (tid >= n || id < 0 || id >= a.V) id = -1;
+    }
+    if (tid == kDT - 1) {                       // the warp that has a list only if it is a long one
         Place &at = sh.place;
         const float w0 = a.weight ? a.weight[row] : 1.f;
         const unsigned b0 = row32 / (unsigned)a.L, l0 = row32 - b0 * (unsigned)a.L;
@@ -463,19 +480,9 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         at.w = w0;
         sh.timed_out = 0;
         mbar_init(&sh.bar, 1);
+        mbar_init(&sh.got, 1);
         mbar_init_fence();
         if (w0 != 0.f) send_copies<DT>(x0, p, at.p0, min(at.p1, at.p0 + a.buf_vecs), buf, sh);
-    }
-    // ---- the teacher's list, one slot a thread: its probabilities are formed while the copies are under way ----
-    int id = -1;
-    float t = -CUDART_INF_F;
-    const bool tail = a.tlse != nullptr;
-    const float t_lse = tail ? a.tlse[row] : 0.f;
-    if (tid < a.K) {
-        id = a.id[row * a.K + tid];
-        t = a.val[row * a.K + tid];
-        const int n = a.count ? a.count[row] : a.K;
-        if (tid >= n || id < 0 || id >= a.V) id = -1;
     }
     sh.id[tid] = id;
     __syncthreads();
@@ -502,6 +509,11 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     };
     double lp, pk, P;                           // log p_k, p_k, their sum (tail: of the warp's, in sh.red)
     probabilities(a, id, t, t_lse, sh.id, sh.red, lp, pk, P);
+    if (C > 1) {
+        const int known = __syncthreads_count(id >= 0);
+        if (tid == 0) mbar_expect_tx(&sh.got, (uint32_t)(C * kWarps * sizeof(Part)) + (rank == 0 ? 4u * (uint32_t)known : 0u));
+        cluster_wait();                         // the other CTAs are there
+    }
     const int piece = id >= 0 ? (p.h + id) / N : -1;      // where the slot's token lies
     const bool mine = piece >= p0 && piece < p1;
 
@@ -534,18 +546,14 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
         w1.E = sum_of_warp(mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f);
     }
     if (C > 1) {
-        cluster_wait();                         // the other CTAs are there
-        if (mine) put_remote(at_rank(&sh.xk[tid], 0), xk);
-        if (lane < C) put_remote(at_rank(&sh.part[rank * kWarps + warp], lane), w1.c, w1.S, w1.ct, w1.E);
-        __syncwarp();
-        cluster_arrive();
+        if (mine) send_counted(at_rank(&sh.xk[tid], 0), at_rank(&sh.got, 0), xk);
+        if (lane < C) send_counted(at_rank(&sh.part[rank * kWarps + warp], lane), at_rank(&sh.got, lane), w1.c, w1.S, w1.ct, w1.E);
+        if (warp == 0) take(sh.got, sh, 0u);
     } else {
         if (mine) sh.xk[tid] = xk;
         if (lane == 0) sh.part[warp] = w1;
+        __syncthreads();
     }
-
-    if (C > 1) cluster_wait();
-    else __syncthreads();
 
     // ---- the row, by one warp for all ----
     if (warp == 0) {
