@@ -13,13 +13,12 @@
 // four numbers (two references, two sums) to all CTAs of the row over distributed shared memory, once.  The CTAs of an SM belong to
 // different rows, so one loads while another sums.
 //
-// Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 252 us, which is
-// 4.7 TB/s or 0.73 of a plain copy's rate; 999 rows of 32003 fp32 61 us (0.65); 512 rows of 152064 bf16 in two calls 91 us (0.79; the gradient's
-// call alone 46 us, a copy's rate); 16 rows 9 us.  Of 512 rows in one call, 75 us under the profiler, 49% of the issue slots and 56% of the
-// exponential unit are taken, half of the 1100 instructions a warp belong to the row and not to its logits, and 41% of the warps' waits are at
-// barriers, for the copies and the exchange, which five CTAs an SM cover in part.  Other forms measured on 2048 rows: clusters that
-// stay and load the next row into a second buffer 434 us, a row in one CTA with what does not fit read again from L2 276 us; a cubic for part
-// of the exponentials: within 2%.
+// Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 218 us, which is
+// 5.4 TB/s or 0.84 of a plain copy's rate; 999 rows of 32003 fp32 50.5 us (0.79); 512 rows of 152064 bf16 in two calls 91 us (0.80; the gradient's
+// call alone 46 us, a copy's rate); 16 rows 7.8 us.  What bounds the one call is the chain of a row: list, copies, sums, exchange, factors, gradient,
+// of which five CTAs an SM cover most.  On 2048 rows the exchange with a cluster barrier's fences took 250 us, counted stores 228, the loss beside the
+// gradient 218.  Other forms measured there, before these: clusters that stay and load the next row into a second buffer 434 us, a row in one CTA
+// with what does not fit read again from L2 276 us; a cubic for part of the exponentials: within 2%.
 #include "stream_core.cuh"
 
 namespace dsp {
@@ -29,7 +28,7 @@ constexpr int kDT = 256;                        // threads of a CTA: one per tea
 static_assert(kDT == DSP_MAX_TEACHER && kDT == kThreads, "one thread per slot");
 constexpr int kMaxCluster = 8;
 // A CTA's share of a row, 64 KB, unless the cluster is at its largest.  Measured with 40 KB (us, 40 / 64 KB): 1000 rows of 100000 bf16 112 / 91,
-// of 128256 126 / 116, of 32000 35.3 / 33.1, 999 of 32003 fp32 64 / 61; with 80 KB 2048 rows of 152064 bf16 take 285 instead of 255.
+// of 128256 126 / 116, of 32000 35.3 / 33.1, 999 of 32003 fp32 64 / 61; with 80 KB 2048 rows of 152064 bf16 took 285 instead of 255.
 constexpr int kSliceVecs = 4096;
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no part
 
@@ -106,9 +105,8 @@ struct Pieces {
 };
 // Calls at(element, place) for the elements of the partly outside pieces among [a, b), one element a thread; outside: element -1.
 template <typename DT, typename At>
-__device__ __forceinline__ void edges(const Pieces<DT> &p, int V, int a, int b, At at) {
+__device__ __forceinline__ void edges(const Pieces<DT> &p, int V, int a, int b, int tid, At at) {
     constexpr int N = Elem<DT>::N;
-    const int tid = threadIdx.x;
     auto one = [&](int piece, int e) {
         const int v = piece * N + e - p.h;
         at(v >= 0 && v < V ? v : -1, (piece - a) * N + e);
@@ -134,7 +132,7 @@ __device__ __forceinline__ void send_copies(const DT *row, const Pieces<DT> &p, 
 template <typename DT>
 __device__ __forceinline__ void read_edges(const DT *row, const Pieces<DT> &p, int V, int a, int b, DT *buf) {
     if (p.lo == 0 && p.hi == p.n) return;
-    edges<DT>(p, V, a, b, [&](int v, int place) {
+    edges<DT>(p, V, a, b, threadIdx.x, [&](int v, int place) {
         if (v >= 0) buf[place] = row[v];
         else if constexpr (Elem<DT>::N == 8) reinterpret_cast<unsigned short *>(buf)[place] = 0xFF80u;
         else reinterpret_cast<uint32_t *>(buf)[place] = 0xFF800000u;
@@ -182,7 +180,7 @@ __device__ __forceinline__ float sum_of_warp(float v) {
 // Sum of 2^(x s - c) over the buffer's pieces, by this thread's share.  The reference c of a warp is the largest exponent of its
 // first pieces: an fp32 sum also holds what exceeds it, so the others need no look at their maximum.  Where a sum passes 2^64 (or a
 // logit is not finite) the warp sums once more against its true maximum, so that no sum is lost below another warp's reference.
-// Two logits an instruction where the hardware has one (2048 rows of 152064 bf16: 256 to 252 us).
+// Two logits an instruction where the hardware has one (2048 rows of 152064 bf16: 256 to 252 us at the time).
 template <typename DT>
 __device__ __forceinline__ void add_piece(const uint4 &v, float s, float c, unsigned long long &S) {
     const unsigned long long s2 = pack2(s, s), nc2 = pack2(-c, -c);
@@ -261,29 +259,29 @@ __device__ __forceinline__ void put_one(DT *to, const uint4 &t, int e) {
     }
 }
 // The gradient of pieces [a, b) from their logits in the buffer, the teacher's tokens aside.  Rows of the gradient that start where the
-// logits' do within 16 bytes take whole pieces, others are written element by element.
+// logits' do within 16 bytes take whole pieces (then the first `skip` threads may stay away), others are written element by element.
 template <typename DT>
-__device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf, float s, float c, float f) {
+__device__ __forceinline__ bool same_start(const DT *grow, const Pieces<DT> &p) {
+    return (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % Elem<DT>::N) == p.h;
+}
+template <typename DT>
+__device__ __forceinline__ void write_pieces(DT *grow, const Pieces<DT> &p, int V, int a, int b, DT *buf, float s, float c, float f, int skip = 0) {
     constexpr int N = Elem<DT>::N;
     uint4 *bp = reinterpret_cast<uint4 *>(buf);
-    const bool same = (int)((reinterpret_cast<uintptr_t>(grow) / sizeof(DT)) % N) == p.h;
-    if (same) {
+    if (same_start(grow, p)) {
         const int l = max(a, p.lo), u = min(b, p.hi);
         uint4 *gp = reinterpret_cast<uint4 *>(grow + ((long long)l * N - p.h));
         const uint4 *from = bp + (l - a);
-        const int tid = threadIdx.x, rest = (u - l) % kDT;
-        from += tid;
-        gp += tid;
-        int k = (u - l) / kDT;
-        for (; k >= 2; k -= 2, from += 2 * kDT, gp += 2 * kDT) {
-            const uint4 v0 = from[0], v1 = from[kDT];
-            gp[0] = turned<DT>(v0, s, c, f);
-            gp[kDT] = turned<DT>(v1, s, c, f);
+        const int me = (int)threadIdx.x - skip, step = kDT - skip;
+        int i = me;
+        for (; i + step < u - l; i += 2 * step) {
+            const uint4 v0 = from[i], v1 = from[i + step];
+            gp[i] = turned<DT>(v0, s, c, f);
+            gp[i + step] = turned<DT>(v1, s, c, f);
         }
-        if (k) { gp[0] = turned<DT>(from[0], s, c, f); from += kDT; gp += kDT; }
-        if (tid < rest) gp[0] = turned<DT>(from[0], s, c, f);
+        if (i < u - l) gp[i] = turned<DT>(from[i], s, c, f);
         if (p.lo == 0 && p.hi == p.n) return;
-        edges<DT>(p, V, a, b, [&](int v, int place) {
+        edges<DT>(p, V, a, b, me, [&](int v, int place) {
             if (v < 0) return;
             put_one<DT>(grow + v, turned<DT>(bp[place / N], s, c, f), place % N);
         });
@@ -355,11 +353,11 @@ __device__ __forceinline__ void probabilities(const DistillArgs &a, int &id, flo
     }
 }
 
-// Loss and what else a row is told, by every thread of a CTA; x: the slot's token under the student.  The student's mass of the teacher's
+// Loss and what else a row is told, by the first n threads of a CTA, all that have slots among them; x: the slot's token under the student.  The student's mass of the teacher's
 // tokens is summed once more in 64 bits: with dloss = (s - r) dS / S + (1 - s) dE / E, an error of the other tokens' sum S nearly cancels where
 // the drafter is near the teacher, one of E does not (mean error of losses around 0.03: 1e-6 of themselves with 32 bits).
 __device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int id, double lp, double pk, double P, float xt, const Known &kn,
-                                         double (*red)[3]) {
+                                         double (*red)[3], int n) {
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_index();
     float *state = a.state ? a.state + (long long)row * (a.K + 4) : nullptr;
     if (warp * 32 < a.K) {
@@ -375,7 +373,7 @@ __device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int
         if (lane == 0) { red[warp][0] = h; red[warp][1] = m; red[warp][2] = e; }
     }
     if (state && tid < a.K && id < 0) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
-    __syncthreads();
+    asm volatile("bar.sync 1, %0;" ::"r"(n) : "memory");
     if (tid == 0) {
         double H = 0.0, accept = 0.0, E = 0.0;
         for (int i = 0; i * 32 < a.K; ++i) { H += red[i][0]; accept += red[i][1]; E += red[i][2]; }
@@ -444,7 +442,7 @@ __device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *part
     return kn;
 }
 
-// Five CTAs an SM: 2048 rows of 152064 bf16 255 us, with four (and more registers) 271; 16 rows 9.0 and 8.6.
+// Five CTAs an SM, not four with more registers: 2048 rows of 152064 bf16 255 and 271 us, 16 rows 9.0 and 8.6 (before the counted exchange).
 template <typename DT, bool GRAD>
 __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     constexpr int N = Elem<DT>::N;
@@ -568,6 +566,15 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
     float gk = 0.f;                             // the slot's gradient for a weight of 1
     if (mine) gk = none ? 0.f : (float)(((double)__fdividef(ex2_approx((float)(zs - (double)c_all)), all) - pk) * a.inv_t);
     if (state && mine) state[4 + tid] = gk;
+    // Loss and what else the row is told, by the first CTA: while the others write the gradient by the warps with slots alone, if those are few and
+    // the pieces are whole ones (us, so / by all warps after the gradient: 1000 rows of 32000 bf16 30.7 / 33.9, 999 of 32003 fp32 50.5 / 55.2, 16 of 152064 7.8 / 8.7).
+    int skip = 0;
+    if (rank == 0) {
+        const int listed = (a.K + 31) / 32 * 32;
+        if (GRAD && listed <= kDT / 4 && chunks == 1 && same_start(g, p)) skip = listed;
+        if (skip == 0 || tid < skip)
+            tell_row(a, row32, id, lp, pk, P, tid < a.K && id >= 0 ? sh.xk[tid] : 0.f, sh.known, sh.red, skip ? skip : kDT);
+    }
     if constexpr (GRAD) {
         for (int k = 0;;) {
             // one chunk: it is in the buffer still, without the teacher's tokens; several: once more from the first on
@@ -581,14 +588,12 @@ __global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
                 parity ^= 1u;
                 __syncthreads();
             }
-            write_pieces<DT>(g, p, a.V, q0, q1, buf, a.s, c_f, f * w);
+            if (tid >= skip) write_pieces<DT>(g, p, a.V, q0, q1, buf, a.s, c_f, f * w, skip);
             __syncthreads();                    // the token's own element comes after the piece that it lies in
             if (piece >= q0 && piece < q1) g[id] = rounded<DT>(gk * w);
             if (++k >= chunks) break;
         }
     }
-    // ---- loss and what else the row is told: the first CTA, while the stores are under way ----
-    if (rank == 0) tell_row(a, row32, id, lp, pk, P, tid < a.K && id >= 0 ? sh.xk[tid] : 0.f, sh.known, sh.red);
     if (tid == 0 && sh.timed_out && a.status) atomicOr(&a.status[row32 / (unsigned)a.L], DSP_ROW_TIMEOUT);
 }
 
@@ -776,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const Distill
         const float q = __fdividef(ex2_approx((float)((double)xt * (double)a.s - (double)s_known.c_all)), s_known.all);
         a.state[row * (a.K + 4) + 4 + tid] = s_known.none ? 0.f : (float)(((double)q - pk) * a.inv_t);
     }
-    tell_row(a, row32, id, lp, pk, P, xt, s_known, s_red);
+    tell_row(a, row32, id, lp, pk, P, xt, s_known, s_red, kThreads);
     if (tid == 0 && bars.timed_out && a.status) atomicOr(&a.status[b], DSP_ROW_TIMEOUT);
 }
 
