@@ -442,9 +442,9 @@ __device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *part
     return kn;
 }
 
-// Five CTAs an SM, not four with more registers: 2048 rows of 152064 bf16 255 and 271 us, 16 rows 9.0 and 8.6 (before the counted exchange).
-template <typename DT, bool GRAD>
-__global__ void __launch_bounds__(kDT, 5) distill_kernel(const DistillArgs a) {
+// CTAS: of an SM.
+template <typename DT, bool GRAD, int CTAS>
+__global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a) {
     constexpr int N = Elem<DT>::N;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ Shared sh;
@@ -848,6 +848,26 @@ inline int pieces_at_most(int V, int N) { return (int)(((long long)V + 2 * N - 2
 
 constexpr int kMaxBufVecs = 216 * 1024 / 16;
 
+template <typename DT, bool GRAD, int CTAS>
+int32_t launch_distill_rows(const DistillArgs &a, long long rows, cudaStream_t st) {
+    static std::atomic<unsigned long long> smem_done{0};
+    DSP_CUDA_TRY(allow_shared(distill_kernel<DT, GRAD, CTAS>, kMaxBufVecs * 16, smem_done));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * a.C));
+    cfg.blockDim = dim3(kDT);
+    cfg.dynamicSmemBytes = (size_t)a.buf_vecs * 16;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.C > 1 ? 1 : 0;
+    DSP_CUDA_TRY(cudaLaunchKernelEx(&cfg, distill_kernel<DT, GRAD, CTAS>, a));
+    DSP_CUDA_TRY(cudaGetLastError());
+    return DSP_OK;
+}
+
 template <typename DT, bool GRAD>
 int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     constexpr int N = Elem<DT>::N;
@@ -862,22 +882,10 @@ int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     const int per = (n + C - 1) / C;
     a.buf_vecs = per < kMaxBufVecs ? per : kMaxBufVecs;
     if (rows * C > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
-    static std::atomic<unsigned long long> smem_done{0};
-    DSP_CUDA_TRY(allow_shared(distill_kernel<DT, GRAD>, kMaxBufVecs * 16, smem_done));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * C));
-    cfg.blockDim = dim3(kDT);
-    cfg.dynamicSmemBytes = (size_t)a.buf_vecs * 16;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)C;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 1 : 0;
-    DSP_CUDA_TRY(cudaLaunchKernelEx(&cfg, distill_kernel<DT, GRAD>, (const DistillArgs)a));
-    DSP_CUDA_TRY(cudaGetLastError());
-    return DSP_OK;
+    // Five CTAs an SM where their buffers fit and there are as many, else four, with more registers.  Measured (us, five / four): 2048 rows of
+    // 152064 bf16 217 / 235; 1000 of 100000 79.2 / 77.2, of 32000 30.7 / 29.9, 999 of 32003 fp32 50.5 / 49.1, whose buffers let three fit.
+    if (a.buf_vecs <= 2560 && rows * C > 4 * device_sm_count()) return launch_distill_rows<DT, GRAD, 5>(a, rows, st);
+    return launch_distill_rows<DT, GRAD, 4>(a, rows, st);
 }
 
 constexpr int kLongRow = 75000;                 // logits from which a row is streamed for its loss: see dsp_distill's dispatch
