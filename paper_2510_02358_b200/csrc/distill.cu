@@ -14,9 +14,9 @@
 // different rows, so one loads while another sums.
 //
 // Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 218 us, which is
-// 5.4 TB/s or 0.84 of a plain copy's rate; 999 rows of 32003 fp32 50.5 us (0.79); 512 rows of 152064 bf16 in two calls 91 us (0.80; the gradient's
-// call alone 46 us, a copy's rate); 16 rows 7.8 us.  What bounds the one call is the chain of a row: list, copies, sums, exchange, factors, gradient,
-// of which five CTAs an SM cover most.  On 2048 rows the exchange with a cluster barrier's fences took 250 us, counted stores 228, the loss beside the
+// 5.4 TB/s or 0.84 of a plain copy's rate; 999 rows of 32003 fp32 49 us (0.81); 512 rows of 152064 bf16 in two calls 91 us (0.80; the gradient's
+// call alone 46 us, a copy's rate); 16 rows 7.7 us.  What bounds the one call is the chain of a row: list, copies, sums, exchange, factors, gradient,
+// of which the four or five CTAs of an SM cover most.  On 2048 rows the exchange with a cluster barrier's fences took 250 us, counted stores 228, the loss beside the
 // gradient 218.  Other forms measured there, before these: clusters that stay and load the next row into a second buffer 434 us, a row in one CTA
 // with what does not fit read again from L2 276 us; a cubic for part of the exponentials: within 2%.
 #include "stream_core.cuh"
@@ -954,8 +954,8 @@ extern "C" int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_
     const long long rows = (long long)B * L;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     // The loss alone of many long bf16 rows streams each in a CTA; measured with the gradient's call behind it, K = 16 (us, streamed / by
-    // clusters): 600 rows of 100000 76 / 90, of 200000 131 / 146, of 64000 57 / 55; 148 rows of 152064 32 / 33, 32 rows 22 / 13;
-    // fp32 (half the logits for the same bytes, the same work a tile) 600 rows of 100000 152 / 137.
+    // clusters): 512 rows of 152064 91 / 95, 148 rows 31.6 / 30.9, 32 rows 22 / 13; 600 rows of 100000 76 / 74, of 200000 131 / 136, of 64000 57 / 50;
+    // 2000 rows of 110000 225 / 252, of 80000 179 / 179; fp32 (half the logits for the same bytes, the same work a tile) 600 rows of 100000 152 / 127.
     if (!grad && dtype == DSP_BF16 && rows >= device_sm_count() && V >= kLongRow) return launch_distill_loss(a, rows, st);
     if (dtype == DSP_BF16)
         return grad ? launch_distill<__nv_bfloat16, true>(a, rows, st) : launch_distill<__nv_bfloat16, false>(a, rows, st);
