@@ -140,9 +140,9 @@ __device__ __forceinline__ void read_edges(const DT *row, const Pieces<DT> &p, i
 }
 
 // Waits for a buffer's copies (or what `bar` counts), asleep for a microsecond at a time: other CTAs of the SM have the issue slots meanwhile.
-__device__ __forceinline__ void take(uint64_t &bar, CopyBar &sh, uint32_t parity) {
+__device__ __forceinline__ void take(uint64_t &bar, CopyBar &sh, uint32_t parity, int turns = 2) {
     const long long t0 = clock64();
-    for (int turn = 0; turn < 2; ++turn) {
+    for (int turn = 0; turn < turns; ++turn) {
         do {
             uint32_t ok;
             asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
     if (C > 1) {
         if (mine) send_counted(at_rank(&sh.xk[tid], 0), at_rank(&sh.got, 0), xk);
         if (lane < C) send_counted(at_rank(&sh.part[rank * kWarps + warp], lane), at_rank(&sh.got, lane), w1.c, w1.S, w1.ct, w1.E);
-        if (warp == 0) take(sh.got, sh, 0u);
+        if (warp == 0) take(sh.got, sh, 0u, 4); // longer than a CTA waits for its copies: what it sends arrives before this one leaves
     } else {
         if (mine) sh.xk[tid] = xk;
         if (lane == 0) sh.part[warp] = w1;

@@ -419,15 +419,12 @@ constexpr int kMaxCluster = 8;
 constexpr int kClusterTiles = 4;             // tiles of a CTA, all in its ring at once
 constexpr int kFinishArea = kFinishBytes + kMaxCluster * kThreads * 8;
 struct HandIn {                              // in the first CTA
-    __align__(8) WarpPartial wp[kMaxCluster * kWarps];
-    unsigned counted[kMaxCluster * kWarps];
-    unsigned timed_out[kMaxCluster];
+    uint64_t got;                            // its barrier
+    __align__(8) WarpPartial wp[kMaxCluster * kWarps];     // pad: the warp's count of logits before the first token, its top bit a wait that ran out
 };
-__device__ __forceinline__ void put_remote(uint32_t addr, unsigned long long v) {
-    asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
-}
-__device__ __forceinline__ void put_remote(uint32_t addr, unsigned v) {
-    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+// Stores into the first CTA that are counted, in bytes, by a barrier there: no fence is needed on either side.
+__device__ __forceinline__ void send_counted(uint32_t addr, uint32_t bar, unsigned long long v) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(addr), "l"(v), "r"(bar) : "memory");
 }
 
 template <typename DT>
@@ -444,7 +441,6 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
         if (rank == 0 && warp == 0) score_nothing(a, row, lane);
         return;
     }
-    cluster_arrive_empty();
     const DT *rowp = reinterpret_cast<const DT *>(a.logits) + b * a.stride_b + l * a.stride_l;
     const int head = a.inner == a.V ? 0 : (int)((N - (reinterpret_cast<uintptr_t>(rowp) / sizeof(DT)) % N) % N);
     TokenPass<DT> pass;
@@ -455,7 +451,12 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
     pass.acc = nullptr;
     pass.s = a.s; pass.low = a.low;
     pass.V = a.V; pass.head = head; pass.inner = a.inner;
+    if (tid == 0) {                                      // before stream_begin's fence and barrier
+        mbar_init(&hand.got, 1);
+        mbar_expect_tx(&hand.got, C * (kWarps * (unsigned)sizeof(WarpPartial) + (a.K ? kThreads * 8u : 0u)));
+    }
     stream_begin(bars, a.nstages);
+    cluster_arrive_empty();
     int s0, s1;
     slice_range<DT>((int)rank, (int)C, a.ntiles_row, a.inner, s0, s1);
     ColTop top;
@@ -466,23 +467,22 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
     const unsigned counted = __reduce_add_sync(0xFFFFFFFFu, (unsigned)pass.n);
     unsigned char *area = ring + a.nstages * kTileBytes;
     cluster_wait();                                      // the first CTA is there
+    const uint32_t bar = at_rank(&hand.got, 0);
     if (a.K) {
         const uint2 col = pack_col(top);
-        put_remote(at_rank(area + kFinishBytes + (rank * kThreads + tid) * 8, 0), (unsigned long long)col.y << 32 | col.x);
+        send_counted(at_rank(area + kFinishBytes + (rank * kThreads + tid) * 8, 0), bar, (unsigned long long)col.y << 32 | col.x);
     }
     if (lane == 0) {
         const uint32_t to = at_rank(&hand.wp[rank * kWarps + warp], 0);
-        put_remote(to, (unsigned long long)__double_as_longlong(p.S));
-        put_remote(to + 8, (unsigned long long)__double_as_longlong(p.T));
-        put_remote(to + 16, __float_as_uint(p.c));
-        put_remote(at_rank(&hand.counted[rank * kWarps + warp], 0), counted);
+        const unsigned late = *static_cast<volatile int *>(&bars.timed_out) ? 0x80000000u : 0u;       // the warp saw its own waits run out
+        send_counted(to, bar, (unsigned long long)__double_as_longlong(p.S));
+        send_counted(to + 8, bar, (unsigned long long)__double_as_longlong(p.T));
+        send_counted(to + 16, bar, (unsigned long long)(counted | late) << 32 | __float_as_uint(p.c));
     }
-    __syncthreads();                                     // every warp's waits are over
-    if (tid == 0) put_remote(at_rank(&hand.timed_out[rank], 0), bars.timed_out ? (unsigned)DSP_ROW_TIMEOUT : 0u);
-    __syncwarp();
-    cluster_arrive();
-    cluster_wait();
     if (rank != 0) return;
+    volatile int never = 0;                              // twice as long as a CTA waits for its copies: what it sends arrives here before this one leaves
+    const bool there = mbar_wait(&hand.got, 0u, &never) || mbar_wait(&hand.got, 0u, &never);
+    unsigned trouble = __syncthreads_or(!there) ? (unsigned)DSP_ROW_TIMEOUT : 0u;
     RowResult r;
     if (a.K) {
         if (!row_finish<DT>(rowp + head, a.inner, a.K, true, row, (int)C, a.ntiles_row, a.rs, hand.wp, area, r)) return;
@@ -492,10 +492,13 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
         r.key = 0ull;
         r.nonfinite = false;
     }
-    unsigned before = 0u, trouble = lane < (int)C ? hand.timed_out[lane] : 0u;
-    for (unsigned i = lane; i < C * kWarps; i += 32) before += hand.counted[i];
+    unsigned before = 0u, late = 0u;
+    for (unsigned i = lane; i < C * kWarps; i += 32) {
+        before += (unsigned)hand.wp[i].pad & 0x7FFFFFFFu;
+        late |= (unsigned)hand.wp[i].pad >> 31;
+    }
     before = __reduce_add_sync(0xFFFFFFFFu, before);
-    trouble = __reduce_or_sync(0xFFFFFFFFu, trouble);
+    if (__any_sync(0xFFFFFFFFu, late != 0u)) trouble = DSP_ROW_TIMEOUT;
     grid_dependency_wait();                              // status words that several rows share are zeroed
     score_row<DT>(a, row, b, rowp, head, pass, r, a.K == 0, before, trouble, lane);
 }
@@ -575,7 +578,7 @@ int32_t launch_score(ScoreArgs &a, void *workspace, size_t workspace_bytes, cuda
     if (workspace_bytes < w.rs.end) return DSP_ERR_WORKSPACE;
     const int C = a.ntiles_row < kMaxCluster ? a.ntiles_row : kMaxCluster;
     // Few rows go to clusters, as long as an SM gets two or three tiles.  Measured (us, cluster / slices and tickets; bf16, 5 alternatives if
-    // not said otherwise): 1 row of 152064 9.5 / 13.2, without alternatives 6.6 / 9.6, fp32 9.8 / 15.0; 17 rows 11.6 / 14.3, fp32 15.9 / 14.9;
+    // not said otherwise): 1 row of 152064 8.9 / 13.2, without alternatives 6.4 / 9.6, fp32 9.2 / 15.0; 17 rows 11.6 / 14.3, fp32 15.9 / 14.9;
     // 34 rows 15.5 / 15.3; of 32003 68 rows 11.1 / 12.9, 136 rows 15.6 / 14.2.
     if (C > 1 && a.ntiles_row <= kClusterTiles * kMaxCluster && 2 * rows * a.ntiles_row <= 5 * device_sm_count())
         return launch_score_cluster<DT>(a, rows, C, st);
