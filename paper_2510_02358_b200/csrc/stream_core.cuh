@@ -77,14 +77,13 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
 // alone runs are then single instructions.
 __device__ __forceinline__ int warp_index() { return __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0); }
 
-// Clusters of CTAs: place in the cluster; a barrier of all its threads, whose writes before arrive are seen after wait (arrive_empty: nothing
-// is ordered).
+// Clusters of CTAs: place in the cluster; a barrier of all its threads, by which they know that the other CTAs are there and their shared
+// barriers set up (it orders no other writes).
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive_empty() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
