@@ -404,8 +404,13 @@ __device__ __forceinline__ void tell_nothing(const DistillArgs &a, unsigned row)
     }
     if (state && tid < a.K) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
 }
-// What follows from the sums of a row's n parts, by one warp (P: the list's sum).
-__device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, int lane) {
+// What follows from the sums of a row's n parts, by one warp (P: the list's sum, t_lse: the teacher's log-sum-exp).
+//
+// r = 1 - P has the rounding of the teacher's log-sum-exp in it, 2^-24 |t_lse| and as much again for whoever summed it, and a few 2^-24 of the
+// sum's own: where the list is all that the teacher allows, that is all that r is.  r log s would turn it into a loss of any size where the
+// drafter gives the others next to nothing (a common mask: s = 0, or e^-10000), so there it counts as nothing.  Where s is above r / 1024 the
+// formula stays: its term is within 7 r then.
+__device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, float t_lse, int lane) {
     Part q[kMaxCluster * kWarps / 32];
     float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
 #pragma unroll
@@ -436,6 +441,8 @@ __device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *part
     kn.all = (S != 0.f ? S * kn.to_all : 0.f) + (E != 0.f ? E * ex2_approx(cl - kn.c_all) : 0.f);
     const double r = a.tlse ? 1.0 - P : 0.0;
     kn.r = r < 0.0 ? 0.0 : r;               // NaN stays
+    const float rest = (float)kn.r;
+    if (rest > 0.f && rest <= 0x1p-23f * (fabsf(t_lse) + 4.f) && S * kn.to_all < rest * 0x1p-10f * kn.all) kn.r = 0.0;
     kn.none = !a.tlse && P == 0.0;           // the list says nothing: no gradient
     kn.f = kn.none || S == 0.f ? 0.f : (__fdividef(kn.to_all, kn.all) - __fdividef((float)kn.r, S)) * (float)a.inv_t;
     kn.c_f = S != 0.f ? cs : -kRefFloor;    // nothing to scale: every exponential is 0
@@ -557,7 +564,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
     if (warp == 0) {
         if (tail)
             for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
-        const Known kn = known_of(a, sh.part, C * kWarps, P, lane);
+        const Known kn = known_of(a, sh.part, C * kWarps, P, t_lse, lane);
         if (lane == 0) sh.known = kn;
     }
     __syncthreads();
@@ -772,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const Distill
     if (warp == 0) {
         if (a.tlse)
             for (int i = 0; i * 32 < a.K; ++i) P += s_red[i][0];
-        const Known kn = known_of(a, s_part, kWarps, P, lane);
+        const Known kn = known_of(a, s_part, kWarps, P, a.tlse ? a.tlse[row] : 0.f, lane);
         if (lane == 0) s_known = kn;
     }
     __syncthreads();

@@ -80,6 +80,8 @@ def distill(x, ids, t, T, lse=None, count=None, weight=None):
     others = logq.masked_fill(inside, -math.inf)
     log_s = torch.logsumexp(others, -1)
     s = log_s.exp()
+    if lse is not None:                                 # a rest that rounding alone can leave of a complete list, where s is nothing beside it
+        r = r.masked_fill((r <= 2.0 ** -23 * (lse.double().abs() + 4)) & (s < r / 1024), 0.0)
     qk = torch.where(use, q.gather(-1, at), torch.zeros_like(p))
     logk = logq.gather(-1, at)
     loss = torch.where(p > 0, p * (p.log() - logk), torch.zeros_like(p)).sum(-1) + torch.where(r > 0, r * (r.log() - log_s), torch.zeros_like(r))

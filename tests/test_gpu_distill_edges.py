@@ -1,0 +1,79 @@
+"""dsp_distill where the teacher's list is all that there is, or where nothing was read."""
+import math
+
+import pytest
+import torch
+
+import after_reference as ref
+from paper_2510_02358_b200 import binding as dsp
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+# rows of a cluster with and without the gradient, and rows that are streamed for their loss
+FORMS = [(2, 500, 5003, F32, True), (2, 500, 5003, F32, False), (3, 7, 40000, BF, True), (3, 7, 40000, BF, False), (4, 80, 80003, BF, False)]
+
+
+def grammar(B, L, V, dtype, allowed, mask, seed):
+    """Logits of which `allowed` tokens a row are not masked."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.full((B, L, V), mask, device="cuda").to(dtype)
+    at = torch.rand(B, L, V, generator=g, device="cuda").topk(allowed, -1).indices
+    return x.scatter_(2, at, (3.0 * torch.randn(B, L, allowed, generator=g, device="cuda")).to(dtype)), at
+
+
+@pytest.mark.parametrize("B,L,V,dtype,grad", FORMS)
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e9, -1e4])
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_a_teacher_under_the_drafters_mask(B, L, V, dtype, grad, mask, T):
+    """Scores of a masked target as the teacher's list.  Of the drafter equal to it the loss is the difference of the two log-sum-exps: each
+    off by the error of its sum, the teacher's rounded to 32 bits (2^-24 of it), the loss rounded too."""
+    mask = torch.finfo(dtype).min if mask == "lowest" else mask
+    x, at = grammar(B, L, V, dtype, 6, mask, V)
+    t = dsp.dsp_token_logprobs(x, K=8, temperature=T)
+    status = torch.zeros(B, dtype=torch.int32, device="cuda")
+    r = dsp.dsp_distill(x, t.top_id, t.top_logit, teacher_lse=t.lse, temperature=T, grad=grad, row_status=status)
+    mine = torch.full_like(x, -math.inf).scatter_(2, at, x.gather(2, at))
+    err = 2 * ref.exponent_error(mine, T, ref.terms(V)) + 2.0 ** -24 * (t.lse.double().abs() + 1)
+    assert not status.any()
+    assert (r.loss.double().abs() <= err).all(), (r.loss.abs().max().item(), err.max().item())
+    assert ((r.accept.double() - 1).abs() <= 2 * err).all()
+    g = r.grad if grad else dsp.dsp_distill_grad(x, t.top_id, r.state, torch.ones(B, L, device="cuda"), temperature=T)
+    assert (g.double().abs() <= 4 * err[..., None] / T).all()
+    # another drafter under the mask: the loss that the allowed tokens alone give.  With every log p_k off by d, which is the same for all,
+    # the sum of p (log p - log q) is off by d (1 + itself)
+    y = x.scatter(2, at, x.gather(2, at) + torch.randn(B, L, 6, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(dtype))
+    got = dsp.dsp_distill(y, t.top_id, t.top_logit, teacher_lse=t.lse, temperature=T, grad=grad).loss.double()
+    want = ref.distill(y, at, x.gather(2, at), T)[0]
+    yours = torch.full_like(y, -math.inf).scatter_(2, at, y.gather(2, at))
+    off = err + 2 * ref.exponent_error(yours, T, ref.terms(V))
+    assert ((got - want).abs() <= off * (1 + want) + 2.0 ** -24 * want).all(), (got - want).abs().max().item()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,K", [(1, 1), (2, 2), (9, 9), (9, 12), (32, 32), (200, 256)])
+def test_a_list_of_the_whole_vocabulary(V, K, dtype):
+    B, L = 5, 60
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (3.0 * torch.randn(B, L, V, generator=g, device="cuda")).to(dtype)
+    ids = torch.full((B, L, K), -1, dtype=torch.int32, device="cuda")
+    val = torch.zeros(B, L, K, device="cuda")
+    ids[..., :V], val[..., :V] = torch.arange(V, device="cuda", dtype=torch.int32), x.float()
+    lse = x.double().logsumexp(-1).float()
+    err = 2 * ref.exponent_error(x, 1.0, ref.terms(V)) + 2.0 ** -24 * (lse.double().abs() + 1)
+    for grad in (True, False):
+        r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, grad=grad)
+        assert (r.loss.double().abs() <= err).all(), r.loss.abs().max().item()
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_mass_of_the_teacher_that_the_drafter_has_no_token_for(grad):
+    """More than rounding: the loss is infinite, and the gradient is not."""
+    x, at = grammar(2, 40, 5003, F32, 6, -math.inf, 3)
+    t = dsp.dsp_token_logprobs(x, K=5)                               # a token short of all
+    y = torch.full_like(x, -math.inf).scatter_(2, t.top_id.long(), t.top_logit)
+    r = dsp.dsp_distill(y, t.top_id, t.top_logit, teacher_lse=t.lse, grad=grad)
+    some = 1 - (t.top_logp.double()).exp().sum(-1) > 1e-5
+    assert some.any() and (r.loss[some] == math.inf).all() and not r.loss.isnan().any()
+    if grad:
+        assert torch.isfinite(r.grad).all()
