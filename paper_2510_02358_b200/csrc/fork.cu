@@ -22,6 +22,9 @@ constexpr int kNobody = 0x7F7F7F7F;              // what a fill with bytes leave
 // 5.0 / 10.3, 16 + 16 of 8000 12.8 / 27.8, 32 + 32 of 500 9.5 / 9.3, of 2000 10.3 / 12.2, 40 + 40 of 500 11.2 / 9.3, 64 + 64 13.2 / 9.5, 500 + 500 67 / 10.6.
 constexpr long long kOneCtaRows = 64;
 constexpr int kOneCtaShared = 200 * 1024;
+constexpr int kPrefixWarps = 32;                 // of a CTA, at most: their sums lie in static shared memory
+// Dynamic shared memory of a launch that has not asked for more: 48 KB with the kernel's static share in them.
+constexpr int kSharedByDefault = 48 * 1024 - kPrefixWarps * 8;
 constexpr int kU = 4;                            // entries a lane has under way
 
 struct ForkArgs {
@@ -128,7 +131,7 @@ __device__ void part2(const ForkArgs &a, Crew c, int lane) {
 
 // Exclusive prefix sums over the rows of the blocks needed (low half) and given back (high half): [n] holds the totals.  Every thread of the CTA.
 __device__ void prefix(const ForkArgs &a, int n, unsigned long long *out) {
-    __shared__ unsigned long long s_warp[32];
+    __shared__ unsigned long long s_warp[kPrefixWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int per = (n + blockDim.x - 1) / blockDim.x;
     const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
@@ -268,13 +271,13 @@ int32_t launch_fork(const ForkArgs &a, size_t mark_bytes, cudaStream_t st) {
     const long long one = one_cta_bytes(a.Bi, a.Bo, a.n_blocks);
     if (rows <= kOneCtaRows && one <= kOneCtaShared) {
         static std::atomic<unsigned long long> done{0};
-        if (one > 48 * 1024) DSP_CUDA_TRY(allow_shared(fork_kernel, kOneCtaShared, done));
+        if (one > kSharedByDefault) DSP_CUDA_TRY(allow_shared(fork_kernel, kOneCtaShared, done));
         const unsigned threads = rows <= 8 ? 256u : 1024u;       // a warp for each row
         fork_kernel<<<1, threads, (size_t)one, st>>>(a);
     } else {
         static std::atomic<unsigned long long> done{0};
         const size_t smem = ((size_t)(a.Bi > a.Bo ? a.Bi : a.Bo) + 1) * 8;
-        if (smem > 48 * 1024) DSP_CUDA_TRY(allow_shared(fork_part_kernel<3>, (DSP_MAX_PLAN_ROWS + 1) * 8, done));
+        if (smem > kSharedByDefault) DSP_CUDA_TRY(allow_shared(fork_part_kernel<3>, (DSP_MAX_PLAN_ROWS + 1) * 8, done));
         constexpr int kTh = 256;
         long long grid = (rows + kTh / 32 - 1) / (kTh / 32);
         if (grid > 4 * 148) grid = 4 * 148;
