@@ -280,7 +280,7 @@ int32_t launch_fork(const ForkArgs &a, size_t mark_bytes, cudaStream_t st) {
         if (smem > kSharedByDefault) DSP_CUDA_TRY(allow_shared(fork_part_kernel<3>, (DSP_MAX_PLAN_ROWS + 1) * 8, done));
         constexpr int kTh = 256;
         long long grid = (rows + kTh / 32 - 1) / (kTh / 32);
-        if (grid > 4 * 148) grid = 4 * 148;
+        grid = grid < 1 ? 1 : grid > 4 * 148 ? 4 * 148 : grid;   // without rows the ring's ends are handed on
         DSP_CUDA_TRY(cudaMemsetAsync(a.holder, kNobody & 0xFF, mark_bytes, st));
         fork_part_kernel<1><<<(unsigned)grid, kTh, 0, st>>>(a);
         DSP_CUDA_TRY(cudaGetLastError());

@@ -37,3 +37,15 @@ def test_pools_and_rows_of_any_number(few, many):
     code = CHILD % (os.path.dirname(HERE), HERE)
     p = subprocess.run([sys.executable, "-c", code] + list(map(str, few + many)), capture_output=True, text=True, timeout=300)
     assert p.returncode == 0 and p.stdout.count("served") == 2, p.stderr[-2000:]
+
+
+@pytest.mark.parametrize("blocks", [1, 100, 30000])
+def test_no_rows_at_all(blocks):
+    """Nothing comes in and nothing goes out: the ring's ends are handed on, however large the pool is."""
+    import torch
+
+    from paper_2510_02358_b200 import binding as dsp
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    table, ring, pos = none.view(0, 4), torch.arange(blocks, dtype=torch.int32, device="cuda"), torch.tensor([3, 3 + blocks], device="cuda")
+    got = dsp.dsp_cache_fork(none, None, none, none, pos, table, ring, 16, table.clone())
+    assert got.ring_pos.tolist() == [3, 3 + blocks] and torch.equal(ring, torch.arange(blocks, dtype=torch.int32, device="cuda"))
