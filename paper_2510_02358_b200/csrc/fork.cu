@@ -291,10 +291,21 @@ int32_t launch_fork(const ForkArgs &a, size_t mark_bytes, cudaStream_t st) {
     return DSP_OK;
 }
 
-// Do two tables [n, width] share memory?
+// Do two tables [n, width] share memory?  The rows of one may lie in the gaps of the other (two halves of a wider tensor).
 bool overlap(const int32_t *a, long long sa, long long na, const int32_t *b, long long sb, long long nb, int width) {
     if (na < 1 || nb < 1) return false;
-    return a < b + (nb - 1) * sb + width && b < a + (na - 1) * sa + width;
+    // entries from the start of b to that of a's row i; rows of b begin every sb
+    const long long between = (long long)(reinterpret_cast<intptr_t>(a) - reinterpret_cast<intptr_t>(b)) / (long long)sizeof(int32_t);
+    const long long end = (nb - 1) * sb + width;
+    if (between >= end || between + (na - 1) * sa + width <= 0) return false;
+    for (long long i = 0; i < na; ++i) {
+        const long long at = between + i * sa;
+        if (at + width <= 0 || at >= end) continue;
+        const long long row = at < 0 ? 0 : at / sb, past = at - row * sb;    // the last row of b that begins at or before `at`, or the first
+        if (past < width) return true;
+        if (row + 1 < nb && sb - past < width) return true;
+    }
+    return false;
 }
 
 }  // namespace
