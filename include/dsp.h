@@ -966,7 +966,8 @@ int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t
  *          aligned; its layout is the library's own); grad [B,L,V] (dtype, strides in elements; nullable);
  *          row_status uint32 [B] (nullable): flags OR-ed into existing content, DSP_ROW_NONFINITE_INPUT
  *          (NaN or +inf logit of a row that is read, no finite logit, or a NaN or +inf among the teacher's values: that
- *          row's outputs are NaN or unspecified), DSP_ROW_TIMEOUT.
+ *          row's outputs are NaN or unspecified), DSP_ROW_TIMEOUT (the row did not come in time: its loss, accept, lse and state
+ *          are NaN, and so is the gradient of its tokens, of those at least that waited; DSP_ROW_NONFINITE_INPUT may be set beside it).
  * Errors : INVALID_ARG (null pointer, sizes, strides, alignment, temperature, K < 1), UNSUPPORTED (dtype,
  *          K > DSP_MAX_TEACHER, V > 2^30, more than 2^24 rows), CUDA.  B == 0 is a no-op returning DSP_OK.
  */

@@ -404,15 +404,17 @@ __device__ __forceinline__ void tell_nothing(const DistillArgs &a, unsigned row)
     }
     if (state && tid < a.K) reinterpret_cast<uint32_t *>(state)[4 + tid] = kNoEntry;
 }
-// What follows from the sums of a row's n parts, by one warp (P: the list's sum, t_lse: the teacher's log-sum-exp).
+__device__ __forceinline__ float lost_if(int timed_out) { return timed_out ? CUDART_NAN_F : 0.f; }
+// What follows from the sums of a row's n parts, by one warp (P: the list's sum, t_lse: the teacher's log-sum-exp; lost: 0, or NaN where copies
+// or parts did not all come in time: then everything that follows from the sums is NaN).
 //
 // r = 1 - P has the rounding of the teacher's log-sum-exp in it, 2^-24 |t_lse| and as much again for whoever summed it, and a few 2^-24 of the
 // sum's own: where the list is all that the teacher allows, that is all that r is.  r log s would turn it into a loss of any size where the
 // drafter gives the others next to nothing (a common mask: s = 0, or e^-10000), so there it counts as nothing.  Where s is above r / 1024 the
 // formula stays: its term is within 7 r then.
-__device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, float t_lse, int lane) {
+__device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, float t_lse, float lost, int lane) {
     Part q[kMaxCluster * kWarps / 32];
-    float cs = kRefFloor, cl = kRefFloor, S = 0.f, E = 0.f;
+    float cs = kRefFloor, cl = kRefFloor, S = lost, E = 0.f;
 #pragma unroll
     for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
         q[i] = lane + 32 * i < n ? parts[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
@@ -528,6 +530,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
         if (warp == 0) take_copies(sh, parity);
         parity ^= 1u;
         __syncthreads();                        // the edges are in place too
+        if (sh.timed_out) Sc = CUDART_NAN_F;    // a copy that came too late: no sum, for all of the row's CTAs
         if (piece >= q0 && piece < q1) {
             const int at = p.h + id - q0 * N;
             xk = elem_of<DT>(buf, at);
@@ -564,7 +567,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
     if (warp == 0) {
         if (tail)
             for (int i = 0; i * 32 < a.K; ++i) P += sh.red[i][0];
-        const Known kn = known_of(a, sh.part, C * kWarps, P, t_lse, lane);
+        const Known kn = known_of(a, sh.part, C * kWarps, P, t_lse, lost_if(*static_cast<volatile int *>(&sh.timed_out)), lane);
         if (lane == 0) sh.known = kn;
     }
     __syncthreads();
@@ -595,7 +598,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
                 parity ^= 1u;
                 __syncthreads();
             }
-            if (tid >= skip) write_pieces<DT>(g, p, a.V, q0, q1, buf, a.s, c_f, f * w, skip);
+            if (tid >= skip) write_pieces<DT>(g, p, a.V, q0, q1, buf, a.s, c_f, chunks > 1 && sh.timed_out ? CUDART_NAN_F : f * w, skip);
             __syncthreads();                    // the token's own element comes after the piece that it lies in
             if (piece >= q0 && piece < q1) g[id] = rounded<DT>(gk * w);
             if (++k >= chunks) break;
@@ -779,7 +782,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const Distill
     if (warp == 0) {
         if (a.tlse)
             for (int i = 0; i * 32 < a.K; ++i) P += s_red[i][0];
-        const Known kn = known_of(a, s_part, kWarps, P, a.tlse ? a.tlse[row] : 0.f, lane);
+        const Known kn = known_of(a, s_part, kWarps, P, a.tlse ? a.tlse[row] : 0.f, lost_if(bars.timed_out), lane);
         if (lane == 0) s_known = kn;
     }
     __syncthreads();
