@@ -954,7 +954,8 @@ int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t
  * is read once, stays in the shared memory of a cluster of CTAs (rows up to 1.7 MB), and its gradient is written
  * once.  A row of weight 0 is not read: loss, accept 0, lse -inf, gradient 0.
  * dsp_distill_grad computes row_grad * dloss/dx from the student's logits and what dsp_distill left in
- * `state`, for callers whose factor comes later (an autograd graph); row_grad 0 gives 0 without reading the row.
+ * `state`, for callers whose factor comes later (an autograd graph).  Rows with row_grad 0, or that dsp_distill did not read
+ * (weight 0), give 0 and are not read.
  * The gradient has the logits' dtype, one rounding; sums, statistics and factors are kept in 32 bits or more.
  * grad may be the logits themselves (same address and strides) and must not overlap them otherwise.
  *

@@ -822,9 +822,25 @@ __global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs
     DT *g = reinterpret_cast<DT *>(a.g) + b * a.gsb + l * a.gsl;
     const Pieces<DT> p(x, a.V);
     const int p0 = (int)min(slice * (unsigned)a.per, (unsigned)p.n), p1 = (int)min((slice + 1) * (unsigned)a.per, (unsigned)p.n);
-    const float w = a.factor[row];
-    if (w == 0.f) {
+    const float *state = a.state + row * (a.K + 4);
+    const float w = a.factor[row], c = state[0], f = state[1];
+    // the slot's own element, if it lies in this slice (-1: none), and its gradient
+    int at = -1;
+    float gk = 0.f;
+    auto own = [&]() {
+        if (tid >= a.K || __float_as_uint(state[4 + tid]) == kNoEntry) return;
+        const int id = a.id[row * a.K + tid];
+        if (id < 0 || id >= a.V) return;
+        const int piece = (p.h + id) / N;
+        if (piece < p0 || piece >= p1) return;
+        at = id;
+        gk = state[4 + tid] * w;
+    };
+    if (w == 0.f || f == 0.f) {                 // nothing for the others, whatever their logits are: dsp_distill may not have read them either
+        if (w != 0.f) own();
         store_zeros<DT>(g, max(0, p0 * N - p.h), min(a.V, p1 * N - p.h));
+        __syncthreads();
+        if (at >= 0) g[at] = rounded<DT>(gk);
         return;
     }
     if (tid == 0) {
@@ -835,21 +851,10 @@ __global__ void __launch_bounds__(kDT) distill_grad_kernel(const DistillGradArgs
     __syncthreads();
     if (tid == 0) send_copies<DT>(x, p, p0, p1, buf, sh);
     read_edges<DT>(x, p, a.V, p0, p1, buf);
-    const float *state = a.state + row * (a.K + 4);
-    const float c = state[0], f = state[1] * w;
-    int at = -1;
-    float gk = 0.f;
-    if (tid < a.K && __float_as_uint(state[4 + tid]) != kNoEntry) {
-        const int id = a.id[row * a.K + tid];
-        const int piece = (p.h + id) / N;
-        if (id >= 0 && id < a.V && piece >= p0 && piece < p1) {
-            at = id;
-            gk = state[4 + tid] * w;
-        }
-    }
+    own();
     if (tid < 32) take_copies(sh, 0u);
     __syncthreads();
-    write_pieces<DT>(g, p, a.V, p0, p1, buf, a.s, c, sh.timed_out ? CUDART_NAN_F : f);
+    write_pieces<DT>(g, p, a.V, p0, p1, buf, a.s, c, sh.timed_out ? CUDART_NAN_F : f * w);
     __syncthreads();                            // the token's own element comes after the piece that it lies in
     if (at >= 0) g[at] = rounded<DT>(gk);
 }

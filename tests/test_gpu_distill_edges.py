@@ -77,3 +77,23 @@ def test_mass_of_the_teacher_that_the_drafter_has_no_token_for(grad):
     assert some.any() and (r.loss[some] == math.inf).all() and not r.loss.isnan().any()
     if grad:
         assert torch.isfinite(r.grad).all()
+
+
+@pytest.mark.parametrize("B,L,V,dtype,offset", [(3, 4, 4099, F32, 1), (2, 3, 40000, BF, 0), (3, 60, 80000, BF, 0)])
+def test_the_gradient_of_a_row_that_the_loss_did_not_read(B, L, V, dtype, offset):
+    """A row of weight 0 is not read: whatever its logits are (a padded batch's are anything), its loss is 0 and so is the gradient, with any factor."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    buf = torch.randn(B * L * V + offset, generator=g, device="cuda").to(dtype)
+    x = buf[offset:].view(B, L, V)
+    ids = torch.randint(0, V, (B, L, 4), generator=g, device="cuda", dtype=torch.int32)
+    val, w = torch.randn(B, L, 4, generator=g, device="cuda"), torch.ones(B, L, device="cuda")
+    lse, up = torch.full((B, L), 9.0, device="cuda"), torch.rand(B, L, generator=g, device="cuda") + 0.5
+    w[0, 1], w[1] = 0.0, 0.0
+    want = dsp.dsp_distill_grad(x, ids, dsp.dsp_distill(x, ids, val, teacher_lse=lse).state, up)
+    want[w == 0] = 0.0
+    x[0, 1, ::2], x[1, 0], x[1, 1, 5], x[1, 2] = math.nan, math.nan, math.inf, -math.inf
+    r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, weight=w)
+    assert not r.loss[w == 0].any()
+    assert torch.equal(dsp.dsp_distill_grad(x, ids, r.state, up), want)
+    y = x.clone()
+    assert torch.equal(dsp.dsp_distill_grad(y, ids, r.state, up, grad=y), want)
