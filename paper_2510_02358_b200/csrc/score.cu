@@ -93,7 +93,7 @@ struct TokenPass {
             const int v = outer_at(lane);
             x_outer = v >= 0 ? Elem<DT>::load1(row + v) : -CUDART_INF_F;
         }
-        tok = ranked ? tokens[0] : -1;
+        tok = G > 0 ? tokens[0] : -1;            // kept out of the sums with a rank and without
         if (tok < 0 || tok >= V) { tok = -1; xt = CUDART_INF_F; ge = gt = N == 8 ? 0x7F807F80u : 0x7F800000u; return; }   // above everything
         xt = Elem<DT>::load1(row + tok);
         vec = tok < head ? 0 : min((tok - head) / N, inner / N);
