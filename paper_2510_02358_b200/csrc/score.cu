@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) score_kernel(const ScoreArgs a
     const int b = (int)(row32 / (unsigned)a.L), l = (int)(row32 - (unsigned)b * (unsigned)a.L), lane = threadIdx.x & 31;
     if (a.row_len && l >= a.row_len[b]) {                // whole CTA alike
         if (slice == 0 && threadIdx.x < 32) score_nothing(a, row, lane);
+        grid_dependency_wait();                          // a call may have no other row: what follows it has to find the preparation ended
         return;
     }
     const DT *rowp = reinterpret_cast<const DT *>(a.logits) + b * a.stride_b + l * a.stride_l;
@@ -439,6 +440,7 @@ __global__ void __launch_bounds__(kThreads, 2) score_cluster_kernel(const ScoreA
     const int b = (int)(row32 / (unsigned)a.L), l = (int)(row32 - (unsigned)b * (unsigned)a.L);
     if (a.row_len && l >= a.row_len[b]) {                // the whole cluster alike
         if (rank == 0 && warp == 0) score_nothing(a, row, lane);
+        grid_dependency_wait();                          // as in score_kernel
         return;
     }
     const DT *rowp = reinterpret_cast<const DT *>(a.logits) + b * a.stride_b + l * a.stride_l;

@@ -31,3 +31,17 @@ def test_a_distillation_whose_copies_or_parts_come_too_late_gives_nan():
     # a NaN sum of one warp reaches the row's sum, and no rule makes it a number again
     assert "S = lost," in known and "w2 == 0.f && q[i].S < CUDART_INF_F ? 0.f : q[i].S * w2" in known
     assert "S = (S != 0.f ? S * ex2_approx(c - cn) : 0.f) + " in function(text, "void sum_pieces")
+
+
+def test_kernels_that_start_early_do_not_end_before_the_launch_that_they_depend_on():
+    """If no thread of such a kernel waits, nothing orders what the launch before it writes (status words, tickets) before what follows the
+    kernel.  So each way out lies behind a wait: of the kernel itself, or of the row's pass that it calls."""
+    text = source("score.cu")
+    for name in (") score_kernel", ") score_cluster_kernel"):
+        body = function(text, name)
+        unread = body[body.index("score_nothing("):]
+        unread = unread[:unread.index("return;")]
+        assert "grid_dependency_wait();" in unread, name
+    assert "grid_dependency_wait();" in function(text, "bool score_sums") and "grid_dependency_wait();" in function(source("row_engine.cuh"), "bool row_engine")
+    fork = function(source("fork.cu"), ") fork_part_kernel")
+    assert "return" not in fork and "grid_dependency_wait();" in fork

@@ -30,3 +30,34 @@ def test_scores_do_not_depend_on_whether_a_rank_is_asked_for(L, V, K, boost, dty
     err, other = ref.exponent_error(x, 1.0, ref.terms(V)), -torch.expm1(logp[..., 0])
     assert ((got.logp.double() - logp).abs() <= (err * other)[..., None] + 2.0 ** -24 * logp.abs() + 1e-13).all()
     assert ((got.entropy.double() - entropy).abs() <= 2 * err * (entropy + 2 * other) + 2.0 ** -24 * entropy + 1e-13).all()
+
+
+@pytest.mark.parametrize("B,L,V,K", [(3, 2, 152064, 5), (3, 300, 32003, 0), (1, 1, 152064, 0), (4, 2, 11, 3), (700, 3, 5001, 2)])
+def test_a_call_without_a_row_to_read(B, L, V, K):
+    """Every length is 0: nothing is left of the outputs' old contents, and what follows in the stream or the graph finds them written."""
+    x = torch.full((B, L, V), math.nan, device="cuda").to(BF)
+    tokens, lens = torch.zeros(B, L, 1, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    out = dsp.dsp_token_logprobs(x, tokens, K=K, row_len=lens)
+
+    def run():
+        for t in vars(out).values():
+            if t is not None:
+                t.fill_(77)
+        dsp.dsp_token_logprobs(x, tokens, K=K, row_len=lens, out=out)
+        return {k: t.clone() for k, t in vars(out).items() if t is not None}
+
+    def look(got):
+        assert not got["row_status"].any() and (got["lse"] == -math.inf).all() and (got["logp"] == -math.inf).all()
+        assert (got["rank"] == -1).all() and not got["entropy"].any() and (K == 0 or (got["top_id"] == -1).all())
+
+    for _ in range(20):
+        look(run())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for _ in range(20):
+        for t in got.values():
+            t.fill_(55)
+        graph.replay()
+        look(got)
