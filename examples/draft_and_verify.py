@@ -115,10 +115,12 @@ class Decoder:
         self.proxy = -8.0 * torch.rand(1 << 10, generator=g, device=dev)
         self.texts = [[] for _ in range(B)]
         self.margins = [[] for _ in range(B)]                                      # plain_step: the logits, for comparisons
+        self.on = torch.ones(B, dtype=torch.bool, device=dev)                      # requests that go on: the places of the others are empty
 
     def emit(self, tokens: torch.Tensor, count: torch.Tensor):
+        count = count * self.on
         self.pending, self.pending_len = tokens, count                             # what the drafter has not seen yet
-        self.last = tokens.gather(1, (count - 1)[:, None].long())[:, 0]
+        self.last = tokens.gather(1, (count - 1).clamp_min(0)[:, None].long())[:, 0]
         for b, (t, c) in enumerate(zip(tokens.tolist(), count.tolist())):
             self.texts[b] += t[:c]
 
@@ -132,26 +134,31 @@ class Decoder:
 
     def plain_step(self):
         tokens = self.last[:, None]
-        one = torch.ones(self.B, dtype=torch.int32, device=self.dev)
-        logits = self.target.leaning(self.target.forward(tokens, one), self.chain[tokens.long()])[:, 0]
-        self.target.pool.seq_len = self.target.pool.seq_len + 1
+        one = self.on.int()
+        logits = self.logits(self.target.forward(tokens, one), tokens)[:, 0]
+        self.target.pool.seq_len = self.target.pool.seq_len + one
         for b in range(self.B):
             self.margins[b].append(logits[b])
         self.emit(logits.argmax(-1).int()[:, None], one)
+
+    def logits(self, logits: torch.Tensor, tokens: torch.Tensor) -> torch.Tensor:
+        """The target's, with its leaning; zeros for requests that have ended, which no row was computed for."""
+        return self.target.leaning(logits.masked_fill(~self.on[:, None, None], 0.0), self.chain[tokens.long()])
 
     def draft(self):
         n = self.pending.shape[1] + self.L
         at = torch.arange(n, device=self.dev)[None]
         tokens = torch.nn.functional.pad(self.pending, (0, self.L), value=MASK).masked_fill(at >= self.pending_len[:, None], MASK)
-        logits = self.drafter.forward(tokens, self.pending_len + self.L, mask="full")
+        logits = self.drafter.forward(tokens, (self.pending_len + self.L) * self.on, mask="full")
         self.drafter.pool.seq_len = self.drafter.pool.seq_len + self.pending_len   # the masks are not kept
         block = (self.pending_len[:, None] + torch.arange(self.L, device=self.dev)).long()
         guess = [self.chain[self.last.long()]]
         for _ in range(self.L - 1):
             guess.append(self.chain[guess[-1].long()])
-        logits = logits.gather(1, block[..., None].expand(-1, -1, VOCAB))
+        off = ~self.on[:, None, None]                                              # no rows were computed for these
+        logits = logits.gather(1, block[..., None].expand(-1, -1, VOCAB)).masked_fill(off, 0.0)
         logits = self.drafter.leaning(logits, torch.stack(guess, 1))
-        self.drafted = logits, self.drafter.hidden.gather(1, block[..., None].expand(-1, -1, WIDTH))
+        self.drafted = logits, self.drafter.hidden.gather(1, block[..., None].expand(-1, -1, WIDTH)).masked_fill(off, 0.0)
         lat = dsp.dsp_lattice_build(logits, self.K)
         cps = dsp.dsp_cps_search(lat, self.last, self.proxy, W=self.W, lam=0.9, table_log2=10, V=VOCAB, row_status=lat.row_status)
         return lat, cps
@@ -162,31 +169,31 @@ class Decoder:
         pool, last = self.target.pool, self.last[:, None]
         if not tree:
             tokens = torch.cat([last, cps.path.clamp_min(0)], 1)
-            logits = self.target.leaning(self.target.forward(tokens, 1 + cps.path_len), self.chain[tokens.long()])
+            logits = self.logits(self.target.forward(tokens, (1 + cps.path_len) * self.on), tokens)
             ver = dsp.dsp_verify(logits, None, cps, None, all_greedy=True, row_status=lat.row_status)
-            accepted, path = ver.accepted_len, cps.path
+            accepted, path = ver.accepted_len * self.on, cps.path
         else:
             t = dsp.dsp_beam_tree(cps)
             tokens = torch.cat([last, t.node_token.clamp_min(0)], 1)
-            logits = self.target.leaning(self.target.forward(tokens, 1 + t.n_nodes, tree=t), self.chain[tokens.long()])
+            logits = self.logits(self.target.forward(tokens, (1 + t.n_nodes) * self.on, tree=t), tokens)
             ver = dsp.dsp_verify_tree(logits, t, self.L)
-            accepted = ver.accepted_len
+            accepted = ver.accepted_len * self.on
             path = t.node_token.gather(1, ver.accepted_node.clamp_min(0).long())
             dsp.dsp_kv4_compact(pool.cache, D, pool.block_table, pool.seq_len, ver.accepted_node, accepted)
         self.rows, self.path, self.right = logits[:, :self.L], cps.path, (cps.path == path).int().cumprod(1).sum(1).minimum(accepted)
-        pool.seq_len = pool.seq_len + 1 + accepted
+        pool.seq_len = pool.seq_len + (1 + accepted) * self.on
         new = torch.cat([path.clamp_min(0), path[:, :1]], 1).scatter(1, accepted[:, None].long(), ver.next_token[:, None])
         self.emit(new, accepted + 1)
         return accepted
 
-
     def fork(self, src):
-        """Request r goes on from where request src[r] is (-1: it ends, and its place stays empty)."""
+        """Request r goes on from where request src[r] is (-1: it ends, and its place stays empty until a later fork takes it)."""
         src_t = torch.tensor(src, dtype=torch.int32, device=self.dev)
         for pool in (self.target.pool, self.drafter.pool):
             pool.fork(src_t)
         at = src_t.clamp_min(0).long()
-        self.last, self.pending, self.pending_len = self.last[at], self.pending[at], self.pending_len[at]
+        self.on = self.on[at] & (src_t >= 0)
+        self.last, self.pending, self.pending_len = self.last[at], self.pending[at], self.pending_len[at] * self.on
         self.texts = [list(self.texts[s]) if s >= 0 else [] for s in src]
         self.margins = [list(self.margins[s]) if s >= 0 else [] for s in src]
 
@@ -194,7 +201,7 @@ class Decoder:
         """What the drafter can learn from the last step: its block against the target's rows of the best path, whose positions count up to
         the first token that the target did not take.  Returns loss and accept [B, L] and the gradient for the drafter's head."""
         logits, hidden = self.drafted
-        n = (self.right + 1).clamp_max(self.L).int()                               # rows that follow accepted tokens
+        n = (self.right + 1).clamp_max(self.L).int() * self.on                     # rows that follow accepted tokens
         teacher = dsp.dsp_token_logprobs(self.rows, self.path, K=K, temperature=temperature, row_len=n)
         weight = (torch.arange(self.L, device=self.dev) < n[:, None]).float() / n.sum()
         r = dsp.dsp_distill(logits, teacher.top_id, teacher.top_logit, teacher_lse=teacher.lse, weight=weight, temperature=temperature, grad=True)
