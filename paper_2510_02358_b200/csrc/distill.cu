@@ -13,11 +13,12 @@
 // four numbers (two references, two sums) to all CTAs of the row over distributed shared memory, once.  The CTAs of an SM belong to
 // different rows, so one loads while another sums.
 //
-// Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 218 us, which is
-// 5.4 TB/s or 0.84 of a plain copy's rate; 999 rows of 32003 fp32 49 us (0.81); 512 rows of 152064 bf16 in two calls 91 us (0.80; the gradient's
-// call alone 46 us, a copy's rate); 16 rows 7.7 us.  What bounds the one call is the chain of a row: list, copies, sums, exchange, factors, gradient,
+// Measured (device time; loss and gradient in one call, K = 32): 2048 rows of 152064 bf16, a tenth of them without weight, 211 us, which is
+// 5.6 TB/s or 0.87 of a plain copy's rate; 999 rows of 32003 fp32 49.5 us (0.80), 600 of 152064 148 us (0.77); 512 rows of 152064 bf16 in two calls
+// 91 us (0.80; the gradient's call alone 46 us, a copy's rate); 16 rows 7.5 us.  Longer lists cost: 2048 rows, all with weight, K = 32 225 us,
+// 64 230, 100 237, 128 239, 256 278.  What bounds the one call is the chain of a row: list, copies, sums, exchange, factors, gradient,
 // of which the four or five CTAs of an SM cover most.  On 2048 rows the exchange with a cluster barrier's fences took 250 us, counted stores 228, the loss beside the
-// gradient 218.  Other forms measured there, before these: clusters that stay and load the next row into a second buffer 434 us, a row in one CTA
+// gradient 218 (211 now).  Other forms measured there, before these: clusters that stay and load the next row into a second buffer 434 us, a row in one CTA
 // with what does not fit read again from L2 276 us; a cubic for part of the exponentials: within 2%.
 #include "stream_core.cuh"
 
@@ -27,8 +28,9 @@ namespace {
 constexpr int kDT = 256;                        // threads of a CTA: one per teacher slot
 static_assert(kDT == DSP_MAX_TEACHER && kDT == kThreads, "one thread per slot");
 constexpr int kMaxCluster = 8;
-// A CTA's share of a row, 64 KB, unless the cluster is at its largest.  Measured with 40 KB (us, 40 / 64 KB): 1000 rows of 100000 bf16 112 / 91,
-// of 128256 126 / 116, of 32000 35.3 / 33.1, 999 of 32003 fp32 64 / 61; with 80 KB 2048 rows of 152064 bf16 took 285 instead of 255.
+// A CTA's share of a row, 64 KB, unless the cluster is at its largest.  Measured with 40 KB (us, 40 / 64 KB): 1000 rows of 100000 bf16 91 / 75,
+// of 110000 96 / 91, of 128256 105 / 100, of 32000 30.0 / 29.5, fp32 999 of 32003 52.4 / 48.9, 1000 of 64000 93 / 88, 600 of 152064 148 / 148; with
+// 80 KB 2048 rows of 152064 bf16 took 261 instead of 225, the others the same.
 constexpr int kSliceVecs = 4096;
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no part
 
@@ -412,6 +414,11 @@ __device__ __forceinline__ float lost_if(int timed_out) { return timed_out ? CUD
 // sum's own: where the list is all that the teacher allows, that is all that r is.  r log s would turn it into a loss of any size where the
 // drafter gives the others next to nothing (a common mask: s = 0, or e^-10000), so there it counts as nothing.  Where s is above r / 1024 the
 // formula stays: its term is within 7 r then.
+//
+// All of this is in 32 bits, because the gradient waits for it (with it, five CTAs an SM and the loss out of the way 2048 rows of 152064 went from 480 us
+// to 368): the sums are off by
+// a few 2^-24, the two quotients of f and the q of a listed token by 2^-22.  f and q - p are differences, so the gradient's error is some
+// 2^-21 of q_v, not of itself: 2^-21 / (1 - r/s) of itself for the others, 5e-5 where r/s is within a hundredth of 1.
 __device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, float t_lse, float lost, int lane) {
     Part q[kMaxCluster * kWarps / 32];
     float cs = kRefFloor, cl = kRefFloor, S = lost, E = 0.f;
@@ -577,7 +584,8 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
     if (mine) gk = none ? 0.f : (float)(((double)__fdividef(ex2_approx((float)(zs - (double)c_all)), all) - pk) * a.inv_t);
     if (state && mine) state[4 + tid] = gk;
     // Loss and what else the row is told, by the first CTA: while the others write the gradient by the warps with slots alone, if those are few and
-    // the pieces are whole ones (us, so / by all warps after the gradient: 1000 rows of 32000 bf16 30.7 / 33.9, 999 of 32003 fp32 50.5 / 55.2, 16 of 152064 7.8 / 8.7).
+    // the pieces are whole ones (us, so / by all warps before the gradient: 2048 rows of 152064 bf16 225 / 258; K = 64: 230 / 261, 1000 of 32000
+    // 30.1 / 31.1, 999 of 32003 fp32 48.6 / 51.4).  Lists of 65 to 128 would gain as well (K = 100: 230 / 237, 31.2 / 32.2, 50.7 / 53.5).
     int skip = 0;
     if (rank == 0) {
         const int listed = (a.K + 31) / 32 * 32;
@@ -889,8 +897,8 @@ int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     const int n = pieces_at_most(a.V, N);
     int C = 1;
     while (C < kMaxCluster && (long long)n > (long long)C * kSliceVecs) C *= 2;
-    // Few rows are cut finer, as long as a thread keeps a piece (us, without / with): 100 rows of 64000 bf16 11.5 / 10.6, 40 of 32003 fp32
-    // 8.3 / 7.8; up to three CTAs an SM instead of two: 100 rows of 32000 12.3 / 8.4.
+    // Few rows are cut finer, as long as a thread keeps a piece (us, without / with): 100 rows of 64000 bf16 10.3 / 9.6, 40 of 32003 fp32
+    // 7.2 / 7.1; up to three CTAs an SM instead of two: 100 rows of 32000 10.9 / 7.4, of 64000 12.6 / 9.6.
     while (C < kMaxCluster && rows * C < 2 * device_sm_count() && n >= 2 * C * kDT) C *= 2;
     a.C = C;
     while ((1 << a.log2_c) < C) ++a.log2_c;
@@ -898,7 +906,7 @@ int32_t launch_distill(DistillArgs &a, long long rows, cudaStream_t st) {
     a.buf_vecs = per < kMaxBufVecs ? per : kMaxBufVecs;
     if (rows * C > 0x7FFFFFFFLL) return DSP_ERR_UNSUPPORTED;
     // Five CTAs an SM where their buffers fit and there are as many, else four, with more registers.  Measured (us, five / four): 2048 rows of
-    // 152064 bf16 217 / 235; 1000 of 100000 79.2 / 77.2, of 32000 30.7 / 29.9, 999 of 32003 fp32 50.5 / 49.1, whose buffers let three fit.
+    // 152064 bf16 225 / 245, with K = 256 278 / 311; 1000 of 100000 76.8 / 75.5, of 32000 30.4 / 30.1, 999 of 32003 fp32 49.8 / 49.2, whose buffers let three fit.
     if (a.buf_vecs <= 2560 && rows * C > 4 * device_sm_count()) return launch_distill_rows<DT, GRAD, 5>(a, rows, st);
     return launch_distill_rows<DT, GRAD, 4>(a, rows, st);
 }
@@ -969,8 +977,9 @@ extern "C" int32_t dsp_distill(const void *student_logits, int32_t dtype, int32_
     const long long rows = (long long)B * L;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     // The loss alone of many long bf16 rows streams each in a CTA; measured with the gradient's call behind it, K = 16 (us, streamed / by
-    // clusters): 512 rows of 152064 91 / 95, 148 rows 31.6 / 30.9, 32 rows 22 / 13; 600 rows of 100000 76 / 74, of 200000 131 / 136, of 64000 57 / 50;
-    // 2000 rows of 110000 225 / 252, of 80000 179 / 179; fp32 (half the logits for the same bytes, the same work a tile) 600 rows of 100000 152 / 127.
+    // clusters): 512 rows of 152064 90 / 95, 148 rows 32.3 / 32.3, 32 rows 22 / 13; 600 rows of 100000 76 / 73, of 200000 131 / 133, of 64000 57 / 50;
+    // 2000 rows of 110000 225 / 248, of 80000 179 / 179; fp32 (half the logits for the same bytes, the same work a tile) 600 rows of 100000 152 / 127.
+    // By clusters, both calls: 600 rows of 64000 bf16 50, fp32 86, 2000 of 32003 fp32 140; streamed with K = 256: 512 rows of 152064 153.
     if (!grad && dtype == DSP_BF16 && rows >= device_sm_count() && V >= kLongRow) return launch_distill_loss(a, rows, st);
     if (dtype == DSP_BF16)
         return grad ? launch_distill<__nv_bfloat16, true>(a, rows, st) : launch_distill<__nv_bfloat16, false>(a, rows, st);
