@@ -901,7 +901,7 @@ int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t
  *               (0: it is the argmax); -1 for a token outside 0..V-1
  *   the K best tokens in the total order with their logits x and log-probabilities;
  *   -inf logits are not among them, unused slots (fewer tokens than K) are id -1, logit and logp -inf.
- *   In the sums, logits below about -1e37 (-1.38e38 * temperature, where that is higher) count as -inf.
+ *   In the sums, logits below about -1.48e9 * temperature (an exponent of -2^31) count as -inf.
  * Rows from row_len[b] on (clipped to 0..L) are not read: logp and lse -inf, rank -1,
  * entropy 0, no alternatives.  Everything but the scalars of a row is read once.
  * Any V and any row start run at full speed: what lies outside of whole 16-byte pieces

@@ -308,8 +308,8 @@ __device__ bool row_engine(const DT *__restrict__ rowp, int V, int K, bool sums,
     if (sums) stream_slice<DT, true>(rowp, s0, s1, nstages, bars, ring, top, cs, pass);
     else      stream_slice<DT, false>(rowp, s0, s1, nstages, bars, ring, top, cs, pass);
 
-    // masked (-inf) logits leave 0 * -inf in T only: such columns are summed once more, clamped
-    const bool poisoned = sums && cs.T != cs.T && cs.S == cs.S && cs.S < CUDART_INF_F;
+    // masked (-inf) logits leave 0 * -inf in T only: such columns are summed once more, clamped (a pass with sums of its own raises them)
+    const bool poisoned = !Pass::kOwnTile && sums && cs.T != cs.T && cs.S == cs.S && cs.S < CUDART_INF_F;
     if (__syncthreads_or(poisoned)) {                  // also: every warp is through with the ring
         if (poisoned) redo_column_sums<DT>(rowp, s0, s1, tid, cs);
     }

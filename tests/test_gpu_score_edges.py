@@ -61,3 +61,53 @@ def test_a_call_without_a_row_to_read(B, L, V, K):
             t.fill_(55)
         graph.replay()
         look(got)
+
+
+# as the call takes them: in 32 bits
+TEMPERATURES = torch.tensor([1.0, 0.7, 0.5, 0.3, 0.1, 0.05, 0.01, 1e-3, 1.3, 2.0, 3.0, 10.0, 100.0, 1e3]).clamp(min=1.001e-3).tolist()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,L,V", [(2, 3, 152064), (4, 80, 80003), (3, 100, 32003), (3, 5, 50), (2, 2, 13)])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e37, -7e34, -1e30, -1e20, -1e13])
+def test_masks_of_any_size_at_any_temperature(B, L, V, dtype, mask):
+    """A few tokens of a row are allowed, so most threads, and whole tiles, see masked logits alone."""
+    mask = torch.finfo(dtype).min if mask == "lowest" else mask
+    g = torch.Generator(device="cuda").manual_seed(V)
+    at = torch.rand(B, L, V, generator=g, device="cuda").topk(6, -1).indices
+    x = torch.full((B, L, V), mask, device="cuda").to(dtype)
+    x.scatter_(2, at, (3.0 * torch.randn(B, L, 6, generator=g, device="cuda")).to(dtype))
+    mine = torch.full_like(x, -math.inf).scatter_(2, at, x.gather(2, at))
+    tokens = torch.cat([at[..., :2], (at[..., :1] + 1) % V], -1).int()       # the last one is likely to be masked
+    for T in TEMPERATURES:
+        if mask > -3e9 * T and mask != -math.inf:
+            continue                                                         # next to the bound, or no mask at this temperature
+        # the masks weigh nothing in 64 bits either: exp(-10^9 / T) = 0
+        logp, rank, lse, entropy, _, _, _ = ref.score(mine, T, tokens, 1)
+        given = x.double().gather(-1, tokens.long()) / T - lse[..., None]
+        err = ref.exponent_error(mine, T, ref.terms(V))
+        for K in (0, 5):
+            got = dsp.dsp_token_logprobs(x, tokens, K=K, temperature=T)
+            assert not got.row_status.any(), T
+            assert ((got.lse.double() - lse).abs() <= err + 2.0 ** -24 * lse.abs()).all(), (T, K)
+            near = (got.logp.double() == given.float().double()) | ((got.logp.double() - given).abs() <= err[..., None] + 2.0 ** -24 * given.abs())
+            assert near.all() and torch.equal(got.rank.long(), rank), (T, K)
+            assert ((got.entropy.double() - entropy).abs() <= err * (2 + math.log2(V + 1)) + 2.0 ** -24 * entropy).all(), (T, K)
+            if K:
+                order = mine.sort(dim=-1, descending=True, stable=True).indices[..., :5]
+                assert torch.equal(got.top_id.long(), order), (T, K)
+
+
+@pytest.mark.parametrize("T", [1.0, 0.3, 0.05, 100.0])
+@pytest.mark.parametrize("K", [0, 3])
+@pytest.mark.parametrize("L,V", [(1, 40000), (400, 30000), (3, 11)])
+def test_rows_without_an_allowed_token_are_named(L, V, K, T):
+    for dtype in (BF, F32):
+        for mask in (-math.inf, torch.finfo(dtype).min, -1e30, -1e13):
+            if mask > -3e9 * T:
+                continue
+            x = torch.full((2, L, V), mask, device="cuda").to(dtype)
+            x[1] = 0.0
+            got = dsp.dsp_token_logprobs(x, torch.zeros(2, L, 1, dtype=torch.int32, device="cuda"), K=K, temperature=T)
+            assert got.row_status.tolist() == [dsp.ROW_NONFINITE_INPUT, 0] and got.lse[0].isnan().all()
+            assert ((got.lse[1] - math.log(V)).abs() < 1e-5).all()
