@@ -946,6 +946,7 @@ int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t
  *   dloss / dx_v = (q_v - p_v) / T for the teacher's tokens, q_v (1 - r / s) / T for all others
  * (the gradient of others is 0 where s is 0).  With teacher_lse, an r of at most 2^-23 (|teacher_lse| + 4), which rounding alone
  * can leave of a complete list, counts as 0 where s < r / 1024: no loss comes of it under a mask that teacher and student share.
+ * Logits below about -1.48e9 * temperature (an exponent of -2^31) count as -inf, but for their own share in the loss.
  * A slot takes no part if it is at or beyond teacher_count, its id is outside 0..V-1, or an earlier slot has the same id.  A row
  * without any such token, or with teacher_lse null and no finite t_k, has loss 0 and gradient 0.  loss is +inf where
  * p_k > 0 = q_k or r > 0 = s; the gradient stays finite.

@@ -33,6 +33,9 @@ constexpr int kMaxCluster = 8;
 // 80 KB 2048 rows of 152064 bf16 took 261 instead of 225, the others the same.
 constexpr int kSliceVecs = 4096;
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no part
+// The lowest exponent that counts: logits below it have no mass.  A reference c = fl(x s) above it is off by 2^6 at most (half a step), which
+// the sums bear; where a warp saw nothing but masks of -1e12 or -1e30, c was off by so much that 2^(x s - c) was infinite or 0.
+constexpr float kLowest = -0x1p31f;
 
 struct DistillArgs {
     const void *x;
@@ -205,7 +208,7 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     float m = -CUDART_INF_F;
     if (tid < n) m = Elem<DT>::vmax(at[0]);
     if (tid + kDT < n) m = fmaxf(m, Elem<DT>::vmax(at[kDT]));
-    float c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
+    float c1 = fmaxf(max_of_warp(m) * s, kLowest);
     unsigned long long s0 = 0ull, t0 = 0ull;             // pairs of sums
     int k = full;
     for (; k >= 2; k -= 2, at += 2 * kDT) {
@@ -218,7 +221,7 @@ __device__ __forceinline__ void sum_pieces(const uint4 *buf, int n, float s, flo
     float sum = both(add2(s0, t0));
     if (__any_sync(0xFFFFFFFFu, !(sum < 0x1p64f))) {
         for (int i = tid; i < n; i += kDT) m = fmaxf(m, Elem<DT>::vmax(buf[i]));
-        c1 = fmaxf(max_of_warp(m) * s, kRefFloor);
+        c1 = fmaxf(max_of_warp(m) * s, kLowest);
         s0 = 0ull;
         for (int i = tid; i < n; i += kDT) add_piece<DT>(buf[i], s, c1, s0);
         sum = both(s0);
@@ -379,7 +382,7 @@ __device__ __forceinline__ void tell_row(const DistillArgs &a, unsigned row, int
     if (tid == 0) {
         double H = 0.0, accept = 0.0, E = 0.0;
         for (int i = 0; i * 32 < a.K; ++i) { H += red[i][0]; accept += red[i][1]; E += red[i][2]; }
-        const bool ok = kn.all > 0.f && kn.all < CUDART_INF_F && kn.c_all > kRefFloor && kn.c_all < CUDART_INF_F;
+        const bool ok = kn.all > 0.f && kn.all < CUDART_INF_F && kn.c_all > kLowest && kn.c_all < CUDART_INF_F;
         const float cs = kn.cs, S = kn.S;
         const double others = S != 0.f ? (double)S * exp(((double)cs - (double)kn.c_all) * a.inv_s) : 0.0, total = others + E;
         const double lse = ok ? (double)kn.c_all * a.inv_s + kLn2 * log2(total) : CUDART_NAN;
@@ -421,10 +424,10 @@ __device__ __forceinline__ float lost_if(int timed_out) { return timed_out ? CUD
 // 2^-21 of q_v, not of itself: 2^-21 / (1 - r/s) of itself for the others, 5e-5 where r/s is within a hundredth of 1.
 __device__ __forceinline__ Known known_of(const DistillArgs &a, const Part *parts, int n, double P, float t_lse, float lost, int lane) {
     Part q[kMaxCluster * kWarps / 32];
-    float cs = kRefFloor, cl = kRefFloor, S = lost, E = 0.f;
+    float cs = kLowest, cl = kLowest, S = lost, E = 0.f;
 #pragma unroll
     for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
-        q[i] = lane + 32 * i < n ? parts[lane + 32 * i] : Part{kRefFloor, 0.f, kRefFloor, 0.f};
+        q[i] = lane + 32 * i < n ? parts[lane + 32 * i] : Part{kLowest, 0.f, kLowest, 0.f};
         cs = fmaxf(cs, q[i].c);
         cl = fmaxf(cl, q[i].ct);
     }
@@ -532,7 +535,7 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
     const bool mine = piece >= p0 && piece < p1;
 
     // ---- the slice: the teacher's tokens taken out, the others summed ----
-    float xk = 0.f, c = kRefFloor, Sc = 0.f;
+    float xk = 0.f, c = kLowest, Sc = 0.f;
     for (int k = 0;;) {
         if (warp == 0) take_copies(sh, parity);
         parity ^= 1u;
@@ -555,9 +558,9 @@ __global__ void __launch_bounds__(kDT, CTAS) distill_kernel(const DistillArgs a)
 
     // ---- what the warp knows, to every CTA of the row: all that the gradient waits for is in single precision ----
     const double zs = (double)xk * (double)a.s; // the token's exponent
-    Part w1 = {c, sum_of_warp(Sc), kRefFloor, 0.f};
+    Part w1 = {c, sum_of_warp(Sc), kLowest, 0.f};
     if (warp * 32 < a.K) {                      // the warps that have slots
-        w1.ct = max_of_warp(mine && (float)zs > kRefFloor ? (float)zs : kRefFloor);
+        w1.ct = max_of_warp(mine && (float)zs > kLowest ? (float)zs : kLowest);
         w1.E = sum_of_warp(mine ? ex2_approx((float)(zs - (double)w1.ct)) : 0.f);
     }
     if (C > 1) {
@@ -653,7 +656,7 @@ struct LossPass {
     float *xk;
     float s;
     int token = 0, next = 0;
-    float c = kRefFloor, S = 0.f, ct = kRefFloor, E = 0.f;
+    float c = kLowest, S = 0.f, ct = kLowest, E = 0.f;
     bool first = true;
 
     __device__ __forceinline__ LossPass(List &list, const int *pl, float *x, float scale) : make_list(list), place(pl), xk(x), s(scale) {}
@@ -685,7 +688,7 @@ struct LossPass {
         }
         if (first) {
             first = false;
-            c = fmaxf(max_of_warp(fmaxf(Elem<DT>::vmax(v[0]), Elem<DT>::vmax(v[1]))) * s, kRefFloor);
+            c = fmaxf(max_of_warp(fmaxf(Elem<DT>::vmax(v[0]), Elem<DT>::vmax(v[1]))) * s, kLowest);
         }
         float s0 = S, s1 = 0.f;
 #pragma unroll
@@ -778,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_loss_kernel(const Distill
     if (id >= 0 && rank < 0) pass.add_token(x_mine);
     if (warp == 0) {                             // the elements outside of the streamed part
         const bool other = lane < a.V - inner && !(s_outer >> lane & 1u);
-        const float c1 = fmaxf(max_of_warp(other ? outer_x * a.s : kRefFloor), pass.c);
+        const float c1 = fmaxf(max_of_warp(other ? outer_x * a.s : kLowest), pass.c);
         pass.S = pass.S != 0.f ? pass.S * ex2_approx(pass.c - c1) : 0.f;
         if (other) pass.S += ex2_approx(fmaf(outer_x, a.s, -c1));
         pass.c = c1;

@@ -97,3 +97,63 @@ def test_the_gradient_of_a_row_that_the_loss_did_not_read(B, L, V, dtype, offset
     assert torch.equal(dsp.dsp_distill_grad(x, ids, r.state, up), want)
     y = x.clone()
     assert torch.equal(dsp.dsp_distill_grad(y, ids, r.state, up, grad=y), want)
+
+
+@pytest.mark.parametrize("B,L,V,dtype,grad", FORMS + [(3, 5, 50, F32, True), (2, 3, 152064, BF, True), (4, 80, 80000, BF, False)])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest", -1e37, -7e34, -1e30, -1e20, -1e13])
+@pytest.mark.parametrize("tail", [True, False])
+def test_masks_of_any_size_at_any_temperature(B, L, V, dtype, grad, mask, tail):
+    """Most threads and warps see masked logits alone; the list has some of the allowed tokens, and a masked one that the teacher does not have
+    either.  Error of the row's sums as in the other tests: each of loss, accept and gradient has it a few times."""
+    mask = torch.finfo(dtype).min if mask == "lowest" else mask
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x, at = grammar(B, L, V, dtype, 6, mask, V)
+    mine = torch.full_like(x, -math.inf).scatter_(2, at, x.gather(2, at))
+    free = (at.sort(-1).values[..., :1] + 1) % V
+    free = torch.where((free == at).any(-1, keepdim=True), torch.full_like(free, V), free)             # no second slot of an allowed token
+    ids = torch.cat([at[..., :3], free], -1).int()
+    val = torch.cat([x.gather(2, at[..., :3]).float() + torch.randn(B, L, 3, generator=g, device="cuda"), torch.full((B, L, 1), -math.inf, device="cuda")], -1)
+    # in 32 bits, as the call takes them
+    for T in torch.tensor([1.0, 0.7, 0.3, 0.05, 1e-2, 2.0, 10.0, 100.0, 1e3]).tolist():
+        if mask > -3e9 * T and mask != -math.inf:
+            continue
+        lse = ((val.double() / T).logsumexp(-1) + 0.25).float() if tail else None
+        loss, accept, full, want = ref.distill(mine, ids, val, T, lse)
+        err = 2.0 ** -20 + 4 * ref.exponent_error(mine, T, ref.terms(V))
+        status = torch.zeros(B, dtype=torch.int32, device="cuda")
+        r = dsp.dsp_distill(x, ids, val, teacher_lse=lse, temperature=T, grad=grad, row_status=status)
+        got = r.grad if grad else dsp.dsp_distill_grad(x, ids, r.state, torch.ones(B, L, device="cuda"), temperature=T)
+        assert not status.any(), T
+        # p (log p - x / T + lse): a listed term is in 64 bits, their sum rounded to 32
+        size = (val[..., :3].double() - x.gather(2, at[..., :3]).double()).abs().amax(-1) / T + full.abs()
+        assert ((r.loss.double() - loss).abs() <= err + 2.0 ** -22 * (loss.abs() + size)).all(), T
+        assert ((r.accept.double() - accept).abs() <= err).all() and ((r.lse.double() - full).abs() <= err + 2.0 ** -24 * full.abs()).all(), T
+        assert ((got.double() - want).abs() <= 2 * err[..., None] / T + torch.finfo(dtype).eps / 2 * want.abs()).all(), T
+
+
+@pytest.mark.parametrize("B,L,V,dtype,grad", FORMS)
+@pytest.mark.parametrize("mask", [-1e4, -1e9, -1e20, -1e30, -1e37])
+def test_listed_tokens_that_the_drafter_has_masked(B, L, V, dtype, grad, mask):
+    """The teacher's best tokens are masked: the loss is p times the mask, and the gradient -p there, finite everywhere."""
+    x, at = grammar(B, L, V, dtype, 6, mask, V)
+    x.scatter_(2, at[..., :2], torch.full_like(x[..., :2], mask))
+    ids, val = at[..., :3].int(), torch.tensor([1.0, 0.0, 0.5], device="cuda").expand(B, L, 3).contiguous()
+    r = dsp.dsp_distill(x, ids, val, grad=grad)
+    p = torch.softmax(val.double(), -1)
+    want = (p * (p.log() - torch.log_softmax(x.double(), -1).gather(-1, at[..., :3]))).sum(-1)
+    assert ((r.loss.double() - want).abs() <= 2.0 ** -20 * want).all()
+    got = r.grad if grad else dsp.dsp_distill_grad(x, ids, r.state, torch.ones(B, L, device="cuda"))
+    assert torch.isfinite(got).all()
+    assert ((got.double().gather(2, at[..., :2]) + p[..., :2]).abs() <= torch.finfo(dtype).eps / 2 * p[..., :2] + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_rows_without_an_allowed_token_are_named(grad):
+    for B, L, V, dtype in ((2, 5, 5003, F32), (2, 90, 80003, BF)):
+        for T, mask in ((1.0, -math.inf), (0.3, -1e30), (100.0, -1e30), (1.0, -1e13), (2.0, torch.finfo(dtype).min)):
+            x = torch.full((B, L, V), mask, device="cuda").to(dtype)
+            x[1] = 0.0
+            status = torch.zeros(B, dtype=torch.int32, device="cuda")
+            ids = torch.zeros(B, L, 1, dtype=torch.int32, device="cuda")
+            r = dsp.dsp_distill(x, ids, torch.zeros(B, L, 1, device="cuda"), temperature=T, grad=grad, row_status=status)
+            assert status.tolist() == [dsp.ROW_NONFINITE_INPUT, 0] and r.loss[0].isnan().all() and ((r.loss[1] - math.log(V)).abs() < 1e-5).all()
