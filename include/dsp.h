@@ -29,7 +29,9 @@
  *  - Positions, ranks and slots are 0-based (the paper counts from 1).
  *  - -inf logits are legal (masked tokens).  NaN or +inf logits, or a row with
  *    no finite logit, set DSP_ROW_NONFINITE_INPUT; that row's outputs are then
- *    unspecified but in bounds.  Finite logits must exceed -1e37.
+ *    unspecified but in bounds.  Masks may also be finite: logits below -1.49e9 (in
+ *    calls with a temperature, times it) weigh nothing in sums, and a row without
+ *    others counts as one without a finite logit.
  *  - The total order on tokens of one row is (logit descending, token id
  *    ascending): the lowest id wins every tie (-0.0 and +0.0 are equal).
  */
@@ -901,7 +903,7 @@ int32_t dsp_attn_kv4(const void *q, int32_t dtype, int32_t B, int32_t T, int32_t
  *               (0: it is the argmax); -1 for a token outside 0..V-1
  *   the K best tokens in the total order with their logits x and log-probabilities;
  *   -inf logits are not among them, unused slots (fewer tokens than K) are id -1, logit and logp -inf.
- *   In the sums, logits below about -1.48e9 * temperature (an exponent of -2^31) count as -inf.
+ *   In the sums, logits below about -1.49e9 * temperature (an exponent of -2^31) count as -inf.
  * Rows from row_len[b] on (clipped to 0..L) are not read: logp and lse -inf, rank -1,
  * entropy 0, no alternatives.  Everything but the scalars of a row is read once.
  * Any V and any row start run at full speed: what lies outside of whole 16-byte pieces
@@ -946,7 +948,7 @@ int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t B, int32_t
  *   dloss / dx_v = (q_v - p_v) / T for the teacher's tokens, q_v (1 - r / s) / T for all others
  * (the gradient of others is 0 where s is 0).  With teacher_lse, an r of at most 2^-23 (|teacher_lse| + 4), which rounding alone
  * can leave of a complete list, counts as 0 where s < r / 1024: no loss comes of it under a mask that teacher and student share.
- * Logits below about -1.48e9 * temperature (an exponent of -2^31) count as -inf, but for their own share in the loss.
+ * Logits below about -1.49e9 * temperature (an exponent of -2^31) count as -inf, but for their own share in the loss.
  * A slot takes no part if it is at or beyond teacher_count, its id is outside 0..V-1, or an earlier slot has the same id.  A row
  * without any such token, or with teacher_lse null and no finite t_k, has loss 0 and gradient 0.  loss is +inf where
  * p_k > 0 = q_k or r > 0 = s; the gradient stays finite.

@@ -33,9 +33,6 @@ constexpr int kMaxCluster = 8;
 // 80 KB 2048 rows of 152064 bf16 took 261 instead of 225, the others the same.
 constexpr int kSliceVecs = 4096;
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;      // state: a slot that takes no part
-// The lowest exponent that counts: logits below it have no mass.  A reference c = fl(x s) above it is off by 2^6 at most (half a step), which
-// the sums bear; where a warp saw nothing but masks of -1e12 or -1e30, c was off by so much that 2^(x s - c) was infinite or 0.
-constexpr float kLowest = -0x1p31f;
 
 struct DistillArgs {
     const void *x;

@@ -22,6 +22,9 @@ constexpr double kLn2 = 0.693147180559945309417232;
 // finaliser removes to first order with the row's mean logit.
 constexpr double kTilt = 1.0 - (double)kLog2e * kLn2;
 constexpr float kRefFloor = -3.0e38f;          // finite stand-in for "no reference exponent yet"
+// The lowest exponent that counts: logits below it weigh nothing in any sum, as -inf.  A reference c = fl(x s) above it is off by 2^6 at most (half
+// a step), which the sums bear; where a thread saw nothing but masks of -1e12 or -1e30, c was off by so much that 2^(x s - c) was infinite or 0.
+constexpr float kLowest = -0x1p31f;
 
 // Host-side record of the last CUDA error seen by an entry point.
 extern int32_t g_last_cuda_error;

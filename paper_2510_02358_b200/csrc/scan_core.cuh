@@ -219,8 +219,8 @@ __device__ void reduce_sums(const DT *__restrict__ row, int s0, int s1, ScanSmem
 // Scan [s0, s1) of `row`.  On return (after a block barrier) sm.cand[0 .. sm.cnt) holds the
 // slice's best min(K, #finite) keys, sorted; with SUMS the slice's
 //   S = sum 2^(x*kLog2e - c),  T = sum 2^(x*kLog2e - c) * (x*kLog2e - c)
-// are returned relative to the reference exponent c (kRefFloor if the slice has no finite
-// logit).  -inf logits contribute nothing; NaN / +inf logits leave S non-finite.
+// are returned relative to the reference exponent c (kLowest if the slice has no logit that
+// counts).  -inf logits contribute nothing; NaN / +inf logits leave S non-finite.
 template <typename DT, bool SUMS>
 __device__ void scan_slice(const DT *__restrict__ row, int s0, int s1, int K, ScanSmem &sm,
                            float &c_out, double &S_out, double &T_out) {
@@ -233,7 +233,7 @@ __device__ void scan_slice(const DT *__restrict__ row, int s0, int s1, int K, Sc
     if (tid == 0) { sm.cnt = 0; sm.thrkey = 0ull; sm.thr_v = -CUDART_INF_F; sm.overflow = 0; }
     __syncthreads();
 
-    float c = kRefFloor, S = 0.f, T = 0.f;
+    float c = kLowest, S = 0.f, T = 0.f;
     float thr = -CUDART_INF_F;
 
     for (int t = 0; t < ntiles; ++t) {

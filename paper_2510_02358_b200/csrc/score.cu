@@ -663,10 +663,9 @@ extern "C" int32_t dsp_token_logprobs(const void *logits, int32_t dtype, int32_t
     a.inv_t = 1.0 / (double)temperature;
     a.s = (float)(a.inv_t / kLn2);
     a.inv_s = a.inv_t / (double)a.s;
-    // What masked logits are raised to: an exponent of -2^31, by a logit that bf16 holds, for both types.  It is the reference c = fl(low s) of a
-    // thread that sees nothing else; c is off by up to half a step, 2^6, which the sums bear (2^64 a logit).  Of -1e37 it was off by 2^99 and the
-    // sums infinite at about every other temperature.
-    const float low = -0x1p31f / a.s;
+    // What masked logits are raised to: the lowest exponent, by a logit that bf16 holds, for both types.  fl(low s) is the reference of a thread that
+    // sees nothing else (with -1e37 its sums were infinite at about every other temperature).
+    const float low = kLowest / a.s;
     memcpy(&a.low, &low, 4);
     a.low &= 0xFFFF0000u;
     float held;

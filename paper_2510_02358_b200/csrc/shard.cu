@@ -102,7 +102,7 @@ __device__ unsigned long long warp_row_elementwise(const DT *__restrict__ row, i
         }
     }
     m = warp_max(m);
-    const float c = m > -CUDART_INF_F ? m * kLog2e : kRefFloor;
+    const float c = fmaxf(m * kLog2e, kLowest);
     double S = 0.0, T = 0.0;
     for (int v0 = lane; v0 < V; v0 += 32 * 64) {         // fp32 partial sums of 64 terms, added up in double
         float s = 0.f, t = 0.f;
@@ -111,7 +111,8 @@ __device__ unsigned long long warp_row_elementwise(const DT *__restrict__ row, i
             if (v < V) {
                 const float x = Elem<DT>::load1(row + v);
                 if (x > -CUDART_INF_F || x != x) {       // -inf adds nothing; NaN / +inf must show in the sums
-                    const float a2 = fmaf(x, kLog2e, -c);
+                    float a2 = fmaf(x, kLog2e, -c);
+                    if (a2 < -1000.f) a2 = -1000.f;      // the type's lowest number would leave 0 * -inf in T; NaN stays
                     const float ex = ex2_approx(a2);
                     s += ex;
                     t = fmaf(ex, a2, t);

@@ -307,7 +307,7 @@ __device__ void redo_column_sums(const DT *__restrict__ row, int s0, int s1, int
 
 // Streams [s0, s1) of `row` through the ring (all kThreads threads of the CTA; `nstages` stages of
 // kTileBytes in `ring`).  On return `top` holds the thread's column record and, with SUMS, `cs`
-// its sums (c = kRefFloor, S = 0 if the thread saw no finite logit).
+// its sums (c = kLowest, S = 0 if the thread saw no logit that counts).
 template <typename DT, bool SUMS, typename Pass>
 __device__ void stream_slice(const DT *__restrict__ row, int s0, int s1, int nstages, StreamBars &bars,
                              unsigned char *ring, ColTop &top, ColSums &cs, Pass &pass) {
@@ -319,7 +319,7 @@ __device__ void stream_slice(const DT *__restrict__ row, int s0, int s1, int nst
     volatile int *abort = &bars.timed_out;
 
     top.rm1 = -CUDART_INF_F; top.rm2 = -CUDART_INF_F; top.t1 = 0; top.seen = -CUDART_INF_F;
-    float c = kRefFloor;
+    float c = kLowest;
     // the sums of this thread's even and odd logits (register pairs), against the reference exponent c
     unsigned long long S2 = pack2(0.f, 0.f), T2 = pack2(0.f, 0.f);
 
